@@ -442,6 +442,150 @@ int token_logprob_packed(const void *h, const void *W_packed, const int32_t *tar
                          void *workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * Drawing tokens: one token a row from a row of logits (Sec. 3.3.2: every agent step is a
+ * completion; Sec. 3.3.3: each generated token is returned with its log-probability), by
+ * the row's own sampling parameters and a given uniform random number. Stands behind the
+ * LM head as token_logprob does: that scores given tokens, this draws them.
+ * For row n, with z the logits (NaN counts as -inf) and M the largest:
+ *   1. weight of v: e_v = exp((z_v - M) / T), T = temperature[n] (NULL: 1);
+ *   2. order the elements by logit, largest first, equal ones by index, lowest first;
+ *   3. top-k keeps the first k = top_k[n] (NULL, k <= 0 or k >= V: all);
+ *   4. top-p keeps, of those, each whose predecessors weigh less than p = top_p[n] times
+ *      what top-k kept (NULL, p >= 1 or NaN: all), always the first one;
+ *   5. min-p keeps, of those, each with e_v >= min(min_p[n], 1) (NULL, <= 0 or NaN: all);
+ *   6. the token is the first v, in the order of the indices, at which the running sum of
+ *      the kept weights exceeds uniform[n] times their whole sum S;
+ *      logprob = (z_v - M) / T - ln S: under the distribution that was drawn from.
+ * T <= 0 or NaN is greedy: the lowest index of M, logprob 0. Logits of -inf are never
+ * drawn; a row of nothing else gives token -1 and logprob NaN. If M is +inf the elements
+ * at +inf share the weight. uniform[n] is taken into [0, 1) (NaN as 0). Weights are summed
+ * as whole numbers of 2^-44 of the largest one (exact in any order; weights below half of
+ * that are never drawn), so that the draw is that of sums in 64-bit floating point.
+ *
+ *   logits       fp32 or bf16 (logits_dtype) [N] rows of V, row_stride elements apart
+ *                (any alignment of an element)
+ *   temperature  fp32 [N] or NULL; top_k int32 [N] or NULL; top_p, min_p fp32 [N] or NULL
+ *   uniform      fp32 [N] in [0, 1)
+ *   tokens       int32 [N]
+ *   logprob      fp32 [N] or NULL
+ *   workspace    device scratch of at least token_sample_workspace_size(N, V) bytes
+ *                (contents on entry ignored; NULL where the size is 0)
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (N < 0, V <= 0, row_stride < V with N > 1);
+ *         RA_ERR_UNSUPPORTED (an unknown logits_dtype, V > 2^19, N > 2^20);
+ *         RA_ERR_WORKSPACE; RA_ERR_HIP. N == 0 returns RA_OK without launching anything.
+ */
+typedef enum { RA_LOGITS_FP32 = 0, RA_LOGITS_BF16 = 1 } ra_logits_dtype;
+size_t token_sample_workspace_size(int32_t N, int32_t V);
+int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
+                 int64_t row_stride, const float *temperature, const int32_t *top_k,
+                 const float *top_p, const float *min_p, const float *uniform, int32_t *tokens,
+                 float *logprob, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Linear attention with a decay for each KV head: decode and append for layers that keep a
+ * state of fixed size instead of cached keys (the paper does not describe model internals;
+ * such layers take the place of the paged attention in some of a model's layers, and serve
+ * the same steps: Sec. 3.3.2 one token against the whole history, Sec. 3.3.3 the
+ * observation tokens after it). For query head h and KV head g = h / (Hq / Hkv), with
+ * l_g = exp(log_decay[g]):
+ *   S_t = l_g S_{t-1} + k_t v_t^T         (S [128 key dims][128 value dims], fp32)
+ *   o_t = scale * S_t^T q_t
+ * A row's state lives in a pool, states[slots[b]], and is updated in place; the state
+ * before a row's first token is zero whatever the pool holds. Slots of one call must
+ * differ. The state is kept to fp32 accuracy: append multiplies the decayed keys in three
+ * bf16 parts each. Its scores, and the state as it meets the queries, are rounded to bf16
+ * operands, and out is rounded to bf16 (nearest even) in both calls.
+ *
+ * rollout_linear_attn_decode: one token a row.
+ *   q          bf16 [B][Hq][128];  k_new, v_new  bf16 [B][Hkv][128]
+ *   states     fp32 [num_slots][Hkv][128][128], read and written
+ *   slots      int32 [B]; a row whose slot is outside [0, num_slots) gives out = 0
+ *   kv_lens    int32 [B]: tokens of the row with this one (1: its first). Rows with
+ *              kv_lens[b] <= 0 give out = 0 and leave their state as it is.
+ *   log_decay  fp32 [Hkv], <= 0 (larger values and NaN count as 0; -inf: no memory)
+ *   out        bf16 [B][Hq][128]
+ * rollout_linear_attn_append: row b's new tokens are packed rows cu_q[b] .. cu_q[b+1]-1.
+ *   q          bf16 [total_q][Hq][128];  k_new, v_new  bf16 [total_q][Hkv][128]
+ *   cu_q       int32 [B+1]; tokens behind cu_q[B] are not touched
+ *   ctx_lens   int32 [B]: tokens of the row before these (<= 0: none, the state is zero)
+ *   max_q_len  host: an upper bound of cu_q[b+1] - cu_q[b]
+ *   out        bf16 [total_q][Hq][128]
+ *   workspace  device scratch of at least rollout_linear_attn_append_workspace_size(B, Hq,
+ *              Hkv, total_q, max_q_len) bytes (contents on entry ignored; NULL where the
+ *              size is 0). Calls that share one must not overlap.
+ *   The rest as for decode; rows without tokens leave their state as it is. How a long row
+ *   is cut into stretches, and with it the order of fp32 sums, depends on B, Hq, Hkv,
+ *   total_q and max_q_len alone.
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, Hq or Hkv or num_slots <= 0, Hq % Hkv,
+ *         total_q < 0, max_q_len < 0, scale not finite); RA_ERR_UNSUPPORTED (Hq / Hkv > 32,
+ *         B > 65535, Hkv > 65535); RA_ERR_WORKSPACE; RA_ERR_HIP. B == 0, total_q == 0 or
+ *         max_q_len == 0 launch nothing.
+ */
+int rollout_linear_attn_decode(const void *q, const void *k_new, const void *v_new, float *states,
+                               const int32_t *slots, int32_t num_slots, const int32_t *kv_lens,
+                               const float *log_decay, int32_t B, int32_t Hq, int32_t Hkv,
+                               float scale, void *out, hipStream_t stream);
+size_t rollout_linear_attn_append_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
+                                                 int32_t total_q, int32_t max_q_len);
+int rollout_linear_attn_append(const void *q, const void *k_new, const void *v_new,
+                               const int32_t *cu_q, const int32_t *ctx_lens, float *states,
+                               const int32_t *slots, int32_t num_slots, const float *log_decay,
+                               int32_t B, int32_t Hq, int32_t Hkv, int32_t total_q,
+                               int32_t max_q_len, float scale, void *out, void *workspace,
+                               size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Block tables from lengths: the bookkeeping of a step on the GPU, so that a step whose
+ * lengths are only known there (sampled stops, captured graphs) needs no host between its
+ * calls. Pages that no row owns are on a free list (free_pages[0 .. *free_count), taken
+ * and given back at its end).
+ *
+ * kv_block_table_extend gives row b the pages that its tokens start_pos[b] ..
+ * start_pos[b] + num_new[b] - 1 need beyond the ceil(start_pos[b] / 16) it has:
+ *   block_table[b][j] = the next page off the list, rows in order, for
+ *       j in [ceil(start_pos / 16), ceil((start_pos + num_new) / 16)); other entries stay
+ *   cu_new[b]   = sum of num_new before b (B+1 entries)        } the arguments of
+ *   kv_lens[b]  = start_pos[b] + num_new[b]                    } kv_page_write and decode
+ *   slot_map[cu_new[b] + t] = page * 16 + (start_pos[b] + t) % 16 of each new token (its
+ *       place in a pool laid out by tokens), -1 from cu_new[B] on
+ *   *taken      = pages taken off the list
+ * All or nothing: if the list is too short, a row would pass its table (bt_stride * 16
+ * tokens), the new tokens are more than total_new, or a length or the list's count is out
+ * of range, *taken = -1, the list and the table stay, and the outputs are those of no new
+ * token (cu_new 0, kv_lens = start_pos, slot_map -1): a kv_page_write that follows writes
+ * nothing.
+ * kv_block_table_release puts the pages ceil(keep_lens[b] / 16) .. ceil(lens[b] / 16) - 1
+ * of every row back on the list (a row that ends: keep 0; a draft that is cut: its new
+ * length); table entries stay. Releasing what an extend took, with lens its kv_lens and
+ * keep_lens its start_pos, restores the list exactly. *released = pages given back, or -1
+ * with nothing changed if keep_lens[b] is not in [0, lens[b]], a length passes the table,
+ * or the list would pass its capacity.
+ *
+ *   start_pos, num_new, lens, keep_lens  int32 [B]
+ *   free_pages   int32 [free_capacity], free_count int32 [1] (read and written)
+ *   block_table  int32 [B][bt_stride], written by extend
+ *   total_new    host: an upper bound of the sum of num_new; slot_map's length
+ *   max_pages    host: how many pages a release may give back (more are correct, but
+ *                slower: it sizes the launch); B * bt_stride always holds
+ *   cu_new       int32 [B+1];  kv_lens int32 [B];  taken, released int32 [1]
+ *   slot_map     int64 [total_new] or NULL
+ * Outputs must not overlap inputs. Calls on one free list must not overlap in time.
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, bt_stride <= 0, total_new < 0, max_pages < 0,
+ *         free_capacity < 0); RA_ERR_UNSUPPORTED (B > 65535, bt_stride * 16 > 2^31 - 1);
+ *         RA_ERR_HIP. With B == 0 (row arrays may be NULL) extend writes cu_new[0] = 0,
+ *         *taken = 0 and the slots' -1, release *released = 0.
+ */
+int kv_block_table_extend(const int32_t *start_pos, const int32_t *num_new,
+                          const int32_t *free_pages, int32_t *free_count, int32_t free_capacity,
+                          int32_t *block_table, int32_t B, int32_t bt_stride, int32_t total_new,
+                          int32_t *cu_new, int32_t *kv_lens, int64_t *slot_map, int32_t *taken,
+                          hipStream_t stream);
+int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
+                           const int32_t *block_table, int32_t B, int32_t bt_stride,
+                           int32_t *free_pages, int32_t *free_count, int32_t free_capacity,
+                           int32_t max_pages, int32_t *released, hipStream_t stream);
+
+/*
  * Page write: append new tokens' keys and values to each trajectory's cache
  * (Sec. 3.3.3: the tokens of earlier turns are kept as they are and only the
  * new observation tokens are tokenised and added after them; Sec. 3.3.2: each

@@ -37,6 +37,8 @@ __all__ = ["PagedKV", "decode", "decode_noalloc", "decode_shared_prefix", "appen
            "kv_page_gather", "token_logprob", "decode_workspace_size",
            "decode_shared_prefix_workspace_size", "append_workspace_size", "mixed_workspace_size",
            "token_logprob_workspace_size", "token_logprob_pack_weight", "token_logprob_packed",
+           "token_sample", "token_sample_workspace_size", "linear_decode", "linear_append",
+           "linear_append_workspace_size", "block_table_extend", "block_table_release",
            "abi_version", "RolloutAttnError"]
 
 
@@ -619,3 +621,234 @@ def token_logprob_packed(h: torch.Tensor, W_packed: torch.Tensor, V: int, target
                          ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """token_logprob with the packed matrix from token_logprob_pack_weight (V rows)."""
     return _token_logprob(h, W_packed, targets, scale, out, lse, want_lse, workspace, stream, V)
+
+
+def token_sample_workspace_size(N: int, V: int) -> int:
+    return int(_lib.load().token_sample_workspace_size(N, V))
+
+
+def _per_row(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, N: int, dev) -> None:
+    if t is not None:
+        _need(t, name, dtype, dev)
+        _shape(t, (N,), name)
+
+
+def token_sample(logits: torch.Tensor, uniform: torch.Tensor,
+                 temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+                 top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                 tokens: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+                 want_logprob: bool = False, workspace: Optional[torch.Tensor] = None, stream=None
+                 ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """One token a row, drawn from logits (bf16 or fp32 [N][V], rows any stride >= V apart)
+    by the rows' temperature, top-k, top-p and min-p (fp32 / int32 / fp32 / fp32 [N], None:
+    off) at the given uniform numbers (fp32 [N] in [0, 1)).
+
+    Returns tokens int32 [N] and, if wanted, logprob fp32 [N] under the distribution drawn
+    from. temperature <= 0 is greedy; a row of nothing but -inf gives -1.
+    """
+    lib = _lib.load()
+    dev = logits.device
+    bf16 = logits.dtype == torch.bfloat16
+    if logits.device.type != "cuda":
+        raise ValueError(f"logits must be a GPU tensor, got one on {logits.device}")
+    if not bf16 and logits.dtype != torch.float32:
+        raise TypeError(f"logits must be torch.float32 or torch.bfloat16, got {logits.dtype}")
+    if logits.dim() != 2:
+        raise ValueError(f"logits must be [N][V], got {tuple(logits.shape)}")
+    N, V = logits.shape
+    row_stride = logits.stride(0) if N > 1 else V
+    if (V > 1 and logits.stride(1) != 1) or row_stride < V:
+        raise ValueError("logits must have contiguous rows that do not overlap, got strides "
+                         f"{tuple(logits.stride())}")
+    _need(uniform, "uniform", torch.float32, dev)
+    _shape(uniform, (N,), "uniform")
+    _per_row(temperature, "temperature", torch.float32, N, dev)
+    _per_row(top_k, "top_k", torch.int32, N, dev)
+    _per_row(top_p, "top_p", torch.float32, N, dev)
+    _per_row(min_p, "min_p", torch.float32, N, dev)
+    if tokens is None:
+        tokens = _empty((N,), torch.int32, dev, stream)
+    _per_row(tokens, "tokens", torch.int32, N, dev)
+    if logprob is None and want_logprob:
+        logprob = _empty((N,), torch.float32, dev, stream)
+    _per_row(logprob, "logprob", torch.float32, N, dev)
+    if workspace is None:
+        workspace = _empty(max(lib.token_sample_workspace_size(N, V), 1), torch.uint8, dev, stream,
+                           scratch=True)
+    _need(workspace, "workspace", torch.uint8, dev)
+    _lib.check("token_sample", lib.token_sample(
+        logits.data_ptr(), _lib.RA_LOGITS_BF16 if bf16 else _lib.RA_LOGITS_FP32, N, V, row_stride,
+        _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p), uniform.data_ptr(),
+        tokens.data_ptr(), _ptr(logprob), workspace.data_ptr(), workspace.numel(),
+        _stream(dev, stream)))
+    return tokens, logprob
+
+
+def _linear_inputs(q, k_new, v_new, states, slots, log_decay):
+    """Checks the tensors of the linear attention; returns (dev, total, Hq, Hkv)."""
+    dev = q.device
+    for t, n in ((q, "q"), (k_new, "k_new"), (v_new, "v_new")):
+        _need(t, n, torch.bfloat16, dev)
+    _need(states, "states", torch.float32, dev)
+    _need(slots, "slots", torch.int32, dev)
+    _need(log_decay, "log_decay", torch.float32, dev)
+    total, Hq, _ = q.shape
+    _shape(q, (total, Hq, HEAD_DIM), "q")
+    if states.dim() != 4 or tuple(states.shape[2:]) != (HEAD_DIM, HEAD_DIM):
+        raise ValueError(f"states must be [slots][Hkv][128][128], got {tuple(states.shape)}")
+    Hkv = states.shape[1]
+    _shape(k_new, (total, Hkv, HEAD_DIM), "k_new")
+    _shape(v_new, (total, Hkv, HEAD_DIM), "v_new")
+    _shape(log_decay, (Hkv,), "log_decay")
+    return dev, total, Hq, Hkv
+
+
+def linear_decode(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, states: torch.Tensor,
+                  slots: torch.Tensor, kv_lens: torch.Tensor, log_decay: torch.Tensor,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None
+                  ) -> torch.Tensor:
+    """Linear attention of one token a row: states[slots[b]] (fp32 [slots][Hkv][128][128]) is
+    decayed by exp(log_decay), takes k_new v_new^T (bf16 [B][Hkv][128]) and is read by q
+    (bf16 [B][Hq][128]) -> out bf16 [B][Hq][128]. kv_lens counts the row's tokens with this
+    one (1: the state before is zero; <= 0: nothing happens, out is zero)."""
+    lib = _lib.load()
+    dev, B, Hq, Hkv = _linear_inputs(q, k_new, v_new, states, slots, log_decay)
+    _need(kv_lens, "kv_lens", torch.int32, dev)
+    _shape(slots, (B,), "slots")
+    _shape(kv_lens, (B,), "kv_lens")
+    if scale is None:
+        scale = 1.0 / math.sqrt(HEAD_DIM)
+    if out is None:
+        out = _empty((B, Hq, HEAD_DIM), torch.bfloat16, dev, stream)
+    _need(out, "out", torch.bfloat16, dev)
+    _shape(out, (B, Hq, HEAD_DIM), "out")
+    _lib.check("rollout_linear_attn_decode", lib.rollout_linear_attn_decode(
+        q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), states.data_ptr(), slots.data_ptr(),
+        states.shape[0], kv_lens.data_ptr(), log_decay.data_ptr(), B, Hq, Hkv, float(scale),
+        out.data_ptr(), _stream(dev, stream)))
+    return out
+
+
+def linear_append_workspace_size(B: int, Hq: int, Hkv: int, total_q: int, max_q_len: int) -> int:
+    return int(_lib.load().rollout_linear_attn_append_workspace_size(B, Hq, Hkv, total_q,
+                                                                     max_q_len))
+
+
+def linear_append(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cu_q: torch.Tensor,
+                  ctx_lens: torch.Tensor, states: torch.Tensor, slots: torch.Tensor,
+                  log_decay: torch.Tensor, max_q_len: Optional[int] = None,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Linear attention of new tokens (packed by cu_q like append's) after ctx_lens earlier
+    ones whose state is states[slots[b]]: q bf16 [total_q][Hq][128], k_new and v_new bf16
+    [total_q][Hkv][128] -> out bf16 [total_q][Hq][128]; the states are updated in place."""
+    lib = _lib.load()
+    dev, total_q, Hq, Hkv = _linear_inputs(q, k_new, v_new, states, slots, log_decay)
+    _need(cu_q, "cu_q", torch.int32, dev)
+    _need(ctx_lens, "ctx_lens", torch.int32, dev)
+    B = ctx_lens.shape[0]
+    _shape(ctx_lens, (B,), "ctx_lens")
+    _shape(cu_q, (B + 1,), "cu_q")
+    _shape(slots, (B,), "slots")
+    if max_q_len is None:
+        max_q_len = int((cu_q[1:] - cu_q[:-1]).max().item()) if B else 0
+    if scale is None:
+        scale = 1.0 / math.sqrt(HEAD_DIM)
+    if out is None:
+        out = _empty((total_q, Hq, HEAD_DIM), torch.bfloat16, dev, stream)
+    _need(out, "out", torch.bfloat16, dev)
+    _shape(out, (total_q, Hq, HEAD_DIM), "out")
+    if workspace is None:
+        ws_bytes = lib.rollout_linear_attn_append_workspace_size(B, Hq, Hkv, total_q, max_q_len)
+        workspace = _empty(max(ws_bytes, 1), torch.uint8, dev, stream, scratch=True)
+    _need(workspace, "workspace", torch.uint8, dev)
+    _lib.check("rollout_linear_attn_append", lib.rollout_linear_attn_append(
+        q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), cu_q.data_ptr(), ctx_lens.data_ptr(),
+        states.data_ptr(), slots.data_ptr(), states.shape[0], log_decay.data_ptr(), B, Hq, Hkv,
+        total_q, max_q_len, float(scale), out.data_ptr(), workspace.data_ptr(), workspace.numel(),
+        _stream(dev, stream)))
+    return out
+
+
+def _table_inputs(block_table, free_pages, free_count, rows, names):
+    """Checks the tensors of the block-table calls; returns (dev, B, bt_stride)."""
+    dev = block_table.device
+    _need(block_table, "block_table", torch.int32, dev)
+    _need(free_pages, "free_pages", torch.int32, dev)
+    _need(free_count, "free_count", torch.int32, dev)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B][stride]")
+    _shape(free_pages, (free_pages.numel(),), "free_pages")
+    _shape(free_count, (1,), "free_count")
+    B = rows[0].shape[0]
+    for t, n in zip(rows, names):
+        _need(t, n, torch.int32, dev)
+        _shape(t, (B,), n)
+    if block_table.shape[0] < B:
+        raise ValueError(f"block_table has {block_table.shape[0]} rows, batch has {B}")
+    return dev, B, block_table.shape[1]
+
+
+def block_table_extend(block_table: torch.Tensor, start_pos: torch.Tensor, num_new: torch.Tensor,
+                       free_pages: torch.Tensor, free_count: torch.Tensor,
+                       total_new: Optional[int] = None, cu_new: Optional[torch.Tensor] = None,
+                       kv_lens: Optional[torch.Tensor] = None,
+                       slot_map: Optional[torch.Tensor] = None,
+                       taken: Optional[torch.Tensor] = None, stream=None
+                       ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Takes the pages that num_new more tokens a row need (after start_pos earlier ones) off
+    the end of the free list (free_pages[:free_count], int32) into block_table, in place.
+
+    Returns (cu_new int32 [B+1], kv_lens int32 [B], slot_map int64 [total_new], taken int32
+    [1]): the arguments of kv_page_write and decode, each new token's page * 16 + slot (-1
+    behind the last), and the pages taken, -1 if the call was refused as a whole (the list
+    too short, a row past its table, more than total_new tokens, a length out of range):
+    then nothing changed and the outputs are those of no new token.
+    """
+    lib = _lib.load()
+    dev, B, stride = _table_inputs(block_table, free_pages, free_count, (start_pos, num_new),
+                                   ("start_pos", "num_new"))
+    if total_new is None:
+        total_new = slot_map.shape[0] if slot_map is not None else int(num_new.sum().item())
+    if cu_new is None:
+        cu_new = _empty((B + 1,), torch.int32, dev, stream)
+    if kv_lens is None:
+        kv_lens = _empty((B,), torch.int32, dev, stream)
+    if slot_map is None:
+        slot_map = _empty((max(total_new, 0),), torch.int64, dev, stream)
+    if taken is None:
+        taken = _empty((1,), torch.int32, dev, stream)
+    for t, n, dt, size in ((cu_new, "cu_new", torch.int32, B + 1),
+                           (kv_lens, "kv_lens", torch.int32, B),
+                           (slot_map, "slot_map", torch.int64, max(total_new, 0)),
+                           (taken, "taken", torch.int32, 1)):
+        _need(t, n, dt, dev)
+        _shape(t, (size,), n)
+    _lib.check("kv_block_table_extend", lib.kv_block_table_extend(
+        start_pos.data_ptr(), num_new.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+        free_pages.numel(), block_table.data_ptr(), B, stride, total_new, cu_new.data_ptr(),
+        kv_lens.data_ptr(), slot_map.data_ptr(), taken.data_ptr(), _stream(dev, stream)))
+    return cu_new, kv_lens, slot_map, taken
+
+
+def block_table_release(block_table: torch.Tensor, lens: torch.Tensor, keep_lens: torch.Tensor,
+                        free_pages: torch.Tensor, free_count: torch.Tensor,
+                        max_pages: Optional[int] = None, released: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """Puts the pages of tokens keep_lens .. lens - 1 of every row (whole pages only) back on
+    the free list. Returns the pages given back (int32 [1]), -1 if the call was refused as a
+    whole. max_pages: how many to expect (sizes the launch; default: the whole table)."""
+    lib = _lib.load()
+    dev, B, stride = _table_inputs(block_table, free_pages, free_count, (lens, keep_lens),
+                                   ("lens", "keep_lens"))
+    if max_pages is None:
+        max_pages = min(B * stride, 2**31 - 1)
+    if released is None:
+        released = _empty((1,), torch.int32, dev, stream)
+    _need(released, "released", torch.int32, dev)
+    _shape(released, (1,), "released")
+    _lib.check("kv_block_table_release", lib.kv_block_table_release(
+        lens.data_ptr(), keep_lens.data_ptr(), block_table.data_ptr(), B, stride,
+        free_pages.data_ptr(), free_count.data_ptr(), free_pages.numel(), max_pages,
+        released.data_ptr(), _stream(dev, stream)))
+    return released

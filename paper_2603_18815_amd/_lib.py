@@ -15,6 +15,9 @@ RA_ERR_HIP = 5
 RA_KV_BF16 = 0
 RA_KV_FP8_E4M3 = 1
 
+RA_LOGITS_FP32 = 0
+RA_LOGITS_BF16 = 1
+
 RA_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 EXPORTS = (
@@ -39,6 +42,13 @@ EXPORTS = (
     "token_logprob_packed_weight_size",
     "token_logprob_pack_weight",
     "token_logprob_packed",
+    "token_sample_workspace_size",
+    "token_sample",
+    "rollout_linear_attn_decode",
+    "rollout_linear_attn_append_workspace_size",
+    "rollout_linear_attn_append",
+    "kv_block_table_extend",
+    "kv_block_table_release",
 )
 
 
@@ -78,6 +88,7 @@ def load() -> ctypes.CDLL:
             "(or __graft_entry__.build()) first")
     lib = ctypes.CDLL(LIB_PATH)
     i32, vp, sz, f32 = ctypes.c_int32, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
+    i64 = ctypes.c_int64
     kvp = ctypes.POINTER(RaPagedKV)
     lib.ra_abi_version.argtypes = []
     lib.ra_abi_version.restype = ctypes.c_int
@@ -127,6 +138,23 @@ def load() -> ctypes.CDLL:
     lib.kv_page_write_rope.restype = ctypes.c_int
     lib.kv_page_gather.argtypes = [kvp, vp, vp, i32, i32, i32, vp, vp, vp]
     lib.kv_page_gather.restype = ctypes.c_int
+    lib.token_sample_workspace_size.argtypes = [i32, i32]
+    lib.token_sample_workspace_size.restype = sz
+    lib.token_sample.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.token_sample.restype = ctypes.c_int
+    lib.rollout_linear_attn_decode.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, i32, f32,
+                                               vp, vp]
+    lib.rollout_linear_attn_decode.restype = ctypes.c_int
+    lib.rollout_linear_attn_append_workspace_size.argtypes = [i32, i32, i32, i32, i32]
+    lib.rollout_linear_attn_append_workspace_size.restype = sz
+    lib.rollout_linear_attn_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, i32, i32, i32,
+                                               i32, i32, f32, vp, vp, sz, vp]
+    lib.rollout_linear_attn_append.restype = ctypes.c_int
+    lib.kv_block_table_extend.argtypes = [vp, vp, vp, vp, i32, vp, i32, i32, i32, vp, vp, vp, vp,
+                                          vp]
+    lib.kv_block_table_extend.restype = ctypes.c_int
+    lib.kv_block_table_release.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp]
+    lib.kv_block_table_release.restype = ctypes.c_int
     _lib = lib
     return lib
 

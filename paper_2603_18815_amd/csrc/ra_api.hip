@@ -296,6 +296,21 @@ int page_write_impl(const void *k_new, const void *v_new, const int32_t *cu_new,
                                           cos_sin, rope_rows));
 }
 
+// Checks shared by the linear attention's entry points.
+int check_linear(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_slots, float scale) {
+  if (B < 0 || Hq <= 0 || Hkv <= 0 || num_slots <= 0 || Hq % Hkv != 0 || !std::isfinite(scale))
+    return RA_ERR_SHAPE;
+  if (Hq / Hkv > 32 || B > kMaxGridYZ || Hkv > kMaxGridYZ) return RA_ERR_UNSUPPORTED;
+  return RA_OK;
+}
+
+// Checks shared by the block table's entry points.
+int check_table(int32_t B, int32_t bt_stride, int32_t free_capacity) {
+  if (B < 0 || bt_stride <= 0 || free_capacity < 0) return RA_ERR_SHAPE;
+  if (B > kMaxGridYZ || (int64_t)bt_stride * RA_PAGE_SIZE > INT32_MAX) return RA_ERR_UNSUPPORTED;
+  return RA_OK;
+}
+
 // A rotary table must cover every position the call uses: [0, max_pos).
 int check_rope(const float *cos_sin, int32_t rope_rows, int32_t max_pos) {
   if (rope_rows <= 0 || max_pos > rope_rows) return RA_ERR_SHAPE;
@@ -444,6 +459,98 @@ int token_logprob_packed(const void *h, const void *W_packed, const int32_t *tar
   return hip_status(ra::launch_logprob(static_cast<const uint16_t *>(h),
                                        static_cast<const uint16_t *>(W_packed), targets, N, V, D,
                                        scale, logprob, lse, workspace, true, stream));
+}
+
+size_t token_sample_workspace_size(int32_t N, int32_t V) {
+  if (N <= 0 || V <= 0 || V > ra::kSampleMaxVocab) return 0;
+  return ra::sample_workspace_bytes(N, V);
+}
+
+int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
+                 int64_t row_stride, const float *temperature, const int32_t *top_k,
+                 const float *top_p, const float *min_p, const float *uniform, int32_t *tokens,
+                 float *logprob, void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (N < 0 || V <= 0 || (N > 1 && row_stride < V)) return RA_ERR_SHAPE;
+  if (logits_dtype != RA_LOGITS_FP32 && logits_dtype != RA_LOGITS_BF16) return RA_ERR_UNSUPPORTED;
+  if (V > ra::kSampleMaxVocab || N > (1 << 20)) return RA_ERR_UNSUPPORTED;
+  if (N == 0) return RA_OK;
+  if (!logits || !uniform || !tokens) return RA_ERR_NULL;
+  const size_t need = ra::sample_workspace_bytes(N, V);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
+  return hip_status(ra::launch_sample(logits, logits_dtype == RA_LOGITS_BF16, N, V, row_stride,
+                                      temperature, top_k, top_p, min_p, uniform, tokens, logprob,
+                                      workspace, stream));
+}
+
+int rollout_linear_attn_decode(const void *q, const void *k_new, const void *v_new, float *states,
+                               const int32_t *slots, int32_t num_slots, const int32_t *kv_lens,
+                               const float *log_decay, int32_t B, int32_t Hq, int32_t Hkv,
+                               float scale, void *out, hipStream_t stream) {
+  const int s = check_linear(B, Hq, Hkv, num_slots, scale);
+  if (s != RA_OK) return s;
+  if (B == 0) return RA_OK;
+  if (!q || !k_new || !v_new || !states || !slots || !kv_lens || !log_decay || !out)
+    return RA_ERR_NULL;
+  return hip_status(ra::launch_linear_decode(
+      static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new),
+      static_cast<const uint16_t *>(v_new), states, slots, num_slots, kv_lens, log_decay, B, Hq,
+      Hkv, scale, static_cast<uint16_t *>(out), stream));
+}
+
+size_t rollout_linear_attn_append_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
+                                                 int32_t total_q, int32_t max_q_len) {
+  if (check_linear(B, Hq, Hkv, 1, 1.f) != RA_OK || B == 0 || total_q <= 0 || max_q_len <= 0)
+    return 0;
+  return ra::linear_append_workspace_bytes(B, Hq, Hkv, total_q, max_q_len);
+}
+
+int rollout_linear_attn_append(const void *q, const void *k_new, const void *v_new,
+                               const int32_t *cu_q, const int32_t *ctx_lens, float *states,
+                               const int32_t *slots, int32_t num_slots, const float *log_decay,
+                               int32_t B, int32_t Hq, int32_t Hkv, int32_t total_q,
+                               int32_t max_q_len, float scale, void *out, void *workspace,
+                               size_t workspace_bytes, hipStream_t stream) {
+  if (total_q < 0 || max_q_len < 0) return RA_ERR_SHAPE;
+  const int s = check_linear(B, Hq, Hkv, num_slots, scale);
+  if (s != RA_OK) return s;
+  if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
+  if (!q || !k_new || !v_new || !cu_q || !ctx_lens || !states || !slots || !log_decay || !out)
+    return RA_ERR_NULL;
+  const size_t need = ra::linear_append_workspace_bytes(B, Hq, Hkv, total_q, max_q_len);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
+  return hip_status(ra::launch_linear_append(
+      static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new),
+      static_cast<const uint16_t *>(v_new), cu_q, ctx_lens, states, slots, num_slots, log_decay,
+      B, Hq, Hkv, total_q, max_q_len, scale, static_cast<uint16_t *>(out), workspace, stream));
+}
+
+int kv_block_table_extend(const int32_t *start_pos, const int32_t *num_new,
+                          const int32_t *free_pages, int32_t *free_count, int32_t free_capacity,
+                          int32_t *block_table, int32_t B, int32_t bt_stride, int32_t total_new,
+                          int32_t *cu_new, int32_t *kv_lens, int64_t *slot_map, int32_t *taken,
+                          hipStream_t stream) {
+  if (total_new < 0) return RA_ERR_SHAPE;
+  const int s = check_table(B, bt_stride, free_capacity);
+  if (s != RA_OK) return s;
+  if (!free_count || !cu_new || !taken || (free_capacity > 0 && !free_pages)) return RA_ERR_NULL;
+  if (B > 0 && (!start_pos || !num_new || !block_table || !kv_lens)) return RA_ERR_NULL;
+  return hip_status(ra::launch_table_extend(start_pos, num_new, free_pages, free_count,
+                                            free_capacity, block_table, B, bt_stride, total_new,
+                                            cu_new, kv_lens, slot_map, taken, stream));
+}
+
+int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
+                           const int32_t *block_table, int32_t B, int32_t bt_stride,
+                           int32_t *free_pages, int32_t *free_count, int32_t free_capacity,
+                           int32_t max_pages, int32_t *released, hipStream_t stream) {
+  if (max_pages < 0) return RA_ERR_SHAPE;
+  const int s = check_table(B, bt_stride, free_capacity);
+  if (s != RA_OK) return s;
+  if (!free_count || !released || (free_capacity > 0 && !free_pages)) return RA_ERR_NULL;
+  if (B > 0 && (!lens || !keep_lens || !block_table)) return RA_ERR_NULL;
+  return hip_status(ra::launch_table_release(lens, keep_lens, block_table, B, bt_stride,
+                                             free_pages, free_count, free_capacity, max_pages,
+                                             released, stream));
 }
 
 int kv_page_write(const void *k_new, const void *v_new, const int32_t *cu_new,

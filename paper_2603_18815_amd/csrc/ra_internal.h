@@ -100,6 +100,40 @@ size_t logprob_packed_bytes(int32_t V, int32_t D);
 hipError_t launch_logprob_pack(const uint16_t *W, int32_t V, int32_t D, uint16_t *Wp,
                                hipStream_t stream);
 
+// ---- drawing tokens from logits ----
+constexpr int32_t kSampleMaxVocab = 1 << 19;   // a row's sum of weights stays below 2^63
+size_t sample_workspace_bytes(int32_t N, int32_t V);
+hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, int64_t row_stride,
+                         const float *temperature, const int32_t *top_k, const float *top_p,
+                         const float *min_p, const float *uniform, int32_t *tokens,
+                         float *logprob, void *workspace, hipStream_t stream);
+
+// ---- linear attention with a decay per head ----
+hipError_t launch_linear_decode(const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                                float *states, const int32_t *slots, int32_t num_slots,
+                                const int32_t *kv_lens, const float *log_decay, int32_t B,
+                                int32_t hq, int32_t hkv, float scale, uint16_t *out,
+                                hipStream_t stream);
+size_t linear_append_workspace_bytes(int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
+                                     int32_t max_q_len);
+hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint16_t *v,
+                                const int32_t *cu_q, const int32_t *ctx_lens, float *states,
+                                const int32_t *slots, int32_t num_slots, const float *log_decay,
+                                int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
+                                int32_t max_q_len, float scale, uint16_t *out, void *workspace,
+                                hipStream_t stream);
+
+// ---- block tables from lengths ----
+hipError_t launch_table_extend(const int32_t *start_pos, const int32_t *num_new,
+                               const int32_t *free_pages, int32_t *free_count, int32_t capacity,
+                               int32_t *block_table, int32_t B, int32_t bt_stride,
+                               int32_t total_new, int32_t *cu_new, int32_t *kv_lens,
+                               int64_t *slot_map, int32_t *taken, hipStream_t stream);
+hipError_t launch_table_release(const int32_t *lens, const int32_t *keep_lens,
+                                const int32_t *block_table, int32_t B, int32_t bt_stride,
+                                int32_t *free_pages, int32_t *free_count, int32_t capacity,
+                                int32_t max_pages, int32_t *released, hipStream_t stream);
+
 // ---- page write / gather ----
 hipError_t launch_page_write(const uint16_t *k_new, const uint16_t *v_new, const int32_t *cu_new,
                              const int32_t *start_pos, const PagedKV &kv, int32_t B,

@@ -1,0 +1,178 @@
+"""token_sample on the GPU against a plain 64-bit implementation on the host.
+
+Tokens must be equal: the kernel's weights are whole numbers of 2^-44 of the largest, so a
+border of the cumulative distribution is off by at most V 2^-45 <= 2^-26 of the largest
+weight at V = 2^19 (2^-28 at the vocabularies here), and a uniform number falls that near
+one of V borders with a probability below 2^-9 for a flat row of 2^17 (borders 2^-17 apart,
+each off by 2^-45 V / V relative: 2^17 2^-45). logprob is a difference rounded to fp32 once:
+|error| <= 2^-24 |logprob| + 2^-28.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18815_amd as ra
+
+pytestmark = pytest.mark.gpu
+NINF = float("-inf")
+
+
+def host(z, u, T=1.0, k=0, p=1.0, m=0.0):
+    """One row, by the definition in the header."""
+    z = np.asarray(z, np.float64)
+    z = np.where(np.isnan(z), NINF, z)
+    top = z.max()
+    if top == NINF:
+        return -1, np.nan
+    if not T > 0:
+        return int(np.argmax(z)), 0.0
+    with np.errstate(invalid="ignore"):
+        x = np.where(z == top, 0.0, (z - top) / T)
+    e = np.exp(x)
+    order = np.argsort(-z, kind="stable")
+    if 0 < k < z.size:
+        order = order[:k]
+    if p < 1:
+        w = e[order]
+        ahead = np.cumsum(w) - w
+        ahead[0] = -1.0
+        order = order[ahead < p * w.sum()] if p > 0 else order[:1]
+    if m > 0:
+        order = order[e[order] >= min(m, 1.0)]
+    kept = np.sort(order)
+    run = np.cumsum(e[kept])
+    u = min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
+    t = kept[min(np.searchsorted(run, u * run[-1], side="right"), kept.size - 1)]
+    return int(t), float(x[t] - np.log(run[-1]))
+
+
+def check(z, u, T=None, k=None, p=None, m=None, what=""):
+    """z [N][V] on the GPU, parameters lists of N or None."""
+    f = lambda x: None if x is None else torch.tensor(x, dtype=torch.float32, device="cuda:0")
+    kk = None if k is None else torch.tensor(k, dtype=torch.int32, device="cuda:0")
+    ut, Tt, pt, mt = f(u), f(T), f(p), f(m)
+    tokens, logp = ra.token_sample(z, ut, Tt, kk, pt, mt, want_logprob=True)
+    rows = z.double().cpu().numpy()
+    get = lambda x, n, off: off if x is None else x[n].item()
+    want = [host(rows[n], get(ut, n, 0), get(Tt, n, 1.0), get(kk, n, 0), get(pt, n, 1.0),
+                 get(mt, n, 0.0)) for n in range(rows.shape[0])]
+    assert tokens.tolist() == [w[0] for w in want], what
+    wl = np.array([w[1] for w in want])
+    got = logp.double().cpu().numpy()
+    assert np.array_equal(np.isnan(got), np.isnan(wl))
+    ok = ~np.isnan(wl)
+    assert np.all(np.abs(got - wl)[ok] <= 2.0 ** -24 * np.abs(wl[ok]) + 2.0 ** -28), what
+    again, lagain = ra.token_sample(z, ut, Tt, kk, pt, mt, want_logprob=True)
+    assert torch.equal(tokens, again) and torch.equal(logp.view(torch.int32), lagain.view(torch.int32))
+
+
+def logits(N, V, dtype, seed, sharp=2.0, pad=0):
+    g = torch.Generator(device="cuda:0").manual_seed(seed)
+    z = sharp * torch.randn((N, V + pad), generator=g, device="cuda:0")
+    return z.to(dtype)[:, :V]
+
+
+def uniforms(N, seed):
+    return np.random.default_rng(seed).random(N, dtype=np.float32).tolist()
+
+
+SIZES = [1, 2, 3, 63, 64, 65, 1000, 4095, 4096, 4097, 8192, 8193, 32000, 65537, 151936]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", SIZES)
+def test_every_filter_at_every_size(V, dtype, device):
+    N = 8
+    z = logits(N, V, dtype, V)
+    u = uniforms(N, V)
+    T = [1.0, 0.7, 1.3, 0.0, 0.05, 20.0, 1.0, 0.9]
+    k = [0, 1, 5, 50, V - 1, V, V + 1, 1000]
+    p = [1.0, 0.9, 0.5, 0.1, 0.999, 0.0, 0.3, 1.5]
+    m = [0.0, 0.1, 0.02, 0.5, 1.0, 1e-5, 2.0, -1.0]
+    check(z, u, what="plain")
+    check(z, u, T, what="temperature")
+    check(z, u, None, k, what="top-k")
+    check(z, u, T, k, what="top-k, T")
+    check(z, u, None, None, p, what="top-p")
+    check(z, u, T, None, p, what="top-p, T")
+    check(z, u, None, None, None, m, what="min-p")
+    check(z, u, None, k, p, what="top-k, top-p")
+    check(z, u, T, k, p, m, what="all")
+    check(z, u, T, k[::-1], p[3:] + p[:3], m[5:] + m[:5], what="all, turned")
+
+
+@pytest.mark.parametrize("N,V,pad", [(1, 151936, 0), (3, 128257, 7), (70, 50001, 1), (300, 5000, 3)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_batches_and_row_strides(N, V, pad, dtype, device):
+    z = logits(N, V, dtype, N, 3.0, pad)
+    r = np.random.default_rng(N)
+    check(z, uniforms(N, N), r.uniform(0.3, 1.5, N).tolist(), r.integers(0, 300, N).tolist(),
+          r.uniform(0.5, 1.05, N).tolist(), r.uniform(-0.05, 0.1, N).tolist())
+
+
+@pytest.mark.parametrize("V", [512, 40000, 151936])
+@pytest.mark.parametrize("scale", [0.0, 0.01, 1.0, 8.0])
+def test_flat_and_tied_rows(V, scale, device):
+    """Logits of a few values each: long runs of equal elements, whose lowest indices count."""
+    g = torch.Generator(device="cuda:0").manual_seed(V)
+    z = scale * torch.randint(0, 5, (6, V), generator=g, device="cuda:0").float()
+    check(z, uniforms(6, V), None, [1, V // 3, V // 2, V - 1, 7, 100], what="top-k")
+    check(z, uniforms(6, V), None, None, [0.5, 0.25, 0.99, 0.001, 0.75, 0.125], what="top-p")
+    check(z, uniforms(6, V), None, [V // 2, V // 3, 9, V, V, V - 5],
+          [0.5, 0.25, 0.99, 0.001, 0.75, 0.125], [0, 0, 0.9, 0.5, 0.01, 1.0], what="all")
+
+
+def test_first_and_last_uniform(device):
+    z = torch.tensor([[0.0, 1.0, NINF, 2.0, 1.0]] * 5, device="cuda:0")
+    top = float(np.nextafter(np.float32(1), np.float32(0)))
+    check(z, [0.0, top, 1.0, -3.0, float("nan")])
+    check(z, [0.0, top, 0.5, 7.0, 0.999], None, [3, 3, 3, 2, 1])
+
+
+@pytest.mark.parametrize("V", [5, 300, 70000])
+def test_masks_infinities_and_nan(V, device):
+    low = torch.finfo(torch.float32).min
+    z = logits(10, V, torch.float32, 5)
+    z[0] = NINF                                    # nothing is left
+    z[1] = float("nan")
+    z[2] = low                                     # all at the lowest value: a flat row
+    z[3, : V - 1] = low                            # one token left
+    z[4, : V // 2] = NINF
+    z[5, ::2] = float("nan")
+    z[6, V // 2] = float("inf")
+    z[7, 1::3] = float("inf")                      # several share the weight
+    z[8] = 0.0
+    z[8, ::2] = -0.0                               # equal values of two signs
+    z[9, : V // 2] = low
+    u = uniforms(10, V)
+    check(z, u)
+    check(z, u, [0.0] * 10)
+    check(z, u, [0.5] * 10, [3] * 10, [0.9] * 10, [0.01] * 10)
+    check(z, u, [float("inf"), 1e-30, 1e30, 1.0, 2.0, float("nan"), 1.0, -1.0, 3.0, 1e-38])
+    check(z, u, None, [V // 2 + 1] * 10, [0.999] * 10)
+
+
+def test_a_row_of_wide_range(device):
+    """Weights from 1 down to nothing: 2^-44 of the largest and below are never drawn."""
+    V = 60000
+    z = -torch.arange(V, device="cuda:0", dtype=torch.float32).remainder(2000)[None] * 0.05
+    z = z.repeat(4, 1)
+    check(z, uniforms(4, 1), None, [50000, 500, 0, 0], [1.0, 0.99999, 0.9999999, 1.0])
+
+
+def test_refusals(device):
+    z, u = torch.zeros((4, 100), device="cuda:0"), torch.zeros(4, device="cuda:0")
+    with pytest.raises(ValueError, match="contiguous rows"):
+        ra.token_sample(z.t().contiguous().t(), u)
+    with pytest.raises(ValueError, match="contiguous rows"):
+        ra.token_sample(z[:1].expand(4, 100), u)
+    with pytest.raises(TypeError, match="float32 or torch.bfloat16"):
+        ra.token_sample(z.half(), u)
+    with pytest.raises(ValueError, match="uniform"):
+        ra.token_sample(z, u[:3])
+    with pytest.raises(TypeError, match="top_k"):
+        ra.token_sample(z, u, top_k=torch.zeros(4, dtype=torch.int64, device="cuda:0"))
+    with pytest.raises(ra.RolloutAttnError):
+        ra.token_sample(torch.zeros((1, (1 << 19) + 1), device="cuda:0"), u[:1])
+    tokens, logp = ra.token_sample(z[:0], u[:0], want_logprob=True)
+    assert tokens.shape == (0,) and logp.shape == (0,)
