@@ -132,6 +132,24 @@ __device__ __forceinline__ bf16x8 take_bf16(f32x8 &x) {
 
 enum { kWhole, kStates, kOutputs };
 
+// 16 bytes a lane from global memory to LDS, lane l's at `lds` + 16 l (lds and lane 0's
+// address are the wave's). In assembly: behind the builtin the compiler waits for all such
+// loads before any LDS read; here await_loads() does, before the barrier that hands the
+// tile over.
+__device__ __forceinline__ void load_to_lds(const uint16_t *g, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off"
+      :
+      : "s"(lds), "v"(g)
+      : "memory", "m0");
+}
+__device__ __forceinline__ void await_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const uint16_t *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
 // One stretch of a (row, KV head): chunks in order, the state in the accumulators. Wave w
 // holds the 32 value dims from 32 w, all 128 key dims: tile (t, u), t < 8, u < 2, has key
 // dims 16 t + 0..15 as its rows and value dims 32 w + 8 (c / 4) + 4 u + c % 4 as its
@@ -139,9 +157,16 @@ enum { kWhole, kStates, kOutputs };
 // value dims of a token. An accumulator tile of the state is the matrix operand of
 // S^T Q^T as it stands, rounded to bf16. Scores go through LDS: wave w computes those of
 // tokens 16 w .. 16 w + 15, all waves use all of them.
+//
+// A step is a chunk and a query head of the group, with two barriers: the step's tiles are
+// there (scores, then with the chunk's last head the state's update); the scores are there
+// (outputs, while the next chunk's K and V load; V's tile is free once the first head
+// has its operands, K's after the update). Q has two tiles. 72 KB of LDS: two workgroups
+// per CU, whose steps overlap.
 template <int kMode>
 __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a) {
-  const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
   int unit = blockIdx.x;
   const int split = kMode == kStates ? 0 : unit % a.head_splits;
@@ -166,9 +191,11 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
     return;
   }
 
-  __shared__ __align__(16) uint16_t sk[kChunk * kHeadDim], sv[kChunk * kHeadDim];
-  __shared__ __align__(16) uint16_t sq[kMode == kStates ? 8 : kChunk * kHeadDim];
-  __shared__ __align__(16) uint16_t sp[kMode == kStates ? 8 : kChunk * kChunk];
+  constexpr int kTile = kChunk * kHeadDim;
+  constexpr int kVTiles = kMode == kStates ? 2 : 1, kKTiles = kMode == kStates ? 2 : 1;
+  __shared__ __align__(1024) uint16_t sk[kKTiles * kTile], sv[kVTiles * kTile];
+  __shared__ __align__(1024) uint16_t sq[kMode == kStates ? 8 : 2 * kTile];
+  __shared__ __align__(1024) uint16_t sp[kMode == kStates ? 8 : kChunk * kChunk];
   __shared__ float power[kChunk + 1], power_low[kChunk + 1];   // l^n and what fp32 leaves out
   const double ld = log_decay_of(a.log_decay, g);
   const float l2 = (float)(ld * 1.4426950408889634);
@@ -177,6 +204,25 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
     power[tid] = (float)p;
     power_low[tid] = (float)(p - (double)(float)p);
   }
+
+  // loads: wave w takes rows 16 w .. 16 w + 15 of a tile, four rows an instruction, lane l
+  // the unit of row l / 16 that belongs at l % 16; rows past the end repeat the last one
+  const uint32_t lds_k = lds_address(sk) + wave * 4096, lds_v = lds_address(sv) + wave * 4096;
+  const uint32_t lds_q = lds_address(sq) + wave * 4096;
+  const int ld_unit = (lane % 16) ^ (lane / 16 << 1);
+  auto load = [&](uint32_t lds, const uint16_t *src, int c, int heads, int head) {
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const int t = min(c * kChunk + 16 * wave + 4 * m + lane / 16, len - 1);
+      load_to_lds(src + ((tok0 + t) * heads + head) * kHeadDim +
+                      ((ld_unit ^ ((m & 1) << 3 | m >> 1)) << 3),
+                  lds + 1024 * m);
+    }
+  };
+  const int chunks = (len + kChunk - 1) / kChunk;
+  load(lds_k, a.k, 0, a.hkv, g);
+  load(lds_v, a.v, 0, a.hkv, g);
+  if (kMode != kStates) load(lds_q, a.q, 0, a.hq, g * group + h0);
 
   // state tile (t, u), register i: key dim 16 t + 4 quad + i, value dim `dv` + 4 u
   const int dv = 32 * wave + 8 * (r >> 2) + (r & 3);
@@ -188,39 +234,82 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
 #pragma unroll
   for (int t = 0; t < 8; ++t)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) s[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (!zero) {
+    const float *at = carry + 4 * quad * kHeadDim + dv;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        s[t][u][i] = zero ? 0.f : carry[(16 * t + 4 * quad + i) * kHeadDim + dv + 4 * u];
-
-  // loads: thread t takes 16-byte unit t % 16 of rows t / 16 + 16 i (past the end: the last)
-  const int ld_row = tid / 16, ld_unit = tid % 16;
-  const int st_at = ld_row * kHeadDim + ((ld_unit ^ swizzle(ld_row)) << 3);
-  u32x4 kr[4], vr[4], qr[4];
-  auto load = [&](u32x4(&x)[4], const uint16_t *src, int c, int heads, int head) {
+    for (int t = 0; t < 8; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = min(c * kChunk + ld_row + 16 * i, len - 1);
-      x[i] = load_u32x4(src + ((tok0 + t) * heads + head) * kHeadDim + ld_unit * 8);
-    }
-  };
-  auto store = [&](uint16_t *tile, const u32x4(&x)[4]) {
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store_u32x4(tile + st_at + 16 * i * kHeadDim, x[i]);
-  };
-  const int chunks = (len + kChunk - 1) / kChunk;
-  load(kr, a.k, 0, a.hkv, g);
-  load(vr, a.v, 0, a.hkv, g);
-  if (kMode != kStates) load(qr, a.q, 0, a.hq, g * group + h0);
+        for (int i = 0; i < 4; ++i) s[t][u][i] = at[(16 * t + i) * kHeadDim + 4 * u];
+  }
 
   const int tr_row = 4 * quad + (r >> 2);               // transposing reads: this lane's row
+  // V^T of a chunk, rows the wave's value dims: [u][32 tokens x]
+  auto read_v = [&](bf16x8(&vf)[2][2], const uint16_t *tile) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int d = 32 * wave + 8 * (r & 3) + 4 * u, row = 32 * x + tr_row;
+        vf[u][x] = join(read_transposed(tile + tile_at(row, d)),
+                        read_transposed(tile + tile_at(row + 16, d)));
+      }
+  };
+  // S' = l^n S + K^T (l^(n-1-j) V): the decayed values in three bf16 parts, which hold all
+  // 24 bits (the outputs pass needs the state as bf16 operands only: one part)
+  auto update = [&](const bf16x8(&vf)[2][2], const uint16_t *tile, int n) {
+    const float dh = power[n], dl = power_low[n];
+#pragma unroll
+    for (int t = 0; t < 8; ++t)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][u][i] = fmaf(s[t][u][i], dh, s[t][u][i] * dl);
+    constexpr int kParts = kMode == kOutputs ? 1 : 3;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      bf16x8 part[2][kParts];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x8 y = to_f32x8(vf[u][x]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = 32 * x + 4 * quad + (e & 3) + (e & 4) * 4;
+          y[e] = j < n ? y[e] * power[max(n - 1 - j, 0)] : 0.f;
+        }
+#pragma unroll
+        for (int m = 0; m < kParts; ++m) part[u][m] = take_bf16(y);
+      }
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int row = 32 * x + tr_row, d = 16 * t + 4 * (r & 3);
+        const bf16x8 kf = join(read_transposed(tile + tile_at(row, d)),
+                               read_transposed(tile + tile_at(row + 16, d)));
+#pragma unroll
+        for (int m = 0; m < kParts; ++m)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) s[t][u] = mfma16x16x32(kf, part[u][m], s[t][u]);
+      }
+    }
+  };
+
+  int buf = 0;
   for (int c = 0; c < chunks; ++c) {
     const int n = min(len - c * kChunk, kChunk);
-    store(sk, kr);
-    store(sv, vr);
-    bf16x8 vf[2][2];                                    // [u][slots 32 x]: V^T, value dim rows
-    if (kMode == kStates) __syncthreads();
-    if (kMode != kStates) {
+    bf16x8 vf[2][2];
+    if constexpr (kMode == kStates) {
+      await_loads();
+      __syncthreads();
+      if (c + 1 < chunks) {
+        load(lds_k + (buf ^ 1) * kTile * 2, a.k, c + 1, a.hkv, g);
+        load(lds_v + (buf ^ 1) * kTile * 2, a.v, c + 1, a.hkv, g);
+      }
+      read_v(vf, sv + buf * kTile);
+      update(vf, sk + buf * kTile, n);
+      buf ^= 1;
+    } else {
       bf16x8 sb[2][4];                                  // the state before the chunk, in bf16
 #pragma unroll
       for (int u = 0; u < 2; ++u)
@@ -229,22 +318,18 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
           sb[u][x] = to_bf16x8(__builtin_shufflevector(s[2 * x][u], s[2 * x + 1][u], 0, 1, 2, 3, 4,
                                                        5, 6, 7));
       for (int h = h0; h < h1; ++h) {
-        store(sq, qr);
+        const uint16_t *tq = sq + buf * kTile;
+        const bool last = h + 1 == h1;
+        await_loads();
         __syncthreads();
-        if (h + 1 < h1) {
-          load(qr, a.q, c, a.hq, g * group + h + 1);
-        } else if (c + 1 < chunks) {
-          load(qr, a.q, c + 1, a.hq, g * group + h0);
-        }
-        if (h == h0 && c + 1 < chunks) {
-          load(kr, a.k, c + 1, a.hkv, g);
-          load(vr, a.v, c + 1, a.hkv, g);
-        }
+        buf ^= 1;
+        if (!last || c + 1 < chunks)
+          load(lds_q + buf * kTile * 2, a.q, last ? c + 1 : c, a.hq, g * group + (last ? h0 : h + 1));
         // scores of tokens 16 wave + r against tokens 16 jt + 4 quad + 0..3
         {
           bf16x8 qf[4];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) qf[x] = read_rows(sq, 16 * wave + r, 32 * x + 4 * quad);
+          for (int x = 0; x < 4; ++x) qf[x] = read_rows(tq, 16 * wave + r, 32 * x + 4 * quad);
           for (int jt = 0; jt <= (wave | 1); ++jt) {
             f32x4 p = {0.f, 0.f, 0.f, 0.f};
             if (jt <= wave) {
@@ -261,24 +346,20 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
             *reinterpret_cast<bf16x4 *>(sp + score_at(16 * wave + r, 16 * jt + 4 * quad)) = w;
           }
         }
-        if (h == h0) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int d = 32 * wave + 8 * (r & 3) + 4 * u, row = 32 * x + tr_row;
-              vf[u][x] = join(read_transposed(sv + tile_at(row, d)),
-                              read_transposed(sv + tile_at(row + 16, d)));
-            }
-        }
+        if (h == h0) read_v(vf, sv);
+        if (last && (kMode == kWhole || c + 1 < chunks)) update(vf, sk, n);
         __syncthreads();
+        if (c + 1 < chunks) {
+          if (h == h0) load(lds_v, a.v, c + 1, a.hkv, g);
+          if (last) load(lds_k, a.k, c + 1, a.hkv, g);
+        }
 #pragma unroll
         for (int it = 0; it < 4; ++it) {
           if (16 * it >= n) break;
           f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            const bf16x8 qf = read_rows(sq, 16 * it + r, 32 * x + 4 * quad);
+            const bf16x8 qf = read_rows(tq, 16 * it + r, 32 * x + 4 * quad);
 #pragma unroll
             for (int u = 0; u < 2; ++u) acc[u] = mfma16x16x32(sb[u][x], qf, acc[u]);
           }
@@ -301,69 +382,17 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
                         __builtin_bit_cast(u32x4, to_bf16x8(o)));
           }
         }
-        if (h + 1 < h1) __syncthreads();
-      }
-    } else {
-      if (c + 1 < chunks) {
-        load(kr, a.k, c + 1, a.hkv, g);
-        load(vr, a.v, c + 1, a.hkv, g);
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const int d = 32 * wave + 8 * (r & 3) + 4 * u, row = 32 * x + tr_row;
-          vf[u][x] = join(read_transposed(sv + tile_at(row, d)),
-                          read_transposed(sv + tile_at(row + 16, d)));
-        }
-    }
-    if (kMode != kOutputs || c + 1 < chunks) {
-      // S' = l^n S + K^T (l^(n-1-j) V): the decayed values in three bf16 parts, which hold
-      // all 24 bits (the outputs' own state is rounded to bf16 anyway: one part)
-      const float dh = power[n], dl = power_low[n];
-#pragma unroll
-      for (int t = 0; t < 8; ++t)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[t][u][i] = fmaf(s[t][u][i], dh, s[t][u][i] * dl);
-      constexpr int kParts = kMode == kOutputs ? 1 : 3;
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        bf16x8 part[2][kParts];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          f32x8 y = to_f32x8(vf[u][x]);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int j = 32 * x + 4 * quad + (e & 3) + (e & 4) * 4;
-            y[e] = j < n ? y[e] * power[max(n - 1 - j, 0)] : 0.f;
-          }
-#pragma unroll
-          for (int m = 0; m < kParts; ++m) part[u][m] = take_bf16(y);
-        }
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-          const int row = 32 * x + tr_row, d = 16 * t + 4 * (r & 3);
-          const bf16x8 kf = join(read_transposed(sk + tile_at(row, d)),
-                                 read_transposed(sk + tile_at(row + 16, d)));
-#pragma unroll
-          for (int m = 0; m < kParts; ++m)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) s[t][u] = mfma16x16x32(kf, part[u][m], s[t][u]);
-        }
       }
     }
-    __syncthreads();
   }
   if (kMode != kOutputs) {
+    float *at = carry + 4 * quad * kHeadDim + dv;
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          carry[(16 * t + 4 * quad + i) * kHeadDim + dv + 4 * u] = s[t][u][i];
+        for (int i = 0; i < 4; ++i) at[(16 * t + i) * kHeadDim + 4 * u] = s[t][u][i];
   }
 }
 
