@@ -518,7 +518,7 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
  *   total_q and max_q_len alone.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, Hq or Hkv or num_slots <= 0, Hq % Hkv,
  *         total_q < 0, max_q_len < 0, scale not finite); RA_ERR_UNSUPPORTED (Hq / Hkv > 32,
- *         B > 65535, Hkv > 65535); RA_ERR_WORKSPACE; RA_ERR_HIP. B == 0, total_q == 0 or
+ *         B > 65535, Hq > 65535, B * Hkv > 2^25); RA_ERR_WORKSPACE; RA_ERR_HIP. B == 0, total_q == 0 or
  *         max_q_len == 0 launch nothing.
  */
 int rollout_linear_attn_decode(const void *q, const void *k_new, const void *v_new, float *states,

@@ -300,7 +300,8 @@ int page_write_impl(const void *k_new, const void *v_new, const int32_t *cu_new,
 int check_linear(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_slots, float scale) {
   if (B < 0 || Hq <= 0 || Hkv <= 0 || num_slots <= 0 || Hq % Hkv != 0 || !std::isfinite(scale))
     return RA_ERR_SHAPE;
-  if (Hq / Hkv > 32 || B > kMaxGridYZ || Hkv > kMaxGridYZ) return RA_ERR_UNSUPPORTED;
+  if (Hq / Hkv > 32 || B > kMaxGridYZ || Hq > kMaxGridYZ) return RA_ERR_UNSUPPORTED;
+  if ((int64_t)B * Hkv > INT32_MAX / 64) return RA_ERR_UNSUPPORTED;   // a grid of pairs
   return RA_OK;
 }
 

@@ -12,6 +12,8 @@
 // A row's chunks follow one another; with too few (row, KV head) pairs to fill the GPU the
 // row is cut into stretches: their own contributions to the state first (states pass), then
 // the state before each (scan), then the outputs (outputs pass).
+#include <type_traits>
+
 #include "ra_device.h"
 #include "ra_internal.h"
 
@@ -93,78 +95,93 @@ __global__ __launch_bounds__(kThreads) void linear_decode_kernel(
 }
 
 // ---- append: LDS tiles ----------------------------------------------------------------
-// A tile holds 64 tokens of 128 bf16 in 16-byte units, unit u of row r at u ^ swizzle(r):
-// 16 rows at one unit, and 4 rows at two neighbouring units, fall on different banks, so
-// that the reads along a token and the transposing reads along a dim are both spread.
-__device__ __forceinline__ int swizzle(int row) { return (row & 7) << 1 | (row >> 3 & 1); }
-__device__ __forceinline__ int tile_at(int row, int dim) {     // in elements; dim % 4 == 0
-  return row * kHeadDim + (((dim >> 3) ^ swizzle(row)) << 3) + (dim & 4);
-}
-__device__ __forceinline__ int score_at(int row, int col) {    // [64][64] scores, col % 4 == 0
-  return row * kChunk + (((col >> 3) ^ (row >> 1 & 7)) << 3) + (col & 4);
-}
+constexpr int kAppendThreads = 512;
+constexpr int kTile = kChunk * kHeadDim;
 
-__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) {
-  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-}
+// A tile holds 64 tokens of 128 bf16 in 16-byte units, unit u of row x at u ^ swizzle(x):
+// 16 rows at one unit, and four neighbouring rows at four neighbouring units, fall on
+// different banks, so that the reads along a token and the transposing reads along a dim
+// are both spread.
+__device__ __forceinline__ int swizzle(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
+constexpr int kRowBytes = 2 * kHeadDim, kScoreRowBytes = 2 * kChunk;
 
-// Operands of 32 contraction slots: lane l's eight are 4 (l / 16) + 0..3 and 16 more, the
-// order in which two accumulator tiles hold their rows.
-__device__ __forceinline__ bf16x8 read_rows(const uint16_t *tile, int row, int dim) {
-  return join(*reinterpret_cast<const bf16x4 *>(tile + tile_at(row, dim)),
-              *reinterpret_cast<const bf16x4 *>(tile + tile_at(row, dim + 16)));
+__device__ __forceinline__ bf16x8 lds_bf16x8(const uint16_t *tile, int byte) {
+  return load_bf16x8(tile + byte / 2);
 }
 
 // ds_read_b64_tr_b16: of 16 lanes, lane i supplies the address of row i / 4's four columns
-// at i % 4 and receives column i of the four rows.
-__device__ __forceinline__ bf16x4 read_transposed(const uint16_t *at) {
+// at i % 4 and receives column i of the four rows. Two of them: eight rows (the second
+// four's swizzle differs in bit 0).
+__device__ __forceinline__ bf16x8 read_transposed(const uint16_t *tile, int byte) {
   typedef __attribute__((address_space(3))) s16x4 lds_t;
-  return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                        (lds_t *)const_cast<uint16_t *>(at)));
+  const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_t *)const_cast<uint16_t *>(tile + byte / 2));
+  const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_t *)const_cast<uint16_t *>(tile + 4 * kHeadDim + (byte ^ 16) / 2));
+  return __builtin_shufflevector(__builtin_bit_cast(bf16x4, a), __builtin_bit_cast(bf16x4, b), 0,
+                                 1, 2, 3, 4, 5, 6, 7);
 }
 
-// The bf16 rounding of x, taken off x.
+// x's upper 16 bits as bf16, taken off x: three times, and the parts hold all 24 bits.
 __device__ __forceinline__ bf16x8 take_bf16(f32x8 &x) {
-  const bf16x8 h = to_bf16x8(x);
-  x -= to_f32x8(h);
-  return h;
+  u32x4 packed;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t lo = __float_as_uint(x[2 * i]), hi = __float_as_uint(x[2 * i + 1]);
+    packed[i] = __builtin_amdgcn_perm(hi, lo, 0x07060302);
+    x[2 * i] -= __uint_as_float(lo & 0xffff0000u);
+    x[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
+  }
+  return __builtin_bit_cast(bf16x8, packed);
 }
 
-enum { kWhole, kStates, kOutputs };
-
-// 16 bytes a lane from global memory to LDS, lane l's at `lds` + 16 l (lds and lane 0's
-// address are the wave's). In assembly: behind the builtin the compiler waits for all such
-// loads before any LDS read; here await_loads() does, before the barrier that hands the
-// tile over.
-__device__ __forceinline__ void load_to_lds(const uint16_t *g, uint32_t lds) {
+// 16 bytes a lane from global memory (base + the lane's byte offset) to LDS, lane l's at
+// `lds` + 16 l; base and lds are the wave's. In assembly: behind the builtin the compiler
+// waits for all such loads before any LDS read; here await_loads() does, before the
+// barrier that hands the tile over.
+__device__ __forceinline__ void load_to_lds(const uint16_t *base, uint32_t offset, uint32_t lds) {
   asm volatile(
       "s_mov_b32 m0, %0\n\t"
       "s_nop 0\n\t"
-      "global_load_lds_dwordx4 %1, off"
+      "global_load_lds_dwordx4 %1, %2"
       :
-      : "s"(lds), "v"(g)
+      : "s"(lds), "v"(offset), "s"(base)
       : "memory", "m0");
 }
 __device__ __forceinline__ void await_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// The same for loads with four stores issued behind them (counted in order): the stores
+// may still be on their way.
+__device__ __forceinline__ void await_loads_before_4() {
+  asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+}
 __device__ __forceinline__ uint32_t lds_address(const uint16_t *p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
 }
 
+// x, as a value the compiler computes from anew: what follows from it is not kept in
+// registers around a loop, of which the state leaves few.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+enum { kWhole, kStates, kOutputs };
+
 // One stretch of a (row, KV head): chunks in order, the state in the accumulators. Wave w
-// holds the 32 value dims from 32 w, all 128 key dims: tile (t, u), t < 8, u < 2, has key
-// dims 16 t + 0..15 as its rows and value dims 32 w + 8 (c / 4) + 4 u + c % 4 as its
-// columns c, so that a lane's accumulators of two result tiles are eight neighbouring
-// value dims of a token. An accumulator tile of the state is the matrix operand of
-// S^T Q^T as it stands, rounded to bf16. Scores go through LDS: wave w computes those of
-// tokens 16 w .. 16 w + 15, all waves use all of them.
+// of 8 holds the 16 value dims from 16 w, all 128 key dims: tile t = 2 x + y has key dims
+// 32 x + 8 (m / 4) + 4 y + m % 4 as its rows m, so that two accumulator tiles, rounded to
+// bf16, are the operand of S^T Q^T for the 32 key dims from 32 x as they stand (a lane's
+// eight contraction slots: 8 (l / 16) + 0..7), and a lane's results are four neighbouring
+// value dims of a token. Scores go through LDS: a wave computes two of the 16 tiles, all
+// waves use all of them.
 //
 // A step is a chunk and a query head of the group, with two barriers: the step's tiles are
 // there (scores, then with the chunk's last head the state's update); the scores are there
 // (outputs, while the next chunk's K and V load; V's tile is free once the first head
-// has its operands, K's after the update). Q has two tiles. 72 KB of LDS: two workgroups
-// per CU, whose steps overlap.
+// has its operands, K's after the update). Q has two tiles. 73 KB of LDS and 128 registers:
+// two workgroups per CU, whose steps overlap.
 template <int kMode>
-__global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a) {
+__global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
@@ -186,213 +203,244 @@ __global__ __launch_bounds__(kThreads, 2) void linear_chunk_kernel(LinearArgs a)
   if (slot < 0 || slot >= a.num_slots) {
     if (kMode != kStates)
       for (int t = 0; t < len; ++t)
-        for (int i = tid; i < (h1 - h0) * kHeadDim; i += kThreads)
+        for (int i = tid; i < (h1 - h0) * kHeadDim; i += kAppendThreads)
           a.out[((tok0 + t) * a.hq + g * group + h0) * kHeadDim + i] = 0;
     return;
   }
 
-  constexpr int kTile = kChunk * kHeadDim;
-  constexpr int kVTiles = kMode == kStates ? 2 : 1, kKTiles = kMode == kStates ? 2 : 1;
-  __shared__ __align__(1024) uint16_t sk[kKTiles * kTile], sv[kVTiles * kTile];
+  constexpr int kKVTiles = kMode == kStates ? 2 : 1;
+  __shared__ __align__(1024) uint16_t sk[kKVTiles * kTile], sv[kKVTiles * kTile];
   __shared__ __align__(1024) uint16_t sq[kMode == kStates ? 8 : 2 * kTile];
   __shared__ __align__(1024) uint16_t sp[kMode == kStates ? 8 : kChunk * kChunk];
-  __shared__ float power[kChunk + 1], power_low[kChunk + 1];   // l^n and what fp32 leaves out
+  // l^n; scale l^n; l^(63 - j), then zeros
+  __shared__ float power[kChunk + 1], weight[2 * kChunk];
+  __shared__ double decays[kChunk + 1];
   const double ld = log_decay_of(a.log_decay, g);
   const float l2 = (float)(ld * 1.4426950408889634);
   if (tid <= kChunk) {
     const double p = exp(ld * tid);
-    power[tid] = (float)p;
-    power_low[tid] = (float)(p - (double)(float)p);
+    decays[tid] = p;
+    power[tid] = (float)(a.scale * p);
+    if (tid < kChunk) {
+      weight[kChunk - 1 - tid] = (float)p;
+      weight[kChunk + tid] = 0.f;
+    }
   }
 
-  // loads: wave w takes rows 16 w .. 16 w + 15 of a tile, four rows an instruction, lane l
-  // the unit of row l / 16 that belongs at l % 16; rows past the end repeat the last one
-  const uint32_t lds_k = lds_address(sk) + wave * 4096, lds_v = lds_address(sv) + wave * 4096;
-  const uint32_t lds_q = lds_address(sq) + wave * 4096;
-  const int ld_unit = (lane % 16) ^ (lane / 16 << 1);
-  auto load = [&](uint32_t lds, const uint16_t *src, int c, int heads, int head) {
+  // loads: wave w takes rows 8 w .. 8 w + 7 of a tile, four rows an instruction, lane l the
+  // unit of row l / 16 that belongs at l % 16; rows past the end repeat the last one
+  const uint32_t lds_k = lds_address(sk) + wave * 2048, lds_v = lds_address(sv) + wave * 2048;
+  const uint32_t lds_q = lds_address(sq) + wave * 2048;
+  const int ld_unit = (lane % 16) ^ (lane / 16 << 2) ^ (wave & 1) << 1;
+  const int q_stride = a.hq * kRowBytes, kv_stride = a.hkv * kRowBytes;
+  const uint32_t q_off = __umul24(lane / 16, q_stride) + (ld_unit << 4);
+  const uint32_t kv_off = __umul24(lane / 16, kv_stride) + (ld_unit << 4);
+  auto load = [&](uint32_t lds, const uint16_t *src, int c, int heads, int head, uint32_t off,
+                  int stride) {
+    const int row = c * kChunk + 8 * wave, left = len - 1 - row;
+    const uint16_t *base = src + ((tok0 + row) * heads + head) * kHeadDim;
+    if (left >= 7) {
+      load_to_lds(base, off, lds);
+      load_to_lds(base, (off ^ 16) + 4 * stride, lds + 1024);
+    } else {
+      const uint16_t *first = src + ((tok0 + c * kChunk) * heads + head) * kHeadDim;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      const int t = min(c * kChunk + 16 * wave + 4 * m + lane / 16, len - 1);
-      load_to_lds(src + ((tok0 + t) * heads + head) * kHeadDim +
-                      ((ld_unit ^ ((m & 1) << 3 | m >> 1)) << 3),
-                  lds + 1024 * m);
+      for (int m = 0; m < 2; ++m) {
+        const int t = 8 * wave + min(4 * m + lane / 16, left);
+        load_to_lds(first, __umul24(t, stride) + ((ld_unit ^ m) << 4), lds + 1024 * m);
+      }
     }
   };
   const int chunks = (len + kChunk - 1) / kChunk;
-  load(lds_k, a.k, 0, a.hkv, g);
-  load(lds_v, a.v, 0, a.hkv, g);
-  if (kMode != kStates) load(lds_q, a.q, 0, a.hq, g * group + h0);
+  load(lds_k, a.k, 0, a.hkv, g, kv_off, kv_stride);
+  load(lds_v, a.v, 0, a.hkv, g, kv_off, kv_stride);
+  if (kMode != kStates) load(lds_q, a.q, 0, a.hq, g * group + h0, q_off, q_stride);
 
-  // state tile (t, u), register i: key dim 16 t + 4 quad + i, value dim `dv` + 4 u
-  const int dv = 32 * wave + 8 * (r >> 2) + (r & 3);
-  f32x4 s[8][2];
+  // state tile t = 2 x + y, register i: key dim 32 x + 8 quad + 4 y + i, value dim 16 wave + r
+  f32x4 s[8];
   float *pool = a.states + ((int64_t)slot * a.hkv + g) * kStateSize;
   float *carry = kMode == kWhole ? pool
                                  : a.carry + (((int64_t)b * a.hkv + g) * a.segments + seg) * kStateSize;
   const bool zero = kMode == kStates || (kMode == kWhole && a.ctx_lens[b] <= 0);
+  float *const s_at = carry + 8 * quad * kHeadDim + 16 * wave + r;
 #pragma unroll
-  for (int t = 0; t < 8; ++t)
-#pragma unroll
-    for (int u = 0; u < 2; ++u) s[t][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int t = 0; t < 8; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (!zero) {
-    const float *at = carry + 4 * quad * kHeadDim + dv;
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][u][i] = at[(16 * t + i) * kHeadDim + 4 * u];
+      for (int i = 0; i < 4; ++i)
+        s[t][i] = s_at[(32 * (t / 2) + 4 * (t % 2) + i) * kHeadDim];
   }
 
-  const int tr_row = 4 * quad + (r >> 2);               // transposing reads: this lane's row
-  // V^T of a chunk, rows the wave's value dims: [u][32 tokens x]
-  auto read_v = [&](bf16x8(&vf)[2][2], const uint16_t *tile) {
+  // byte addresses in the tiles: rows r at unit quad (32 dims on: ^ 64), and for the
+  // transposing reads rows 8 quad + r / 4 at this lane's four dims of the first K tile, the
+  // wave's of V
+  const int at_row = r * kRowBytes + ((quad ^ swizzle(r)) << 4);
+  const int tr_row = 8 * quad + (r >> 2), tr_swizzle = swizzle(tr_row);
+  const int at_k = tr_row * kRowBytes + (((r & 3) ^ tr_swizzle) << 4);
+  const int at_v = tr_row * kRowBytes + (((2 * wave + (r >> 1 & 1)) ^ tr_swizzle) << 4) + (r & 1) * 8;
+  const int at_score = r * kScoreRowBytes + ((quad ^ (r >> 1)) << 4);
+
+  // V^T of a chunk, rows the wave's value dims, slots the 32 tokens from 32 x
+  auto read_v = [&](bf16x8(&vf)[2], const uint16_t *tile) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int d = 32 * wave + 8 * (r & 3) + 4 * u, row = 32 * x + tr_row;
-        vf[u][x] = join(read_transposed(tile + tile_at(row, d)),
-                        read_transposed(tile + tile_at(row + 16, d)));
-      }
+    for (int x = 0; x < 2; ++x) vf[x] = read_transposed(tile + 32 * x * kHeadDim, at_v);
   };
-  // S' = l^n S + K^T (l^(n-1-j) V): the decayed values in three bf16 parts, which hold all
-  // 24 bits (the outputs pass needs the state as bf16 operands only: one part)
-  auto update = [&](const bf16x8(&vf)[2][2], const uint16_t *tile, int n) {
-    const float dh = power[n], dl = power_low[n];
+  // S' = decay S + K^T (after l^(n-1-j) V), n the chunk's tokens: the decayed values in
+  // three bf16 parts, which hold all 24 bits (the outputs pass needs the state as bf16
+  // operands only: one part). The states pass has no state to decay: its weights reach to
+  // the end of the stretch (after = l^tokens behind the chunk).
+  auto update = [&](const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay, float after) {
+    const int at = fresh(at_k);
+    if (kMode != kStates) {
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][u][i] = fmaf(s[t][u][i], dh, s[t][u][i] * dl);
+      for (int t = 0; t < 8; ++t) s[t] *= decay;
+    }
     constexpr int kParts = kMode == kOutputs ? 1 : 3;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      bf16x8 part[2][kParts];
+      bf16x8 part[kParts];
+      f32x8 y = to_f32x8(vf[x]);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        f32x8 y = to_f32x8(vf[u][x]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = 32 * x + 4 * quad + (e & 3) + (e & 4) * 4;
-          y[e] = j < n ? y[e] * power[max(n - 1 - j, 0)] : 0.f;
-        }
-#pragma unroll
-        for (int m = 0; m < kParts; ++m) part[u][m] = take_bf16(y);
+      for (int e = 0; e < 8; ++e) {
+        const float w = weight[kChunk - n + 32 * x + 8 * quad + e];
+        y[e] *= kMode == kStates ? w * after : w;
       }
+      if (kParts == 1) part[0] = to_bf16x8(y);
+#pragma unroll
+      for (int m = 0; m < (kParts == 1 ? 0 : kParts); ++m) part[m] = take_bf16(y);
 #pragma unroll
       for (int t = 0; t < 8; ++t) {
-        const int row = 32 * x + tr_row, d = 16 * t + 4 * (r & 3);
-        const bf16x8 kf = join(read_transposed(tile + tile_at(row, d)),
-                               read_transposed(tile + tile_at(row + 16, d)));
+        const bf16x8 kf = read_transposed(tile + 32 * x * kHeadDim + 4 * (t % 2), at ^ (t / 2 << 6));
 #pragma unroll
-        for (int m = 0; m < kParts; ++m)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) s[t][u] = mfma16x16x32(kf, part[u][m], s[t][u]);
+        for (int m = 0; m < kParts; ++m) s[t] = mfma16x16x32(kf, part[m], s[t]);
       }
     }
   };
 
+  // where the lane's scores of tokens 16 (wave % 4) + r against 16 (wave / 4) + 4 quad + 0..3 go
+  const int at_p = (16 * (wave & 3) + r) * kScoreRowBytes +
+                   (((2 * (wave >> 2) + (quad >> 1)) ^ (r >> 1)) << 4) + (quad & 1) * 8;
+  // scores: this wave's two tiles' scale l^(i - j), zero above the diagonal; the lane's four
+  // j are 4 quad + 0..3
+  float mult[2][4];
+#pragma unroll
+  for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int d = 16 * ((wave & 3) - (wave >> 2) - 2 * jj) + r - 4 * quad - i;
+      mult[jj][i] = d >= 0 ? a.scale * __builtin_amdgcn_exp2f(l2 * (float)d) : 0.f;
+    }
+
   int buf = 0;
+  double drift = 1.0;
   for (int c = 0; c < chunks; ++c) {
     const int n = min(len - c * kChunk, kChunk);
-    bf16x8 vf[2][2];
+    bf16x8 vf[2];
     if constexpr (kMode == kStates) {
       await_loads();
       __syncthreads();
       if (c + 1 < chunks) {
-        load(lds_k + (buf ^ 1) * kTile * 2, a.k, c + 1, a.hkv, g);
-        load(lds_v + (buf ^ 1) * kTile * 2, a.v, c + 1, a.hkv, g);
+        load(lds_k + (buf ^ 1) * kTile * 2, a.k, c + 1, a.hkv, g, kv_off, kv_stride);
+        load(lds_v + (buf ^ 1) * kTile * 2, a.v, c + 1, a.hkv, g, kv_off, kv_stride);
       }
       read_v(vf, sv + buf * kTile);
-      update(vf, sk + buf * kTile, n);
+      update(vf, sk + buf * kTile, n, 1.f,
+             __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
       buf ^= 1;
     } else {
-      bf16x8 sb[2][4];                                  // the state before the chunk, in bf16
+      bf16x8 sb[4];                                     // the state before the chunk, in bf16
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          sb[u][x] = to_bf16x8(__builtin_shufflevector(s[2 * x][u], s[2 * x + 1][u], 0, 1, 2, 3, 4,
-                                                       5, 6, 7));
+      for (int x = 0; x < 4; ++x)
+        sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
       for (int h = h0; h < h1; ++h) {
         const uint16_t *tq = sq + buf * kTile;
         const bool last = h + 1 == h1;
-        await_loads();
+        // behind the tiles' loads: the step before's stores, four where its chunk was full
+        if (n == kChunk && (c > 0 || h > h0)) {
+          await_loads_before_4();
+        } else {
+          await_loads();
+        }
         __syncthreads();
         buf ^= 1;
         if (!last || c + 1 < chunks)
-          load(lds_q + buf * kTile * 2, a.q, last ? c + 1 : c, a.hq, g * group + (last ? h0 : h + 1));
-        // scores of tokens 16 wave + r against tokens 16 jt + 4 quad + 0..3
+          load(lds_q + buf * kTile * 2, a.q, last ? c + 1 : c, a.hq, g * group + (last ? h0 : h + 1),
+               q_off, q_stride);
+        // scores of tokens 16 it + r against tokens 16 jt + 4 quad + 0..3; tiles above the
+        // diagonal are zero, and needed where they share 32 slots with one on it
         {
+          const int it = wave & 3, at = fresh(at_row), pt = fresh(at_p);
           bf16x8 qf[4];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) qf[x] = read_rows(tq, 16 * wave + r, 32 * x + 4 * quad);
-          for (int jt = 0; jt <= (wave | 1); ++jt) {
+          for (int x = 0; x < 4; ++x) qf[x] = lds_bf16x8(tq + 16 * it * kHeadDim, at ^ (x << 6));
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) {
+            const int jt = (wave >> 2) + 2 * jj;
+            if (jt > (it | 1)) break;
             f32x4 p = {0.f, 0.f, 0.f, 0.f};
-            if (jt <= wave) {
+            if (jt <= it) {
 #pragma unroll
               for (int x = 0; x < 4; ++x)
-                p = mfma16x16x32(read_rows(sk, 16 * jt + r, 32 * x + 4 * quad), qf[x], p);
+                p = mfma16x16x32(lds_bf16x8(sk + 16 * jt * kHeadDim, at ^ (x << 6)), qf[x], p);
             }
             bf16x4 w;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const int d = 16 * (wave - jt) + r - 4 * quad - i;
-              w[i] = (__bf16)(d >= 0 ? p[i] * __builtin_amdgcn_exp2f(l2 * (float)d) : 0.f);
-            }
-            *reinterpret_cast<bf16x4 *>(sp + score_at(16 * wave + r, 16 * jt + 4 * quad)) = w;
+            for (int i = 0; i < 4; ++i) w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[i] * mult[jj][i]);
+            *reinterpret_cast<bf16x4 *>(sp + (pt ^ (jj << 6)) / 2) = w;
           }
         }
         if (h == h0) read_v(vf, sv);
-        if (last && (kMode == kWhole || c + 1 < chunks)) update(vf, sk, n);
+        if (last && (kMode == kWhole || c + 1 < chunks)) {
+          // the product of the chunks' decays as they were rounded is kept at l^tokens: what
+          // one rounding adds, the next chunk's takes off
+          const double exact = decays[n];
+          const float decay = (float)(exact * drift);
+          if (kMode == kWhole && exact > 1e-30) drift = exact * drift / decay;
+          update(vf, sk, n, decay, 1.f);
+        }
         __syncthreads();
         if (c + 1 < chunks) {
-          if (h == h0) load(lds_v, a.v, c + 1, a.hkv, g);
-          if (last) load(lds_k, a.k, c + 1, a.hkv, g);
+          if (h == h0) load(lds_v, a.v, c + 1, a.hkv, g, kv_off, kv_stride);
+          if (last) load(lds_k, a.k, c + 1, a.hkv, g, kv_off, kv_stride);
         }
+        const int at = fresh(at_row), pt = fresh(at_score);
+        uint16_t *const o_row = a.out + ((tok0 + c * kChunk) * a.hq + g * group + h) * kHeadDim;
+        const uint32_t o_at = __umul24(r, a.hq * kHeadDim) + 16 * wave + 4 * quad;
+        // a full chunk's four token tiles have no branch between them, so that their reads
+        // and products interleave
+        auto outputs = [&](auto full) {
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-          if (16 * it >= n) break;
-          f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+          for (int it = 0; it < 4; ++it) {
+            if (!full && 16 * it >= n) break;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const bf16x8 qf = read_rows(tq, 16 * it + r, 32 * x + 4 * quad);
+            for (int x = 0; x < 4; ++x)
+              acc = mfma16x16x32(sb[x], lds_bf16x8(tq + 16 * it * kHeadDim, at ^ (x << 6)), acc);
+            acc *= power[16 * it + r + 1];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) acc[u] = mfma16x16x32(sb[u][x], qf, acc[u]);
+            for (int x = 0; x <= it / 2; ++x)
+              acc = mfma16x16x32(vf[x], lds_bf16x8(sp + 16 * it * kChunk, pt ^ (x << 6)), acc);
+            if (full || 16 * it + r < n)
+              *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
+                  __builtin_convertvector(acc, bf16x4);
           }
-          const float w = power[16 * it + r + 1];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) acc[u] *= w;
-#pragma unroll
-          for (int x = 0; x <= it / 2; ++x) {
-            const int row = 16 * it + r;
-            const bf16x8 pf = join(
-                *reinterpret_cast<const bf16x4 *>(sp + score_at(row, 32 * x + 4 * quad)),
-                *reinterpret_cast<const bf16x4 *>(sp + score_at(row, 32 * x + 16 + 4 * quad)));
-#pragma unroll
-            for (int u = 0; u < 2; ++u) acc[u] = mfma16x16x32(vf[u][x], pf, acc[u]);
-          }
-          if (16 * it + r < n) {
-            const f32x8 o = __builtin_shufflevector(acc[0], acc[1], 0, 1, 2, 3, 4, 5, 6, 7) * a.scale;
-            const int64_t t = tok0 + c * kChunk + 16 * it + r;
-            store_u32x4(a.out + (t * a.hq + g * group + h) * kHeadDim + 32 * wave + 8 * quad,
-                        __builtin_bit_cast(u32x4, to_bf16x8(o)));
-          }
+        };
+        if (n == kChunk) {
+          outputs(std::true_type());
+        } else {
+          outputs(std::false_type());
         }
       }
     }
   }
   if (kMode != kOutputs) {
-    float *at = carry + 4 * quad * kHeadDim + dv;
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) at[(16 * t + i) * kHeadDim + 4 * u] = s[t][u][i];
+      for (int i = 0; i < 4; ++i)
+        s_at[(32 * (t / 2) + 4 * (t % 2) + i) * kHeadDim] = s[t][i];
   }
 }
 
@@ -470,14 +518,14 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
                   p.segments, p.segment_len, p.head_splits, scale};
   const unsigned pairs = (unsigned)B * (unsigned)hkv;
   if (p.segments == 1) {
-    hipLaunchKernelGGL(linear_chunk_kernel<kWhole>, dim3(pairs), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL(linear_chunk_kernel<kWhole>, dim3(pairs), dim3(kAppendThreads), 0, stream, a);
   } else {
-    hipLaunchKernelGGL(linear_chunk_kernel<kStates>, dim3(pairs * p.segments), dim3(kThreads), 0,
+    hipLaunchKernelGGL(linear_chunk_kernel<kStates>, dim3(pairs * p.segments), dim3(kAppendThreads), 0,
                        stream, a);
     hipLaunchKernelGGL(linear_scan_kernel, dim3(kStateSize / (4 * kThreads), pairs),
                        dim3(kThreads), 0, stream, a);
     hipLaunchKernelGGL(linear_chunk_kernel<kOutputs>, dim3(pairs * p.segments * p.head_splits),
-                       dim3(kThreads), 0, stream, a);
+                       dim3(kAppendThreads), 0, stream, a);
   }
   return hipGetLastError();
 }
