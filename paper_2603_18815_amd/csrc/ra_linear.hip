@@ -102,22 +102,25 @@ constexpr int kTile = kChunk * kHeadDim;
 // 16 rows at one unit, and four neighbouring rows at four neighbouring units, fall on
 // different banks, so that the reads along a token and the transposing reads along a dim
 // are both spread.
-__device__ __forceinline__ int swizzle(int row) { return (row & 3) << 2 | (row >> 2 & 3); }
+__device__ __forceinline__ int swizzle(int row) {
+  return (row & 3) << 2 | ((row >> 2 ^ row >> 3) & 1) << 1 | (row >> 3 & 1);
+}
 constexpr int kRowBytes = 2 * kHeadDim, kScoreRowBytes = 2 * kChunk;
 
 __device__ __forceinline__ bf16x8 lds_bf16x8(const uint16_t *tile, int byte) {
-  return load_bf16x8(tile + byte / 2);
+  return *reinterpret_cast<const bf16x8 *>(reinterpret_cast<const char *>(tile) + byte);
 }
 
 // ds_read_b64_tr_b16: of 16 lanes, lane i supplies the address of row i / 4's four columns
 // at i % 4 and receives column i of the four rows. Two of them: eight rows (the second
-// four's swizzle differs in bit 0).
+// four's swizzle differs in bit 1).
 __device__ __forceinline__ bf16x8 read_transposed(const uint16_t *tile, int byte) {
   typedef __attribute__((address_space(3))) s16x4 lds_t;
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (lds_t *)const_cast<uint16_t *>(tile + byte / 2));
+      (lds_t *)(const_cast<char *>(reinterpret_cast<const char *>(tile)) + byte));
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (lds_t *)const_cast<uint16_t *>(tile + 4 * kHeadDim + (byte ^ 16) / 2));
+      (lds_t *)(const_cast<char *>(reinterpret_cast<const char *>(tile + 4 * kHeadDim)) +
+                (byte ^ 32)));
   return __builtin_shufflevector(__builtin_bit_cast(bf16x4, a), __builtin_bit_cast(bf16x4, b), 0,
                                  1, 2, 3, 4, 5, 6, 7);
 }
@@ -158,6 +161,9 @@ __device__ __forceinline__ uint32_t lds_address(const uint16_t *p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
 }
 
+// Nothing moves across: reads placed before a group of products are issued before it.
+__device__ __forceinline__ void keep_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // x, as a value the compiler computes from anew: what follows from it is not kept in
 // registers around a loop, of which the state leaves few.
 __device__ __forceinline__ int fresh(int x) {
@@ -181,7 +187,7 @@ enum { kWhole, kStates, kOutputs };
 // has its operands, K's after the update). Q has two tiles. 73 KB of LDS and 128 registers:
 // two workgroups per CU, whose steps overlap.
 template <int kMode>
-__global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearArgs a) {
+__global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void linear_chunk_kernel(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
@@ -208,8 +214,7 @@ __global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearA
     return;
   }
 
-  constexpr int kKVTiles = kMode == kStates ? 2 : 1;
-  __shared__ __align__(1024) uint16_t sk[kKVTiles * kTile], sv[kKVTiles * kTile];
+  __shared__ __align__(1024) uint16_t sk[2 * kTile], sv[2 * kTile];
   __shared__ __align__(1024) uint16_t sq[kMode == kStates ? 8 : 2 * kTile];
   __shared__ __align__(1024) uint16_t sp[kMode == kStates ? 8 : kChunk * kChunk];
   // l^n; scale l^n; l^(63 - j), then zeros
@@ -231,30 +236,33 @@ __global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearA
   // unit of row l / 16 that belongs at l % 16; rows past the end repeat the last one
   const uint32_t lds_k = lds_address(sk) + wave * 2048, lds_v = lds_address(sv) + wave * 2048;
   const uint32_t lds_q = lds_address(sq) + wave * 2048;
-  const int ld_unit = (lane % 16) ^ (lane / 16 << 2) ^ (wave & 1) << 1;
+  const int ld_unit = (lane % 16) ^ swizzle(8 * wave + lane / 16);
   const int q_stride = a.hq * kRowBytes, kv_stride = a.hkv * kRowBytes;
-  const uint32_t q_off = __umul24(lane / 16, q_stride) + (ld_unit << 4);
-  const uint32_t kv_off = __umul24(lane / 16, kv_stride) + (ld_unit << 4);
-  auto load = [&](uint32_t lds, const uint16_t *src, int c, int heads, int head, uint32_t off,
-                  int stride) {
-    const int row = c * kChunk + 8 * wave, left = len - 1 - row;
-    const uint16_t *base = src + ((tok0 + row) * heads + head) * kHeadDim;
-    if (left >= 7) {
+  const uint32_t q_off = __umul24(8 * wave + lane / 16, q_stride) + (ld_unit << 4);
+  const uint32_t kv_off = __umul24(8 * wave + lane / 16, kv_stride) + (ld_unit << 4);
+  // base: row 0 of the tile, left: rows behind it
+  auto load = [&](uint32_t lds, const uint16_t *base, uint32_t off, int stride, int left) {
+    if (left >= kChunk - 1) {
       load_to_lds(base, off, lds);
-      load_to_lds(base, (off ^ 16) + 4 * stride, lds + 1024);
+      load_to_lds(base, (off ^ 32) + 4 * stride, lds + 1024);
     } else {
-      const uint16_t *first = src + ((tok0 + c * kChunk) * heads + head) * kHeadDim;
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const int t = 8 * wave + min(4 * m + lane / 16, left);
-        load_to_lds(first, __umul24(t, stride) + ((ld_unit ^ m) << 4), lds + 1024 * m);
-      }
+      for (int m = 0; m < 2; ++m)
+        load_to_lds(base,
+                    __umul24(min(8 * wave + 4 * m + lane / 16, left), stride) + ((ld_unit ^ 2 * m) << 4),
+                    lds + 1024 * m);
     }
   };
   const int chunks = (len + kChunk - 1) / kChunk;
-  load(lds_k, a.k, 0, a.hkv, g, kv_off, kv_stride);
-  load(lds_v, a.v, 0, a.hkv, g, kv_off, kv_stride);
-  if (kMode != kStates) load(lds_q, a.q, 0, a.hq, g * group + h0, q_off, q_stride);
+  const size_t q_chunk = (size_t)kChunk * a.hq * kHeadDim, kv_chunk = (size_t)kChunk * a.hkv * kHeadDim;
+  const size_t q_first = ((size_t)tok0 * a.hq + g * group) * kHeadDim;
+  const uint16_t *kp = a.k + ((size_t)tok0 * a.hkv + g) * kHeadDim;   // the chunk to load next
+  const uint16_t *vp = a.v + ((size_t)tok0 * a.hkv + g) * kHeadDim;
+  const uint16_t *qp = a.q + q_first;                                 // the chunk at hand
+  uint16_t *op = a.out + q_first;
+  load(lds_k, kp, kv_off, kv_stride, len - 1);
+  load(lds_v, vp, kv_off, kv_stride, len - 1);
+  if (kMode != kStates) load(lds_q, qp + h0 * kHeadDim, q_off, q_stride, len - 1);
 
   // state tile t = 2 x + y, register i: key dim 32 x + 8 quad + 4 y + i, value dim 16 wave + r
   f32x4 s[8];
@@ -297,7 +305,15 @@ __global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearA
 #pragma unroll
       for (int t = 0; t < 8; ++t) s[t] *= decay;
     }
+    // K's operands are read a pair of tiles ahead of the products
     constexpr int kParts = kMode == kOutputs ? 1 : 3;
+    bf16x8 kf[2][2];
+    auto read_pair = [&](int i) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+        kf[i % 2][y] = read_transposed(tile + 32 * (i / 4) * kHeadDim + 4 * y, at ^ (i % 4 << 6));
+    };
+    read_pair(0);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       bf16x8 part[kParts];
@@ -311,10 +327,15 @@ __global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearA
 #pragma unroll
       for (int m = 0; m < (kParts == 1 ? 0 : kParts); ++m) part[m] = take_bf16(y);
 #pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const bf16x8 kf = read_transposed(tile + 32 * x * kHeadDim + 4 * (t % 2), at ^ (t / 2 << 6));
+      for (int i = 4 * x; i < 4 * x + 4; ++i) {
+        if (i + 1 < 8) read_pair(i + 1);
+        keep_order();
 #pragma unroll
-        for (int m = 0; m < kParts; ++m) s[t] = mfma16x16x32(kf, part[m], s[t]);
+        for (int m = 0; m < kParts; ++m)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            s[2 * (i % 4) + y] = mfma16x16x32(kf[i % 2][y], part[m], s[2 * (i % 4) + y]);
+        keep_order();
       }
     }
   };
@@ -333,29 +354,37 @@ __global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearA
       mult[jj][i] = d >= 0 ? a.scale * __builtin_amdgcn_exp2f(l2 * (float)d) : 0.f;
     }
 
-  int buf = 0;
+  int q_buf = 0;
   double drift = 1.0;
   for (int c = 0; c < chunks; ++c) {
     const int n = min(len - c * kChunk, kChunk);
     bf16x8 vf[2];
+    const int buf = c & 1;
+    const bool more = c + 1 < chunks;
+    const int left = len - 1 - (c + 1) * kChunk;        // rows behind the next chunk's first
+    const uint16_t *const tk = sk + buf * kTile, *const tv = sv + buf * kTile;
+    kp += kv_chunk;
+    vp += kv_chunk;
+    auto load_k = [&]() {
+      if (more) load(lds_k + (buf ^ 1) * kTile * 2, kp, kv_off, kv_stride, left);
+    };
+    auto load_v = [&]() {
+      if (more) load(lds_v + (buf ^ 1) * kTile * 2, vp, kv_off, kv_stride, left);
+    };
     if constexpr (kMode == kStates) {
       await_loads();
       __syncthreads();
-      if (c + 1 < chunks) {
-        load(lds_k + (buf ^ 1) * kTile * 2, a.k, c + 1, a.hkv, g, kv_off, kv_stride);
-        load(lds_v + (buf ^ 1) * kTile * 2, a.v, c + 1, a.hkv, g, kv_off, kv_stride);
-      }
-      read_v(vf, sv + buf * kTile);
-      update(vf, sk + buf * kTile, n, 1.f,
-             __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
-      buf ^= 1;
+      load_k();
+      load_v();
+      read_v(vf, tv);
+      update(vf, tk, n, 1.f, __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
     } else {
       bf16x8 sb[4];                                     // the state before the chunk, in bf16
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
       for (int h = h0; h < h1; ++h) {
-        const uint16_t *tq = sq + buf * kTile;
+        const uint16_t *const tq = sq + q_buf * kTile;
         const bool last = h + 1 == h1;
         // behind the tiles' loads: the step before's stores, four where its chunk was full
         if (n == kChunk && (c > 0 || h > h0)) {
@@ -364,75 +393,94 @@ __global__ __launch_bounds__(kAppendThreads, 4) void linear_chunk_kernel(LinearA
           await_loads();
         }
         __syncthreads();
-        buf ^= 1;
-        if (!last || c + 1 < chunks)
-          load(lds_q + buf * kTile * 2, a.q, last ? c + 1 : c, a.hq, g * group + (last ? h0 : h + 1),
-               q_off, q_stride);
-        // scores of tokens 16 it + r against tokens 16 jt + 4 quad + 0..3; tiles above the
-        // diagonal are zero, and needed where they share 32 slots with one on it
-        {
-          const int it = wave & 3, at = fresh(at_row), pt = fresh(at_p);
-          bf16x8 qf[4];
+        // Q of all tokens; K of the wave's two score tiles: those of tokens 16 it + r against
+        // 16 jt + 4 quad + 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero,
+        // and needed where a tile shares 32 slots with one on it.
+        const int it_p = wave & 3, jt_p = wave >> 2, at = fresh(at_row), pt = fresh(at_p);
+        bf16x8 qf[4][4], kf[2][4];
 #pragma unroll
-          for (int x = 0; x < 4; ++x) qf[x] = lds_bf16x8(tq + 16 * it * kHeadDim, at ^ (x << 6));
+        for (int x = 0; x < 4; ++x) kf[0][x] = lds_bf16x8(tk + 16 * jt_p * kHeadDim, at ^ (x << 6));
 #pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            const int jt = (wave >> 2) + 2 * jj;
-            if (jt > (it | 1)) break;
-            f32x4 p = {0.f, 0.f, 0.f, 0.f};
-            if (jt <= it) {
+        for (int x = 0; x < 4; ++x)
 #pragma unroll
-              for (int x = 0; x < 4; ++x)
-                p = mfma16x16x32(lds_bf16x8(sk + 16 * jt * kHeadDim, at ^ (x << 6)), qf[x], p);
-            }
-            bf16x4 w;
+          for (int it = 0; it < 4; ++it) qf[it][x] = lds_bf16x8(tq + 16 * it * kHeadDim, at ^ (x << 6));
+        bf16x8 qp_f[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[i] * mult[jj][i]);
-            *reinterpret_cast<bf16x4 *>(sp + (pt ^ (jj << 6)) / 2) = w;
-          }
+        for (int x = 0; x < 4; ++x) qp_f[x] = lds_bf16x8(tq + 16 * it_p * kHeadDim, at ^ (x << 6));
+        if (it_p >= 2)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            kf[1][x] = lds_bf16x8(tk + 16 * (jt_p + 2) * kHeadDim, at ^ (x << 6));
+        if (h == h0) read_v(vf, tv);
+        q_buf ^= 1;
+        if (!last) {
+          load(lds_q + q_buf * kTile * 2, qp + (h + 1) * kHeadDim, q_off, q_stride, left + kChunk);
+        } else if (more) {
+          load(lds_q + q_buf * kTile * 2, qp + q_chunk + h0 * kHeadDim, q_off, q_stride, left);
         }
-        if (h == h0) read_v(vf, sv);
-        if (last && (kMode == kWhole || c + 1 < chunks)) {
+        keep_order();
+        f32x4 acc[4], p[2];
+#pragma unroll
+        for (int it = 0; it < 4; ++it) acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
+        p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          p[0] = mfma16x16x32(kf[0][x], qp_f[x], p[0]);
+#pragma unroll
+          for (int it = 0; it < 4; ++it) acc[it] = mfma16x16x32(sb[x], qf[it][x], acc[it]);
+        }
+        if (it_p >= 2)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) p[1] = mfma16x16x32(kf[1][x], qp_f[x], p[1]);
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) {
+          if (jj == 1 && it_p < 2) break;
+          bf16x4 w;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i]);
+          *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(sp) + (pt ^ (jj << 6))) = w;
+        }
+#pragma unroll
+        for (int it = 0; it < 4; ++it) acc[it] *= power[16 * it + r + 1];
+        if (h == h0) load_k();
+        if (last && (kMode == kWhole || more)) {
           // the product of the chunks' decays as they were rounded is kept at l^tokens: what
           // one rounding adds, the next chunk's takes off
           const double exact = decays[n];
           const float decay = (float)(exact * drift);
           if (kMode == kWhole && exact > 1e-30) drift = exact * drift / decay;
-          update(vf, sk, n, decay, 1.f);
+          update(vf, tk, n, decay, 1.f);
         }
+        if (h == h0) load_v();
         __syncthreads();
-        if (c + 1 < chunks) {
-          if (h == h0) load(lds_v, a.v, c + 1, a.hkv, g, kv_off, kv_stride);
-          if (last) load(lds_k, a.k, c + 1, a.hkv, g, kv_off, kv_stride);
-        }
-        const int at = fresh(at_row), pt = fresh(at_score);
-        uint16_t *const o_row = a.out + ((tok0 + c * kChunk) * a.hq + g * group + h) * kHeadDim;
+        const int st = fresh(at_score);
+        bf16x8 pf[4][2];
+#pragma unroll
+        for (int it = 0; it < 4; ++it)
+#pragma unroll
+          for (int x = 0; x <= it / 2; ++x) pf[it][x] = lds_bf16x8(sp + 16 * it * kChunk, st ^ (x << 6));
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int it = 2 * x; it < 4; ++it) acc[it] = mfma16x16x32(vf[x], pf[it][x], acc[it]);
+        uint16_t *const o_row = op + h * kHeadDim;
         const uint32_t o_at = __umul24(r, a.hq * kHeadDim) + 16 * wave + 4 * quad;
-        // a full chunk's four token tiles have no branch between them, so that their reads
-        // and products interleave
-        auto outputs = [&](auto full) {
-#pragma unroll
-          for (int it = 0; it < 4; ++it) {
-            if (!full && 16 * it >= n) break;
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-              acc = mfma16x16x32(sb[x], lds_bf16x8(tq + 16 * it * kHeadDim, at ^ (x << 6)), acc);
-            acc *= power[16 * it + r + 1];
-#pragma unroll
-            for (int x = 0; x <= it / 2; ++x)
-              acc = mfma16x16x32(vf[x], lds_bf16x8(sp + 16 * it * kChunk, pt ^ (x << 6)), acc);
-            if (full || 16 * it + r < n)
-              *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
-                  __builtin_convertvector(acc, bf16x4);
-          }
-        };
         if (n == kChunk) {
-          outputs(std::true_type());
+#pragma unroll
+          for (int it = 0; it < 4; ++it)
+            *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
+                __builtin_convertvector(acc[it], bf16x4);
         } else {
-          outputs(std::false_type());
+#pragma unroll
+          for (int it = 0; it < 4; ++it)
+            if (16 * it + r < n)
+              *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
+                  __builtin_convertvector(acc[it], bf16x4);
         }
       }
+      qp += q_chunk;
+      op += q_chunk;
     }
   }
   if (kMode != kOutputs) {
