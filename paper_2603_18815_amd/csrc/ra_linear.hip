@@ -97,6 +97,7 @@ __global__ __launch_bounds__(kThreads) void linear_decode_kernel(
 // ---- append: LDS tiles ----------------------------------------------------------------
 constexpr int kAppendThreads = 512;
 constexpr int kTile = kChunk * kHeadDim;
+constexpr int kComputeUnits = 256;
 
 // A tile holds 64 tokens of 128 bf16 in 16-byte units, unit u of row x at u ^ swizzle(x):
 // 16 rows at one unit, and four neighbouring rows at four neighbouring units, fall on
@@ -171,7 +172,6 @@ __device__ __forceinline__ int fresh(int x) {
   return x;
 }
 
-enum { kWhole, kStates, kOutputs };
 
 // One stretch of a (row, KV head): chunks in order, the state in the accumulators. Wave w
 // of 8 holds the 16 value dims from 16 w, all 128 key dims: tile t = 2 x + y has key dims
@@ -186,28 +186,31 @@ enum { kWhole, kStates, kOutputs };
 // (outputs, while the next chunk's K and V load; V's tile is free once the first head
 // has its operands, K's after the update). Q has two tiles. 73 KB of LDS and 128 registers:
 // two workgroups per CU, whose steps overlap.
-template <int kMode>
-__global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void linear_chunk_kernel(LinearArgs a) {
+template <bool kStates>
+__global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_kernel(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
-  int unit = blockIdx.x;
-  const int split = kMode == kStates ? 0 : unit % a.head_splits;
-  if (kMode != kStates) unit /= a.head_splits;
-  const int seg = kMode == kWhole ? 0 : unit % a.segments;
-  if (kMode != kWhole) unit /= a.segments;
+  // the outputs pass starts with what the states pass read last, and may still be cached
+  int unit = kStates ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
+  const int split = kStates ? 0 : unit % a.head_splits;
+  if (!kStates) unit /= a.head_splits;
+  const int seg = unit % a.segments;
+  unit /= a.segments;
   const int g = unit % a.hkv, b = unit / a.hkv, group = a.hq / a.hkv;
 
   const int row0 = min(max(a.cu_q[b], 0), a.total_q);
   const int T = min(min(max(a.cu_q[b + 1], row0), a.total_q) - row0, a.max_q_len);
-  const int from = kMode == kWhole ? 0 : seg * a.segment_len;
+  const int from = seg * a.segment_len;
   if (from >= T) return;
-  const int len = kMode == kWhole ? T : min(T - from, a.segment_len);
+  const int len = min(T - from, a.segment_len);
+  const bool whole = T <= a.segment_len;    // an uncut row keeps its own state
+  if (kStates && whole) return;
   const int h0 = group * split / a.head_splits, h1 = group * (split + 1) / a.head_splits;
   const int64_t tok0 = row0 + from;
   const int slot = a.slots[b];
   if (slot < 0 || slot >= a.num_slots) {
-    if (kMode != kStates)
+    if (!kStates)
       for (int t = 0; t < len; ++t)
         for (int i = tid; i < (h1 - h0) * kHeadDim; i += kAppendThreads)
           a.out[((tok0 + t) * a.hq + g * group + h0) * kHeadDim + i] = 0;
@@ -215,8 +218,8 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
   }
 
   __shared__ __align__(1024) uint16_t sk[2 * kTile], sv[2 * kTile];
-  __shared__ __align__(1024) uint16_t sq[kMode == kStates ? 8 : 2 * kTile];
-  __shared__ __align__(1024) uint16_t sp[kMode == kStates ? 8 : kChunk * kChunk];
+  __shared__ __align__(1024) uint16_t sq[kStates ? 8 : 2 * kTile];
+  __shared__ __align__(1024) uint16_t sp[kStates ? 8 : kChunk * kChunk];
   // l^n; scale l^n; l^(63 - j), then zeros
   __shared__ float power[kChunk + 1], weight[2 * kChunk];
   __shared__ double decays[kChunk + 1];
@@ -262,14 +265,13 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
   uint16_t *op = a.out + q_first;
   load(lds_k, kp, kv_off, kv_stride, len - 1);
   load(lds_v, vp, kv_off, kv_stride, len - 1);
-  if (kMode != kStates) load(lds_q, qp + h0 * kHeadDim, q_off, q_stride, len - 1);
+  if (!kStates) load(lds_q, qp + h0 * kHeadDim, q_off, q_stride, len - 1);
 
   // state tile t = 2 x + y, register i: key dim 32 x + 8 quad + 4 y + i, value dim 16 wave + r
   f32x4 s[8];
   float *pool = a.states + ((int64_t)slot * a.hkv + g) * kStateSize;
-  float *carry = kMode == kWhole ? pool
-                                 : a.carry + (((int64_t)b * a.hkv + g) * a.segments + seg) * kStateSize;
-  const bool zero = kMode == kStates || (kMode == kWhole && a.ctx_lens[b] <= 0);
+  float *carry = whole ? pool : a.carry + (((int64_t)b * a.hkv + g) * a.segments + seg) * kStateSize;
+  const bool zero = kStates || (whole && a.ctx_lens[b] <= 0);
   float *const s_at = carry + 8 * quad * kHeadDim + 16 * wave + r;
 #pragma unroll
   for (int t = 0; t < 8; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -296,17 +298,18 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
     for (int x = 0; x < 2; ++x) vf[x] = read_transposed(tile + 32 * x * kHeadDim, at_v);
   };
   // S' = decay S + K^T (after l^(n-1-j) V), n the chunk's tokens: the decayed values in
-  // three bf16 parts, which hold all 24 bits (the outputs pass needs the state as bf16
+  // three bf16 parts, which hold all 24 bits (a stretch of a cut row needs the state as bf16
   // operands only: one part). The states pass has no state to decay: its weights reach to
   // the end of the stretch (after = l^tokens behind the chunk).
-  auto update = [&](const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay, float after) {
+  auto update = [&](auto parts, const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay,
+                    float after) {
+    constexpr int kParts = decltype(parts)::value;
     const int at = fresh(at_k);
-    if (kMode != kStates) {
+    if (!kStates) {
 #pragma unroll
       for (int t = 0; t < 8; ++t) s[t] *= decay;
     }
     // K's operands are read a pair of tiles ahead of the products
-    constexpr int kParts = kMode == kOutputs ? 1 : 3;
     bf16x8 kf[2][2];
     auto read_pair = [&](int i) {
 #pragma unroll
@@ -321,7 +324,7 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float w = weight[kChunk - n + 32 * x + 8 * quad + e];
-        y[e] *= kMode == kStates ? w * after : w;
+        y[e] *= kStates ? w * after : w;
       }
       if (kParts == 1) part[0] = to_bf16x8(y);
 #pragma unroll
@@ -371,13 +374,14 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
     auto load_v = [&]() {
       if (more) load(lds_v + (buf ^ 1) * kTile * 2, vp, kv_off, kv_stride, left);
     };
-    if constexpr (kMode == kStates) {
+    if constexpr (kStates) {
       await_loads();
       __syncthreads();
       load_k();
       load_v();
       read_v(vf, tv);
-      update(vf, tk, n, 1.f, __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
+      update(std::integral_constant<int, 3>(), vf, tk, n, 1.f,
+             __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
     } else {
       bf16x8 sb[4];                                     // the state before the chunk, in bf16
 #pragma unroll
@@ -444,13 +448,15 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
 #pragma unroll
         for (int it = 0; it < 4; ++it) acc[it] *= power[16 * it + r + 1];
         if (h == h0) load_k();
-        if (last && (kMode == kWhole || more)) {
+        if (last && whole) {
           // the product of the chunks' decays as they were rounded is kept at l^tokens: what
           // one rounding adds, the next chunk's takes off
           const double exact = decays[n];
           const float decay = (float)(exact * drift);
-          if (kMode == kWhole && exact > 1e-30) drift = exact * drift / decay;
-          update(vf, tk, n, decay, 1.f);
+          if (exact > 1e-30) drift = exact * drift / decay;
+          update(std::integral_constant<int, 3>(), vf, tk, n, decay, 1.f);
+        } else if (last && more) {
+          update(std::integral_constant<int, 1>(), vf, tk, n, (float)decays[kChunk], 1.f);
         }
         if (h == h0) load_v();
         __syncthreads();
@@ -483,7 +489,7 @@ __global__ __launch_bounds__(kAppendThreads, kMode == kStates ? 4 : 2) void line
       op += q_chunk;
     }
   }
-  if (kMode != kOutputs) {
+  if (kStates || whole) {
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
@@ -499,7 +505,7 @@ __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
   const int row0 = min(max(a.cu_q[b], 0), a.total_q);
   const int T = min(min(max(a.cu_q[b + 1], row0), a.total_q) - row0, a.max_q_len);
   const int slot = a.slots[b];
-  if (T == 0 || slot < 0 || slot >= a.num_slots) return;
+  if (T <= a.segment_len || slot < 0 || slot >= a.num_slots) return;
   const int at = (blockIdx.x * kThreads + threadIdx.x) * 4;
   float *pool = a.states + ((int64_t)slot * a.hkv + g) * kStateSize + at;
   float *carry = a.carry + ((int64_t)b * a.hkv + g) * a.segments * kStateSize + at;
@@ -523,15 +529,15 @@ struct LinearPlan {
   int32_t segments, segment_len, head_splits;
 };
 LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int32_t max_q_len) {
+  // a workgroup's even share of the call's chunks; a longest row up to twice as long is
+  // left whole
+  const int64_t chunks = ((int64_t)max_q_len + kChunk - 1) / kChunk;
+  const int64_t share = ((int64_t)total_q * hkv / kComputeUnits + kChunk - 1) / kChunk;
   LinearPlan p = {1, max_q_len, 1};
-  const int64_t pairs = (int64_t)B * hkv;
-  const int32_t chunks = (max_q_len + kChunk - 1) / kChunk;
-  if (pairs < 512 && chunks >= 8) {
-    const int32_t want = (int32_t)((512 + pairs - 1) / pairs);
-    int32_t per = (chunks + want - 1) / want;
-    if (per < 4) per = 4;
-    p.segment_len = per * kChunk;
-    p.segments = (chunks + per - 1) / per;
+  if (chunks > 2 * share && chunks > 1) {
+    const int64_t per = share < 1 ? 1 : share;
+    p.segment_len = (int32_t)(per * kChunk);
+    p.segments = (int32_t)((chunks + per - 1) / per);
   }
   return p;
 }
@@ -565,16 +571,14 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
                   static_cast<float *>(workspace), num_slots, B, hq, hkv, total_q, max_q_len,
                   p.segments, p.segment_len, p.head_splits, scale};
   const unsigned pairs = (unsigned)B * (unsigned)hkv;
-  if (p.segments == 1) {
-    hipLaunchKernelGGL(linear_chunk_kernel<kWhole>, dim3(pairs), dim3(kAppendThreads), 0, stream, a);
-  } else {
-    hipLaunchKernelGGL(linear_chunk_kernel<kStates>, dim3(pairs * p.segments), dim3(kAppendThreads), 0,
+  if (p.segments > 1) {
+    hipLaunchKernelGGL(linear_chunk_kernel<true>, dim3(pairs * p.segments), dim3(kAppendThreads), 0,
                        stream, a);
     hipLaunchKernelGGL(linear_scan_kernel, dim3(kStateSize / (4 * kThreads), pairs),
                        dim3(kThreads), 0, stream, a);
-    hipLaunchKernelGGL(linear_chunk_kernel<kOutputs>, dim3(pairs * p.segments * p.head_splits),
-                       dim3(kAppendThreads), 0, stream, a);
   }
+  hipLaunchKernelGGL(linear_chunk_kernel<false>, dim3(pairs * p.segments * p.head_splits),
+                     dim3(kAppendThreads), 0, stream, a);
   return hipGetLastError();
 }
 
