@@ -8,18 +8,20 @@
 // V <= 2^19. The other sums are taken in a fixed order.
 //
 // All filters keep a prefix of the order (logit descending, index ascending), so what is
-// sought is where it ends. Rows are cut into chunks, a workgroup each, in three passes, and
-// a workgroup per row ends the call:
-//   stats   each chunk's largest and smallest logit, and its sum of weights below its own
-//           largest one (rows without filters, or with top-p alone)
-//   bins    counts and weights by (M - z) / T in 512 bins over the range that can hold the
-//           end (rows with top-k or top-p)
-//   border  from the bins: the bin or bins that hold the end. What lies above is kept:
-//           each chunk sums it; the elements in them are listed
-//   pick    the listed elements sorted, the end found, the chunk of the drawn token from
-//           the chunks' sums, the token from the chunk's elements
-// Bound by the first pass's read of the logits (the others find them in the caches) and,
-// for few rows, by the launches. Without filters stats and pick are the whole call.
+// sought is where it ends. Rows are cut into chunks, a workgroup each, and the call runs:
+//   stats   each chunk's and each of its threads' largest logit, the chunk's smallest, and
+//           its sum of weights (rows without filters, or with top-p alone)
+//   range   a workgroup a row: how far below M the end can lie. Top-k: the k-th of the
+//           threads' largest logits is no larger than the k-th logit. Top-p: elements below
+//           (1 - p) sum / V weigh less than (1 - p) sum together.
+//   bins    counts and weights of the elements in the range, in 512 bins of it
+//   border  the bin or bins that hold the end. What lies above is kept: each chunk sums it;
+//           the elements in them are listed
+//   pick    a workgroup a row: the listed elements sorted, the end found, the chunk of the
+//           drawn token from the chunks' sums, the token from the chunk's elements
+// Bound by the first pass's read of the logits and, for few rows, by the launches: bins and
+// border read only what the threads' largest logits put into the range. Without filters
+// stats and pick are the whole call; with min-p alone there are no bins.
 #include "ra_device.h"
 #include "ra_internal.h"
 
@@ -28,6 +30,7 @@ namespace {
 
 constexpr int kThreads = 256;           // of a chunk's workgroup
 constexpr int kPickThreads = 1024;
+constexpr int kRowThreads = 1024;       // of a row's range
 constexpr int kBins = 512;
 constexpr int kMaxChunks = 256;         // of a row
 constexpr int kMaxSorted = 4096;        // listed elements that the pick sorts
@@ -82,6 +85,36 @@ __device__ __forceinline__ double scaled(float z, float top, double inv_t) {
 }
 __device__ __forceinline__ uint64_t units(double e) { return (uint64_t)(e * kUnit + 0.5); }
 
+// The same for many elements: exp(d inv_t), d <= 0, as 2^(j / 128) by table times the rest of
+// the exponent, at most ln 2 / 256, by the Taylor series to r^4, whose next term is below
+// 2^-49. No branch: NaN and what lies below -64 count as 2^-92. The constants are held in
+// scalar registers, where an addend costs no move.
+constexpr int kExpTable = 128;
+constexpr double kStep = 0.6931471805599453 / kExpTable;
+struct TableExp {
+  const double *table;
+  double scale, low, round, c1, c2, c3, c4;
+  __device__ __forceinline__ TableExp(const double *t, double inv_t)
+      : table(t), scale(inv_t * (1.4426950408889634 * kExpTable)),
+        low(-64.0 * (1.4426950408889634 * kExpTable)), round(0x1.8p52), c1(kStep),
+        c2(kStep * kStep / 2.0), c3(kStep * kStep * kStep / 6.0),
+        c4(kStep * kStep * kStep * kStep / 24.0) {
+    asm volatile("" : "+s"(low), "+s"(round), "+s"(c1), "+s"(c2), "+s"(c3), "+v"(c4));
+  }
+  __device__ __forceinline__ double operator()(double d) const {
+    // adding `round` rounds to whole numbers, in the low bits
+    const double y = fmax(d * scale, low), t = y + round, f = y - (t - round);
+    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+    double p = __builtin_fma(c4, f, c3);
+    p = __builtin_fma(p, f, c2);
+    p = __builtin_fma(p, f, c1);
+    const uint64_t pow2 = __builtin_bit_cast(uint64_t, table[n & (kExpTable - 1)]) +
+                          ((uint64_t)(uint32_t)(n >> 7 << 20) << 32);
+    const double e = __builtin_bit_cast(double, pow2);
+    return __builtin_fma(e, p * f, e);
+  }
+};
+
 struct SampleArgs {
   const void *logits;
   const float *temperature;
@@ -93,6 +126,7 @@ struct SampleArgs {
   int32_t N, V, chunks, per;            // elements of a chunk: kThreads * per
   // workspace
   float *c_top, *c_low;                 // [N][chunks] largest and smallest finite logit
+  float *t_top;                         // [N][chunks][kThreads] largest of a thread's
   uint32_t *c_first;                    // [N][chunks] lowest index of the largest one
   double *c_sum;                        // [N][chunks] sum of weights against c_top
   uint64_t *bin_mass;                   // [N][kBins]
@@ -101,7 +135,7 @@ struct SampleArgs {
   uint32_t *c_listed;                   // [N][chunks] elements in the border's bins
   uint32_t *c_keys;                     // [N][chunks][2] their largest and smallest key
   uint64_t *list;                       // [N][chunks][per * 8] key << 32 | ~index
-  struct Border *border;                // [N]
+  struct Border *border, *ends;         // [N] with the range; with the end's bins too
 };
 __host__ __device__ constexpr int list_cap(int per) { return per * 8; }
 
@@ -225,97 +259,134 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
   __shared__ float part[kThreads / kWave];
   __shared__ double dpart[kThreads / kWave];
   __shared__ int ipart[kThreads / kWave];
+  __shared__ double table[kExpTable];
   float z[kPer];
   load_chunk<T, kPer>(a, n, c, z);
   const Row row(a, n);
-  float top = z[0], low = __builtin_inff();
+  if (row.needs_sums() && tid < kExpTable)   // reaches the others by the next barrier
+    table[tid] = 2.0 * weight_exp((tid - kExpTable) * kStep);
+  float mine = z[0], low = __builtin_inff();
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    top = fmaxf(top, z[i]);
-    low = z[i] > -__builtin_inff() ? fminf(low, z[i]) : low;
-  }
-  top = group_reduce<kThreads>(top, max_of, part);
+  for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, z[i]);
+  const float top = group_reduce<kThreads>(mine, max_of, part);
   const int64_t at = (int64_t)n * a.chunks + c;
+  if (tid == 0) a.c_top[at] = top;
   if (row.greedy) {
     int first = a.V;
 #pragma unroll
     for (int i = kPer - 1; i >= 0; --i) first = z[i] == top ? index_of<T, kPer>(c, i) : first;
     first = group_reduce<kThreads>(first, [](int x, int y) { return min(x, y); }, ipart);
     if (tid == 0) a.c_first[at] = first;
-  } else if (row.binned()) {
+    return;
+  }
+  if (row.filtered()) a.t_top[at * kThreads + tid] = mine;
+  if (row.binned()) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) low = z[i] > -__builtin_inff() ? fminf(low, z[i]) : low;
     low = group_reduce<kThreads>(low, min_of, part);
     if (tid == 0) a.c_low[at] = low;
-    // the row's bins start at zero
-    for (int i = c * kThreads + tid; i < kBins; i += a.chunks * kThreads) {
-      a.bin_mass[(int64_t)n * kBins + i] = 0;
-      a.bin_count[(int64_t)n * kBins + i] = 0;
-    }
   }
   if (row.needs_sums()) {
     double sum = 0.0;
-    if (top > -__builtin_inff())
+    if (top > -__builtin_inff()) {
+      const TableExp weight(table, row.inv_t);
+      const bool infinite = top == __builtin_inff();   // those at it share the weight
+      const double from = infinite ? 0.0 : (double)top;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) sum += weight_exp(scaled(z[i], top, row.inv_t));
+      for (int i = 0; i < kPer; ++i) {
+        if (infinite) z[i] = z[i] == top ? 0.f : -__builtin_inff();
+        sum += weight((double)z[i] - from);
+      }
+    }
     sum = group_reduce<kThreads>(sum, [](double x, double y) { return x + y; }, dpart);
     if (tid == 0) a.c_sum[at] = sum;
   }
-  if (tid == 0) a.c_top[at] = top;
 }
 
-// The row's largest logit, from its chunks'.
-template <int kN>
-__device__ __forceinline__ float row_top(const SampleArgs &a, int n, float *part) {
+// Thresholds of rows with filters; the rows' bins start at zero.
+__global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a) {
+  const int n = blockIdx.x, tid = threadIdx.x;
+  const Row row(a, n);
+  if (!row.filtered()) return;
+  __shared__ float part[kRowThreads / kWave];
+  __shared__ double dpart[kRowThreads / kWave];
+  __shared__ uint32_t cpart[kRowThreads / kWave];
+  __shared__ uint32_t count[kBins];
+  __shared__ int s_bin;
   const int64_t at = (int64_t)n * a.chunks;
-  const float x = threadIdx.x < a.chunks ? a.c_top[at + threadIdx.x] : -__builtin_inff();
-  return group_reduce<kN>(x, max_of, part);
-}
-
-// The bins' range and, for top-p alone, the sum of all weights.
-__device__ __forceinline__ void row_range(const SampleArgs &a, int n, const Row &row, Border &b,
-                                          float *part, double *dpart) {
-  const int64_t at = (int64_t)n * a.chunks;
-  const int tid = threadIdx.x;
+  const bool have = tid < a.chunks;
+  const float c_top = have ? a.c_top[at + tid] : -__builtin_inff();
+  Border b = Border();
   b.inv_t = row.inv_t;
-  b.top = row_top<kThreads>(a, n, part);
-  const float low = group_reduce<kThreads>(tid < a.chunks ? a.c_low[at + tid] : __builtin_inff(),
-                                           min_of, part);
-  double range = fmin(kRange, -scaled(fminf(low, b.top), b.top, row.inv_t));
-  b.sum = 0.0;
-  if (row.needs_sums()) {
-    double x = 0.0;
-    if (tid < a.chunks)
-      x = a.c_sum[at + tid] * weight_exp(scaled(a.c_top[at + tid], b.top, row.inv_t));
-    b.sum = group_reduce<kThreads>(x, [](double u, double v) { return u + v; }, dpart);
-    // elements lighter than (1 - p) sum / V weigh less than (1 - p) sum together: the end
-    // lies before them
-    if (row.p > 0.0) range = fmin(range, log((double)a.V / ((1.0 - row.p) * b.sum)) + 1e-3);
+  b.top = group_reduce<kRowThreads>(c_top, max_of, part);
+  double range = kRange;
+  if (row.binned()) {
+    if (tid < kBins) {
+      count[tid] = 0;
+      a.bin_mass[(int64_t)n * kBins + tid] = 0;
+      a.bin_count[(int64_t)n * kBins + tid] = 0;
+    }
+    if (tid == 0) s_bin = kBins;
+    const float low = group_reduce<kRowThreads>(have ? a.c_low[at + tid] : __builtin_inff(), min_of, part);
+    range = fmin(range, -scaled(fminf(low, b.top), b.top, row.inv_t));
+    if (row.k > 0) {
+      // the k-th of the threads' largest logits, as far as a bin tells
+      const double scale = kBins / (fmax(range, 1e-30) * (1.0 + 1e-9));
+      const int parts = a.chunks * kThreads;
+      for (int i = tid; i < parts; i += kRowThreads) {
+        const int bin = bin_of(scaled(a.t_top[at * kThreads + i], b.top, row.inv_t), scale);
+        if (bin < kBins) atomicAdd(&count[bin], 1u);
+      }
+      __syncthreads();
+      const uint32_t own = tid < kBins ? count[tid] : 0;
+      uint32_t all;
+      const uint32_t before = group_scan<kRowThreads>(own, all, cpart);
+      if (before < (uint32_t)row.k && before + own >= (uint32_t)row.k) s_bin = tid;
+      __syncthreads();
+      if (s_bin < kBins) range = fmin(range, (s_bin + 1) / scale * (1.0 + 1e-9));
+    } else {
+      const double x = have ? a.c_sum[at + tid] * weight_exp(scaled(c_top, b.top, row.inv_t)) : 0.0;
+      b.sum = group_reduce<kRowThreads>(x, [](double u, double v) { return u + v; }, dpart);
+      if (row.p > 0.0) range = fmin(range, log((double)a.V / ((1.0 - row.p) * b.sum)) + 1e-3);
+    }
+  } else {
+    range = fmin(range, -log(row.m) + 1e-12);
   }
   // the last element falls into the last bin
   b.bin_scale = kBins / (fmax(range, 1e-30) * (1.0 + 1e-9));
+  if (tid == 0) a.border[n] = b;
+}
+
+// Whether a logit is in the row's range.
+__device__ __forceinline__ bool in_range(const Border &b, float z) {
+  return bin_of(scaled(z, b.top, b.inv_t), b.bin_scale) < kBins;
 }
 
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   const int n = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+  const int64_t at = (int64_t)n * a.chunks + c;
+  const float c_top = a.c_top[at];
   const Row row(a, n);
   if (!row.binned()) return;
-  __shared__ float part[kThreads / kWave];
-  __shared__ double dpart[kThreads / kWave];
+  const Border b = a.border[n];
+  if (b.top == -__builtin_inff() || !in_range(b, c_top)) return;
   __shared__ uint64_t mass[kBins];
   __shared__ uint32_t count[kBins];
-  float z[kPer];
-  load_chunk<T, kPer>(a, n, c, z);
   for (int i = tid; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
-  Border b;
-  row_range(a, n, row, b, part, dpart);   // barriers: the bins are clear
-  if (b.top == -__builtin_inff()) return;
+  __syncthreads();
+  if (in_range(b, a.t_top[at * kThreads + tid])) {
+    float z[kPer];
+    load_chunk<T, kPer>(a, n, c, z);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const double x = scaled(z[i], b.top, b.inv_t);
-    const int bin = bin_of(x, b.bin_scale);
-    if (bin < kBins) {
-      if (row.k > 0) atomicAdd(&count[bin], 1u);
-      if (row.p < 1.0) atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)units(weight_exp(x)));
+    for (int i = 0; i < kPer; ++i) {
+      const double x = scaled(z[i], b.top, b.inv_t);
+      const int bin = bin_of(x, b.bin_scale);
+      if (bin < kBins) {
+        if (row.k > 0) atomicAdd(&count[bin], 1u);
+        if (row.p < 1.0)
+          atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)units(weight_exp(x)));
+      }
     }
   }
   __syncthreads();
@@ -326,477 +397,632 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   }
 }
 
-// The end's bins, from the row's bins.
-__device__ __forceinline__ void find_border(const SampleArgs &a, int n, const Row &row, Border &b,
-                                            uint64_t *mpart, uint32_t *cpart, Border *shared) {
-  static_assert(kBins == 2 * kThreads, "two bins a thread");
-  const int tid = threadIdx.x;
-  const int64_t at = (int64_t)n * kBins + 2 * tid;
-  uint64_t m0 = a.bin_mass[at], m1 = a.bin_mass[at + 1], mass_all;
-  uint32_t c0 = a.bin_count[at], c1 = a.bin_count[at + 1], count_all;
-  const uint64_t mass_before = group_scan<kThreads>(m0 + m1, mass_all, mpart);
-  const uint32_t count_before = group_scan<kThreads>(c0 + c1, count_all, cpart);
-  if (tid == 0) {
-    shared->lo = shared->hi = shared->bin_k = kBins;
-    shared->count_lo = shared->count_k = 0;
-    shared->mass_lo = shared->mass_k = mass_all;
-    shared->mass_all = mass_all;
-  }
-  __syncthreads();
-  // bin_k: where the count reaches k
-  if (row.k > 0) {
-    const uint32_t k = (uint32_t)row.k;
-    if (count_before < k && count_before + c0 + c1 >= k) {
-      const bool second = count_before + c0 < k;
-      shared->bin_k = 2 * tid + second;
-      shared->count_k = count_before + (second ? c0 : 0);
-      shared->mass_k = mass_before + (second ? m0 : 0);
-      if (!(row.p < 1.0)) {
-        shared->lo = shared->hi = shared->bin_k;
-        shared->count_lo = shared->count_k;
-      }
-    }
-    __syncthreads();
-  }
-  // lo, hi: where the weight reaches p of the least and of the most that top-k can keep
-  if (row.p < 1.0) {
-    const int bin_k = shared->bin_k;
-    double least, most;
-    if (row.k > 0) {
-      least = (double)shared->mass_k;
-      most = least + (bin_k < kBins ? (double)a.bin_mass[(int64_t)n * kBins + bin_k] : 0.0);
-    } else {
-      least = most = b.sum * kUnit;
-    }
-    least = fmax(row.p * least, 0.5);
-    most = fmax(row.p * most, 0.5);
+// Sums over the lanes before this one, and over all.
+template <typename V>
+__device__ __forceinline__ V wave_scan(V x, V &total) {
+  const int lane = threadIdx.x % kWave;
+  V s = x;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint64_t before = mass_before + (i ? m0 : 0), after = before + (i ? m1 : m0);
-      if ((double)before < least && !((double)after < least) && 2 * tid + i <= bin_k) {
-        shared->lo = 2 * tid + i;
-        shared->mass_lo = before;
-        shared->count_lo = count_before + (i ? c0 : 0);
-      }
-      if ((double)before < most && !((double)after < most) && 2 * tid + i <= bin_k)
-        shared->hi = 2 * tid + i;
+  for (int d = 1; d < kWave; d *= 2) {
+    const V y = __shfl_up(s, d);
+    if (lane >= d) s += y;
+  }
+  total = __shfl(s, kWave - 1);
+  return s - x;
+}
+
+// The end's bins, from the row's bins. Every wave finds them by itself: a lane holds eight
+// neighbouring bins, and no barrier is needed.
+__device__ __forceinline__ void find_border(const SampleArgs &a, int n, const Row &row, Border &b) {
+  constexpr int kOwn = kBins / kWave;
+  const int lane = threadIdx.x % kWave;
+  const int64_t at = (int64_t)n * kBins + kOwn * lane;
+  uint64_t m[kOwn], m_own = 0, m_all = 0, m_before = 0;
+  uint32_t c[kOwn], c_own = 0, c_all = 0, c_before = 0;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    m[i] = row.p < 1.0 ? a.bin_mass[at + i] : 0;
+    c[i] = row.k > 0 ? a.bin_count[at + i] : 0;
+    m_own += m[i];
+    c_own += c[i];
+  }
+  if (row.p < 1.0) m_before = wave_scan(m_own, m_all);
+  if (row.k > 0) c_before = wave_scan(c_own, c_all);
+  b.lo = b.hi = b.bin_k = kBins;
+  b.count_lo = b.count_k = 0;
+  b.mass_lo = b.mass_k = b.mass_all = m_all;
+  uint64_t of_bin_k = 0;
+  if (row.k > 0) {
+    // where the count reaches k
+    int bin = kBins;
+    uint32_t count = c_before, c_at = 0;
+    uint64_t mass = m_before, m_at = 0, m_in = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      if (count < (uint32_t)row.k && count + c[i] >= (uint32_t)row.k)
+        bin = kOwn * lane + i, c_at = count, m_at = mass, m_in = m[i];
+      count += c[i];
+      mass += m[i];
     }
-    __syncthreads();
-    // rounding aside the weight reaches it no later than in bin_k
-    if (tid == 0) {
-      if (shared->lo == kBins && bin_k < kBins) {
-        shared->lo = bin_k;
-        shared->mass_lo = shared->mass_k;
-        shared->count_lo = shared->count_k;
-      }
-      if (shared->hi == kBins) shared->hi = bin_k;
+    const uint64_t found = __ballot(bin < kBins);
+    if (found) {
+      const int from = __ffsll((unsigned long long)found) - 1;
+      b.bin_k = __shfl(bin, from);
+      b.count_k = __shfl(c_at, from);
+      b.mass_k = __shfl(m_at, from);
+      of_bin_k = __shfl(m_in, from);
+      b.lo = b.hi = b.bin_k;
+      b.count_lo = b.count_k;
+      b.mass_lo = b.mass_k;
     }
   }
-  __syncthreads();
-  const double inv_t = b.inv_t, bin_scale = b.bin_scale, sum = b.sum;
-  const float top = b.top;
-  b = *shared;
-  b.inv_t = inv_t, b.bin_scale = bin_scale, b.sum = sum, b.top = top;
+  if (row.p < 1.0) {
+    // lo, hi: where the weight reaches p of the least and of the most that top-k can keep; by
+    // rounding alone it might not by bin_k, which then is the end's
+    const double of_k = row.k > 0 ? (double)b.mass_k : b.sum * kUnit;
+    const double least = fmax(row.p * of_k, 0.5);
+    const double most = fmax(row.p * (of_k + (double)of_bin_k), 0.5);
+    int lo = kBins, hi = kBins;
+    uint32_t count = c_before, c_at = 0;
+    uint64_t mass = m_before, m_at = 0;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) {
+      const int bin = kOwn * lane + i;
+      const uint64_t after = mass + m[i];
+      if (bin <= b.bin_k) {
+        if ((double)mass < least && !((double)after < least)) lo = bin, c_at = count, m_at = mass;
+        if ((double)mass < most && !((double)after < most)) hi = bin;
+      }
+      mass = after;
+      count += c[i];
+    }
+    const uint64_t has_lo = __ballot(lo < kBins), has_hi = __ballot(hi < kBins);
+    b.hi = has_hi ? __shfl(hi, __ffsll((unsigned long long)has_hi) - 1) : b.bin_k;
+    if (has_lo) {
+      const int from = __ffsll((unsigned long long)has_lo) - 1;
+      b.lo = __shfl(lo, from);
+      b.count_lo = __shfl(c_at, from);
+      b.mass_lo = __shfl(m_at, from);
+    }
+  }
 }
 
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   const int n = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
+  const int64_t at = (int64_t)n * a.chunks + c;
+  const float c_top = a.c_top[at];
   const Row row(a, n);
   if (!row.filtered()) return;
-  __shared__ float part[kThreads / kWave];
-  __shared__ double dpart[kThreads / kWave];
-  __shared__ uint64_t mpart[kThreads / kWave];
-  __shared__ uint32_t cpart[kThreads / kWave];
-  __shared__ Border shared;
+  Border b = a.border[n];
+  if (b.top == -__builtin_inff()) return;
+  if (!in_range(b, c_top)) {
+    if (tid == 0) a.c_kept[at] = 0, a.c_listed[at] = 0;
+    return;
+  }
   __shared__ uint32_t listed, key_high, key_low;
-  float z[kPer];
-  load_chunk<T, kPer>(a, n, c, z);
-  if (tid == 0) listed = 0, key_high = 0, key_low = 0xffffffffu;
-  Border b;
+  __shared__ uint64_t sure;
+  if (tid == 0) listed = 0, key_high = 0, key_low = 0xffffffffu, sure = 0;
+  const float t_top = a.t_top[at * kThreads + tid];
   if (row.binned()) {
-    row_range(a, n, row, b, part, dpart);
-    find_border(a, n, row, b, mpart, cpart, &shared);
+    find_border(a, n, row, b);
   } else {
-    b = Border();
-    b.inv_t = row.inv_t;
-    b.top = row_top<kThreads>(a, n, part);
     b.lo = b.hi = b.bin_k = kBins;
   }
   __syncthreads();
-  if (b.top == -__builtin_inff()) return;
-  const int64_t at = (int64_t)n * a.chunks + c;
   uint64_t *list = a.list + at * list_cap(kPer);
   uint64_t kept = 0;
+  uint32_t high = 0, low = 0xffffffffu;
+  if (in_range(b, t_top)) {
+    float z[kPer];
+    load_chunk<T, kPer>(a, n, c, z);
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const double x = scaled(z[i], b.top, b.inv_t);
-    if (!(x >= -kRange)) continue;
-    const int bin = row.binned() ? bin_of(x, b.bin_scale) : 0;
-    if (bin < b.lo) {
-      const double e = weight_exp(x);
-      if (e >= row.m) kept += units(e);
-    } else if (bin < kBins && (bin <= b.hi || bin == b.bin_k)) {
-      const uint32_t slot = atomicAdd(&listed, 1u), key = key_of(z[i]);
-      if (slot < (uint32_t)list_cap(kPer))
-        list[slot] = (uint64_t)key << 32 | (uint32_t)~index_of<T, kPer>(c, i);
-      atomicMax(&key_high, key);
-      atomicMin(&key_low, key);
+    for (int i = 0; i < kPer; ++i) {
+      const double x = scaled(z[i], b.top, b.inv_t);
+      const int bin = bin_of(x, b.bin_scale);
+      if (bin < b.lo) {
+        const double e = weight_exp(x);
+        if (e >= row.m) kept += units(e);
+      } else if (bin < kBins && (bin <= b.hi || bin == b.bin_k)) {
+        const uint32_t slot = atomicAdd(&listed, 1u), key = key_of(z[i]);
+        if (slot < (uint32_t)list_cap(kPer))
+          list[slot] = (uint64_t)key << 32 | (uint32_t)~index_of<T, kPer>(c, i);
+        high = key > high ? key : high;
+        low = key < low ? key : low;
+      }
+    }
+    if (kept) atomicAdd((unsigned long long *)&sure, (unsigned long long)kept);
+    if (high) {
+      atomicMax(&key_high, high);
+      atomicMin(&key_low, low);
     }
   }
-  kept = group_reduce<kThreads>(kept, [](uint64_t x, uint64_t y) { return x + y; }, mpart);
+  __syncthreads();
   if (tid == 0) {
-    a.c_kept[at] = kept;
+    a.c_kept[at] = sure;
     a.c_listed[at] = listed;
     a.c_keys[2 * at] = key_high;
     a.c_keys[2 * at + 1] = key_low;
-    if (c == 0) a.border[n] = b;
+    if (c_top == b.top) a.ends[n] = b;    // one of the chunks that hold it: all write the same
   }
 }
 
 // ---- pick -----------------------------------------------------------------------------
+// Neighbouring logits of a thread from index v0 on; -inf past the row.
+template <typename T, int kOwn>
+__device__ __forceinline__ void load_neighbours(const T *row, int v0, int V, float (&z)[kOwn]) {
+  constexpr int kVec = kVector<T>;
+  if (kOwn % kVec == 0 && v0 + kOwn <= V) {
+#pragma unroll
+    for (int j = 0; j < kOwn / kVec; ++j) {
+      const u32x4_any w = *reinterpret_cast<const u32x4_any *>(row + v0 + j * kVec);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        if constexpr (sizeof(T) == 4)
+          z[j * kVec + e] = __uint_as_float(w[e]);
+        else
+          z[j * kVec + e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) z[e] = v0 + e < V ? logit_value(row[v0 + e]) : -__builtin_inff();
+  }
+#pragma unroll
+  for (int e = 0; e < kOwn; ++e) z[e] = clean(z[e]);
+}
+
+// What the pick's waves share.
+struct PickLds {
+  uint64_t sorted[kMaxSorted];          // the listed elements, or 256 bins of a pass
+  uint64_t kept_of[kMaxChunks];         // weight kept of each chunk
+  uint32_t ties_of[kMaxChunks];         // of each chunk: elements at the edge
+  uint64_t mpart[kPickThreads / kWave];
+  double dpart[kPickThreads / kWave];
+  uint32_t cpart[kPickThreads / kWave];
+  uint64_t sum;
+  uint32_t key, count, ties;
+  int token;
+};
+
+// The end of the kept prefix: keys above `key`, and of those at it the first `ties` of the
+// row or, with ties = kByIndex, those up to `index`.
+constexpr uint64_t kByIndex = ~0ull;
+struct Edge {
+  uint32_t key, index;
+  uint64_t ties;
+};
+
+// Sums as functions of what is listed.
+struct Goals {
+  const Row &row;
+  const Border &b;
+  __device__ __forceinline__ double weight(uint32_t key) const {
+    return weight_exp(scaled(value_of(key), b.top, row.inv_t));
+  }
+  __device__ __forceinline__ bool ends_in_k() const { return row.k > 0 && b.bin_k < kBins; }
+  // the weight at which top-p ends, given what top-k keeps of bin_k
+  __device__ __forceinline__ double goal(uint64_t of_bin_k) const {
+    return fmax(row.p * (row.k > 0 ? (double)(b.mass_k + of_bin_k) : b.sum * kUnit), 0.5);
+  }
+  // how many of `avail` elements of weight w, `before` ahead of them, the goal lets in
+  __device__ __forceinline__ uint64_t let_in(double goal, uint64_t before, uint64_t w,
+                                             uint64_t avail) const {
+    if (!((double)before < goal)) return 0;
+    if (w == 0) return avail;
+    const double r = __builtin_ceil((goal - (double)before) / (double)w);
+    return r < 1.0 ? 1 : r >= (double)avail ? avail : (uint64_t)r;
+  }
+  // the rank in the row of the i-th listed element, n_p of them in bins lo .. hi
+  __device__ __forceinline__ uint64_t rank(uint64_t i, int bin, uint64_t n_p) const {
+    return bin == b.bin_k && b.bin_k > b.hi ? b.count_k + (i - n_p) : b.count_lo + i;
+  }
+  __device__ __forceinline__ bool keeps(uint64_t rank, int bin, uint64_t before, double goal) const {
+    return bin <= b.hi && !(ends_in_k() && rank >= (uint64_t)row.k) &&
+           !(row.p < 1.0 && !((double)before < goal));
+  }
+};
+
+// Up to 64 listed elements, by one wave: lane i has one of them in `x` (0: none); adds what
+// is kept to the chunks' sums.
+__device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int chunk_len, PickLds &lds) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int len = 2; len <= kWave; len *= 2)
+#pragma unroll
+    for (int step = len / 2; step > 0; step /= 2) {
+      const uint64_t y = __shfl_xor(x, step);
+      const bool first = (lane & step) == 0, falling = (lane & len) == 0;
+      x = (x < y) == (first == falling) ? y : x;
+    }
+  uint64_t w = 0, all;
+  double e = 0.0;
+  int bin = kBins;
+  if (x) {
+    const double d = scaled(value_of((uint32_t)(x >> 32)), g.b.top, g.row.inv_t);
+    e = weight_exp(d);
+    w = units(e);
+    bin = bin_of(d, g.b.bin_scale);
+  }
+  const uint64_t before = wave_scan(w, all);
+  const uint64_t n_p = __popcll(__ballot(x && bin <= g.b.hi)), rank = g.rank(lane, bin, n_p);
+  const bool of_k = g.ends_in_k() && x && bin == g.b.bin_k && rank < (uint64_t)g.row.k;
+  const uint64_t mass_k = wave_reduce(of_k ? w : (uint64_t)0, [](uint64_t u, uint64_t v) { return u + v; });
+  const double goal = g.row.p < 1.0 ? g.goal(mass_k) : 0.0;
+  const bool kept = x && g.keeps(rank, bin, g.b.mass_lo + before, goal);
+  const uint64_t mask = __ballot(kept);
+  const uint32_t v = ~(uint32_t)x;
+  if (kept && e >= g.row.m)
+    atomicAdd((unsigned long long *)&lds.kept_of[v / chunk_len], (unsigned long long)w);
+  if (!mask) return {0xffffffffu, 0, kByIndex};
+  const uint64_t last = __shfl(x, __popcll(mask) - 1);
+  return {(uint32_t)(last >> 32), ~(uint32_t)last, kByIndex};
+}
+
+// Up to kMaxSorted listed elements, in lds.sorted.
+__device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int chunk_len, PickLds &lds) {
+  const int tid = threadIdx.x;
+  int size = 64;
+  while (size < count) size *= 2;
+  for (int i = count + tid; i < size; i += kPickThreads) lds.sorted[i] = 0;
+  __syncthreads();
+  for (int len = 2; len <= size; len *= 2)
+    for (int step = len / 2; step > 0; step /= 2) {
+      for (int i = tid; i < size / 2; i += kPickThreads) {
+        const int lo = i / step * 2 * step + i % step, hi = lo + step;
+        const uint64_t x = lds.sorted[lo], y = lds.sorted[hi];
+        if ((x < y) == ((lo & len) == 0)) lds.sorted[lo] = y, lds.sorted[hi] = x;
+      }
+      __syncthreads();
+    }
+  // four neighbouring elements a thread: their weights, and the sums before them
+  constexpr int kOwn = kMaxSorted / kPickThreads;
+  auto add = [](uint64_t x, uint64_t y) { return x + y; };
+  uint64_t w[kOwn], own = 0, of_k = 0, in_p = 0, all;
+  int bin[kOwn];
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    const int i = tid * kOwn + j;
+    w[j] = 0, bin[j] = kBins;
+    if (i < count) {
+      const double x = scaled(value_of((uint32_t)(lds.sorted[i] >> 32)), g.b.top, g.row.inv_t);
+      w[j] = units(weight_exp(x));
+      bin[j] = bin_of(x, g.b.bin_scale);
+      in_p += bin[j] <= g.b.hi;
+    }
+    own += w[j];
+  }
+  uint64_t run = group_scan<kPickThreads>(own, all, lds.mpart);
+  const uint64_t n_p = group_reduce<kPickThreads>(in_p, add, lds.mpart);
+  if (g.ends_in_k() && g.row.p < 1.0) {
+#pragma unroll
+    for (int j = 0; j < kOwn; ++j)
+      if (bin[j] == g.b.bin_k && g.rank(tid * kOwn + j, bin[j], n_p) < (uint64_t)g.row.k) of_k += w[j];
+    of_k = group_reduce<kPickThreads>(of_k, add, lds.mpart);
+  }
+  const double goal = g.row.p < 1.0 ? g.goal(of_k) : 0.0;
+  if (tid == 0) lds.count = 0;
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kOwn; ++j) {
+    const int i = tid * kOwn + j;
+    if (i < count && g.keeps(g.rank(i, bin[j], n_p), bin[j], g.b.mass_lo + run, goal)) {
+      atomicMax(&lds.count, (uint32_t)i + 1);         // kept: a prefix of the sorted elements
+      const uint32_t v = ~(uint32_t)lds.sorted[i];
+      if (g.weight((uint32_t)(lds.sorted[i] >> 32)) >= g.row.m)
+        atomicAdd((unsigned long long *)&lds.kept_of[v / chunk_len], (unsigned long long)w[j]);
+    }
+    run += w[j];
+  }
+  __syncthreads();
+  if (lds.count == 0) return {0xffffffffu, 0, kByIndex};
+  const uint64_t last = lds.sorted[lds.count - 1];
+  return {(uint32_t)(last >> 32), ~(uint32_t)last, kByIndex};
+}
+
+// Any number: the edge by eight bits of the key a pass over the row, first that of top-k,
+// then that of top-p among what top-k keeps. The chunks' sums are those of the whole prefix.
 template <typename T>
+__device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goals &g, int chunks,
+                                           int chunk_len, PickLds &lds) {
+  const int tid = threadIdx.x;
+  uint64_t *mass = lds.sorted;
+  uint32_t *counts = reinterpret_cast<uint32_t *>(lds.sorted + 256);
+  auto add = [](uint64_t x, uint64_t y) { return x + y; };
+  auto key_at = [&](int v) { return key_of(clean(logit_value(logits[v]))); };
+  Edge end = {0, 0, ~0ull >> 1};
+  for (int round = 0; round < 2; ++round) {
+    const bool by_mass = round == 1;
+    if (by_mass ? !(g.row.p < 1.0) : !(g.row.k > 0)) continue;
+    double goal = 0.0;
+    if (by_mass) {
+      // the weight that top-k keeps
+      uint64_t sum = 0, equal = 0;
+      for (int v = tid; v < V; v += kPickThreads) {
+        const uint32_t key = key_at(v);
+        if (key > end.key) sum += units(g.weight(key));
+        equal += key == end.key;
+      }
+      sum = group_reduce<kPickThreads>(sum, add, lds.mpart);
+      equal = group_reduce<kPickThreads>(equal, add, lds.mpart);
+      if (end.key) sum += (equal < end.ties ? equal : end.ties) * units(g.weight(end.key));
+      goal = fmax(g.row.p * (g.row.k > 0 ? (double)sum : g.b.sum * kUnit), 0.5);
+    }
+    uint32_t prefix = 0;
+    uint64_t ahead = 0;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+      __syncthreads();
+      if (tid < 256) mass[tid] = 0, counts[tid] = 0;
+      __syncthreads();
+      for (int v = tid; v < V; v += kPickThreads) {
+        const uint32_t key = key_at(v);
+        if (shift < 24 && key >> (shift + 8) != prefix >> (shift + 8)) continue;
+        if (key < end.key) continue;
+        if (by_mass)
+          atomicAdd((unsigned long long *)&mass[key >> shift & 255],
+                    (unsigned long long)units(g.weight(key)));
+        atomicAdd(&counts[key >> shift & 255], 1u);
+      }
+      __syncthreads();
+      if (tid == 0) {
+        uint64_t run = ahead;
+        int i = 255;
+        for (; i > 0; --i) {
+          const uint64_t next = run + (by_mass ? mass[i] : (uint64_t)counts[i]);
+          if (by_mass ? !((double)next < goal) : next >= (uint64_t)g.row.k) break;
+          run = next;
+        }
+        lds.key = prefix | (uint32_t)i << shift;
+        lds.sum = run;
+        lds.ties = counts[i];
+      }
+      __syncthreads();
+      prefix = lds.key;
+      ahead = lds.sum;
+    }
+    uint64_t r = (uint64_t)g.row.k - ahead;
+    if (by_mass) {
+      r = g.let_in(goal, ahead, units(g.weight(prefix)), lds.ties);
+      if (prefix == end.key && r > end.ties) r = end.ties;
+    }
+    end = {prefix, 0, r};
+    __syncthreads();
+  }
+  // each chunk's elements at the edge, then what it keeps, a wave a chunk
+  const int lane = tid % kWave;
+  for (int c = tid / kWave; c < chunks; c += kPickThreads / kWave) {
+    uint32_t equal = 0;
+    const int last = min(V, (c + 1) * chunk_len);
+    for (int v = c * chunk_len + lane; v < last; v += kWave) equal += key_at(v) == end.key;
+    equal = wave_reduce(equal, [](uint32_t x, uint32_t y) { return x + y; });
+    if (lane == 0) lds.ties_of[c] = equal;
+  }
+  __syncthreads();
+  for (int c = tid / kWave; c < chunks; c += kPickThreads / kWave) {
+    uint64_t ahead = 0, sum = 0;
+    for (int i = 0; i < c; ++i) ahead += lds.ties_of[i];
+    const int last = min(V, (c + 1) * chunk_len);
+    for (int v = c * chunk_len + lane; v < last; v += kWave) {
+      const uint32_t key = key_at(v);
+      const double e = g.weight(key);
+      if (key > end.key && e >= g.row.m) sum += units(e);
+    }
+    sum = wave_reduce(sum, add);
+    const uint64_t left = end.ties > ahead ? end.ties - ahead : 0;
+    if (lane == 0) {
+      const double e = g.weight(end.key);
+      lds.kept_of[c] =
+          sum + (e >= g.row.m ? (left < lds.ties_of[c] ? left : lds.ties_of[c]) * units(e) : 0);
+    }
+  }
+  return end;
+}
+
+// The last chunk whose sums begin at or before u of the whole and that weighs anything, from
+// the four chunks a lane holds: found by every wave by itself.
+struct Drawn {
+  int chunk;
+  double before, total;
+};
+template <typename V>
+__device__ __forceinline__ Drawn draw_chunk(const V (&x)[4], float u) {
+  const int lane = threadIdx.x % kWave;
+  V total, run = wave_scan(x[0] + x[1] + x[2] + x[3], total);
+  const double goal = (double)u * (double)total;
+  int chunk = -1;
+  V before = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (x[i] > (V)0 && (double)run <= goal) chunk = 4 * lane + i, before = run;
+    run += x[i];
+  }
+  const uint64_t found = __ballot(chunk >= 0);       // never empty: the first that weighs is in
+  const int from = kWave - 1 - __clzll((long long)found);
+  return {__shfl(chunk, from), (double)__shfl(before, from), (double)total};
+}
+
+template <typename T, int kPer>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
-  const int n = blockIdx.x, tid = threadIdx.x;
+  const int n = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const T *logits = static_cast<const T *>(a.logits) + n * a.row_stride;
-  __shared__ float part[kPickThreads / kWave];
-  __shared__ double dpart[kPickThreads / kWave];
-  __shared__ uint64_t mpart[kPickThreads / kWave];
-  __shared__ uint32_t cpart[kPickThreads / kWave];
-  __shared__ uint64_t sorted[kMaxSorted];        // the listed elements, or 256 bins of a pass
-  __shared__ uint64_t kept_of[kMaxChunks];       // weight kept of each chunk
-  __shared__ uint32_t ties_of[kMaxChunks];       // of each chunk: elements at the edge
-  __shared__ uint64_t s_mass, s_sum;
-  __shared__ uint32_t s_key, s_count, s_ties;
-  __shared__ int s_chunk, s_token;
-  __shared__ double s_before;
+  __shared__ PickLds lds;
+  constexpr int chunk_len = kThreads * kPer;
+  static_assert(kMaxChunks == 4 * kWave, "four chunks a lane");
 
   const Row row(a, n);
-  const int64_t at = (int64_t)n * a.chunks;
-  const float top = row_top<kPickThreads>(a, n, part);
-  if (top == -__builtin_inff()) {
-    if (tid == 0) {
-      a.tokens[n] = -1;
-      if (a.logprob) a.logprob[n] = __builtin_nanf("");
-    }
-    return;
+  const int64_t at = (int64_t)n * a.chunks + 4 * lane;
+  const int mine = a.chunks - 4 * lane;               // of the lane's four chunks: how many are
+  float c_top[4], top = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c_top[i] = i < mine ? a.c_top[at + i] : -__builtin_inff();
+    top = fmaxf(top, c_top[i]);
   }
-  if (row.greedy) {
-    int first = tid < a.chunks && a.c_top[at + tid] == top ? (int)a.c_first[at + tid] : a.V;
-    first = group_reduce<kPickThreads>(first, [](int x, int y) { return min(x, y); }, (int *)cpart);
-    if (tid == 0) {
-      a.tokens[n] = first;
-      if (a.logprob) a.logprob[n] = 0.f;
-    }
-    return;
-  }
+  top = wave_reduce(top, max_of);
   float u = a.uniform[n];
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-  const int chunk_len = kThreads * a.per;
-
-  // the prefix's end: keys above `edge`, and of those at it the first `ties` by index
-  // (tie_index: those up to this index)
-  uint32_t edge = 0, tie_index = 0xffffffffu;
-  uint64_t ties = ~0ull;                          // counted over the row; ~0: by tie_index
-  Border b = Border();
-  double total;
-  if (!row.filtered()) {
-    double x = 0.0;
-    if (tid < a.chunks)
-      x = a.c_sum[at + tid] * weight_exp(scaled(a.c_top[at + tid], top, row.inv_t));
-    const double before = group_scan<kPickThreads>(x, total, dpart);
-    const double goal = (double)u * total;
-    if (tid == 0) s_chunk = -1;
-    __syncthreads();
-    // the last chunk whose sums begin at or before the goal and that weighs anything
-    if (x > 0.0 && before <= goal) atomicMax(&s_chunk, tid);
-    __syncthreads();
-    if (tid == s_chunk) s_before = before;
-    __syncthreads();
-  } else {
-    b = a.border[n];
-    const uint32_t mine = tid < a.chunks ? a.c_listed[at + tid] : 0;
-    const uint32_t high = tid < a.chunks && mine ? a.c_keys[2 * (at + tid)] : 0;
-    const uint32_t low = tid < a.chunks && mine ? a.c_keys[2 * (at + tid) + 1] : 0xffffffffu;
-    const uint32_t cap = list_cap(a.per);
-    uint32_t count;
-    const uint32_t first = group_scan<kPickThreads>(mine, count, cpart);
-    auto umax = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
-    auto umin = [](uint32_t x, uint32_t y) { return x < y ? x : y; };
-    const uint32_t key_high = group_reduce<kPickThreads>(high, umax, cpart);
-    const uint32_t key_low = group_reduce<kPickThreads>(low, umin, cpart);
-    const uint32_t longest = group_reduce<kPickThreads>(mine, umax, cpart);
-    if (tid < kMaxChunks) {
-      kept_of[tid] = tid < a.chunks ? a.c_kept[at + tid] : 0;
-      ties_of[tid] = mine;
+  if (top == -__builtin_inff() || row.greedy) {
+    int first = a.V;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row.greedy && i < mine && c_top[i] == top) first = min(first, (int)a.c_first[at + i]);
+    first = wave_reduce(first, [](int x, int y) { return min(x, y); });
+    if (tid == 0) {
+      const bool none = top == -__builtin_inff();
+      a.tokens[n] = none ? -1 : first;
+      if (a.logprob) a.logprob[n] = none ? __builtin_nanf("") : 0.f;
     }
-    auto weight_of = [&](uint32_t key) { return weight_exp(scaled(value_of(key), top, row.inv_t)); };
-    // the sum that top-p takes its share of, given what bin_k's listed elements add
-    auto goal_of = [&](uint64_t of_bin_k) {
-      const double z = row.k > 0 ? (double)(b.mass_k + of_bin_k) : b.sum * kUnit;
-      return fmax(row.p * z, 0.5);
-    };
-    // the first r of `avail` equal elements of weight w, `before` ahead of them, that the
-    // goal lets in
-    auto ties_in = [](double goal, uint64_t before, uint64_t w, uint64_t avail) -> uint64_t {
-      if (!((double)before < goal)) return 0;
-      if (w == 0) return avail;
-      const double r = __builtin_ceil((goal - (double)before) / (double)w);
-      return r < 1.0 ? 1 : r >= (double)avail ? avail : (uint64_t)r;
-    };
-    __syncthreads();
+    return;
+  }
+
+  Edge end = {0, 0, kByIndex};                        // everything
+  Border b = Border();
+  Drawn drawn;
+  if (!row.filtered()) {
+    double x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      x[i] = i < mine ? a.c_sum[at + i] * weight_exp(scaled(c_top[i], top, row.inv_t)) : 0.0;
+    drawn = draw_chunk(x, u);
+  } else {
+    b = a.ends[n];
+    const Goals g = {row, b};
+    const uint32_t cap = list_cap(kPer);
+    uint32_t listed[4], first[4], count, longest = 0, high = 0, low = 0xffffffffu;
+    uint64_t kept[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      listed[i] = i < mine ? a.c_listed[at + i] : 0;
+      kept[i] = i < mine ? a.c_kept[at + i] : 0;
+      if (listed[i]) {
+        const uint32_t kh = a.c_keys[2 * (at + i)], kl = a.c_keys[2 * (at + i) + 1];
+        high = kh > high ? kh : high;
+        low = kl < low ? kl : low;
+        longest = listed[i] > longest ? listed[i] : longest;
+      }
+    }
+    auto umax = [](uint32_t x, uint32_t y) { return x > y ? x : y; };
+    high = wave_reduce(high, umax);
+    low = wave_reduce(low, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+    longest = wave_reduce(longest, umax);
+    first[0] = wave_scan(listed[0] + listed[1] + listed[2] + listed[3], count);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) first[i] = first[i - 1] + listed[i - 1];
     if (count == 0) {
       // everything in the bins is kept (min-p alone: everything)
-      if (row.binned()) edge = 0xffffffffu;
-    } else if (key_high == key_low) {
+      if (row.binned()) end.key = 0xffffffffu;
+    } else if (high == low) {
       // equal elements, however many
-      edge = key_high;
-      ties = count;
-      const uint64_t w = units(weight_of(edge));
-      const bool in_k = row.k > 0 && b.bin_k < kBins;
-      if (in_k) ties = (uint64_t)row.k - b.count_k < ties ? (uint64_t)row.k - b.count_k : ties;
-      if (row.p < 1.0) ties = ties_in(goal_of(in_k ? ties * w : 0), b.mass_lo, w, ties);
-      if (tid < a.chunks) {
-        const uint64_t left = ties > first ? ties - first : 0;
-        if (weight_of(edge) >= row.m) kept_of[tid] += (left < mine ? left : mine) * w;
-      }
-    } else if (count <= kMaxSorted && longest <= cap) {
-      // sort them, heaviest and then lowest index first
-      for (int c = tid / kWave; c < a.chunks; c += kPickThreads / kWave) {
-        const uint32_t m = a.c_listed[at + c];
-        uint32_t to = 0;
-        for (int i = tid % kWave; i < c; i += kWave) to += ties_of[i];
-        to = wave_reduce(to, [](uint32_t x, uint32_t y) { return x + y; });
-        for (uint32_t i = tid % kWave; i < m; i += kWave) sorted[to + i] = a.list[(at + c) * cap + i];
-      }
-      int size = 64;
-      while (size < (int)count) size *= 2;
-      for (int i = count + tid; i < size; i += kPickThreads) sorted[i] = 0;
-      __syncthreads();
-      for (int len = 2; len <= size; len *= 2)
-        for (int step = len / 2; step > 0; step /= 2) {
-          for (int i = tid; i < size / 2; i += kPickThreads) {
-            const int lo = i / step * 2 * step + i % step, hi = lo + step;
-            const uint64_t x = sorted[lo], y = sorted[hi];
-            if ((x < y) == ((lo & len) == 0)) sorted[lo] = y, sorted[hi] = x;
-          }
-          __syncthreads();
-        }
-      // four neighbouring elements a thread: their weights, and the sums before them
-      constexpr int kOwn = kMaxSorted / kPickThreads;
-      uint64_t w[kOwn], own = 0, of_k = 0, in_p = 0;
-      int bin[kOwn];
+      const uint64_t w = units(g.weight(high));
+      uint64_t ties = count;
+      if (g.ends_in_k()) ties = (uint64_t)row.k - b.count_k < ties ? (uint64_t)row.k - b.count_k : ties;
+      if (row.p < 1.0) ties = g.let_in(g.goal(g.ends_in_k() ? ties * w : 0), b.mass_lo, w, ties);
+      const bool heavy = g.weight(high) >= row.m;
 #pragma unroll
-      for (int j = 0; j < kOwn; ++j) {
-        const int i = tid * kOwn + j;
-        w[j] = 0, bin[j] = kBins;
-        if (i < (int)count) {
-          const double x = scaled(value_of((uint32_t)(sorted[i] >> 32)), top, row.inv_t);
-          w[j] = units(weight_exp(x));
-          bin[j] = bin_of(x, b.bin_scale);
-          in_p += bin[j] <= b.hi;
-        }
-        own += w[j];
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t left = ties > first[i] ? ties - first[i] : 0;
+        if (heavy) kept[i] += (left < listed[i] ? left : listed[i]) * w;
+        if (tid < kWave) lds.ties_of[4 * lane + i] = listed[i];
       }
-      uint64_t all, before = group_scan<kPickThreads>(own, all, mpart);
-      // listed elements of bins lo .. hi come first; with both filters bin_k may lie behind
-      const uint64_t n_p = group_reduce<kPickThreads>(in_p, [](uint64_t x, uint64_t y) { return x + y; }, mpart);
-      const bool both = row.k > 0 && row.p < 1.0 && b.bin_k < kBins;
-      // the rank of the i-th in the row's order, as far as top-k asks
-      auto rank_of = [&](int i, int bin_i) -> uint64_t {
-        return bin_i == b.bin_k && b.bin_k > b.hi ? (uint64_t)b.count_k + (i - n_p)
-                                                  : (uint64_t)b.count_lo + i;
-      };
+      end = {high, 0, ties};
+      __syncthreads();                                // ties_of
+    } else if (longest <= cap && count <= kMaxSorted) {
+      if (tid < kWave) {
 #pragma unroll
-      for (int j = 0; j < kOwn; ++j)
-        if (both && bin[j] == b.bin_k && rank_of(tid * kOwn + j, bin[j]) < (uint64_t)row.k) of_k += w[j];
-      of_k = group_reduce<kPickThreads>(of_k, [](uint64_t x, uint64_t y) { return x + y; }, mpart);
-      const double goal = row.p < 1.0 ? goal_of(of_k) : 0.0;
-      if (tid == 0) s_count = 0;
-      __syncthreads();
-      uint64_t run = before;
-#pragma unroll
-      for (int j = 0; j < kOwn; ++j) {
-        const int i = tid * kOwn + j;
-        if (i < (int)count && bin[j] <= b.hi &&
-            !(row.k > 0 && b.bin_k < kBins && rank_of(i, bin[j]) >= (uint64_t)row.k) &&
-            !(row.p < 1.0 && !((double)(b.mass_lo + run) < goal))) {
-          atomicMax(&s_count, (uint32_t)i + 1);     // kept: a prefix of the sorted elements
-          const uint32_t v = ~(uint32_t)sorted[i];
-          if (weight_of((uint32_t)(sorted[i] >> 32)) >= row.m)
-            atomicAdd((unsigned long long *)&kept_of[v / chunk_len], (unsigned long long)w[j]);
-        }
-        run += w[j];
+        for (int i = 0; i < 4; ++i) lds.kept_of[4 * lane + i] = kept[i];
       }
-      __syncthreads();
-      if (s_count == 0) {
-        edge = 0xffffffffu, tie_index = 0;          // none of them
+      if (count <= kWave) {
+        if (tid < kWave) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            for (uint32_t j = 0; j < listed[i]; ++j)
+              lds.sorted[first[i] + j] = a.list[(at + i) * cap + j];
+          __builtin_amdgcn_wave_barrier();
+          end = end_in_a_wave((uint32_t)lane < count ? lds.sorted[lane] : 0, g, chunk_len, lds);
+          if (lane == 0) lds.key = end.key, lds.ties = end.index;
+        }
+        __syncthreads();
+        end.key = lds.key, end.index = lds.ties;
       } else {
-        edge = (uint32_t)(sorted[s_count - 1] >> 32);
-        tie_index = ~(uint32_t)sorted[s_count - 1];
-      }
-    } else {
-      // too many: the edge by eight bits of the key a pass over the row, first that of
-      // top-k, then that of top-p among what top-k keeps
-      uint64_t *mass = sorted;
-      uint32_t *counts = reinterpret_cast<uint32_t *>(sorted + 256);
-      ties = ~0ull >> 1;
-      for (int round = 0; round < 2; ++round) {
-        const bool by_mass = round == 1;
-        if (by_mass ? !(row.p < 1.0) : !(row.k > 0)) continue;
-        double goal = 0.0;
-        if (by_mass) {
-          // the weight that top-k keeps
-          uint64_t sum = 0, equal = 0;
-          for (int v = tid; v < a.V; v += kPickThreads) {
-            const uint32_t key = key_of(clean(logit_value(logits[v])));
-            if (key > edge) sum += units(weight_of(key));
-            equal += key == edge;
-          }
-          auto add = [](uint64_t x, uint64_t y) { return x + y; };
-          sum = group_reduce<kPickThreads>(sum, add, mpart);
-          equal = group_reduce<kPickThreads>(equal, add, mpart);
-          if (edge) sum += (equal < ties ? equal : ties) * units(weight_of(edge));
-          goal = fmax(row.p * (row.k > 0 ? (double)sum : b.sum * kUnit), 0.5);
+        // a wave a chunk
+        if (tid < kWave)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lds.ties_of[4 * lane + i] = first[i];
+        __syncthreads();
+        for (int c = tid / kWave; c < a.chunks; c += kPickThreads / kWave) {
+          const int64_t c_at = (int64_t)n * a.chunks + c;
+          const uint32_t m = a.c_listed[c_at];
+          for (uint32_t j = lane; j < m; j += kWave)
+            lds.sorted[lds.ties_of[c] + j] = a.list[c_at * cap + j];
         }
-        uint32_t prefix = 0;
-        uint64_t ahead = 0;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-          __syncthreads();
-          if (tid < 256) mass[tid] = 0, counts[tid] = 0;
-          __syncthreads();
-          for (int v = tid; v < a.V; v += kPickThreads) {
-            const uint32_t key = key_of(clean(logit_value(logits[v])));
-            if (shift < 24 && key >> (shift + 8) != prefix >> (shift + 8)) continue;
-            if (key < edge) continue;
-            if (by_mass)
-              atomicAdd((unsigned long long *)&mass[key >> shift & 255],
-                        (unsigned long long)units(weight_of(key)));
-            atomicAdd(&counts[key >> shift & 255], 1u);
-          }
-          __syncthreads();
-          if (tid == 0) {
-            uint64_t run = ahead;
-            int i = 255;
-            for (; i > 0; --i) {
-              const uint64_t next = run + (by_mass ? mass[i] : (uint64_t)counts[i]);
-              if (by_mass ? !((double)next < goal) : next >= (uint64_t)row.k) break;
-              run = next;
-            }
-            s_key = prefix | (uint32_t)i << shift;
-            s_sum = run;
-            s_ties = counts[i];
-          }
-          __syncthreads();
-          prefix = s_key;
-          ahead = s_sum;
-        }
-        uint64_t r = (uint64_t)row.k - ahead;
-        if (by_mass) {
-          r = ties_in(goal, ahead, units(weight_of(prefix)), s_ties);
-          if (prefix == edge && r > ties) r = ties;
-        }
-        edge = prefix;
-        ties = r;
+        end = end_by_sorting(count, g, chunk_len, lds);
         __syncthreads();
       }
-      // each chunk's elements at the edge, then what it keeps, a wave a chunk
-      for (int c = tid / kWave; c < a.chunks; c += kPickThreads / kWave) {
-        uint32_t equal = 0;
-        const int end = min(a.V, (c + 1) * chunk_len);
-        for (int v = c * chunk_len + tid % kWave; v < end; v += kWave)
-          equal += key_of(clean(logit_value(logits[v]))) == edge;
-        equal = wave_reduce(equal, [](uint32_t x, uint32_t y) { return x + y; });
-        if (tid % kWave == 0) ties_of[c] = equal;
-      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kept[i] = lds.kept_of[4 * lane + i];
+    } else {
+      end = end_by_passes(logits, a.V, g, a.chunks, chunk_len, lds);
+      b.lo = -1;                                      // the bins say nothing
       __syncthreads();
-      for (int c = tid / kWave; c < a.chunks; c += kPickThreads / kWave) {
-        uint64_t ahead = 0, sum = 0;
-        for (int i = 0; i < c; ++i) ahead += ties_of[i];
-        const int end = min(a.V, (c + 1) * chunk_len);
-        for (int v = c * chunk_len + tid % kWave; v < end; v += kWave) {
-          const uint32_t key = key_of(clean(logit_value(logits[v])));
-          const double e = weight_of(key);
-          if (key > edge && e >= row.m) sum += units(e);
-        }
-        sum = wave_reduce(sum, [](uint64_t x, uint64_t y) { return x + y; });
-        const uint64_t left = ties > ahead ? ties - ahead : 0;
-        if (tid % kWave == 0) {
-          const double e = weight_of(edge);
-          kept_of[c] = sum + (e >= row.m ? (left < ties_of[c] ? left : ties_of[c]) * units(e) : 0);
-        }
-      }
-      b.lo = -1;                                     // the bins say nothing
+#pragma unroll
+      for (int i = 0; i < 4; ++i) kept[i] = i < mine ? lds.kept_of[4 * lane + i] : 0;
     }
-    __syncthreads();
-    // the chunk of the draw
-    const uint64_t x = tid < a.chunks ? kept_of[tid] : 0;
-    uint64_t sum;
-    const uint64_t before = group_scan<kPickThreads>(x, sum, mpart);
-    total = (double)sum;
-    const double goal = (double)u * total;
-    if (tid == 0) s_chunk = -1;
-    __syncthreads();
-    if (x > 0 && (double)before <= goal) atomicMax(&s_chunk, tid);
-    __syncthreads();
-    if (tid == s_chunk) s_mass = before;
-    __syncthreads();
+    drawn = draw_chunk(kept, u);
   }
 
   // the draw within the chunk: neighbouring elements a thread
-  const int c = s_chunk, per = chunk_len / kPickThreads;
-  const double goal = (double)u * total;
-  const int v0 = c * chunk_len + tid * per;
-  uint64_t tie0 = 0;
-  if (ties != ~0ull) {
-    uint64_t equal = 0, unused;
-    for (int i = 0; i < per; ++i)
-      equal += v0 + i < a.V && key_of(clean(logit_value(logits[v0 + i]))) == edge;
-    tie0 = group_scan<kPickThreads>(equal, unused, mpart);
-    for (int i = 0; i < c; ++i) tie0 += ties_of[i];
+  constexpr int kOwn = chunk_len / kPickThreads;
+  const int v0 = drawn.chunk * chunk_len + tid * kOwn;
+  const double goal = (double)u * drawn.total;
+  float z[kOwn];
+  load_neighbours<T, kOwn>(logits, v0, a.V, z);
+  uint64_t seen = 0;
+  if (end.ties != kByIndex) {
+    uint64_t equal = 0, all;
+#pragma unroll
+    for (int i = 0; i < kOwn; ++i) equal += v0 + i < a.V && key_of(z[i]) == end.key;
+    seen = group_scan<kPickThreads>(equal, all, lds.mpart);
+    for (int c = 0; c < drawn.chunk; ++c) seen += lds.ties_of[c];
   }
-  auto weight_at = [&](int v, uint64_t &seen, double &x) -> double {
-    const float z = clean(logit_value(logits[v]));
-    x = scaled(z, top, row.inv_t);
+  double w[kOwn], own = 0.0, all;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const double x = scaled(z[i], top, row.inv_t);
+    bool in = true;
     if (row.filtered()) {
-      const uint32_t key = key_of(z);
-      const bool tied = key == edge && (ties == ~0ull ? (uint32_t)v <= tie_index : seen++ < ties);
+      const uint32_t key = key_of(z[i]);
+      const bool tied = key == end.key && (end.ties == kByIndex ? (uint32_t)(v0 + i) <= end.index
+                                                                : seen++ < end.ties);
       const bool sure = b.lo >= 0 && (!row.binned() || bin_of(x, b.bin_scale) < b.lo);
-      if (!(key > edge || tied || sure)) return 0.0;
+      in = key > end.key || tied || sure;
     }
-    const double e = weight_exp(x);
-    if (e < row.m) return 0.0;
-    return row.filtered() ? (double)units(e) : e;
-  };
-  double own = 0.0, x, unused;
-  uint64_t seen = tie0;
-  for (int i = 0; i < per; ++i)
-    if (v0 + i < a.V) own += weight_at(v0 + i, seen, x);
-  const double start = row.filtered() ? (double)s_mass : s_before;
-  const double before = start + group_scan<kPickThreads>(own, unused, dpart);
-  if (tid == 0) s_token = -1;
-  __syncthreads();
+    const double e = in ? weight_exp(x) : 0.0;
+    w[i] = e < row.m ? 0.0 : row.filtered() ? (double)units(e) : e;
+    own += w[i];
+  }
+  if (tid == 0) lds.token = -1;
+  const double before = drawn.before + group_scan<kPickThreads>(own, all, lds.dpart);
   // the first element whose running sum passes the goal; should rounding leave none, the
   // last that weighs anything
   int token = -1;
-  bool past = false;
   double run = before;
-  seen = tie0;
-  for (int i = 0; i < per && !past; ++i) {
-    if (v0 + i >= a.V) break;
-    const double w = weight_at(v0 + i, seen, x);
-    run += w;
-    if (w > 0.0) token = v0 + i;
-    past = w > 0.0 && run > goal;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) {
+    const bool past = run > goal;                     // an element before did
+    run += w[i];
+    if (w[i] > 0.0 && !past) token = v0 + i;
   }
-  if (token >= 0 && before <= goal) atomicMax(&s_token, token);
+  if (token >= 0 && before <= goal) atomicMax(&lds.token, token);
   __syncthreads();
-  if (tid == 0) {
-    const int t = s_token;
-    a.tokens[n] = t;
-    if (a.logprob)
-      a.logprob[n] = (float)(scaled(clean(logit_value(logits[t])), top, row.inv_t) -
-                             log(row.filtered() ? total / kUnit : total));
+  if (token >= 0 && token == lds.token) {
+    a.tokens[n] = token;
+    if (a.logprob) {
+      float zt = 0.f;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) zt = v0 + i == token ? z[i] : zt;
+      a.logprob[n] = (float)(scaled(zt, top, row.inv_t) -
+                             log(row.filtered() ? drawn.total / kUnit : drawn.total));
+    }
   }
 }
 
@@ -809,7 +1035,8 @@ int32_t sample_per(int32_t N, int32_t V) {
 
 struct SampleLayout {
   int32_t per, chunks;
-  size_t c_top, c_low, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_keys, list, border;
+  size_t c_top, c_low, t_top, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_keys, list;
+  size_t border, ends;
   size_t bytes;
 };
 SampleLayout sample_layout(int32_t N, int32_t V) {
@@ -825,6 +1052,7 @@ SampleLayout sample_layout(int32_t N, int32_t V) {
   };
   l.c_top = take(parts * 4);
   l.c_low = take(parts * 4);
+  l.t_top = take(parts * kThreads * 4);
   l.c_first = take(parts * 4);
   l.c_sum = take(parts * 8);
   l.bin_mass = take((size_t)N * kBins * 8);
@@ -834,6 +1062,7 @@ SampleLayout sample_layout(int32_t N, int32_t V) {
   l.c_keys = take(parts * 8);
   l.list = take(parts * list_cap(l.per) * 8);
   l.border = take((size_t)N * sizeof(Border));
+  l.ends = take((size_t)N * sizeof(Border));
   l.bytes = at;
   return l;
 }
@@ -843,10 +1072,12 @@ void launch_passes(const SampleArgs &a, hipStream_t stream) {
   const dim3 grid((unsigned)a.N * (unsigned)a.chunks);
   const bool bins = a.top_k || a.top_p;
   hipLaunchKernelGGL((sample_stats_kernel<T, kPer>), grid, dim3(kThreads), 0, stream, a);
+  if (bins || a.min_p)
+    hipLaunchKernelGGL(sample_range_kernel, dim3(a.N), dim3(kRowThreads), 0, stream, a);
   if (bins) hipLaunchKernelGGL((sample_bins_kernel<T, kPer>), grid, dim3(kThreads), 0, stream, a);
   if (bins || a.min_p)
     hipLaunchKernelGGL((sample_border_kernel<T, kPer>), grid, dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL(sample_pick_kernel<T>, dim3(a.N), dim3(kPickThreads), 0, stream, a);
+  hipLaunchKernelGGL((sample_pick_kernel<T, kPer>), dim3(a.N), dim3(kPickThreads), 0, stream, a);
 }
 
 }  // namespace
@@ -883,7 +1114,9 @@ hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, in
   a.c_listed = reinterpret_cast<uint32_t *>(ws + l.c_listed);
   a.c_keys = reinterpret_cast<uint32_t *>(ws + l.c_keys);
   a.list = reinterpret_cast<uint64_t *>(ws + l.list);
+  a.t_top = reinterpret_cast<float *>(ws + l.t_top);
   a.border = reinterpret_cast<Border *>(ws + l.border);
+  a.ends = reinterpret_cast<Border *>(ws + l.ends);
   if (bf16) {
     if (l.per == 8)
       launch_passes<uint16_t, 8>(a, stream);
