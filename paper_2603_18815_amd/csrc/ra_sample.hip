@@ -8,32 +8,37 @@
 // V <= 2^19. The other sums are taken in a fixed order.
 //
 // All filters keep a prefix of the order (logit descending, index ascending), so what is
-// sought is where it ends. Rows are cut into chunks, a workgroup each, and the call runs:
-//   stats   each chunk's and each of its threads' largest logit, the chunk's smallest, and
-//           its sum of weights (rows without filters, or with top-p alone)
+// sought is where it ends. Rows are cut into chunks, a wave each, and the call runs:
+//   stats   each chunk's and each of its lanes' largest logit, the chunk's smallest, and its
+//           sum of weights (rows without filters, or with top-p alone)
 //   range   a workgroup a row: how far below M the end can lie. Top-k: the k-th of the
-//           threads' largest logits is no larger than the k-th logit. Top-p: elements below
+//           lanes' largest logits is no larger than the k-th logit. Top-p: elements below
 //           (1 - p) sum / V weigh less than (1 - p) sum together.
 //   bins    counts and weights of the elements in the range, in 512 bins of it
 //   border  the bin or bins that hold the end. What lies above is kept: each chunk sums it;
 //           the elements in them are listed
-//   pick    a workgroup a row: the listed elements sorted, the end found, the chunk of the
-//           drawn token from the chunks' sums, the token from the chunk's elements
+//   pick    a workgroup a row: the listed elements binned again and the few in question
+//           sorted, the end found, the chunk of the drawn token from the chunks' sums, the
+//           token from the chunk's elements
 // Bound by the first pass's read of the logits and, for few rows, by the launches: bins and
-// border read only what the threads' largest logits put into the range. Without filters
+// border read only what the lanes' largest logits put into the range. Without filters
 // stats and pick are the whole call; with min-p alone there are no bins.
+#include <type_traits>
+
 #include "ra_device.h"
 #include "ra_internal.h"
 
 namespace ra {
 namespace {
 
-constexpr int kThreads = 256;           // of a chunk's workgroup
-constexpr int kPickThreads = 1024;
-constexpr int kRowThreads = 1024;       // of a row's range
+constexpr int kThreads = 256;           // four chunks
+constexpr int kGroup = kThreads / kWave;
+constexpr int kPickThreads = 256;
+constexpr int kRowThreads = 512;        // of a row's range
 constexpr int kBins = 512;
 constexpr int kMaxChunks = 256;         // of a row
-constexpr int kMaxSorted = 4096;        // listed elements that the pick sorts
+constexpr int kListed = 256;            // elements that a chunk can list
+constexpr int kMaxSorted = 2048;        // of them, that the pick sorts
 constexpr double kUnit = 0x1p44;
 constexpr double kRange = 31.5;         // weights end before this
 
@@ -123,10 +128,10 @@ struct SampleArgs {
   int32_t *tokens;
   float *logprob;
   int64_t row_stride;
-  int32_t N, V, chunks, per;            // elements of a chunk: kThreads * per
+  int32_t N, V, chunks, groups;         // groups: of kGroup chunks
   // workspace
   float *c_top, *c_low;                 // [N][chunks] largest and smallest finite logit
-  float *t_top;                         // [N][chunks][kThreads] largest of a thread's
+  float *l_top;                         // [N][chunks][kWave] largest of a lane's
   uint32_t *c_first;                    // [N][chunks] lowest index of the largest one
   double *c_sum;                        // [N][chunks] sum of weights against c_top
   uint64_t *bin_mass;                   // [N][kBins]
@@ -134,10 +139,9 @@ struct SampleArgs {
   uint64_t *c_kept;                     // [N][chunks] weight kept for certain
   uint32_t *c_listed;                   // [N][chunks] elements in the border's bins
   uint32_t *c_keys;                     // [N][chunks][2] their largest and smallest key
-  uint64_t *list;                       // [N][chunks][per * 8] key << 32 | ~index
+  uint64_t *list;                       // [N][chunks][kListed] key << 32 | ~index
   struct Border *border, *ends;         // [N] with the range; with the end's bins too
 };
-__host__ __device__ constexpr int list_cap(int per) { return per * 8; }
 
 // What a row asks for.
 struct Row {
@@ -168,7 +172,7 @@ struct Border {
   float top;
   int lo, hi, bin_k;                    // kBins: none
   uint32_t count_lo, count_k;           // elements before bin lo, bin_k
-  uint64_t mass_lo, mass_k, mass_all;   // weights before them; of all bins
+  uint64_t mass_lo, mass_k;             // weights before them
 };
 
 // The bin of a logit: non-decreasing as z falls. kBins: beyond.
@@ -217,74 +221,97 @@ __device__ __forceinline__ V group_scan(V x, V &total, V *part) {
   return before + (s - x);
 }
 
+// Sums over the lanes before this one, and over all.
+template <typename V>
+__device__ __forceinline__ V wave_scan(V x, V &total) {
+  const int lane = threadIdx.x % kWave;
+  V s = x;
+#pragma unroll
+  for (int d = 1; d < kWave; d *= 2) {
+    const V y = __shfl_up(s, d);
+    if (lane >= d) s += y;
+  }
+  total = __shfl(s, kWave - 1);
+  return s - x;
+}
+
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float min_of(float a, float b) { return fminf(a, b); }
 
-// Chunk c's logits of a thread: vectors tid, tid + kThreads, ...; -inf past the row.
+// Chunk c's logits of a lane: vectors lane, lane + kWave, ...; -inf past the row.
 template <typename T, int kPer>
 __device__ __forceinline__ void load_chunk(const SampleArgs &a, int n, int c, float (&z)[kPer]) {
   constexpr int kVec = kVector<T>;
+  const int lane = threadIdx.x % kWave;
   const T *row = static_cast<const T *>(a.logits) + n * a.row_stride;
+  u32x4_any w[kPer / kVec];
+  if ((c + 1) * kWave * kPer <= a.V) {
 #pragma unroll
-  for (int j = 0; j < kPer / kVec; ++j) {
-    const int v0 = c * kThreads * kPer + (j * kThreads + threadIdx.x) * kVec;
-    if (v0 + kVec <= a.V) {
-      const u32x4_any w = *reinterpret_cast<const u32x4_any *>(row + v0);
+    for (int j = 0; j < kPer / kVec; ++j)
+      w[j] = *reinterpret_cast<const u32x4_any *>(row + c * kWave * kPer + (j * kWave + lane) * kVec);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        if constexpr (sizeof(T) == 4)
-          z[j * kVec + e] = __uint_as_float(w[e]);
-        else
-          z[j * kVec + e] = __uint_as_float(e % 2 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-      }
-    } else {
+    for (int i = 0; i < kPer; ++i) {
+      if constexpr (sizeof(T) == 4)
+        z[i] = __uint_as_float(w[i / kVec][i % kVec]);
+      else
+        z[i] = __uint_as_float(i % 2 ? w[i / kVec][i % kVec / 2] & 0xffff0000u
+                                     : w[i / kVec][i % kVec / 2] << 16);
+    }
+  } else {
 #pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        z[j * kVec + e] = v0 + e < a.V ? logit_value(row[v0 + e]) : -__builtin_inff();
+    for (int i = 0; i < kPer; ++i) {
+      const int v = c * kWave * kPer + (i / kVec * kWave + lane) * kVec + i % kVec;
+      z[i] = v < a.V ? logit_value(row[v]) : -__builtin_inff();
     }
   }
 #pragma unroll
   for (int i = 0; i < kPer; ++i) z[i] = clean(z[i]);
 }
-// The index of a thread's i-th logit.
+// The index of a lane's i-th logit.
 template <typename T, int kPer>
 __device__ __forceinline__ int index_of(int c, int i) {
   constexpr int kVec = kVector<T>;
-  return c * kThreads * kPer + (i / kVec * kThreads + threadIdx.x) * kVec + i % kVec;
+  return c * kWave * kPer + (i / kVec * kWave + (int)(threadIdx.x % kWave)) * kVec + i % kVec;
+}
+
+// 2^(j / kExpTable) for TableExp, by the workgroup's threads.
+__device__ __forceinline__ void fill_table(double *table) {
+  for (int i = threadIdx.x; i < kExpTable; i += blockDim.x)
+    table[i] = 2.0 * weight_exp((i - kExpTable) * kStep);
+  __syncthreads();
 }
 
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
-  const int n = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-  __shared__ float part[kThreads / kWave];
-  __shared__ double dpart[kThreads / kWave];
-  __shared__ int ipart[kThreads / kWave];
+  const int n = blockIdx.x / a.groups, lane = threadIdx.x % kWave;
+  const int c = blockIdx.x % a.groups * kGroup + threadIdx.x / kWave;
   __shared__ double table[kExpTable];
+  const Row row(a, n);
+  if (row.needs_sums()) fill_table(table);
+  if (c >= a.chunks) return;
   float z[kPer];
   load_chunk<T, kPer>(a, n, c, z);
-  const Row row(a, n);
-  if (row.needs_sums() && tid < kExpTable)   // reaches the others by the next barrier
-    table[tid] = 2.0 * weight_exp((tid - kExpTable) * kStep);
-  float mine = z[0], low = __builtin_inff();
+  float mine = z[0];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, z[i]);
-  const float top = group_reduce<kThreads>(mine, max_of, part);
+  for (int i = 1; i < kPer; ++i) mine = fmaxf(mine, z[i]);
+  const float top = wave_reduce(mine, max_of);
   const int64_t at = (int64_t)n * a.chunks + c;
-  if (tid == 0) a.c_top[at] = top;
+  if (lane == 0) a.c_top[at] = top;
   if (row.greedy) {
     int first = a.V;
 #pragma unroll
     for (int i = kPer - 1; i >= 0; --i) first = z[i] == top ? index_of<T, kPer>(c, i) : first;
-    first = group_reduce<kThreads>(first, [](int x, int y) { return min(x, y); }, ipart);
-    if (tid == 0) a.c_first[at] = first;
+    first = wave_reduce(first, [](int x, int y) { return min(x, y); });
+    if (lane == 0) a.c_first[at] = first;
     return;
   }
-  if (row.filtered()) a.t_top[at * kThreads + tid] = mine;
+  if (row.filtered()) a.l_top[at * kWave + lane] = mine;
   if (row.binned()) {
+    float low = __builtin_inff();
 #pragma unroll
     for (int i = 0; i < kPer; ++i) low = z[i] > -__builtin_inff() ? fminf(low, z[i]) : low;
-    low = group_reduce<kThreads>(low, min_of, part);
-    if (tid == 0) a.c_low[at] = low;
+    low = wave_reduce(low, min_of);
+    if (lane == 0) a.c_low[at] = low;
   }
   if (row.needs_sums()) {
     double sum = 0.0;
@@ -298,55 +325,85 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
         sum += weight((double)z[i] - from);
       }
     }
-    sum = group_reduce<kThreads>(sum, [](double x, double y) { return x + y; }, dpart);
-    if (tid == 0) a.c_sum[at] = sum;
+    sum = wave_reduce(sum, [](double x, double y) { return x + y; });
+    if (lane == 0) a.c_sum[at] = sum;
   }
 }
 
-// Thresholds of rows with filters; the rows' bins start at zero.
+// A row's chunks, four a lane, for every wave by itself.
+__device__ __forceinline__ void load_tops(const SampleArgs &a, int n, float (&c_top)[4], float &top) {
+  const int lane = threadIdx.x % kWave;
+  static_assert(kMaxChunks == 4 * kWave, "four chunks a lane");
+  top = -__builtin_inff();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    c_top[i] = 4 * lane + i < a.chunks ? a.c_top[(int64_t)n * a.chunks + 4 * lane + i] : -__builtin_inff();
+    top = fmaxf(top, c_top[i]);
+  }
+  top = wave_reduce(top, max_of);
+}
+// Their sums of weights against the row's largest logit.
+__device__ __forceinline__ void load_sums(const SampleArgs &a, int n, const float (&c_top)[4], float top,
+                                          double inv_t, double (&x)[4]) {
+  const int lane = threadIdx.x % kWave;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] = 4 * lane + i < a.chunks ? a.c_sum[(int64_t)n * a.chunks + 4 * lane + i] *
+                                         weight_exp(scaled(c_top[i], top, inv_t))
+                                   : 0.0;
+}
+
+// Ranges of rows with filters; their bins start at zero.
 __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a) {
-  const int n = blockIdx.x, tid = threadIdx.x;
+  const int n = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const Row row(a, n);
   if (!row.filtered()) return;
-  __shared__ float part[kRowThreads / kWave];
-  __shared__ double dpart[kRowThreads / kWave];
-  __shared__ uint32_t cpart[kRowThreads / kWave];
   __shared__ uint32_t count[kBins];
-  __shared__ int s_bin;
   const int64_t at = (int64_t)n * a.chunks;
-  const bool have = tid < a.chunks;
-  const float c_top = have ? a.c_top[at + tid] : -__builtin_inff();
+  float c_top[4];
   Border b = Border();
   b.inv_t = row.inv_t;
-  b.top = group_reduce<kRowThreads>(c_top, max_of, part);
+  load_tops(a, n, c_top, b.top);
   double range = kRange;
   if (row.binned()) {
-    if (tid < kBins) {
-      count[tid] = 0;
-      a.bin_mass[(int64_t)n * kBins + tid] = 0;
-      a.bin_count[(int64_t)n * kBins + tid] = 0;
-    }
-    if (tid == 0) s_bin = kBins;
-    const float low = group_reduce<kRowThreads>(have ? a.c_low[at + tid] : __builtin_inff(), min_of, part);
+    static_assert(kRowThreads == kBins, "a bin a thread");
+    a.bin_mass[(int64_t)n * kBins + tid] = 0;
+    a.bin_count[(int64_t)n * kBins + tid] = 0;
+    float low = __builtin_inff();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * lane + i < a.chunks) low = fminf(low, a.c_low[at + 4 * lane + i]);
+    low = wave_reduce(low, min_of);
     range = fmin(range, -scaled(fminf(low, b.top), b.top, row.inv_t));
     if (row.k > 0) {
-      // the k-th of the threads' largest logits, as far as a bin tells
+      // the k-th of the lanes' largest logits, as far as a bin tells
+      count[tid] = 0;
+      __syncthreads();
       const double scale = kBins / (fmax(range, 1e-30) * (1.0 + 1e-9));
-      const int parts = a.chunks * kThreads;
+      const int parts = a.chunks * kWave;
+#pragma unroll 4
       for (int i = tid; i < parts; i += kRowThreads) {
-        const int bin = bin_of(scaled(a.t_top[at * kThreads + i], b.top, row.inv_t), scale);
+        const int bin = bin_of(scaled(a.l_top[at * kWave + i], b.top, row.inv_t), scale);
         if (bin < kBins) atomicAdd(&count[bin], 1u);
       }
       __syncthreads();
-      const uint32_t own = tid < kBins ? count[tid] : 0;
-      uint32_t all;
-      const uint32_t before = group_scan<kRowThreads>(own, all, cpart);
-      if (before < (uint32_t)row.k && before + own >= (uint32_t)row.k) s_bin = tid;
-      __syncthreads();
-      if (s_bin < kBins) range = fmin(range, (s_bin + 1) / scale * (1.0 + 1e-9));
+      constexpr int kOwn = kBins / kWave;
+      uint32_t own = 0, all, c[kOwn];
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) own += c[i] = count[kOwn * lane + i];
+      uint32_t before = wave_scan(own, all);
+      int bin = kBins;
+#pragma unroll
+      for (int i = 0; i < kOwn; ++i) {
+        if (before < (uint32_t)row.k && before + c[i] >= (uint32_t)row.k) bin = kOwn * lane + i;
+        before += c[i];
+      }
+      bin = wave_reduce(bin, [](int x, int y) { return min(x, y); });
+      if (bin < kBins) range = fmin(range, (bin + 1) / scale * (1.0 + 1e-9));
     } else {
-      const double x = have ? a.c_sum[at + tid] * weight_exp(scaled(c_top, b.top, row.inv_t)) : 0.0;
-      b.sum = group_reduce<kRowThreads>(x, [](double u, double v) { return u + v; }, dpart);
+      double x[4];
+      load_sums(a, n, c_top, b.top, row.inv_t, x);
+      b.sum = wave_reduce(x[0] + x[1] + x[2] + x[3], [](double u, double v) { return u + v; });
       if (row.p > 0.0) range = fmin(range, log((double)a.V / ((1.0 - row.p) * b.sum)) + 1e-3);
     }
   } else {
@@ -364,28 +421,38 @@ __device__ __forceinline__ bool in_range(const Border &b, float z) {
 
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
-  const int n = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-  const int64_t at = (int64_t)n * a.chunks + c;
-  const float c_top = a.c_top[at];
+  const int n = blockIdx.x / a.groups, tid = threadIdx.x, lane = tid % kWave;
+  const int c0 = blockIdx.x % a.groups * kGroup, c = c0 + tid / kWave;
   const Row row(a, n);
   if (!row.binned()) return;
   const Border b = a.border[n];
-  if (b.top == -__builtin_inff() || !in_range(b, c_top)) return;
+  if (b.top == -__builtin_inff()) return;
+  const int64_t at = (int64_t)n * a.chunks + c0;
+  bool any = false, mine = false;
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) {
+    const bool in = c0 + i < a.chunks && in_range(b, a.c_top[at + i]);
+    any |= in;
+    mine = c == c0 + i ? in : mine;
+  }
+  if (!any) return;
   __shared__ uint64_t mass[kBins];
   __shared__ uint32_t count[kBins];
+  __shared__ double table[kExpTable];
   for (int i = tid; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
-  __syncthreads();
-  if (in_range(b, a.t_top[at * kThreads + tid])) {
+  fill_table(table);
+  if (mine && in_range(b, a.l_top[((int64_t)n * a.chunks + c) * kWave + lane])) {
     float z[kPer];
     load_chunk<T, kPer>(a, n, c, z);
+    const TableExp weight(table, row.inv_t);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const double x = scaled(z[i], b.top, b.inv_t);
-      const int bin = bin_of(x, b.bin_scale);
+      const int bin = bin_of(scaled(z[i], b.top, b.inv_t), b.bin_scale);
       if (bin < kBins) {
         if (row.k > 0) atomicAdd(&count[bin], 1u);
         if (row.p < 1.0)
-          atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)units(weight_exp(x)));
+          atomicAdd((unsigned long long *)&mass[bin],
+                    (unsigned long long)units(weight(z[i] == b.top ? 0.0 : (double)z[i] - (double)b.top)));
       }
     }
   }
@@ -397,77 +464,55 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   }
 }
 
-// Sums over the lanes before this one, and over all.
-template <typename V>
-__device__ __forceinline__ V wave_scan(V x, V &total) {
+// The end's bins, from weights and counts of eight neighbouring bins a lane, for every wave
+// by itself. `mass0` and `count0` are ahead of the first bin; by_k: top-k may end in a bin;
+// `all`: what top-p takes its share of if it does not.
+constexpr int kOwnBins = kBins / kWave;
+__device__ __forceinline__ void locate(const uint64_t (&m)[kOwnBins], const uint32_t (&c)[kOwnBins],
+                                       uint64_t mass0, uint32_t count0, bool by_k, uint32_t k,
+                                       double p, double all, Border &b) {
   const int lane = threadIdx.x % kWave;
-  V s = x;
+  uint64_t m_own = 0, m_all;
+  uint32_t c_own = 0, c_all;
 #pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const V y = __shfl_up(s, d);
-    if (lane >= d) s += y;
-  }
-  total = __shfl(s, kWave - 1);
-  return s - x;
-}
-
-// The end's bins, from the row's bins. Every wave finds them by itself: a lane holds eight
-// neighbouring bins, and no barrier is needed.
-__device__ __forceinline__ void find_border(const SampleArgs &a, int n, const Row &row, Border &b) {
-  constexpr int kOwn = kBins / kWave;
-  const int lane = threadIdx.x % kWave;
-  const int64_t at = (int64_t)n * kBins + kOwn * lane;
-  uint64_t m[kOwn], m_own = 0, m_all = 0, m_before = 0;
-  uint32_t c[kOwn], c_own = 0, c_all = 0, c_before = 0;
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    m[i] = row.p < 1.0 ? a.bin_mass[at + i] : 0;
-    c[i] = row.k > 0 ? a.bin_count[at + i] : 0;
-    m_own += m[i];
-    c_own += c[i];
-  }
-  if (row.p < 1.0) m_before = wave_scan(m_own, m_all);
-  if (row.k > 0) c_before = wave_scan(c_own, c_all);
+  for (int i = 0; i < kOwnBins; ++i) m_own += m[i], c_own += c[i];
+  const uint64_t m_before = mass0 + wave_scan(m_own, m_all);
+  const uint32_t c_before = count0 + wave_scan(c_own, c_all);
   b.lo = b.hi = b.bin_k = kBins;
-  b.count_lo = b.count_k = 0;
-  b.mass_lo = b.mass_k = b.mass_all = m_all;
+  b.count_lo = b.count_k = count0;
+  b.mass_lo = b.mass_k = mass0 + m_all;
   uint64_t of_bin_k = 0;
-  if (row.k > 0) {
+  if (by_k) {
     // where the count reaches k
     int bin = kBins;
     uint32_t count = c_before, c_at = 0;
     uint64_t mass = m_before, m_at = 0, m_in = 0;
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      if (count < (uint32_t)row.k && count + c[i] >= (uint32_t)row.k)
-        bin = kOwn * lane + i, c_at = count, m_at = mass, m_in = m[i];
+    for (int i = 0; i < kOwnBins; ++i) {
+      if (count < k && count + c[i] >= k) bin = kOwnBins * lane + i, c_at = count, m_at = mass, m_in = m[i];
       count += c[i];
       mass += m[i];
     }
     const uint64_t found = __ballot(bin < kBins);
     if (found) {
       const int from = __ffsll((unsigned long long)found) - 1;
-      b.bin_k = __shfl(bin, from);
-      b.count_k = __shfl(c_at, from);
-      b.mass_k = __shfl(m_at, from);
+      b.lo = b.hi = b.bin_k = __shfl(bin, from);
+      b.count_lo = b.count_k = __shfl(c_at, from);
+      b.mass_lo = b.mass_k = __shfl(m_at, from);
       of_bin_k = __shfl(m_in, from);
-      b.lo = b.hi = b.bin_k;
-      b.count_lo = b.count_k;
-      b.mass_lo = b.mass_k;
+      all = (double)b.mass_k;
     }
   }
-  if (row.p < 1.0) {
+  if (p < 1.0) {
     // lo, hi: where the weight reaches p of the least and of the most that top-k can keep; by
     // rounding alone it might not by bin_k, which then is the end's
-    const double of_k = row.k > 0 ? (double)b.mass_k : b.sum * kUnit;
-    const double least = fmax(row.p * of_k, 0.5);
-    const double most = fmax(row.p * (of_k + (double)of_bin_k), 0.5);
+    const double least = fmax(p * all, 0.5), most = fmax(p * (all + (double)of_bin_k), 0.5);
     int lo = kBins, hi = kBins;
     uint32_t count = c_before, c_at = 0;
     uint64_t mass = m_before, m_at = 0;
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      const int bin = kOwn * lane + i;
+    for (int i = 0; i < kOwnBins; ++i) {
+      const int bin = kOwnBins * lane + i;
       const uint64_t after = mass + m[i];
       if (bin <= b.bin_k) {
         if ((double)mass < least && !((double)after < least)) lo = bin, c_at = count, m_at = mass;
@@ -487,62 +532,80 @@ __device__ __forceinline__ void find_border(const SampleArgs &a, int n, const Ro
   }
 }
 
+// From the row's bins.
+__device__ __forceinline__ void find_border(const SampleArgs &a, int n, const Row &row, Border &b) {
+  const int64_t at = (int64_t)n * kBins + kOwnBins * (threadIdx.x % kWave);
+  uint64_t m[kOwnBins], sum = 0;
+  uint32_t c[kOwnBins];
+#pragma unroll
+  for (int i = 0; i < kOwnBins; ++i) {
+    m[i] = row.p < 1.0 ? a.bin_mass[at + i] : 0;
+    c[i] = row.k > 0 ? a.bin_count[at + i] : 0;
+    sum += m[i];
+  }
+  double all = b.sum * kUnit;
+  if (row.k > 0) all = (double)wave_reduce(sum, [](uint64_t x, uint64_t y) { return x + y; });
+  locate(m, c, 0, 0, row.k > 0, (uint32_t)row.k, row.p, all, b);
+}
+
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
-  const int n = blockIdx.x / a.chunks, c = blockIdx.x % a.chunks, tid = threadIdx.x;
-  const int64_t at = (int64_t)n * a.chunks + c;
-  const float c_top = a.c_top[at];
+  const int n = blockIdx.x / a.groups, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int c0 = blockIdx.x % a.groups * kGroup, c = c0 + wave;
   const Row row(a, n);
   if (!row.filtered()) return;
   Border b = a.border[n];
   if (b.top == -__builtin_inff()) return;
+  const int64_t at = (int64_t)n * a.chunks + c;
+  __shared__ double table[kExpTable];
+  __shared__ uint32_t s_listed[kGroup];
+  if (lane == 0) s_listed[wave] = 0;
+  const float c_top = c < a.chunks ? a.c_top[at] : -__builtin_inff();
+  if (__syncthreads_or(in_range(b, c_top))) fill_table(table);   // each wave has its own counter
+  if (c >= a.chunks) return;
   if (!in_range(b, c_top)) {
-    if (tid == 0) a.c_kept[at] = 0, a.c_listed[at] = 0;
+    if (lane == 0) a.c_kept[at] = 0, a.c_listed[at] = 0;
     return;
   }
-  __shared__ uint32_t listed, key_high, key_low;
-  __shared__ uint64_t sure;
-  if (tid == 0) listed = 0, key_high = 0, key_low = 0xffffffffu, sure = 0;
-  const float t_top = a.t_top[at * kThreads + tid];
+  const float l_top = a.l_top[at * kWave + lane];
   if (row.binned()) {
     find_border(a, n, row, b);
   } else {
     b.lo = b.hi = b.bin_k = kBins;
   }
-  __syncthreads();
-  uint64_t *list = a.list + at * list_cap(kPer);
   uint64_t kept = 0;
   uint32_t high = 0, low = 0xffffffffu;
-  if (in_range(b, t_top)) {
+  if (in_range(b, l_top)) {
     float z[kPer];
     load_chunk<T, kPer>(a, n, c, z);
+    const TableExp weight(table, row.inv_t);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const double x = scaled(z[i], b.top, b.inv_t);
-      const int bin = bin_of(x, b.bin_scale);
+      const int bin = bin_of(scaled(z[i], b.top, b.inv_t), b.bin_scale);
       if (bin < b.lo) {
-        const double e = weight_exp(x);
+        const double e = weight(z[i] == b.top ? 0.0 : (double)z[i] - (double)b.top);
         if (e >= row.m) kept += units(e);
       } else if (bin < kBins && (bin <= b.hi || bin == b.bin_k)) {
-        const uint32_t slot = atomicAdd(&listed, 1u), key = key_of(z[i]);
-        if (slot < (uint32_t)list_cap(kPer))
-          list[slot] = (uint64_t)key << 32 | (uint32_t)~index_of<T, kPer>(c, i);
+        const uint32_t slot = atomicAdd(&s_listed[wave], 1u), key = key_of(z[i]);
+        if (slot < (uint32_t)kListed)
+          a.list[at * kListed + slot] = (uint64_t)key << 32 | (uint32_t)~index_of<T, kPer>(c, i);
         high = key > high ? key : high;
         low = key < low ? key : low;
       }
     }
-    if (kept) atomicAdd((unsigned long long *)&sure, (unsigned long long)kept);
-    if (high) {
-      atomicMax(&key_high, high);
-      atomicMin(&key_low, low);
-    }
   }
-  __syncthreads();
-  if (tid == 0) {
-    a.c_kept[at] = sure;
+  __builtin_amdgcn_wave_barrier();
+  const uint32_t listed = __shfl(lane == 0 ? s_listed[wave] : 0u, 0);
+  kept = wave_reduce(kept, [](uint64_t x, uint64_t y) { return x + y; });
+  if (listed) {
+    high = wave_reduce(high, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+    low = wave_reduce(low, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+  }
+  if (lane == 0) {
+    a.c_kept[at] = kept;
     a.c_listed[at] = listed;
-    a.c_keys[2 * at] = key_high;
-    a.c_keys[2 * at + 1] = key_low;
+    a.c_keys[2 * at] = high;
+    a.c_keys[2 * at + 1] = low;
     if (c_top == b.top) a.ends[n] = b;    // one of the chunks that hold it: all write the same
   }
 }
@@ -574,14 +637,16 @@ __device__ __forceinline__ void load_neighbours(const T *row, int v0, int V, flo
 
 // What the pick's waves share.
 struct PickLds {
-  uint64_t sorted[kMaxSorted];          // the listed elements, or 256 bins of a pass
+  uint64_t sorted[kMaxSorted];          // listed elements
+  uint64_t mass[kBins];                 // finer bins
+  uint32_t counts[kBins];
   uint64_t kept_of[kMaxChunks];         // weight kept of each chunk
   uint32_t ties_of[kMaxChunks];         // of each chunk: elements at the edge
   uint64_t mpart[kPickThreads / kWave];
   double dpart[kPickThreads / kWave];
   uint32_t cpart[kPickThreads / kWave];
   uint64_t sum;
-  uint32_t key, count, ties;
+  uint32_t key, count, ties, high, low;
   int token;
 };
 
@@ -597,13 +662,20 @@ struct Edge {
 struct Goals {
   const Row &row;
   const Border &b;
+  double all;                           // what top-p takes its share of if top-k keeps all
+  uint32_t high;                        // key of the first of finer bins,
+  int shift;                            // and their width; < 0: the row's bins
+  __device__ __forceinline__ int bin(uint32_t key) const {
+    if (shift >= 0) return (int)((high - key) >> shift);
+    return bin_of(scaled(value_of(key), b.top, row.inv_t), b.bin_scale);
+  }
   __device__ __forceinline__ double weight(uint32_t key) const {
     return weight_exp(scaled(value_of(key), b.top, row.inv_t));
   }
   __device__ __forceinline__ bool ends_in_k() const { return row.k > 0 && b.bin_k < kBins; }
   // the weight at which top-p ends, given what top-k keeps of bin_k
   __device__ __forceinline__ double goal(uint64_t of_bin_k) const {
-    return fmax(row.p * (row.k > 0 ? (double)(b.mass_k + of_bin_k) : b.sum * kUnit), 0.5);
+    return fmax(row.p * (ends_in_k() ? (double)(b.mass_k + of_bin_k) : all), 0.5);
   }
   // how many of `avail` elements of weight w, `before` ahead of them, the goal lets in
   __device__ __forceinline__ uint64_t let_in(double goal, uint64_t before, uint64_t w,
@@ -637,12 +709,11 @@ __device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int ch
     }
   uint64_t w = 0, all;
   double e = 0.0;
-  int bin = kBins;
+  int bin = kBins << 10;
   if (x) {
-    const double d = scaled(value_of((uint32_t)(x >> 32)), g.b.top, g.row.inv_t);
-    e = weight_exp(d);
+    e = g.weight((uint32_t)(x >> 32));
     w = units(e);
-    bin = bin_of(d, g.b.bin_scale);
+    bin = g.bin((uint32_t)(x >> 32));
   }
   const uint64_t before = wave_scan(w, all);
   const uint64_t n_p = __popcll(__ballot(x && bin <= g.b.hi)), rank = g.rank(lane, bin, n_p);
@@ -675,7 +746,7 @@ __device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int ch
       }
       __syncthreads();
     }
-  // four neighbouring elements a thread: their weights, and the sums before them
+  // neighbouring elements a thread: their weights, and the sums before them
   constexpr int kOwn = kMaxSorted / kPickThreads;
   auto add = [](uint64_t x, uint64_t y) { return x + y; };
   uint64_t w[kOwn], own = 0, of_k = 0, in_p = 0, all;
@@ -683,11 +754,10 @@ __device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int ch
 #pragma unroll
   for (int j = 0; j < kOwn; ++j) {
     const int i = tid * kOwn + j;
-    w[j] = 0, bin[j] = kBins;
+    w[j] = 0, bin[j] = kBins << 10;
     if (i < count) {
-      const double x = scaled(value_of((uint32_t)(lds.sorted[i] >> 32)), g.b.top, g.row.inv_t);
-      w[j] = units(weight_exp(x));
-      bin[j] = bin_of(x, g.b.bin_scale);
+      w[j] = units(g.weight((uint32_t)(lds.sorted[i] >> 32)));
+      bin[j] = g.bin((uint32_t)(lds.sorted[i] >> 32));
       in_p += bin[j] <= g.b.hi;
     }
     own += w[j];
@@ -726,8 +796,8 @@ template <typename T>
 __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goals &g, int chunks,
                                            int chunk_len, PickLds &lds) {
   const int tid = threadIdx.x;
-  uint64_t *mass = lds.sorted;
-  uint32_t *counts = reinterpret_cast<uint32_t *>(lds.sorted + 256);
+  uint64_t *mass = lds.mass;
+  uint32_t *counts = lds.counts;
   auto add = [](uint64_t x, uint64_t y) { return x + y; };
   auto key_at = [&](int v) { return key_of(clean(logit_value(logits[v]))); };
   Edge end = {0, 0, ~0ull >> 1};
@@ -746,7 +816,7 @@ __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goal
       sum = group_reduce<kPickThreads>(sum, add, lds.mpart);
       equal = group_reduce<kPickThreads>(equal, add, lds.mpart);
       if (end.key) sum += (equal < end.ties ? equal : end.ties) * units(g.weight(end.key));
-      goal = fmax(g.row.p * (g.row.k > 0 ? (double)sum : g.b.sum * kUnit), 0.5);
+      goal = fmax(g.row.p * (g.row.k > 0 ? (double)sum : g.all), 0.5);
     }
     uint32_t prefix = 0;
     uint64_t ahead = 0;
@@ -841,24 +911,29 @@ __device__ __forceinline__ Drawn draw_chunk(const V (&x)[4], float u) {
   return {__shfl(chunk, from), (double)__shfl(before, from), (double)total};
 }
 
+// The listed elements, by whom: calls take(chunk, entry) for each of them.
+template <typename Take>
+__device__ __forceinline__ void for_listed(const SampleArgs &a, int n, Take take) {
+  const int lane = threadIdx.x % kWave;
+  for (int c = threadIdx.x / kWave; c < a.chunks; c += kPickThreads / kWave) {
+    const int64_t at = (int64_t)n * a.chunks + c;
+    const uint32_t m = a.c_listed[at];
+    for (uint32_t j = lane; j < m; j += kWave) take(c, a.list[at * kListed + j]);
+  }
+}
+
 template <typename T, int kPer>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
   const int n = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const T *logits = static_cast<const T *>(a.logits) + n * a.row_stride;
   __shared__ PickLds lds;
-  constexpr int chunk_len = kThreads * kPer;
-  static_assert(kMaxChunks == 4 * kWave, "four chunks a lane");
+  constexpr int chunk_len = kWave * kPer;
 
   const Row row(a, n);
   const int64_t at = (int64_t)n * a.chunks + 4 * lane;
   const int mine = a.chunks - 4 * lane;               // of the lane's four chunks: how many are
-  float c_top[4], top = -__builtin_inff();
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c_top[i] = i < mine ? a.c_top[at + i] : -__builtin_inff();
-    top = fmaxf(top, c_top[i]);
-  }
-  top = wave_reduce(top, max_of);
+  float c_top[4], top;
+  load_tops(a, n, c_top, top);
   float u = a.uniform[n];
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
   if (top == -__builtin_inff() || row.greedy) {
@@ -880,14 +955,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   Drawn drawn;
   if (!row.filtered()) {
     double x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      x[i] = i < mine ? a.c_sum[at + i] * weight_exp(scaled(c_top[i], top, row.inv_t)) : 0.0;
+    load_sums(a, n, c_top, top, row.inv_t, x);
     drawn = draw_chunk(x, u);
   } else {
     b = a.ends[n];
-    const Goals g = {row, b};
-    const uint32_t cap = list_cap(kPer);
     uint32_t listed[4], first[4], count, longest = 0, high = 0, low = 0xffffffffu;
     uint64_t kept[4];
 #pragma unroll
@@ -908,64 +979,126 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     first[0] = wave_scan(listed[0] + listed[1] + listed[2] + listed[3], count);
 #pragma unroll
     for (int i = 1; i < 4; ++i) first[i] = first[i - 1] + listed[i - 1];
+    Border fine = b;                                  // of what is still in question
+    const double all = row.k > 0 ? (double)b.mass_k : b.sum * kUnit;
+    const Goals rough = {row, b, all, 0, -1};
+    Goals g = {row, fine, all, high, -1};
+    // `ties` of the equal elements `key`, listed[] and first[] of them in the chunks
+    auto split_ties = [&](uint32_t key, uint32_t of_them) {
+      const double e = g.weight(key);
+      const uint64_t w = units(e);
+      uint64_t ties = of_them;
+      if (g.ends_in_k()) ties = (uint64_t)row.k - fine.count_k < ties ? (uint64_t)row.k - fine.count_k : ties;
+      if (row.p < 1.0) ties = g.let_in(g.goal(g.ends_in_k() ? ties * w : 0), fine.mass_lo, w, ties);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint64_t left = ties > first[i] ? ties - first[i] : 0;
+        if (e >= row.m) kept[i] += (left < listed[i] ? left : listed[i]) * w;
+      }
+      end = {key, 0, ties};
+    };
+    const bool apart = rough.ends_in_k() && b.bin_k > b.hi;   // bin_k behind the others
     if (count == 0) {
       // everything in the bins is kept (min-p alone: everything)
       if (row.binned()) end.key = 0xffffffffu;
     } else if (high == low) {
       // equal elements, however many
-      const uint64_t w = units(g.weight(high));
-      uint64_t ties = count;
-      if (g.ends_in_k()) ties = (uint64_t)row.k - b.count_k < ties ? (uint64_t)row.k - b.count_k : ties;
-      if (row.p < 1.0) ties = g.let_in(g.goal(g.ends_in_k() ? ties * w : 0), b.mass_lo, w, ties);
-      const bool heavy = g.weight(high) >= row.m;
+      split_ties(high, count);
+      if (tid < kWave)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint64_t left = ties > first[i] ? ties - first[i] : 0;
-        if (heavy) kept[i] += (left < listed[i] ? left : listed[i]) * w;
-        if (tid < kWave) lds.ties_of[4 * lane + i] = listed[i];
-      }
-      end = {high, 0, ties};
-      __syncthreads();                                // ties_of
-    } else if (longest <= cap && count <= kMaxSorted) {
-      if (tid < kWave) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lds.kept_of[4 * lane + i] = kept[i];
-      }
-      if (count <= kWave) {
-        if (tid < kWave) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            for (uint32_t j = 0; j < listed[i]; ++j)
-              lds.sorted[first[i] + j] = a.list[(at + i) * cap + j];
-          __builtin_amdgcn_wave_barrier();
-          end = end_in_a_wave((uint32_t)lane < count ? lds.sorted[lane] : 0, g, chunk_len, lds);
-          if (lane == 0) lds.key = end.key, lds.ties = end.index;
-        }
-        __syncthreads();
-        end.key = lds.key, end.index = lds.ties;
-      } else {
-        // a wave a chunk
-        if (tid < kWave)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) lds.ties_of[4 * lane + i] = first[i];
-        __syncthreads();
-        for (int c = tid / kWave; c < a.chunks; c += kPickThreads / kWave) {
-          const int64_t c_at = (int64_t)n * a.chunks + c;
-          const uint32_t m = a.c_listed[c_at];
-          for (uint32_t j = lane; j < m; j += kWave)
-            lds.sorted[lds.ties_of[c] + j] = a.list[c_at * cap + j];
-        }
-        end = end_by_sorting(count, g, chunk_len, lds);
-        __syncthreads();
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) kept[i] = lds.kept_of[4 * lane + i];
-    } else {
-      end = end_by_passes(logits, a.V, g, a.chunks, chunk_len, lds);
+        for (int i = 0; i < 4; ++i) lds.ties_of[4 * lane + i] = listed[i];
+      __syncthreads();
+    } else if (longest > (uint32_t)kListed || (apart && count > (uint32_t)kMaxSorted)) {
+      end = end_by_passes(logits, a.V, rough, a.chunks, chunk_len, lds);
       b.lo = -1;                                      // the bins say nothing
       __syncthreads();
 #pragma unroll
       for (int i = 0; i < 4; ++i) kept[i] = i < mine ? lds.kept_of[4 * lane + i] : 0;
+    } else {
+      if (tid < kWave)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds.kept_of[4 * lane + i] = kept[i];
+      if (tid == 0) lds.count = 0, lds.high = 0, lds.low = 0xffffffffu;
+      uint32_t below = 0xffffffffu;                   // keys above it are kept if none listed is
+      if (count <= kWave || apart) {
+        __syncthreads();
+        for_listed(a, n, [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
+        __syncthreads();
+      } else {
+        // 512 bins of the listed keys' range, and the end's among them
+        const uint32_t span = high - low;
+        g.shift = span < (uint32_t)kBins ? 0 : 32 - __clz(span / kBins);
+        for (int i = tid; i < kBins; i += kPickThreads) lds.mass[i] = 0, lds.counts[i] = 0;
+        __syncthreads();
+        for_listed(a, n, [&](int, uint64_t x) {
+          const uint32_t key = (uint32_t)(x >> 32);
+          atomicAdd(&lds.counts[g.bin(key)], 1u);
+          atomicAdd((unsigned long long *)&lds.mass[g.bin(key)], (unsigned long long)units(g.weight(key)));
+        });
+        __syncthreads();
+        uint64_t m[kOwnBins];
+        uint32_t c[kOwnBins];
+#pragma unroll
+        for (int i = 0; i < kOwnBins; ++i)
+          m[i] = lds.mass[kOwnBins * lane + i], c[i] = lds.counts[kOwnBins * lane + i];
+        locate(m, c, b.mass_lo, b.count_lo, rough.ends_in_k(), (uint32_t)row.k, row.p, all, fine);
+        if (fine.lo > 0) below = high - ((uint32_t)fine.lo << g.shift);
+        for_listed(a, n, [&](int chunk, uint64_t x) {
+          const uint32_t key = (uint32_t)(x >> 32);
+          const int bin = g.bin(key);
+          if (bin < fine.lo) {
+            const double e = g.weight(key);
+            if (e >= row.m)
+              atomicAdd((unsigned long long *)&lds.kept_of[chunk], (unsigned long long)units(e));
+          } else if (bin <= fine.hi || bin == fine.bin_k) {
+            const uint32_t slot = atomicAdd(&lds.count, 1u);
+            if (slot < (uint32_t)kMaxSorted) lds.sorted[slot] = x;
+            atomicMax(&lds.high, key);
+            atomicMin(&lds.low, key);
+          }
+        });
+        __syncthreads();
+        count = lds.count;
+        high = lds.high;
+        low = lds.low;
+      }
+      if (count > 0 && high == low) {
+        if (tid < kMaxChunks) lds.ties_of[tid] = 0;
+        __syncthreads();
+        for_listed(a, n, [&](int chunk, uint64_t x) {
+          if ((uint32_t)(x >> 32) == high) atomicAdd(&lds.ties_of[chunk], 1u);
+        });
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          listed[i] = lds.ties_of[4 * lane + i];
+          kept[i] = lds.kept_of[4 * lane + i];
+        }
+        first[0] = wave_scan(listed[0] + listed[1] + listed[2] + listed[3], count);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) first[i] = first[i - 1] + listed[i - 1];
+        split_ties(high, count);
+      } else if (count > (uint32_t)kMaxSorted) {
+        end = end_by_passes(logits, a.V, rough, a.chunks, chunk_len, lds);
+        b.lo = -1;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kept[i] = i < mine ? lds.kept_of[4 * lane + i] : 0;
+      } else {
+        if (count <= kWave) {
+          if (tid < kWave) {
+            end = end_in_a_wave((uint32_t)lane < count ? lds.sorted[lane] : 0, g, chunk_len, lds);
+            if (lane == 0) lds.key = end.key, lds.ties = end.index;
+          }
+          __syncthreads();
+          end.key = lds.key, end.index = lds.ties;
+        } else {
+          end = end_by_sorting(count, g, chunk_len, lds);
+        }
+        if (end.key == 0xffffffffu) end = {below, 0, below == 0xffffffffu ? kByIndex : 0};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) kept[i] = lds.kept_of[4 * lane + i];
+      }
     }
     drawn = draw_chunk(kept, u);
   }
@@ -982,7 +1115,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) equal += v0 + i < a.V && key_of(z[i]) == end.key;
     seen = group_scan<kPickThreads>(equal, all, lds.mpart);
-    for (int c = 0; c < drawn.chunk; ++c) seen += lds.ties_of[c];
+    if (end.ties > 0)
+      for (int c = 0; c < drawn.chunk; ++c) seen += lds.ties_of[c];
   }
   double w[kOwn], own = 0.0, all;
 #pragma unroll
@@ -1026,23 +1160,26 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   }
 }
 
-// Elements a thread holds of a chunk: 32 (chunks of 8,192); 8 where the call has too few
-// chunks of that size to fill the GPU, the rows still fit kMaxChunks and a load is one.
+// Elements a lane holds of a chunk: 32 (chunks of 2,048), or 16 or 8 where the call would
+// have too few workgroups to fill the GPU and the row's chunks still fit.
 int32_t sample_per(int32_t N, int32_t V) {
-  const int64_t chunks = ((int64_t)V + kThreads * 32 - 1) / (kThreads * 32) * N;
-  return chunks < 512 ? 8 : 32;
+  for (int32_t per = 32;; per /= 2) {
+    const int64_t chunks = ((int64_t)V + kWave * per - 1) / (kWave * per);
+    const bool halved_fits = ((int64_t)V + kWave * per / 2 - 1) / (kWave * per / 2) <= kMaxChunks;
+    if (per == 8 || !halved_fits || N * chunks >= 2 * kGroup * 256) return per;
+  }
 }
 
 struct SampleLayout {
   int32_t per, chunks;
-  size_t c_top, c_low, t_top, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_keys, list;
+  size_t c_top, c_low, l_top, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_keys, list;
   size_t border, ends;
   size_t bytes;
 };
 SampleLayout sample_layout(int32_t N, int32_t V) {
   SampleLayout l;
   l.per = sample_per(N, V);
-  l.chunks = (V + kThreads * l.per - 1) / (kThreads * l.per);
+  l.chunks = (V + kWave * l.per - 1) / (kWave * l.per);
   const size_t parts = (size_t)N * l.chunks;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1052,7 +1189,7 @@ SampleLayout sample_layout(int32_t N, int32_t V) {
   };
   l.c_top = take(parts * 4);
   l.c_low = take(parts * 4);
-  l.t_top = take(parts * kThreads * 4);
+  l.l_top = take(parts * kWave * 4);
   l.c_first = take(parts * 4);
   l.c_sum = take(parts * 8);
   l.bin_mass = take((size_t)N * kBins * 8);
@@ -1060,7 +1197,7 @@ SampleLayout sample_layout(int32_t N, int32_t V) {
   l.c_kept = take(parts * 8);
   l.c_listed = take(parts * 4);
   l.c_keys = take(parts * 8);
-  l.list = take(parts * list_cap(l.per) * 8);
+  l.list = take(parts * kListed * 8);
   l.border = take((size_t)N * sizeof(Border));
   l.ends = take((size_t)N * sizeof(Border));
   l.bytes = at;
@@ -1069,7 +1206,7 @@ SampleLayout sample_layout(int32_t N, int32_t V) {
 
 template <typename T, int kPer>
 void launch_passes(const SampleArgs &a, hipStream_t stream) {
-  const dim3 grid((unsigned)a.N * (unsigned)a.chunks);
+  const dim3 grid((unsigned)a.N * (unsigned)a.groups);
   const bool bins = a.top_k || a.top_p;
   hipLaunchKernelGGL((sample_stats_kernel<T, kPer>), grid, dim3(kThreads), 0, stream, a);
   if (bins || a.min_p)
@@ -1103,7 +1240,7 @@ hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, in
   a.N = N;
   a.V = V;
   a.chunks = l.chunks;
-  a.per = l.per;
+  a.groups = (l.chunks + kGroup - 1) / kGroup;
   a.c_top = reinterpret_cast<float *>(ws + l.c_top);
   a.c_low = reinterpret_cast<float *>(ws + l.c_low);
   a.c_first = reinterpret_cast<uint32_t *>(ws + l.c_first);
@@ -1114,20 +1251,22 @@ hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, in
   a.c_listed = reinterpret_cast<uint32_t *>(ws + l.c_listed);
   a.c_keys = reinterpret_cast<uint32_t *>(ws + l.c_keys);
   a.list = reinterpret_cast<uint64_t *>(ws + l.list);
-  a.t_top = reinterpret_cast<float *>(ws + l.t_top);
+  a.l_top = reinterpret_cast<float *>(ws + l.l_top);
   a.border = reinterpret_cast<Border *>(ws + l.border);
   a.ends = reinterpret_cast<Border *>(ws + l.ends);
-  if (bf16) {
-    if (l.per == 8)
-      launch_passes<uint16_t, 8>(a, stream);
+  auto launch = [&](auto per) {
+    constexpr int kPer = decltype(per)::value;
+    if (bf16)
+      launch_passes<uint16_t, kPer>(a, stream);
     else
-      launch_passes<uint16_t, 32>(a, stream);
-  } else {
-    if (l.per == 8)
-      launch_passes<float, 8>(a, stream);
-    else
-      launch_passes<float, 32>(a, stream);
-  }
+      launch_passes<float, kPer>(a, stream);
+  };
+  if (l.per == 8)
+    launch(std::integral_constant<int, 8>());
+  else if (l.per == 16)
+    launch(std::integral_constant<int, 16>());
+  else
+    launch(std::integral_constant<int, 32>());
   return hipGetLastError();
 }
 
