@@ -96,6 +96,18 @@ __device__ __forceinline__ uint64_t units(double e) { return (uint64_t)(e * kUni
 // scalar registers, where an addend costs no move.
 constexpr int kExpTable = 128;
 constexpr double kStep = 0.6931471805599453 / kExpTable;
+struct Pow2Table {
+  double at[kExpTable];
+  constexpr Pow2Table() : at() {
+    for (int j = 0; j < kExpTable; ++j) {
+      double sum = 0.0;                              // the Taylor series from its small end
+      for (int i = 20; i > 0; --i) sum = (sum + 1.0) * (j * kStep) / i;
+      at[j] = 1.0 + sum;
+    }
+  }
+};
+__constant__ Pow2Table kPow2 = Pow2Table();
+
 struct TableExp {
   const double *table;
   double scale, low, round, c1, c2, c3, c4;
@@ -113,9 +125,9 @@ struct TableExp {
     double p = __builtin_fma(c4, f, c3);
     p = __builtin_fma(p, f, c2);
     p = __builtin_fma(p, f, c1);
-    const uint64_t pow2 = __builtin_bit_cast(uint64_t, table[n & (kExpTable - 1)]) +
-                          ((uint64_t)(uint32_t)(n >> 7 << 20) << 32);
-    const double e = __builtin_bit_cast(double, pow2);
+    const uint64_t pow2 = __builtin_bit_cast(uint64_t, table[n & (kExpTable - 1)]);
+    const uint32_t high = (uint32_t)(pow2 >> 32) + ((uint32_t)(n >> 7) << 20);   // times 2^(n / 128)
+    const double e = __builtin_bit_cast(double, (uint64_t)high << 32 | (uint32_t)pow2);
     return __builtin_fma(e, p * f, e);
   }
 };
@@ -168,17 +180,22 @@ struct Row {
 // Where a row's kept prefix ends: bins before `lo` are kept; the end is in lo .. hi, or (no
 // top-p) in bin_k = lo = hi; with top-k and top-p, what top-k keeps of bin_k also decides.
 struct Border {
-  double inv_t, bin_scale, sum;         // bins an exp, sum of the weights (top-p alone)
-  float top;
+  double sum;                           // of the weights (top-p alone)
+  float top, rate;                      // largest logit; bins a unit of logit
   int lo, hi, bin_k;                    // kBins: none
   uint32_t count_lo, count_k;           // elements before bin lo, bin_k
   uint64_t mass_lo, mass_k;             // weights before them
 };
 
-// The bin of a logit: non-decreasing as z falls. kBins: beyond.
-__device__ __forceinline__ int bin_of(double x, double bin_scale) {
-  const double b = -x * bin_scale;
+// The bin of a logit, `below` under the largest one: non-decreasing in it. kBins: beyond.
+__device__ __forceinline__ int bin_of(float below, float rate) {
+  const float b = below * rate;
   return b < kBins ? (int)b : kBins;
+}
+__device__ __forceinline__ float below(float top, float z) { return z == top ? 0.f : top - z; }
+// Bins a unit of logit, for a range of (M - z) / T. The slack takes in what rounds past it.
+__device__ __forceinline__ float rate_of(double range, double inv_t) {
+  return (float)fmin(inv_t * (kBins / (fmax(range, 1e-30) * (1.0 + 1e-6))), 0x1.fp127);
 }
 
 // ---- reductions over a workgroup, in a fixed order ----
@@ -238,7 +255,8 @@ __device__ __forceinline__ V wave_scan(V x, V &total) {
 __device__ __forceinline__ float max_of(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ float min_of(float a, float b) { return fminf(a, b); }
 
-// Chunk c's logits of a lane: vectors lane, lane + kWave, ...; -inf past the row.
+// Chunk c's logits of a lane: vectors lane, lane + kWave, ...; -inf past the row. NaN stays:
+// no comparison takes it in.
 template <typename T, int kPer>
 __device__ __forceinline__ void load_chunk(const SampleArgs &a, int n, int c, float (&z)[kPer]) {
   constexpr int kVec = kVector<T>;
@@ -264,9 +282,17 @@ __device__ __forceinline__ void load_chunk(const SampleArgs &a, int n, int c, fl
       z[i] = v < a.V ? logit_value(row[v]) : -__builtin_inff();
     }
   }
-#pragma unroll
-  for (int i = 0; i < kPer; ++i) z[i] = clean(z[i]);
 }
+// Where logits are weighed from: the largest, or 0 once those at +inf are at 0 and the rest
+// at -inf.
+template <int kPer>
+__device__ __forceinline__ float flatten(float (&z)[kPer], float top) {
+  if (top < __builtin_inff()) return top;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) z[i] = z[i] == top ? 0.f : -__builtin_inff();
+  return 0.f;
+}
+
 // The index of a lane's i-th logit.
 template <typename T, int kPer>
 __device__ __forceinline__ int index_of(int c, int i) {
@@ -274,11 +300,9 @@ __device__ __forceinline__ int index_of(int c, int i) {
   return c * kWave * kPer + (i / kVec * kWave + (int)(threadIdx.x % kWave)) * kVec + i % kVec;
 }
 
-// 2^(j / kExpTable) for TableExp, by the workgroup's threads.
+// 2^(j / kExpTable) for TableExp; there by the next barrier.
 __device__ __forceinline__ void fill_table(double *table) {
-  for (int i = threadIdx.x; i < kExpTable; i += blockDim.x)
-    table[i] = 2.0 * weight_exp((i - kExpTable) * kStep);
-  __syncthreads();
+  if (threadIdx.x < kExpTable) table[threadIdx.x] = kPow2.at[threadIdx.x];
 }
 
 template <typename T, int kPer>
@@ -287,13 +311,16 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
   const int c = blockIdx.x % a.groups * kGroup + threadIdx.x / kWave;
   __shared__ double table[kExpTable];
   const Row row(a, n);
-  if (row.needs_sums()) fill_table(table);
+  if (row.needs_sums()) {
+    fill_table(table);
+    __syncthreads();
+  }
   if (c >= a.chunks) return;
   float z[kPer];
   load_chunk<T, kPer>(a, n, c, z);
-  float mine = z[0];
+  float mine = -__builtin_inff();
 #pragma unroll
-  for (int i = 1; i < kPer; ++i) mine = fmaxf(mine, z[i]);
+  for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, z[i]);
   const float top = wave_reduce(mine, max_of);
   const int64_t at = (int64_t)n * a.chunks + c;
   if (lane == 0) a.c_top[at] = top;
@@ -317,13 +344,9 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
     double sum = 0.0;
     if (top > -__builtin_inff()) {
       const TableExp weight(table, row.inv_t);
-      const bool infinite = top == __builtin_inff();   // those at it share the weight
-      const double from = infinite ? 0.0 : (double)top;
+      const double from = flatten(z, top);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        if (infinite) z[i] = z[i] == top ? 0.f : -__builtin_inff();
-        sum += weight((double)z[i] - from);
-      }
+      for (int i = 0; i < kPer; ++i) sum += weight((double)z[i] - from);
     }
     sum = wave_reduce(sum, [](double x, double y) { return x + y; });
     if (lane == 0) a.c_sum[at] = sum;
@@ -362,7 +385,6 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
   const int64_t at = (int64_t)n * a.chunks;
   float c_top[4];
   Border b = Border();
-  b.inv_t = row.inv_t;
   load_tops(a, n, c_top, b.top);
   double range = kRange;
   if (row.binned()) {
@@ -379,12 +401,17 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
       // the k-th of the lanes' largest logits, as far as a bin tells
       count[tid] = 0;
       __syncthreads();
-      const double scale = kBins / (fmax(range, 1e-30) * (1.0 + 1e-9));
-      const int parts = a.chunks * kWave;
+      const float rate = rate_of(range, row.inv_t);
+      const int parts = a.chunks * kWave / 4;
+      const f32x4 *l_top = reinterpret_cast<const f32x4 *>(a.l_top + at * kWave);
 #pragma unroll 4
       for (int i = tid; i < parts; i += kRowThreads) {
-        const int bin = bin_of(scaled(a.l_top[at * kWave + i], b.top, row.inv_t), scale);
-        if (bin < kBins) atomicAdd(&count[bin], 1u);
+        const f32x4 z = l_top[i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int bin = bin_of(below(b.top, z[e]), rate);
+          if (bin < kBins) atomicAdd(&count[bin], 1u);
+        }
       }
       __syncthreads();
       constexpr int kOwn = kBins / kWave;
@@ -399,7 +426,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
         before += c[i];
       }
       bin = wave_reduce(bin, [](int x, int y) { return min(x, y); });
-      if (bin < kBins) range = fmin(range, (bin + 1) / scale * (1.0 + 1e-9));
+      if (bin < kBins) range = fmin(range, (bin + 1) / (double)rate * row.inv_t * (1.0 + 1e-6));
     } else {
       double x[4];
       load_sums(a, n, c_top, b.top, row.inv_t, x);
@@ -409,29 +436,43 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
   } else {
     range = fmin(range, -log(row.m) + 1e-12);
   }
-  // the last element falls into the last bin
-  b.bin_scale = kBins / (fmax(range, 1e-30) * (1.0 + 1e-9));
+  b.rate = rate_of(range, row.inv_t);
   if (tid == 0) a.border[n] = b;
 }
 
+// The weight of a logit in the row's range.
+struct Weigh {
+  TableExp exp;
+  double top;
+  bool infinite;
+  __device__ __forceinline__ Weigh(const double *table, double inv_t, float t)
+      : exp(table, inv_t), top((double)t), infinite(t == __builtin_inff()) {}
+  __device__ __forceinline__ double operator()(float z) const {
+    return infinite ? 1.0 : exp((double)z - top);
+  }
+};
+
 // Whether a logit is in the row's range.
 __device__ __forceinline__ bool in_range(const Border &b, float z) {
-  return bin_of(scaled(z, b.top, b.inv_t), b.bin_scale) < kBins;
+  return bin_of(below(b.top, z), b.rate) < kBins;
 }
 
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   const int n = blockIdx.x / a.groups, tid = threadIdx.x, lane = tid % kWave;
   const int c0 = blockIdx.x % a.groups * kGroup, c = c0 + tid / kWave;
-  const Row row(a, n);
-  if (!row.binned()) return;
-  const Border b = a.border[n];
-  if (b.top == -__builtin_inff()) return;
   const int64_t at = (int64_t)n * a.chunks + c0;
+  const Border b = a.border[n];
+  float c_top[kGroup];
+#pragma unroll
+  for (int i = 0; i < kGroup; ++i) c_top[i] = c0 + i < a.chunks ? a.c_top[at + i] : -__builtin_inff();
+  const float l_top = c < a.chunks ? a.l_top[((int64_t)n * a.chunks + c) * kWave + lane] : 0.f;
+  const Row row(a, n);
+  if (!row.binned() || b.top == -__builtin_inff()) return;
   bool any = false, mine = false;
 #pragma unroll
   for (int i = 0; i < kGroup; ++i) {
-    const bool in = c0 + i < a.chunks && in_range(b, a.c_top[at + i]);
+    const bool in = in_range(b, c_top[i]);
     any |= in;
     mine = c == c0 + i ? in : mine;
   }
@@ -440,19 +481,19 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   __shared__ uint32_t count[kBins];
   __shared__ double table[kExpTable];
   for (int i = tid; i < kBins; i += kThreads) mass[i] = 0, count[i] = 0;
-  fill_table(table);
-  if (mine && in_range(b, a.l_top[((int64_t)n * a.chunks + c) * kWave + lane])) {
+  if (row.p < 1.0) fill_table(table);
+  __syncthreads();
+  if (mine && in_range(b, l_top)) {
     float z[kPer];
     load_chunk<T, kPer>(a, n, c, z);
-    const TableExp weight(table, row.inv_t);
+    const Weigh weigh(table, row.inv_t, b.top);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int bin = bin_of(scaled(z[i], b.top, b.inv_t), b.bin_scale);
+      const int bin = bin_of(below(b.top, z[i]), b.rate);
       if (bin < kBins) {
         if (row.k > 0) atomicAdd(&count[bin], 1u);
         if (row.p < 1.0)
-          atomicAdd((unsigned long long *)&mass[bin],
-                    (unsigned long long)units(weight(z[i] == b.top ? 0.0 : (double)z[i] - (double)b.top)));
+          atomicAdd((unsigned long long *)&mass[bin], (unsigned long long)units(weigh(z[i])));
       }
     }
   }
@@ -552,22 +593,22 @@ template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   const int n = blockIdx.x / a.groups, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int c0 = blockIdx.x % a.groups * kGroup, c = c0 + wave;
-  const Row row(a, n);
-  if (!row.filtered()) return;
-  Border b = a.border[n];
-  if (b.top == -__builtin_inff()) return;
   const int64_t at = (int64_t)n * a.chunks + c;
+  Border b = a.border[n];
+  const float c_top = c < a.chunks ? a.c_top[at] : -__builtin_inff();
+  const float l_top = c < a.chunks ? a.l_top[at * kWave + lane] : -__builtin_inff();
+  const Row row(a, n);
+  if (!row.filtered() || b.top == -__builtin_inff()) return;
   __shared__ double table[kExpTable];
   __shared__ uint32_t s_listed[kGroup];
-  if (lane == 0) s_listed[wave] = 0;
-  const float c_top = c < a.chunks ? a.c_top[at] : -__builtin_inff();
-  if (__syncthreads_or(in_range(b, c_top))) fill_table(table);   // each wave has its own counter
+  if (lane == 0) s_listed[wave] = 0;      // each wave has its own
+  fill_table(table);
+  __syncthreads();
   if (c >= a.chunks) return;
   if (!in_range(b, c_top)) {
     if (lane == 0) a.c_kept[at] = 0, a.c_listed[at] = 0;
     return;
   }
-  const float l_top = a.l_top[at * kWave + lane];
   if (row.binned()) {
     find_border(a, n, row, b);
   } else {
@@ -578,12 +619,12 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   if (in_range(b, l_top)) {
     float z[kPer];
     load_chunk<T, kPer>(a, n, c, z);
-    const TableExp weight(table, row.inv_t);
+    const Weigh weigh(table, row.inv_t, b.top);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int bin = bin_of(scaled(z[i], b.top, b.inv_t), b.bin_scale);
+      const int bin = bin_of(below(b.top, z[i]), b.rate);
       if (bin < b.lo) {
-        const double e = weight(z[i] == b.top ? 0.0 : (double)z[i] - (double)b.top);
+        const double e = weigh(z[i]);
         if (e >= row.m) kept += units(e);
       } else if (bin < kBins && (bin <= b.hi || bin == b.bin_k)) {
         const uint32_t slot = atomicAdd(&s_listed[wave], 1u), key = key_of(z[i]);
@@ -642,6 +683,7 @@ struct PickLds {
   uint32_t counts[kBins];
   uint64_t kept_of[kMaxChunks];         // weight kept of each chunk
   uint32_t ties_of[kMaxChunks];         // of each chunk: elements at the edge
+  uint32_t first_of[kMaxChunks];        // and where its listed elements start
   uint64_t mpart[kPickThreads / kWave];
   double dpart[kPickThreads / kWave];
   uint32_t cpart[kPickThreads / kWave];
@@ -667,7 +709,7 @@ struct Goals {
   int shift;                            // and their width; < 0: the row's bins
   __device__ __forceinline__ int bin(uint32_t key) const {
     if (shift >= 0) return (int)((high - key) >> shift);
-    return bin_of(scaled(value_of(key), b.top, row.inv_t), b.bin_scale);
+    return bin_of(below(b.top, value_of(key)), b.rate);
   }
   __device__ __forceinline__ double weight(uint32_t key) const {
     return weight_exp(scaled(value_of(key), b.top, row.inv_t));
@@ -911,14 +953,17 @@ __device__ __forceinline__ Drawn draw_chunk(const V (&x)[4], float u) {
   return {__shfl(chunk, from), (double)__shfl(before, from), (double)total};
 }
 
-// The listed elements, by whom: calls take(chunk, entry) for each of them.
+// Calls take(chunk, entry) for every listed element; first_of: where each chunk's start.
 template <typename Take>
-__device__ __forceinline__ void for_listed(const SampleArgs &a, int n, Take take) {
-  const int lane = threadIdx.x % kWave;
-  for (int c = threadIdx.x / kWave; c < a.chunks; c += kPickThreads / kWave) {
-    const int64_t at = (int64_t)n * a.chunks + c;
-    const uint32_t m = a.c_listed[at];
-    for (uint32_t j = lane; j < m; j += kWave) take(c, a.list[at * kListed + j]);
+__device__ __forceinline__ void for_listed(const SampleArgs &a, int n, uint32_t count,
+                                           const uint32_t *first_of, Take take) {
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < count; i += kPickThreads) {
+    int c = 0;                            // the last chunk that starts at or before i
+#pragma unroll
+    for (int step = kMaxChunks / 2; step > 0; step /= 2)
+      if (first_of[c + step] <= i) c += step;
+    take(c, a.list[((int64_t)n * a.chunks + c) * kListed + (i - first_of[c])]);
   }
 }
 
@@ -1017,12 +1062,13 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     } else {
       if (tid < kWave)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds.kept_of[4 * lane + i] = kept[i];
+        for (int i = 0; i < 4; ++i) lds.kept_of[4 * lane + i] = kept[i], lds.first_of[4 * lane + i] = first[i];
+      const uint32_t listed_all = count;
       if (tid == 0) lds.count = 0, lds.high = 0, lds.low = 0xffffffffu;
       uint32_t below = 0xffffffffu;                   // keys above it are kept if none listed is
       if (count <= kWave || apart) {
         __syncthreads();
-        for_listed(a, n, [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
+        for_listed(a, n, listed_all, lds.first_of, [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
         __syncthreads();
       } else {
         // 512 bins of the listed keys' range, and the end's among them
@@ -1030,7 +1076,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
         g.shift = span < (uint32_t)kBins ? 0 : 32 - __clz(span / kBins);
         for (int i = tid; i < kBins; i += kPickThreads) lds.mass[i] = 0, lds.counts[i] = 0;
         __syncthreads();
-        for_listed(a, n, [&](int, uint64_t x) {
+        for_listed(a, n, listed_all, lds.first_of, [&](int, uint64_t x) {
           const uint32_t key = (uint32_t)(x >> 32);
           atomicAdd(&lds.counts[g.bin(key)], 1u);
           atomicAdd((unsigned long long *)&lds.mass[g.bin(key)], (unsigned long long)units(g.weight(key)));
@@ -1043,7 +1089,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
           m[i] = lds.mass[kOwnBins * lane + i], c[i] = lds.counts[kOwnBins * lane + i];
         locate(m, c, b.mass_lo, b.count_lo, rough.ends_in_k(), (uint32_t)row.k, row.p, all, fine);
         if (fine.lo > 0) below = high - ((uint32_t)fine.lo << g.shift);
-        for_listed(a, n, [&](int chunk, uint64_t x) {
+        for_listed(a, n, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
           const uint32_t key = (uint32_t)(x >> 32);
           const int bin = g.bin(key);
           if (bin < fine.lo) {
@@ -1065,7 +1111,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       if (count > 0 && high == low) {
         if (tid < kMaxChunks) lds.ties_of[tid] = 0;
         __syncthreads();
-        for_listed(a, n, [&](int chunk, uint64_t x) {
+        for_listed(a, n, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
           if ((uint32_t)(x >> 32) == high) atomicAdd(&lds.ties_of[chunk], 1u);
         });
         __syncthreads();
@@ -1127,7 +1173,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       const uint32_t key = key_of(z[i]);
       const bool tied = key == end.key && (end.ties == kByIndex ? (uint32_t)(v0 + i) <= end.index
                                                                 : seen++ < end.ties);
-      const bool sure = b.lo >= 0 && (!row.binned() || bin_of(x, b.bin_scale) < b.lo);
+      const bool sure = b.lo >= 0 && (!row.binned() || bin_of(below(top, z[i]), b.rate) < b.lo);
       in = key > end.key || tied || sure;
     }
     const double e = in ? weight_exp(x) : 0.0;
