@@ -150,23 +150,30 @@ struct SampleArgs {
   uint32_t *bin_count;                  // [N][kBins]
   uint64_t *c_kept;                     // [N][chunks] weight kept for certain
   uint32_t *c_listed;                   // [N][chunks] elements in the border's bins
-  uint32_t *c_keys;                     // [N][chunks][2] their largest and smallest key
+  uint32_t *c_high, *c_lowest;          // [N][chunks] their largest and smallest key
   uint64_t *list;                       // [N][chunks][kListed] key << 32 | ~index
   struct Border *border, *ends;         // [N] with the range; with the end's bins too
 };
 
-// What a row asks for.
+// What a row asks for. The four loads go out together: a parameter that is not given is read
+// from kNotGiven instead of being branched around.
+struct NotGiven {
+  float temperature, top_p, min_p;
+  int32_t top_k;
+};
+__constant__ NotGiven kNotGiven = {1.f, 1.f, 0.f, 0};
 struct Row {
   double inv_t, p, m;                   // p < 1: top-p, m > 0: min-p
   int k;                                // 0: no top-k
   bool greedy;
   __device__ __forceinline__ Row(const SampleArgs &a, int n) {
-    const float t = a.temperature ? a.temperature[n] : 1.f;
+    const float t = *(a.temperature ? a.temperature + n : &kNotGiven.temperature);
+    const float tp = *(a.top_p ? a.top_p + n : &kNotGiven.top_p);
+    const float mp = *(a.min_p ? a.min_p + n : &kNotGiven.min_p);
+    k = *(a.top_k ? a.top_k + n : &kNotGiven.top_k);
     greedy = !(t > 0.f);
     inv_t = 1.0 / (double)t;
-    k = a.top_k ? a.top_k[n] : 0;
     if (k < 0 || k >= a.V) k = 0;
-    const float tp = a.top_p ? a.top_p[n] : 1.f, mp = a.min_p ? a.min_p[n] : 0.f;
     p = tp < 1.f ? (double)tp : 1.0;
     m = mp > 0.f ? (double)fminf(mp, 1.f) : 0.0;
   }
@@ -353,27 +360,19 @@ __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
   }
 }
 
-// A row's chunks, four a lane, for every wave by itself.
-__device__ __forceinline__ void load_tops(const SampleArgs &a, int n, float (&c_top)[4], float &top) {
-  const int lane = threadIdx.x % kWave;
-  static_assert(kMaxChunks == 4 * kWave, "four chunks a lane");
-  top = -__builtin_inff();
+// A value of a lane's i-th of four chunks, for every wave by itself: read whether there is
+// such a chunk or not (the last one instead), so that the loads go out together.
+static_assert(kMaxChunks == 4 * kWave, "four chunks a lane");
+template <typename V>
+__device__ __forceinline__ void load_four(const V *of_row, int chunks, V none, V (&x)[4]) {
+  const int c = 4 * (threadIdx.x % kWave);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    c_top[i] = 4 * lane + i < a.chunks ? a.c_top[(int64_t)n * a.chunks + 4 * lane + i] : -__builtin_inff();
-    top = fmaxf(top, c_top[i]);
-  }
-  top = wave_reduce(top, max_of);
+  for (int i = 0; i < 4; ++i) x[i] = of_row[min(c + i, chunks - 1)];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = c + i < chunks ? x[i] : none;
 }
-// Their sums of weights against the row's largest logit.
-__device__ __forceinline__ void load_sums(const SampleArgs &a, int n, const float (&c_top)[4], float top,
-                                          double inv_t, double (&x)[4]) {
-  const int lane = threadIdx.x % kWave;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    x[i] = 4 * lane + i < a.chunks ? a.c_sum[(int64_t)n * a.chunks + 4 * lane + i] *
-                                         weight_exp(scaled(c_top[i], top, inv_t))
-                                   : 0.0;
+__device__ __forceinline__ float top_of(const float (&c_top)[4]) {
+  return wave_reduce(fmaxf(fmaxf(c_top[0], c_top[1]), fmaxf(c_top[2], c_top[3])), max_of);
 }
 
 // Ranges of rows with filters; their bins start at zero.
@@ -383,19 +382,19 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
   if (!row.filtered()) return;
   __shared__ uint32_t count[kBins];
   const int64_t at = (int64_t)n * a.chunks;
-  float c_top[4];
+  float c_top[4], c_low[4];
+  load_four(a.c_top + at, a.chunks, -__builtin_inff(), c_top);
+  if (row.binned()) load_four(a.c_low + at, a.chunks, __builtin_inff(), c_low);
+  double c_sum[4];
+  if (row.needs_sums()) load_four(a.c_sum + at, a.chunks, 0.0, c_sum);
   Border b = Border();
-  load_tops(a, n, c_top, b.top);
+  b.top = top_of(c_top);
   double range = kRange;
   if (row.binned()) {
     static_assert(kRowThreads == kBins, "a bin a thread");
     a.bin_mass[(int64_t)n * kBins + tid] = 0;
     a.bin_count[(int64_t)n * kBins + tid] = 0;
-    float low = __builtin_inff();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * lane + i < a.chunks) low = fminf(low, a.c_low[at + 4 * lane + i]);
-    low = wave_reduce(low, min_of);
+    const float low = wave_reduce(fminf(fminf(c_low[0], c_low[1]), fminf(c_low[2], c_low[3])), min_of);
     range = fmin(range, -scaled(fminf(low, b.top), b.top, row.inv_t));
     if (row.k > 0) {
       // the k-th of the lanes' largest logits, as far as a bin tells
@@ -428,9 +427,10 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
       bin = wave_reduce(bin, [](int x, int y) { return min(x, y); });
       if (bin < kBins) range = fmin(range, (bin + 1) / (double)rate * row.inv_t * (1.0 + 1e-6));
     } else {
-      double x[4];
-      load_sums(a, n, c_top, b.top, row.inv_t, x);
-      b.sum = wave_reduce(x[0] + x[1] + x[2] + x[3], [](double u, double v) { return u + v; });
+      double x = 0.0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x += c_sum[i] * weight_exp(scaled(c_top[i], b.top, row.inv_t));
+      b.sum = wave_reduce(x, [](double u, double v) { return u + v; });
       if (row.p > 0.0) range = fmin(range, log((double)a.V / ((1.0 - row.p) * b.sum)) + 1e-3);
     }
   } else {
@@ -645,8 +645,8 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   if (lane == 0) {
     a.c_kept[at] = kept;
     a.c_listed[at] = listed;
-    a.c_keys[2 * at] = high;
-    a.c_keys[2 * at + 1] = low;
+    a.c_high[at] = high;
+    a.c_lowest[at] = low;
     if (c_top == b.top) a.ends[n] = b;    // one of the chunks that hold it: all write the same
   }
 }
@@ -977,9 +977,23 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   const Row row(a, n);
   const int64_t at = (int64_t)n * a.chunks + 4 * lane;
   const int mine = a.chunks - 4 * lane;               // of the lane's four chunks: how many are
-  float c_top[4], top;
-  load_tops(a, n, c_top, top);
+  float c_top[4];
+  double c_sum[4];
+  uint32_t listed[4], key_high[4], key_low[4];
+  uint64_t kept[4];
+  load_four(a.c_top + (at - 4 * lane), a.chunks, -__builtin_inff(), c_top);
   float u = a.uniform[n];
+  Border b = Border();
+  if (row.filtered()) {
+    load_four(a.c_listed + (at - 4 * lane), a.chunks, 0u, listed);
+    load_four(a.c_high + (at - 4 * lane), a.chunks, 0u, key_high);
+    load_four(a.c_lowest + (at - 4 * lane), a.chunks, 0xffffffffu, key_low);
+    load_four(a.c_kept + (at - 4 * lane), a.chunks, (uint64_t)0, kept);
+    b = a.ends[n];
+  } else if (!row.greedy) {
+    load_four(a.c_sum + (at - 4 * lane), a.chunks, 0.0, c_sum);
+  }
+  const float top = top_of(c_top);
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
   if (top == -__builtin_inff() || row.greedy) {
     int first = a.V;
@@ -996,24 +1010,18 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   }
 
   Edge end = {0, 0, kByIndex};                        // everything
-  Border b = Border();
   Drawn drawn;
   if (!row.filtered()) {
-    double x[4];
-    load_sums(a, n, c_top, top, row.inv_t, x);
-    drawn = draw_chunk(x, u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c_sum[i] *= weight_exp(scaled(c_top[i], top, row.inv_t));
+    drawn = draw_chunk(c_sum, u);
   } else {
-    b = a.ends[n];
-    uint32_t listed[4], first[4], count, longest = 0, high = 0, low = 0xffffffffu;
-    uint64_t kept[4];
+    uint32_t first[4], count, longest = 0, high = 0, low = 0xffffffffu;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      listed[i] = i < mine ? a.c_listed[at + i] : 0;
-      kept[i] = i < mine ? a.c_kept[at + i] : 0;
-      if (listed[i]) {
-        const uint32_t kh = a.c_keys[2 * (at + i)], kl = a.c_keys[2 * (at + i) + 1];
-        high = kh > high ? kh : high;
-        low = kl < low ? kl : low;
+      if (listed[i]) {                                // only then are there keys
+        high = key_high[i] > high ? key_high[i] : high;
+        low = key_low[i] < low ? key_low[i] : low;
         longest = listed[i] > longest ? listed[i] : longest;
       }
     }
@@ -1218,7 +1226,7 @@ int32_t sample_per(int32_t N, int32_t V) {
 
 struct SampleLayout {
   int32_t per, chunks;
-  size_t c_top, c_low, l_top, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_keys, list;
+  size_t c_top, c_low, l_top, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_high, c_lowest, list;
   size_t border, ends;
   size_t bytes;
 };
@@ -1242,7 +1250,8 @@ SampleLayout sample_layout(int32_t N, int32_t V) {
   l.bin_count = take((size_t)N * kBins * 4);
   l.c_kept = take(parts * 8);
   l.c_listed = take(parts * 4);
-  l.c_keys = take(parts * 8);
+  l.c_high = take(parts * 4);
+  l.c_lowest = take(parts * 4);
   l.list = take(parts * kListed * 8);
   l.border = take((size_t)N * sizeof(Border));
   l.ends = take((size_t)N * sizeof(Border));
@@ -1295,7 +1304,8 @@ hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, in
   a.bin_count = reinterpret_cast<uint32_t *>(ws + l.bin_count);
   a.c_kept = reinterpret_cast<uint64_t *>(ws + l.c_kept);
   a.c_listed = reinterpret_cast<uint32_t *>(ws + l.c_listed);
-  a.c_keys = reinterpret_cast<uint32_t *>(ws + l.c_keys);
+  a.c_high = reinterpret_cast<uint32_t *>(ws + l.c_high);
+  a.c_lowest = reinterpret_cast<uint32_t *>(ws + l.c_lowest);
   a.list = reinterpret_cast<uint64_t *>(ws + l.list);
   a.l_top = reinterpret_cast<float *>(ws + l.l_top);
   a.border = reinterpret_cast<Border *>(ws + l.border);
