@@ -505,8 +505,7 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   }
 }
 
-// The end's bins, from weights and counts of eight neighbouring bins a lane, for every wave
-// by itself. `mass0` and `count0` are ahead of the first bin; by_k: top-k may end in a bin;
+// The end's bins, from weights and counts of eight neighbouring bins a lane, by one wave. `mass0` and `count0` are ahead of the first bin; by_k: top-k may end in a bin;
 // `all`: what top-p takes its share of if it does not.
 constexpr int kOwnBins = kBins / kWave;
 __device__ __forceinline__ void locate(const uint64_t (&m)[kOwnBins], const uint32_t (&c)[kOwnBins],
@@ -601,18 +600,28 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   if (!row.filtered() || b.top == -__builtin_inff()) return;
   __shared__ double table[kExpTable];
   __shared__ uint32_t s_listed[kGroup];
-  if (lane == 0) s_listed[wave] = 0;      // each wave has its own
-  fill_table(table);
-  __syncthreads();
-  if (c >= a.chunks) return;
-  if (!in_range(b, c_top)) {
-    if (lane == 0) a.c_kept[at] = 0, a.c_listed[at] = 0;
+  __shared__ Border found;
+  const bool mine = in_range(b, c_top);
+  if (!__syncthreads_or(mine)) {
+    if (lane == 0 && c < a.chunks) a.c_kept[at] = 0, a.c_listed[at] = 0;
     return;
   }
-  if (row.binned()) {
-    find_border(a, n, row, b);
-  } else {
+  if (lane == 0) s_listed[wave] = 0;      // each wave has its own
+  fill_table(table);
+  if (!row.binned()) {
     b.lo = b.hi = b.bin_k = kBins;
+    __syncthreads();
+  } else {
+    if (wave == 0) {                      // 6 KB of bins: read by one of the waves
+      find_border(a, n, row, b);
+      if (lane == 0) found = b;
+    }
+    __syncthreads();
+    b = found;
+  }
+  if (!mine) {
+    if (lane == 0 && c < a.chunks) a.c_kept[at] = 0, a.c_listed[at] = 0;
+    return;
   }
   uint64_t kept = 0;
   uint32_t high = 0, low = 0xffffffffu;
