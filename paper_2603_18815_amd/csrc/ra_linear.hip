@@ -25,6 +25,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kChunk = 64;              // tokens of a chunk
+constexpr int kComputeUnits = 256;
 constexpr int kStateSize = kHeadDim * kHeadDim;
 
 struct LinearArgs {
@@ -47,57 +48,84 @@ __device__ __forceinline__ double log_decay_of(const float *log_decay, int g) {
 }
 
 // ---- decode ---------------------------------------------------------------------------
-// A workgroup per (row, KV head). Thread t holds column t % 128 of the state, the 64 key
-// dims of half t / 128, in registers.
+// A workgroup takes kCols value dims of a (row, KV head)'s state, all 128 key dims: a thread
+// four neighbouring columns of every kGroups-th row, so that a wave's load is contiguous and
+// all loads of the state are in flight before anything waits. The products with q over the
+// rows are joined in the wave, then between the waves through LDS.
+constexpr int kHeadsAtOnce = 4;
+template <int kCols>
 __global__ __launch_bounds__(kThreads) void linear_decode_kernel(
     const uint16_t *q, const uint16_t *k, const uint16_t *v, const int32_t *kv_lens,
     float *states, const int32_t *slots, int32_t num_slots, const float *log_decay, int32_t hq,
     int32_t hkv, float scale, uint16_t *out) {
-  const int b = blockIdx.y, g = blockIdx.x, tid = threadIdx.x;
-  const int col = tid % kHeadDim, half = tid / kHeadDim, group = hq / hkv;
+  constexpr int kLanes = kCols / 4, kGroups = kThreads / kLanes, kRows = kHeadDim / kGroups;
+  constexpr int kWaves = kThreads / kWave;
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int g = blockIdx.x / (kHeadDim / kCols), col0 = blockIdx.x % (kHeadDim / kCols) * kCols;
+  const int group = hq / hkv, col = tid % kLanes * 4, row = tid / kLanes;
   const int slot = slots[b], len = kv_lens[b];
-  uint16_t *o_row = out + ((int64_t)b * hq + g * group) * kHeadDim;
+  const int64_t head0 = (int64_t)b * hq + g * group;
   if (slot < 0 || slot >= num_slots || len <= 0) {
-    for (int i = tid; i < group * kHeadDim; i += kThreads) o_row[i] = 0;
+    for (int i = tid; i < group * kCols; i += kThreads)
+      out[(head0 + i / kCols) * kHeadDim + col0 + i % kCols] = 0;
     return;
   }
-  __shared__ float sk[kHeadDim], sq[kHeadDim], part[kHeadDim];
-  float *state = states + ((int64_t)slot * hkv + g) * kStateSize;
+  __shared__ float sk[kHeadDim], sq[kHeadsAtOnce][kHeadDim], part[kWaves][kHeadsAtOnce][kCols];
+  float *state = states + ((int64_t)slot * hkv + g) * kStateSize + row * kHeadDim + col0 + col;
+  f32x4 s[kRows];
+#pragma unroll
+  for (int i = 0; i < kRows; ++i)
+    s[i] = len > 1 ? *reinterpret_cast<const f32x4 *>(state + i * kGroups * kHeadDim)
+                   : f32x4{0.f, 0.f, 0.f, 0.f};
+  const uint16_t *kv_row = k + ((int64_t)b * hkv + g) * kHeadDim;
+  if (tid < kHeadDim) sk[tid] = __uint_as_float((uint32_t)kv_row[tid] << 16);
+  const bf16x4 vb = *reinterpret_cast<const bf16x4 *>(v + ((int64_t)b * hkv + g) * kHeadDim + col0 + col);
+  const f32x4 vc = __builtin_convertvector(vb, f32x4);
   // the decay in two parts: its rounding to fp32 alone would be felt after 2^24 / t of t steps
   const double decay = exp(log_decay_of(log_decay, g));
   const float l = (float)decay, l_low = (float)(decay - (double)l);
-  if (tid < kHeadDim)
-    sk[tid] = __uint_as_float((uint32_t)k[((int64_t)b * hkv + g) * kHeadDim + tid] << 16);
-  const float vc = __uint_as_float((uint32_t)v[((int64_t)b * hkv + g) * kHeadDim + col] << 16);
   __syncthreads();
-  float s[64];
 #pragma unroll
-  for (int i = 0; i < 64; ++i)
-    s[i] = len == 1 ? 0.f : state[(half * 64 + i) * kHeadDim + col];
+  for (int i = 0; i < kRows; ++i) {
+    const float kr = sk[row + i * kGroups];
 #pragma unroll
-  for (int i = 0; i < 64; ++i) {
-    s[i] = fmaf(l, s[i], fmaf(l_low, s[i], sk[half * 64 + i] * vc));
-    state[(half * 64 + i) * kHeadDim + col] = s[i];
+    for (int e = 0; e < 4; ++e) s[i][e] = fmaf(l, s[i][e], fmaf(l_low, s[i][e], kr * vc[e]));
+    *reinterpret_cast<f32x4 *>(state + i * kGroups * kHeadDim) = s[i];
   }
-  for (int h = 0; h < group; ++h) {
+  for (int h0 = 0; h0 < group; h0 += kHeadsAtOnce) {
+    const int heads = min(group - h0, kHeadsAtOnce);
+    if (h0 > 0) __syncthreads();                      // part and sq are read no more
+    for (int i = tid; i < heads * kHeadDim; i += kThreads)
+      sq[i / kHeadDim][i % kHeadDim] = __uint_as_float((uint32_t)q[(head0 + h0) * kHeadDim + i] << 16);
     __syncthreads();
-    if (tid < kHeadDim)
-      sq[tid] = __uint_as_float((uint32_t)q[((int64_t)b * hq + g * group + h) * kHeadDim + tid] << 16);
-    __syncthreads();
-    float o = 0.f;
+    for (int h = 0; h < heads; ++h) {
+      f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 64; ++i) o = fmaf(sq[half * 64 + i], s[i], o);
-    if (half) part[col] = o;
+      for (int i = 0; i < kRows; ++i) {
+        const float qr = sq[h][row + i * kGroups];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(qr, s[i][e], o[e]);
+      }
+#pragma unroll
+      for (int d = kLanes; d < kWave; d *= 2)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], d);
+      if (lane < kLanes) *reinterpret_cast<f32x4 *>(&part[wave][h][col]) = o;
+    }
     __syncthreads();
-    if (!half)
-      o_row[h * kHeadDim + col] = __builtin_bit_cast(uint16_t, (__bf16)(scale * (o + part[col])));
+    for (int i = tid; i < heads * kCols; i += kThreads) {
+      float o = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) o += part[w][i / kCols][i % kCols];
+      out[(head0 + h0 + i / kCols) * kHeadDim + col0 + i % kCols] =
+          __builtin_bit_cast(uint16_t, (__bf16)(scale * o));
+    }
   }
 }
 
 // ---- append: LDS tiles ----------------------------------------------------------------
 constexpr int kAppendThreads = 512;
 constexpr int kTile = kChunk * kHeadDim;
-constexpr int kComputeUnits = 256;
 
 // A tile holds 64 tokens of 128 bf16 in 16-byte units, unit u of row x at u ^ swizzle(x):
 // 16 rows at one unit, and four neighbouring rows at four neighbouring units, fall on
@@ -555,8 +583,14 @@ hipError_t launch_linear_decode(const uint16_t *q, const uint16_t *k, const uint
                                 const int32_t *kv_lens, const float *log_decay, int32_t B,
                                 int32_t hq, int32_t hkv, float scale, uint16_t *out,
                                 hipStream_t stream) {
-  hipLaunchKernelGGL(linear_decode_kernel, dim3(hkv, B), dim3(kThreads), 0, stream, q, k, v,
-                     kv_lens, states, slots, num_slots, log_decay, hq, hkv, scale, out);
+  // whole states a workgroup, or quarters where those are too few to fill the GPU
+  const bool quarters = (int64_t)B * hkv < 2 * kComputeUnits;
+  if (quarters)
+    hipLaunchKernelGGL(linear_decode_kernel<32>, dim3(hkv * 4, B), dim3(kThreads), 0, stream, q, k,
+                       v, kv_lens, states, slots, num_slots, log_decay, hq, hkv, scale, out);
+  else
+    hipLaunchKernelGGL(linear_decode_kernel<128>, dim3(hkv, B), dim3(kThreads), 0, stream, q, k, v,
+                       kv_lens, states, slots, num_slots, log_decay, hq, hkv, scale, out);
   return hipGetLastError();
 }
 

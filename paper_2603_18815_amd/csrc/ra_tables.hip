@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(
   if (tid == 0) bad = 0;
   __syncthreads();
   const int64_t limit = (int64_t)bt_stride * kPage;
-  int64_t tokens = 0, pages = 0;
+  int64_t tokens = 0, pages = 0, total_n = 0, total_need = 0, after = 0, page_after = 0;
   for (int base = 0; base < B; base += kThreads) {
     int64_t n = 0, need = 0;
     if (base + tid < B) {
@@ -84,10 +84,10 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(
       if (s < 0 || n < 0 || s + n > limit) bad = 1;
       need = pages_of(s + n) - pages_of(s);
     }
-    int64_t total_n, total_need;
     group_scan(n, need, total_n, total_need, part);
     tokens += total_n;
     pages += total_need;
+    after = n, page_after = need;
   }
   __syncthreads();
   const int32_t count = *free_count;
@@ -112,8 +112,12 @@ __global__ __launch_bounds__(kThreads) void extend_kernel(
         need = pages_of(s + n) - pages_of(s);
       }
     }
-    int64_t after = n, page_after = need, total_n, total_need;
-    group_scan(after, page_after, total_n, total_need, part);   // also: LDS is free again
+    if (B > kThreads) {                   // else the sums of the pass before are at hand
+      after = n, page_after = need;
+      group_scan(after, page_after, total_n, total_need, part);   // also: LDS is free again
+    } else if (!ok) {
+      after = page_after = total_n = total_need = 0;
+    }
     if (b < B) {
       first[tid] = (int)(token_base + after - n);
       page0[tid] = (int)(page_base + page_after - need);
