@@ -38,7 +38,6 @@ struct LinearArgs {
   float *carry;                         // [B][Hkv][segments] states (cut rows only)
   int32_t num_slots, B, hq, hkv, total_q, max_q_len;
   int32_t segments, segment_len;        // stretches a row has at most, tokens of each
-  int32_t head_splits;                  // workgroups that share a group's query heads
   float scale;
 };
 
@@ -181,10 +180,11 @@ __device__ __forceinline__ void load_to_lds(const uint16_t *base, uint32_t offse
       : "memory", "m0");
 }
 __device__ __forceinline__ void await_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-// The same for loads with four stores issued behind them (counted in order): the stores
+// The same for loads with kStores stores issued behind them (counted in order): the stores
 // may still be on their way.
-__device__ __forceinline__ void await_loads_before_4() {
-  asm volatile("s_waitcnt vmcnt(4)" ::: "memory");
+template <int kStores>
+__device__ __forceinline__ void await_loads_before() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kStores) : "memory");
 }
 __device__ __forceinline__ uint32_t lds_address(const uint16_t *p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
@@ -214,15 +214,13 @@ __device__ __forceinline__ int fresh(int x) {
 // (outputs, while the next chunk's K and V load; V's tile is free once the first head
 // has its operands, K's after the update). Q has two tiles. 73 KB of LDS and 128 registers:
 // two workgroups per CU, whose steps overlap.
-template <bool kStates>
+template <bool kStates, int kHeads>
 __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_kernel(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
   // the outputs pass starts with what the states pass read last, and may still be cached
   int unit = kStates ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
-  const int split = kStates ? 0 : unit % a.head_splits;
-  if (!kStates) unit /= a.head_splits;
   const int seg = unit % a.segments;
   unit /= a.segments;
   const int g = unit % a.hkv, b = unit / a.hkv, group = a.hq / a.hkv;
@@ -234,20 +232,19 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   const int len = min(T - from, a.segment_len);
   const bool whole = T <= a.segment_len;    // an uncut row keeps its own state
   if (kStates && whole) return;
-  const int h0 = group * split / a.head_splits, h1 = group * (split + 1) / a.head_splits;
   const int64_t tok0 = row0 + from;
   const int slot = a.slots[b];
   if (slot < 0 || slot >= a.num_slots) {
     if (!kStates)
       for (int t = 0; t < len; ++t)
-        for (int i = tid; i < (h1 - h0) * kHeadDim; i += kAppendThreads)
-          a.out[((tok0 + t) * a.hq + g * group + h0) * kHeadDim + i] = 0;
+        for (int i = tid; i < group * kHeadDim; i += kAppendThreads)
+          a.out[((tok0 + t) * a.hq + g * group) * kHeadDim + i] = 0;
     return;
   }
 
   __shared__ __align__(1024) uint16_t sk[2 * kTile], sv[2 * kTile];
-  __shared__ __align__(1024) uint16_t sq[kStates ? 8 : 2 * kTile];
-  __shared__ __align__(1024) uint16_t sp[kStates ? 8 : kChunk * kChunk];
+  __shared__ __align__(1024) uint16_t sq[kStates ? 8 : 2 * kHeads * kTile];
+  __shared__ __align__(1024) uint16_t sp[kStates ? 8 : kHeads * kChunk * kChunk];
   // l^n; scale l^n; l^(63 - j), then zeros
   __shared__ float power[kChunk + 1], weight[2 * kChunk];
   __shared__ double decays[kChunk + 1];
@@ -293,7 +290,12 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   uint16_t *op = a.out + q_first;
   load(lds_k, kp, kv_off, kv_stride, len - 1);
   load(lds_v, vp, kv_off, kv_stride, len - 1);
-  if (!kStates) load(lds_q, qp + h0 * kHeadDim, q_off, q_stride, len - 1);
+  auto load_q = [&](int buf, const uint16_t *base, int left) {
+#pragma unroll
+    for (int j = 0; j < kHeads; ++j)
+      load(lds_q + (buf * kHeads + j) * kTile * 2, base + j * kHeadDim, q_off, q_stride, left);
+  };
+  if (!kStates) load_q(0, qp, len - 1);
 
   // state tile t = 2 x + y, register i: key dim 32 x + 8 quad + 4 y + i, value dim 16 wave + r
   f32x4 s[8];
@@ -415,67 +417,75 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
 #pragma unroll
       for (int x = 0; x < 4; ++x)
         sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-      for (int h = h0; h < h1; ++h) {
-        const uint16_t *const tq = sq + q_buf * kTile;
-        const bool last = h + 1 == h1;
-        // behind the tiles' loads: the step before's stores, four where its chunk was full
-        if (n == kChunk && (c > 0 || h > h0)) {
-          await_loads_before_4();
+      for (int h = 0; h < group; h += kHeads) {
+        const uint16_t *const tq = sq + q_buf * kHeads * kTile;
+        const bool last = h + kHeads == group;
+        // behind the tiles' loads: the step before's stores, four a head where its chunk was full
+        if (n == kChunk && (c > 0 || h > 0)) {
+          await_loads_before<4 * kHeads>();
         } else {
           await_loads();
         }
         __syncthreads();
-        // Q of all tokens; K of the wave's two score tiles: those of tokens 16 it + r against
-        // 16 jt + 4 quad + 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero,
-        // and needed where a tile shares 32 slots with one on it.
+        // K of the wave's two score tiles: those of tokens 16 it + r against 16 jt + 4 quad +
+        // 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero, and needed where a
+        // tile shares 32 slots with one on it.
         const int it_p = wave & 3, jt_p = wave >> 2, at = fresh(at_row), pt = fresh(at_p);
-        bf16x8 qf[4][4], kf[2][4];
+        bf16x8 kf[2][4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) kf[0][x] = lds_bf16x8(tk + 16 * jt_p * kHeadDim, at ^ (x << 6));
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int it = 0; it < 4; ++it) qf[it][x] = lds_bf16x8(tq + 16 * it * kHeadDim, at ^ (x << 6));
-        bf16x8 qp_f[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) qp_f[x] = lds_bf16x8(tq + 16 * it_p * kHeadDim, at ^ (x << 6));
         if (it_p >= 2)
 #pragma unroll
           for (int x = 0; x < 4; ++x)
             kf[1][x] = lds_bf16x8(tk + 16 * (jt_p + 2) * kHeadDim, at ^ (x << 6));
-        if (h == h0) read_v(vf, tv);
+        if (h == 0) read_v(vf, tv);
         q_buf ^= 1;
         if (!last) {
-          load(lds_q + q_buf * kTile * 2, qp + (h + 1) * kHeadDim, q_off, q_stride, left + kChunk);
+          load_q(q_buf, qp + (h + kHeads) * kHeadDim, left + kChunk);
         } else if (more) {
-          load(lds_q + q_buf * kTile * 2, qp + q_chunk + h0 * kHeadDim, q_off, q_stride, left);
+          load_q(q_buf, qp + q_chunk, left);
         }
-        keep_order();
-        f32x4 acc[4], p[2];
+        f32x4 acc[kHeads][4];
 #pragma unroll
-        for (int it = 0; it < 4; ++it) acc[it] = f32x4{0.f, 0.f, 0.f, 0.f};
-        p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < kHeads; ++j) {
+          const uint16_t *const tj = tq + j * kTile;
+          // Q of all tokens, and of those of the wave's scores
+          bf16x8 qf[4][4], qs[4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          p[0] = mfma16x16x32(kf[0][x], qp_f[x], p[0]);
+          for (int x = 0; x < 4; ++x) qs[x] = lds_bf16x8(tj + 16 * it_p * kHeadDim, at ^ (x << 6));
 #pragma unroll
-          for (int it = 0; it < 4; ++it) acc[it] = mfma16x16x32(sb[x], qf[it][x], acc[it]);
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int it = 0; it < 4; ++it)
+              qf[it][x] = lds_bf16x8(tj + 16 * it * kHeadDim, at ^ (x << 6));
+          keep_order();
+          f32x4 p[2];
+          p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int it = 0; it < 4; ++it) acc[j][it] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            p[0] = mfma16x16x32(kf[0][x], qs[x], p[0]);
+#pragma unroll
+            for (int it = 0; it < 4; ++it) acc[j][it] = mfma16x16x32(sb[x], qf[it][x], acc[j][it]);
+          }
+          if (it_p >= 2)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) p[1] = mfma16x16x32(kf[1][x], qs[x], p[1]);
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) {
+            if (jj == 1 && it_p < 2) break;
+            bf16x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i]);
+            *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(sp + j * kChunk * kChunk) +
+                                        (pt ^ (jj << 6))) = w;
+          }
+#pragma unroll
+          for (int it = 0; it < 4; ++it) acc[j][it] *= power[16 * it + r + 1];
         }
-        if (it_p >= 2)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) p[1] = mfma16x16x32(kf[1][x], qp_f[x], p[1]);
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj) {
-          if (jj == 1 && it_p < 2) break;
-          bf16x4 w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i]);
-          *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(sp) + (pt ^ (jj << 6))) = w;
-        }
-#pragma unroll
-        for (int it = 0; it < 4; ++it) acc[it] *= power[16 * it + r + 1];
-        if (h == h0) load_k();
+        if (h == 0) load_k();
         if (last && whole) {
           // the product of the chunks' decays as they were rounded is kept at l^tokens: what
           // one rounding adds, the next chunk's takes off
@@ -486,31 +496,31 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
         } else if (last && more) {
           update(std::integral_constant<int, 1>(), vf, tk, n, (float)decays[kChunk], 1.f);
         }
-        if (h == h0) load_v();
+        if (h == 0) load_v();
         __syncthreads();
         const int st = fresh(at_score);
-        bf16x8 pf[4][2];
-#pragma unroll
-        for (int it = 0; it < 4; ++it)
-#pragma unroll
-          for (int x = 0; x <= it / 2; ++x) pf[it][x] = lds_bf16x8(sp + 16 * it * kChunk, st ^ (x << 6));
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-#pragma unroll
-          for (int it = 2 * x; it < 4; ++it) acc[it] = mfma16x16x32(vf[x], pf[it][x], acc[it]);
-        uint16_t *const o_row = op + h * kHeadDim;
         const uint32_t o_at = __umul24(r, a.hq * kHeadDim) + 16 * wave + 4 * quad;
-        if (n == kChunk) {
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j) {
+          bf16x8 pf[4][2];
 #pragma unroll
           for (int it = 0; it < 4; ++it)
-            *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
-                __builtin_convertvector(acc[it], bf16x4);
-        } else {
+#pragma unroll
+            for (int x = 0; x <= it / 2; ++x)
+              pf[it][x] = lds_bf16x8(sp + j * kChunk * kChunk + 16 * it * kChunk, st ^ (x << 6));
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int it = 2 * x; it < 4; ++it) acc[j][it] = mfma16x16x32(vf[x], pf[it][x], acc[j][it]);
+        }
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j) {
+          uint16_t *const o_row = op + (h + j) * kHeadDim;
 #pragma unroll
           for (int it = 0; it < 4; ++it)
-            if (16 * it + r < n)
+            if (n == kChunk || 16 * it + r < n)
               *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
-                  __builtin_convertvector(acc[it], bf16x4);
+                  __builtin_convertvector(acc[j][it], bf16x4);
         }
       }
       qp += q_chunk;
@@ -554,14 +564,14 @@ __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
 
 // How an append call is cut.
 struct LinearPlan {
-  int32_t segments, segment_len, head_splits;
+  int32_t segments, segment_len;
 };
 LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int32_t max_q_len) {
   // a workgroup's even share of the call's chunks; a longest row up to twice as long is
   // left whole
   const int64_t chunks = ((int64_t)max_q_len + kChunk - 1) / kChunk;
   const int64_t share = ((int64_t)total_q * hkv / kComputeUnits + kChunk - 1) / kChunk;
-  LinearPlan p = {1, max_q_len, 1};
+  LinearPlan p = {1, max_q_len};
   if (chunks > 2 * share && chunks > 1) {
     const int64_t per = share < 1 ? 1 : share;
     p.segment_len = (int32_t)(per * kChunk);
@@ -603,16 +613,19 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
   const LinearPlan p = linear_plan(B, hq, hkv, total_q, max_q_len);
   LinearArgs a = {q, k, v, cu_q, ctx_lens, states, slots, log_decay, out,
                   static_cast<float *>(workspace), num_slots, B, hq, hkv, total_q, max_q_len,
-                  p.segments, p.segment_len, p.head_splits, scale};
+                  p.segments, p.segment_len, scale};
   const unsigned pairs = (unsigned)B * (unsigned)hkv;
+  const dim3 grid(pairs * p.segments), threads(kAppendThreads);
   if (p.segments > 1) {
-    hipLaunchKernelGGL(linear_chunk_kernel<true>, dim3(pairs * p.segments), dim3(kAppendThreads), 0,
-                       stream, a);
+    hipLaunchKernelGGL((linear_chunk_kernel<true, 1>), grid, threads, 0, stream, a);
     hipLaunchKernelGGL(linear_scan_kernel, dim3(kStateSize / (4 * kThreads), pairs),
                        dim3(kThreads), 0, stream, a);
   }
-  hipLaunchKernelGGL(linear_chunk_kernel<false>, dim3(pairs * p.segments * p.head_splits),
-                     dim3(kAppendThreads), 0, stream, a);
+  // two query heads a step share K's operands and the step's waits
+  if (hq / hkv % 2 == 0)
+    hipLaunchKernelGGL((linear_chunk_kernel<false, 2>), grid, threads, 0, stream, a);
+  else
+    hipLaunchKernelGGL((linear_chunk_kernel<false, 1>), grid, threads, 0, stream, a);
   return hipGetLastError();
 }
 
