@@ -320,6 +320,8 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   const int tr_row = 8 * quad + (r >> 2), tr_swizzle = swizzle(tr_row);
   const int at_k = tr_row * kRowBytes + (((r & 3) ^ tr_swizzle) << 4);
   const int at_v = tr_row * kRowBytes + (((2 * wave + (r >> 1 & 1)) ^ tr_swizzle) << 4) + (r & 1) * 8;
+  // results: rows r at the wave's four value dims of the quad
+  const int at_o = r * kRowBytes + (((2 * wave + (quad >> 1)) ^ swizzle(r)) << 4) + (quad & 1) * 8;
   const int at_score = r * kScoreRowBytes + ((quad ^ (r >> 1)) << 4);
 
   // V^T of a chunk, rows the wave's value dims, slots the 32 tokens from 32 x
@@ -418,11 +420,11 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
       for (int x = 0; x < 4; ++x)
         sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
       for (int h = 0; h < group; h += kHeads) {
-        const uint16_t *const tq = sq + q_buf * kHeads * kTile;
+        uint16_t *const tq = sq + q_buf * kHeads * kTile;
         const bool last = h + kHeads == group;
-        // behind the tiles' loads: the step before's stores, four a head where its chunk was full
+        // behind the tiles' loads: the step before's stores, two a head where its chunk was full
         if (n == kChunk && (c > 0 || h > 0)) {
-          await_loads_before<4 * kHeads>();
+          await_loads_before<2 * kHeads>();
         } else {
           await_loads();
         }
@@ -499,7 +501,6 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
         if (h == 0) load_v();
         __syncthreads();
         const int st = fresh(at_score);
-        const uint32_t o_at = __umul24(r, a.hq * kHeadDim) + 16 * wave + 4 * quad;
 #pragma unroll
         for (int j = 0; j < kHeads; ++j) {
           bf16x8 pf[4][2];
@@ -513,15 +514,26 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
 #pragma unroll
             for (int it = 2 * x; it < 4; ++it) acc[j][it] = mfma16x16x32(vf[x], pf[it][x], acc[j][it]);
         }
+        // the results through Q's tiles, which nothing reads any more: a wave has 32 bytes of
+        // each token, whose stores alone took longer than the products; whole rows leave
+        const int ot = fresh(at_o);
 #pragma unroll
-        for (int j = 0; j < kHeads; ++j) {
-          uint16_t *const o_row = op + (h + j) * kHeadDim;
+        for (int j = 0; j < kHeads; ++j)
 #pragma unroll
           for (int it = 0; it < 4; ++it)
-            if (n == kChunk || 16 * it + r < n)
-              *reinterpret_cast<bf16x4 *>(o_row + (size_t)(16 * it) * a.hq * kHeadDim + o_at) =
-                  __builtin_convertvector(acc[j][it], bf16x4);
-        }
+            *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(tq + j * kTile + 16 * it * kHeadDim) +
+                                        ot) = __builtin_convertvector(acc[j][it], bf16x4);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            const u32x4 w = load_u32x4(tq + j * kTile + (8 * wave + 4 * m) * kHeadDim + lane * 8);
+            char *const o_row = reinterpret_cast<char *>(op + (h + j) * kHeadDim);
+            if (n == kChunk || 8 * wave + 4 * m + lane / 16 < n)
+              store_u32x4(reinterpret_cast<uint16_t *>(
+                              o_row + (m ? (q_off ^ 32) + 4 * q_stride : q_off)), w);
+          }
       }
       qp += q_chunk;
       op += q_chunk;
