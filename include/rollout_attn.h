@@ -468,8 +468,9 @@ int token_logprob_packed(const void *h, const void *W_packed, const int32_t *tar
  *   uniform      fp32 [N] in [0, 1)
  *   tokens       int32 [N]
  *   logprob      fp32 [N] or NULL
- *   workspace    device scratch of at least token_sample_workspace_size(N, V) bytes
- *                (contents on entry ignored; NULL where the size is 0)
+ *   workspace    device scratch of at least token_sample_workspace_size(N, V) bytes,
+ *                16-byte aligned (contents on entry ignored). Calls that share one must
+ *                not overlap.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (N < 0, V <= 0, row_stride < V with N > 1);
  *         RA_ERR_UNSUPPORTED (an unknown logits_dtype, V > 2^19, N > 2^20);
  *         RA_ERR_WORKSPACE; RA_ERR_HIP. N == 0 returns RA_OK without launching anything.
@@ -511,14 +512,15 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
  *   max_q_len  host: an upper bound of cu_q[b+1] - cu_q[b]
  *   out        bf16 [total_q][Hq][128]
  *   workspace  device scratch of at least rollout_linear_attn_append_workspace_size(B, Hq,
- *              Hkv, total_q, max_q_len) bytes (contents on entry ignored; NULL where the
- *              size is 0). Calls that share one must not overlap.
+ *              Hkv, total_q, max_q_len) bytes (contents on entry ignored), 16-byte
+ *              aligned; NULL where the size is 0. Calls that share one must not overlap.
  *   The rest as for decode; rows without tokens leave their state as it is. How a long row
  *   is cut into stretches, and with it the order of fp32 sums, depends on B, Hq, Hkv,
  *   total_q and max_q_len alone.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, Hq or Hkv or num_slots <= 0, Hq % Hkv,
  *         total_q < 0, max_q_len < 0, scale not finite); RA_ERR_UNSUPPORTED (Hq / Hkv > 32,
- *         B > 65535, Hq > 65535, B * Hkv > 2^25); RA_ERR_WORKSPACE; RA_ERR_HIP. B == 0, total_q == 0 or
+ *         B > 65535, Hq > 65535, B * Hkv > 2^25, or q, k_new, v_new, states or out not
+ *         16-byte aligned); RA_ERR_WORKSPACE; RA_ERR_HIP. B == 0, total_q == 0 or
  *         max_q_len == 0 launch nothing.
  */
 int rollout_linear_attn_decode(const void *q, const void *k_new, const void *v_new, float *states,

@@ -296,6 +296,8 @@ int page_write_impl(const void *k_new, const void *v_new, const int32_t *cu_new,
                                           cos_sin, rope_rows));
 }
 
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
 // Checks shared by the linear attention's entry points.
 int check_linear(int32_t B, int32_t Hq, int32_t Hkv, int32_t num_slots, float scale) {
   if (B < 0 || Hq <= 0 || Hkv <= 0 || num_slots <= 0 || Hq % Hkv != 0 || !std::isfinite(scale))
@@ -477,7 +479,8 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
   if (N == 0) return RA_OK;
   if (!logits || !uniform || !tokens) return RA_ERR_NULL;
   const size_t need = ra::sample_workspace_bytes(N, V);
-  if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+    return RA_ERR_WORKSPACE;
   return hip_status(ra::launch_sample(logits, logits_dtype == RA_LOGITS_BF16, N, V, row_stride,
                                       temperature, top_k, top_p, min_p, uniform, tokens, logprob,
                                       workspace, stream));
@@ -492,6 +495,9 @@ int rollout_linear_attn_decode(const void *q, const void *k_new, const void *v_n
   if (B == 0) return RA_OK;
   if (!q || !k_new || !v_new || !states || !slots || !kv_lens || !log_decay || !out)
     return RA_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(states) ||
+      !aligned16(out))
+    return RA_ERR_UNSUPPORTED;
   return hip_status(ra::launch_linear_decode(
       static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new),
       static_cast<const uint16_t *>(v_new), states, slots, num_slots, kv_lens, log_decay, B, Hq,
@@ -517,8 +523,12 @@ int rollout_linear_attn_append(const void *q, const void *k_new, const void *v_n
   if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
   if (!q || !k_new || !v_new || !cu_q || !ctx_lens || !states || !slots || !log_decay || !out)
     return RA_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(states) ||
+      !aligned16(out))
+    return RA_ERR_UNSUPPORTED;
   const size_t need = ra::linear_append_workspace_bytes(B, Hq, Hkv, total_q, max_q_len);
-  if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
+  if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
+    return RA_ERR_WORKSPACE;
   return hip_status(ra::launch_linear_append(
       static_cast<const uint16_t *>(q), static_cast<const uint16_t *>(k_new),
       static_cast<const uint16_t *>(v_new), cu_q, ctx_lens, states, slots, num_slots, log_decay,

@@ -76,7 +76,7 @@ def uniforms(N, seed):
     return np.random.default_rng(seed).random(N, dtype=np.float32).tolist()
 
 
-SIZES = [1, 2, 3, 63, 64, 65, 1000, 4095, 4096, 4097, 8192, 8193, 32000, 65537, 151936]
+SIZES = [1, 2, 3, 63, 64, 65, 1000, 4095, 4096, 4097, 8192, 8193, 32000, 65537, 131073, 151936, 1 << 19]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -176,3 +176,39 @@ def test_refusals(device):
         ra.token_sample(torch.zeros((1, (1 << 19) + 1), device="cuda:0"), u[:1])
     tokens, logp = ra.token_sample(z[:0], u[:0], want_logprob=True)
     assert tokens.shape == (0,) and logp.shape == (0,)
+
+
+def test_many_short_rows(device):
+    """More rows than a grid dimension's 65,535."""
+    N = 70000
+    z = logits(N, 40, torch.float32, 3)
+    u = torch.rand(N, generator=torch.Generator(device="cuda:0").manual_seed(4), device="cuda:0")
+    k = torch.full((N,), 10, dtype=torch.int32, device="cuda:0")
+    p = torch.full((N,), 0.75, device="cuda:0")
+    tokens, logp = ra.token_sample(z, u, None, k, p, want_logprob=True)
+    rows = np.random.default_rng(1).choice(N, 200, replace=False).tolist() + [0, 65535, 65536, N - 1]
+    for n in rows:
+        want = host(z[n].double().cpu().numpy(), u[n].item(), 1.0, 10, 0.75)
+        assert tokens[n].item() == want[0], n
+        assert abs(logp[n].item() - want[1]) <= 2.0 ** -24 * abs(want[1]) + 2.0 ** -28
+
+
+@pytest.mark.parametrize("T", [20.0, 1.0])
+def test_many_elements_around_the_end(T, device):
+    """Rows so narrow that a good part of them lies in the bin where the prefix ends: the end
+    is found by finer bins, by sorting and by passes over the row."""
+    V = 120000
+    g = torch.Generator(device="cuda:0").manual_seed(8)
+    z = torch.randn((6, V), generator=g, device="cuda:0")
+    z[1] *= 1e-3
+    z[2] = (z[2] * 8).round() / 8
+    z[3] = z[3].bfloat16().float()
+    z[3, 0] = -1e30                                # a mask of a large finite value
+    z[4, ::2] = -1e30
+    z[5] = 1e-4 * torch.randint(0, 3, (V,), generator=g, device="cuda:0") + 1e-7 * z[0]
+    z[5, 7] = -50.0
+    u = uniforms(6, 3)
+    check(z, u, [T] * 6, None, [0.9, 0.5, 0.7, 0.99, 0.3, 0.45], what="top-p")
+    check(z, u, [T] * 6, [40000, 119000, 60000, 3000, 60001, 33333], what="top-k")
+    check(z, u, [T] * 6, [40000, 119000, 60000, 3000, 60001, 33333], [0.9, 0.5, 0.7, 0.99, 0.3, 0.45],
+          [0.0, 0.9, 0.0, 0.1, 0.0, 0.0], what="all")

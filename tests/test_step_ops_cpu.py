@@ -36,9 +36,9 @@ def test_token_sample_validation(lib):
     size = lib.token_sample_workspace_size
     assert size(0, 100) == 0 and size(4, 0) == 0 and size(4, (1 << 19) + 1) == 0
     need = size(4, 1 << 19)
-    if need:
-        assert call(V=1 << 19, stride=1 << 19, bytes=need - 1) == _lib.RA_ERR_WORKSPACE
-        assert call(V=1 << 19, stride=1 << 19, ws=None) == _lib.RA_ERR_WORKSPACE
+    assert call(V=1 << 19, stride=1 << 19, bytes=need - 1) == _lib.RA_ERR_WORKSPACE
+    assert call(V=1 << 19, stride=1 << 19, ws=None) == _lib.RA_ERR_WORKSPACE
+    assert call(ws=ctypes.c_void_p(0x1008)) == _lib.RA_ERR_WORKSPACE          # 16 bytes
 
 
 LINEAR = dict(q=FAKE, k=FAKE, v=FAKE, cu=FAKE, lens=FAKE, st=FAKE, slots=FAKE, ns=8, g=FAKE, B=4,
@@ -71,6 +71,10 @@ def test_linear_validation(lib, call):
         assert call(lib, scale=bad) == _lib.RA_ERR_SHAPE
     assert call(lib, Hq=66) == _lib.RA_ERR_UNSUPPORTED
     assert call(lib, B=65536) == _lib.RA_ERR_UNSUPPORTED
+    assert call(lib, Hq=65568, Hkv=2049) == _lib.RA_ERR_UNSUPPORTED
+    assert call(lib, B=65535, Hq=1024, Hkv=1024) == _lib.RA_ERR_UNSUPPORTED     # pairs
+    for name in ("q", "k", "v", "st", "out"):
+        assert call(lib, **{name: ctypes.c_void_p(0x1002)}) == _lib.RA_ERR_UNSUPPORTED, name
     assert call(lib, B=0, q=None, st=None) == _lib.RA_OK
 
 
@@ -84,10 +88,11 @@ def test_linear_append_validation(lib):
     assert size(0, 8, 2, 100, 50) == 0 and size(4, 7, 2, 100, 50) == 0
     assert size(4, 8, 2, 0, 50) == 0 and size(4, 8, 2, 100, 0) == 0
     need = size(1, 32, 32, 16384, 16384)
-    if need:
-        one = dict(B=1, Hq=32, Hkv=32, total=16384, mq=16384)
-        assert _append(lib, bytes=need - 1, **one) == _lib.RA_ERR_WORKSPACE
-        assert _append(lib, ws=None, **one) == _lib.RA_ERR_WORKSPACE
+    one = dict(B=1, Hq=32, Hkv=32, total=16384, mq=16384)
+    assert _append(lib, bytes=need - 1, **one) == _lib.RA_ERR_WORKSPACE
+    assert _append(lib, ws=None, **one) == _lib.RA_ERR_WORKSPACE
+    assert _append(lib, ws=ctypes.c_void_p(0x1008), **one) == _lib.RA_ERR_WORKSPACE
+    assert size(256, 32, 32, 25600, 100) == 0                         # whole rows need none
 
 
 def test_table_validation(lib):
