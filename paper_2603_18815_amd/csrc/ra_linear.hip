@@ -331,7 +331,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   };
   // S' = decay S + K^T (after l^(n-1-j) V), n the chunk's tokens: the decayed values in
   // three bf16 parts, which hold all 24 bits (a stretch of a cut row needs the state as bf16
-  // operands only: one part). The states pass has no state to decay: its weights reach to
+  // operands only: two parts, so that nothing but the operands' own rounding counts). The states pass has no state to decay: its weights reach to
   // the end of the stretch (after = l^tokens behind the chunk).
   auto update = [&](auto parts, const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay,
                     float after) {
@@ -358,9 +358,8 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
         const float w = weight[kChunk - n + 32 * x + 8 * quad + e];
         y[e] *= kStates ? w * after : w;
       }
-      if (kParts == 1) part[0] = to_bf16x8(y);
 #pragma unroll
-      for (int m = 0; m < (kParts == 1 ? 0 : kParts); ++m) part[m] = take_bf16(y);
+      for (int m = 0; m < kParts; ++m) part[m] = take_bf16(y);
 #pragma unroll
       for (int i = 4 * x; i < 4 * x + 4; ++i) {
         if (i + 1 < 8) read_pair(i + 1);
@@ -496,7 +495,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
           if (exact > 1e-30) drift = exact * drift / decay;
           update(std::integral_constant<int, 3>(), vf, tk, n, decay, 1.f);
         } else if (last && more) {
-          update(std::integral_constant<int, 1>(), vf, tk, n, (float)decays[kChunk], 1.f);
+          update(std::integral_constant<int, 2>(), vf, tk, n, (float)decays[kChunk], 1.f);
         }
         if (h == 0) load_v();
         __syncthreads();

@@ -88,7 +88,10 @@ __device__ __forceinline__ double weight_exp(double x) {
 __device__ __forceinline__ double scaled(float z, float top, double inv_t) {
   return z == top ? 0.0 : ((double)z - (double)top) * inv_t;
 }
-__device__ __forceinline__ uint64_t units(double e) { return (uint64_t)(e * kUnit + 0.5); }
+// Its whole units: in the low bits of the sum with 2^52.
+__device__ __forceinline__ uint64_t units(double e) {
+  return __builtin_bit_cast(uint64_t, __builtin_fma(e, kUnit, 0x1p52)) & 0xfffffffffffffull;
+}
 
 // The same for many elements: exp(d inv_t), d <= 0, as 2^(j / 128) by table times the rest of
 // the exponent, at most ln 2 / 256, by the Taylor series to r^4, whose next term is below
@@ -962,16 +965,20 @@ __device__ __forceinline__ Drawn draw_chunk(const V (&x)[4], float u) {
   return {__shfl(chunk, from), (double)__shfl(before, from), (double)total};
 }
 
-// Calls take(chunk, entry) for every listed element; first_of: where each chunk's start.
-template <typename Take>
-__device__ __forceinline__ void for_listed(const SampleArgs &a, int n, uint32_t count,
-                                           const uint32_t *first_of, Take take) {
-#pragma unroll 4
-  for (uint32_t i = threadIdx.x; i < count; i += kPickThreads) {
-    int c = 0;                            // the last chunk that starts at or before i
+// The chunk of the i-th listed element; first_of: where each chunk's start.
+__device__ __forceinline__ int chunk_of(const uint32_t *first_of, uint32_t i) {
+  int c = 0;                              // the last chunk that starts at or before i
 #pragma unroll
-    for (int step = kMaxChunks / 2; step > 0; step /= 2)
-      if (first_of[c + step] <= i) c += step;
+  for (int step = kMaxChunks / 2; step > 0; step /= 2)
+    if (first_of[c + step] <= i) c += step;
+  return c;
+}
+// Calls take(chunk, entry) for the listed elements from `from` on.
+template <typename Take>
+__device__ __forceinline__ void for_listed(const SampleArgs &a, int n, uint32_t from, uint32_t count,
+                                           const uint32_t *first_of, Take take) {
+  for (uint32_t i = from + threadIdx.x; i < count; i += kPickThreads) {
+    const int c = chunk_of(first_of, i);
     take(c, a.list[((int64_t)n * a.chunks + c) * kListed + (i - first_of[c])]);
   }
 }
@@ -1085,19 +1092,37 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       uint32_t below = 0xffffffffu;                   // keys above it are kept if none listed is
       if (count <= kWave || apart) {
         __syncthreads();
-        for_listed(a, n, listed_all, lds.first_of, [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
+        for_listed(a, n, 0, listed_all, lds.first_of, [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
         __syncthreads();
       } else {
-        // 512 bins of the listed keys' range, and the end's among them
+        // 512 bins of the listed keys' range, and the end's among them. The first elements of
+        // a thread, mostly all, stay in registers from one pass to the next.
         const uint32_t span = high - low;
         g.shift = span < (uint32_t)kBins ? 0 : 32 - __clz(span / kBins);
         for (int i = tid; i < kBins; i += kPickThreads) lds.mass[i] = 0, lds.counts[i] = 0;
+        constexpr int kHeld = 8;
+        uint64_t held[kHeld], weight[kHeld];
+        int of_chunk[kHeld];
         __syncthreads();
-        for_listed(a, n, listed_all, lds.first_of, [&](int, uint64_t x) {
-          const uint32_t key = (uint32_t)(x >> 32);
-          atomicAdd(&lds.counts[g.bin(key)], 1u);
-          atomicAdd((unsigned long long *)&lds.mass[g.bin(key)], (unsigned long long)units(g.weight(key)));
-        });
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+          const uint32_t i = tid + j * kPickThreads;
+          of_chunk[j] = chunk_of(lds.first_of, i);
+          held[j] = i < listed_all ? a.list[((int64_t)n * a.chunks + of_chunk[j]) * kListed +
+                                            (i - lds.first_of[of_chunk[j]])]
+                                   : 0;
+        }
+        auto put = [&](uint64_t x, uint64_t w) {
+          const int bin = g.bin((uint32_t)(x >> 32));
+          atomicAdd(&lds.counts[bin], 1u);
+          atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)w);
+        };
+        auto weigh = [&](uint64_t x) { return units(g.weight((uint32_t)(x >> 32))); };
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+          if (held[j]) put(held[j], weight[j] = weigh(held[j]));
+        for_listed(a, n, kHeld * kPickThreads, listed_all, lds.first_of,
+                   [&](int, uint64_t x) { put(x, weigh(x)); });
         __syncthreads();
         uint64_t m[kOwnBins];
         uint32_t c[kOwnBins];
@@ -1106,20 +1131,24 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
           m[i] = lds.mass[kOwnBins * lane + i], c[i] = lds.counts[kOwnBins * lane + i];
         locate(m, c, b.mass_lo, b.count_lo, rough.ends_in_k(), (uint32_t)row.k, row.p, all, fine);
         if (fine.lo > 0) below = high - ((uint32_t)fine.lo << g.shift);
-        for_listed(a, n, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
+        auto settle = [&](int chunk, uint64_t x, uint64_t w) {
           const uint32_t key = (uint32_t)(x >> 32);
           const int bin = g.bin(key);
           if (bin < fine.lo) {
-            const double e = g.weight(key);
-            if (e >= row.m)
-              atomicAdd((unsigned long long *)&lds.kept_of[chunk], (unsigned long long)units(e));
+            if (row.m == 0.0 || g.weight(key) >= row.m)
+              atomicAdd((unsigned long long *)&lds.kept_of[chunk], (unsigned long long)w);
           } else if (bin <= fine.hi || bin == fine.bin_k) {
             const uint32_t slot = atomicAdd(&lds.count, 1u);
             if (slot < (uint32_t)kMaxSorted) lds.sorted[slot] = x;
             atomicMax(&lds.high, key);
             atomicMin(&lds.low, key);
           }
-        });
+        };
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j)
+          if (held[j]) settle(of_chunk[j], held[j], weight[j]);
+        for_listed(a, n, kHeld * kPickThreads, listed_all, lds.first_of,
+                   [&](int chunk, uint64_t x) { settle(chunk, x, weigh(x)); });
         __syncthreads();
         count = lds.count;
         high = lds.high;
@@ -1128,7 +1157,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       if (count > 0 && high == low) {
         if (tid < kMaxChunks) lds.ties_of[tid] = 0;
         __syncthreads();
-        for_listed(a, n, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
+        for_listed(a, n, 0, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
           if ((uint32_t)(x >> 32) == high) atomicAdd(&lds.ties_of[chunk], 1u);
         });
         __syncthreads();
