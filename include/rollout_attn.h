@@ -493,9 +493,11 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
  *   o_t = scale * S_t^T q_t
  * A row's state lives in a pool, states[slots[b]], and is updated in place; the state
  * before a row's first token is zero whatever the pool holds. Slots of one call must
- * differ. The state is kept to fp32 accuracy: append multiplies the decayed keys in three
+ * differ. The state is kept to fp32 accuracy: append multiplies the decayed values in three
  * bf16 parts each. Its scores, and the state as it meets the queries, are rounded to bf16
- * operands, and out is rounded to bf16 (nearest even) in both calls.
+ * operands, and out is rounded to bf16 (nearest even) in both calls. An infinite or NaN
+ * input never reaches an earlier token's results; the state it reaches may hold NaN where
+ * the formula has an infinity.
  *
  * rollout_linear_attn_decode: one token a row.
  *   q          bf16 [B][Hq][128];  k_new, v_new  bf16 [B][Hkv][128]
@@ -519,7 +521,7 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
  *   total_q and max_q_len alone.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, Hq or Hkv or num_slots <= 0, Hq % Hkv,
  *         total_q < 0, max_q_len < 0, scale not finite); RA_ERR_UNSUPPORTED (Hq / Hkv > 32,
- *         B > 65535, Hq > 65535, B * Hkv > 2^25, or q, k_new, v_new, states or out not
+ *         B > 65535, Hq > 65535, B * Hkv > 2^22, or q, k_new, v_new, states or out not
  *         16-byte aligned); RA_ERR_WORKSPACE; RA_ERR_HIP. B == 0, total_q == 0 or
  *         max_q_len == 0 launch nothing.
  */

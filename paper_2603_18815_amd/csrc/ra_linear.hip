@@ -35,9 +35,11 @@ struct LinearArgs {
   const int32_t *slots;
   const float *log_decay;
   uint16_t *out;
-  float *carry;                         // [B][Hkv][segments] states (cut rows only)
+  float *carry;                         // [Hkv][carry_slots] states (cut rows only)
   int32_t num_slots, B, hq, hkv, total_q, max_q_len;
-  int32_t segments, segment_len;        // stretches a row has at most, tokens of each
+  int32_t segment_len;                  // tokens of a stretch; longer rows are cut
+  int32_t carry_slots;                  // 0: no row is cut
+  bool by_row;
   float scale;
 };
 
@@ -200,6 +202,33 @@ __device__ __forceinline__ int fresh(int x) {
   return x;
 }
 
+// Where stretches are, without a pass that counts them. With L a stretch's tokens, the
+// stretches of row b can have the places from floor((cu_q[b] - b) / L) + b on: ceil(T / L)
+// of them end by the next row's. Cut rows alone can have those from 2 cu_q[b] / L on, as
+// T > L: of these there are no more with more rows. The carry takes the fewer.
+__device__ __forceinline__ int start_of(const LinearArgs &a, int b) {
+  return min(max(a.cu_q[b], 0), a.total_q);
+}
+__device__ __forceinline__ int place_of(const LinearArgs &a, int start, int b, bool by_row) {
+  if (!by_row) return (int)(2u * (uint32_t)start / (uint32_t)a.segment_len);
+  return b + (start >= b ? (start - b) / a.segment_len : -((b - start + a.segment_len - 1) / a.segment_len));
+}
+// The last row whose value (non-decreasing) is no larger than x, by every wave for itself.
+template <typename Value>
+__device__ __forceinline__ int last_row(int rows, int x, Value value) {
+  int lo = 0, end = rows;
+  while (end - lo > 1) {
+    const int step = (end - lo + kWave - 1) / kWave, b = lo + (int)(threadIdx.x % kWave) * step;
+    const int n = __popcll(__ballot(b < end && value(min(b, end - 1)) <= x));
+    lo += max(n - 1, 0) * step;
+    end = min(lo + step, end);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+// The states before a cut row's stretches.
+__device__ __forceinline__ float *carry_of(const LinearArgs &a, int start, int b, int g) {
+  return a.carry + ((int64_t)g * a.carry_slots + place_of(a, start, b, a.by_row)) * kStateSize;
+}
 
 // One stretch of a (row, KV head): chunks in order, the state in the accumulators. Wave w
 // of 8 holds the 16 value dims from 16 w, all 128 key dims: tile t = 2 x + y has key dims
@@ -209,28 +238,34 @@ __device__ __forceinline__ int fresh(int x) {
 // value dims of a token. Scores go through LDS: a wave computes two of the 16 tiles, all
 // waves use all of them.
 //
-// A step is a chunk and a query head of the group, with two barriers: the step's tiles are
-// there (scores, then with the chunk's last head the state's update); the scores are there
-// (outputs, while the next chunk's K and V load; V's tile is free once the first head
-// has its operands, K's after the update). Q has two tiles. 73 KB of LDS and 128 registers:
-// two workgroups per CU, whose steps overlap.
-template <bool kStates, int kHeads>
+// A step is a chunk and kHeads query heads of the group, with three barriers: the step's
+// tiles are there (scores, the state's part of the results, and with the chunk's last heads
+// the state's update); the scores are there (their part of the results, which go into Q's
+// tiles); the results are there (they leave as whole rows). K and V have two stages, the next
+// chunk's loads go out during the first heads' step; Q has two buffers of kHeads tiles. 108 KB
+// of LDS (149 KB with two heads) and up to 256 registers: one workgroup per CU.
+template <bool kStates, int kHeads, bool kCut>
 __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_kernel(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
   // the outputs pass starts with what the states pass read last, and may still be cached
-  int unit = kStates ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
-  const int seg = unit % a.segments;
-  unit /= a.segments;
-  const int g = unit % a.hkv, b = unit / a.hkv, group = a.hq / a.hkv;
-
-  const int row0 = min(max(a.cu_q[b], 0), a.total_q);
+  const int unit = kStates ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
+  const int items = gridDim.x / a.hkv, group = a.hq / a.hkv;
+  int g = unit % a.hkv, b = unit / a.hkv, seg = 0;
+  if (kCut) {
+    const bool by_row = !kStates || a.by_row;
+    const int item = unit % items;
+    g = unit / items;
+    b = last_row(a.B, item, [&](int i) { return place_of(a, start_of(a, i), i, by_row); });
+    seg = max(item - place_of(a, start_of(a, b), b, by_row), 0);
+  }
+  const int row0 = start_of(a, b);
   const int T = min(min(max(a.cu_q[b + 1], row0), a.total_q) - row0, a.max_q_len);
+  if (seg >= (T + a.segment_len - 1) / a.segment_len) return;
   const int from = seg * a.segment_len;
-  if (from >= T) return;
   const int len = min(T - from, a.segment_len);
-  const bool whole = T <= a.segment_len;    // an uncut row keeps its own state
+  const bool whole = !kCut || T <= a.segment_len;    // an uncut row keeps its own state
   if (kStates && whole) return;
   const int64_t tok0 = row0 + from;
   const int slot = a.slots[b];
@@ -300,7 +335,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   // state tile t = 2 x + y, register i: key dim 32 x + 8 quad + 4 y + i, value dim 16 wave + r
   f32x4 s[8];
   float *pool = a.states + ((int64_t)slot * a.hkv + g) * kStateSize;
-  float *carry = whole ? pool : a.carry + (((int64_t)b * a.hkv + g) * a.segments + seg) * kStateSize;
+  float *carry = whole ? pool : carry_of(a, row0, b, g) + (int64_t)seg * kStateSize;
   const bool zero = kStates || (whole && a.ctx_lens[b] <= 0);
   float *const s_at = carry + 8 * quad * kHeadDim + 16 * wave + r;
 #pragma unroll
@@ -329,10 +364,46 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
 #pragma unroll
     for (int x = 0; x < 2; ++x) vf[x] = read_transposed(tile + 32 * x * kHeadDim, at_v);
   };
+  // An infinite or NaN value makes NaN of a score of zero: tokens before it would have it too.
+  // A wave with such values multiplies with zeros in their place, and makes NaN of their dims
+  // from their tokens on.
+  auto not_finite = [](uint32_t bits) { return (bits & 0x7f80u) == 0x7f80u; };
+  auto strange = [&](const bf16x8(&vf)[2]) {
+    uint32_t any = 0;                                   // an exponent of ones carries into the sign
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const u32x4 w = __builtin_bit_cast(u32x4, vf[x]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) any |= (w[e] & 0x7f807f80u) + 0x00800080u;
+    }
+    return __ballot(any & 0x80008000u) != 0;
+  };
+  auto zero_strange = [&](bf16x8(&vf)[2]) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      u32x4 w = __builtin_bit_cast(u32x4, vf[x]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        w[e] &= (not_finite(w[e]) ? 0u : 0xffffu) | (not_finite(w[e] >> 16) ? 0u : 0xffff0000u);
+      vf[x] = __builtin_bit_cast(bf16x8, w);
+    }
+  };
+  auto fill_strange = [&](uint16_t *results, const uint16_t *tile, int n) {
+    uint32_t bad = 0;
+    const int l = fresh(lane), unit = 2 * wave + (l >> 5), half = (l >> 4 & 1) * 4;
+#pragma unroll 1
+    for (int t = 0; t < n; ++t) {
+      const int at = t * kHeadDim + ((unit ^ swizzle(t)) << 3) + half;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        bad |= not_finite(tile[at + e]) << e;
+        if (t % 16 == l % 16 && (bad >> e & 1)) results[at + e] = 0x7fc0;
+      }
+    }
+  };
   // S' = decay S + K^T (after l^(n-1-j) V), n the chunk's tokens: the decayed values in
-  // three bf16 parts, which hold all 24 bits (a stretch of a cut row needs the state as bf16
-  // operands only: two parts, so that nothing but the operands' own rounding counts). The states pass has no state to decay: its weights reach to
-  // the end of the stretch (after = l^tokens behind the chunk).
+  // bf16 parts, of which three hold all 24 bits. The states pass has no state to decay: its
+  // weights reach to the end of the stretch (after = l^tokens behind the chunk).
   auto update = [&](auto parts, const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay,
                     float after) {
     constexpr int kParts = decltype(parts)::value;
@@ -388,155 +459,169 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
       mult[jj][i] = d >= 0 ? a.scale * __builtin_amdgcn_exp2f(l2 * (float)d) : 0.f;
     }
 
-  int q_buf = 0;
-  double drift = 1.0;
-  for (int c = 0; c < chunks; ++c) {
-    const int n = min(len - c * kChunk, kChunk);
-    bf16x8 vf[2];
-    const int buf = c & 1;
-    const bool more = c + 1 < chunks;
-    const int left = len - 1 - (c + 1) * kChunk;        // rows behind the next chunk's first
-    const uint16_t *const tk = sk + buf * kTile, *const tv = sv + buf * kTile;
-    kp += kv_chunk;
-    vp += kv_chunk;
-    auto load_k = [&]() {
-      if (more) load(lds_k + (buf ^ 1) * kTile * 2, kp, kv_off, kv_stride, left);
-    };
-    auto load_v = [&]() {
-      if (more) load(lds_v + (buf ^ 1) * kTile * 2, vp, kv_off, kv_stride, left);
-    };
-    if constexpr (kStates) {
-      await_loads();
-      __syncthreads();
-      load_k();
-      load_v();
-      read_v(vf, tv);
-      update(std::integral_constant<int, 3>(), vf, tk, n, 1.f,
-             __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
-    } else {
-      bf16x8 sb[4];                                     // the state before the chunk, in bf16
-#pragma unroll
-      for (int x = 0; x < 4; ++x)
-        sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-      for (int h = 0; h < group; h += kHeads) {
-        uint16_t *const tq = sq + q_buf * kHeads * kTile;
-        const bool last = h + kHeads == group;
-        // behind the tiles' loads: the step before's stores, two a head where its chunk was full
-        if (n == kChunk && (c > 0 || h > 0)) {
-          await_loads_before<2 * kHeads>();
-        } else {
-          await_loads();
-        }
+  auto steps = [&](auto parts) {
+    int q_buf = 0;
+    double drift = 1.0;
+    for (int c = 0; c < chunks; ++c) {
+      const int n = min(len - c * kChunk, kChunk);
+      bf16x8 vf[2];
+      bool odd = false;                                   // values that are infinite or NaN
+      const int buf = c & 1;
+      const bool more = c + 1 < chunks;
+      const int left = len - 1 - (c + 1) * kChunk;        // rows behind the next chunk's first
+      const uint16_t *const tk = sk + buf * kTile, *const tv = sv + buf * kTile;
+      kp += kv_chunk;
+      vp += kv_chunk;
+      auto load_k = [&]() {
+        if (more) load(lds_k + (buf ^ 1) * kTile * 2, kp, kv_off, kv_stride, left);
+      };
+      auto load_v = [&]() {
+        if (more) load(lds_v + (buf ^ 1) * kTile * 2, vp, kv_off, kv_stride, left);
+      };
+      if constexpr (kStates) {
+        await_loads();
         __syncthreads();
-        // K of the wave's two score tiles: those of tokens 16 it + r against 16 jt + 4 quad +
-        // 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero, and needed where a
-        // tile shares 32 slots with one on it.
-        const int it_p = wave & 3, jt_p = wave >> 2, at = fresh(at_row), pt = fresh(at_p);
-        bf16x8 kf[2][4];
+        load_k();
+        load_v();
+        read_v(vf, tv);
+        update(std::integral_constant<int, 3>(), vf, tk, n, 1.f,
+               __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
+      } else {
+        bf16x8 sb[4];                                     // the state before the chunk, in bf16
 #pragma unroll
-        for (int x = 0; x < 4; ++x) kf[0][x] = lds_bf16x8(tk + 16 * jt_p * kHeadDim, at ^ (x << 6));
-        if (it_p >= 2)
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-            kf[1][x] = lds_bf16x8(tk + 16 * (jt_p + 2) * kHeadDim, at ^ (x << 6));
-        if (h == 0) read_v(vf, tv);
-        q_buf ^= 1;
-        if (!last) {
-          load_q(q_buf, qp + (h + kHeads) * kHeadDim, left + kChunk);
-        } else if (more) {
-          load_q(q_buf, qp + q_chunk, left);
-        }
-        f32x4 acc[kHeads][4];
-#pragma unroll
-        for (int j = 0; j < kHeads; ++j) {
-          const uint16_t *const tj = tq + j * kTile;
-          // Q of all tokens, and of those of the wave's scores
-          bf16x8 qf[4][4], qs[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) qs[x] = lds_bf16x8(tj + 16 * it_p * kHeadDim, at ^ (x << 6));
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int it = 0; it < 4; ++it)
-              qf[it][x] = lds_bf16x8(tj + 16 * it * kHeadDim, at ^ (x << 6));
-          keep_order();
-          f32x4 p[2];
-          p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int it = 0; it < 4; ++it) acc[j][it] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            p[0] = mfma16x16x32(kf[0][x], qs[x], p[0]);
-#pragma unroll
-            for (int it = 0; it < 4; ++it) acc[j][it] = mfma16x16x32(sb[x], qf[it][x], acc[j][it]);
+        for (int x = 0; x < 4; ++x)
+          sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+        for (int h = 0; h < group; h += kHeads) {
+          uint16_t *const tq = sq + q_buf * kHeads * kTile;
+          const bool last = h + kHeads == group;
+          // behind the tiles' loads: the step before's stores, two a head where its chunk was full
+          if (n == kChunk && (c > 0 || h > 0)) {
+            await_loads_before<2 * kHeads>();
+          } else {
+            await_loads();
           }
+          __syncthreads();
+          // K of the wave's two score tiles: those of tokens 16 it + r against 16 jt + 4 quad +
+          // 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero, and needed where a
+          // tile shares 32 slots with one on it.
+          const int it_p = wave & 3, jt_p = wave >> 2, at = fresh(at_row), pt = fresh(at_p);
+          bf16x8 kf[2][4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) kf[0][x] = lds_bf16x8(tk + 16 * jt_p * kHeadDim, at ^ (x << 6));
           if (it_p >= 2)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) p[1] = mfma16x16x32(kf[1][x], qs[x], p[1]);
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            if (jj == 1 && it_p < 2) break;
-            bf16x4 w;
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i]);
-            *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(sp + j * kChunk * kChunk) +
-                                        (pt ^ (jj << 6))) = w;
+            for (int x = 0; x < 4; ++x)
+              kf[1][x] = lds_bf16x8(tk + 16 * (jt_p + 2) * kHeadDim, at ^ (x << 6));
+          if (h == 0) read_v(vf, tv);
+          q_buf ^= 1;
+          if (!last) {
+            load_q(q_buf, qp + (h + kHeads) * kHeadDim, left + kChunk);
+          } else if (more) {
+            load_q(q_buf, qp + q_chunk, left);
           }
+          f32x4 acc[kHeads][4];
 #pragma unroll
-          for (int it = 0; it < 4; ++it) acc[j][it] *= power[16 * it + r + 1];
-        }
-        if (h == 0) load_k();
-        if (last && whole) {
-          // the product of the chunks' decays as they were rounded is kept at l^tokens: what
-          // one rounding adds, the next chunk's takes off
-          const double exact = decays[n];
-          const float decay = (float)(exact * drift);
-          if (exact > 1e-30) drift = exact * drift / decay;
-          update(std::integral_constant<int, 3>(), vf, tk, n, decay, 1.f);
-        } else if (last && more) {
-          update(std::integral_constant<int, 2>(), vf, tk, n, (float)decays[kChunk], 1.f);
-        }
-        if (h == 0) load_v();
-        __syncthreads();
-        const int st = fresh(at_score);
+          for (int j = 0; j < kHeads; ++j) {
+            const uint16_t *const tj = tq + j * kTile;
+            // Q of all tokens, and of those of the wave's scores
+            bf16x8 qf[4][4], qs[4];
 #pragma unroll
-        for (int j = 0; j < kHeads; ++j) {
-          bf16x8 pf[4][2];
+            for (int x = 0; x < 4; ++x) qs[x] = lds_bf16x8(tj + 16 * it_p * kHeadDim, at ^ (x << 6));
 #pragma unroll
-          for (int it = 0; it < 4; ++it)
+            for (int x = 0; x < 4; ++x)
 #pragma unroll
-            for (int x = 0; x <= it / 2; ++x)
-              pf[it][x] = lds_bf16x8(sp + j * kChunk * kChunk + 16 * it * kChunk, st ^ (x << 6));
+              for (int it = 0; it < 4; ++it)
+                qf[it][x] = lds_bf16x8(tj + 16 * it * kHeadDim, at ^ (x << 6));
+            keep_order();
+            f32x4 p[2];
+            p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int x = 0; x < 2; ++x)
+            for (int it = 0; it < 4; ++it) acc[j][it] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int it = 2 * x; it < 4; ++it) acc[j][it] = mfma16x16x32(vf[x], pf[it][x], acc[j][it]);
-        }
-        // the results through Q's tiles, which nothing reads any more: a wave has 32 bytes of
-        // each token, whose stores alone took longer than the products; whole rows leave
-        const int ot = fresh(at_o);
+            for (int x = 0; x < 4; ++x) {
+              p[0] = mfma16x16x32(kf[0][x], qs[x], p[0]);
 #pragma unroll
-        for (int j = 0; j < kHeads; ++j)
+              for (int it = 0; it < 4; ++it) acc[j][it] = mfma16x16x32(sb[x], qf[it][x], acc[j][it]);
+            }
+            if (it_p >= 2)
 #pragma unroll
-          for (int it = 0; it < 4; ++it)
-            *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(tq + j * kTile + 16 * it * kHeadDim) +
-                                        ot) = __builtin_convertvector(acc[j][it], bf16x4);
-        __syncthreads();
+              for (int x = 0; x < 4; ++x) p[1] = mfma16x16x32(kf[1][x], qs[x], p[1]);
 #pragma unroll
-        for (int j = 0; j < kHeads; ++j)
+            for (int jj = 0; jj < 2; ++jj) {
+              if (jj == 1 && it_p < 2) break;
+              bf16x4 w;
 #pragma unroll
-          for (int m = 0; m < 2; ++m) {
-            const u32x4 w = load_u32x4(tq + j * kTile + (8 * wave + 4 * m) * kHeadDim + lane * 8);
-            char *const o_row = reinterpret_cast<char *>(op + (h + j) * kHeadDim);
-            if (n == kChunk || 8 * wave + 4 * m + lane / 16 < n)
-              store_u32x4(reinterpret_cast<uint16_t *>(
-                              o_row + (m ? (q_off ^ 32) + 4 * q_stride : q_off)), w);
+              for (int i = 0; i < 4; ++i)
+                w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i]);
+              *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(sp + j * kChunk * kChunk) +
+                                          (pt ^ (jj << 6))) = w;
+            }
+#pragma unroll
+            for (int it = 0; it < 4; ++it) acc[j][it] *= power[16 * it + r + 1];
           }
+          if (h == 0) load_k();
+          if (odd && last) read_v(vf, tv);
+          if (last && (whole || more)) {
+            // the product of the chunks' decays as they were rounded is kept at l^tokens: what
+            // one rounding adds, the next chunk's takes off
+            const double exact = decays[n];
+            const float decay = (float)(exact * drift);
+            if (exact > 1e-30) drift = exact * drift / decay;
+            update(parts, vf, tk, n, decay, 1.f);
+          }
+          if (h == 0) odd = strange(vf);
+          if (odd && (h == 0 || last)) zero_strange(vf);
+          if (h == 0) load_v();
+          __syncthreads();
+          const int st = fresh(at_score);
+#pragma unroll
+          for (int j = 0; j < kHeads; ++j) {
+            bf16x8 pf[4][2];
+#pragma unroll
+            for (int it = 0; it < 4; ++it)
+#pragma unroll
+              for (int x = 0; x <= it / 2; ++x)
+                pf[it][x] = lds_bf16x8(sp + j * kChunk * kChunk + 16 * it * kChunk, st ^ (x << 6));
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+              for (int it = 2 * x; it < 4; ++it) acc[j][it] = mfma16x16x32(vf[x], pf[it][x], acc[j][it]);
+          }
+          // the results through Q's tiles, which nothing reads any more: a wave has 32 bytes of
+          // each token, whose stores alone took longer than the products; whole rows leave
+          const int ot = fresh(at_o);
+#pragma unroll
+          for (int j = 0; j < kHeads; ++j)
+#pragma unroll
+            for (int it = 0; it < 4; ++it)
+              *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(tq + j * kTile + 16 * it * kHeadDim) +
+                                          ot) = __builtin_convertvector(acc[j][it], bf16x4);
+          if (odd)
+            for (int j = 0; j < kHeads; ++j) fill_strange(tq + j * kTile, tv, n);
+          __syncthreads();
+#pragma unroll
+          for (int j = 0; j < kHeads; ++j)
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+              const u32x4 w = load_u32x4(tq + j * kTile + (8 * wave + 4 * m) * kHeadDim + lane * 8);
+              char *const o_row = reinterpret_cast<char *>(op + (h + j) * kHeadDim);
+              if (n == kChunk || 8 * wave + 4 * m + lane / 16 < n)
+                store_u32x4(reinterpret_cast<uint16_t *>(
+                                o_row + (m ? (q_off ^ 32) + 4 * q_stride : q_off)), w);
+            }
+        }
+        qp += q_chunk;
+        op += q_chunk;
       }
-      qp += q_chunk;
-      op += q_chunk;
     }
+  };
+  // a stretch of a cut row needs the state as bf16 operands only: two parts, so that nothing
+  // but the operands' own rounding counts. (Compiled again for these; with two heads a step
+  // that has no registers left.)
+  if (kCut && kHeads == 1 && !whole) {
+    steps(std::integral_constant<int, 2>());
+  } else {
+    steps(std::integral_constant<int, 3>());
   }
   if (kStates || whole) {
 #pragma unroll
@@ -550,14 +635,20 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
 // The state before each stretch of a row in place of the stretch's own contribution, and
 // the state after the last one in the pool. A thread takes four elements.
 __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
-  const int g = blockIdx.y % a.hkv, b = blockIdx.y / a.hkv;
-  const int row0 = min(max(a.cu_q[b], 0), a.total_q);
+  const int g = blockIdx.y % a.hkv;
+  int b = blockIdx.y / a.hkv;
+  if (!a.by_row) {                      // cut rows differ in start / L
+    const int x = b;
+    b = last_row(a.B, x, [&](int i) { return start_of(a, i) / a.segment_len; });
+    if (start_of(a, b) / a.segment_len != x) return;
+  }
+  const int row0 = start_of(a, b);
   const int T = min(min(max(a.cu_q[b + 1], row0), a.total_q) - row0, a.max_q_len);
   const int slot = a.slots[b];
   if (T <= a.segment_len || slot < 0 || slot >= a.num_slots) return;
   const int at = (blockIdx.x * kThreads + threadIdx.x) * 4;
   float *pool = a.states + ((int64_t)slot * a.hkv + g) * kStateSize + at;
-  float *carry = a.carry + ((int64_t)b * a.hkv + g) * a.segments * kStateSize + at;
+  float *carry = carry_of(a, row0, b, g) + at;
   const double ld = log_decay_of(a.log_decay, g);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (a.ctx_lens[b] > 0) s = *reinterpret_cast<const f32x4 *>(pool);
@@ -575,28 +666,30 @@ __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
 
 // How an append call is cut.
 struct LinearPlan {
-  int32_t segments, segment_len;
+  int32_t segment_len, stretches, carry_slots;
+  bool by_row;
 };
-LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int32_t max_q_len) {
+LinearPlan linear_plan(int32_t B, int32_t hkv, int32_t total_q, int32_t max_q_len) {
   // a workgroup's even share of the call's chunks; a longest row up to twice as long is
   // left whole
-  const int64_t chunks = ((int64_t)max_q_len + kChunk - 1) / kChunk;
+  const int32_t longest = max_q_len < total_q ? max_q_len : total_q;
+  const int64_t chunks = ((int64_t)longest + kChunk - 1) / kChunk;
   const int64_t share = ((int64_t)total_q * hkv / kComputeUnits + kChunk - 1) / kChunk;
-  LinearPlan p = {1, max_q_len};
+  LinearPlan p = {longest, B, 0, true};  // whole rows
   if (chunks > 2 * share && chunks > 1) {
-    const int64_t per = share < 1 ? 1 : share;
-    p.segment_len = (int32_t)(per * kChunk);
-    p.segments = (int32_t)((chunks + per - 1) / per);
+    p.segment_len = (int32_t)((share < 1 ? 1 : share) * kChunk);
+    p.stretches = B + (total_q > B ? (total_q - B) / p.segment_len : 0);
+    const int32_t of_cut = (int32_t)(2 * (int64_t)total_q / p.segment_len) + 1;
+    p.by_row = p.stretches <= of_cut;
+    p.carry_slots = p.by_row ? p.stretches : of_cut;
   }
   return p;
 }
 
 }  // namespace
 
-size_t linear_append_workspace_bytes(int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
-                                     int32_t max_q_len) {
-  const LinearPlan p = linear_plan(B, hq, hkv, total_q, max_q_len);
-  return p.segments > 1 ? (size_t)B * hkv * p.segments * kStateSize * sizeof(float) : 0;
+size_t linear_append_workspace_bytes(int32_t B, int32_t hkv, int32_t total_q, int32_t max_q_len) {
+  return (size_t)linear_plan(B, hkv, total_q, max_q_len).carry_slots * hkv * kStateSize * sizeof(float);
 }
 
 hipError_t launch_linear_decode(const uint16_t *q, const uint16_t *k, const uint16_t *v,
@@ -621,22 +714,30 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
                                 int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
                                 int32_t max_q_len, float scale, uint16_t *out, void *workspace,
                                 hipStream_t stream) {
-  const LinearPlan p = linear_plan(B, hq, hkv, total_q, max_q_len);
+  const LinearPlan p = linear_plan(B, hkv, total_q, max_q_len);
   LinearArgs a = {q, k, v, cu_q, ctx_lens, states, slots, log_decay, out,
                   static_cast<float *>(workspace), num_slots, B, hq, hkv, total_q, max_q_len,
-                  p.segments, p.segment_len, scale};
-  const unsigned pairs = (unsigned)B * (unsigned)hkv;
-  const dim3 grid(pairs * p.segments), threads(kAppendThreads);
-  if (p.segments > 1) {
-    hipLaunchKernelGGL((linear_chunk_kernel<true, 1>), grid, threads, 0, stream, a);
-    hipLaunchKernelGGL(linear_scan_kernel, dim3(kStateSize / (4 * kThreads), pairs),
+                  p.segment_len, p.carry_slots, p.by_row, scale};
+  const dim3 threads(kAppendThreads);
+  const dim3 grid((unsigned)p.stretches * (unsigned)hkv);
+  if (p.carry_slots) {
+    const unsigned rows = (unsigned)(p.by_row ? B : total_q / p.segment_len + 1);
+    hipLaunchKernelGGL((linear_chunk_kernel<true, 1, true>), dim3((unsigned)p.carry_slots * (unsigned)hkv),
+                       threads, 0, stream, a);
+    hipLaunchKernelGGL(linear_scan_kernel,
+                       dim3(kStateSize / (4 * kThreads), rows * (unsigned)hkv),
                        dim3(kThreads), 0, stream, a);
   }
   // two query heads a step share K's operands and the step's waits
-  if (hq / hkv % 2 == 0)
-    hipLaunchKernelGGL((linear_chunk_kernel<false, 2>), grid, threads, 0, stream, a);
+  const bool pairs = hq / hkv % 2 == 0, cut = p.carry_slots > 0;
+  if (pairs && cut)
+    hipLaunchKernelGGL((linear_chunk_kernel<false, 2, true>), grid, threads, 0, stream, a);
+  else if (pairs)
+    hipLaunchKernelGGL((linear_chunk_kernel<false, 2, false>), grid, threads, 0, stream, a);
+  else if (cut)
+    hipLaunchKernelGGL((linear_chunk_kernel<false, 1, true>), grid, threads, 0, stream, a);
   else
-    hipLaunchKernelGGL((linear_chunk_kernel<false, 1>), grid, threads, 0, stream, a);
+    hipLaunchKernelGGL((linear_chunk_kernel<false, 1, false>), grid, threads, 0, stream, a);
   return hipGetLastError();
 }
 

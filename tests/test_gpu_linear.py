@@ -2,7 +2,7 @@
 
 Tolerances, relative to a tensor's 2-norm. out: three roundings to bf16 (the scores, the
 state as the query meets it, the result), each at most 2^-8 relative to its value: 3 * 2^-8.
-Decode rounds the result alone: 2^-8. states: fp32 products and sums, the decayed keys in
+Decode rounds the result alone: 2^-8. states: fp32 products and sums, the decayed values in
 three parts (2^-24), over at most T / 64 chunk steps whose errors of 2^-24 add up where a
 state remembers them all: (4 + T / 64) 2^-24.
 """
@@ -101,6 +101,45 @@ def test_append_ragged_rows(device):
 def test_append_long_row_in_stretches(device):
     check_append([5000], [0], 2, 2, seed=2)
     check_append([3001, 17, 1024], [4, 0, 6], 2, 1, seed=3)
+
+
+@pytest.mark.parametrize("T,Hkv", [
+    ([3] * 150 + [2000] + [1] * 30 + [1100, 0, 2], 4),   # more rows than stretches
+    ([1, 0, 700, 129, 0, 640], 1),
+    ([2] * 64 + [900], 1), ([900] + [2] * 65, 1)])
+def test_append_long_rows_among_short_ones(T, Hkv, device):
+    d, out, states = check_append(T, [b % 3 for b in range(len(T))], Hkv, Hkv, seed=len(T))
+    need = ra.linear_append_workspace_size(len(T), Hkv, Hkv, sum(T), max(T))
+    assert 0 < need <= (2 * 256 + Hkv) * 65536            # two stretches a compute unit
+    tight = torch.empty(need, dtype=torch.uint8, device="cuda:0").fill_(0xff)
+    again, states2 = run_append(d, T, workspace=tight)
+    assert torch.equal(again, out) and torch.equal(states2, states)
+
+
+@pytest.mark.parametrize("T,at", [([200, 40], 70), ([200, 40], 199), ([200, 40], 0), ([3000], 1500),
+                                  ([3000], 2999)])
+@pytest.mark.parametrize("what", ["k", "v"])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_append_keeps_what_is_not_finite_behind(T, at, what, bad, device):
+    """An infinite or NaN key or value changes its own token and later ones alone: for a key
+    all of the KV head's dims, for a value its dim."""
+    d = make(T, [3] * len(T), 4, 2, seed=at)
+    out, states = run_append(d, T)
+    d[what][at, 1, 37] = bad
+    out2, states2 = run_append(d, T)
+    own = torch.zeros_like(out, dtype=torch.bool)
+    kept = torch.zeros_like(states, dtype=torch.bool)
+    slot = d["slots"][0].item()
+    if what == "k":
+        own[at:T[0], 2:] = True
+        kept[slot, 1, 37] = True
+    else:
+        own[at:T[0], 2:, 37] = True
+        kept[slot, 1, :, 37] = True
+    assert torch.equal(out2[~own], out[~own])
+    assert torch.equal(states2[~kept], states[~kept])
+    assert not torch.isfinite(out2[at, 2:][own[at, 2:]]).any()
+    assert not torch.isfinite(states2[kept]).any()
 
 
 @pytest.mark.parametrize("decay", [[0.0, -1e-6], [-1e-4, -50.0], [float("-inf"), -1000.0],

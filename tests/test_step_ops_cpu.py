@@ -93,6 +93,11 @@ def test_linear_append_validation(lib):
     assert _append(lib, ws=None, **one) == _lib.RA_ERR_WORKSPACE
     assert _append(lib, ws=ctypes.c_void_p(0x1008), **one) == _lib.RA_ERR_WORKSPACE
     assert size(256, 32, 32, 25600, 100) == 0                         # whole rows need none
+    # the stretches of cut rows take the place, however many rows there are beside them
+    state = 128 * 128 * 4
+    assert size(60000, 8, 8, 200000, 140000) <= (2 * 256 + 8) * state
+    assert size(1, 8, 8, 16384, 2**31 - 1) == size(1, 8, 8, 16384, 16384) <= (256 + 8) * state
+    assert _append(lib, B=65535, Hq=65, Hkv=65) == _lib.RA_ERR_UNSUPPORTED   # 2^22 pairs
 
 
 def test_table_validation(lib):
