@@ -443,7 +443,8 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
   if (tid == 0) a.border[n] = b;
 }
 
-// The weight of a logit in the row's range.
+// The weight of a logit in a row with filters: by this wherever one is taken, so that sums and
+// what they are compared with agree to the last unit.
 struct Weigh {
   TableExp exp;
   double top;
@@ -451,7 +452,7 @@ struct Weigh {
   __device__ __forceinline__ Weigh(const double *table, double inv_t, float t)
       : exp(table, inv_t), top((double)t), infinite(t == __builtin_inff()) {}
   __device__ __forceinline__ double operator()(float z) const {
-    return infinite ? 1.0 : exp((double)z - top);
+    return infinite ? (z == __builtin_inff() ? 1.0 : 0.0) : exp((double)z - top);
   }
 };
 
@@ -508,8 +509,9 @@ __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   }
 }
 
-// The end's bins, from weights and counts of eight neighbouring bins a lane, by one wave. `mass0` and `count0` are ahead of the first bin; by_k: top-k may end in a bin;
-// `all`: what top-p takes its share of if it does not.
+// The end's bins, from weights and counts of eight neighbouring bins a lane, by one wave.
+// `mass0` and `count0` are ahead of the first bin; by_k: top-k may end in a bin; `all`: what
+// top-p takes its share of if it does not.
 constexpr int kOwnBins = kBins / kWave;
 __device__ __forceinline__ void locate(const uint64_t (&m)[kOwnBins], const uint32_t (&c)[kOwnBins],
                                        uint64_t mass0, uint32_t count0, bool by_k, uint32_t k,
@@ -698,7 +700,7 @@ struct PickLds {
   uint32_t first_of[kMaxChunks];        // and where its listed elements start
   uint64_t mpart[kPickThreads / kWave];
   double dpart[kPickThreads / kWave];
-  uint32_t cpart[kPickThreads / kWave];
+  double table[kExpTable];
   uint64_t sum;
   uint32_t key, count, ties, high, low;
   int token;
@@ -716,6 +718,7 @@ struct Edge {
 struct Goals {
   const Row &row;
   const Border &b;
+  const Weigh &weigh;
   double all;                           // what top-p takes its share of if top-k keeps all
   uint32_t high;                        // key of the first of finer bins,
   int shift;                            // and their width; < 0: the row's bins
@@ -724,7 +727,7 @@ struct Goals {
     return bin_of(below(b.top, value_of(key)), b.rate);
   }
   __device__ __forceinline__ double weight(uint32_t key) const {
-    return weight_exp(scaled(value_of(key), b.top, row.inv_t));
+    return weigh(value_of(key));
   }
   __device__ __forceinline__ bool ends_in_k() const { return row.k > 0 && b.bin_k < kBins; }
   // the weight at which top-p ends, given what top-k keeps of bin_k
@@ -1006,6 +1009,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     load_four(a.c_lowest + (at - 4 * lane), a.chunks, 0xffffffffu, key_low);
     load_four(a.c_kept + (at - 4 * lane), a.chunks, (uint64_t)0, kept);
     b = a.ends[n];
+    fill_table(lds.table);
+    __syncthreads();
   } else if (!row.greedy) {
     load_four(a.c_sum + (at - 4 * lane), a.chunks, 0.0, c_sum);
   }
@@ -1025,6 +1030,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     return;
   }
 
+  const Weigh weigh(lds.table, row.inv_t, top);
   Edge end = {0, 0, kByIndex};                        // everything
   Drawn drawn;
   if (!row.filtered()) {
@@ -1050,8 +1056,8 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     for (int i = 1; i < 4; ++i) first[i] = first[i - 1] + listed[i - 1];
     Border fine = b;                                  // of what is still in question
     const double all = row.k > 0 ? (double)b.mass_k : b.sum * kUnit;
-    const Goals rough = {row, b, all, 0, -1};
-    Goals g = {row, fine, all, high, -1};
+    const Goals rough = {row, b, weigh, all, 0, -1};
+    Goals g = {row, fine, weigh, all, high, -1};
     // `ties` of the equal elements `key`, listed[] and first[] of them in the chunks
     auto split_ties = [&](uint32_t key, uint32_t of_them) {
       const double e = g.weight(key);
@@ -1117,12 +1123,12 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
           atomicAdd(&lds.counts[bin], 1u);
           atomicAdd((unsigned long long *)&lds.mass[bin], (unsigned long long)w);
         };
-        auto weigh = [&](uint64_t x) { return units(g.weight((uint32_t)(x >> 32))); };
+        auto units_of = [&](uint64_t x) { return units(g.weight((uint32_t)(x >> 32))); };
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
-          if (held[j]) put(held[j], weight[j] = weigh(held[j]));
+          if (held[j]) put(held[j], weight[j] = units_of(held[j]));
         for_listed(a, n, kHeld * kPickThreads, listed_all, lds.first_of,
-                   [&](int, uint64_t x) { put(x, weigh(x)); });
+                   [&](int, uint64_t x) { put(x, units_of(x)); });
         __syncthreads();
         uint64_t m[kOwnBins];
         uint32_t c[kOwnBins];
@@ -1148,7 +1154,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
         for (int j = 0; j < kHeld; ++j)
           if (held[j]) settle(of_chunk[j], held[j], weight[j]);
         for_listed(a, n, kHeld * kPickThreads, listed_all, lds.first_of,
-                   [&](int chunk, uint64_t x) { settle(chunk, x, weigh(x)); });
+                   [&](int chunk, uint64_t x) { settle(chunk, x, units_of(x)); });
         __syncthreads();
         count = lds.count;
         high = lds.high;
@@ -1213,16 +1219,16 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   double w[kOwn], own = 0.0, all;
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
-    const double x = scaled(z[i], top, row.inv_t);
-    bool in = true;
+    double e = 0.0;
     if (row.filtered()) {
       const uint32_t key = key_of(z[i]);
       const bool tied = key == end.key && (end.ties == kByIndex ? (uint32_t)(v0 + i) <= end.index
                                                                 : seen++ < end.ties);
       const bool sure = b.lo >= 0 && (!row.binned() || bin_of(below(top, z[i]), b.rate) < b.lo);
-      in = key > end.key || tied || sure;
+      if (key > end.key || tied || sure) e = weigh(z[i]);
+    } else {
+      e = weight_exp(scaled(z[i], top, row.inv_t));
     }
-    const double e = in ? weight_exp(x) : 0.0;
     w[i] = e < row.m ? 0.0 : row.filtered() ? (double)units(e) : e;
     own += w[i];
   }
