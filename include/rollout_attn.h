@@ -518,9 +518,9 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
  *   workspace  device scratch of at least rollout_linear_attn_append_workspace_size(B, Hq,
  *              Hkv, total_q, max_q_len) bytes (contents on entry ignored), 16-byte
  *              aligned; NULL where the size is 0. Calls that share one must not overlap.
- *   The rest as for decode; rows without tokens leave their state as it is. How a long row
- *   is cut into stretches, and with it the order of fp32 sums, depends on B, Hq, Hkv,
- *   total_q and max_q_len alone.
+ *   The rest as for decode; rows without tokens leave their state as it is. Whether
+ *   long rows are cut into stretches, and with it the order of fp32 sums, depends on B, Hq,
+ *   Hkv, total_q and max_q_len alone.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, Hq or Hkv or num_slots <= 0, Hq % Hkv,
  *         total_q < 0, max_q_len < 0, scale not finite); RA_ERR_UNSUPPORTED (Hq / Hkv > 32,
  *         B > 65535, Hq > 65535, B * Hkv > 2^22, or q, k_new, v_new, states or out not

@@ -508,7 +508,7 @@ size_t rollout_linear_attn_append_workspace_size(int32_t B, int32_t Hq, int32_t 
                                                  int32_t total_q, int32_t max_q_len) {
   if (check_linear(B, Hq, Hkv, 1, 1.f) != RA_OK || B == 0 || total_q <= 0 || max_q_len <= 0)
     return 0;
-  return ra::linear_append_workspace_bytes(B, Hkv, total_q, max_q_len);
+  return ra::linear_append_workspace_bytes(B, Hq, Hkv, total_q, max_q_len);
 }
 
 int rollout_linear_attn_append(const void *q, const void *k_new, const void *v_new,
@@ -526,7 +526,7 @@ int rollout_linear_attn_append(const void *q, const void *k_new, const void *v_n
   if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(states) ||
       !aligned16(out))
     return RA_ERR_UNSUPPORTED;
-  const size_t need = ra::linear_append_workspace_bytes(B, Hkv, total_q, max_q_len);
+  const size_t need = ra::linear_append_workspace_bytes(B, Hq, Hkv, total_q, max_q_len);
   if (need > 0 && (!workspace || !aligned16(workspace) || workspace_bytes < need))
     return RA_ERR_WORKSPACE;
   return hip_status(ra::launch_linear_append(

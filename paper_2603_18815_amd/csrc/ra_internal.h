@@ -114,7 +114,8 @@ hipError_t launch_linear_decode(const uint16_t *q, const uint16_t *k, const uint
                                 const int32_t *kv_lens, const float *log_decay, int32_t B,
                                 int32_t hq, int32_t hkv, float scale, uint16_t *out,
                                 hipStream_t stream);
-size_t linear_append_workspace_bytes(int32_t B, int32_t hkv, int32_t total_q, int32_t max_q_len);
+size_t linear_append_workspace_bytes(int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
+                                     int32_t max_q_len);
 hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint16_t *v,
                                 const int32_t *cu_q, const int32_t *ctx_lens, float *states,
                                 const int32_t *slots, int32_t num_slots, const float *log_decay,

@@ -35,10 +35,12 @@ struct LinearArgs {
   const int32_t *slots;
   const float *log_decay;
   uint16_t *out;
-  float *carry;                         // [Hkv][carry_slots] states (cut rows only)
+  float *carry;                         // cut rows: [Hkv][carry_slots] states before stretches
+                                        // parts > 1: [B][Hkv] states after the call
   int32_t num_slots, B, hq, hkv, total_q, max_q_len;
   int32_t segment_len;                  // tokens of a stretch; longer rows are cut
   int32_t carry_slots;                  // 0: no row is cut
+  int32_t parts;                        // workgroups that share a whole row's query heads
   bool by_row;
   float scale;
 };
@@ -225,6 +227,18 @@ __device__ __forceinline__ int last_row(int rows, int x, Value value) {
   }
   return __builtin_amdgcn_readfirstlane(lo);
 }
+// The row of that rank, the longest first: of up to 64.
+__device__ __forceinline__ int longest_row(const LinearArgs &a, int rank) {
+  const int lane = threadIdx.x % kWave;
+  const int mine = lane < a.B ? start_of(a, lane + 1) - start_of(a, lane) : -1;
+  int ahead = 0;
+  for (int i = 0; i < a.B; ++i) {
+    const int other = __builtin_amdgcn_readlane(mine, i);
+    ahead += other > mine || (other == mine && i < lane);
+  }
+  return __ffsll((unsigned long long)__ballot(lane < a.B && ahead == rank)) - 1;
+}
+
 // The states before a cut row's stretches.
 __device__ __forceinline__ float *carry_of(const LinearArgs &a, int start, int b, int g) {
   return a.carry + ((int64_t)g * a.carry_slots + place_of(a, start, b, a.by_row)) * kStateSize;
@@ -250,10 +264,13 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int r = lane % 16, quad = lane / 16;
   // the outputs pass starts with what the states pass read last, and may still be cached
-  const int unit = kStates ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
-  const int items = gridDim.x / a.hkv, group = a.hq / a.hkv;
-  int g = unit % a.hkv, b = unit / a.hkv, seg = 0;
-  if (kCut) {
+  const int unit = !kCut || kStates ? blockIdx.x : gridDim.x - 1 - blockIdx.x;
+  const int items = gridDim.x / a.hkv, group = a.hq / a.hkv / a.parts;
+  int g = unit % a.hkv, b = unit / a.hkv / a.parts, seg = 0;
+  const int part = unit / a.hkv % a.parts;
+  if (!kCut) {
+    if (a.B <= kWave) b = longest_row(a, b);
+  } else {
     const bool by_row = !kStates || a.by_row;
     const int item = unit % items;
     g = unit / items;
@@ -268,12 +285,13 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   const bool whole = !kCut || T <= a.segment_len;    // an uncut row keeps its own state
   if (kStates && whole) return;
   const int64_t tok0 = row0 + from;
+  const int head0 = (g * a.parts + part) * group;
   const int slot = a.slots[b];
   if (slot < 0 || slot >= a.num_slots) {
     if (!kStates)
       for (int t = 0; t < len; ++t)
         for (int i = tid; i < group * kHeadDim; i += kAppendThreads)
-          a.out[((tok0 + t) * a.hq + g * group) * kHeadDim + i] = 0;
+          a.out[((tok0 + t) * a.hq + head0) * kHeadDim + i] = 0;
     return;
   }
 
@@ -318,7 +336,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   };
   const int chunks = (len + kChunk - 1) / kChunk;
   const size_t q_chunk = (size_t)kChunk * a.hq * kHeadDim, kv_chunk = (size_t)kChunk * a.hkv * kHeadDim;
-  const size_t q_first = ((size_t)tok0 * a.hq + g * group) * kHeadDim;
+  const size_t q_first = ((size_t)tok0 * a.hq + head0) * kHeadDim;
   const uint16_t *kp = a.k + ((size_t)tok0 * a.hkv + g) * kHeadDim;   // the chunk to load next
   const uint16_t *vp = a.v + ((size_t)tok0 * a.hkv + g) * kHeadDim;
   const uint16_t *qp = a.q + q_first;                                 // the chunk at hand
@@ -561,7 +579,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
           }
           if (h == 0) load_k();
           if (odd && last) read_v(vf, tv);
-          if (last && (whole || more)) {
+          if (last && (more || (whole && part == 0))) {
             // the product of the chunks' decays as they were rounded is kept at l^tokens: what
             // one rounding adds, the next chunk's takes off
             const double exact = decays[n];
@@ -623,12 +641,16 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   } else {
     steps(std::integral_constant<int, 3>());
   }
-  if (kStates || whole) {
+  if (kStates || (whole && part == 0)) {
+    // the other parts may not have read the pool yet
+    float *const to = !kCut && a.parts > 1
+                          ? a.carry + ((int64_t)b * a.hkv + g) * kStateSize + (s_at - carry)
+                          : s_at;
 #pragma unroll
     for (int t = 0; t < 8; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        s_at[(32 * (t / 2) + 4 * (t % 2) + i) * kHeadDim] = s[t][i];
+        to[(32 * (t / 2) + 4 * (t % 2) + i) * kHeadDim] = s[t][i];
   }
 }
 
@@ -664,32 +686,64 @@ __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
   *reinterpret_cast<f32x4 *>(pool) = s;
 }
 
+// The states after the call, where parts of a row's heads shared it, into the pool.
+__global__ __launch_bounds__(kThreads) void linear_states_kernel(LinearArgs a) {
+  const int g = blockIdx.y % a.hkv, b = blockIdx.y / a.hkv, slot = a.slots[b];
+  if (start_of(a, b + 1) <= start_of(a, b) || slot < 0 || slot >= a.num_slots) return;
+  const int at = (blockIdx.x * kThreads + threadIdx.x) * 4;
+  *reinterpret_cast<f32x4 *>(a.states + ((int64_t)slot * a.hkv + g) * kStateSize + at) =
+      *reinterpret_cast<const f32x4 *>(a.carry + (int64_t)blockIdx.y * kStateSize + at);
+}
+
 // How an append call is cut.
 struct LinearPlan {
-  int32_t segment_len, stretches, carry_slots;
+  int32_t segment_len, stretches, carry_slots, parts;
   bool by_row;
 };
-LinearPlan linear_plan(int32_t B, int32_t hkv, int32_t total_q, int32_t max_q_len) {
-  // a workgroup's even share of the call's chunks; a longest row up to twice as long is
-  // left whole
-  const int32_t longest = max_q_len < total_q ? max_q_len : total_q;
+// A chunk's time by a workgroup that takes `heads` query heads of it, in ns (measured, alone
+// on the GPU; an even number is taken two at once).
+int64_t chunk_ns(int32_t heads) {
+  return heads % 2 == 0 ? 1500 + 1160 * (int64_t)heads : 950 + 2000 * (int64_t)heads;
+}
+LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int32_t max_q_len) {
+  const int32_t longest = max_q_len < total_q ? max_q_len : total_q, group = hq / hkv;
   const int64_t chunks = ((int64_t)longest + kChunk - 1) / kChunk;
-  const int64_t share = ((int64_t)total_q * hkv / kComputeUnits + kChunk - 1) / kChunk;
-  LinearPlan p = {longest, B, 0, true};  // whole rows
-  if (chunks > 2 * share && chunks > 1) {
-    p.segment_len = (int32_t)((share < 1 ? 1 : share) * kChunk);
-    p.stretches = B + (total_q > B ? (total_q - B) / p.segment_len : 0);
-    const int32_t of_cut = (int32_t)(2 * (int64_t)total_q / p.segment_len) + 1;
-    p.by_row = p.stretches <= of_cut;
-    p.carry_slots = p.by_row ? p.stretches : of_cut;
-  }
-  return p;
+  // a compute unit's even share of the call's chunks
+  int64_t share = ((int64_t)total_q * hkv / kComputeUnits + kChunk - 1) / kChunk;
+  share = share < 1 ? 1 : share;
+  LinearPlan p = {longest, B, 0, 1, true};  // whole rows
+  if (chunks <= share) return p;
+  // Compute units are idle behind the longest row. Either they share whole rows by their
+  // heads (each part keeps the state for itself, one writes it out, a launch behind sets it in
+  // the pool), where there are that many more of them than of longest rows; or rows are cut.
+  // Measured, 32 heads on 8, rows of 2,048: 16 rows 223 us as they are, 166 by two parts;
+  // 8 rows 213, by four parts 113, cut 146; 4 rows 203, 103, 83; rows of 512: 8 rows 58, 38,
+  // 53; 2 rows 55, 32, 26.
+  while (group % (2 * p.parts) == 0 && 4 * (2 * p.parts) * share <= 5 * chunks &&
+         (int64_t)B * hkv <= 2 * kComputeUnits)
+    p.parts *= 2;
+  // the parts read K and V again
+  const int64_t whole_ns =
+      p.parts > 1 ? chunks * chunk_ns(group / p.parts) * 108 / 100 + 8000 : chunks * chunk_ns(group) + 5000;
+  LinearPlan c = p;
+  c.parts = 1;
+  c.segment_len = (int32_t)(share * kChunk);
+  c.stretches = B + (total_q > B ? (total_q - B) / c.segment_len : 0);
+  const int32_t of_cut = (int32_t)(2 * (int64_t)total_q / c.segment_len) + 1;
+  c.by_row = c.stretches <= of_cut;
+  c.carry_slots = c.by_row ? c.stretches : of_cut;
+  // 2 us of the states pass, 3 us for the bandwidth that all units share, and the states of
+  // the stretches written and read
+  const int64_t cut_ns = share * (chunk_ns(group) + 5000) + 8000 + 85 * (int64_t)c.carry_slots * hkv;
+  return cut_ns < whole_ns ? c : p;
 }
 
 }  // namespace
 
-size_t linear_append_workspace_bytes(int32_t B, int32_t hkv, int32_t total_q, int32_t max_q_len) {
-  return (size_t)linear_plan(B, hkv, total_q, max_q_len).carry_slots * hkv * kStateSize * sizeof(float);
+size_t linear_append_workspace_bytes(int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
+                                     int32_t max_q_len) {
+  const LinearPlan p = linear_plan(B, hq, hkv, total_q, max_q_len);
+  return (size_t)(p.parts > 1 ? B : p.carry_slots) * hkv * kStateSize * sizeof(float);
 }
 
 hipError_t launch_linear_decode(const uint16_t *q, const uint16_t *k, const uint16_t *v,
@@ -714,12 +768,12 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
                                 int32_t B, int32_t hq, int32_t hkv, int32_t total_q,
                                 int32_t max_q_len, float scale, uint16_t *out, void *workspace,
                                 hipStream_t stream) {
-  const LinearPlan p = linear_plan(B, hkv, total_q, max_q_len);
+  const LinearPlan p = linear_plan(B, hq, hkv, total_q, max_q_len);
   LinearArgs a = {q, k, v, cu_q, ctx_lens, states, slots, log_decay, out,
                   static_cast<float *>(workspace), num_slots, B, hq, hkv, total_q, max_q_len,
-                  p.segment_len, p.carry_slots, p.by_row, scale};
+                  p.segment_len, p.carry_slots, p.parts, p.by_row, scale};
   const dim3 threads(kAppendThreads);
-  const dim3 grid((unsigned)p.stretches * (unsigned)hkv);
+  const dim3 grid((unsigned)(p.stretches * p.parts) * (unsigned)hkv);
   if (p.carry_slots) {
     const unsigned rows = (unsigned)(p.by_row ? B : total_q / p.segment_len + 1);
     hipLaunchKernelGGL((linear_chunk_kernel<true, 1, true>), dim3((unsigned)p.carry_slots * (unsigned)hkv),
@@ -729,7 +783,7 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
                        dim3(kThreads), 0, stream, a);
   }
   // two query heads a step share K's operands and the step's waits
-  const bool pairs = hq / hkv % 2 == 0, cut = p.carry_slots > 0;
+  const bool pairs = hq / hkv / p.parts % 2 == 0, cut = p.carry_slots > 0;
   if (pairs && cut)
     hipLaunchKernelGGL((linear_chunk_kernel<false, 2, true>), grid, threads, 0, stream, a);
   else if (pairs)
@@ -738,6 +792,9 @@ hipError_t launch_linear_append(const uint16_t *q, const uint16_t *k, const uint
     hipLaunchKernelGGL((linear_chunk_kernel<false, 1, true>), grid, threads, 0, stream, a);
   else
     hipLaunchKernelGGL((linear_chunk_kernel<false, 1, false>), grid, threads, 0, stream, a);
+  if (p.parts > 1)
+    hipLaunchKernelGGL(linear_states_kernel, dim3(kStateSize / (4 * kThreads), (unsigned)B * (unsigned)hkv),
+                       dim3(kThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -116,6 +116,29 @@ def test_append_long_rows_among_short_ones(T, Hkv, device):
     assert torch.equal(again, out) and torch.equal(states2, states)
 
 
+@pytest.mark.parametrize("Hq,Hkv", [(32, 8), (16, 8), (64, 8)])
+def test_append_rows_shared_by_their_heads(Hq, Hkv, device):
+    """Few rows of some length: workgroups that share a row's query heads, one of which
+    writes the state. With an empty row, one of a token, one without a slot, one that is new."""
+    T = [512, 130, 450, 0, 500, 1, 512, 64, 401]
+    ctx = [3, 0, 1, 5, 9, 7, 0, 2, 4]
+    d = make(T, ctx, Hq, Hkv, seed=Hq)
+    d["slots"][4] = -1
+    states = d["states"].clone()
+    need = ra.linear_append_workspace_size(len(T), Hq, Hkv, sum(T), max(T))
+    assert need == len(T) * Hkv * 65536                   # a state a row
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda:0").fill_(0xff)
+    out = ra.linear_append(d["q"], d["k"], d["v"], d["cu"], d["ctx"], states, d["slots"],
+                           d["decay"], workspace=ws)
+    want, wstates = recurrence(d, T, [c <= 0 for c in ctx])
+    assert rel(out, want) <= 3 * 2.0 ** -8
+    assert (out[sum(T[:4]):sum(T[:5])] == 0).all()
+    assert rel(states, wstates) <= (4 + max(T) / 64) * 2.0 ** -24
+    kept = [i for i in range(states.shape[0]) if i not in
+            [d["slots"][b].item() for b in range(len(T)) if T[b]]]
+    assert torch.equal(states[kept], d["states"][kept])
+
+
 @pytest.mark.parametrize("T,at", [([200, 40], 70), ([200, 40], 199), ([200, 40], 0), ([3000], 1500),
                                   ([3000], 2999)])
 @pytest.mark.parametrize("what", ["k", "v"])
