@@ -12,8 +12,8 @@
 //   stats   each chunk's and each of its lanes' largest logit, the chunk's smallest, and its
 //           sum of weights (rows without filters, or with top-p alone)
 //   range   a workgroup a row: how far below M the end can lie. Top-k: the k-th of the
-//           lanes' largest logits is no larger than the k-th logit. Top-p: elements below
-//           (1 - p) sum / V weigh less than (1 - p) sum together.
+//           largest logits of parts of the row is no larger than the k-th logit. Top-p:
+//           elements below (1 - p) sum / V weigh less than (1 - p) sum together.
 //   bins    counts and weights of the elements in the range, in 512 bins of it
 //   border  the bin or bins that hold the end. What lies above is kept: each chunk sums it;
 //           the elements in them are listed
@@ -135,6 +135,26 @@ struct TableExp {
   }
 };
 
+// What a workgroup has of its chunks, for the next launches: a cache line each, written as a
+// whole.
+struct alignas(128) Stats {
+  float top[kGroup], low[kGroup];       // largest and smallest finite logit
+  double sum[kGroup];                   // of weights against top
+  uint32_t first[kGroup];               // lowest index of the largest one
+};
+struct alignas(128) Kept {
+  uint64_t mass[kGroup];                // weight kept for certain
+  uint32_t listed[kGroup];              // elements in the border's bins
+  uint32_t high[kGroup], low[kGroup];   // their largest and smallest key
+};
+// By the first lanes of a wave, from LDS.
+template <typename Line>
+__device__ __forceinline__ void write_line(Line *to, const Line *lds) {
+  static_assert(sizeof(Line) == 128, "a line");
+  const int lane = threadIdx.x % kWave;
+  if (lane < 32) reinterpret_cast<uint32_t *>(to)[lane] = reinterpret_cast<const uint32_t *>(lds)[lane];
+}
+
 struct SampleArgs {
   const void *logits;
   const float *temperature;
@@ -145,17 +165,13 @@ struct SampleArgs {
   int64_t row_stride;
   int32_t N, V, chunks, groups;         // groups: of kGroup chunks
   // workspace
-  float *c_top, *c_low;                 // [N][chunks] largest and smallest finite logit
+  Stats *stats;                         // [N][groups]
   float *l_top;                         // [N][chunks][kWave] largest of a lane's
-  uint32_t *c_first;                    // [N][chunks] lowest index of the largest one
-  double *c_sum;                        // [N][chunks] sum of weights against c_top
   uint64_t *bin_mass;                   // [N][kBins]
   uint32_t *bin_count;                  // [N][kBins]
-  uint64_t *c_kept;                     // [N][chunks] weight kept for certain
-  uint32_t *c_listed;                   // [N][chunks] elements in the border's bins
-  uint32_t *c_high, *c_lowest;          // [N][chunks] their largest and smallest key
+  Kept *kept;                           // [N][groups]
   uint64_t *list;                       // [N][chunks][kListed] key << 32 | ~index
-  struct Border *border, *ends;         // [N] with the range; with the end's bins too
+  struct BorderLine *border, *ends;     // [N] with the range; with the end's bins too
 };
 
 // What a row asks for. The four loads go out together: a parameter that is not given is read
@@ -195,6 +211,10 @@ struct Border {
   int lo, hi, bin_k;                    // kBins: none
   uint32_t count_lo, count_k;           // elements before bin lo, bin_k
   uint64_t mass_lo, mass_k;             // weights before them
+};
+
+struct alignas(128) BorderLine {
+  Border b;
 };
 
 // The bin of a logit, `below` under the largest one: non-decreasing in it. kBins: beyond.
@@ -317,62 +337,74 @@ __device__ __forceinline__ void fill_table(double *table) {
 
 template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_stats_kernel(SampleArgs a) {
-  const int n = blockIdx.x / a.groups, lane = threadIdx.x % kWave;
-  const int c = blockIdx.x % a.groups * kGroup + threadIdx.x / kWave;
+  const int n = blockIdx.x / a.groups, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int c = blockIdx.x % a.groups * kGroup + wave;
   __shared__ double table[kExpTable];
+  __shared__ Stats own;
   const Row row(a, n);
   if (row.needs_sums()) {
     fill_table(table);
     __syncthreads();
   }
-  if (c >= a.chunks) return;
-  float z[kPer];
-  load_chunk<T, kPer>(a, n, c, z);
-  float mine = -__builtin_inff();
+  float z[kPer], top = -__builtin_inff(), low = __builtin_inff();
+  int first = a.V;
+  double sum = 0.0;
+  if (c < a.chunks) {
+    load_chunk<T, kPer>(a, n, c, z);
+    float mine = -__builtin_inff();
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, z[i]);
-  const float top = wave_reduce(mine, max_of);
-  const int64_t at = (int64_t)n * a.chunks + c;
-  if (lane == 0) a.c_top[at] = top;
-  if (row.greedy) {
-    int first = a.V;
+    for (int i = 0; i < kPer; ++i) mine = fmaxf(mine, z[i]);
+    top = wave_reduce(mine, max_of);
+    if (row.greedy) {
 #pragma unroll
-    for (int i = kPer - 1; i >= 0; --i) first = z[i] == top ? index_of<T, kPer>(c, i) : first;
-    first = wave_reduce(first, [](int x, int y) { return min(x, y); });
-    if (lane == 0) a.c_first[at] = first;
-    return;
-  }
-  if (row.filtered()) a.l_top[at * kWave + lane] = mine;
-  if (row.binned()) {
-    float low = __builtin_inff();
+      for (int i = kPer - 1; i >= 0; --i) first = z[i] == top ? index_of<T, kPer>(c, i) : first;
+      first = wave_reduce(first, [](int x, int y) { return min(x, y); });
+    } else {
+      if (row.filtered()) a.l_top[((int64_t)n * a.chunks + c) * kWave + lane] = mine;
+      if (row.binned()) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) low = z[i] > -__builtin_inff() ? fminf(low, z[i]) : low;
-    low = wave_reduce(low, min_of);
-    if (lane == 0) a.c_low[at] = low;
-  }
-  if (row.needs_sums()) {
-    double sum = 0.0;
-    if (top > -__builtin_inff()) {
-      const TableExp weight(table, row.inv_t);
-      const double from = flatten(z, top);
+        for (int i = 0; i < kPer; ++i) low = z[i] > -__builtin_inff() ? fminf(low, z[i]) : low;
+        low = wave_reduce(low, min_of);
+      }
+      if (row.needs_sums()) {
+        if (top > -__builtin_inff()) {
+          const TableExp weight(table, row.inv_t);
+          const double from = flatten(z, top);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) sum += weight((double)z[i] - from);
+          for (int i = 0; i < kPer; ++i) sum += weight((double)z[i] - from);
+        }
+        sum = wave_reduce(sum, [](double x, double y) { return x + y; });
+      }
     }
-    sum = wave_reduce(sum, [](double x, double y) { return x + y; });
-    if (lane == 0) a.c_sum[at] = sum;
   }
+  if (lane == 0) own.top[wave] = top, own.low[wave] = low, own.sum[wave] = sum, own.first[wave] = first;
+  __syncthreads();
+  if (wave == 0) write_line(a.stats + blockIdx.x, &own);
 }
 
-// A value of a lane's i-th of four chunks, for every wave by itself: read whether there is
-// such a chunk or not (the last one instead), so that the loads go out together.
-static_assert(kMaxChunks == 4 * kWave, "four chunks a lane");
+// A lane holds the four chunks of the group of its number, every wave all of them. Their
+// lines are read whether there is such a group or not (the last one instead) and whatever
+// the row asks for, and awaited together: each load behind a branch is another round trip to
+// memory, 0.7 us for a row by itself and 7 us among 512.
+static_assert(kMaxChunks == kGroup * kWave && kGroup == 4, "a group a lane");
+template <typename Line>
+__device__ __forceinline__ const Line &line_of(const Line *lines, int n, int groups) {
+  return lines[(int64_t)n * groups + min((int)(threadIdx.x % kWave), groups - 1)];
+}
 template <typename V>
-__device__ __forceinline__ void load_four(const V *of_row, int chunks, V none, V (&x)[4]) {
-  const int c = 4 * (threadIdx.x % kWave);
+__device__ __forceinline__ void load_four(const V (&of_group)[kGroup], V (&x)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = of_row[min(c + i, chunks - 1)];
+  for (int i = 0; i < 4; ++i) x[i] = of_group[i];
+}
+// Loads before are issued, and awaited, by here.
+template <typename V>
+__device__ __forceinline__ void here(V (&x)[4]) {
+  asm volatile("" : "+v"(x[0]), "+v"(x[1]), "+v"(x[2]), "+v"(x[3]));
+}
+template <typename V>
+__device__ __forceinline__ void mask_four(int groups, V none, V (&x)[4]) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) x[i] = c + i < chunks ? x[i] : none;
+  for (int i = 0; i < 4; ++i) x[i] = (int)(threadIdx.x % kWave) < groups ? x[i] : none;
 }
 __device__ __forceinline__ float top_of(const float (&c_top)[4]) {
   return wave_reduce(fmaxf(fmaxf(c_top[0], c_top[1]), fmaxf(c_top[2], c_top[3])), max_of);
@@ -382,37 +414,57 @@ __device__ __forceinline__ float top_of(const float (&c_top)[4]) {
 __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a) {
   const int n = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const Row row(a, n);
-  if (!row.filtered()) return;
   __shared__ uint32_t count[kBins];
+  __shared__ BorderLine own;
   const int64_t at = (int64_t)n * a.chunks;
+  const Stats &of = line_of(a.stats, n, a.groups);
   float c_top[4], c_low[4];
-  load_four(a.c_top + at, a.chunks, -__builtin_inff(), c_top);
-  if (row.binned()) load_four(a.c_low + at, a.chunks, __builtin_inff(), c_low);
   double c_sum[4];
-  if (row.needs_sums()) load_four(a.c_sum + at, a.chunks, 0.0, c_sum);
-  Border b = Border();
-  b.top = top_of(c_top);
+  load_four(of.top, c_top);
+  load_four(of.low, c_low);
+  load_four(of.sum, c_sum);
+  here(c_top);
+  here(c_low);
+  here(c_sum);
+  if (!row.filtered()) return;
+  mask_four(a.groups, -__builtin_inff(), c_top);
+  mask_four(a.groups, __builtin_inff(), c_low);
+  mask_four(a.groups, 0.0, c_sum);
+  const float top = top_of(c_top);
+  double sum = 0.0;
   double range = kRange;
   if (row.binned()) {
     static_assert(kRowThreads == kBins, "a bin a thread");
     a.bin_mass[(int64_t)n * kBins + tid] = 0;
     a.bin_count[(int64_t)n * kBins + tid] = 0;
     const float low = wave_reduce(fminf(fminf(c_low[0], c_low[1]), fminf(c_low[2], c_low[3])), min_of);
-    range = fmin(range, -scaled(fminf(low, b.top), b.top, row.inv_t));
+    range = fmin(range, -scaled(fminf(low, top), top, row.inv_t));
     if (row.k > 0) {
-      // the k-th of the lanes' largest logits, as far as a bin tells
+      // the k-th of the largest logits of chunks, of four lanes or of lanes, of the coarsest
+      // that are twice as many: the k-th of any k elements will do. As far as a bin tells.
       count[tid] = 0;
       __syncthreads();
       const float rate = rate_of(range, row.inv_t);
+      auto put = [&](float z) {
+        const int bin = bin_of(below(top, z), rate);
+        if (bin < kBins) atomicAdd(&count[bin], 1u);
+      };
       const int parts = a.chunks * kWave / 4;
-      const f32x4 *l_top = reinterpret_cast<const f32x4 *>(a.l_top + at * kWave);
-#pragma unroll 4
-      for (int i = tid; i < parts; i += kRowThreads) {
-        const f32x4 z = l_top[i];
+      if (2 * row.k <= a.chunks) {
+        if (tid < kWave)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int bin = bin_of(below(b.top, z[e]), rate);
-          if (bin < kBins) atomicAdd(&count[bin], 1u);
+          for (int i = 0; i < 4; ++i) put(c_top[i]);
+      } else {
+        const f32x4 *l_top = reinterpret_cast<const f32x4 *>(a.l_top + at * kWave);
+#pragma unroll 4
+        for (int i = tid; i < parts; i += kRowThreads) {
+          const f32x4 z = l_top[i];
+          if (2 * row.k <= parts) {
+            put(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) put(z[e]);
+          }
         }
       }
       __syncthreads();
@@ -432,15 +484,18 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
     } else {
       double x = 0.0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x += c_sum[i] * weight_exp(scaled(c_top[i], b.top, row.inv_t));
-      b.sum = wave_reduce(x, [](double u, double v) { return u + v; });
-      if (row.p > 0.0) range = fmin(range, log((double)a.V / ((1.0 - row.p) * b.sum)) + 1e-3);
+      for (int i = 0; i < 4; ++i) x += c_sum[i] * weight_exp(scaled(c_top[i], top, row.inv_t));
+      sum = wave_reduce(x, [](double u, double v) { return u + v; });
+      if (row.p > 0.0) range = fmin(range, log((double)a.V / ((1.0 - row.p) * sum)) + 1e-3);
     }
   } else {
     range = fmin(range, -log(row.m) + 1e-12);
   }
-  b.rate = rate_of(range, row.inv_t);
-  if (tid == 0) a.border[n] = b;
+  // member by member: a struct copied here is kept in memory, in LDS by the number of the
+  // thread, for which the launch's packet is read from the host: 5 us, 15 us of 512 workgroups
+  if (tid == 0) own.b.sum = sum, own.b.top = top, own.b.rate = rate_of(range, row.inv_t);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (tid < kWave) write_line(a.border + n, &own);
 }
 
 // The weight of a logit in a row with filters: by this wherever one is taken, so that sums and
@@ -465,11 +520,10 @@ template <typename T, int kPer>
 __global__ __launch_bounds__(kThreads) void sample_bins_kernel(SampleArgs a) {
   const int n = blockIdx.x / a.groups, tid = threadIdx.x, lane = tid % kWave;
   const int c0 = blockIdx.x % a.groups * kGroup, c = c0 + tid / kWave;
-  const int64_t at = (int64_t)n * a.chunks + c0;
-  const Border b = a.border[n];
+  const Border b = a.border[n].b;
   float c_top[kGroup];
 #pragma unroll
-  for (int i = 0; i < kGroup; ++i) c_top[i] = c0 + i < a.chunks ? a.c_top[at + i] : -__builtin_inff();
+  for (int i = 0; i < kGroup; ++i) c_top[i] = a.stats[blockIdx.x].top[i];
   const float l_top = c < a.chunks ? a.l_top[((int64_t)n * a.chunks + c) * kWave + lane] : 0.f;
   const Row row(a, n);
   if (!row.binned() || b.top == -__builtin_inff()) return;
@@ -598,71 +652,68 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   const int n = blockIdx.x / a.groups, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const int c0 = blockIdx.x % a.groups * kGroup, c = c0 + wave;
   const int64_t at = (int64_t)n * a.chunks + c;
-  Border b = a.border[n];
-  const float c_top = c < a.chunks ? a.c_top[at] : -__builtin_inff();
+  Border b = a.border[n].b;
+  const float c_top = a.stats[blockIdx.x].top[wave];
   const float l_top = c < a.chunks ? a.l_top[at * kWave + lane] : -__builtin_inff();
   const Row row(a, n);
   if (!row.filtered() || b.top == -__builtin_inff()) return;
   __shared__ double table[kExpTable];
-  __shared__ uint32_t s_listed[kGroup];
-  __shared__ Border found;
+  __shared__ uint64_t list[kGroup][kListed];
+  __shared__ Kept own;
+  __shared__ BorderLine found;
   const bool mine = in_range(b, c_top);
+  if (lane == 0) own.mass[wave] = 0, own.listed[wave] = 0, own.high[wave] = 0, own.low[wave] = 0xffffffffu;
   if (!__syncthreads_or(mine)) {
-    if (lane == 0 && c < a.chunks) a.c_kept[at] = 0, a.c_listed[at] = 0;
+    if (wave == 0) write_line(a.kept + blockIdx.x, &own);
     return;
   }
-  if (lane == 0) s_listed[wave] = 0;      // each wave has its own
   fill_table(table);
-  if (!row.binned()) {
-    b.lo = b.hi = b.bin_k = kBins;
-    __syncthreads();
-  } else {
-    if (wave == 0) {                      // 6 KB of bins: read by one of the waves
+  if (wave == 0) {                        // 6 KB of bins: read by one of the waves
+    if (row.binned())
       find_border(a, n, row, b);
-      if (lane == 0) found = b;
-    }
-    __syncthreads();
-    b = found;
+    else
+      b.lo = b.hi = b.bin_k = kBins;
+    if (lane == 0) found.b = b;
   }
-  if (!mine) {
-    if (lane == 0 && c < a.chunks) a.c_kept[at] = 0, a.c_listed[at] = 0;
-    return;
-  }
-  uint64_t kept = 0;
-  uint32_t high = 0, low = 0xffffffffu;
-  if (in_range(b, l_top)) {
-    float z[kPer];
-    load_chunk<T, kPer>(a, n, c, z);
-    const Weigh weigh(table, row.inv_t, b.top);
+  __syncthreads();
+  b = found.b;
+  if (mine) {
+    uint64_t kept = 0;
+    uint32_t high = 0, low = 0xffffffffu;
+    if (in_range(b, l_top)) {
+      float z[kPer];
+      load_chunk<T, kPer>(a, n, c, z);
+      const Weigh weigh(table, row.inv_t, b.top);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int bin = bin_of(below(b.top, z[i]), b.rate);
-      if (bin < b.lo) {
-        const double e = weigh(z[i]);
-        if (e >= row.m) kept += units(e);
-      } else if (bin < kBins && (bin <= b.hi || bin == b.bin_k)) {
-        const uint32_t slot = atomicAdd(&s_listed[wave], 1u), key = key_of(z[i]);
-        if (slot < (uint32_t)kListed)
-          a.list[at * kListed + slot] = (uint64_t)key << 32 | (uint32_t)~index_of<T, kPer>(c, i);
-        high = key > high ? key : high;
-        low = key < low ? key : low;
+      for (int i = 0; i < kPer; ++i) {
+        const int bin = bin_of(below(b.top, z[i]), b.rate);
+        if (bin < b.lo) {
+          const double e = weigh(z[i]);
+          if (e >= row.m) kept += units(e);
+        } else if (bin < kBins && (bin <= b.hi || bin == b.bin_k)) {
+          const uint32_t slot = atomicAdd(&own.listed[wave], 1u), key = key_of(z[i]);
+          if (slot < (uint32_t)kListed)
+            list[wave][slot] = (uint64_t)key << 32 | (uint32_t)~index_of<T, kPer>(c, i);
+          high = key > high ? key : high;
+          low = key < low ? key : low;
+        }
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int listed = min(__shfl(lane == 0 ? (int)own.listed[wave] : 0, 0), kListed);
+    for (int i = lane; i < (listed + 15) / 16 * 16; i += kWave)   // whole lines
+      a.list[at * kListed + i] = list[wave][i];
+    kept = wave_reduce(kept, [](uint64_t x, uint64_t y) { return x + y; });
+    if (listed) {
+      high = wave_reduce(high, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
+      low = wave_reduce(low, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
+    }
+    if (lane == 0) own.mass[wave] = kept, own.high[wave] = high, own.low[wave] = low;
+    // one of the chunks that hold the largest: all write the same
+    if (c_top == b.top) write_line(a.ends + n, &found);
   }
-  __builtin_amdgcn_wave_barrier();
-  const uint32_t listed = __shfl(lane == 0 ? s_listed[wave] : 0u, 0);
-  kept = wave_reduce(kept, [](uint64_t x, uint64_t y) { return x + y; });
-  if (listed) {
-    high = wave_reduce(high, [](uint32_t x, uint32_t y) { return x > y ? x : y; });
-    low = wave_reduce(low, [](uint32_t x, uint32_t y) { return x < y ? x : y; });
-  }
-  if (lane == 0) {
-    a.c_kept[at] = kept;
-    a.c_listed[at] = listed;
-    a.c_high[at] = high;
-    a.c_lowest[at] = low;
-    if (c_top == b.top) a.ends[n] = b;    // one of the chunks that hold it: all write the same
-  }
+  __syncthreads();
+  if (wave == 0) write_line(a.kept + blockIdx.x, &own);
 }
 
 // ---- pick -----------------------------------------------------------------------------
@@ -994,25 +1045,34 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   constexpr int chunk_len = kWave * kPer;
 
   const Row row(a, n);
-  const int64_t at = (int64_t)n * a.chunks + 4 * lane;
   const int mine = a.chunks - 4 * lane;               // of the lane's four chunks: how many are
+  const Stats &of = line_of(a.stats, n, a.groups);
   float c_top[4];
   double c_sum[4];
   uint32_t listed[4], key_high[4], key_low[4];
   uint64_t kept[4];
-  load_four(a.c_top + (at - 4 * lane), a.chunks, -__builtin_inff(), c_top);
+  const Kept &sure = line_of(a.kept, n, a.groups);
+  load_four(of.top, c_top);
+  load_four(of.sum, c_sum);
+  load_four(sure.listed, listed);
+  load_four(sure.high, key_high);
+  load_four(sure.low, key_low);
+  load_four(sure.mass, kept);
+  Border b = a.ends[n].b;
   float u = a.uniform[n];
-  Border b = Border();
+  here(c_top);
+  here(c_sum);
+  here(listed);
+  here(key_high);
+  here(key_low);
+  here(kept);
+  mask_four(a.groups, -__builtin_inff(), c_top);
+  mask_four(a.groups, 0.0, c_sum);
+  mask_four(a.groups, 0u, listed);
+  mask_four(a.groups, (uint64_t)0, kept);
   if (row.filtered()) {
-    load_four(a.c_listed + (at - 4 * lane), a.chunks, 0u, listed);
-    load_four(a.c_high + (at - 4 * lane), a.chunks, 0u, key_high);
-    load_four(a.c_lowest + (at - 4 * lane), a.chunks, 0xffffffffu, key_low);
-    load_four(a.c_kept + (at - 4 * lane), a.chunks, (uint64_t)0, kept);
-    b = a.ends[n];
     fill_table(lds.table);
     __syncthreads();
-  } else if (!row.greedy) {
-    load_four(a.c_sum + (at - 4 * lane), a.chunks, 0.0, c_sum);
   }
   const float top = top_of(c_top);
   u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
@@ -1020,7 +1080,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     int first = a.V;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (row.greedy && i < mine && c_top[i] == top) first = min(first, (int)a.c_first[at + i]);
+      if (row.greedy && i < mine && c_top[i] == top) first = min(first, (int)of.first[i]);
     first = wave_reduce(first, [](int x, int y) { return min(x, y); });
     if (tid == 0) {
       const bool none = top == -__builtin_inff();
@@ -1270,36 +1330,29 @@ int32_t sample_per(int32_t N, int32_t V) {
 
 struct SampleLayout {
   int32_t per, chunks;
-  size_t c_top, c_low, l_top, c_first, c_sum, bin_mass, bin_count, c_kept, c_listed, c_high, c_lowest, list;
-  size_t border, ends;
+  size_t stats, l_top, bin_mass, bin_count, kept, list, border, ends;
   size_t bytes;
 };
 SampleLayout sample_layout(int32_t N, int32_t V) {
   SampleLayout l;
   l.per = sample_per(N, V);
   l.chunks = (V + kWave * l.per - 1) / (kWave * l.per);
-  const size_t parts = (size_t)N * l.chunks;
+  const size_t parts = (size_t)N * l.chunks, groups = (size_t)N * ((l.chunks + kGroup - 1) / kGroup);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
     at += (bytes + 255) / 256 * 256;
     return here;
   };
-  l.c_top = take(parts * 4);
-  l.c_low = take(parts * 4);
+  l.stats = take(groups * sizeof(Stats));
   l.l_top = take(parts * kWave * 4);
-  l.c_first = take(parts * 4);
-  l.c_sum = take(parts * 8);
   l.bin_mass = take((size_t)N * kBins * 8);
   l.bin_count = take((size_t)N * kBins * 4);
-  l.c_kept = take(parts * 8);
-  l.c_listed = take(parts * 4);
-  l.c_high = take(parts * 4);
-  l.c_lowest = take(parts * 4);
+  l.kept = take(groups * sizeof(Kept));
   l.list = take(parts * kListed * 8);
-  l.border = take((size_t)N * sizeof(Border));
-  l.ends = take((size_t)N * sizeof(Border));
-  l.bytes = at;
+  l.border = take((size_t)N * sizeof(BorderLine));
+  l.ends = take((size_t)N * sizeof(BorderLine));
+  l.bytes = at + sizeof(Stats);         // to a line's start
   return l;
 }
 
@@ -1325,7 +1378,8 @@ hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, in
                          const float *min_p, const float *uniform, int32_t *tokens,
                          float *logprob, void *workspace, hipStream_t stream) {
   const SampleLayout l = sample_layout(N, V);
-  char *ws = static_cast<char *>(workspace);
+  char *ws = reinterpret_cast<char *>((reinterpret_cast<uintptr_t>(workspace) + sizeof(Stats) - 1) /
+                                      sizeof(Stats) * sizeof(Stats));
   SampleArgs a;
   a.logits = logits;
   a.temperature = temperature;
@@ -1340,20 +1394,14 @@ hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, in
   a.V = V;
   a.chunks = l.chunks;
   a.groups = (l.chunks + kGroup - 1) / kGroup;
-  a.c_top = reinterpret_cast<float *>(ws + l.c_top);
-  a.c_low = reinterpret_cast<float *>(ws + l.c_low);
-  a.c_first = reinterpret_cast<uint32_t *>(ws + l.c_first);
-  a.c_sum = reinterpret_cast<double *>(ws + l.c_sum);
+  a.stats = reinterpret_cast<Stats *>(ws + l.stats);
   a.bin_mass = reinterpret_cast<uint64_t *>(ws + l.bin_mass);
   a.bin_count = reinterpret_cast<uint32_t *>(ws + l.bin_count);
-  a.c_kept = reinterpret_cast<uint64_t *>(ws + l.c_kept);
-  a.c_listed = reinterpret_cast<uint32_t *>(ws + l.c_listed);
-  a.c_high = reinterpret_cast<uint32_t *>(ws + l.c_high);
-  a.c_lowest = reinterpret_cast<uint32_t *>(ws + l.c_lowest);
+  a.kept = reinterpret_cast<Kept *>(ws + l.kept);
   a.list = reinterpret_cast<uint64_t *>(ws + l.list);
   a.l_top = reinterpret_cast<float *>(ws + l.l_top);
-  a.border = reinterpret_cast<Border *>(ws + l.border);
-  a.ends = reinterpret_cast<Border *>(ws + l.ends);
+  a.border = reinterpret_cast<BorderLine *>(ws + l.border);
+  a.ends = reinterpret_cast<BorderLine *>(ws + l.ends);
   auto launch = [&](auto per) {
     constexpr int kPer = decltype(per)::value;
     if (bf16)
