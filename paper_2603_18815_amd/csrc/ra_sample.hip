@@ -228,11 +228,55 @@ __device__ __forceinline__ float rate_of(double range, double inv_t) {
   return (float)fmin(inv_t * (kBins / (fmax(range, 1e-30) * (1.0 + 1e-6))), 0x1.fp127);
 }
 
-// ---- reductions over a workgroup, in a fixed order ----
+// ---- reductions, in a fixed order ----
+// Another lane's value: of the lane that the data path's pattern names (a few cycles, where an
+// exchange through LDS takes over a hundred), 0 where it names none or the row of 16 lanes is
+// not in kRows; and of one lane for all.
+template <int kPattern, int kRows, typename V>
+__device__ __forceinline__ V lane_pattern(V x) {
+  if constexpr (sizeof(V) == 8) {
+    const u32x2 w = __builtin_bit_cast(u32x2, x);
+    u32x2 y;
+    y[0] = lane_pattern<kPattern, kRows>(w[0]);
+    y[1] = lane_pattern<kPattern, kRows>(w[1]);
+    return __builtin_bit_cast(V, y);
+  } else {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), kPattern,
+                                                             kRows, 0xf, false));
+  }
+}
+template <typename V>
+__device__ __forceinline__ V of_lane(V x, int lane) {
+  if constexpr (sizeof(V) == 8) {
+    const u32x2 w = __builtin_bit_cast(u32x2, x);
+    u32x2 y;
+    y[0] = of_lane(w[0], lane);
+    y[1] = of_lane(w[1], lane);
+    return __builtin_bit_cast(V, y);
+  } else {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+  }
+}
+constexpr int kSwapOnes = 0xb1, kSwapTwos = 0x4e, kMirrorHalf = 0x141, kMirrorRow = 0x140;
+constexpr int kShiftRow = 0x110, kLast15 = 0x142, kLast31 = 0x143;
+
 template <typename V, typename Op>
 __device__ __forceinline__ V wave_reduce(V x, Op op) {
-#pragma unroll
-  for (int d = kWave / 2; d > 0; d /= 2) x = op(x, __shfl_xor(x, d));
+  x = op(x, lane_pattern<kSwapOnes, 0xf>(x));
+  x = op(x, lane_pattern<kSwapTwos, 0xf>(x));
+  x = op(x, lane_pattern<kMirrorHalf, 0xf>(x));
+  x = op(x, lane_pattern<kMirrorRow, 0xf>(x));
+  return op(op(of_lane(x, 0), of_lane(x, 16)), op(of_lane(x, 32), of_lane(x, 48)));
+}
+// Sums up to and with this lane.
+template <typename V>
+__device__ __forceinline__ V wave_sums(V x) {
+  x += lane_pattern<kShiftRow + 1, 0xf>(x);
+  x += lane_pattern<kShiftRow + 2, 0xf>(x);
+  x += lane_pattern<kShiftRow + 4, 0xf>(x);
+  x += lane_pattern<kShiftRow + 8, 0xf>(x);
+  x += lane_pattern<kLast15, 0xa>(x);
+  x += lane_pattern<kLast31, 0xc>(x);
   return x;
 }
 template <int kN, typename V, typename Op>
@@ -250,12 +294,7 @@ __device__ __forceinline__ V group_reduce(V x, Op op, V *part) {
 template <int kN, typename V>
 __device__ __forceinline__ V group_scan(V x, V &total, V *part) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  V s = x;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const V y = __shfl_up(s, d);
-    if (lane >= d) s += y;
-  }
+  const V s = wave_sums(x);
   __syncthreads();
   if (lane == kWave - 1) part[wave] = s;
   __syncthreads();
@@ -271,14 +310,8 @@ __device__ __forceinline__ V group_scan(V x, V &total, V *part) {
 // Sums over the lanes before this one, and over all.
 template <typename V>
 __device__ __forceinline__ V wave_scan(V x, V &total) {
-  const int lane = threadIdx.x % kWave;
-  V s = x;
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const V y = __shfl_up(s, d);
-    if (lane >= d) s += y;
-  }
-  total = __shfl(s, kWave - 1);
+  const V s = wave_sums(x);
+  total = of_lane(s, kWave - 1);
   return s - x;
 }
 
@@ -595,10 +628,10 @@ __device__ __forceinline__ void locate(const uint64_t (&m)[kOwnBins], const uint
     const uint64_t found = __ballot(bin < kBins);
     if (found) {
       const int from = __ffsll((unsigned long long)found) - 1;
-      b.lo = b.hi = b.bin_k = __shfl(bin, from);
-      b.count_lo = b.count_k = __shfl(c_at, from);
-      b.mass_lo = b.mass_k = __shfl(m_at, from);
-      of_bin_k = __shfl(m_in, from);
+      b.lo = b.hi = b.bin_k = of_lane(bin, from);
+      b.count_lo = b.count_k = of_lane(c_at, from);
+      b.mass_lo = b.mass_k = of_lane(m_at, from);
+      of_bin_k = of_lane(m_in, from);
       all = (double)b.mass_k;
     }
   }
@@ -621,12 +654,12 @@ __device__ __forceinline__ void locate(const uint64_t (&m)[kOwnBins], const uint
       count += c[i];
     }
     const uint64_t has_lo = __ballot(lo < kBins), has_hi = __ballot(hi < kBins);
-    b.hi = has_hi ? __shfl(hi, __ffsll((unsigned long long)has_hi) - 1) : b.bin_k;
+    b.hi = has_hi ? of_lane(hi, __ffsll((unsigned long long)has_hi) - 1) : b.bin_k;
     if (has_lo) {
       const int from = __ffsll((unsigned long long)has_lo) - 1;
-      b.lo = __shfl(lo, from);
-      b.count_lo = __shfl(c_at, from);
-      b.mass_lo = __shfl(m_at, from);
+      b.lo = of_lane(lo, from);
+      b.count_lo = of_lane(c_at, from);
+      b.mass_lo = of_lane(m_at, from);
     }
   }
 }
@@ -700,7 +733,7 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    const int listed = min(__shfl(lane == 0 ? (int)own.listed[wave] : 0, 0), kListed);
+    const int listed = min(of_lane((int)own.listed[wave], 0), kListed);
     for (int i = lane; i < (listed + 15) / 16 * 16; i += kWave)   // whole lines
       a.list[at * kListed + i] = list[wave][i];
     kept = wave_reduce(kept, [](uint64_t x, uint64_t y) { return x + y; });
@@ -807,14 +840,16 @@ struct Goals {
 // is kept to the chunks' sums.
 __device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int chunk_len, PickLds &lds) {
   const int lane = threadIdx.x % kWave;
+  // each goes where as many larger ones are; the elements differ
+  const uint64_t some = __ballot(x != 0);
+  int place = x ? 0 : __popcll(some) + __popcll(~some & ((1ull << lane) - 1));
 #pragma unroll
-  for (int len = 2; len <= kWave; len *= 2)
-#pragma unroll
-    for (int step = len / 2; step > 0; step /= 2) {
-      const uint64_t y = __shfl_xor(x, step);
-      const bool first = (lane & step) == 0, falling = (lane & len) == 0;
-      x = (x < y) == (first == falling) ? y : x;
-    }
+  for (int i = 0; i < kWave; ++i) place += x && of_lane(x, i) > x;
+  const u32x2 halves = __builtin_bit_cast(u32x2, x);
+  u32x2 sorted;
+  sorted[0] = __builtin_amdgcn_ds_permute(4 * place, halves[0]);
+  sorted[1] = __builtin_amdgcn_ds_permute(4 * place, halves[1]);
+  x = __builtin_bit_cast(uint64_t, sorted);
   uint64_t w = 0, all;
   double e = 0.0;
   int bin = kBins << 10;
@@ -834,7 +869,7 @@ __device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int ch
   if (kept && e >= g.row.m)
     atomicAdd((unsigned long long *)&lds.kept_of[v / chunk_len], (unsigned long long)w);
   if (!mask) return {0xffffffffu, 0, kByIndex};
-  const uint64_t last = __shfl(x, __popcll(mask) - 1);
+  const uint64_t last = of_lane(x, __popcll(mask) - 1);
   return {(uint32_t)(last >> 32), ~(uint32_t)last, kByIndex};
 }
 
@@ -1016,7 +1051,7 @@ __device__ __forceinline__ Drawn draw_chunk(const V (&x)[4], float u) {
   }
   const uint64_t found = __ballot(chunk >= 0);       // never empty: the first that weighs is in
   const int from = kWave - 1 - __clzll((long long)found);
-  return {__shfl(chunk, from), (double)__shfl(before, from), (double)total};
+  return {of_lane(chunk, from), (double)of_lane(before, from), (double)total};
 }
 
 // The chunk of the i-th listed element; first_of: where each chunk's start.
