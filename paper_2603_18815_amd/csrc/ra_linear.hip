@@ -215,18 +215,6 @@ __device__ __forceinline__ int place_of(const LinearArgs &a, int start, int b, b
   if (!by_row) return (int)(2u * (uint32_t)start / (uint32_t)a.segment_len);
   return b + (start >= b ? (start - b) / a.segment_len : -((b - start + a.segment_len - 1) / a.segment_len));
 }
-// The last row whose value (non-decreasing) is no larger than x, by every wave for itself.
-template <typename Value>
-__device__ __forceinline__ int last_row(int rows, int x, Value value) {
-  int lo = 0, end = rows;
-  while (end - lo > 1) {
-    const int step = (end - lo + kWave - 1) / kWave, b = lo + (int)(threadIdx.x % kWave) * step;
-    const int n = __popcll(__ballot(b < end && value(min(b, end - 1)) <= x));
-    lo += max(n - 1, 0) * step;
-    end = min(lo + step, end);
-  }
-  return __builtin_amdgcn_readfirstlane(lo);
-}
 // The row of that rank, the longest first: of up to 64.
 __device__ __forceinline__ int longest_row(const LinearArgs &a, int rank) {
   const int lane = threadIdx.x % kWave;
@@ -274,7 +262,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
     const bool by_row = !kStates || a.by_row;
     const int item = unit % items;
     g = unit / items;
-    b = last_row(a.B, item, [&](int i) { return place_of(a, start_of(a, i), i, by_row); });
+    b = wave_search(a.B, item, [&](int i) { return place_of(a, start_of(a, i), i, by_row); });
     seg = max(item - place_of(a, start_of(a, b), b, by_row), 0);
   }
   const int row0 = start_of(a, b);
@@ -661,7 +649,7 @@ __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
   int b = blockIdx.y / a.hkv;
   if (!a.by_row) {                      // cut rows differ in start / L
     const int x = b;
-    b = last_row(a.B, x, [&](int i) { return start_of(a, i) / a.segment_len; });
+    b = wave_search(a.B, x, [&](int i) { return start_of(a, i) / a.segment_len; });
     if (start_of(a, b) / a.segment_len != x) return;
   }
   const int row0 = start_of(a, b);

@@ -27,6 +27,7 @@
 
 #include "ra_device.h"
 #include "ra_internal.h"
+#include "ra_wave.h"
 
 namespace ra {
 namespace {
@@ -229,37 +230,6 @@ __device__ __forceinline__ float rate_of(double range, double inv_t) {
 }
 
 // ---- reductions, in a fixed order ----
-// Another lane's value: of the lane that the data path's pattern names (a few cycles, where an
-// exchange through LDS takes over a hundred), 0 where it names none or the row of 16 lanes is
-// not in kRows; and of one lane for all.
-template <int kPattern, int kRows, typename V>
-__device__ __forceinline__ V lane_pattern(V x) {
-  if constexpr (sizeof(V) == 8) {
-    const u32x2 w = __builtin_bit_cast(u32x2, x);
-    u32x2 y;
-    y[0] = lane_pattern<kPattern, kRows>(w[0]);
-    y[1] = lane_pattern<kPattern, kRows>(w[1]);
-    return __builtin_bit_cast(V, y);
-  } else {
-    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), kPattern,
-                                                             kRows, 0xf, false));
-  }
-}
-template <typename V>
-__device__ __forceinline__ V of_lane(V x, int lane) {
-  if constexpr (sizeof(V) == 8) {
-    const u32x2 w = __builtin_bit_cast(u32x2, x);
-    u32x2 y;
-    y[0] = of_lane(w[0], lane);
-    y[1] = of_lane(w[1], lane);
-    return __builtin_bit_cast(V, y);
-  } else {
-    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
-  }
-}
-constexpr int kSwapOnes = 0xb1, kSwapTwos = 0x4e, kMirrorHalf = 0x141, kMirrorRow = 0x140;
-constexpr int kShiftRow = 0x110, kLast15 = 0x142, kLast31 = 0x143;
-
 template <typename V, typename Op>
 __device__ __forceinline__ V wave_reduce(V x, Op op) {
   x = op(x, lane_pattern<kSwapOnes, 0xf>(x));
@@ -267,17 +237,6 @@ __device__ __forceinline__ V wave_reduce(V x, Op op) {
   x = op(x, lane_pattern<kMirrorHalf, 0xf>(x));
   x = op(x, lane_pattern<kMirrorRow, 0xf>(x));
   return op(op(of_lane(x, 0), of_lane(x, 16)), op(of_lane(x, 32), of_lane(x, 48)));
-}
-// Sums up to and with this lane.
-template <typename V>
-__device__ __forceinline__ V wave_sums(V x) {
-  x += lane_pattern<kShiftRow + 1, 0xf>(x);
-  x += lane_pattern<kShiftRow + 2, 0xf>(x);
-  x += lane_pattern<kShiftRow + 4, 0xf>(x);
-  x += lane_pattern<kShiftRow + 8, 0xf>(x);
-  x += lane_pattern<kLast15, 0xa>(x);
-  x += lane_pattern<kLast31, 0xc>(x);
-  return x;
 }
 template <int kN, typename V, typename Op>
 __device__ __forceinline__ V group_reduce(V x, Op op, V *part) {

@@ -7,13 +7,15 @@
 // position 16 j is not below start_b), so one pass over the new tokens writes the table
 // (the tokens at slot 0) and the slot map.
 //
-// Bound by latency: some bytes a row, 8 a token. Every workgroup reads all rows twice (the
-// totals decide whether the call is refused, the running sums place its share of the
-// tokens) from cache, which takes the place of a second launch and a workspace. Only the
+// Bound by latency: some bytes a row, 8 a token. Every workgroup reads all rows, twice where
+// they are more than its threads (the totals decide whether the call is refused, the running
+// sums place its share of the tokens), which takes the place of a second launch and a
+// workspace. Only the
 // free list's length cannot change while other workgroups read it: one workgroup sets it
 // itself, several leave it to a launch of one thread behind them.
 #include "ra_device.h"
 #include "ra_internal.h"
+#include "ra_wave.h"
 
 namespace ra {
 namespace {
@@ -22,22 +24,12 @@ constexpr int kThreads = 1024;          // rows a scan step takes, and token slo
 constexpr int kWaves = kThreads / kWave;
 constexpr int kTokensPerGroup = 4096;   // more tokens than this are shared by workgroups
 
-__device__ __forceinline__ int64_t wave_scan(int64_t x) {   // inclusive
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int d = 1; d < kWave; d *= 2) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
-  return x;
-}
-
 // Inclusive sums of two counts over the workgroup's threads; all threads get the totals.
 __device__ __forceinline__ void group_scan(int64_t &a, int64_t &b, int64_t &total_a,
                                            int64_t &total_b, int64_t (*part)[2]) {
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  a = wave_scan(a);
-  b = wave_scan(b);
+  a = wave_sums(a);
+  b = wave_sums(b);
   __syncthreads();                      // part may still be read by the scan before
   if (lane == kWave - 1) part[wave][0] = a, part[wave][1] = b;
   __syncthreads();
