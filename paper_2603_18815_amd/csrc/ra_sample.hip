@@ -20,9 +20,13 @@
 //   pick    a workgroup a row: the listed elements binned again and the few in question
 //           sorted, the end found, the chunk of the drawn token from the chunks' sums, the
 //           token from the chunk's elements
-// Bound by the first pass's read of the logits and, for few rows, by the launches: bins and
-// border read only what the lanes' largest logits put into the range. Without filters
-// stats and pick are the whole call; with min-p alone there are no bins.
+// Without filters stats and pick are the whole call; with min-p alone there are no bins.
+// Bins and border read only what the lanes' largest logits put into the range: of 156 MB of
+// logits (512 rows of 151,936 bf16) 47 and 61. Measured there, all filters: stats 38 us (4.1
+// TB/s), range 6, bins 31, border 42, pick 24, the call 138-142; 64 rows of them with top-p 13,
+// 4, 13, 15, 20 and 66; 64 rows of fp32 without filters 12, 7 and 18 (39 MB); a row of 32,000
+// 3, 4, 5, 6, 8 and 25. The first pass is bound by its read and, where sums are wanted, by 64-bit
+// arithmetic; the others by the round trips of a workgroup that does little.
 #include <type_traits>
 
 #include "ra_device.h"
@@ -580,7 +584,8 @@ __device__ __forceinline__ void locate(const uint64_t (&m)[kOwnBins], const uint
     uint64_t mass = m_before, m_at = 0, m_in = 0;
 #pragma unroll
     for (int i = 0; i < kOwnBins; ++i) {
-      if (count < k && count + c[i] >= k) bin = kOwnBins * lane + i, c_at = count, m_at = mass, m_in = m[i];
+      if (count < k && count + c[i] >= k)
+        bin = kOwnBins * lane + i, c_at = count, m_at = mass, m_in = m[i];
       count += c[i];
       mass += m[i];
     }
@@ -654,7 +659,8 @@ __global__ __launch_bounds__(kThreads) void sample_border_kernel(SampleArgs a) {
   __shared__ Kept own;
   __shared__ BorderLine found;
   const bool mine = in_range(b, c_top);
-  if (lane == 0) own.mass[wave] = 0, own.listed[wave] = 0, own.high[wave] = 0, own.low[wave] = 0xffffffffu;
+  if (lane == 0)
+    own.mass[wave] = 0, own.listed[wave] = 0, own.high[wave] = 0, own.low[wave] = 0xffffffffu;
   if (!__syncthreads_or(mine)) {
     if (wave == 0) write_line(a.kept + blockIdx.x, &own);
     return;
@@ -1117,7 +1123,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       const double e = g.weight(key);
       const uint64_t w = units(e);
       uint64_t ties = of_them;
-      if (g.ends_in_k()) ties = (uint64_t)row.k - fine.count_k < ties ? (uint64_t)row.k - fine.count_k : ties;
+      if (g.ends_in_k()) {
+        const uint64_t of_k = (uint64_t)row.k - fine.count_k;
+        ties = of_k < ties ? of_k : ties;
+      }
       if (row.p < 1.0) ties = g.let_in(g.goal(g.ends_in_k() ? ties * w : 0), fine.mass_lo, w, ties);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -1146,13 +1155,15 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     } else {
       if (tid < kWave)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds.kept_of[4 * lane + i] = kept[i], lds.first_of[4 * lane + i] = first[i];
+        for (int i = 0; i < 4; ++i)
+          lds.kept_of[4 * lane + i] = kept[i], lds.first_of[4 * lane + i] = first[i];
       const uint32_t listed_all = count;
       if (tid == 0) lds.count = 0, lds.high = 0, lds.low = 0xffffffffu;
       uint32_t below = 0xffffffffu;                   // keys above it are kept if none listed is
       if (count <= kWave || apart) {
         __syncthreads();
-        for_listed(a, n, 0, listed_all, lds.first_of, [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
+        for_listed(a, n, 0, listed_all, lds.first_of,
+                   [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
         __syncthreads();
       } else {
         // 512 bins of the listed keys' range, and the end's among them. The first elements of
@@ -1312,14 +1323,15 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   }
 }
 
-// Elements a lane holds of a chunk: 32 (chunks of 2,048), or 16 or 8 where the call would
-// have too few workgroups to fill the GPU and the row's chunks still fit.
+// Elements a lane holds of a chunk: 32 (chunks of 2,048), and fewer where the call would have
+// few workgroups and the row's chunks still fit. Measured, bf16 with top-p, by 8 / 16 / 32: a
+// row of 32,000 24 / 27 / 38 us, 32 of 128,000 41 / 37 / 40, 128 of 32,000 39 / 36 / 42; by
+// 16 / 32: 64 of 100,000 47 / 52, 64 of 151,936 equal, 256 of them 146 / 139.
 int32_t sample_per(int32_t N, int32_t V) {
-  for (int32_t per = 32;; per /= 2) {
-    const int64_t chunks = ((int64_t)V + kWave * per - 1) / (kWave * per);
-    const bool halved_fits = ((int64_t)V + kWave * per / 2 - 1) / (kWave * per / 2) <= kMaxChunks;
-    if (per == 8 || !halved_fits || N * chunks >= 2 * kGroup * 256) return per;
-  }
+  auto chunks = [&](int32_t per) { return ((int64_t)V + kWave * per - 1) / (kWave * per); };
+  if (chunks(16) > kMaxChunks || N * chunks(32) > 8 * kGroup * 256) return 32;
+  if (chunks(8) > kMaxChunks || N * chunks(16) >= 2 * kGroup * 256) return 16;
+  return 8;
 }
 
 struct SampleLayout {
