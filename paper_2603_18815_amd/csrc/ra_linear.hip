@@ -670,14 +670,24 @@ __global__ __launch_bounds__(kThreads) void linear_scan_kernel(LinearArgs a) {
   const double ld = log_decay_of(a.log_decay, g);
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (a.ctx_lens[b] > 0) s = *reinterpret_cast<const f32x4 *>(pool);
-  for (int from = 0; from < T; from += a.segment_len) {
-    const double p = exp(ld * min(T - from, a.segment_len));
-    const float dh = (float)p, dl = (float)(p - (double)dh);
-    const f32x4 own = *reinterpret_cast<const f32x4 *>(carry);
-    *reinterpret_cast<f32x4 *>(carry) = s;
+  // eight stretches' loads at a time: one by one each waits for the store before it
+  constexpr int kAhead = 8;
+  const int stretches = (T + a.segment_len - 1) / a.segment_len;
+  const double full = exp(ld * a.segment_len), last = exp(ld * (T - (stretches - 1) * a.segment_len));
+  for (int first = 0; first < stretches; first += kAhead) {
+    f32x4 own[kAhead];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = fmaf(s[i], dh, fmaf(s[i], dl, own[i]));
-    carry += kStateSize;
+    for (int j = 0; j < kAhead; ++j)
+      own[j] = *reinterpret_cast<const f32x4 *>(carry + (int64_t)min(first + j, stretches - 1) * kStateSize);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (first + j >= stretches) break;
+      const double p = first + j < stretches - 1 ? full : last;
+      const float dh = (float)p, dl = (float)(p - (double)dh);
+      *reinterpret_cast<f32x4 *>(carry + (int64_t)(first + j) * kStateSize) = s;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i] = fmaf(s[i], dh, fmaf(s[i], dl, own[j][i]));
+    }
   }
   *reinterpret_cast<f32x4 *>(pool) = s;
 }
