@@ -23,8 +23,8 @@
 // Without filters stats and pick are the whole call; with min-p alone there are no bins.
 // Bins and border read only what the lanes' largest logits put into the range: of 156 MB of
 // logits (512 rows of 151,936 bf16) 47 and 61. Measured there, all filters: stats 38 us (4.1
-// TB/s), range 6, bins 31, border 42, pick 24, the call 138-142; 64 rows of them with top-p 13,
-// 4, 13, 15, 20 and 66; 64 rows of fp32 without filters 12, 7 and 18 (39 MB); a row of 32,000
+// TB/s), range 6, bins 31, border 42, pick 19, the call 136-139; 64 rows of them with top-p 13,
+// 4, 13, 15, 17 and 63; 64 rows of fp32 without filters 12, 7 and 18 (39 MB); a row of 32,000
 // 3, 4, 5, 6, 8 and 25. The first pass is bound by its read and, where sums are wanted, by 64-bit
 // arithmetic; the others by the round trips of a workgroup that does little.
 #include <type_traits>
@@ -38,7 +38,6 @@ namespace {
 
 constexpr int kThreads = 256;           // four chunks
 constexpr int kGroup = kThreads / kWave;
-constexpr int kPickThreads = 256;
 constexpr int kRowThreads = 512;        // of a row's range
 constexpr int kBins = 512;
 constexpr int kMaxChunks = 256;         // of a row
@@ -739,7 +738,8 @@ __device__ __forceinline__ void load_neighbours(const T *row, int v0, int V, flo
   for (int e = 0; e < kOwn; ++e) z[e] = clean(z[e]);
 }
 
-// What the pick's waves share.
+// What the pick's waves share; kN: its threads.
+template <int kN>
 struct PickLds {
   uint64_t sorted[kMaxSorted];          // listed elements
   uint64_t mass[kBins];                 // finer bins
@@ -747,8 +747,8 @@ struct PickLds {
   uint64_t kept_of[kMaxChunks];         // weight kept of each chunk
   uint32_t ties_of[kMaxChunks];         // of each chunk: elements at the edge
   uint32_t first_of[kMaxChunks];        // and where its listed elements start
-  uint64_t mpart[kPickThreads / kWave];
-  double dpart[kPickThreads / kWave];
+  uint64_t mpart[kN / kWave];
+  double dpart[kN / kWave];
   double table[kExpTable];
   uint64_t sum;
   uint32_t key, count, ties, high, low;
@@ -803,7 +803,8 @@ struct Goals {
 
 // Up to 64 listed elements, by one wave: lane i has one of them in `x` (0: none); adds what
 // is kept to the chunks' sums.
-__device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int chunk_len, PickLds &lds) {
+template <int kN>
+__device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int chunk_len, PickLds<kN> &lds) {
   const int lane = threadIdx.x % kWave;
   // each goes where as many larger ones are; the elements differ
   const uint64_t some = __ballot(x != 0);
@@ -839,15 +840,16 @@ __device__ __forceinline__ Edge end_in_a_wave(uint64_t x, const Goals &g, int ch
 }
 
 // Up to kMaxSorted listed elements, in lds.sorted.
-__device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int chunk_len, PickLds &lds) {
+template <int kN>
+__device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int chunk_len, PickLds<kN> &lds) {
   const int tid = threadIdx.x;
   int size = 64;
   while (size < count) size *= 2;
-  for (int i = count + tid; i < size; i += kPickThreads) lds.sorted[i] = 0;
+  for (int i = count + tid; i < size; i += kN) lds.sorted[i] = 0;
   __syncthreads();
   for (int len = 2; len <= size; len *= 2)
     for (int step = len / 2; step > 0; step /= 2) {
-      for (int i = tid; i < size / 2; i += kPickThreads) {
+      for (int i = tid; i < size / 2; i += kN) {
         const int lo = i / step * 2 * step + i % step, hi = lo + step;
         const uint64_t x = lds.sorted[lo], y = lds.sorted[hi];
         if ((x < y) == ((lo & len) == 0)) lds.sorted[lo] = y, lds.sorted[hi] = x;
@@ -855,7 +857,7 @@ __device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int ch
       __syncthreads();
     }
   // neighbouring elements a thread: their weights, and the sums before them
-  constexpr int kOwn = kMaxSorted / kPickThreads;
+  constexpr int kOwn = kMaxSorted / kN;
   auto add = [](uint64_t x, uint64_t y) { return x + y; };
   uint64_t w[kOwn], own = 0, of_k = 0, in_p = 0, all;
   int bin[kOwn];
@@ -870,13 +872,13 @@ __device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int ch
     }
     own += w[j];
   }
-  uint64_t run = group_scan<kPickThreads>(own, all, lds.mpart);
-  const uint64_t n_p = group_reduce<kPickThreads>(in_p, add, lds.mpart);
+  uint64_t run = group_scan<kN>(own, all, lds.mpart);
+  const uint64_t n_p = group_reduce<kN>(in_p, add, lds.mpart);
   if (g.ends_in_k() && g.row.p < 1.0) {
 #pragma unroll
     for (int j = 0; j < kOwn; ++j)
       if (bin[j] == g.b.bin_k && g.rank(tid * kOwn + j, bin[j], n_p) < (uint64_t)g.row.k) of_k += w[j];
-    of_k = group_reduce<kPickThreads>(of_k, add, lds.mpart);
+    of_k = group_reduce<kN>(of_k, add, lds.mpart);
   }
   const double goal = g.row.p < 1.0 ? g.goal(of_k) : 0.0;
   if (tid == 0) lds.count = 0;
@@ -900,9 +902,9 @@ __device__ __forceinline__ Edge end_by_sorting(int count, const Goals &g, int ch
 
 // Any number: the edge by eight bits of the key a pass over the row, first that of top-k,
 // then that of top-p among what top-k keeps. The chunks' sums are those of the whole prefix.
-template <typename T>
+template <typename T, int kN>
 __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goals &g, int chunks,
-                                           int chunk_len, PickLds &lds) {
+                                           int chunk_len, PickLds<kN> &lds) {
   const int tid = threadIdx.x;
   uint64_t *mass = lds.mass;
   uint32_t *counts = lds.counts;
@@ -916,13 +918,13 @@ __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goal
     if (by_mass) {
       // the weight that top-k keeps
       uint64_t sum = 0, equal = 0;
-      for (int v = tid; v < V; v += kPickThreads) {
+      for (int v = tid; v < V; v += kN) {
         const uint32_t key = key_at(v);
         if (key > end.key) sum += units(g.weight(key));
         equal += key == end.key;
       }
-      sum = group_reduce<kPickThreads>(sum, add, lds.mpart);
-      equal = group_reduce<kPickThreads>(equal, add, lds.mpart);
+      sum = group_reduce<kN>(sum, add, lds.mpart);
+      equal = group_reduce<kN>(equal, add, lds.mpart);
       if (end.key) sum += (equal < end.ties ? equal : end.ties) * units(g.weight(end.key));
       goal = fmax(g.row.p * (g.row.k > 0 ? (double)sum : g.all), 0.5);
     }
@@ -932,7 +934,7 @@ __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goal
       __syncthreads();
       if (tid < 256) mass[tid] = 0, counts[tid] = 0;
       __syncthreads();
-      for (int v = tid; v < V; v += kPickThreads) {
+      for (int v = tid; v < V; v += kN) {
         const uint32_t key = key_at(v);
         if (shift < 24 && key >> (shift + 8) != prefix >> (shift + 8)) continue;
         if (key < end.key) continue;
@@ -968,7 +970,7 @@ __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goal
   }
   // each chunk's elements at the edge, then what it keeps, a wave a chunk
   const int lane = tid % kWave;
-  for (int c = tid / kWave; c < chunks; c += kPickThreads / kWave) {
+  for (int c = tid / kWave; c < chunks; c += kN / kWave) {
     uint32_t equal = 0;
     const int last = min(V, (c + 1) * chunk_len);
     for (int v = c * chunk_len + lane; v < last; v += kWave) equal += key_at(v) == end.key;
@@ -976,7 +978,7 @@ __device__ __forceinline__ Edge end_by_passes(const T *logits, int V, const Goal
     if (lane == 0) lds.ties_of[c] = equal;
   }
   __syncthreads();
-  for (int c = tid / kWave; c < chunks; c += kPickThreads / kWave) {
+  for (int c = tid / kWave; c < chunks; c += kN / kWave) {
     uint64_t ahead = 0, sum = 0;
     for (int i = 0; i < c; ++i) ahead += lds.ties_of[i];
     const int last = min(V, (c + 1) * chunk_len);
@@ -1028,20 +1030,22 @@ __device__ __forceinline__ int chunk_of(const uint32_t *first_of, uint32_t i) {
   return c;
 }
 // Calls take(chunk, entry) for the listed elements from `from` on.
-template <typename Take>
+template <int kN, typename Take>
 __device__ __forceinline__ void for_listed(const SampleArgs &a, int n, uint32_t from, uint32_t count,
                                            const uint32_t *first_of, Take take) {
-  for (uint32_t i = from + threadIdx.x; i < count; i += kPickThreads) {
+  for (uint32_t i = from + threadIdx.x; i < count; i += kN) {
     const int c = chunk_of(first_of, i);
     take(c, a.list[((int64_t)n * a.chunks + c) * kListed + (i - first_of[c])]);
   }
 }
 
-template <typename T, int kPer>
-__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
+// kN threads: 256, or 512 for filters in a call of some size, where more is listed: 64 rows of
+// 151,936 with top-p 20 and 17 us, without filters 6.7 and 7.6, 7 rows with all 9.3 and 10.3.
+template <typename T, int kPer, int kN>
+__global__ __launch_bounds__(kN) void sample_pick_kernel(SampleArgs a) {
   const int n = blockIdx.x, tid = threadIdx.x, lane = tid % kWave;
   const T *logits = static_cast<const T *>(a.logits) + n * a.row_stride;
-  __shared__ PickLds lds;
+  __shared__ PickLds<kN> lds;
   constexpr int chunk_len = kWave * kPer;
 
   const Row row(a, n);
@@ -1162,7 +1166,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       uint32_t below = 0xffffffffu;                   // keys above it are kept if none listed is
       if (count <= kWave || apart) {
         __syncthreads();
-        for_listed(a, n, 0, listed_all, lds.first_of,
+        for_listed<kN>(a, n, 0, listed_all, lds.first_of,
                    [&](int, uint64_t x) { lds.sorted[atomicAdd(&lds.count, 1u)] = x; });
         __syncthreads();
       } else {
@@ -1170,14 +1174,14 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
         // a thread, mostly all, stay in registers from one pass to the next.
         const uint32_t span = high - low;
         g.shift = span < (uint32_t)kBins ? 0 : 32 - __clz(span / kBins);
-        for (int i = tid; i < kBins; i += kPickThreads) lds.mass[i] = 0, lds.counts[i] = 0;
-        constexpr int kHeld = 8;
+        for (int i = tid; i < kBins; i += kN) lds.mass[i] = 0, lds.counts[i] = 0;
+        constexpr int kHeld = 2048 / kN;
         uint64_t held[kHeld], weight[kHeld];
         int of_chunk[kHeld];
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kHeld; ++j) {
-          const uint32_t i = tid + j * kPickThreads;
+          const uint32_t i = tid + j * kN;
           of_chunk[j] = chunk_of(lds.first_of, i);
           held[j] = i < listed_all ? a.list[((int64_t)n * a.chunks + of_chunk[j]) * kListed +
                                             (i - lds.first_of[of_chunk[j]])]
@@ -1192,7 +1196,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
           if (held[j]) put(held[j], weight[j] = units_of(held[j]));
-        for_listed(a, n, kHeld * kPickThreads, listed_all, lds.first_of,
+        for_listed<kN>(a, n, kHeld * kN, listed_all, lds.first_of,
                    [&](int, uint64_t x) { put(x, units_of(x)); });
         __syncthreads();
         uint64_t m[kOwnBins];
@@ -1218,7 +1222,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
 #pragma unroll
         for (int j = 0; j < kHeld; ++j)
           if (held[j]) settle(of_chunk[j], held[j], weight[j]);
-        for_listed(a, n, kHeld * kPickThreads, listed_all, lds.first_of,
+        for_listed<kN>(a, n, kHeld * kN, listed_all, lds.first_of,
                    [&](int chunk, uint64_t x) { settle(chunk, x, units_of(x)); });
         __syncthreads();
         count = lds.count;
@@ -1228,7 +1232,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       if (count > 0 && high == low) {
         if (tid < kMaxChunks) lds.ties_of[tid] = 0;
         __syncthreads();
-        for_listed(a, n, 0, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
+        for_listed<kN>(a, n, 0, listed_all, lds.first_of, [&](int chunk, uint64_t x) {
           if ((uint32_t)(x >> 32) == high) atomicAdd(&lds.ties_of[chunk], 1u);
         });
         __syncthreads();
@@ -1267,7 +1271,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   }
 
   // the draw within the chunk: neighbouring elements a thread
-  constexpr int kOwn = chunk_len / kPickThreads;
+  constexpr int kOwn = chunk_len / kN;
   const int v0 = drawn.chunk * chunk_len + tid * kOwn;
   const double goal = (double)u * drawn.total;
   float z[kOwn];
@@ -1277,7 +1281,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     uint64_t equal = 0, all;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) equal += v0 + i < a.V && key_of(z[i]) == end.key;
-    seen = group_scan<kPickThreads>(equal, all, lds.mpart);
+    seen = group_scan<kN>(equal, all, lds.mpart);
     if (end.ties > 0)
       for (int c = 0; c < drawn.chunk; ++c) seen += lds.ties_of[c];
   }
@@ -1298,7 +1302,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
     own += w[i];
   }
   if (tid == 0) lds.token = -1;
-  const double before = drawn.before + group_scan<kPickThreads>(own, all, lds.dpart);
+  const double before = drawn.before + group_scan<kN>(own, all, lds.dpart);
   // the first element whose running sum passes the goal; should rounding leave none, the
   // last that weighs anything
   int token = -1;
@@ -1372,7 +1376,11 @@ void launch_passes(const SampleArgs &a, hipStream_t stream) {
   if (bins) hipLaunchKernelGGL((sample_bins_kernel<T, kPer>), grid, dim3(kThreads), 0, stream, a);
   if (bins || a.min_p)
     hipLaunchKernelGGL((sample_border_kernel<T, kPer>), grid, dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL((sample_pick_kernel<T, kPer>), dim3(a.N), dim3(kPickThreads), 0, stream, a);
+  constexpr int kMany = kPer > 8 ? 512 : 256;
+  if (bins)
+    hipLaunchKernelGGL((sample_pick_kernel<T, kPer, kMany>), dim3(a.N), dim3(kMany), 0, stream, a);
+  else
+    hipLaunchKernelGGL((sample_pick_kernel<T, kPer, 256>), dim3(a.N), dim3(256), 0, stream, a);
 }
 
 }  // namespace
