@@ -277,3 +277,15 @@ def test_refusals(device):
     empty = ra.linear_append(d["q"][:0], d["k"][:0], d["v"][:0], i32([0, 0]), d["ctx"],
                              d["states"], d["slots"], d["decay"])
     assert empty.shape == (0, 4, 128)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv", [([900, 3, 0, 40], 2, 2), ([512, 300, 480, 512, 512, 500, 401], 32, 8)])
+def test_append_workspace_at_16_bytes_and_no_larger_than_asked(T, Hq, Hkv, device):
+    d = make(T, [1] * len(T), Hq, Hkv, 9)
+    out, states = run_append(d, T)
+    need = ra.linear_append_workspace_size(len(T), Hq, Hkv, sum(T), max(T))
+    assert need > 0
+    store = torch.full((need + 512,), 0xab, dtype=torch.uint8, device="cuda:0")
+    out2, states2 = run_append(d, T, workspace=store[16:16 + need])
+    assert torch.equal(out2, out) and torch.equal(states2, states)
+    assert (store[:16] == 0xab).all() and (store[16 + need:] == 0xab).all()

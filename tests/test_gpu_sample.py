@@ -212,3 +212,18 @@ def test_many_elements_around_the_end(T, device):
     check(z, u, [T] * 6, [40000, 119000, 60000, 3000, 60001, 33333], what="top-k")
     check(z, u, [T] * 6, [40000, 119000, 60000, 3000, 60001, 33333], [0.9, 0.5, 0.7, 0.99, 0.3, 0.45],
           [0.0, 0.9, 0.0, 0.1, 0.0, 0.0], what="all")
+
+
+@pytest.mark.parametrize("shift", [0, 16, 48, 112])
+def test_workspace_at_any_16_bytes_and_no_larger_than_asked(shift, device):
+    N, V = 9, 40000
+    z, u = logits(N, V, torch.bfloat16, 2), torch.tensor(uniforms(N, 2), device="cuda:0")
+    k = torch.full((N,), 300, dtype=torch.int32, device="cuda:0")
+    p = torch.full((N,), 0.95, device="cuda:0")
+    want = ra.token_sample(z, u, None, k, p, want_logprob=True)
+    need = ra.token_sample_workspace_size(N, V)
+    store = torch.full((need + 512,), 0xab, dtype=torch.uint8, device="cuda:0")
+    assert store.data_ptr() % 256 == 0
+    got = ra.token_sample(z, u, None, k, p, want_logprob=True, workspace=store[shift:shift + need])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert (store[:shift] == 0xab).all() and (store[shift + need:] == 0xab).all()
