@@ -496,10 +496,10 @@ int token_sample(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
  * A row's state lives in a pool, states[slots[b]], and is updated in place; the state
  * before a row's first token is zero whatever the pool holds. Slots of one call must
  * differ. The state is kept to fp32 accuracy: append multiplies the decayed values in three
- * bf16 parts each. Its scores, and the state as it meets the queries, are rounded to bf16
- * operands, and out is rounded to bf16 (nearest even) in both calls. An infinite or NaN
- * input never reaches an earlier token's results; the state it reaches may hold NaN where
- * the formula has an infinity.
+ * bf16 parts each. Its scores, and the state as it meets the queries, are taken in two bf16
+ * parts each (off by 2^-17 of every term of their sums), and out is rounded to bf16 (nearest
+ * even) in both calls. An infinite or NaN input never reaches an earlier token's results;
+ * the results and the state it reaches may hold NaN where the formula has an infinity.
  *
  * rollout_linear_attn_decode: one token a row.
  *   q          bf16 [B][Hq][128];  k_new, v_new  bf16 [B][Hkv][128]

@@ -14,11 +14,13 @@
 // idle behind it, workgroups share its query heads, each with the state for itself, or rows
 // are cut into stretches: their own contributions to the state first (states pass), then the
 // state before each (scan), then the outputs (outputs pass).
-// Measured: 32 rows of 120 to 2,038 tokens, 32 heads on 8, 744 MB, 188-194 us (shared by
-// two); a row of 16,384 with 32 heads each, 541 MB of which K and V are read twice, 185-190
-// us (cut into 32: states 66, scan 8, outputs 109); 905 tokens in 2 rows 24 us (cut).
-#include <type_traits>
-
+// The products are of bf16: what has more bits, the state, the scores and the decayed values,
+// goes into them in two or three parts, so that the result's own rounding is the largest. One
+// part each of the state and the scores took 15 to 20 % less time, and was off by 2^-9 of
+// |S| |q|, however little of that a result keeps.
+// Measured: 32 rows of 120 to 2,038 tokens, 32 heads on 8, 744 MB, 230-240 us (shared by
+// two); a row of 16,384 with 32 heads each, 541 MB of which K and V are read twice, 218-224
+// us (cut into 8 stretches of 32 chunks); 905 tokens in 2 rows 25 us (cut).
 #include "ra_device.h"
 #include "ra_internal.h"
 
@@ -145,6 +147,9 @@ __device__ __forceinline__ int swizzle(int row) {
   return (row & 3) << 2 | ((row >> 2 ^ row >> 3) & 1) << 1 | (row >> 3 & 1);
 }
 constexpr int kRowBytes = 2 * kHeadDim, kScoreRowBytes = 2 * kChunk;
+// Scores of a head: 64 rows of 64 bf16, of which tokens 0..31 fill the first half only. Their
+// second parts lie in their rows' second half, those of tokens 32..63 in 32 rows behind.
+constexpr int kScores = (kChunk + kChunk / 2) * kChunk;
 
 __device__ __forceinline__ bf16x8 lds_bf16x8(const uint16_t *tile, int byte) {
   return *reinterpret_cast<const bf16x8 *>(reinterpret_cast<const char *>(tile) + byte);
@@ -175,6 +180,12 @@ __device__ __forceinline__ bf16x8 take_bf16(f32x8 &x) {
     x[2 * i + 1] -= __uint_as_float(hi & 0xffff0000u);
   }
   return __builtin_bit_cast(bf16x8, packed);
+}
+
+// x as the sum of two bf16, off by 2^-17 of it at most (2^-9 of a rest that is 2^-8 of it).
+__device__ __forceinline__ void two_parts(f32x8 x, bf16x8 &high, bf16x8 &low) {
+  high = to_bf16x8(x);
+  low = to_bf16x8(x - to_f32x8(high));
 }
 
 // 16 bytes a lane from global memory (base + the lane's byte offset) to LDS, lane l's at
@@ -242,8 +253,8 @@ __device__ __forceinline__ float *carry_of(const LinearArgs &a, int start, int b
 
 // One stretch of a (row, KV head): chunks in order, the state in the accumulators. Wave w
 // of 8 holds the 16 value dims from 16 w, all 128 key dims: tile t = 2 x + y has key dims
-// 32 x + 8 (m / 4) + 4 y + m % 4 as its rows m, so that two accumulator tiles, rounded to
-// bf16, are the operand of S^T Q^T for the 32 key dims from 32 x as they stand (a lane's
+// 32 x + 8 (m / 4) + 4 y + m % 4 as its rows m, so that two accumulator tiles, in two bf16
+// parts, are the operands of S^T Q^T for the 32 key dims from 32 x as they stand (a lane's
 // eight contraction slots: 8 (l / 16) + 0..7), and a lane's results are four neighbouring
 // value dims of a token. Scores go through LDS: a wave computes two of the 16 tiles, all
 // waves use all of them.
@@ -252,8 +263,8 @@ __device__ __forceinline__ float *carry_of(const LinearArgs &a, int start, int b
 // tiles are there (scores, the state's part of the results, and with the chunk's last heads
 // the state's update); the scores are there (their part of the results, which go into Q's
 // tiles); the results are there (they leave as whole rows). K and V have two stages, the next
-// chunk's loads go out during the first heads' step; Q has two buffers of kHeads tiles. 108 KB
-// of LDS (149 KB with two heads) and up to 256 registers: one workgroup per CU.
+// chunk's loads go out during the first heads' step; Q has two buffers of kHeads tiles. 112 KB
+// of LDS (157 KB with two heads) and up to 256 registers: one workgroup per CU.
 template <bool kStates, int kHeads, bool kCut>
 __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_kernel(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid % kWave;
@@ -293,7 +304,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
 
   __shared__ __align__(1024) uint16_t sk[2 * kTile], sv[2 * kTile];
   __shared__ __align__(1024) uint16_t sq[kStates ? 8 : 2 * kHeads * kTile];
-  __shared__ __align__(1024) uint16_t sp[kStates ? 8 : kHeads * kChunk * kChunk];
+  __shared__ __align__(1024) uint16_t sp[kStates ? 8 : kHeads * kScores];
   // l^n; scale l^n; l^(63 - j), then zeros
   __shared__ float power[kChunk + 1], weight[2 * kChunk];
   __shared__ double decays[kChunk + 1];
@@ -418,9 +429,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
   // S' = decay S + K^T (after l^(n-1-j) V), n the chunk's tokens: the decayed values in
   // bf16 parts, of which three hold all 24 bits. The states pass has no state to decay: its
   // weights reach to the end of the stretch (after = l^tokens behind the chunk).
-  auto update = [&](auto parts, const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay,
-                    float after) {
-    constexpr int kParts = decltype(parts)::value;
+  auto update = [&](const bf16x8(&vf)[2], const uint16_t *tile, int n, float decay, float after) {
     const int at = fresh(at_k);
     if (!kStates) {
 #pragma unroll
@@ -436,7 +445,7 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
     read_pair(0);
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      bf16x8 part[kParts];
+      bf16x8 part[3];
       f32x8 y = to_f32x8(vf[x]);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -444,13 +453,13 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
         y[e] *= kStates ? w * after : w;
       }
 #pragma unroll
-      for (int m = 0; m < kParts; ++m) part[m] = take_bf16(y);
+      for (int m = 0; m < 3; ++m) part[m] = take_bf16(y);
 #pragma unroll
       for (int i = 4 * x; i < 4 * x + 4; ++i) {
         if (i + 1 < 8) read_pair(i + 1);
         keep_order();
 #pragma unroll
-        for (int m = 0; m < kParts; ++m)
+        for (int m = 0; m < 3; ++m)
 #pragma unroll
           for (int y = 0; y < 2; ++y)
             s[2 * (i % 4) + y] = mfma16x16x32(kf[i % 2][y], part[m], s[2 * (i % 4) + y]);
@@ -473,169 +482,174 @@ __global__ __launch_bounds__(kAppendThreads, kStates ? 4 : 2) void linear_chunk_
       mult[jj][i] = d >= 0 ? a.scale * __builtin_amdgcn_exp2f(l2 * (float)d) : 0.f;
     }
 
-  auto steps = [&](auto parts) {
-    int q_buf = 0;
-    double drift = 1.0;
-    for (int c = 0; c < chunks; ++c) {
-      const int n = min(len - c * kChunk, kChunk);
-      bf16x8 vf[2];
-      bool odd = false;                                   // values that are infinite or NaN
-      const int buf = c & 1;
-      const bool more = c + 1 < chunks;
-      const int left = len - 1 - (c + 1) * kChunk;        // rows behind the next chunk's first
-      const uint16_t *const tk = sk + buf * kTile, *const tv = sv + buf * kTile;
-      kp += kv_chunk;
-      vp += kv_chunk;
-      auto load_k = [&]() {
-        if (more) load(lds_k + (buf ^ 1) * kTile * 2, kp, kv_off, kv_stride, left);
-      };
-      auto load_v = [&]() {
-        if (more) load(lds_v + (buf ^ 1) * kTile * 2, vp, kv_off, kv_stride, left);
-      };
-      if constexpr (kStates) {
-        await_loads();
+  int q_buf = 0;
+  double drift = 1.0;
+  for (int c = 0; c < chunks; ++c) {
+    const int n = min(len - c * kChunk, kChunk);
+    bf16x8 vf[2];
+    bool odd = false;                                   // values that are infinite or NaN
+    const int buf = c & 1;
+    const bool more = c + 1 < chunks;
+    const int left = len - 1 - (c + 1) * kChunk;        // rows behind the next chunk's first
+    const uint16_t *const tk = sk + buf * kTile, *const tv = sv + buf * kTile;
+    kp += kv_chunk;
+    vp += kv_chunk;
+    auto load_k = [&]() {
+      if (more) load(lds_k + (buf ^ 1) * kTile * 2, kp, kv_off, kv_stride, left);
+    };
+    auto load_v = [&]() {
+      if (more) load(lds_v + (buf ^ 1) * kTile * 2, vp, kv_off, kv_stride, left);
+    };
+    if constexpr (kStates) {
+      await_loads();
+      __syncthreads();
+      load_k();
+      load_v();
+      read_v(vf, tv);
+      update(vf, tk, n, 1.f, __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
+    } else {
+      bf16x8 sb[2][4];                                  // the state before the chunk, in two parts
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        two_parts(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7), sb[0][x],
+                  sb[1][x]);
+      for (int h = 0; h < group; h += kHeads) {
+        uint16_t *const tq = sq + q_buf * kHeads * kTile;
+        const bool last = h + kHeads == group;
+        // behind the tiles' loads: the step before's stores, two a head where its chunk was full
+        if (n == kChunk && (c > 0 || h > 0)) {
+          await_loads_before<2 * kHeads>();
+        } else {
+          await_loads();
+        }
         __syncthreads();
-        load_k();
-        load_v();
-        read_v(vf, tv);
-        update(std::integral_constant<int, 3>(), vf, tk, n, 1.f,
-               __builtin_amdgcn_exp2f(l2 * (float)(len - c * kChunk - n)));
-      } else {
-        bf16x8 sb[4];                                     // the state before the chunk, in bf16
+        // K of the wave's two score tiles: those of tokens 16 it + r against 16 jt + 4 quad +
+        // 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero, and needed where a
+        // tile shares 32 slots with one on it.
+        const int it_p = wave & 3, jt_p = wave >> 2, at = fresh(at_row), pt = fresh(at_p);
+        bf16x8 kf[2][4];
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          sb[x] = to_bf16x8(__builtin_shufflevector(s[2 * x], s[2 * x + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-        for (int h = 0; h < group; h += kHeads) {
-          uint16_t *const tq = sq + q_buf * kHeads * kTile;
-          const bool last = h + kHeads == group;
-          // behind the tiles' loads: the step before's stores, two a head where its chunk was full
-          if (n == kChunk && (c > 0 || h > 0)) {
-            await_loads_before<2 * kHeads>();
-          } else {
-            await_loads();
-          }
-          __syncthreads();
-          // K of the wave's two score tiles: those of tokens 16 it + r against 16 jt + 4 quad +
-          // 0..3, jt = wave / 4 and 2 more. Above the diagonal they are zero, and needed where a
-          // tile shares 32 slots with one on it.
-          const int it_p = wave & 3, jt_p = wave >> 2, at = fresh(at_row), pt = fresh(at_p);
-          bf16x8 kf[2][4];
+        for (int x = 0; x < 4; ++x) kf[0][x] = lds_bf16x8(tk + 16 * jt_p * kHeadDim, at ^ (x << 6));
+        if (it_p >= 2)
 #pragma unroll
-          for (int x = 0; x < 4; ++x) kf[0][x] = lds_bf16x8(tk + 16 * jt_p * kHeadDim, at ^ (x << 6));
-          if (it_p >= 2)
+          for (int x = 0; x < 4; ++x)
+            kf[1][x] = lds_bf16x8(tk + 16 * (jt_p + 2) * kHeadDim, at ^ (x << 6));
+        if (h == 0) read_v(vf, tv);
+        q_buf ^= 1;
+        if (!last) {
+          load_q(q_buf, qp + (h + kHeads) * kHeadDim, left + kChunk);
+        } else if (more) {
+          load_q(q_buf, qp + q_chunk, left);
+        }
+        f32x4 acc[kHeads][4];
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              kf[1][x] = lds_bf16x8(tk + 16 * (jt_p + 2) * kHeadDim, at ^ (x << 6));
-          if (h == 0) read_v(vf, tv);
-          q_buf ^= 1;
-          if (!last) {
-            load_q(q_buf, qp + (h + kHeads) * kHeadDim, left + kChunk);
-          } else if (more) {
-            load_q(q_buf, qp + q_chunk, left);
-          }
-          f32x4 acc[kHeads][4];
+        for (int j = 0; j < kHeads; ++j) {
+          const uint16_t *const tj = tq + j * kTile;
+          // Q of all tokens, and of those of the wave's scores, a quarter of the dims ahead of
+          // the products
+          bf16x8 qf[2][4], qs[2];
+          auto read_q = [&](int x) {
+            qs[x % 2] = lds_bf16x8(tj + 16 * it_p * kHeadDim, at ^ (x << 6));
 #pragma unroll
-          for (int j = 0; j < kHeads; ++j) {
-            const uint16_t *const tj = tq + j * kTile;
-            // Q of all tokens, and of those of the wave's scores
-            bf16x8 qf[4][4], qs[4];
+            for (int it = 0; it < 4; ++it)
+              qf[x % 2][it] = lds_bf16x8(tj + 16 * it * kHeadDim, at ^ (x << 6));
+          };
+          f32x4 p[2];
+          p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int x = 0; x < 4; ++x) qs[x] = lds_bf16x8(tj + 16 * it_p * kHeadDim, at ^ (x << 6));
+          for (int it = 0; it < 4; ++it) acc[j][it] = f32x4{0.f, 0.f, 0.f, 0.f};
+          read_q(0);
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
+          for (int x = 0; x < 4; ++x) {
+            if (x + 1 < 4) read_q(x + 1);
+            keep_order();
+            p[0] = mfma16x16x32(kf[0][x], qs[x % 2], p[0]);
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
 #pragma unroll
               for (int it = 0; it < 4; ++it)
-                qf[it][x] = lds_bf16x8(tj + 16 * it * kHeadDim, at ^ (x << 6));
+                acc[j][it] = mfma16x16x32(sb[m][x], qf[x % 2][it], acc[j][it]);
+            if (it_p >= 2) p[1] = mfma16x16x32(kf[1][x], qs[x % 2], p[1]);
             keep_order();
-            f32x4 p[2];
-            p[0] = p[1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int it = 0; it < 4; ++it) acc[j][it] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              p[0] = mfma16x16x32(kf[0][x], qs[x], p[0]);
-#pragma unroll
-              for (int it = 0; it < 4; ++it) acc[j][it] = mfma16x16x32(sb[x], qf[it][x], acc[j][it]);
-            }
-            if (it_p >= 2)
-#pragma unroll
-              for (int x = 0; x < 4; ++x) p[1] = mfma16x16x32(kf[1][x], qs[x], p[1]);
-#pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
-              if (jj == 1 && it_p < 2) break;
-              bf16x4 w;
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                w[i] = (__bf16)(mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i]);
-              *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(sp + j * kChunk * kChunk) +
-                                          (pt ^ (jj << 6))) = w;
-            }
-#pragma unroll
-            for (int it = 0; it < 4; ++it) acc[j][it] *= power[16 * it + r + 1];
           }
-          if (h == 0) load_k();
-          if (odd && last) read_v(vf, tv);
-          if (last && (more || (whole && part == 0))) {
-            // the product of the chunks' decays as they were rounded is kept at l^tokens: what
-            // one rounding adds, the next chunk's takes off
-            const double exact = decays[n];
-            const float decay = (float)(exact * drift);
-            if (exact > 1e-30) drift = exact * drift / decay;
-            update(parts, vf, tk, n, decay, 1.f);
-          }
-          if (h == 0) odd = strange(vf);
-          if (odd && (h == 0 || last)) zero_strange(vf);
-          if (h == 0) load_v();
-          __syncthreads();
-          const int st = fresh(at_score);
 #pragma unroll
-          for (int j = 0; j < kHeads; ++j) {
+          for (int jj = 0; jj < 2; ++jj) {
+            if (jj == 1 && it_p < 2) break;
+            bf16x4 w, w2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = mult[jj][i] == 0.f ? 0.f : p[jj][i] * mult[jj][i];
+              w[i] = (__bf16)x;
+              w2[i] = (__bf16)(x - (float)w[i]);
+            }
+            char *const scores = reinterpret_cast<char *>(sp + j * kScores);
+            *reinterpret_cast<bf16x4 *>(scores + (pt ^ (jj << 6))) = w;
+            *reinterpret_cast<bf16x4 *>(scores + (it_p < 2 ? 0 : kChunk / 2 * kScoreRowBytes) +
+                                        (pt ^ ((it_p < 2 ? 1 : jj) << 6))) = w2;
+          }
+#pragma unroll
+          for (int it = 0; it < 4; ++it) acc[j][it] *= power[16 * it + r + 1];
+        }
+        if (h == 0) load_k();
+        if (odd && last) read_v(vf, tv);
+        if (last && (more || (whole && part == 0))) {
+          // the product of the chunks' decays as they were rounded is kept at l^tokens: what
+          // one rounding adds, the next chunk's takes off
+          const double exact = decays[n];
+          const float decay = (float)(exact * drift);
+          if (exact > 1e-30) drift = exact * drift / decay;
+          update(vf, tk, n, decay, 1.f);
+        }
+        if (h == 0) odd = strange(vf);
+        if (odd && (h == 0 || last)) zero_strange(vf);
+        if (h == 0) load_v();
+        __syncthreads();
+        const int st = fresh(at_score);
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j) {
+          const uint16_t *const scores = sp + j * kScores;
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {                 // the scores' two parts
             bf16x8 pf[4][2];
 #pragma unroll
             for (int it = 0; it < 4; ++it)
 #pragma unroll
               for (int x = 0; x <= it / 2; ++x)
-                pf[it][x] = lds_bf16x8(sp + j * kChunk * kChunk + 16 * it * kChunk, st ^ (x << 6));
+                pf[it][x] = lds_bf16x8(scores + (16 * it + (it < 2 ? 0 : m * kChunk / 2)) * kChunk,
+                                       st ^ ((it < 2 ? m : x) << 6));
 #pragma unroll
             for (int x = 0; x < 2; ++x)
 #pragma unroll
-              for (int it = 2 * x; it < 4; ++it) acc[j][it] = mfma16x16x32(vf[x], pf[it][x], acc[j][it]);
+              for (int it = 2 * x; it < 4; ++it)
+                acc[j][it] = mfma16x16x32(vf[x], pf[it][x], acc[j][it]);
           }
-          // the results through Q's tiles, which nothing reads any more: a wave has 32 bytes of
-          // each token, whose stores alone took longer than the products; whole rows leave
-          const int ot = fresh(at_o);
-#pragma unroll
-          for (int j = 0; j < kHeads; ++j)
-#pragma unroll
-            for (int it = 0; it < 4; ++it)
-              *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(tq + j * kTile + 16 * it * kHeadDim) +
-                                          ot) = __builtin_convertvector(acc[j][it], bf16x4);
-          if (odd)
-            for (int j = 0; j < kHeads; ++j) fill_strange(tq + j * kTile, tv, n);
-          __syncthreads();
-#pragma unroll
-          for (int j = 0; j < kHeads; ++j)
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-              const u32x4 w = load_u32x4(tq + j * kTile + (8 * wave + 4 * m) * kHeadDim + lane * 8);
-              char *const o_row = reinterpret_cast<char *>(op + (h + j) * kHeadDim);
-              if (n == kChunk || 8 * wave + 4 * m + lane / 16 < n)
-                store_u32x4(reinterpret_cast<uint16_t *>(
-                                o_row + (m ? (q_off ^ 32) + 4 * q_stride : q_off)), w);
-            }
         }
-        qp += q_chunk;
-        op += q_chunk;
+        // the results through Q's tiles, which nothing reads any more: a wave has 32 bytes of
+        // each token, whose stores alone took longer than the products; whole rows leave
+        const int ot = fresh(at_o);
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j)
+#pragma unroll
+          for (int it = 0; it < 4; ++it)
+            *reinterpret_cast<bf16x4 *>(reinterpret_cast<char *>(tq + j * kTile + 16 * it * kHeadDim) +
+                                        ot) = __builtin_convertvector(acc[j][it], bf16x4);
+        if (odd)
+          for (int j = 0; j < kHeads; ++j) fill_strange(tq + j * kTile, tv, n);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kHeads; ++j)
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+            const u32x4 w = load_u32x4(tq + j * kTile + (8 * wave + 4 * m) * kHeadDim + lane * 8);
+            char *const o_row = reinterpret_cast<char *>(op + (h + j) * kHeadDim);
+            if (n == kChunk || 8 * wave + 4 * m + lane / 16 < n)
+              store_u32x4(reinterpret_cast<uint16_t *>(
+                              o_row + (m ? (q_off ^ 32) + 4 * q_stride : q_off)), w);
+          }
       }
+      qp += q_chunk;
+      op += q_chunk;
     }
-  };
-  // a stretch of a cut row needs the state as bf16 operands only: two parts, so that nothing
-  // but the operands' own rounding counts. (Compiled again for these; with two heads a step
-  // that has no registers left.)
-  if (kCut && kHeads == 1 && !whole) {
-    steps(std::integral_constant<int, 2>());
-  } else {
-    steps(std::integral_constant<int, 3>());
   }
   if (kStates || (whole && part == 0)) {
     // the other parts may not have read the pool yet
@@ -709,7 +723,7 @@ struct LinearPlan {
 // A chunk's time by a workgroup that takes `heads` query heads of it, in ns (measured, alone
 // on the GPU; an even number is taken two at once).
 int64_t chunk_ns(int32_t heads) {
-  return heads % 2 == 0 ? 1500 + 1160 * (int64_t)heads : 950 + 2000 * (int64_t)heads;
+  return heads % 2 == 0 ? 1600 + 1560 * (int64_t)heads : 2000 + 1700 * (int64_t)heads;
 }
 LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int32_t max_q_len) {
   const int32_t longest = max_q_len < total_q ? max_q_len : total_q, group = hq / hkv;
@@ -722,9 +736,9 @@ LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int3
   // Compute units are idle behind the longest row. Either they share whole rows by their
   // heads (each part keeps the state for itself, one writes it out, a launch behind sets it in
   // the pool), where there are that many more of them than of longest rows; or rows are cut.
-  // Measured, 32 heads on 8, rows of 2,048: 16 rows 223 us as they are, 166 by two parts;
-  // 8 rows 213, by four parts 113, cut 146; 4 rows 203, 103, 83; rows of 512: 8 rows 58, 38,
-  // 53; 2 rows 55, 32, 26.
+  // Measured, 32 heads on 8, rows of 2,048: 16 rows 270 us as they are, 205-235 by two parts;
+  // 8 rows 262, by four parts 140-147, cut 174; 4 rows 253, 127, 95; rows of 512: 8 rows 69,
+  // 43, 59; 2 rows 67, 37, 28.
   while (group % (2 * p.parts) == 0 && 4 * (2 * p.parts) * share <= 5 * chunks &&
          (int64_t)B * hkv <= 2 * kComputeUnits)
     p.parts *= 2;
@@ -738,9 +752,9 @@ LinearPlan linear_plan(int32_t B, int32_t hq, int32_t hkv, int32_t total_q, int3
   const int32_t of_cut = (int32_t)(2 * (int64_t)total_q / c.segment_len) + 1;
   c.by_row = c.stretches <= of_cut;
   c.carry_slots = c.by_row ? c.stretches : of_cut;
-  // 2 us of the states pass, 3 us for the bandwidth that all units share, and the states of
+  // 2 us of the states pass, 3.5 us for the bandwidth that all units share, and the states of
   // the stretches written and read
-  const int64_t cut_ns = share * (chunk_ns(group) + 5000) + 8000 + 85 * (int64_t)c.carry_slots * hkv;
+  const int64_t cut_ns = share * (chunk_ns(group) + 5500) + 8000 + 85 * (int64_t)c.carry_slots * hkv;
   return cut_ns < whole_ns ? c : p;
 }
 
