@@ -809,7 +809,11 @@ def block_table_extend(block_table: torch.Tensor, start_pos: torch.Tensor, num_n
     dev, B, stride = _table_inputs(block_table, free_pages, free_count, (start_pos, num_new),
                                    ("start_pos", "num_new"))
     if total_new is None:
-        total_new = slot_map.shape[0] if slot_map is not None else int(num_new.sum().item())
+        # a sum below 0, or past all rows' tables, is the call's to refuse
+        total_new = slot_map.shape[0] if slot_map is not None else \
+            min(max(int(num_new.sum().item()), 0), B * stride * PAGE_SIZE, 2**31 - 1)
+    if total_new >= 2**31:
+        raise ValueError(f"total_new must be below 2^31, got {total_new}")
     if cu_new is None:
         cu_new = _empty((B + 1,), torch.int32, dev, stream)
     if kv_lens is None:

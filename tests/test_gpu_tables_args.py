@@ -1,0 +1,39 @@
+"""Arguments of the block-table calls that stand at the edge of what is documented."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18815_amd as ra
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(x):
+    return torch.as_tensor(np.ascontiguousarray(np.asarray(x, np.int32)), device="cuda:0")
+
+
+def pool(B, stride=4, pages=32):
+    return dev(np.full((B, stride), -7)), dev(np.arange(pages)), dev([pages])
+
+
+# sums below zero, past every row's table, and past 32 bits
+@pytest.mark.parametrize("new", [[-5, 3], [-1], [-2**31, -2**31, 1], [1, 100], [65] * 3,
+                                 [2**31 - 1, 2**31 - 1], [2**31 - 1] * 2 + [7]])
+def test_total_new_left_out_for_lengths_out_of_range(new, device):
+    """The call refuses as a whole; nothing is raised, and the slot map is no longer than the
+    tables."""
+    B = len(new)
+    table, free, count = pool(B)
+    start = dev([2] * B)
+    cu, lens, slots, taken = ra.block_table_extend(table, start, dev(new), free, count)
+    assert taken.item() == -1 and count.item() == 32
+    assert cu.tolist() == [0] * (B + 1) and lens.tolist() == [2] * B
+    assert slots.numel() <= B * 4 * 16 and (slots == -1).all()
+    assert (table == -7).all() and free.tolist() == list(range(32))
+
+
+def test_total_new_beyond_32_bits_is_refused(device):
+    table, free, count = pool(2)
+    with pytest.raises(ValueError, match="total_new"):
+        ra.block_table_extend(table, dev([0, 0]), dev([1, 1]), free, count, total_new=2**32 + 2)
+    assert count.item() == 32 and (table == -7).all()
