@@ -575,10 +575,12 @@ int rollout_linear_attn_append(const void *q, const void *k_new, const void *v_n
  *                slower: it sizes the launch); B * bt_stride always holds
  *   cu_new       int32 [B+1];  kv_lens int32 [B];  taken, released int32 [1]
  *   slot_map     int64 [total_new] or NULL
- * Outputs must not overlap inputs. Calls on one free list must not overlap in time.
+ * What a call writes (the outputs, extend's block_table, the free list) must not share memory
+ * with another of its arrays: extend cannot set the lengths in place. Calls on one free list
+ * must not overlap in time.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (B < 0, bt_stride <= 0, total_new < 0, max_pages < 0,
- *         free_capacity < 0); RA_ERR_UNSUPPORTED (B > 65535, bt_stride * 16 > 2^31 - 1);
- *         RA_ERR_HIP. With B == 0 (row arrays may be NULL) extend writes cu_new[0] = 0,
+ *         free_capacity < 0); RA_ERR_UNSUPPORTED (B > 65535, bt_stride * 16 > 2^31 - 1,
+ *         arrays that share memory as above); RA_ERR_HIP. With B == 0 (row arrays may be NULL) extend writes cu_new[0] = 0,
  *         *taken = 0 and the slots' -1, release *released = 0.
  */
 int kv_block_table_extend(const int32_t *start_pos, const int32_t *num_new,

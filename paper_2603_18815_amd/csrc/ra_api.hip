@@ -314,6 +314,25 @@ int check_table(int32_t B, int32_t bt_stride, int32_t free_capacity) {
   return RA_OK;
 }
 
+// Whether a written array shares memory with another one, which other workgroups may still
+// be reading or writing.
+struct Array {
+  const void *at;                       // NULL: none
+  int64_t bytes;
+  bool written;
+};
+template <size_t kN>
+bool overlap(const Array (&arrays)[kN]) {
+  for (size_t i = 0; i < kN; ++i)
+    for (size_t j = 0; j < i; ++j) {
+      const Array &x = arrays[i], &y = arrays[j];
+      if (!x.at || !y.at || !x.bytes || !y.bytes || !(x.written || y.written)) continue;
+      const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+      if (a < b + (uintptr_t)y.bytes && b < a + (uintptr_t)x.bytes) return true;
+    }
+  return false;
+}
+
 // A rotary table must cover every position the call uses: [0, max_pos).
 int check_rope(const float *cos_sin, int32_t rope_rows, int32_t max_pos) {
   if (rope_rows <= 0 || max_pos > rope_rows) return RA_ERR_SHAPE;
@@ -545,6 +564,12 @@ int kv_block_table_extend(const int32_t *start_pos, const int32_t *num_new,
   if (s != RA_OK) return s;
   if (!free_count || !cu_new || !taken || (free_capacity > 0 && !free_pages)) return RA_ERR_NULL;
   if (B > 0 && (!start_pos || !num_new || !block_table || !kv_lens)) return RA_ERR_NULL;
+  const int64_t rows = 4 * (int64_t)B;
+  if (overlap({{start_pos, rows, false}, {num_new, rows, false},
+               {free_pages, 4 * (int64_t)free_capacity, false}, {free_count, 4, true},
+               {block_table, rows * bt_stride, true}, {cu_new, rows + 4, true},
+               {kv_lens, rows, true}, {slot_map, 8 * (int64_t)total_new, true}, {taken, 4, true}}))
+    return RA_ERR_UNSUPPORTED;
   return hip_status(ra::launch_table_extend(start_pos, num_new, free_pages, free_count,
                                             free_capacity, block_table, B, bt_stride, total_new,
                                             cu_new, kv_lens, slot_map, taken, stream));
@@ -559,6 +584,11 @@ int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
   if (s != RA_OK) return s;
   if (!free_count || !released || (free_capacity > 0 && !free_pages)) return RA_ERR_NULL;
   if (B > 0 && (!lens || !keep_lens || !block_table)) return RA_ERR_NULL;
+  const int64_t rows = 4 * (int64_t)B;
+  if (overlap({{lens, rows, false}, {keep_lens, rows, false}, {block_table, rows * bt_stride, false},
+               {free_pages, 4 * (int64_t)free_capacity, true}, {free_count, 4, true},
+               {released, 4, true}}))
+    return RA_ERR_UNSUPPORTED;
   return hip_status(ra::launch_table_release(lens, keep_lens, block_table, B, bt_stride,
                                              free_pages, free_count, free_capacity, max_pages,
                                              released, stream));

@@ -37,3 +37,17 @@ def test_total_new_beyond_32_bits_is_refused(device):
     with pytest.raises(ValueError, match="total_new"):
         ra.block_table_extend(table, dev([0, 0]), dev([1, 1]), free, count, total_new=2**32 + 2)
     assert count.item() == 32 and (table == -7).all()
+
+
+def test_lengths_in_place_are_refused(device):
+    """Other workgroups may not have read the old lengths yet."""
+    table, free, count = pool(3)
+    start, new = dev([2, 3, 4]), dev([1, 1, 1])
+    for kw in (dict(kv_lens=start), dict(kv_lens=new)):
+        with pytest.raises(ra.RolloutAttnError):
+            ra.block_table_extend(table, start, new, free, count, total_new=3, **kw)
+    with pytest.raises(ra.RolloutAttnError):
+        ra.block_table_release(table, start, new, free, count, released=count)
+    assert start.tolist() == [2, 3, 4] and new.tolist() == [1, 1, 1] and count.item() == 32
+    # what is only read may be the same
+    assert ra.block_table_release(table, start, start, free, count).item() == 0
