@@ -101,7 +101,7 @@ hipError_t launch_logprob_pack(const uint16_t *W, int32_t V, int32_t D, uint16_t
                                hipStream_t stream);
 
 // ---- drawing tokens from logits ----
-constexpr int32_t kSampleMaxVocab = 1 << 19;   // a row's sum of weights stays below 2^63
+constexpr int32_t kSampleMaxVocab = 1 << 19;   // a row's sum of weights is at most 2^63
 size_t sample_workspace_bytes(int32_t N, int32_t V);
 hipError_t launch_sample(const void *logits, bool bf16, int32_t N, int32_t V, int64_t row_stride,
                          const float *temperature, const int32_t *top_k, const float *top_p,

@@ -4,8 +4,8 @@
 // With M the row's largest logit, an element's weight is e = exp((z - M) / T) in 64-bit
 // floating point. Where weights are added up by atomics or in no fixed order they are whole
 // numbers of 2^-44 (0 below half a unit, 31.2 below M), so that no order changes a sum:
-// a sum of V weights is off by at most V half units, and a row's stays below 2^63 for
-// V <= 2^19. The other sums are taken in a fixed order.
+// a sum of V weights is off by at most V half units, and a row's is at most 2^63 for V <= 2^19
+// (2^19 equal logits): sums are unsigned. The other sums are taken in a fixed order.
 //
 // All filters keep a prefix of the order (logit descending, index ascending), so what is
 // sought is where it ends. Rows are cut into chunks, a wave each, and the call runs:

@@ -1,0 +1,49 @@
+"""token_sample at the ends of its ranges, against the 64-bit definition on the host.
+
+The cases are made of weights that 64-bit sums hold exactly (equal logits: powers of two times
+their number), so that tokens are equal whatever the order of the sums; elsewhere the bound is
+that of test_gpu_sample.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18815_amd as ra
+from test_gpu_sample import check, host, uniforms
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [(1 << 19) - 1, 1 << 19])
+def test_flat_rows_of_the_largest_vocabulary(V, dtype, device):
+    """Sums of weights up to 2^63, the most that there are."""
+    z = torch.full((7, V), 1.5, dtype=dtype, device="cuda:0")
+    last = float(np.nextafter(np.float32(1), np.float32(0)))
+    u = [0.0, 0.25, 0.5, last, 0.999, 0.123, 0.75]
+    check(z, u, what="plain")
+    k = [0, V, V - 1, V // 2, 1, 1 << 18, V + 5]
+    p = [last, 0.5, 0.75, 0.25, 1.0, 2.0 ** -19, 0.0]
+    check(z, u, None, k, what="top-k")
+    check(z, u, None, None, p, what="top-p")
+    check(z, u, None, k, p, [0.0, 0.5, 1.0, 0.0, 0.1, 0.0, 1.0], what="all")
+
+
+@pytest.mark.parametrize("N,V", [(1, 1), (5, 300), (9, 40000), (64, 151936)])
+def test_the_log_probability_may_be_left_out(N, V, device):
+    z = 2 * torch.randn((N, V), generator=torch.Generator(device="cuda:0").manual_seed(V),
+                        device="cuda:0")
+    u = torch.tensor(uniforms(N, V), device="cuda:0")
+    p, k = torch.full((N,), 0.9, device="cuda:0"), torch.full((N,), 40, dtype=torch.int32, device="cuda:0")
+    T = torch.full((N,), 0.8, device="cuda:0")
+    T[N // 2] = 0.0                                        # a greedy row
+    for kw in (dict(), dict(temperature=T), dict(temperature=T, top_p=p), dict(temperature=T, top_k=k),
+               dict(temperature=T, top_k=k, top_p=p)):
+        alone, none = ra.token_sample(z, u, **kw)
+        both, logp = ra.token_sample(z, u, want_logprob=True, **kw)
+        assert none is None and torch.equal(alone, both)
+        for n in {0, N // 2, N - 1}:
+            get = lambda name, off: kw[name][n].item() if name in kw else off
+            want = host(z[n].double().cpu().numpy(), u[n].item(), get("temperature", 1.0),
+                        get("top_k", 0), get("top_p", 1.0))
+            assert alone[n].item() == want[0]
