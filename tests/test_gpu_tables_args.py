@@ -51,3 +51,26 @@ def test_lengths_in_place_are_refused(device):
     assert start.tolist() == [2, 3, 4] and new.tolist() == [1, 1, 1] and count.item() == 32
     # what is only read may be the same
     assert ra.block_table_release(table, start, start, free, count).item() == 0
+
+
+@pytest.mark.parametrize("B,nhi", [(1, 1), (64, 1), (40, 300), (1100, 9)])
+def test_without_a_slot_map(B, nhi, device):
+    """Through the C ABI: the same tables, lengths and list as with one."""
+    from paper_2603_18815_amd import _lib
+    rng = np.random.default_rng(B)
+    start, new = dev(rng.integers(0, 64, B)), dev(rng.integers(0, nhi + 1, B))
+    stride, total = (64 + nhi) // 16 + 1, int(new.sum())
+    sides = []
+    for slots in (True, False):
+        table, free, count = pool(B, stride, B * stride)
+        cu, lens, taken = dev(np.full(B + 1, 9)), dev(np.full(B, 9)), dev([9])
+        out = torch.full((total,), 5, dtype=torch.int64, device="cuda:0") if slots else None
+        s = _lib.load().kv_block_table_extend(
+            start.data_ptr(), new.data_ptr(), free.data_ptr(), count.data_ptr(), free.numel(),
+            table.data_ptr(), B, stride, total, cu.data_ptr(), lens.data_ptr(),
+            out.data_ptr() if slots else None, taken.data_ptr(),
+            torch.cuda.current_stream().cuda_stream)
+        assert s == _lib.RA_OK
+        sides.append((table, free, count, cu, lens, taken))
+    assert all(torch.equal(a, b) for a, b in zip(*sides))
+    assert sides[0][5].item() >= 0
