@@ -461,8 +461,6 @@ int token_logprob_packed(const void *h, const void *W_packed, const int32_t *tar
  * at +inf share the weight. uniform[n] is taken into [0, 1) (NaN as 0). Weights are summed
  * as whole numbers of 2^-44 of the largest one (exact in any order; weights below half of
  * that are never drawn), so that the draw is that of sums in 64-bit floating point.
- * With filters, an element farther below M than the largest fp32 number is not drawn
- * either, whatever T is.
  *
  *   logits       fp32 or bf16 (logits_dtype) [N] rows of V, row_stride elements apart
  *                (any alignment of an element)

@@ -211,7 +211,7 @@ struct Row {
 // top-p) in bin_k = lo = hi; with top-k and top-p, what top-k keeps of bin_k also decides.
 struct Border {
   double sum;                           // of the weights (top-p alone)
-  float top, rate;                      // largest logit; bins a unit of logit
+  float top, rate;                      // largest logit; bins two units of logit
   int lo, hi, bin_k;                    // kBins: none
   uint32_t count_lo, count_k;           // elements before bin lo, bin_k
   uint64_t mass_lo, mass_k;             // weights before them
@@ -226,10 +226,13 @@ __device__ __forceinline__ int bin_of(float below, float rate) {
   const float b = below * rate;
   return b < kBins ? (int)b : kBins;
 }
-__device__ __forceinline__ float below(float top, float z) { return z == top ? 0.f : top - z; }
-// Bins a unit of logit, for a range of (M - z) / T. The slack takes in what rounds past it.
+// Half the distance: a whole one can pass the largest fp32 number.
+__device__ __forceinline__ float below(float top, float z) {
+  return z == top ? 0.f : fmaf(-0.5f, z, 0.5f * top);
+}
+// Bins two units of logit, for a range of (M - z) / T. The slack takes in what rounds past it.
 __device__ __forceinline__ float rate_of(double range, double inv_t) {
-  return (float)fmin(inv_t * (kBins / (fmax(range, 1e-30) * (1.0 + 1e-6))), 0x1.fp127);
+  return (float)fmin(inv_t * (2 * kBins / (fmax(range, 1e-30) * (1.0 + 1e-6))), 0x1.fp127);
 }
 
 // ---- reductions, in a fixed order ----
@@ -475,7 +478,7 @@ __global__ __launch_bounds__(kRowThreads) void sample_range_kernel(SampleArgs a)
         before += c[i];
       }
       bin = wave_reduce(bin, [](int x, int y) { return min(x, y); });
-      if (bin < kBins) range = fmin(range, (bin + 1) / (double)rate * row.inv_t * (1.0 + 1e-6));
+      if (bin < kBins) range = fmin(range, 2 * (bin + 1) / (double)rate * row.inv_t * (1.0 + 1e-6));
     } else {
       double x = 0.0;
 #pragma unroll

@@ -12,6 +12,7 @@ import paper_2603_18815_amd as ra
 from test_gpu_sample import check, host, uniforms
 
 pytestmark = pytest.mark.gpu
+NINF = float("-inf")
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
@@ -47,3 +48,42 @@ def test_the_log_probability_may_be_left_out(N, V, device):
             want = host(z[n].double().cpu().numpy(), u[n].item(), get("temperature", 1.0),
                         get("top_k", 0), get("top_p", 1.0))
             assert alone[n].item() == want[0]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [7, 500, 9001, 70000])
+def test_logits_farther_apart_than_the_largest_fp32_number(V, dtype, device):
+    """Temperatures that make such distances small: every filter, and none."""
+    g = torch.Generator(device="cuda:0").manual_seed(V)
+    z = (3.3e38 * (2 * torch.rand((8, V), generator=g, device="cuda:0") - 1)).to(dtype)
+    z[1] = z[1].abs().neg()
+    z[1, V // 2] = 3.3e38                                  # one far above the rest
+    z[2, ::2] = NINF
+    z[3, ::3], z[3, 1::3] = 3.3e38, -3.3e38                # two values and what lies between
+    z[4] *= 1e-3
+    z[5, V - 1] = float("inf")
+    u = uniforms(8, V)
+    for T in ([2e38] * 8, [3e38, 1e38, 5e37, 2e37, 1e36, 2e38, float("inf"), 3e36]):
+        k = [V // 2 + 1, 3, V // 4 + 1, V - 1, 2, 5, V // 3 + 1, 6]
+        p = [0.9, 0.999, 0.5, 0.75, 0.3, 0.9, 0.6, 0.99]
+        m = [0.3, 0.001, 0.1, 0.5, 0.0, 0.2, 0.9, 0.05]
+        check(z, u, T, what="plain")
+        check(z, u, T, k, what="top-k")
+        check(z, u, T, None, p, what="top-p")
+        check(z, u, T, None, None, m, what="min-p")
+        check(z, u, T, k, p, m, what="all")
+
+
+@pytest.mark.parametrize("V", [7, 9001, 70000])
+def test_logits_of_the_smallest_fp32_numbers(V, device):
+    """Distances of a few times 2^-149, at temperatures as small."""
+    g = torch.Generator(device="cuda:0").manual_seed(V)
+    z = torch.randint(0, 9, (6, V), generator=g, device="cuda:0", dtype=torch.int32).view(torch.float32)
+    u, tiny = uniforms(6, V), 2.0 ** -149
+    T = [tiny, 2 * tiny, 3 * tiny, 8 * tiny, 100 * tiny, 1.0]
+    k, p = [V // 2 + 1, 3, V // 4 + 1, V - 1, 2, 5], [0.9, 0.999, 0.5, 0.75, 0.3, 0.9]
+    m = [0.3, 0.001, 0.1, 0.5, 0.0, 0.2]
+    check(z, u, T, what="plain")
+    check(z, u, T, k, what="top-k")
+    check(z, u, T, None, p, what="top-p")
+    check(z, u, T, k, p, m, what="all")
