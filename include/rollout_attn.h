@@ -468,9 +468,9 @@ int token_logprob_packed(const void *h, const void *W_packed, const int32_t *tar
  *   uniform      fp32 [N] in [0, 1)
  *   tokens       int32 [N]
  *   logprob      fp32 [N] or NULL
- *   workspace    device scratch of at least token_sample_workspace_size(N, V) bytes,
- *                16-byte aligned (contents on entry ignored). Calls that share one must
- *                not overlap.
+ *   workspace    device scratch of at least token_sample_workspace_size(N, V) bytes (9 KB a
+ *                row and 1 to 5 bytes a logit), 16-byte aligned (contents on entry ignored).
+ *                Calls that share one must not overlap.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (N < 0, V <= 0, row_stride < V with N > 1);
  *         RA_ERR_UNSUPPORTED (an unknown logits_dtype, V > 2^19, N > 2^20);
  *         RA_ERR_WORKSPACE; RA_ERR_HIP. N == 0 returns RA_OK without launching anything.

@@ -4,7 +4,7 @@
 //   S_t = l S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t,   l = exp(log_decay) per KV head.
 //
 // Decode reads and writes the state, 128 KiB a (row, KV head), and is bound by that: 256
-// rows of 32 KV heads, 1.08 GB, take 190-216 us, 5.0-5.7 TB/s (a large copy: 4.7).
+// rows of 32 KV heads, 1.08 GB, take 216-219 us, 5.0 TB/s (a large copy: 4.75).
 //
 // Append takes chunks of 64 tokens on the matrix cores. With i, j a chunk's tokens, S the
 // state before it and n its length:
@@ -20,7 +20,8 @@
 // |S| |q|, however little of that a result keeps.
 // Measured: 32 rows of 120 to 2,038 tokens, 32 heads on 8, 744 MB, 230-240 us (shared by
 // two); a row of 16,384 with 32 heads each, 541 MB of which K and V are read twice, 218-224
-// us (cut into 8 stretches of 32 chunks); 905 tokens in 2 rows 25 us (cut).
+// us (cut into 8 stretches of 32 chunks: states 65, scan 8, outputs 149); 905 tokens in 2
+// rows 25 us (cut).
 #include "ra_device.h"
 #include "ra_internal.h"
 
