@@ -1,0 +1,775 @@
+"""The operators of a speculative rollout step, and of rollouts that share a prompt: attention
+for a tree of drafted tokens, penalties and masks on logits, the tree's masks and the walk of
+the accepted path, forked and copied pages, and the compaction of the accepted tokens' keys and
+values. One pass each, in a plain form of elementary torch operations or through the library.
+
+A case is a dict of plain values; "lens" seeds its lengths and the shapes of its trees, so that
+the work of a pass is fixed, and all values follow from the seed given to prepare(). A serving
+loop keeps its caches, tables, histories and workspaces, and its output buffers where shapes
+stay the same from step to step; those are made in prepare(). It knows its rows' lengths on the
+host, so the maxima are passed.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+PAGE, DIM = 16, 128
+SCALE = 1.0 / math.sqrt(DIM)
+K_SCALE, V_SCALE = 0.02, 0.03         # of the fp8 pools
+DEVICE = "cuda:0"
+
+# A drawn case does no more than this (the largest listed ones do about as much).
+MOST_KEYS, MOST_SCORES, MOST_LOGITS = 64 * 32768 * 8, 32 * 64 * 24576 * 32, 150_000_000
+MOST_ENTRIES, MOST_COPIES, MOST_NODES = 300_000, 4096, 40_000
+
+
+def listed():
+    return [
+        # A few short trajectories, a handful of drafted tokens each: launch-bound.
+        dict(name="tree_b4", kind="tree", B=4, Hq=8, Hkv=2, lo=32, hi=256, tlo=1, thi=8,
+             pool="bf16", lens=1),
+        # A full batch on the Qwen3-8B shape: eight drafted tokens a trajectory, one read of
+        # 4k..32k cached keys for all of them.
+        dict(name="tree_b64_t8", kind="tree", B=64, Hq=32, Hkv=8, lo=4096, hi=32768, tlo=8, thi=8,
+             pool="bf16", lens=2),
+        # Wide trees, up to 64 nodes, ragged: the matrix cores are as busy as the memory.
+        dict(name="tree_b32_t64", kind="tree", B=32, Hq=32, Hkv=8, lo=2048, hi=24576, tlo=16,
+             thi=64, pool="bf16", lens=3),
+        # One trajectory on a small vocabulary with a short answer so far: launch-bound.
+        dict(name="adjust_n1", kind="adjust", B=1, V=32000, pad=0, dtype="fp32", lo=200, hi=400,
+             nodes=0, use="repetition frequency presence", inplace=False, lens=4),
+        # A decode step of a full batch with long histories: penalties alone, in place.
+        dict(name="adjust_n64_inplace", kind="adjust", B=64, V=151936, pad=0, dtype="fp32",
+             lo=4096, hi=32768, nodes=0, use="repetition frequency presence", inplace=True, lens=5),
+        # The logits of 32 trajectories' trees, with biases and a grammar state for each node.
+        dict(name="adjust_tree_b32", kind="adjust", B=32, V=151936, pad=0, dtype="bf16", lo=2048,
+             hi=24576, nodes=48, use="repetition frequency presence bias allowed", inplace=False,
+             lens=6),
+        # A few small trees: their masks, then the walk of the chosen tokens.
+        dict(name="draft_b8_t16", kind="draft", B=8, tlo=1, thi=16, lens=7),
+        # A large batch of wide ones.
+        dict(name="draft_b512_t64", kind="draft", B=512, tlo=48, thi=64, lens=8),
+        # One short prompt, two rollouts of it.
+        dict(name="fork_1x2", kind="fork", tasks=1, group=2, Hkv=2, lo=100, hi=200, pool="bf16",
+             lens=9),
+        # Eight rollouts for each of 64 prompts.
+        dict(name="fork_64x8", kind="fork", tasks=64, group=8, Hkv=8, lo=2048, hi=8192,
+             pool="bf16", lens=10),
+        # A few rows' accepted tokens.
+        dict(name="compact_b4_t8", kind="compact", B=4, Hkv=2, lo=32, hi=256, tlo=1, thi=8,
+             keep=0.5, pool="bf16", lens=11),
+        # A large batch with long accepted paths.
+        dict(name="compact_b512_t64", kind="compact", B=512, Hkv=8, lo=512, hi=8192, tlo=32,
+             thi=64, keep=0.3, pool="bf16", lens=12),
+    ]
+
+
+HEADS = [(8, 2), (16, 1), (8, 8), (32, 8), (32, 8), (64, 8), (32, 32), (24, 8), (32, 1)]
+USES = ["repetition", "frequency presence", "repetition frequency presence", "allowed",
+        "bias", "repetition frequency presence bias allowed", "repetition bias",
+        "frequency allowed"]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _draw_once(rng):
+    kind = rng.choice(["tree", "tree", "tree", "adjust", "adjust", "adjust", "draft", "fork",
+                       "compact"])
+    lens = rng.randrange(1 << 30)
+    pool = rng.choice(["bf16", "bf16", "fp8"])
+    if kind == "tree":
+        hq, hkv = rng.choice(HEADS)
+        hi = _log_int(rng, 1, 32768)
+        thi = _log_int(rng, 1, 256)
+        return dict(kind=kind, B=_log_int(rng, 1, 64), Hq=hq, Hkv=hkv, lo=rng.choice([0, hi // 2]),
+                    hi=hi, tlo=rng.choice([0, 1, thi]), thi=thi, pool=pool, lens=lens)
+    if kind == "adjust":
+        hi = _log_int(rng, 1, 32768)
+        use = rng.choice(USES)
+        return dict(kind=kind, B=_log_int(rng, 1, 256),
+                    V=rng.choice([151936, 128256 + rng.randrange(64), 32000 - rng.randrange(64),
+                                  _log_int(rng, 2, 65536)]),
+                    pad=rng.choice([0, 0, rng.randrange(1, 64)]), dtype=rng.choice(["fp32", "bf16"]),
+                    lo=rng.choice([0, hi // 2]), hi=hi, nodes=rng.choice([0, 0, 8, 32]), use=use,
+                    inplace=rng.choice([False, False, True]), lens=lens)
+    if kind == "draft":
+        thi = _log_int(rng, 1, 256)
+        return dict(kind=kind, B=_log_int(rng, 1, 1024), tlo=rng.choice([0, thi // 2]), thi=thi,
+                    lens=lens)
+    if kind == "fork":
+        hi = _log_int(rng, 1, 16384)
+        return dict(kind=kind, tasks=_log_int(rng, 1, 128), group=rng.randrange(2, 17),
+                    Hkv=rng.choice([1, 2, 8, 8, 32]), lo=rng.choice([0, hi // 2]), hi=hi,
+                    pool=pool, lens=lens)
+    thi = _log_int(rng, 1, 256)
+    hi = _log_int(rng, 16, 8192)
+    return dict(kind=kind, B=_log_int(rng, 1, 512), Hkv=rng.choice([1, 2, 8, 8, 32]),
+                lo=rng.choice([0, hi // 2]), hi=hi, tlo=rng.choice([0, 1, thi]), thi=thi,
+                keep=rng.choice([0.1, 0.5, 0.8]), pool=pool, lens=lens)
+
+
+def draw(rng):
+    while True:
+        c = _draw_once(rng)
+        kind = c["kind"]
+        if kind == "tree":
+            most = c["hi"] + c["thi"]
+            fits = (c["B"] * most * c["Hkv"] <= MOST_KEYS and
+                    c["B"] * c["thi"] * most * c["Hq"] <= MOST_SCORES)
+        elif kind == "adjust":
+            fits = (c["B"] * max(1, c["nodes"]) * c["V"] <= MOST_LOGITS and
+                    c["B"] * c["hi"] <= 64 * 32768)
+        elif kind == "draft":
+            fits = c["B"] * c["thi"] <= MOST_NODES
+        elif kind == "fork":
+            fits = (c["tasks"] * c["group"] * _pages(c["hi"]) <= MOST_ENTRIES and
+                    c["tasks"] * c["group"] * c["Hkv"] <= MOST_COPIES and
+                    c["tasks"] * _pages(c["hi"]) * c["Hkv"] <= MOST_ENTRIES)
+        else:
+            fits = c["B"] * c["thi"] * c["Hkv"] <= 8 * MOST_NODES
+        if fits:
+            return c
+
+
+# ---- lengths and trees: a case's own ------------------------------------------------------
+def _pages(n):
+    return (n + PAGE - 1) // PAGE
+
+
+def _uniform(r, lo, hi, n):
+    return r.integers(lo, hi + 1, n)
+
+
+def _shapes(case):
+    """Context lengths, nodes and parents [B][most nodes] of the rows (-1: the root)."""
+    r = np.random.default_rng(case["lens"])
+    ctx = _uniform(r, case["lo"], case["hi"], case["B"])
+    T = _uniform(r, case["tlo"], case["thi"], case["B"])
+    T[0] = max(T[0], 1)                                   # rows may be empty, a call is not
+    i = np.arange(max(int(T.max()), 1))
+    # a drafted token follows one of the eight before it, the last one most often
+    back = 1 + np.floor(8 * r.random((case["B"], i.size)) ** 3).astype(np.int64)
+    parents = np.where(i[None] == 0, -1, np.maximum(i[None] - back, 0))
+    return ctx, T, parents, r
+
+
+def _seen(parents):
+    """[B][i][j]: whether node j is node i or above it."""
+    B, n = parents.shape
+    seen = np.zeros((B, n, n), bool)
+    for i in range(n):
+        if i:
+            seen[:, i] = seen[np.arange(B), parents[:, i]]
+        seen[:, i, i] = True
+    return seen
+
+
+def _node_rows(case):
+    """Of the logits of trees: their nodes and parents."""
+    return _shapes(dict(case, tlo=1, thi=case["nodes"]))[1:3]
+
+
+def _kept(case):
+    """Of a compaction: each row's context, nodes, and whether a node is kept."""
+    ctx, T, _, r = _shapes(case)
+    keep = r.random((case["B"], int(T.max()))) < case["keep"]
+    keep[:, 0] = True
+    return ctx, T, keep & (np.arange(keep.shape[1])[None] < T[:, None])
+
+
+def _fork_lens(case):
+    r = np.random.default_rng(case["lens"])
+    return _uniform(r, case["lo"], case["hi"], case["tasks"])
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "tree":
+        ctx, T, parents, _ = _shapes(case)
+        seen = _seen(parents).sum(2)
+        inside = np.arange(seen.shape[1])[None] < T[:, None]
+        keys = int((seen * inside).sum() + (ctx * T).sum())
+        live = int((ctx + T)[T > 0].sum())
+        size = 2 * DIM * case["Hkv"] * (2 if case["pool"] == "bf16" else 1)
+        node = case["Hq"] * (DIM * (2 + 4) + 4) + 8 * ((case["thi"] + 63) // 64)
+        return dict(bytes=live * size + int(T.sum()) * node, flops=4 * DIM * case["Hq"] * keys)
+    if kind == "adjust":
+        hist = _uniform(np.random.default_rng(case["lens"]), case["lo"], case["hi"], case["B"])
+        rows = int(_node_rows(case)[0].sum()) if case["nodes"] else case["B"]
+        es = 4 if case["dtype"] == "fp32" else 2
+        read = 4 * int(hist.sum()) if _penalties(case) else 0
+        bits = rows * case["V"] // 8 if "allowed" in case["use"] else 0
+        touched = rows * case["V"]
+        if case["inplace"] and not bits:                  # what the histories name
+            p = 1.0 / ((np.arange(case["V"]) + 1.0) * math.log(case["V"] + 1.0))
+            mean = float((1.0 - (1.0 - p) ** hist.mean()).sum()) if _penalties(case) else 0.0
+            touched = int(rows * (mean + (64 if "bias" in case["use"] else 0)))
+        return dict(bytes=2 * es * touched + read + bits + 16 * rows, flops=4 * touched)
+    if kind == "draft":
+        nodes = int(_shapes(dict(case, lo=0, hi=32768))[1].sum())
+        return dict(bytes=nodes * (4 * 4 + 8 * ((case["thi"] + 63) // 64) + 4 * 3), flops=0)
+    if kind == "fork":
+        lens, n = _fork_lens(case), case["group"] - 1
+        page = 2 * PAGE * DIM * case["Hkv"] * (2 if case["pool"] == "bf16" else 1)
+        entries = int((lens // PAGE).sum()) * n
+        copies = int((lens % PAGE > 0).sum()) * n
+        # forked: an entry read, one written, its owners read and written; given back: read again
+        return dict(bytes=entries * 28 + copies * (2 * page + 24), flops=0)
+    keep = _kept(case)[2]
+    moved = int((keep & (np.cumsum(keep, 1) - 1 != np.arange(keep.shape[1])[None])).sum())
+    size = 2 * DIM * case["Hkv"] * (2 if case["pool"] == "bf16" else 1)
+    return dict(bytes=2 * size * moved + 4 * int(keep.sum()) + 8 * case["B"], flops=0)
+
+
+# ---- inputs -------------------------------------------------------------------------------
+def _i32(x):
+    return torch.as_tensor(np.ascontiguousarray(np.asarray(x, np.int32)), device=DEVICE)
+
+
+def _pool(shape, pool, g):
+    x = torch.empty(shape, dtype=torch.bfloat16, device=DEVICE).normal_(generator=g)
+    if pool == "bf16":
+        return x
+    return (x * 32.0).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+def _caches(case, pages, g):
+    k = _pool((pages, case["Hkv"], PAGE, DIM), case["pool"], g)
+    v = _pool((pages, case["Hkv"], DIM, PAGE), case["pool"], g)
+    return dict(k_pool=k, v_pool=v, fp8=case["pool"] == "fp8")
+
+
+def _kv(s):
+    import paper_2603_18815_amd as ra
+    return ra.PagedKV(s["k_pool"], s["v_pool"], s["table"], K_SCALE if s["fp8"] else None,
+                      V_SCALE if s["fp8"] else None)
+
+
+def _table(pages_of_row, first, stride, num_pages, g):
+    """Rows' pages in a shuffled order, from entry first[b] on; page 0 elsewhere."""
+    order = (torch.randperm(num_pages - 1, generator=g, device=DEVICE) + 1).to(torch.int32)
+    j = torch.arange(stride, device=DEVICE)[None]
+    mine = (j >= _i32(first)[:, None]) & (j < _i32(first + pages_of_row)[:, None])
+    table = torch.zeros((len(first), stride), dtype=torch.int32, device=DEVICE)
+    table[mine] = order[:int(pages_of_row.sum())]
+    return table
+
+
+def _words(seen, T):
+    """Bit masks int64 [total][words] of the rows' nodes."""
+    B, n, _ = seen.shape
+    words = (n + 63) // 64
+    bits = np.zeros((B, n, 64 * words), bool)
+    bits[:, :, :n] = seen
+    packed = np.packbits(bits, axis=2, bitorder="little").view(np.int64)
+    inside = np.arange(n)[None] < T[:, None]
+    return torch.as_tensor(np.ascontiguousarray(packed[inside]), device=DEVICE)
+
+
+def _cu(T):
+    return np.concatenate([[0], np.cumsum(T)])
+
+
+def _prepare_tree(case, g):
+    B, Hq = case["B"], case["Hq"]
+    ctx, T, parents, _ = _shapes(case)
+    pages = _pages(ctx + T)
+    num_pages = int(pages.sum()) + 16
+    s = _caches(case, num_pages, g)
+    s["table"] = _table(pages, np.zeros(B, np.int64), int(pages.max()) + 1, num_pages, g)
+    total = int(T.sum())
+    s["q"] = torch.randn((total, Hq, DIM), generator=g, device=DEVICE).to(torch.bfloat16)
+    s["mask"] = _words(_seen(parents), T)
+    s.update(cu=_i32(_cu(T)), ctx=_i32(ctx), max_q=int(T.max()), max_kv=int((ctx + T).max()),
+             Hkv=case["Hkv"])
+    if own:
+        import paper_2603_18815_amd as ra
+        s["kv"] = _kv(s)
+        s["out"] = torch.empty((total, Hq, DIM), dtype=torch.float32, device=DEVICE)
+        s["lse"] = torch.empty((total, Hq), dtype=torch.float32, device=DEVICE)
+        size = ra.decode_tree_workspace_size(B, Hq, case["Hkv"], total, s["max_q"], s["max_kv"])
+        s["workspace"] = torch.empty(max(1, size), dtype=torch.uint8, device=DEVICE)
+    return s
+
+
+def _penalties(case):
+    return any(p in case["use"] for p in ("repetition", "frequency", "presence"))
+
+
+def _tokens(shape, V, g):
+    """Token ids as text has them: a few very often, most hardly ever."""
+    u = torch.rand(shape, generator=g, device=DEVICE, dtype=torch.float64)
+    return (torch.exp(u * math.log(V + 1.0)).long() - 1).clamp(0, V - 1).to(torch.int32)
+
+
+def _prepare_adjust(case, g):
+    B, V, use = case["B"], case["V"], case["use"]
+    rnd = lambda *shape: torch.rand(shape, generator=g, device=DEVICE)
+    s = dict(B=B, V=V, inplace=case["inplace"])
+    N = B
+    for name in ("cu_rows", "draft", "mask", "history", "history_lens", "prompt_lens",
+                 "repetition", "frequency", "presence", "bias_tokens", "bias_values", "cu_bias",
+                 "allowed", "allowed_rows"):
+        s[name] = None
+    if case["nodes"]:
+        T, parents = _node_rows(case)
+        N = int(T.sum())
+        s.update(cu_rows=_i32(_cu(T)), mask=_words(_seen(parents), T), draft=_tokens((N,), V, g))
+    store = torch.randn((N, V + case["pad"]), generator=g, device=DEVICE) * 3.0
+    s["logits"] = store.to(torch.bfloat16)[:, :V] if case["dtype"] == "bf16" else store[:, :V]
+    if _penalties(case):
+        lens = _uniform(np.random.default_rng(case["lens"]), case["lo"], case["hi"], B)
+        s.update(history=_tokens((B, int(lens.max()) + 3), V, g), history_lens=_i32(lens),
+                 prompt_lens=_i32(lens // 3))
+    for name, lo, width in (("repetition", 1.0, 0.3), ("frequency", 0.0, 0.4), ("presence", 0.0, 0.6)):
+        if name in use:
+            s[name] = lo + width * rnd(B)
+    if "bias" in use:
+        count = torch.randint(0, 129, (B,), generator=g, device=DEVICE)
+        cu = torch.cat([count.new_zeros(1), torch.cumsum(count, 0)])
+        n = B * 128                                       # room for more than the rows have
+        s.update(cu_bias=cu.to(torch.int32), bias_values=8.0 * rnd(n) - 4.0,
+                 bias_tokens=(rnd(n) * V).long().clamp(max=V - 1).to(torch.int32))
+    if "allowed" in use:                                  # a few grammar states, shared by rows
+        M = min(N, 64)
+        words = (V + 31) // 32
+        few = torch.rand((M, 1), generator=g, device=DEVICE) < 0.5
+        bits = torch.where(few, rnd(M, words) < 0.02, rnd(M, words) < 0.9)
+        full = torch.randint(-2**31, 2**31, (M, words), generator=g, device=DEVICE)
+        s["allowed"] = torch.where(bits, full, 0).to(torch.int32)
+        which = torch.randint(0, M, (N,), generator=g, device=DEVICE)
+        s["allowed_rows"] = torch.where(rnd(N) < 0.7, which, -1).to(torch.int32)
+    if own and not case["inplace"]:
+        s["out"] = torch.empty((N, V), dtype=s["logits"].dtype, device=DEVICE)
+    return s
+
+
+def _prepare_draft(case, g):
+    ctx, T, parents, _ = _shapes(dict(case, lo=0, hi=32768))
+    total = int(T.sum())
+    inside = np.arange(parents.shape[1])[None] < T[:, None]
+    # few different tokens, so that paths are a few nodes long
+    s = dict(cu=_i32(_cu(T)), ctx=_i32(ctx), parents=_i32(parents[inside]), max_q=int(T.max()),
+             draft=torch.randint(0, 3, (total,), generator=g, device=DEVICE).to(torch.int32),
+             chosen=torch.randint(0, 3, (total,), generator=g, device=DEVICE).to(torch.int32))
+    if own:
+        i32 = lambda n: torch.empty(n, dtype=torch.int32, device=DEVICE)
+        words = (s["max_q"] + 63) // 64
+        s["mask"] = torch.empty((total, words), dtype=torch.int64, device=DEVICE)
+        s["positions"] = i32(total)
+        s["outs"] = dict(path=i32(total), tokens=i32(total), accepted=i32(case["B"]),
+                         kv_lens=i32(case["B"]), next_tokens=i32(case["B"]))
+    return s
+
+
+def _prepare_fork(case, g):
+    lens, n = _fork_lens(case), case["group"] - 1
+    rows, pages = case["tasks"] * case["group"], _pages(lens)
+    num_pages = int(pages.sum()) + case["tasks"] * n + 8
+    s = _caches(case, num_pages, g)
+    first = np.zeros(rows, np.int64)
+    held = np.zeros(rows, np.int64)
+    held[::case["group"]] = pages
+    stride = int(pages.max()) + 2
+    s["table"] = _table(held, first, stride, num_pages, g)
+    used = torch.zeros(num_pages, dtype=torch.bool, device=DEVICE)
+    used[s["table"].long().view(-1)] = True
+    used[0] = True
+    free = torch.nonzero(~used)[:, 0]
+    free = free[torch.randperm(free.numel(), generator=g, device=DEVICE)].to(torch.int32)
+    s["free"] = torch.zeros(num_pages, dtype=torch.int32, device=DEVICE)
+    s["free"][:free.numel()] = free
+    s["count"] = _i32([free.numel()])
+    s["shares"] = torch.zeros(num_pages, dtype=torch.int32, device=DEVICE)
+    task = np.repeat(np.arange(case["tasks"]), n)
+    member = np.tile(1 + np.arange(n), case["tasks"])
+    row_lens = np.where(np.arange(rows) % case["group"] > 0, np.repeat(lens, case["group"]), 0)
+    s.update(src=_i32(task * case["group"]), dst=_i32(task * case["group"] + member),
+             lens=_i32(lens[task]), row_lens=_i32(row_lens), none=_i32(np.zeros(rows)))
+    if own:
+        import paper_2603_18815_amd as ra
+        s["kv"] = _kv(s)
+        i32 = lambda n: torch.empty(n, dtype=torch.int32, device=DEVICE)
+        s["outs"] = dict(copy_src=i32(len(task)), copy_dst=i32(len(task)), taken=i32(1))
+        s["released"] = i32(1)
+        s["max_pages"] = int(_pages(row_lens).sum())
+        size = ra.block_table_release_shared_workspace_size(rows)
+        s["workspace"] = torch.empty(max(1, size), dtype=torch.uint8, device=DEVICE)
+    return s
+
+
+def _prepare_compact(case, g):
+    ctx, T, keep = _kept(case)
+    B, first = case["B"], ctx // PAGE                     # the pages before are not touched
+    pages = _pages(ctx + T) - first
+    num_pages = int(pages.sum()) + 16
+    s = _caches(case, num_pages, g)
+    s["table"] = _table(pages, first, int(_pages(ctx + T).max()) + 1, num_pages, g)
+    counts = keep.sum(1)
+    order = np.argsort(~keep, axis=1, kind="stable")      # the kept nodes of a row first
+    inside = np.arange(keep.shape[1])[None] < T[:, None]
+    rank = np.arange(keep.shape[1])[None]
+    index = np.where(rank < counts[:, None], order, -1)
+    s.update(start=_i32(ctx), cu=_i32(_cu(T)), index=_i32(index[inside]), counts=_i32(counts),
+             max_count=int(counts.max()))
+    if own:
+        s["kv"] = _kv(s)
+    return s
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(seed)
+    make = dict(tree=_prepare_tree, adjust=_prepare_adjust, draft=_prepare_draft,
+                fork=_prepare_fork, compact=_prepare_compact)[case["kind"]]
+    return dict(make(case, g), kind=case["kind"])
+
+
+# ---- plain forms --------------------------------------------------------------------------
+def _row_and_index(cu, total):
+    """Of every packed entry: its row and its place in it."""
+    t = torch.arange(total, device=DEVICE)
+    row = torch.searchsorted(cu.long(), t, right=True) - 1
+    return row, t - cu.long()[row]
+
+
+def _values(pool, fp8, scale):
+    return pool.view(torch.float8_e4m3fn).float() * scale if fp8 else pool.float()
+
+
+def _tree_plain(s):
+    table, ctx, cu, q = s["table"].long(), s["ctx"].long(), s["cu"], s["q"].float()
+    B, Hkv, total = ctx.numel(), s["Hkv"], q.shape[0]
+    G = q.shape[1] // Hkv
+    row, i = _row_and_index(cu, total)
+    n, P = s["max_q"], table.shape[1]
+    L = P * PAGE
+    T = (cu[1:] - cu[:-1]).long()
+    pos = torch.arange(L, device=DEVICE)
+    live = pos[None] < (ctx + T)[:, None]                                    # [B, L]
+    k = _values(s["k_pool"][table.view(-1)], s["fp8"], K_SCALE)
+    k = k.view(B, P, Hkv, PAGE, DIM).permute(0, 2, 1, 3, 4).reshape(B, Hkv, L, DIM)
+    v = _values(s["v_pool"][table.view(-1)], s["fp8"], V_SCALE)
+    v = v.view(B, P, Hkv, DIM, PAGE).permute(0, 2, 1, 4, 3).reshape(B, Hkv, L, DIM)
+    v = torch.where(live[:, None, :, None], v, 0.0)
+    qp = torch.zeros((B, n, Hkv, G, DIM), device=DEVICE)
+    qp[row, i] = q.view(total, Hkv, G, DIM)
+    qp = qp.permute(0, 2, 1, 3, 4).reshape(B, Hkv, n * G, DIM)
+    # what node i may see: the context, and the nodes of its mask
+    j = pos[None] - ctx[:, None]                                             # [B, L]
+    bits = torch.zeros((B, n, s["mask"].shape[1]), dtype=torch.int64, device=DEVICE)
+    bits[row, i] = s["mask"]
+    word = (j // 64).clamp(0, s["mask"].shape[1] - 1)[:, None].expand(B, n, L)
+    bit = (torch.gather(bits, 2, word) >> (j % 64)[:, None]) & 1
+    sees = live[:, None] & ((j < 0)[:, None] | (bit > 0))                    # [B, n, L]
+    x = SCALE * torch.matmul(qp, k.transpose(2, 3)).view(B, Hkv, n, G, L)
+    x = torch.where(sees[:, None, :, None], x, float("-inf"))
+    top = x.amax(-1, keepdim=True)
+    top = torch.where(top == float("-inf"), 0.0, top)
+    e = torch.exp(x - top)
+    total_e = e.sum(-1, keepdim=True)
+    out = torch.matmul(e.view(B, Hkv, n * G, L), v).view(B, Hkv, n, G, DIM)
+    out = torch.where(total_e > 0, out / total_e, 0.0)
+    lse = (top + torch.log(total_e))[..., 0]
+    out = out.permute(0, 2, 1, 3, 4)[row, i].reshape(total, Hkv * G, DIM)
+    return dict(out=out, lse=lse.permute(0, 2, 1, 3)[row, i].reshape(total, Hkv * G))
+
+
+def _adjust_plain(s):
+    z = s["logits"].float()
+    N, V = z.shape
+    B = s["B"]
+    row = torch.arange(N, device=DEVICE) if s["cu_rows"] is None else _row_and_index(s["cu_rows"], N)[0]
+    if s["history"] is not None:
+        t = torch.arange(s["history"].shape[1], device=DEVICE)[None]
+        ids = s["history"].long()
+        inside = t < s["history_lens"][:, None]
+        answer = inside & (t >= s["prompt_lens"][:, None])
+        zeros = torch.zeros((B, V), dtype=torch.int32, device=DEVICE)
+        seen = zeros.scatter_add(1, ids, inside.to(torch.int32))[row]
+        count = zeros.scatter_add(1, ids, answer.to(torch.int32))[row]
+        if s["draft"] is not None:
+            _, i = _row_and_index(s["cu_rows"], N)
+            j = torch.arange(64 * s["mask"].shape[1], device=DEVICE)
+            first = s["cu_rows"].long()[row]
+            on_path = (s["mask"][:, j // 64] >> (j % 64)[None]) & 1
+            token = s["draft"].long()[(first[:, None] + j[None]).clamp(max=N - 1)]
+            count.scatter_add_(1, token, on_path.to(torch.int32))
+            seen.scatter_add_(1, token, on_path.to(torch.int32))
+        if s["repetition"] is not None:
+            r = s["repetition"][row][:, None]
+            z = torch.where(seen > 0, torch.where(z > 0, z / r, z * r), z)
+        if s["frequency"] is not None:
+            z = z - s["frequency"][row][:, None] * count
+        if s["presence"] is not None:
+            z = z - torch.where(count > 0, s["presence"][row][:, None], 0.0)
+    if s["bias_tokens"] is not None:
+        cu = s["cu_bias"].long()
+        at = torch.arange(s["bias_tokens"].numel(), device=DEVICE)
+        mine = (torch.searchsorted(cu, at, right=True) - 1).clamp(max=B)
+        last = torch.full((B + 1, V), -1, dtype=torch.int64, device=DEVICE)  # the last entry counts
+        last.view(-1).scatter_reduce_(0, mine * V + s["bias_tokens"].long(), at, "amax")
+        bias = torch.where(last >= 0, s["bias_values"][last.clamp(min=0)], 0.0)
+        z = z + bias[row]
+    if s["allowed"] is not None:
+        v = torch.arange(V, device=DEVICE)
+        which = s["allowed_rows"].long()
+        bit = (s["allowed"][:, v // 32] >> (v % 32)[None]) & 1
+        z = torch.where((which < 0)[:, None] | (bit[which.clamp(min=0)] > 0), z, float("-inf"))
+    z = z.to(s["logits"].dtype)
+    return s["logits"].copy_(z) if s["inplace"] else z
+
+
+def _draft_plain(s):
+    cu, parents, total = s["cu"].long(), s["parents"].long(), s["parents"].numel()
+    row, i = _row_and_index(s["cu"], total)
+    first, n = cu[row], s["max_q"]
+    # ancestors: reachability by squaring, 2^k steps up at a time
+    B = cu.numel() - 1
+    up = torch.zeros((B, n, n), device=DEVICE)
+    has = parents >= 0
+    up[row[has], i[has], parents[has]] = 1.0
+    reach = up + torch.eye(n, device=DEVICE)[None]
+    step, span = reach, 1
+    while span < n:
+        step, span = (torch.matmul(step, step) > 0).float(), 2 * span
+    mine = step[row, i] > 0                                                   # [total, n]
+    depth = mine.sum(1) - 1
+    words = (n + 63) // 64
+    padded = torch.zeros((total, 64 * words), dtype=torch.int64, device=DEVICE)
+    padded[:, :n] = mine
+    shift = torch.arange(64, device=DEVICE)
+    mask = (padded.view(total, words, 64) << shift).sum(2)
+    # a node is reached if every node below the root on its way is the first child of its
+    # parent that holds the token chosen there
+    fits = has & (s["draft"] == s["chosen"][(first + parents.clamp(min=0))])
+    key = torch.where(fits, first + parents, total)
+    firsts = torch.full((total + 1,), total, dtype=torch.int64, device=DEVICE)
+    firsts.scatter_reduce_(0, key, torch.arange(total, device=DEVICE), "amin")
+    good = (fits & (firsts[key] == torch.arange(total, device=DEVICE))) | (i == 0)
+    padded_good = torch.zeros((B, n), dtype=torch.bool, device=DEVICE)
+    padded_good[row, i] = good
+    taken = (mine & ~padded_good[row]).sum(1) == 0
+    accepted = torch.zeros(B, dtype=torch.int64, device=DEVICE).scatter_add_(0, row, taken.long())
+    path = torch.full((total,), -1, dtype=torch.int64, device=DEVICE)
+    tokens = path.clone()
+    at = (first + depth)[taken]
+    path[at] = i[taken]
+    tokens[at] = s["chosen"].long()[taken]
+    last = torch.where(accepted > 0, tokens[(cu[:-1] + accepted - 1).clamp(min=0)], -1)
+    i32 = lambda x: x.to(torch.int32)
+    return dict(mask=mask, positions=i32(s["ctx"].long()[row] + depth), path=i32(path),
+                tokens=i32(tokens), accepted=i32(accepted), kv_lens=i32(s["ctx"] + accepted),
+                next_tokens=i32(last))
+
+
+def _bits(x):
+    return x.view(torch.int16) if x.dtype == torch.bfloat16 else x
+
+
+def _fork_plain(s):
+    """Forks the rows, copies their last pages, then gives the forked rows back."""
+    table, free, count, shares = s["table"], s["free"], s["count"], s["shares"]
+    src, dst, lens = s["src"].long(), s["dst"].long(), s["lens"].long()
+    full, part = lens // PAGE, lens % PAGE > 0
+    before = torch.cumsum(part, 0) - part.long()
+    j = torch.arange(table.shape[1], device=DEVICE)[None]
+    whole = j < full[:, None]
+    page = free[(count - 1 - before).clamp(min=0)]
+    from_ = table[src]
+    new = torch.where(whole, from_, table[dst])
+    tail = part[:, None] & (j == full[:, None])
+    copy_src = torch.where(part, torch.gather(from_, 1, full[:, None].clamp(max=table.shape[1] - 1))[:, 0], -1)
+    copy_dst = torch.where(part, page, -1)
+    table[dst] = torch.where(tail, page[:, None], new)
+    shares.scatter_add_(0, from_.long().view(-1), whole.to(torch.int32).view(-1))
+    taken = part.sum().to(torch.int32).view(1)
+    count.sub_(taken)
+    some = part.nonzero()[:, 0]
+    s["k_pool"][copy_dst[some].long()] = s["k_pool"][copy_src[some].long()]
+    s["v_pool"][copy_dst[some].long()] = s["v_pool"][copy_src[some].long()]
+    shared = shares.clone()
+    # back: the pages of every row's tokens, an owner less each; free where none is left
+    gone = j < _pages(s["row_lens"].long())[:, None]
+    entries = table[gone].long()
+    times = torch.zeros_like(shares).scatter_add_(0, entries, torch.ones_like(entries, dtype=torch.int32))
+    freed = (times > 0) & (times > shares)
+    order = torch.arange(entries.numel(), device=DEVICE)
+    last = torch.full((shares.numel(),), -1, dtype=torch.int64, device=DEVICE)
+    last.scatter_reduce_(0, entries, order, "amax")
+    mine = freed[entries] & (last[entries] == order)
+    rank = torch.cumsum(mine, 0) - 1
+    released = mine.sum()
+    to = torch.where(mine, count + released - 1 - rank, free.numel())
+    longer = torch.cat([free, free.new_zeros(1)])
+    longer.scatter_(0, to, entries.to(torch.int32))
+    free.copy_(longer[:-1])
+    shares.copy_(torch.where(freed, 0, shares - times))
+    count.add_(released)
+    return dict(copy_src=copy_src, copy_dst=copy_dst, taken=taken, shared=shared, table=table,
+                released=released.to(torch.int32).view(1), shares=shares, free=free, count=count,
+                k_pool=_bits(s["k_pool"]), v_pool=_bits(s["v_pool"]))
+
+
+def _compact_plain(s):
+    row, i = _row_and_index(s["cu"], s["index"].numel())
+    kept = (i < s["counts"][row]).nonzero()[:, 0]
+    row, i = row[kept], i[kept]
+    place = lambda pos: (s["table"][row, pos // PAGE].long(), pos % PAGE)
+    start = s["start"].long()[row]
+    (p0, s0), (p1, s1) = place(start + s["index"].long()[kept]), place(start + i)
+    s["k_pool"][p1, :, s1] = s["k_pool"][p0, :, s0]
+    s["v_pool"][p1, :, :, s1] = s["v_pool"][p0, :, :, s0]
+    return dict(k_pool=_bits(s["k_pool"]), v_pool=_bits(s["v_pool"]))
+
+
+# ---- through the library ------------------------------------------------------------------
+def _tree_own(s):
+    import paper_2603_18815_amd as ra
+    out, lse = ra.decode_tree(s["q"], s["cu"], s["ctx"], s["mask"], s["kv"], max_q_len=s["max_q"],
+                              max_kv_len=s["max_kv"], out=s["out"], lse=s["lse"],
+                              workspace=s["workspace"])
+    return dict(out=out, lse=lse)
+
+
+def _adjust_own(s):
+    import paper_2603_18815_amd as ra
+    return ra.token_logits_adjust(
+        s["logits"], history=s["history"], history_lens=s["history_lens"],
+        prompt_lens=s["prompt_lens"], repetition=s["repetition"], frequency=s["frequency"],
+        presence=s["presence"], bias_tokens=s["bias_tokens"], bias_values=s["bias_values"],
+        cu_bias=s["cu_bias"], allowed=s["allowed"], allowed_rows=s["allowed_rows"],
+        cu_rows=s["cu_rows"], draft_tokens=s["draft"], tree_mask=s["mask"],
+        out=s["logits"] if s["inplace"] else s["out"])
+
+
+def _draft_own(s):
+    import paper_2603_18815_amd as ra
+    mask, positions = ra.draft_tree_mask(s["parents"], s["cu"], s["ctx"], max_q_len=s["max_q"],
+                                         tree_mask=s["mask"], positions=s["positions"])
+    path, tokens, accepted, kv_lens, next_tokens = ra.draft_tree_accept(
+        s["parents"], s["draft"], s["chosen"], s["cu"], s["ctx"], max_q_len=s["max_q"], **s["outs"])
+    return dict(mask=mask, positions=positions, path=path, tokens=tokens, accepted=accepted,
+                kv_lens=kv_lens, next_tokens=next_tokens)
+
+
+def _fork_own(s):
+    import paper_2603_18815_amd as ra
+    copy_src, copy_dst, taken = ra.block_table_fork(s["table"], s["src"], s["dst"], s["lens"],
+                                                    s["shares"], s["free"], s["count"], **s["outs"])
+    ra.kv_page_copy(s["kv"], copy_src, copy_dst)
+    shared = s["shares"].clone()
+    released = ra.block_table_release_shared(s["table"], s["row_lens"], s["none"], s["shares"],
+                                             s["free"], s["count"], max_pages=s["max_pages"],
+                                             released=s["released"], workspace=s["workspace"])
+    return dict(copy_src=copy_src, copy_dst=copy_dst, taken=taken, shared=shared, table=s["table"],
+                released=released, shares=s["shares"], free=s["free"], count=s["count"],
+                k_pool=_bits(s["k_pool"]), v_pool=_bits(s["v_pool"]))
+
+
+def _compact_own(s):
+    import paper_2603_18815_amd as ra
+    ra.kv_page_compact(s["kv"], s["start"], s["cu"], s["index"], s["counts"],
+                       max_count=s["max_count"])
+    return dict(k_pool=_bits(s["k_pool"]), v_pool=_bits(s["v_pool"]))
+
+
+def run(state):
+    if own:
+        call = dict(tree=_tree_own, adjust=_adjust_own, draft=_draft_own, fork=_fork_own,
+                    compact=_compact_own)
+    else:
+        call = dict(tree=_tree_plain, adjust=_adjust_plain, draft=_draft_plain, fork=_fork_plain,
+                    compact=_compact_plain)
+    return call[state["kind"]](state)
+
+
+# ---- the definitions in 64 bits -----------------------------------------------------------
+def _exact_tree(s):
+    """Row by row: the tokens' keys and values by their places, then a node's visible ones."""
+    table, Hkv = s["table"].cpu().numpy(), s["Hkv"]
+    ctx, cu = s["ctx"].cpu().numpy(), s["cu"].cpu().numpy()
+    masks = s["mask"].cpu().numpy().view(np.uint64)
+    decode = (lambda x, c: x.view(torch.float8_e4m3fn).double() * np.float64(np.float32(c))) \
+        if s["fp8"] else (lambda x, c: x.double())
+    total, Hq, _ = s["q"].shape
+    out = torch.zeros((total, Hq, DIM), dtype=torch.float64, device=DEVICE)
+    lse = torch.full((total, Hq), float("-inf"), dtype=torch.float64, device=DEVICE)
+    for b in range(ctx.size):
+        T = int(cu[b + 1] - cu[b])
+        L = int(ctx[b]) + T
+        if T == 0:
+            continue
+        pages = torch.as_tensor(table[b, :_pages(L)], device=DEVICE).long()
+        k = decode(s["k_pool"][pages], K_SCALE).transpose(1, 2).reshape(-1, Hkv, DIM)[:L]
+        v = decode(s["v_pool"][pages], V_SCALE).permute(0, 3, 1, 2).reshape(-1, Hkv, DIM)[:L]
+        sees = np.ones((T, L), bool)
+        for i in range(T):
+            for j in range(T):
+                word = int(masks[cu[b] + i, j // 64])
+                sees[i, int(ctx[b]) + j] = (word >> (j % 64)) & 1
+        hide = torch.as_tensor(~sees, device=DEVICE)[:, None]
+        q = s["q"][cu[b]:cu[b + 1]].double().view(T, Hkv, -1, DIM)
+        for h in range(Hkv):
+            x = SCALE * (q[:, h].reshape(-1, DIM) @ k[:, h].t()).view(T, -1, L)
+            x = x.masked_fill(hide, float("-inf"))
+            at, G = slice(int(cu[b]), int(cu[b + 1])), x.shape[1]
+            z = torch.logsumexp(x, 2)
+            w = torch.exp(x - torch.where(torch.isinf(z), 0.0, z)[..., None])
+            out[at, h * G:(h + 1) * G] = (w.reshape(-1, L) @ v[:, h]).view(T, G, DIM)
+            lse[at, h * G:(h + 1) * G] = z
+    return dict(out=out, lse=lse)
+
+
+def _exact_adjust(s):
+    """Row by row: counts by unique tokens, then one kind of change after the other."""
+    z = s["logits"].double()
+    N, V = z.shape
+    host = lambda x: None if x is None else x.cpu().numpy()
+    hist, lens, prompt = host(s["history"]), host(s["history_lens"]), host(s["prompt_lens"])
+    cu = np.arange(N + 1) if s["cu_rows"] is None else host(s["cu_rows"])
+    draft, masks = host(s["draft"]), host(s["mask"])
+    cu_bias, ids, values = host(s["cu_bias"]), host(s["bias_tokens"]), host(s["bias_values"])
+    param = lambda name, b, off: off if s[name] is None else float(s[name][b])
+    on = lambda x, **k: torch.as_tensor(x, device=DEVICE, **k)
+    which = host(s["allowed_rows"])
+    for b in range(s["B"]):
+        rep, freq, pres = param("repetition", b, 1.0), param("frequency", b, 0.0), param("presence", b, 0.0)
+        bias = {}
+        if ids is not None:
+            for e in range(cu_bias[b], cu_bias[b + 1]):
+                bias[int(ids[e])] = float(values[e])
+        for n in range(cu[b], cu[b + 1]):
+            if hist is not None:
+                prompt_ids = hist[b, :min(prompt[b], lens[b])]
+                answer = hist[b, prompt[b]:lens[b]]
+                if draft is not None:
+                    word = [int(w) & (2**64 - 1) for w in masks[n]]
+                    path = [draft[cu[b] + j] for j in range(cu[b + 1] - cu[b])
+                            if word[j // 64] >> (j % 64) & 1]
+                    answer = np.concatenate([answer, np.array(path, answer.dtype)])
+                known = on(np.unique(np.concatenate([prompt_ids, answer])).astype(np.int64))
+                x = z[n, known]
+                z[n, known] = torch.where(x > 0, x / rep, x * rep)
+                ids_, times = np.unique(answer, return_counts=True)
+                z[n, on(ids_.astype(np.int64))] -= on(freq * times + pres, dtype=torch.float64)
+            if bias:
+                z[n, on(list(bias.keys()))] += on(list(bias.values()), dtype=torch.float64)
+            if which is not None and which[n] >= 0:
+                words = s["allowed"][int(which[n])].cpu().numpy().view(np.uint8)
+                bits = np.unpackbits(words, bitorder="little")[:V].astype(bool)
+                z[n].masked_fill_(on(~bits), float("-inf"))
+    return z
+
+
+def exact(case, seed):
+    if case["kind"] == "tree":
+        return _exact_tree(prepare(case, seed))
+    if case["kind"] == "adjust":
+        return _exact_adjust(prepare(case, seed))
+    return None
