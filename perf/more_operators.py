@@ -397,7 +397,6 @@ def _prepare_fork(case, g):
         i32 = lambda n: torch.empty(n, dtype=torch.int32, device=DEVICE)
         s["outs"] = dict(copy_src=i32(len(task)), copy_dst=i32(len(task)), taken=i32(1))
         s["released"] = i32(1)
-        s["max_pages"] = int(_pages(row_lens).sum())
         size = ra.block_table_release_shared_workspace_size(rows)
         s["workspace"] = torch.empty(max(1, size), dtype=torch.uint8, device=DEVICE)
     return s
@@ -665,8 +664,8 @@ def _fork_own(s):
     ra.kv_page_copy(s["kv"], copy_src, copy_dst)
     shared = s["shares"].clone()
     released = ra.block_table_release_shared(s["table"], s["row_lens"], s["none"], s["shares"],
-                                             s["free"], s["count"], max_pages=s["max_pages"],
-                                             released=s["released"], workspace=s["workspace"])
+                                             s["free"], s["count"], released=s["released"],
+                                             workspace=s["workspace"])
     return dict(copy_src=copy_src, copy_dst=copy_dst, taken=taken, shared=shared, table=s["table"],
                 released=released, shares=s["shares"], free=s["free"], count=s["count"],
                 k_pool=_bits(s["k_pool"]), v_pool=_bits(s["v_pool"]))
