@@ -592,6 +592,222 @@ int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
                            int32_t max_pages, int32_t *released, hipStream_t stream);
 
 /*
+ * Trees of drafted tokens: a step that checks several guessed continuations of a trajectory
+ * at once, for rollouts that are bound by decode (Sec. 3.3.1, 3.3.2: an agent's steps wait for
+ * its completions one after the other). A row's tree has T nodes, packed at cu_q[b] ..
+ * cu_q[b+1]-1; node 0, the root, is the token that is known (the last one drawn), and every
+ * other node is a guess that follows its parent, a node before it. A step is
+ *   kv_block_table_extend, draft_tree_mask, kv_page_write (node i at position ctx + i, its key
+ *   and query rotated at positions[i]), rollout_attn_decode_tree in each layer, the LM head,
+ *   token_logits_adjust, token_sample (one token a node: chosen), draft_tree_accept,
+ *   kv_page_compact in each layer, kv_block_table_release (keep_lens = the new kv_lens).
+ * The tokens it emits are those that were drawn, node after node, so their distribution is
+ * that of steps of one token whatever the guesses are.
+ *
+ * draft_tree_mask: from the parents, the mask of each node (itself and its ancestors) and
+ * its position.
+ *   parents     int32 [total_q]: the parent's index in its row, below the node's own; anything
+ *               else: the node has none
+ *   cu_q        int32 [B+1];  ctx_lens  int32 [B] or NULL (0)
+ *   max_q_len   host: an upper bound of T, at most RA_MAX_DRAFT_NODES
+ *   mask_words  host: 64-bit words of a mask, at least ceil(max_q_len / 64)
+ *   tree_mask   uint64 [total_q][mask_words]: bit j of a node's mask (word j / 64, bit j % 64)
+ *   positions   int32 [total_q] or NULL: ctx_lens[b] + ancestors of the node
+ * draft_tree_accept: the walk of the chosen tokens down the tree. From the root on, the next
+ * node is the first child (lowest index) of the last one whose drafted token is the one chosen
+ * there; the walk ends where there is none.
+ *   draft_tokens  int32 [total_q];  chosen  int32 [total_q], the token drawn behind each node
+ *                 (negative: none, the walk ends)
+ *   path        int32 [total_q]: row b's nodes on the walk, ascending, from cu_q[b] on, then -1
+ *   tokens      int32 [total_q]: chosen[] of those nodes: the tokens that the step emits
+ *   accepted    int32 [B]: nodes on the walk (0 for a row without nodes)
+ *   kv_lens     int32 [B]: ctx_lens[b] + accepted[b]
+ *   next_tokens int32 [B]: the last of the row's tokens, the next step's root (-1: no nodes)
+ * Entries behind cu_q[B] are not touched; what a call writes must not share memory with another
+ * of its arrays.
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (negative sizes, too few mask_words);
+ *         RA_ERR_UNSUPPORTED (B > 65535, max_q_len > RA_MAX_DRAFT_NODES, shared memory);
+ *         RA_ERR_HIP. B == 0, total_q == 0 or max_q_len == 0 launch nothing.
+ */
+#define RA_MAX_DRAFT_NODES 1024
+int draft_tree_mask(const int32_t *parents, const int32_t *cu_q, const int32_t *ctx_lens,
+                    int32_t B, int32_t total_q, int32_t max_q_len, int32_t mask_words,
+                    uint64_t *tree_mask, int32_t *positions, hipStream_t stream);
+int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const int32_t *chosen,
+                      const int32_t *cu_q, const int32_t *ctx_lens, int32_t B, int32_t total_q,
+                      int32_t max_q_len, int32_t *path, int32_t *tokens, int32_t *accepted,
+                      int32_t *kv_lens, int32_t *next_tokens, hipStream_t stream);
+
+/*
+ * Decode of drafted trees: attention of every node over the row's cache and over the nodes
+ * that its mask names. Node i of row b (packed t = cu_q[b] + i, its key and value in the pool at
+ * position ctx_lens[b] + i) attends keys 0 .. ctx_lens[b] - 1 and ctx_lens[b] + j for every
+ * j < T whose bit in tree_mask[t] is set:
+ *   out[t][h] = softmax_j(scale * <q[t][h], K_j>) . V_j,  lse likewise.
+ * One node that sees itself is rollout_attn_decode with kv_lens = ctx_lens + 1; a chain is
+ * rollout_attn_append, with decode's precision. A node that sees no key gives out = 0 and lse
+ * = -inf. A masked key and value reach no result, infinite or NaN as they may be (a result that an
+ * infinite value of a node reaches may hold NaN where the formula has an infinity).
+ *
+ *   q           bf16 [total_q][Hq][128]
+ *   cu_q        int32 [B+1];  ctx_lens  int32 [B]
+ *   tree_mask   uint64 [total_q][mask_words]; bits at and past T are ignored
+ *   max_q_len   host: an upper bound of T, at most RA_MAX_DRAFT_NODES
+ *   max_kv_len  host: an upper bound of ctx_lens[b] + T; <= bt_stride * 16
+ *   out         fp32 [total_q][Hq][128];  lse  fp32 [total_q][Hq] or NULL; rows behind cu_q[B]
+ *               are not touched
+ *   workspace   device scratch of at least rollout_attn_decode_tree_workspace_size(B, Hq, Hkv,
+ *               total_q, max_q_len, max_kv_len) bytes (contents on entry ignored); NULL where
+ *               the size is 0. Calls that share one must not overlap.
+ * How keys are split, and with it the order of fp32 sums, depends on B, Hq, Hkv, total_q,
+ * max_q_len and max_kv_len alone.
+ * Errors: as rollout_attn_append; RA_ERR_SHAPE also for too few mask_words; RA_ERR_UNSUPPORTED
+ *         (Hq / Hkv > 256, B > 65535, max_q_len > RA_MAX_DRAFT_NODES, 2^31 or more workgroups,
+ *         q, pools, out or workspace not 16-byte aligned). B == 0, total_q == 0 or max_q_len ==
+ *         0 launch nothing.
+ */
+size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
+                                               int32_t total_q, int32_t max_q_len,
+                                               int32_t max_kv_len);
+int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *ctx_lens,
+                             const uint64_t *tree_mask, int32_t mask_words, const ra_paged_kv *kv,
+                             int32_t B, int32_t Hq, int32_t total_q, int32_t max_q_len,
+                             int32_t max_kv_len, float scale, float *out, float *lse,
+                             void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Logits before a token is drawn: penalties for tokens that a trajectory holds already, biases,
+ * and masks of what a grammar (a tool call's schema) allows. Stands between the LM head and
+ * token_sample. For row n of logits, with b its history row, s_v whether token v is in the
+ * history, c_v how often it is in the part behind the prompt:
+ *   1. z_v <- (z_v > 0 ? z_v / repetition[b] : z_v * repetition[b])   where s_v
+ *   2. z_v <- z_v - frequency[b] * c_v - presence[b]                  where c_v > 0
+ *   3. z_v <- z_v + bias_values[e]   for the last e in cu_bias[b] .. cu_bias[b+1]-1 with
+ *                                    bias_tokens[e] = v
+ *   4. z_v <- -inf                   where the row's mask has bit v clear
+ * in fp32, rounded once (to nearest even) to the type of the logits; elements that none of them
+ * concerns keep their bits. Tokens outside [0, V) are passed over. A repetition that is not
+ * finite and > 0 counts as 1, a frequency or presence that is not finite as 0.
+ *
+ *   logits        fp32 or bf16 (logits_dtype) [N] rows of V, row_stride elements apart (any
+ *                 alignment of an element); out likewise, out_stride apart; out = logits with
+ *                 the same stride works in place (and reads and writes only what changes)
+ * ra_logits_adjust (all arrays may be NULL where not said otherwise):
+ *   history       int32 [B] rows, history_stride apart, of which history_lens[b] (int32 [B],
+ *                 needed with history; at most history_stride) are the row's tokens, the first
+ *                 prompt_lens[b] (int32 [B]; NULL: 0) of them its prompt
+ *   repetition, frequency, presence  fp32 [B] (NULL: off)
+ *   bias_tokens   int32, bias_values fp32, cu_bias int32 [B+1] (needed with bias_tokens)
+ *   allowed       uint32 [num_allowed] rows of bits, allowed_stride words apart: bit v % 32 of
+ *                 word v / 32; allowed_rows int32 [N]: the row's mask (outside
+ *                 [0, num_allowed): none; NULL: mask n)
+ *   cu_rows       int32 [B+1]: history row b has the rows cu_rows[b] .. cu_rows[b+1]-1 of
+ *                 logits (rows behind cu_rows[B] are not touched); NULL: B = N, a row each
+ *   draft_tokens  int32 [N], tree_mask uint64 [N][mask_words] (both or neither, with cu_rows):
+ *                 the rows are nodes of drafted trees; the drafted tokens of the nodes in row
+ *                 n's mask are in its history, behind the prompt
+ * What is written must not share memory with another array (but in place as above).
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (N < 0, B < 0, V <= 0, a stride < V with N > 1,
+ *         history_stride < 0, allowed_stride < ceil(V / 32), num_allowed < 0, mask_words <= 0
+ *         with tree_mask, B != N without cu_rows); RA_ERR_UNSUPPORTED (an unknown
+ *         logits_dtype, V > 2^24, 2^31 or more workgroups, shared memory); RA_ERR_HIP.
+ *         N == 0 or B == 0 launch nothing.
+ */
+typedef struct {
+  const int32_t *history, *history_lens, *prompt_lens;
+  int64_t history_stride;
+  const float *repetition, *frequency, *presence;
+  const int32_t *bias_tokens;
+  const float *bias_values;
+  const int32_t *cu_bias;
+  const uint32_t *allowed;
+  const int32_t *allowed_rows;
+  int64_t allowed_stride;
+  int32_t num_allowed;
+  int32_t mask_words;
+  const int32_t *cu_rows;
+  const int32_t *draft_tokens;
+  const uint64_t *tree_mask;
+} ra_logits_adjust;
+int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
+                        int64_t row_stride, const ra_logits_adjust *adjust, int32_t B, void *out,
+                        int64_t out_stride, hipStream_t stream);
+
+/*
+ * Rows that share pages (Sec. 4: several rollouts of one task; rollout_attn_decode_shared_prefix
+ * reads such pages once for a group). shares[p] (int32 [num_pages], zeros to begin with) counts
+ * the rows that hold page p beyond the first; kv_block_table_extend's pages have none.
+ *
+ * kv_block_table_fork gives row dst_rows[i] the first lens[i] tokens of row src_rows[i]: its
+ * whole pages are shared (the same entries, one more share each), and where lens[i] is not a
+ * multiple of 16 the last page is one off the free list (in the order of the forks), to be
+ * filled by kv_page_copy in each layer:
+ *   copy_src[i], copy_dst[i] = the pages to copy between; -1, -1 where there is none
+ *   *taken = pages taken off the list
+ * dst_rows' earlier entries are overwritten, not released. All or nothing: if the list is too
+ * short, a row is outside [0, B), a length outside [0, bt_stride * 16], two forks go into one
+ * row, one goes into a row that another (or itself) comes from, or the list's count is out of
+ * range, *taken = -1, copy_src and copy_dst are -1 and nothing else changes.
+ * A shared page must not be written: append behind lens[i], and do not cut a row back into a
+ * page that it shares (whole pages may be released).
+ *
+ * kv_block_table_release_shared is kv_block_table_release for such rows: each entry it covers
+ * takes one holder off its page, and a page goes back on the free list when none is left (its
+ * last entry in the order of rows counts for its place). *released = pages put on the list, or
+ * -1 with nothing changed where kv_block_table_release would refuse for a length or the list's
+ * count. Entries that name no page are passed over.
+ *   workspace   at least kv_block_table_release_shared_workspace_size(B) bytes, 16-byte aligned
+ *
+ * kv_page_copy copies the pages src_pages[i] to dst_pages[i] (int32 [n]) of both pools, all KV
+ * heads, bit for bit; pairs with a page outside [0, num_pages) are passed over. No page may be
+ * the destination of two pairs, or of one and the source of another. The block table is
+ * not used and may be NULL.
+ *
+ * What is written must not share memory with another array. Calls on one free list must not
+ * overlap in time.
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (negative sizes, bt_stride <= 0, num_pages <= 0,
+ *         free_capacity < num_pages for the release); RA_ERR_UNSUPPORTED (B > 65535, n > 65535
+ *         for a fork, n * Hkv >= 2^31, B * bt_stride >= 2^30 for the release, bt_stride * 16 >
+ *         2^31 - 1, shared memory, pools not 16-byte aligned); RA_ERR_WORKSPACE; RA_ERR_HIP.
+ *         n == 0 forks set *taken = 0, B == 0 releases *released = 0; n == 0 copies launch
+ *         nothing.
+ */
+int kv_block_table_fork(const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens,
+                        int32_t n, int32_t *block_table, int32_t B, int32_t bt_stride,
+                        int32_t *shares, int32_t num_pages, const int32_t *free_pages,
+                        int32_t *free_count, int32_t free_capacity, int32_t *copy_src,
+                        int32_t *copy_dst, int32_t *taken, hipStream_t stream);
+size_t kv_block_table_release_shared_workspace_size(int32_t B);
+int kv_block_table_release_shared(const int32_t *lens, const int32_t *keep_lens,
+                                  const int32_t *block_table, int32_t B, int32_t bt_stride,
+                                  int32_t *shares, int32_t num_pages, int32_t *free_pages,
+                                  int32_t *free_count, int32_t free_capacity, int32_t *released,
+                                  void *workspace, size_t workspace_bytes, hipStream_t stream);
+int kv_page_copy(const ra_paged_kv *kv, const int32_t *src_pages, const int32_t *dst_pages,
+                 int32_t n, hipStream_t stream);
+
+/*
+ * Compaction: the kept tokens at a row's end move together, e.g. the accepted path of a drafted
+ * tree behind the context (src_index = path, counts = accepted, start_pos = ctx_lens).
+ * Token start_pos[b] + src_index[cu_src[b] + i] of row b moves to position start_pos[b] + i,
+ * for i in [0, counts[b]), keys and values of all KV heads, bit for bit (codes of fp8 pools).
+ * A row's indices must ascend strictly from 0 or more (so no token moves back); entries that
+ * are below their own i, or past the row's table, are passed over. Slots that no token moves
+ * to keep their contents. Rows of one call must not share the pages that they move in.
+ *
+ *   kv         pools written in place, block table read
+ *   start_pos  int32 [B];  cu_src  int32 [B+1];  src_index  int32 [total]
+ *   counts     int32 [B] or NULL (all of cu_src[b] .. cu_src[b+1]-1)
+ *   max_count  host: an upper bound of the tokens of a row
+ * Errors: RA_ERR_NULL; RA_ERR_SHAPE (negative sizes); RA_ERR_UNSUPPORTED (the page layout,
+ *         B > 65535, B * Hkv >= 2^31, pools not 16-byte aligned); RA_ERR_HIP. B == 0, total == 0
+ *         or max_count == 0 launch nothing.
+ */
+int kv_page_compact(const ra_paged_kv *kv, const int32_t *start_pos, const int32_t *cu_src,
+                    const int32_t *src_index, const int32_t *counts, int32_t B, int32_t total,
+                    int32_t max_count, hipStream_t stream);
+
+/*
  * Page write: append new tokens' keys and values to each trajectory's cache
  * (Sec. 3.3.3: the tokens of earlier turns are kept as they are and only the
  * new observation tokens are tokenised and added after them; Sec. 3.3.2: each

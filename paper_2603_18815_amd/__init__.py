@@ -39,6 +39,9 @@ __all__ = ["PagedKV", "decode", "decode_noalloc", "decode_shared_prefix", "appen
            "token_logprob_workspace_size", "token_logprob_pack_weight", "token_logprob_packed",
            "token_sample", "token_sample_workspace_size", "linear_decode", "linear_append",
            "linear_append_workspace_size", "block_table_extend", "block_table_release",
+           "draft_tree_mask", "draft_tree_accept", "decode_tree", "decode_tree_workspace_size",
+           "token_logits_adjust", "block_table_fork", "block_table_release_shared",
+           "block_table_release_shared_workspace_size", "kv_page_copy", "kv_page_compact",
            "abi_version", "RolloutAttnError"]
 
 
@@ -770,7 +773,7 @@ def linear_append(q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, cu_
     return out
 
 
-def _table_inputs(block_table, free_pages, free_count, rows, names):
+def _table_inputs(block_table, free_pages, free_count, rows, names, rows_of_table=True):
     """Checks the tensors of the block-table calls; returns (dev, B, bt_stride)."""
     dev = block_table.device
     _need(block_table, "block_table", torch.int32, dev)
@@ -784,7 +787,7 @@ def _table_inputs(block_table, free_pages, free_count, rows, names):
     for t, n in zip(rows, names):
         _need(t, n, torch.int32, dev)
         _shape(t, (B,), n)
-    if block_table.shape[0] < B:
+    if rows_of_table and block_table.shape[0] < B:
         raise ValueError(f"block_table has {block_table.shape[0]} rows, batch has {B}")
     return dev, B, block_table.shape[1]
 
@@ -856,3 +859,361 @@ def block_table_release(block_table: torch.Tensor, lens: torch.Tensor, keep_lens
         free_pages.data_ptr(), free_count.data_ptr(), free_pages.numel(), max_pages,
         released.data_ptr(), _stream(dev, stream)))
     return released
+
+
+def _nodes(cu_q: torch.Tensor, max_q_len: Optional[int]) -> int:
+    """Nodes of the largest tree, read from the device where they are not given."""
+    if max_q_len is not None:
+        return max_q_len
+    return int((cu_q[1:] - cu_q[:-1]).max().item()) if cu_q.shape[0] > 1 else 0
+
+
+def _out(t: Optional[torch.Tensor], name: str, shape, dtype: torch.dtype, dev, stream
+         ) -> torch.Tensor:
+    """The output given, checked, or a new one."""
+    if t is None:
+        t = _empty(shape, dtype, dev, stream)
+    _need(t, name, dtype, dev)
+    _shape(t, shape, name)
+    return t
+
+
+def _draft_inputs(cu_q, ctx_lens, nodes):
+    """Checks the tensors of the calls on drafted trees; returns (dev, B, total)."""
+    dev = cu_q.device
+    _need(cu_q, "cu_q", torch.int32, dev)
+    B = cu_q.shape[0] - 1
+    _shape(cu_q, (max(B, 0) + 1,), "cu_q")
+    if ctx_lens is not None:
+        _need(ctx_lens, "ctx_lens", torch.int32, dev)
+        _shape(ctx_lens, (B,), "ctx_lens")
+    total = nodes[0][0].shape[0]
+    for t, n in nodes:
+        _need(t, n, torch.int32, dev)
+        _shape(t, (total,), n)
+    return dev, B, total
+
+
+def draft_tree_mask(parents: torch.Tensor, cu_q: torch.Tensor,
+                    ctx_lens: Optional[torch.Tensor] = None, max_q_len: Optional[int] = None,
+                    tree_mask: Optional[torch.Tensor] = None,
+                    positions: Optional[torch.Tensor] = None, stream=None
+                    ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Masks and positions of drafted trees (row b's nodes packed at cu_q[b] .. cu_q[b+1]-1):
+    parents int32 [total] (a node's parent in its row, before it; -1: none) -> tree_mask int64
+    [total][words], bit j of word j / 64 for the node itself and its ancestors, and positions
+    int32 [total], ctx_lens[b] + the node's depth. words: those of the tree_mask given, or as
+    many as max_q_len nodes need."""
+    lib = _lib.load()
+    dev, B, total = _draft_inputs(cu_q, ctx_lens, ((parents, "parents"),))
+    max_q_len = _nodes(cu_q, max_q_len)
+    words = tree_mask.shape[1] if tree_mask is not None else max(1, (max_q_len + 63) // 64)
+    tree_mask = _out(tree_mask, "tree_mask", (total, words), torch.int64, dev, stream)
+    positions = _out(positions, "positions", (total,), torch.int32, dev, stream)
+    _lib.check("draft_tree_mask", lib.draft_tree_mask(
+        parents.data_ptr(), cu_q.data_ptr(), _ptr(ctx_lens), B, total, max_q_len, words,
+        tree_mask.data_ptr(), positions.data_ptr(), _stream(dev, stream)))
+    return tree_mask, positions
+
+
+def draft_tree_accept(parents: torch.Tensor, draft_tokens: torch.Tensor, chosen: torch.Tensor,
+                      cu_q: torch.Tensor, ctx_lens: torch.Tensor,
+                      max_q_len: Optional[int] = None, path: Optional[torch.Tensor] = None,
+                      tokens: Optional[torch.Tensor] = None,
+                      accepted: Optional[torch.Tensor] = None,
+                      kv_lens: Optional[torch.Tensor] = None,
+                      next_tokens: Optional[torch.Tensor] = None, stream=None
+                      ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor,
+                                 torch.Tensor]:
+    """The walk down each tree from its root, node 0, along the children that hold the token
+    chosen at their parent (int32 [total]; draft_tokens likewise).
+
+    Returns (path int32 [total]: row b's nodes on the walk from cu_q[b] on, then -1; tokens int32
+    [total]: the tokens chosen at them, which the step emits; accepted int32 [B]: how many;
+    kv_lens int32 [B]: ctx_lens + accepted; next_tokens int32 [B]: the last one, the next root).
+    """
+    lib = _lib.load()
+    dev, B, total = _draft_inputs(cu_q, ctx_lens, ((parents, "parents"),
+                                                   (draft_tokens, "draft_tokens"),
+                                                   (chosen, "chosen")))
+    max_q_len = _nodes(cu_q, max_q_len)
+    path = _out(path, "path", (total,), torch.int32, dev, stream)
+    tokens = _out(tokens, "tokens", (total,), torch.int32, dev, stream)
+    accepted = _out(accepted, "accepted", (B,), torch.int32, dev, stream)
+    kv_lens = _out(kv_lens, "kv_lens", (B,), torch.int32, dev, stream)
+    next_tokens = _out(next_tokens, "next_tokens", (B,), torch.int32, dev, stream)
+    _lib.check("draft_tree_accept", lib.draft_tree_accept(
+        parents.data_ptr(), draft_tokens.data_ptr(), chosen.data_ptr(), cu_q.data_ptr(),
+        ctx_lens.data_ptr(), B, total, max_q_len, path.data_ptr(), tokens.data_ptr(),
+        accepted.data_ptr(), kv_lens.data_ptr(), next_tokens.data_ptr(), _stream(dev, stream)))
+    return path, tokens, accepted, kv_lens, next_tokens
+
+
+def decode_tree_workspace_size(B: int, Hq: int, Hkv: int, total_q: int, max_q_len: int,
+                               max_kv_len: int) -> int:
+    return int(_lib.load().rollout_attn_decode_tree_workspace_size(B, Hq, Hkv, total_q, max_q_len,
+                                                                   max_kv_len))
+
+
+def decode_tree(q: torch.Tensor, cu_q: torch.Tensor, ctx_lens: torch.Tensor,
+                tree_mask: torch.Tensor, kv: PagedKV, max_q_len: Optional[int] = None,
+                max_kv_len: Optional[int] = None, scale: Optional[float] = None,
+                out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                want_lse: bool = False, workspace: Optional[torch.Tensor] = None, stream=None
+                ) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Attention of drafted trees: node i of row b (q bf16 [total_q][Hq][128], packed by cu_q;
+    its key and value in the pages at ctx_lens[b] + i) over the row's ctx_lens[b] cached tokens
+    and over the nodes j of its row whose bit is set in its tree_mask (int64 [total_q][words])
+    -> out fp32 [total_q][Hq][128] (, lse fp32 [total_q][Hq])."""
+    lib = _lib.load()
+    dev = kv.device
+    _need(q, "q", torch.bfloat16, dev)
+    _need(cu_q, "cu_q", torch.int32, dev)
+    _need(ctx_lens, "ctx_lens", torch.int32, dev)
+    _need(tree_mask, "tree_mask", torch.int64, dev)
+    total_q, Hq, D = q.shape
+    _shape(q, (total_q, Hq, HEAD_DIM), "q")
+    B = ctx_lens.shape[0]
+    _shape(ctx_lens, (B,), "ctx_lens")
+    _shape(cu_q, (B + 1,), "cu_q")
+    if tree_mask.dim() != 2:
+        raise ValueError(f"tree_mask must be [total_q][words], got {tuple(tree_mask.shape)}")
+    words = tree_mask.shape[1]
+    _shape(tree_mask, (total_q, words), "tree_mask")
+    _rows(kv, B)
+    max_q_len = _nodes(cu_q, max_q_len)
+    if max_kv_len is None:
+        max_kv_len = int((cu_q[1:] - cu_q[:-1] + ctx_lens).max().item()) if B else 0
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    out = _out(out, "out", (total_q, Hq, HEAD_DIM), torch.float32, dev, stream)
+    if lse is not None or want_lse:
+        lse = _out(lse, "lse", (total_q, Hq), torch.float32, dev, stream)
+    if workspace is None:
+        ws_bytes = lib.rollout_attn_decode_tree_workspace_size(B, Hq, kv.num_kv_heads, total_q,
+                                                               max_q_len, max_kv_len)
+        workspace = _empty(max(ws_bytes, 1), torch.uint8, dev, stream, scratch=True)
+    _need(workspace, "workspace", torch.uint8, dev)
+    s = kv.struct()
+    _lib.check("rollout_attn_decode_tree", lib.rollout_attn_decode_tree(
+        q.data_ptr(), cu_q.data_ptr(), ctx_lens.data_ptr(), tree_mask.data_ptr(), words,
+        ctypes.byref(s), B, Hq, total_q, max_q_len, max_kv_len, float(scale), out.data_ptr(),
+        _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream(dev, stream)))
+    return out, lse
+
+
+def _strided_rows(t: torch.Tensor, name: str, dev) -> int:
+    """Elements between the rows of a matrix whose rows are contiguous and do not overlap."""
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a GPU tensor, got one on {t.device}")
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}, got {t.device}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix, got {tuple(t.shape)}")
+    n, w = t.shape
+    stride = t.stride(0) if n > 1 else w
+    if (w > 1 and t.stride(1) != 1) or stride < w:
+        raise ValueError(f"{name} must have contiguous rows that do not overlap, got strides "
+                         f"{tuple(t.stride())}")
+    return stride
+
+
+def token_logits_adjust(logits: torch.Tensor, history: Optional[torch.Tensor] = None,
+                        history_lens: Optional[torch.Tensor] = None,
+                        prompt_lens: Optional[torch.Tensor] = None,
+                        repetition: Optional[torch.Tensor] = None,
+                        frequency: Optional[torch.Tensor] = None,
+                        presence: Optional[torch.Tensor] = None,
+                        bias_tokens: Optional[torch.Tensor] = None,
+                        bias_values: Optional[torch.Tensor] = None,
+                        cu_bias: Optional[torch.Tensor] = None,
+                        allowed: Optional[torch.Tensor] = None,
+                        allowed_rows: Optional[torch.Tensor] = None,
+                        cu_rows: Optional[torch.Tensor] = None,
+                        draft_tokens: Optional[torch.Tensor] = None,
+                        tree_mask: Optional[torch.Tensor] = None,
+                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Logits (bf16 or fp32 [N][V], rows any stride >= V apart) with penalties, biases and masks
+    applied, for token_sample; out=logits works in place.
+
+    history int32 [B][longest] with history_lens tokens a row, the first prompt_lens (None: 0) of
+    them the prompt: tokens in it are divided by (or, below 0, multiplied with) repetition,
+    those behind the prompt also lose frequency times their count, and presence (fp32 [B]).
+    bias_tokens int32 / bias_values fp32 packed by cu_bias int32 [B+1] are added (a token's last
+    entry). allowed int32 [M][>= ceil(V / 32)] holds masks of bits, allowed_rows int32 [N] a
+    row's mask (outside [0, M): none; None: mask n): tokens whose bit is clear become -inf.
+    Row n of the logits has history row n, or with cu_rows int32 [B+1] the b with cu_rows[b] <=
+    n < cu_rows[b+1]; draft_tokens int32 [N] and tree_mask int64 [N][words] then add the drafted
+    tokens of the nodes in row n's mask to its history.
+    """
+    lib = _lib.load()
+    dev = logits.device
+    bf16 = logits.dtype == torch.bfloat16
+    row_stride = _strided_rows(logits, "logits", dev)
+    if not bf16 and logits.dtype != torch.float32:
+        raise TypeError(f"logits must be torch.float32 or torch.bfloat16, got {logits.dtype}")
+    N, V = logits.shape
+    B = N if cu_rows is None else cu_rows.shape[0] - 1
+    a = _lib.RaLogitsAdjust()
+
+    def give(name, t, dtype, shape):
+        if t is not None:
+            _need(t, name, dtype, dev)
+            _shape(t, shape, name)
+            setattr(a, name, t.data_ptr())
+    if (history is None) != (history_lens is None):
+        raise ValueError("history and history_lens go together")
+    if history is not None:
+        a.history_stride = _strided_rows(history, "history", dev)
+        if history.dtype != torch.int32:
+            raise TypeError(f"history must be torch.int32, got {history.dtype}")
+        _shape(history, (B, history.shape[1]), "history")
+        if B <= 1:
+            a.history_stride = history.shape[1]
+        a.history = history.data_ptr()
+    give("history_lens", history_lens, torch.int32, (B,))
+    give("prompt_lens", prompt_lens, torch.int32, (B,))
+    give("repetition", repetition, torch.float32, (B,))
+    give("frequency", frequency, torch.float32, (B,))
+    give("presence", presence, torch.float32, (B,))
+    if bias_tokens is not None:
+        if bias_values is None or cu_bias is None:
+            raise ValueError("bias_tokens need bias_values and cu_bias")
+        give("bias_tokens", bias_tokens, torch.int32, (bias_tokens.numel(),))
+        give("bias_values", bias_values, torch.float32, (bias_tokens.numel(),))
+        give("cu_bias", cu_bias, torch.int32, (B + 1,))
+    elif bias_values is not None or cu_bias is not None:
+        raise ValueError("bias_values and cu_bias need bias_tokens")
+    if allowed is not None:
+        a.allowed_stride = _strided_rows(allowed, "allowed", dev)
+        if allowed.dtype != torch.int32:
+            raise TypeError(f"allowed must be torch.int32, got {allowed.dtype}")
+        a.num_allowed = allowed.shape[0]
+        if allowed.shape[1] * 32 < V:
+            raise ValueError(f"allowed has {allowed.shape[1]} words a row, {V} logits need "
+                             f"{(V + 31) // 32}")
+        a.allowed = allowed.data_ptr()
+    elif allowed_rows is not None:
+        raise ValueError("allowed_rows need allowed")
+    give("allowed_rows", allowed_rows, torch.int32, (N,))
+    give("cu_rows", cu_rows, torch.int32, (max(B, 0) + 1,))
+    if (draft_tokens is None) != (tree_mask is None):
+        raise ValueError("draft_tokens and tree_mask go together")
+    if draft_tokens is not None:
+        if cu_rows is None:
+            raise ValueError("draft_tokens need cu_rows")
+        give("draft_tokens", draft_tokens, torch.int32, (N,))
+        if tree_mask.dim() != 2:
+            raise ValueError(f"tree_mask must be [N][words], got {tuple(tree_mask.shape)}")
+        a.mask_words = tree_mask.shape[1]
+        give("tree_mask", tree_mask, torch.int64, (N, a.mask_words))
+    if out is None:
+        out = _empty((N, V), logits.dtype, dev, stream)
+    out_stride = _strided_rows(out, "out", dev)
+    if out.dtype != logits.dtype:
+        raise TypeError(f"out must be {logits.dtype}, got {out.dtype}")
+    _shape(out, (N, V), "out")
+    _lib.check("token_logits_adjust", lib.token_logits_adjust(
+        logits.data_ptr(), _lib.RA_LOGITS_BF16 if bf16 else _lib.RA_LOGITS_FP32, N, V, row_stride,
+        ctypes.byref(a), B, out.data_ptr(), out_stride, _stream(dev, stream)))
+    return out
+
+
+def block_table_fork(block_table: torch.Tensor, src_rows: torch.Tensor, dst_rows: torch.Tensor,
+                     lens: torch.Tensor, shares: torch.Tensor, free_pages: torch.Tensor,
+                     free_count: torch.Tensor, copy_src: Optional[torch.Tensor] = None,
+                     copy_dst: Optional[torch.Tensor] = None,
+                     taken: Optional[torch.Tensor] = None, stream=None
+                     ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gives row dst_rows[i] of the table the first lens[i] tokens of row src_rows[i] (int32
+    [n]): whole pages are shared (shares int32 [num_pages] counts a page's rows beyond the
+    first), a partly filled last one comes off the free list.
+
+    Returns (copy_src, copy_dst int32 [n]: the pages for kv_page_copy, -1 where there is none;
+    taken int32 [1]: pages taken, -1 if the call was refused as a whole)."""
+    lib = _lib.load()
+    dev, n, stride = _table_inputs(block_table, free_pages, free_count,
+                                   (src_rows, dst_rows, lens), ("src_rows", "dst_rows", "lens"),
+                                   rows_of_table=False)
+    _need(shares, "shares", torch.int32, dev)
+    _shape(shares, (shares.numel(),), "shares")
+    copy_src = _out(copy_src, "copy_src", (n,), torch.int32, dev, stream)
+    copy_dst = _out(copy_dst, "copy_dst", (n,), torch.int32, dev, stream)
+    taken = _out(taken, "taken", (1,), torch.int32, dev, stream)
+    _lib.check("kv_block_table_fork", lib.kv_block_table_fork(
+        src_rows.data_ptr(), dst_rows.data_ptr(), lens.data_ptr(), n, block_table.data_ptr(),
+        block_table.shape[0], stride, shares.data_ptr(), shares.numel(), free_pages.data_ptr(),
+        free_count.data_ptr(), free_pages.numel(), copy_src.data_ptr(), copy_dst.data_ptr(),
+        taken.data_ptr(), _stream(dev, stream)))
+    return copy_src, copy_dst, taken
+
+
+def block_table_release_shared_workspace_size(B: int) -> int:
+    return int(_lib.load().kv_block_table_release_shared_workspace_size(B))
+
+
+def block_table_release_shared(block_table: torch.Tensor, lens: torch.Tensor,
+                               keep_lens: torch.Tensor, shares: torch.Tensor,
+                               free_pages: torch.Tensor, free_count: torch.Tensor,
+                               released: Optional[torch.Tensor] = None,
+                               workspace: Optional[torch.Tensor] = None, stream=None
+                               ) -> torch.Tensor:
+    """block_table_release for rows that share pages: a page goes back on the free list (which
+    has room for all pages) when its last holder gives it up. Returns the pages put there
+    (int32 [1]), -1 if the call was refused as a whole."""
+    lib = _lib.load()
+    dev, B, stride = _table_inputs(block_table, free_pages, free_count, (lens, keep_lens),
+                                   ("lens", "keep_lens"))
+    _need(shares, "shares", torch.int32, dev)
+    _shape(shares, (shares.numel(),), "shares")
+    released = _out(released, "released", (1,), torch.int32, dev, stream)
+    if workspace is None:
+        size = lib.kv_block_table_release_shared_workspace_size(B)
+        workspace = _empty(max(size, 1), torch.uint8, dev, stream, scratch=True)
+    _need(workspace, "workspace", torch.uint8, dev)
+    _lib.check("kv_block_table_release_shared", lib.kv_block_table_release_shared(
+        lens.data_ptr(), keep_lens.data_ptr(), block_table.data_ptr(), B, stride,
+        shares.data_ptr(), shares.numel(), free_pages.data_ptr(), free_count.data_ptr(),
+        free_pages.numel(), released.data_ptr(), workspace.data_ptr(), workspace.numel(),
+        _stream(dev, stream)))
+    return released
+
+
+def kv_page_copy(kv: PagedKV, src_pages: torch.Tensor, dst_pages: torch.Tensor,
+                 stream=None) -> None:
+    """Copies pages src_pages[i] to dst_pages[i] (int32 [n]) of both pools; pairs that name no
+    page (-1) are passed over."""
+    lib = _lib.load()
+    dev = kv.device
+    n = src_pages.shape[0]
+    for t, name in ((src_pages, "src_pages"), (dst_pages, "dst_pages")):
+        _need(t, name, torch.int32, dev)
+        _shape(t, (n,), name)
+    s = kv.struct()
+    _lib.check("kv_page_copy", lib.kv_page_copy(
+        ctypes.byref(s), src_pages.data_ptr(), dst_pages.data_ptr(), n, _stream(dev, stream)))
+
+
+def kv_page_compact(kv: PagedKV, start_pos: torch.Tensor, cu_src: torch.Tensor,
+                    src_index: torch.Tensor, counts: Optional[torch.Tensor] = None,
+                    max_count: Optional[int] = None, stream=None) -> None:
+    """Moves row b's tokens start_pos[b] + src_index[cu_src[b] + i] to start_pos[b] + i, for i <
+    counts[b] (None: all of the row's entries); a row's indices ascend. The accepted path of a
+    tree: src_index = path, counts = accepted, cu_src = cu_q, start_pos = ctx_lens."""
+    lib = _lib.load()
+    dev = kv.device
+    B = start_pos.shape[0]
+    _need(start_pos, "start_pos", torch.int32, dev)
+    _shape(start_pos, (B,), "start_pos")
+    _need(cu_src, "cu_src", torch.int32, dev)
+    _shape(cu_src, (B + 1,), "cu_src")
+    _need(src_index, "src_index", torch.int32, dev)
+    _shape(src_index, (src_index.numel(),), "src_index")
+    _per_row(counts, "counts", torch.int32, B, dev)
+    _rows(kv, B)
+    if max_count is None:
+        max_count = src_index.numel()
+    s = kv.struct()
+    _lib.check("kv_page_compact", lib.kv_page_compact(
+        ctypes.byref(s), start_pos.data_ptr(), cu_src.data_ptr(), src_index.data_ptr(),
+        _ptr(counts), B, src_index.numel(), max_count, _stream(dev, stream)))

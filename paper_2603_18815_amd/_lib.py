@@ -19,6 +19,7 @@ RA_LOGITS_FP32 = 0
 RA_LOGITS_BF16 = 1
 
 RA_NOALLOC_SCRATCH_BYTES = 64 << 20
+RA_MAX_DRAFT_NODES = 1024
 
 EXPORTS = (
     "ra_abi_version",
@@ -49,6 +50,16 @@ EXPORTS = (
     "rollout_linear_attn_append",
     "kv_block_table_extend",
     "kv_block_table_release",
+    "draft_tree_mask",
+    "draft_tree_accept",
+    "rollout_attn_decode_tree_workspace_size",
+    "rollout_attn_decode_tree",
+    "token_logits_adjust",
+    "kv_block_table_fork",
+    "kv_block_table_release_shared_workspace_size",
+    "kv_block_table_release_shared",
+    "kv_page_copy",
+    "kv_page_compact",
 )
 
 
@@ -65,6 +76,29 @@ class RaPagedKV(ctypes.Structure):
         ("kv_dtype", ctypes.c_int32),
         ("k_scale", ctypes.c_float),
         ("v_scale", ctypes.c_float),
+    ]
+
+
+class RaLogitsAdjust(ctypes.Structure):
+    _fields_ = [
+        ("history", ctypes.c_void_p),
+        ("history_lens", ctypes.c_void_p),
+        ("prompt_lens", ctypes.c_void_p),
+        ("history_stride", ctypes.c_int64),
+        ("repetition", ctypes.c_void_p),
+        ("frequency", ctypes.c_void_p),
+        ("presence", ctypes.c_void_p),
+        ("bias_tokens", ctypes.c_void_p),
+        ("bias_values", ctypes.c_void_p),
+        ("cu_bias", ctypes.c_void_p),
+        ("allowed", ctypes.c_void_p),
+        ("allowed_rows", ctypes.c_void_p),
+        ("allowed_stride", ctypes.c_int64),
+        ("num_allowed", ctypes.c_int32),
+        ("mask_words", ctypes.c_int32),
+        ("cu_rows", ctypes.c_void_p),
+        ("draft_tokens", ctypes.c_void_p),
+        ("tree_mask", ctypes.c_void_p),
     ]
 
 
@@ -155,6 +189,30 @@ def load() -> ctypes.CDLL:
     lib.kv_block_table_extend.restype = ctypes.c_int
     lib.kv_block_table_release.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp]
     lib.kv_block_table_release.restype = ctypes.c_int
+    lib.draft_tree_mask.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]
+    lib.draft_tree_mask.restype = ctypes.c_int
+    lib.draft_tree_accept.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp, vp]
+    lib.draft_tree_accept.restype = ctypes.c_int
+    lib.rollout_attn_decode_tree_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32]
+    lib.rollout_attn_decode_tree_workspace_size.restype = sz
+    lib.rollout_attn_decode_tree.argtypes = [vp, vp, vp, vp, i32, kvp, i32, i32, i32, i32, i32, f32,
+                                             vp, vp, vp, sz, vp]
+    lib.rollout_attn_decode_tree.restype = ctypes.c_int
+    lib.token_logits_adjust.argtypes = [vp, i32, i32, i32, i64, ctypes.POINTER(RaLogitsAdjust), i32,
+                                        vp, i64, vp]
+    lib.token_logits_adjust.restype = ctypes.c_int
+    lib.kv_block_table_fork.argtypes = [vp, vp, vp, i32, vp, i32, i32, vp, i32, vp, vp, i32, vp, vp,
+                                        vp, vp]
+    lib.kv_block_table_fork.restype = ctypes.c_int
+    lib.kv_block_table_release_shared_workspace_size.argtypes = [i32]
+    lib.kv_block_table_release_shared_workspace_size.restype = sz
+    lib.kv_block_table_release_shared.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, vp, i32, vp,
+                                                  vp, sz, vp]
+    lib.kv_block_table_release_shared.restype = ctypes.c_int
+    lib.kv_page_copy.argtypes = [kvp, vp, vp, i32, vp]
+    lib.kv_page_copy.restype = ctypes.c_int
+    lib.kv_page_compact.argtypes = [kvp, vp, vp, vp, vp, i32, i32, i32, vp]
+    lib.kv_page_compact.restype = ctypes.c_int
     _lib = lib
     return lib
 

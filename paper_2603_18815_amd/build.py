@@ -17,7 +17,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librollout_attn.so")
 SOURCES = ["ra_api.hip", "ra_page.hip", "ra_decode.hip", "ra_persistent.hip",
-           "ra_logprob.hip", "ra_sample.hip", "ra_linear.hip", "ra_tables.hip"]
+           "ra_logprob.hip", "ra_sample.hip", "ra_linear.hip", "ra_tables.hip",
+           "ra_tree.hip", "ra_draft.hip", "ra_adjust.hip", "ra_fork.hip"]
 MICROBENCH_LIB = os.path.join(HERE, "libra_microbench.so")
 MICROBENCH_SOURCES = ["ra_microbench.hip"]
 ARCH = "gfx950"

@@ -12,6 +12,8 @@ namespace {
 
 constexpr int32_t kMaxGridYZ = 65535;
 
+static_assert(RA_MAX_DRAFT_NODES == ra::kMaxDraftNodes, "the kernels' arrays of a tree");
+
 bool valid_status(int s) { return s >= RA_OK && s <= RA_ERR_HIP; }
 
 bool valid_pool_scale(float s) { return std::isfinite(s) && s > 0.f && std::isfinite(1.0f / s); }
@@ -333,6 +335,13 @@ bool overlap(const Array (&arrays)[kN]) {
   return false;
 }
 
+// Sizes of the calls on drafted trees.
+int check_draft(int32_t B, int32_t total_q, int32_t max_q_len) {
+  if (B < 0 || total_q < 0 || max_q_len < 0) return RA_ERR_SHAPE;
+  if (B > kMaxGridYZ || max_q_len > RA_MAX_DRAFT_NODES) return RA_ERR_UNSUPPORTED;
+  return RA_OK;
+}
+
 // A rotary table must cover every position the call uses: [0, max_pos).
 int check_rope(const float *cos_sin, int32_t rope_rows, int32_t max_pos) {
   if (rope_rows <= 0 || max_pos > rope_rows) return RA_ERR_SHAPE;
@@ -592,6 +601,224 @@ int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
   return hip_status(ra::launch_table_release(lens, keep_lens, block_table, B, bt_stride,
                                              free_pages, free_count, free_capacity, max_pages,
                                              released, stream));
+}
+
+int draft_tree_mask(const int32_t *parents, const int32_t *cu_q, const int32_t *ctx_lens,
+                    int32_t B, int32_t total_q, int32_t max_q_len, int32_t mask_words,
+                    uint64_t *tree_mask, int32_t *positions, hipStream_t stream) {
+  const int s = check_draft(B, total_q, max_q_len);
+  if (s != RA_OK) return s;
+  if ((int64_t)mask_words * 64 < max_q_len) return RA_ERR_SHAPE;
+  if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
+  if (!parents || !cu_q || !tree_mask) return RA_ERR_NULL;
+  const int64_t rows = 4 * (int64_t)B, nodes = 4 * (int64_t)total_q;
+  if (overlap({{parents, nodes, false}, {cu_q, rows + 4, false}, {ctx_lens, rows, false},
+               {tree_mask, 2 * nodes * mask_words, true}, {positions, nodes, true}}))
+    return RA_ERR_UNSUPPORTED;
+  return hip_status(ra::launch_draft_mask(parents, cu_q, ctx_lens, B, total_q, max_q_len,
+                                          mask_words, tree_mask, positions, stream));
+}
+
+int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const int32_t *chosen,
+                      const int32_t *cu_q, const int32_t *ctx_lens, int32_t B, int32_t total_q,
+                      int32_t max_q_len, int32_t *path, int32_t *tokens, int32_t *accepted,
+                      int32_t *kv_lens, int32_t *next_tokens, hipStream_t stream) {
+  const int s = check_draft(B, total_q, max_q_len);
+  if (s != RA_OK) return s;
+  if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
+  if (!parents || !draft_tokens || !chosen || !cu_q || !ctx_lens || !path || !tokens ||
+      !accepted || !kv_lens || !next_tokens)
+    return RA_ERR_NULL;
+  const int64_t rows = 4 * (int64_t)B, nodes = 4 * (int64_t)total_q;
+  if (overlap({{parents, nodes, false}, {draft_tokens, nodes, false}, {chosen, nodes, false},
+               {cu_q, rows + 4, false}, {ctx_lens, rows, false}, {path, nodes, true},
+               {tokens, nodes, true}, {accepted, rows, true}, {kv_lens, rows, true},
+               {next_tokens, rows, true}}))
+    return RA_ERR_UNSUPPORTED;
+  return hip_status(ra::launch_draft_accept(parents, draft_tokens, chosen, cu_q, ctx_lens, B,
+                                            total_q, max_q_len, path, tokens, accepted, kv_lens,
+                                            next_tokens, stream));
+}
+
+size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
+                                               int32_t total_q, int32_t max_q_len,
+                                               int32_t max_kv_len) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || total_q <= 0 || max_q_len <= 0 ||
+      max_q_len > RA_MAX_DRAFT_NODES || max_kv_len <= 0)
+    return 0;
+  return ra::tree_workspace_bytes(total_q, Hq, ra::tree_plan(B, Hq, Hkv, max_q_len, max_kv_len));
+}
+
+int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *ctx_lens,
+                             const uint64_t *tree_mask, int32_t mask_words, const ra_paged_kv *kv,
+                             int32_t B, int32_t Hq, int32_t total_q, int32_t max_q_len,
+                             int32_t max_kv_len, float scale, float *out, float *lse,
+                             void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (Hq <= 0 || max_kv_len < 0 || !std::isfinite(scale)) return RA_ERR_SHAPE;
+  int s = check_draft(B, total_q, max_q_len);
+  if (s != RA_OK) return s;
+  if ((int64_t)mask_words * 64 < max_q_len) return RA_ERR_SHAPE;
+  if ((s = check_kv(kv)) != RA_OK) return s;
+  if (Hq % kv->num_kv_heads != 0 || !positions_fit(kv, max_kv_len)) return RA_ERR_SHAPE;
+  if (Hq / kv->num_kv_heads > 256) return RA_ERR_UNSUPPORTED;
+  if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
+  if (!q || !cu_q || !ctx_lens || !tree_mask || !out) return RA_ERR_NULL;
+  if (!aligned16(q) || !aligned16(out) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool))
+    return RA_ERR_UNSUPPORTED;
+  const ra::TreePlan plan = ra::tree_plan(B, Hq, kv->num_kv_heads, max_q_len, max_kv_len);
+  if (plan.groups > INT32_MAX) return RA_ERR_UNSUPPORTED;
+  const size_t need = ra::tree_workspace_bytes(total_q, Hq, plan);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
+  if (need > 0 && !aligned16(workspace)) return RA_ERR_UNSUPPORTED;
+  return hip_status(ra::launch_tree(static_cast<const uint16_t *>(q), cu_q, ctx_lens, tree_mask,
+                                    mask_words, to_internal(kv), B, Hq, total_q, max_q_len,
+                                    max_kv_len, scale, out, lse, workspace, plan, stream));
+}
+
+int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int32_t V,
+                        int64_t row_stride, const ra_logits_adjust *adjust, int32_t B, void *out,
+                        int64_t out_stride, hipStream_t stream) {
+  if (N < 0 || B < 0 || V <= 0 || (N > 1 && (row_stride < V || out_stride < V)))
+    return RA_ERR_SHAPE;
+  if (logits_dtype != RA_LOGITS_FP32 && logits_dtype != RA_LOGITS_BF16) return RA_ERR_UNSUPPORTED;
+  if (V > (1 << 24)) return RA_ERR_UNSUPPORTED;
+  if (!adjust) return RA_ERR_NULL;
+  const ra_logits_adjust &j = *adjust;
+  if (!j.cu_rows && B != N) return RA_ERR_SHAPE;
+  if ((j.history && j.history_stride < 0) || (j.tree_mask && j.mask_words <= 0) ||
+      (j.allowed && (j.num_allowed < 0 || j.allowed_stride < (V + 31) / 32)))
+    return RA_ERR_SHAPE;
+  if (N == 0 || B == 0) return RA_OK;
+  if (!logits || !out || (j.history && !j.history_lens) ||
+      (j.bias_tokens && (!j.bias_values || !j.cu_bias)) || !j.draft_tokens != !j.tree_mask ||
+      (j.draft_tokens && !j.cu_rows))
+    return RA_ERR_NULL;
+  if (ra::adjust_groups(N, V, j.cu_rows != nullptr) > INT32_MAX) return RA_ERR_UNSUPPORTED;
+  const bool bf16 = logits_dtype == RA_LOGITS_BF16;
+  const int64_t size = bf16 ? 2 : 4, rows = 4 * (int64_t)B, each = 4 * (int64_t)N;
+  const bool in_place = out == logits && (N == 1 || out_stride == row_stride);
+  const int64_t bits = j.allowed && j.num_allowed > 0
+                           ? 4 * ((j.num_allowed - 1) * j.allowed_stride + (V + 31) / 32) : 0;
+  const int64_t written = ((N - 1) * out_stride + V) * size;
+  if (overlap({{out, written, true},
+               {in_place ? nullptr : logits, ((N - 1) * row_stride + V) * size, false},
+               {j.history, 4 * B * j.history_stride, false}, {j.history_lens, rows, false},
+               {j.prompt_lens, rows, false}, {j.repetition, rows, false},
+               {j.frequency, rows, false}, {j.presence, rows, false},
+               {j.cu_bias, rows + 4, false}, {j.allowed, bits, false},
+               {j.allowed_rows, each, false}, {j.cu_rows, rows + 4, false},
+               {j.draft_tokens, each, false}, {j.tree_mask, 2 * each * j.mask_words, false}}))
+    return RA_ERR_UNSUPPORTED;
+  ra::AdjustArgs a;
+  a.logits = logits;
+  a.out = out;
+  a.row_stride = row_stride;
+  a.out_stride = out_stride;
+  a.N = N;
+  a.V = V;
+  a.B = B;
+  a.history = j.history;
+  a.history_lens = j.history_lens;
+  a.prompt_lens = j.prompt_lens;
+  a.history_stride = j.history_stride;
+  a.repetition = j.repetition;
+  a.frequency = j.frequency;
+  a.presence = j.presence;
+  a.bias_tokens = j.bias_tokens;
+  a.cu_bias = j.cu_bias;
+  a.bias_values = j.bias_values;
+  a.allowed = j.allowed;
+  a.allowed_rows = j.allowed_rows;
+  a.allowed_stride = j.allowed_stride;
+  a.num_allowed = j.num_allowed;
+  a.mask_words = j.mask_words;
+  a.cu_rows = j.cu_rows;
+  a.draft_tokens = j.draft_tokens;
+  a.tree_mask = j.tree_mask;
+  return hip_status(ra::launch_adjust(a, bf16, stream));
+}
+
+int kv_block_table_fork(const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens,
+                        int32_t n, int32_t *block_table, int32_t B, int32_t bt_stride,
+                        int32_t *shares, int32_t num_pages, const int32_t *free_pages,
+                        int32_t *free_count, int32_t free_capacity, int32_t *copy_src,
+                        int32_t *copy_dst, int32_t *taken, hipStream_t stream) {
+  if (n < 0 || num_pages <= 0) return RA_ERR_SHAPE;
+  const int s = check_table(B, bt_stride, free_capacity);
+  if (s != RA_OK) return s;
+  if (n > kMaxGridYZ) return RA_ERR_UNSUPPORTED;
+  if (!shares || !free_count || !taken || (free_capacity > 0 && !free_pages)) return RA_ERR_NULL;
+  if (n > 0 && (!src_rows || !dst_rows || !lens || !copy_src || !copy_dst)) return RA_ERR_NULL;
+  if (n > 0 && B > 0 && !block_table) return RA_ERR_NULL;
+  const int64_t each = 4 * (int64_t)n;
+  if (overlap({{src_rows, each, false}, {dst_rows, each, false}, {lens, each, false},
+               {block_table, 4 * (int64_t)B * bt_stride, true},
+               {shares, 4 * (int64_t)num_pages, true},
+               {free_pages, 4 * (int64_t)free_capacity, false}, {free_count, 4, true},
+               {copy_src, each, true}, {copy_dst, each, true}, {taken, 4, true}}))
+    return RA_ERR_UNSUPPORTED;
+  return hip_status(ra::launch_table_fork(src_rows, dst_rows, lens, n, block_table, B, bt_stride,
+                                          shares, num_pages, free_pages, free_count,
+                                          free_capacity, copy_src, copy_dst, taken, stream));
+}
+
+size_t kv_block_table_release_shared_workspace_size(int32_t B) {
+  return B < 0 ? 0 : ra::table_release_shared_bytes(B);
+}
+
+int kv_block_table_release_shared(const int32_t *lens, const int32_t *keep_lens,
+                                  const int32_t *block_table, int32_t B, int32_t bt_stride,
+                                  int32_t *shares, int32_t num_pages, int32_t *free_pages,
+                                  int32_t *free_count, int32_t free_capacity, int32_t *released,
+                                  void *workspace, size_t workspace_bytes, hipStream_t stream) {
+  const int s = check_table(B, bt_stride, free_capacity);
+  if (s != RA_OK) return s;
+  if (num_pages <= 0 || free_capacity < num_pages) return RA_ERR_SHAPE;
+  if ((int64_t)B * bt_stride >= (1 << 30)) return RA_ERR_UNSUPPORTED;
+  if (!shares || !free_pages || !free_count || !released) return RA_ERR_NULL;
+  if (B > 0 && (!lens || !keep_lens || !block_table)) return RA_ERR_NULL;
+  const size_t need = ra::table_release_shared_bytes(B);
+  if (!workspace || !aligned16(workspace) || workspace_bytes < need) return RA_ERR_WORKSPACE;
+  const int64_t rows = 4 * (int64_t)B;
+  if (overlap({{lens, rows, false}, {keep_lens, rows, false}, {block_table, rows * bt_stride, false},
+               {shares, 4 * (int64_t)num_pages, true},
+               {free_pages, 4 * (int64_t)free_capacity, true}, {free_count, 4, true},
+               {released, 4, true}, {workspace, (int64_t)need, true}}))
+    return RA_ERR_UNSUPPORTED;
+  return hip_status(ra::launch_table_release_shared(lens, keep_lens, block_table, B, bt_stride,
+                                                    shares, num_pages, free_pages, free_count,
+                                                    free_capacity, released, workspace, stream));
+}
+
+int kv_page_copy(const ra_paged_kv *kv, const int32_t *src_pages, const int32_t *dst_pages,
+                 int32_t n, hipStream_t stream) {
+  if (n < 0) return RA_ERR_SHAPE;
+  if (!kv) return RA_ERR_NULL;
+  ra_paged_kv pools = *kv;   // the table is not used
+  if (!pools.block_table) pools.block_table = static_cast<const int32_t *>(pools.k_pool);
+  const int s = check_kv(&pools);
+  if (s != RA_OK) return s;
+  if (n == 0) return RA_OK;
+  if (!src_pages || !dst_pages) return RA_ERR_NULL;
+  if ((int64_t)n * kv->num_kv_heads > INT32_MAX || !aligned16(kv->k_pool) ||
+      !aligned16(kv->v_pool))
+    return RA_ERR_UNSUPPORTED;
+  return hip_status(ra::launch_page_copy(to_internal(&pools), src_pages, dst_pages, n, stream));
+}
+
+int kv_page_compact(const ra_paged_kv *kv, const int32_t *start_pos, const int32_t *cu_src,
+                    const int32_t *src_index, const int32_t *counts, int32_t B, int32_t total,
+                    int32_t max_count, hipStream_t stream) {
+  if (B < 0 || total < 0 || max_count < 0) return RA_ERR_SHAPE;
+  const int s = check_kv(kv);
+  if (s != RA_OK) return s;
+  if (B > kMaxGridYZ || (int64_t)B * kv->num_kv_heads > INT32_MAX || !aligned16(kv->k_pool) ||
+      !aligned16(kv->v_pool))
+    return RA_ERR_UNSUPPORTED;
+  if (B == 0 || total == 0 || max_count == 0) return RA_OK;
+  if (!start_pos || !cu_src || !src_index) return RA_ERR_NULL;
+  return hip_status(ra::launch_page_compact(to_internal(kv), start_pos, cu_src, src_index, counts,
+                                            B, total, max_count, stream));
 }
 
 int kv_page_write(const void *k_new, const void *v_new, const int32_t *cu_new,

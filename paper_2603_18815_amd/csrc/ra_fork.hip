@@ -1,0 +1,353 @@
+// Rows that share pages: kv_block_table_fork gives a row the pages of another row's tokens,
+// kv_page_copy copies the last, partly filled page that they cannot share, and
+// kv_block_table_release_shared gives pages back once no row is left that holds them.
+// kv_page_compact moves the kept tokens of a row's end together.
+//
+// shares[p] counts the rows that hold page p beyond the first. A release takes one off for
+// every table entry it covers; a page is free if that leaves less than none. Which entry of
+// such a page counts must not depend on the order of atomics: the last one in the order of rows
+// and entries does, found by an atomic minimum of codes that fall as the entry's place rises
+// and lie below what any count can reach.
+#include "ra_device.h"
+#include "ra_internal.h"
+#include "ra_wave.h"
+
+namespace ra {
+namespace {
+
+constexpr int kForkThreads = 256;
+constexpr int kMaxRows = 65536;            // rows a block table can have
+constexpr int kCode = 1 << 30;             // codes of entries: -(kCode + 1 + place), place < kCode
+
+__device__ __forceinline__ bool page_ok(int id, int num_pages) { return (unsigned)id < (unsigned)num_pages; }
+
+// A workgroup a fork. Every workgroup looks at all forks: whether the call holds decides what
+// each does, and the forks before it say which page is its own. Bound by latency and, for long
+// prompts, by the atomics on the shared pages' counts.
+__global__ __launch_bounds__(kForkThreads) void fork_kernel(
+    const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens, int32_t n,
+    int32_t *block_table, int32_t B, int32_t bt_stride, int32_t *shares, int32_t num_pages,
+    const int32_t *free_pages, int32_t *free_count, int32_t capacity, int32_t *copy_src,
+    int32_t *copy_dst, int32_t *taken) {
+  __shared__ uint32_t is_dst[kMaxRows / 32];
+  __shared__ int bad, need, before;
+  const int tid = threadIdx.x, me = blockIdx.x;
+  for (int i = tid; i < (B + 31) / 32; i += kForkThreads) is_dst[i] = 0;
+  if (tid == 0) bad = need = before = 0;
+  __syncthreads();
+  const int64_t limit = (int64_t)bt_stride * kPage;
+  for (int i = tid; i < n; i += kForkThreads) {
+    const int s = src_rows[i], d = dst_rows[i], len = lens[i];
+    if (s < 0 || s >= B || d < 0 || d >= B || len < 0 || len > limit) {
+      bad = 1;
+      continue;
+    }
+    const uint32_t bit = 1u << (d & 31);
+    if (atomicOr(&is_dst[d >> 5], bit) & bit) bad = 1;   // two forks into one row
+    if (len % kPage) {
+      atomicAdd(&need, 1);
+      if (i < me) atomicAdd(&before, 1);
+    }
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += kForkThreads) {          // a row forked from is not forked into
+    const int s = src_rows[i];
+    if (s >= 0 && s < B && (is_dst[s >> 5] >> (s & 31) & 1)) bad = 1;
+  }
+  __syncthreads();
+  const int count = *free_count;
+  const bool ok = !bad && count >= 0 && count <= capacity && need <= count;
+  if (me < n) {
+    int from = -1, to = -1;
+    if (ok) {
+      const int64_t src = (int64_t)src_rows[me] * bt_stride, dst = (int64_t)dst_rows[me] * bt_stride;
+      const int len = lens[me], full = len / kPage;
+      for (int j = tid; j < full; j += kForkThreads) {
+        const int page = block_table[src + j];
+        block_table[dst + j] = page;
+        if (page_ok(page, num_pages)) atomicAdd(&shares[page], 1);
+      }
+      if (tid == 0 && len % kPage) {
+        from = block_table[src + full];
+        to = free_pages[count - 1 - before];
+        block_table[dst + full] = to;
+      }
+    }
+    if (tid == 0) {
+      copy_src[me] = from;
+      copy_dst[me] = to;
+    }
+  }
+  if (me == 0 && tid == 0) {
+    *taken = ok ? need : -1;
+    if (gridDim.x == 1 && ok) *free_count = count - need;
+  }
+}
+
+// The free list's new length, behind a launch of several workgroups.
+__global__ void fork_count_kernel(int32_t *free_count, const int32_t *taken) {
+  if (*taken > 0) *free_count -= *taken;
+}
+
+constexpr int kRowThreads = 256;
+
+// What a release keeps in its workspace: whether it goes ahead, the free list's length before
+// it, and the pages that each row frees.
+struct SharedRelease {
+  const int32_t *lens, *keep_lens, *block_table;
+  int32_t B, bt_stride, num_pages, capacity;
+  int32_t *shares, *free_pages, *free_count, *released;
+  int32_t *head;      // [2]: goes ahead, length
+  int32_t *freed;     // [B]
+};
+
+__device__ __forceinline__ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
+
+// Takes an owner off every entry that is given up.
+__global__ __launch_bounds__(kRowThreads) void shared_sub_kernel(SharedRelease r) {
+  __shared__ int bad;
+  const int tid = threadIdx.x, b = blockIdx.x;
+  if (tid == 0) bad = 0;
+  __syncthreads();
+  const int64_t limit = (int64_t)r.bt_stride * kPage;
+  for (int i = tid; i < r.B; i += kRowThreads) {
+    const int64_t len = r.lens[i], keep = r.keep_lens[i];
+    if (keep < 0 || keep > len || len > limit) bad = 1;
+  }
+  __syncthreads();
+  const int count = *r.free_count;
+  const bool ok = !bad && count >= 0 && count <= r.capacity;
+  if (b == 0 && tid == 0) {
+    r.head[0] = ok;
+    r.head[1] = count;
+    if (!ok || r.B == 0) *r.released = ok ? 0 : -1;
+  }
+  if (!ok || b >= r.B) return;
+  const int32_t *row = r.block_table + (int64_t)b * r.bt_stride;
+  const int end = (int)pages_of(r.lens[b]);
+  for (int j = (int)pages_of(r.keep_lens[b]) + tid; j < end; j += kRowThreads) {
+    const int page = row[j];
+    if (page_ok(page, r.num_pages)) atomicSub(&r.shares[page], 1);
+  }
+}
+
+// Names the last entry of every page that nobody holds any more.
+__global__ __launch_bounds__(kRowThreads) void shared_last_kernel(SharedRelease r) {
+  if (!r.head[0]) return;
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const int32_t *row = r.block_table + (int64_t)b * r.bt_stride;
+  const int end = (int)pages_of(r.lens[b]);
+  for (int j = (int)pages_of(r.keep_lens[b]) + tid; j < end; j += kRowThreads) {
+    const int page = row[j];
+    if (page_ok(page, r.num_pages) && r.shares[page] < 0)
+      atomicMin(&r.shares[page], -(kCode + 1) - (b * r.bt_stride + j));
+  }
+}
+
+__device__ __forceinline__ bool frees(const SharedRelease &r, int b, int j, int &page) {
+  page = r.block_table[(int64_t)b * r.bt_stride + j];
+  return page_ok(page, r.num_pages) && r.shares[page] == -(kCode + 1) - (b * r.bt_stride + j);
+}
+
+// How many pages each row frees.
+__global__ __launch_bounds__(kRowThreads) void shared_count_kernel(SharedRelease r) {
+  __shared__ int sum;
+  if (!r.head[0]) return;
+  const int tid = threadIdx.x, b = blockIdx.x;
+  if (tid == 0) sum = 0;
+  __syncthreads();
+  const int end = (int)pages_of(r.lens[b]);
+  int mine = 0, page;
+  for (int j = (int)pages_of(r.keep_lens[b]) + tid; j < end; j += kRowThreads)
+    mine += frees(r, b, j, page);
+  if (mine) atomicAdd(&sum, mine);
+  __syncthreads();
+  if (tid == 0) r.freed[b] = sum;
+}
+
+// Puts them on the list: entry rank of the freed ones, in the order of rows and entries, goes
+// to place count + all - 1 - rank, as kv_block_table_release does with every entry.
+__global__ __launch_bounds__(kRowThreads) void shared_put_kernel(SharedRelease r) {
+  __shared__ int all, before, wave_sum[kRowThreads / kWave];
+  if (!r.head[0]) return;
+  const int tid = threadIdx.x, b = blockIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  if (tid == 0) all = before = 0;
+  __syncthreads();
+  int a = 0, f = 0;
+  for (int i = tid; i < r.B; i += kRowThreads) {
+    const int n = r.freed[i];
+    a += n;
+    if (i < b) f += n;
+  }
+  if (a) atomicAdd(&all, a);
+  if (f) atomicAdd(&before, f);
+  __syncthreads();
+  const int count = r.head[1];
+  if (b == 0 && tid == 0) {
+    *r.released = all;
+    *r.free_count = min(count + all, r.capacity);
+  }
+  const int first = (int)pages_of(r.keep_lens[b]), end = (int)pages_of(r.lens[b]);
+  int rank = before;
+  for (int j0 = first; j0 < end; j0 += kRowThreads) {
+    const int j = j0 + tid;
+    int page = 0;
+    const bool mine = j < end && frees(r, b, j, page);
+    const uint64_t votes = __ballot(mine);
+    if (lane == 0) wave_sum[wave] = (int)__popcll(votes);
+    __syncthreads();
+    int at = rank + (int)__popcll(votes & ((1ull << lane) - 1));
+    int step = 0;
+    for (int w = 0; w < kRowThreads / kWave; ++w) {
+      if (w < wave) at += wave_sum[w];
+      step += wave_sum[w];
+    }
+    if (mine) {
+      const int64_t to = (int64_t)count + all - 1 - at;
+      if (to < r.capacity) r.free_pages[to] = page;
+      r.shares[page] = 0;   // (no other entry's code, so none is found free again)
+    }
+    rank += step;
+    __syncthreads();
+  }
+}
+
+// ---- pages' contents ----
+constexpr int kCopyThreads = 256;
+
+// One page of one KV head a workgroup, 16 bytes a thread and pool. Bound by HBM.
+template <bool kFp8>
+__global__ __launch_bounds__(kCopyThreads) void page_copy_kernel(uint8_t *k_pool, uint8_t *v_pool,
+                                                                 const int32_t *src,
+                                                                 const int32_t *dst, int32_t hkv,
+                                                                 int32_t num_pages) {
+  constexpr int kBytes = kPage * kHeadDim * (kFp8 ? 1 : 2);
+  const int i = blockIdx.x / hkv, g = blockIdx.x - i * hkv;
+  const int from = src[i], to = dst[i];
+  if (!page_ok(from, num_pages) || !page_ok(to, num_pages) || from == to) return;
+  const size_t at = threadIdx.x * 16;
+  if (at >= kBytes) return;
+  const size_t f = ((size_t)from * hkv + g) * kBytes + at, t = ((size_t)to * hkv + g) * kBytes + at;
+  const u32x4 k = *reinterpret_cast<const u32x4 *>(k_pool + f);
+  const u32x4 v = *reinterpret_cast<const u32x4 *>(v_pool + f);
+  *reinterpret_cast<u32x4 *>(k_pool + t) = k;
+  *reinterpret_cast<u32x4 *>(v_pool + t) = v;
+}
+
+constexpr int kMoveTokens = 32;            // moved together through LDS
+constexpr int kMoveThreads = 256;
+
+// The kept tokens of one row and KV head. Indices rise, so a token never moves behind where it
+// was and the tokens of one step lie before the sources of all later ones: a step reads all
+// its tokens into LDS before it writes any.
+template <typename E>
+__global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
+    E *k_pool, E *v_pool, const int32_t *block_table, int32_t bt_stride, int32_t num_pages,
+    int32_t hkv, const int32_t *start_pos, const int32_t *cu_src, const int32_t *src_index,
+    const int32_t *counts, int32_t total, int32_t max_count) {
+  __shared__ E sk[kMoveTokens][kHeadDim], sv[kMoveTokens][kHeadDim];
+  __shared__ int64_t from[kMoveTokens], to[kMoveTokens];   // page * 16 + slot; -1: stays
+  const int b = blockIdx.x / hkv, g = blockIdx.x - b * hkv, tid = threadIdx.x;
+  const int first = min(max(cu_src[b], 0), total);
+  int n = min(min(max(cu_src[b + 1] - first, 0), total - first), max_count);
+  if (counts) n = min(n, max(counts[b], 0));
+  const int64_t start = max(start_pos[b], 0), limit = (int64_t)bt_stride * kPage;
+  const int32_t *bt = block_table + (int64_t)b * bt_stride;
+  for (int i0 = 0; i0 < n; i0 += kMoveTokens) {
+    __syncthreads();
+    const int m = min(kMoveTokens, n - i0);
+    if (tid < m) {
+      const int i = i0 + tid, j = src_index[first + i];
+      int64_t f = -1, t = -1;
+      if (j > i && start + j < limit) {
+        const int64_t p = start + j, q = start + i;
+        f = (int64_t)clamp_page(bt[p / kPage], num_pages) * kPage + p % kPage;
+        t = (int64_t)clamp_page(bt[q / kPage], num_pages) * kPage + q % kPage;
+      }
+      from[tid] = f;
+      to[tid] = t;
+    }
+    __syncthreads();
+    for (int x = tid; x < m * kHeadDim; x += kMoveThreads) {
+      const int k = x / kHeadDim, d = x % kHeadDim;
+      if (from[k] < 0) continue;
+      const size_t block = ((size_t)(from[k] / kPage) * hkv + g) * kPage * kHeadDim;
+      const int slot = (int)(from[k] % kPage);
+      sk[k][d] = k_pool[block + slot * kHeadDim + d];
+      sv[k][d] = v_pool[block + d * kPage + slot];
+    }
+    __syncthreads();
+    for (int x = tid; x < m * kHeadDim; x += kMoveThreads) {
+      const int k = x / kHeadDim, d = x % kHeadDim;
+      if (to[k] < 0) continue;
+      const size_t block = ((size_t)(to[k] / kPage) * hkv + g) * kPage * kHeadDim;
+      const int slot = (int)(to[k] % kPage);
+      k_pool[block + slot * kHeadDim + d] = sk[k][d];
+      v_pool[block + d * kPage + slot] = sv[k][d];
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_table_fork(const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens,
+                             int32_t n, int32_t *block_table, int32_t B, int32_t bt_stride,
+                             int32_t *shares, int32_t num_pages, const int32_t *free_pages,
+                             int32_t *free_count, int32_t capacity, int32_t *copy_src,
+                             int32_t *copy_dst, int32_t *taken, hipStream_t stream) {
+  fork_kernel<<<n > 0 ? n : 1, kForkThreads, 0, stream>>>(
+      src_rows, dst_rows, lens, n, block_table, B, bt_stride, shares, num_pages, free_pages,
+      free_count, capacity, copy_src, copy_dst, taken);
+  if (n > 1) fork_count_kernel<<<1, 1, 0, stream>>>(free_count, taken);
+  return hipGetLastError();
+}
+
+size_t table_release_shared_bytes(int32_t B) { return ((size_t)B + 2) * sizeof(int32_t); }
+
+hipError_t launch_table_release_shared(const int32_t *lens, const int32_t *keep_lens,
+                                       const int32_t *block_table, int32_t B, int32_t bt_stride,
+                                       int32_t *shares, int32_t num_pages, int32_t *free_pages,
+                                       int32_t *free_count, int32_t capacity, int32_t *released,
+                                       void *workspace, hipStream_t stream) {
+  int32_t *head = static_cast<int32_t *>(workspace);
+  const SharedRelease r = {lens, keep_lens, block_table, B, bt_stride, num_pages, capacity,
+                           shares, free_pages, free_count, released, head, head + 2};
+  shared_sub_kernel<<<B > 0 ? B : 1, kRowThreads, 0, stream>>>(r);
+  if (B > 0) {
+    shared_last_kernel<<<B, kRowThreads, 0, stream>>>(r);
+    shared_count_kernel<<<B, kRowThreads, 0, stream>>>(r);
+    shared_put_kernel<<<B, kRowThreads, 0, stream>>>(r);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_page_copy(const PagedKV &kv, const int32_t *src_pages, const int32_t *dst_pages,
+                            int32_t n, hipStream_t stream) {
+  uint8_t *k = reinterpret_cast<uint8_t *>(kv.k_pool), *v = reinterpret_cast<uint8_t *>(kv.v_pool);
+  const unsigned grid = (unsigned)n * (unsigned)kv.hkv;
+  if (kv.fp8)
+    page_copy_kernel<true><<<grid, kCopyThreads, 0, stream>>>(k, v, src_pages, dst_pages, kv.hkv,
+                                                             kv.num_pages);
+  else
+    page_copy_kernel<false><<<grid, kCopyThreads, 0, stream>>>(k, v, src_pages, dst_pages, kv.hkv,
+                                                              kv.num_pages);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_compact(const PagedKV &kv, const int32_t *start_pos, const int32_t *cu_src,
+                               const int32_t *src_index, const int32_t *counts, int32_t B,
+                               int32_t total, int32_t max_count, hipStream_t stream) {
+  const unsigned grid = (unsigned)B * (unsigned)kv.hkv;
+  if (kv.fp8)
+    page_compact_kernel<uint8_t><<<grid, kMoveThreads, 0, stream>>>(
+        reinterpret_cast<uint8_t *>(kv.k_pool), reinterpret_cast<uint8_t *>(kv.v_pool),
+        kv.block_table, kv.bt_stride, kv.num_pages, kv.hkv, start_pos, cu_src, src_index, counts,
+        total, max_count);
+  else
+    page_compact_kernel<uint16_t><<<grid, kMoveThreads, 0, stream>>>(
+        kv.k_pool, kv.v_pool, kv.block_table, kv.bt_stride, kv.num_pages, kv.hkv, start_pos,
+        cu_src, src_index, counts, total, max_count);
+  return hipGetLastError();
+}
+
+}  // namespace ra

@@ -134,6 +134,71 @@ hipError_t launch_table_release(const int32_t *lens, const int32_t *keep_lens,
                                 int32_t *free_pages, int32_t *free_count, int32_t capacity,
                                 int32_t max_pages, int32_t *released, hipStream_t stream);
 
+// ---- trees of drafted tokens ----
+constexpr int32_t kMaxDraftNodes = 1024;       // nodes of a tree
+struct TreePlan {
+  bool wide;              // 32 query rows a workgroup, else 16
+  int64_t tiles;          // of the query rows of the largest tree, a KV head
+  int32_t split_tokens;   // keys a split
+  int32_t slots;          // splits of the longest row
+  int64_t groups;         // workgroups
+};
+TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len);
+size_t tree_workspace_bytes(int32_t total_q, int32_t hq, const TreePlan &p);
+hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ctx_lens,
+                       const uint64_t *mask, int32_t words, const PagedKV &kv, int32_t B,
+                       int32_t hq, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
+                       float scale, float *out, float *lse, void *workspace, const TreePlan &p,
+                       hipStream_t stream);
+hipError_t launch_draft_mask(const int32_t *parents, const int32_t *cu_q, const int32_t *ctx_lens,
+                             int32_t B, int32_t total_q, int32_t max_q_len, int32_t words,
+                             uint64_t *tree_mask, int32_t *positions, hipStream_t stream);
+hipError_t launch_draft_accept(const int32_t *parents, const int32_t *draft_tokens,
+                               const int32_t *chosen, const int32_t *cu_q,
+                               const int32_t *ctx_lens, int32_t B, int32_t total_q,
+                               int32_t max_q_len, int32_t *path, int32_t *tokens,
+                               int32_t *accepted, int32_t *kv_lens, int32_t *next_tokens,
+                               hipStream_t stream);
+
+// ---- logits before a token is drawn ----
+struct AdjustArgs {
+  const void *logits;
+  void *out;
+  int64_t row_stride, out_stride;
+  int32_t N, V, B;
+  const int32_t *history, *history_lens, *prompt_lens;
+  int64_t history_stride;
+  const float *repetition, *frequency, *presence;
+  const int32_t *bias_tokens, *cu_bias;
+  const float *bias_values;
+  const uint32_t *allowed;
+  const int32_t *allowed_rows;
+  int64_t allowed_stride;
+  int32_t num_allowed, mask_words;
+  const int32_t *cu_rows, *draft_tokens;
+  const uint64_t *tree_mask;
+};
+int64_t adjust_groups(int32_t N, int32_t V, bool trees);   // workgroups
+hipError_t launch_adjust(const AdjustArgs &a, bool bf16, hipStream_t stream);
+
+// ---- rows that share pages ----
+hipError_t launch_table_fork(const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens,
+                             int32_t n, int32_t *block_table, int32_t B, int32_t bt_stride,
+                             int32_t *shares, int32_t num_pages, const int32_t *free_pages,
+                             int32_t *free_count, int32_t capacity, int32_t *copy_src,
+                             int32_t *copy_dst, int32_t *taken, hipStream_t stream);
+size_t table_release_shared_bytes(int32_t B);
+hipError_t launch_table_release_shared(const int32_t *lens, const int32_t *keep_lens,
+                                       const int32_t *block_table, int32_t B, int32_t bt_stride,
+                                       int32_t *shares, int32_t num_pages, int32_t *free_pages,
+                                       int32_t *free_count, int32_t capacity, int32_t *released,
+                                       void *workspace, hipStream_t stream);
+hipError_t launch_page_copy(const PagedKV &kv, const int32_t *src_pages, const int32_t *dst_pages,
+                            int32_t n, hipStream_t stream);
+hipError_t launch_page_compact(const PagedKV &kv, const int32_t *start_pos, const int32_t *cu_src,
+                               const int32_t *src_index, const int32_t *counts, int32_t B,
+                               int32_t total, int32_t max_count, hipStream_t stream);
+
 // ---- page write / gather ----
 hipError_t launch_page_write(const uint16_t *k_new, const uint16_t *v_new, const int32_t *cu_new,
                              const int32_t *start_pos, const PagedKV &kv, int32_t B,

@@ -1,0 +1,172 @@
+"""Attention of drafted trees against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18815_amd as ra
+from tests.draft_util import (DEV, SCALE, Cache, ancestors, assert_within, cu, i32, pack,
+                              random_tree, tree_reference)
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(seed, Hq, Hkv, ctx, T, fp8=False, kind="tree", words=None, stride=None):
+    rng = np.random.default_rng(seed)
+    cache = Cache(seed, [c + t for c, t in zip(ctx, T)], Hkv, fp8, stride=stride)
+    if kind == "tree":
+        masks = [ancestors(random_tree(rng, t)) for t in T]
+    elif kind == "random":                     # any bits, rows of none among them
+        masks = [rng.random((t, t)) < rng.choice([0.0, 0.3, 1.0], (t, 1)) for t in T]
+    else:
+        masks = [np.zeros((t, t), bool) for t in T]
+    need = max(1, -(-max(T, default=0) // 64))
+    g = torch.Generator(device=DEV).manual_seed(seed + 1)
+    q = torch.randn((sum(T), Hq, 128), generator=g, device=DEV).bfloat16()
+    bits = pack(masks, words or need)
+    return cache, q, masks, torch.as_tensor(bits, device=DEV)
+
+
+def run(cache, q, mask, ctx, T, max_q=None, max_kv=None, pad=2, **kw):
+    """The call on outputs with rows behind the last one, which have to stay."""
+    total, Hq, _ = q.shape
+    max_q = max(T) if max_q is None else max_q
+    max_kv = max(c + t for c, t in zip(ctx, T)) if max_kv is None else max_kv
+    qp = torch.cat([q, torch.full((pad, Hq, 128), float("nan"), device=DEV).bfloat16()])
+    mp = torch.cat([mask, torch.full((pad, mask.shape[1]), -1, device=DEV)])
+    out = torch.full((total + pad, Hq, 128), 7.5, device=DEV)
+    lse = torch.full((total + pad, Hq), 7.5, device=DEV)
+    ra.decode_tree(qp, i32(cu(T)), i32(ctx), mp, cache.kv(), max_q, max_kv, out=out, lse=lse, **kw)
+    assert bool((out[total:] == 7.5).all()) and bool((lse[total:] == 7.5).all())
+    return out[:total], lse[:total]
+
+
+def check(cache, q, masks, mask, ctx, T, scale=SCALE, **kw):
+    out, lse = run(cache, q, mask, ctx, T, scale=scale, **kw)
+    want, want_lse, tol, ltol = tree_reference(q, T, ctx, masks, cache, scale)
+    assert_within(lse, want_lse, ltol, "lse")
+    assert_within(out, want, tol, "out")
+    return out, lse
+
+
+HEADS = [(8, 2), (16, 1), (4, 4), (64, 2), (5, 1), (24, 8), (256, 1)]
+LENS = {
+    "single": ([0], [1]),
+    "ragged": ([0, 1, 15, 16, 17, 300, 0, 40], [1, 2, 17, 16, 0, 33, 5, 64]),
+    "split": ([1500, 0, 2047, 511, 512], [3, 20, 1, 1, 9]),
+    "wide": ([100, 700], [150, 65]),
+}
+
+
+@pytest.mark.parametrize("lens", LENS)
+@pytest.mark.parametrize("Hq,Hkv", HEADS)
+@pytest.mark.parametrize("fp8", [False, True])
+def test_trees(device, Hq, Hkv, lens, fp8):
+    ctx, T = LENS[lens]
+    print(f"[gpu-test] trees Hq={Hq} Hkv={Hkv} {lens} fp8={fp8}", flush=True)
+    check(*(lambda c, q, m, b: (c, q, m, b, ctx, T))(*inputs(5, Hq, Hkv, ctx, T, fp8)))
+
+
+@pytest.mark.parametrize("kind", ["random", "none"])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (32, 1)])
+def test_masks_that_leave_nodes_without_keys(device, Hq, Hkv, kind):
+    ctx, T = [0, 0, 20, 0, 513], [1, 40, 7, 0, 70]
+    cache, q, masks, bits = inputs(6, Hq, Hkv, ctx, T, kind=kind)
+    out, lse = check(cache, q, masks, bits, ctx, T)
+    if kind == "none":
+        assert bool((out[:41] == 0).all()) and bool((lse[:41] == float("-inf")).all())
+
+
+@pytest.mark.parametrize("scale", [SCALE, -0.2, 0.0, 3.0])
+def test_scales(device, scale):
+    ctx, T = [33, 600], [9, 40]
+    check(*(lambda c, q, m, b: (c, q, m, b, ctx, T))(*inputs(7, 8, 2, ctx, T)), scale=scale)
+
+
+def test_more_mask_words_and_bits_past_the_nodes(device):
+    """Words that no node needs, and set bits at and past T, change nothing."""
+    ctx, T = [10, 530, 3], [5, 33, 64]
+    cache, q, masks, bits = inputs(8, 8, 2, ctx, T, words=3)
+    a = run(cache, q, bits, ctx, T)
+    past = pack([np.tile(np.arange(192) >= n, (n, 1)) for n in T], 3)
+    noisy = bits | torch.as_tensor(past, device=DEV)
+    b = run(cache, q, noisy, ctx, T)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    c = run(cache, q, bits[:, :1].contiguous(), ctx, T)
+    assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 2), (64, 2)])
+def test_infinite_and_nan_nodes_reach_only_those_that_see_them(device, bad, Hq, Hkv):
+    ctx, T = [70, 5, 1030], [30, 64, 12]
+    cache, q, masks, bits = inputs(9, Hq, Hkv, ctx, T)
+    clean = check(cache, q, masks, bits, ctx, T)
+    for b, node in ((0, 7), (1, 33), (2, 3)):
+        page, slot = cache.place(b, ctx[b] + node)
+        cache.k[page, 0, slot, 5] = bad
+        cache.v[page, 1, 9, slot] = bad
+    out, lse = run(cache, q, bits, ctx, T)
+    touched = np.concatenate([masks[b][:, n] for b, n in ((0, 7), (1, 33), (2, 3))])
+    free = torch.as_tensor(~touched, device=DEV)
+    assert torch.equal(out[free], clean[0][free]) and torch.equal(lse[free], clean[1][free])
+    met = torch.as_tensor(touched, device=DEV)
+    G = Hq // Hkv
+    assert not bool(torch.isfinite(out[met][:, G:, 9]).any())        # the value's own dimension
+    assert bool(torch.isfinite(out[met][:, G:, 8]).all())
+    if bad != bad:
+        assert bool(torch.isnan(out[met][:, :G]).all())              # the key's heads
+
+
+def test_one_node_is_decode_and_a_chain_is_append(device):
+    Hq, Hkv, ctx = 16, 4, [0, 31, 700, 2000]
+    cache, q, _, _ = inputs(10, Hq, Hkv, ctx, [1] * 4)
+    one = torch.ones((4, 1), dtype=torch.int64, device=DEV)
+    out, lse = run(cache, q, one, ctx, [1] * 4)
+    ref, ref_lse = ra.decode(q, cache.kv(), i32([c + 1 for c in ctx]), want_lse=True)
+    # each is off by half the sum of the tolerances at most
+    _, _, tol, ltol = tree_reference(q, [1] * 4, ctx, [np.ones((1, 1), bool)] * 4, cache)
+    assert_within(out, ref.double(), 2 * tol, "out")
+    assert_within(lse, ref_lse.double(), 2 * ltol, "lse")
+    T = [5, 40, 3, 100]
+    cache, q, _, _ = inputs(11, Hq, Hkv, ctx, T)
+    chain = [np.tril(np.ones((t, t), bool)) for t in T]
+    out, lse = check(cache, q, chain, torch.as_tensor(pack(chain, 2), device=DEV), ctx, T)
+
+
+def test_shorter_bounds_and_unused_rows(device):
+    """Bounds above the lengths, and rows of the table that no row uses."""
+    ctx, T = [40, 0, 300], [6, 2, 11]
+    cache, q, masks, bits = inputs(12, 8, 2, ctx, T, stride=80)
+    a = check(cache, q, masks, bits, ctx, T, max_q=64, max_kv=80 * 16)
+    b = run(cache, q, bits, ctx, T, max_q=64, max_kv=80 * 16)
+    assert torch.equal(a[0], b[0])
+
+
+def test_largest_tree(device):
+    ctx, T = [77], [1024]
+    check(*(lambda c, q, m, b: (c, q, m, b, ctx, T))(*inputs(13, 4, 2, ctx, T)))
+
+
+def test_no_lse_and_allocated_outputs(device):
+    ctx, T = [900, 4], [8, 3]
+    cache, q, masks, bits = inputs(14, 8, 2, ctx, T)
+    a, _ = run(cache, q, bits, ctx, T)
+    b, none = ra.decode_tree(q, i32(cu(T)), i32(ctx), bits, cache.kv())
+    assert none is None and torch.equal(a, b)
+    c, lse = ra.decode_tree(q, i32(cu(T)), i32(ctx), bits, cache.kv(), want_lse=True)
+    assert torch.equal(a, c) and lse.shape == (11, 8)
+
+
+def test_exact_workspace_and_its_refusal(device):
+    ctx, T = [1400, 30], [8, 3]
+    cache, q, masks, bits = inputs(15, 8, 2, ctx, T)
+    need = ra.decode_tree_workspace_size(2, 8, 2, 13, 8, 1408)
+    assert need > 0
+    ws = torch.full((need + 16,), 0xff, dtype=torch.uint8, device=DEV)
+    a = run(cache, q, bits, ctx, T, workspace=ws[:need])
+    assert bool((ws[need:] == 0xff).all())
+    b = run(cache, q, bits, ctx, T)
+    assert torch.equal(a[0], b[0])
+    with pytest.raises(ra.RolloutAttnError) as e:
+        run(cache, q, bits, ctx, T, workspace=ws[:need - 4])
+    assert e.value.status == ra._lib.RA_ERR_WORKSPACE
