@@ -137,7 +137,7 @@ hipError_t launch_table_release(const int32_t *lens, const int32_t *keep_lens,
 // ---- trees of drafted tokens ----
 constexpr int32_t kMaxDraftNodes = 1024;       // nodes of a tree
 struct TreePlan {
-  bool wide;              // 32 query rows a workgroup, else 16
+  int32_t rows;           // query rows a workgroup takes: 16, 32 or 256
   int64_t tiles;          // of the query rows of the largest tree, a KV head
   int32_t split_tokens;   // keys a split
   int32_t slots;          // splits of the longest row
