@@ -666,7 +666,7 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
   if (!aligned16(q) || !aligned16(out) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool))
     return RA_ERR_UNSUPPORTED;
   const ra::TreePlan plan = ra::tree_plan(B, Hq, kv->num_kv_heads, max_q_len, max_kv_len);
-  if (plan.groups > INT32_MAX) return RA_ERR_UNSUPPORTED;
+  if (plan.groups > INT32_MAX || (int64_t)total_q * Hq > INT32_MAX) return RA_ERR_UNSUPPORTED;
   const size_t need = ra::tree_workspace_bytes(total_q, Hq, plan);
   if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
   if (need > 0 && !aligned16(workspace)) return RA_ERR_UNSUPPORTED;

@@ -7,6 +7,7 @@
 // splits, whose partial results a second launch joins.
 #include "ra_device.h"
 #include "ra_internal.h"
+#include "ra_lds.h"
 
 namespace ra {
 namespace {
@@ -44,6 +45,18 @@ __device__ __forceinline__ TreeRow tree_row(const TreeArgs &a, int b) {
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
          ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
+// Which of the 32 keys from position pos on node `mask` sees: those of the context, and the
+// nodes below T that its mask names.
+__device__ __forceinline__ uint32_t seen_keys(const uint64_t *mask, int pos, int ctx, int T) {
+  const int j0 = pos - ctx, j = max(j0, 0);
+  uint64_t bits = mask[min(j, T - 1) >> 6] >> (j & 63);
+  if ((j & 63) > 32 && ((j + 31) >> 6) <= (T - 1) >> 6) bits |= mask[(j >> 6) + 1] << (64 - (j & 63));
+  const int nodes = T - j;                   // bits of nodes that there are
+  uint32_t w = nodes >= 32 ? (uint32_t)bits : nodes <= 0 ? 0u : (uint32_t)bits & ((1u << nodes) - 1);
+  if (j0 < 0) w = j0 <= -32 ? ~0u : (w << -j0) | ((1u << -j0) - 1);
+  return w;
 }
 
 // The lower n (0, 1, or 2 and more) of a pair of bf16 values.
@@ -127,38 +140,98 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
   }
   uint32_t odd = 0;                         // infinite or NaN values of nodes
   const size_t head_stride = (size_t)kPage * kHeadDim;
-  for (int pr = wave; pr < npairs; pr += kSplitWaves) {
-    const int tok = t0 + pr * kPair, pg = tok / kPage;
+  // A pair's keys are loaded while the pair before meets its values, its values while it meets
+  // its own keys.
+  size_t kbase = 0, vbase = 0;
+  auto pages = [&](int pr) __attribute__((always_inline)) {
+    const int pg = (t0 + pr * kPair) / kPage;
     const int id0 = clamp_page(bt[pg], a.num_pages);
     const int id1 = pg + 1 < row_pages ? clamp_page(bt[pg + 1], a.num_pages) : id0;
-    const size_t kbase = ((size_t)(ka_sel ? id1 : id0) * a.hkv + g) * head_stride;
-    const size_t vbase = ((size_t)(sv_sel ? id1 : id0) * a.hkv + g) * head_stride;
-    bf16x8 ka[2][4], va[8];
+    kbase = ((size_t)(ka_sel ? id1 : id0) * a.hkv + g) * head_stride;
+    vbase = ((size_t)(sv_sel ? id1 : id0) * a.hkv + g) * head_stride;
+  };
+  constexpr int kRaw = kFp8 ? 4 : 8;
+  u32x4 kraw[kRaw];
+  u32x4 vraw[kFp8 ? 4 : 8];
+  auto load_k = [&]() __attribute__((always_inline)) {
     if constexpr (kFp8) {
       const uint8_t *kb = reinterpret_cast<const uint8_t *>(a.k_pool) + kbase;
-      const uint8_t *vb = reinterpret_cast<const uint8_t *>(a.v_pool) + vbase;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const u32x4 w = *reinterpret_cast<const u32x4 *>(kb + (ka_slot + 4 * t) * kHeadDim +
-                                                           64 * h + 16 * kgrp);
-          ka[t][2 * h] = fp8x8_to_bf16x8(u32x2{w[0], w[1]});
-          ka[t][2 * h + 1] = fp8x8_to_bf16x8(u32x2{w[2], w[3]});
-        }
-#pragma unroll
-      for (int mt = 0; mt < 8; ++mt)
-        va[mt] = fp8x8_to_bf16x8(
-            *reinterpret_cast<const u32x2 *>(vb + (16 * mt + col) * kPage + sv_slot));
+        for (int h = 0; h < 2; ++h)
+          kraw[2 * t + h] = *reinterpret_cast<const u32x4 *>(kb + (ka_slot + 4 * t) * kHeadDim +
+                                                             64 * h + 16 * kgrp);
     } else {
-      const uint16_t *kb = a.k_pool + kbase, *vb = a.v_pool + vbase;
+      const uint16_t *kb = a.k_pool + kbase;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
-          ka[t][kk] = load_bf16x8(kb + (ka_slot + 4 * t) * kHeadDim + 32 * kk + 8 * kgrp);
+          kraw[4 * t + kk] = load_u32x4(kb + (ka_slot + 4 * t) * kHeadDim + 32 * kk + 8 * kgrp);
+    }
+  };
+  // (values are read once, in whole lines: marked so that they do not displace the keys' lines,
+  // of which two loads take a half each)
+  auto load_v = [&]() __attribute__((always_inline)) {
+    if constexpr (kFp8) {
+      // whole 16-slot rows: lane l loads row 16 (2 j + l / 16 % 2) + col of its page
+      const uint8_t *vb = reinterpret_cast<const uint8_t *>(a.v_pool) + vbase;
 #pragma unroll
-      for (int mt = 0; mt < 8; ++mt) va[mt] = load_bf16x8(vb + (16 * mt + col) * kPage + sv_slot);
+      for (int j = 0; j < 4; ++j)
+        vraw[j] = load_stream_u32x4(vb + (16 * (2 * j + (kgrp & 1)) + col) * kPage);
+    } else {
+      const uint16_t *vb = a.v_pool + vbase;
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) vraw[mt] = load_stream_u32x4(vb + (16 * mt + col) * kPage + sv_slot);
+    }
+  };
+  if (wave < npairs) {
+    pages(wave);
+    load_k();
+    load_v();
+  }
+  for (int pr = wave; pr < npairs; pr += kSplitWaves) {
+    const int tok = t0 + pr * kPair;
+    const bool more = pr + kSplitWaves < npairs;
+    bf16x8 ka[2][4], va[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if constexpr (kFp8) {
+          ka[t][2 * h] = fp8x8_to_bf16x8(u32x2{kraw[2 * t + h][0], kraw[2 * t + h][1]});
+          ka[t][2 * h + 1] = fp8x8_to_bf16x8(u32x2{kraw[2 * t + h][2], kraw[2 * t + h][3]});
+        } else {
+          ka[t][2 * h] = __builtin_bit_cast(bf16x8, kraw[4 * t + 2 * h]);
+          ka[t][2 * h + 1] = __builtin_bit_cast(bf16x8, kraw[4 * t + 2 * h + 1]);
+        }
+    f32x4 st[kTiles][2];
+#pragma unroll
+    for (int nt = 0; nt < kTiles; ++nt)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        st[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) st[nt][t] = mfma16x16x32(ka[t][kk], qop[nt][kk], st[nt][t]);
+      }
+    if (more) {
+      pages(pr + kSplitWaves);
+      load_k();
+    }
+    if constexpr (kFp8) {
+      // lanes l and l ^ 16 hold rows 2 j and 2 j + 1 of one page: exchanged, each has the slots
+      // that it supplies of both
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const auto s0 = __builtin_amdgcn_permlane16_swap(vraw[j][0], vraw[j][2], false, false);
+        const auto s1 = __builtin_amdgcn_permlane16_swap(vraw[j][1], vraw[j][3], false, false);
+        va[2 * j] = fp8x8_to_bf16x8(u32x2{s0[0], s1[0]});
+        va[2 * j + 1] = fp8x8_to_bf16x8(u32x2{s0[1], s1[1]});
+      }
+    } else {
+#pragma unroll
+      for (int mt = 0; mt < 8; ++mt) va[mt] = __builtin_bit_cast(bf16x8, vraw[mt]);
     }
     // Pairs that reach past the context: keys at or past the row's end are not attended (their
     // values replaced by zeros), the nodes' keys by those whose masks name them.
@@ -181,25 +254,15 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
     }
 #pragma unroll
     for (int nt = 0; nt < kTiles; ++nt) {
-      f32x4 st[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        st[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk) st[t] = mfma16x16x32(ka[t][kk], qop[nt][kk], st[t]);
-      }
       float sc[8];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) sc[4 * t + r] = st[t][r] * a.scale_log2;
+        for (int r = 0; r < 4; ++r) sc[4 * t + r] = st[nt][t][r] * a.scale_log2;
       if (tail) {
+        const uint32_t sees = seen_keys(mask[nt], tok, row.ctx, row.T) >> (first - tok);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = first + e - row.ctx;
-          const bool sees = j < 0 || (first + e < t1 && (mask[nt][j >> 6] >> (j & 63) & 1));
-          sc[e] = sees ? sc[e] : -INFINITY;
-        }
+        for (int e = 0; e < 8; ++e) sc[e] = sees >> e & 1 ? sc[e] : -INFINITY;
       }
       float mx = sc[0];
 #pragma unroll
@@ -226,6 +289,7 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
         o[nt][mt] = mfma16x16x32(va[mt], p_lo, o[nt][mt]);
       }
     }
+    if (more) load_v();
   }
 
   // join the waves
@@ -277,45 +341,43 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
 
 // ---- wide tiles ----
 // 256 query rows of one KV head, by eight waves of 32 rows each: the columns of 32 x 32 matrix
-// tiles, their queries in registers. Blocks of 128 keys are loaded into registers one block
-// ahead and stored to one of two LDS buffers, one barrier a block:
+// tiles, their queries in registers. Blocks of 64 keys are loaded straight into a ring of four
+// LDS buffers, three blocks ahead, one barrier a block:
 //   S^T[key][row] = K[key][:] . Q^T[:][row]       (8 products of 32 x 32 x 16 for 32 keys)
 //   O^T[d][row]  += V^T[d][key] . P^T[key][row]   (8, twice: the weights' two bf16 parts)
 // Keys are ordered inside a pair of pages so that the 16 scores of a lane are the weights it
-// supplies to the second product. Tiles with fewer live rows split the pairs of a block over
-// the waves that have none of their own, and join them at the end. The running maximum moves
+// supplies to the second product. Tiles with fewer live rows split the pairs of keys over the
+// waves that have none of their own, and join them at the end. The running maximum moves
 // only when a score passes it by 8 (in powers of two), so that O is rescaled rarely; weights
 // are at most 2^8 then.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kWideWaves = 8, kWideThreads = kWideWaves * kWave;
 constexpr int kWideRows = 32 * kWideWaves;
-constexpr int kWideKeys = 128, kWidePages = kWideKeys / kPage, kWidePairs = kWideKeys / kPair;
-constexpr int kWKPitch = kHeadDim + 8;                    // of a key's row in LDS (elements)
-constexpr int kWKElems = kWideKeys * kWKPitch, kWVElems = kWideKeys * kHeadDim;
+constexpr int kWideKeys = 64, kWidePages = kWideKeys / kPage, kWidePairs = kWideKeys / kPair;
+constexpr int kRing = 4;
+constexpr int kPageElems = kPage * kHeadDim;
+constexpr int kMaxSplit = 8192;                 // keys of a split
 constexpr float kSlack = 8.f;
 
 struct WideLds {
   union {
-    struct {
-      __attribute__((aligned(16))) uint16_t k[2][kWKElems];
-      __attribute__((aligned(16))) uint16_t v[2][kWVElems];
-    } in;
+    __attribute__((aligned(16))) uint16_t in[kRing][2 * kWidePages][kPageElems];   // K, then V
     __attribute__((aligned(16))) float o[kWideWaves][32][kOPitch];
   };
   float m[kWideWaves][32], l[kWideWaves][32];
+  int32_t page[kMaxSplit / kPage + kWidePages];   // of the split's keys, clamped
 };
 static_assert(sizeof(WideLds) <= 160 * 1024, "LDS of a compute unit");
 
+// LDS places. Unit c (16 bytes) of key `slot` of a page is at 16 slot + (c ^ slot), half h of value
+// row d at 2 d + (h ^ bit 3 of d): 16 lanes that read together meet no bank twice. Codes (fp8): 8
+// units a key, unit c at 8 slot + (c ^ slot / 2), one unit a value row.
+__device__ __forceinline__ u32x4 read_lds(uint32_t at) {
+  return *(const __attribute__((address_space(3))) u32x4 *)(uintptr_t)at;
+}
+
 __device__ __forceinline__ f32x16 mfma32x32x16(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ bf16x8 lds_bf16x8(const uint16_t *p) {
-  return __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p));
-}
-// The two 8-slot halves of V row d change places where bit 3 of d is set: rows 8 apart would
-// meet in the same banks.
-__device__ __forceinline__ int wide_v(int page, int d, int half) {
-  return (page * kHeadDim + d) * kPage + ((half ^ ((d >> 3) & 1)) * 8);
 }
 // Of the two lanes of a column.
 __device__ __forceinline__ float pair_max(float x) {
@@ -326,7 +388,7 @@ __device__ __forceinline__ float pair_max(float x) {
 
 template <bool kFp8>
 __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
-  __shared__ WideLds lds;
+  __shared__ __attribute__((aligned(1024))) WideLds lds;
   int id = blockIdx.x;
   const int g = id % a.hkv;
   id /= a.hkv;
@@ -344,90 +406,58 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
   const int nblocks = (t1 - t0 + kWideKeys - 1) / kWideKeys;
   const int row_pages = (t1 + kPage - 1) / kPage;
   const int32_t *bt = a.block_table + (size_t)b * a.bt_stride;
-  const size_t head_stride = (size_t)kPage * kHeadDim;
 
-  // which rows and which pairs of a block are this wave's
-  const int parts = (rows + 31) / 32;
-  const int lanes_log = parts <= 1 ? 0 : parts <= 2 ? 1 : parts <= 4 ? 2 : 3;
-  const int share = wave >> lanes_log, shares = min(kWideWaves >> lanes_log, kWidePairs);
-  const int part = wave & ((1 << lanes_log) - 1);
-  const bool live = part < parts && share < shares;
+  // Which rows and which pairs of a block are this wave's: 8 / parts waves share a part, or one
+  // more; the parts with fewer have the first waves, which do more and lie on different SIMDs.
+  const int parts = (rows + 31) / 32, base = kWideWaves / parts, extra = kWideWaves % parts;
+  const int few = parts - extra, heavy = few * base;
+  const bool first_waves = wave < heavy;
+  const int part = first_waves ? extra + wave % few : (wave - heavy) % extra;
+  const int share = first_waves ? wave / few : (wave - heavy) / extra;
+  const int shares = first_waves ? base : base + 1;
 
   const int r = r0 + min(32 * part + col, rows - 1), node = r / G;
   const size_t t = row.first + node;
   const uint64_t *mask = a.mask + t * a.words;
-  bf16x8 q[8];
+  bf16x8 q[8];                                  // dims 16 kk + 8 grp .. (fp8: see read_k)
   {
-    const uint16_t *qrow = a.q + (t * a.hq + (size_t)g * G + (r - node * G)) * kHeadDim + 8 * grp;
+    const uint16_t *qrow = a.q + (t * a.hq + (size_t)g * G + (r - node * G)) * kHeadDim;
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) q[kk] = load_bf16x8(qrow + 16 * kk);
+    for (int kk = 0; kk < 8; ++kk)
+      q[kk] = load_bf16x8(qrow + (kFp8 ? 32 * (kk >> 1) + 16 * grp + 8 * (kk & 1) : 16 * kk + 8 * grp));
+    // arrived before the loads to LDS begin: a wait for them later would wait for those too
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(q[kk]));
   }
+  // ---- loads: a wave the keys or the values of one page of the block, 1 KB an instruction,
+  // each lane the unit that belongs to its place in LDS
+  constexpr int kLoads = kFp8 ? 2 : 4;
+  const int my_page = wave >> 1, is_v = wave & 1;
+  // the unit in the i-th KB at this lane's place: of values the same in each, of keys xor 4 i
+  const uint32_t unit = is_v ? (kFp8 ? lane : lane ^ (lane >> 4 & 1)) : lane ^ (lane >> 4);
+  const uint32_t turn = is_v ? 0 : 64;
+  const uint16_t *pool = is_v ? a.v_pool : a.k_pool;
+  const uint32_t ring = lds_address(lds.in[0][0]);
+  constexpr uint32_t kPageBytes = 2 * kPageElems, kBlockBytes = 2 * kWidePages * kPageBytes;
+  // (page ids by way of LDS: a load of them between those to LDS would wait for these)
+  for (int i = tid; i < nblocks * kWidePages; i += kWideThreads)
+    lds.page[i] = clamp_page(bt[min(t0 / kPage + i, row_pages - 1)], a.num_pages);
+  __syncthreads();
+  int next_id = lds.page[my_page];
+  auto load = [&](int blk) __attribute__((always_inline)) {
+    const size_t at = ((size_t)__builtin_amdgcn_readfirstlane(next_id) * a.hkv + g) * kPageElems;
+    const uint16_t *base = pool + (kFp8 ? at / 2 : at);
+    const uint32_t to = __builtin_amdgcn_readfirstlane(
+        ring + blk % kRing * kBlockBytes + (is_v * kWidePages + my_page) * kPageBytes);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) load_to_lds(base, (16 * unit ^ turn * i) + 1024 * i, to + i * 1024);
+    next_id = lds.page[(blk + 1) * kWidePages + my_page];
+  };
+#pragma unroll
+  for (int i = 0; i < kRing - 1; ++i)
+    if (i < nblocks) load(i);
 
   uint32_t odd = 0;                             // infinite or NaN values of nodes
-
-  // ---- staging: a wave a page of the block, 16 bytes a lane and load
-  u32x4 kreg[4], vreg[4];
-  auto page_id = [&](int blk) {
-    const int pg = t0 / kPage + blk * kWidePages + wave;
-    return clamp_page(bt[pg < row_pages ? pg : row_pages - 1], a.num_pages);
-  };
-  int next_id = page_id(0);
-  auto load = [&](int blk) __attribute__((always_inline)) {
-    const size_t base = ((size_t)next_id * a.hkv + g) * head_stride;
-    if (blk + 1 < nblocks) next_id = page_id(blk + 1);
-    constexpr int kLoads = kFp8 ? 2 : 4;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      if constexpr (kFp8) {
-        kreg[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint8_t *>(a.k_pool) +
-                                                   base + (i * kWave + lane) * 16);
-        vreg[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const uint8_t *>(a.v_pool) +
-                                                   base + (i * kWave + lane) * 16);
-      } else {
-        kreg[i] = load_u32x4(a.k_pool + base + (i * kWave + lane) * 8);
-        vreg[i] = load_u32x4(a.v_pool + base + (i * kWave + lane) * 8);
-      }
-    }
-  };
-  auto store = [&](int blk) __attribute__((always_inline)) {
-    uint16_t *sk = lds.in.k[blk & 1], *sv = lds.in.v[blk & 1];
-    const int pos = t0 + blk * kWideKeys + wave * kPage;   // the page's first key
-    const bool tail = pos + kPage > row.ctx;
-    // values past the row's end, and those of nodes that are infinite or NaN, become zeros
-    auto alive = [&](u32x4 w, int first) __attribute__((always_inline)) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[e] &= low_keys(end - first - 2 * e);
-        const uint32_t bad = not_finite(w[e]) & ~low_keys(row.ctx - first - 2 * e);
-        odd |= bad;
-        w[e] &= ~bad;
-      }
-      return w;
-    };
-    if constexpr (kFp8) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int c = i * kWave + lane;
-        uint16_t *kd = sk + (wave * kPage + (c >> 3)) * kWKPitch + (c & 7) * 16;
-        *reinterpret_cast<bf16x8 *>(kd) = fp8x8_to_bf16x8(u32x2{kreg[i][0], kreg[i][1]});
-        *reinterpret_cast<bf16x8 *>(kd + 8) = fp8x8_to_bf16x8(u32x2{kreg[i][2], kreg[i][3]});
-        u32x4 v0 = __builtin_bit_cast(u32x4, fp8x8_to_bf16x8(u32x2{vreg[i][0], vreg[i][1]}));
-        u32x4 v1 = __builtin_bit_cast(u32x4, fp8x8_to_bf16x8(u32x2{vreg[i][2], vreg[i][3]}));
-        if (tail) v0 = alive(v0, pos), v1 = alive(v1, pos + 8);
-        *reinterpret_cast<u32x4 *>(sv + wide_v(wave, c, 0)) = v0;
-        *reinterpret_cast<u32x4 *>(sv + wide_v(wave, c, 1)) = v1;
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int c = i * kWave + lane;
-        *reinterpret_cast<u32x4 *>(sk + (wave * kPage + (c >> 4)) * kWKPitch + (c & 15) * 8) = kreg[i];
-        u32x4 w = vreg[i];
-        if (tail) w = alive(w, pos + (c & 1) * 8);
-        *reinterpret_cast<u32x4 *>(sv + wide_v(wave, c >> 1, c & 1)) = w;
-      }
-    }
-  };
 
   f32x16 o[4];
 #pragma unroll
@@ -438,26 +468,55 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
   // row i of a tile of scores is key i with bits 2 and 3 exchanged
   const int key = (col & ~12) | ((col & 4) << 1) | ((col & 8) >> 1);
 
-  auto pair = [&](int blk, int pp) __attribute__((always_inline)) {
+  constexpr int kKReads = kFp8 ? 4 : 8;
+  const int slot = key & 15;
+  const uint32_t k_at = (key >> 4) * kPageBytes + 16 * (kFp8 ? slot * 8 + (grp ^ (slot >> 1)) : slot * 16 + (grp ^ slot));
+  const uint32_t v_at = kWidePages * kPageBytes + 16 * (kFp8 ? 32 * grp + col : 2 * col + (grp ^ (col >> 3 & 1)));
+  u32x4 kraw[kKReads];
+  auto read_k = [&](int blk, int pp) __attribute__((always_inline)) {
+    const uint32_t at = ring + blk % kRing * kBlockBytes + 2 * pp * kPageBytes + k_at;
+#pragma unroll
+    for (int i = 0; i < kKReads; ++i) kraw[i] = read_lds(at ^ (32 * i));   // unit 2 i + grp
+  };
+  // Reads are issued a phase ahead: the values before the scores' products, the next pair's keys
+  // behind them.
+  auto pair = [&](int blk, int pp, bool more) __attribute__((always_inline)) {
     const int tok = t0 + blk * kWideKeys + pp * kPair;
-    if (tok >= t1) return;
-    const uint16_t *sk = lds.in.k[blk & 1] + (pp * kPair + key) * kWKPitch + 8 * grp;
-    const uint16_t *sv = lds.in.v[blk & 1];
+    const bool tail = tok + kPair > row.ctx;
+    u32x4 vraw[kFp8 ? 4 : 8];
+    const uint32_t from = ring + blk % kRing * kBlockBytes + 2 * pp * kPageBytes + v_at;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if constexpr (kFp8) {
+        // lane groups 0 and 1 read rows 32 apart, whole; see below
+#pragma unroll
+        for (int j = 0; j < 2; ++j) vraw[2 * h + j] = read_lds(from + h * kPageBytes + j * 1024);
+      } else {
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) vraw[4 * h + mt] = read_lds(from + h * kPageBytes + mt * 1024);
+      }
+    keep_order();
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) s = mfma32x32x16(lds_bf16x8(sk + 16 * kk), q[kk], s);
-    const bool tail = tok + kPair > row.ctx;
+    for (int kk = 0; kk < 8; ++kk) {
+      bf16x8 k;
+      if constexpr (kFp8)
+        k = fp8x8_to_bf16x8(u32x2{kraw[kk >> 1][2 * (kk & 1)], kraw[kk >> 1][2 * (kk & 1) + 1]});
+      else
+        k = __builtin_bit_cast(bf16x8, kraw[kk]);
+      s = mfma32x32x16(k, q[kk], s);
+    }
+    keep_order();
+    if (more) read_k(blk, pp + 1);             // (shares is 1)
+    keep_order();
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] *= a.scale_log2;
     if (tail) {
+      const uint32_t sees = seen_keys(mask, tok, row.ctx, row.T) >> (8 * grp);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int pos = tok + 16 * (i >> 3) + 8 * grp + (i & 7), j = pos - row.ctx;
-        const bool sees = j < 0 || (pos < end && (mask[j >> 6] >> (j & 63) & 1));
-        s[i] = sees ? s[i] : -INFINITY;
-      }
+      for (int i = 0; i < 16; ++i) s[i] = sees >> (16 * (i >> 3) + (i & 7)) & 1 ? s[i] : -INFINITY;
     }
     float mx = s[0];
 #pragma unroll
@@ -477,36 +536,74 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
     for (int h = 0; h < 2; ++h) {
       f32x8 p;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = fast_exp2(s[8 * h + e] - m_use);
-        l_run += p[e];
-      }
+      for (int e = 0; e < 8; ++e) p[e] = fast_exp2(s[8 * h + e] - m_use);
+      l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
       hi[h] = to_bf16x8(p);
       lo[h] = to_bf16x8(p - to_f32x8(hi[h]));
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 2; ++h) {
+      bf16x8 v[4];
+      if constexpr (kFp8) {
+        // lanes l and l ^ 32 hold rows d and d + 32, all slots: exchanged, each has the slots
+        // that it supplies of both
 #pragma unroll
-      for (int mt = 0; mt < 4; ++mt) {
-        const bf16x8 v = lds_bf16x8(sv + wide_v(2 * pp + h, 32 * mt + col, grp));
-        o[mt] = mfma32x32x16(v, hi[h], o[mt]);
-        o[mt] = mfma32x32x16(v, lo[h], o[mt]);
+        for (int j = 0; j < 2; ++j) {
+          const u32x4 w = vraw[2 * h + j];
+          const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+          const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+          v[2 * j] = fp8x8_to_bf16x8(u32x2{s0[0], s1[0]});
+          v[2 * j + 1] = fp8x8_to_bf16x8(u32x2{s0[1], s1[1]});
+        }
+      } else {
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) v[mt] = __builtin_bit_cast(bf16x8, vraw[4 * h + mt]);
       }
+      if (tail) {
+        // values past the row's end, and those of nodes that are not finite, become zeros
+        const int first = tok + 16 * h + 8 * grp, alive = end - first, context = row.ctx - first;
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) {
+          u32x4 w = __builtin_bit_cast(u32x4, v[mt]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            w[e] &= low_keys(alive - 2 * e);
+            const uint32_t bad = not_finite(w[e]) & ~low_keys(context - 2 * e);
+            odd |= bad;
+            w[e] &= ~bad;
+          }
+          v[mt] = __builtin_bit_cast(bf16x8, w);
+        }
+      }
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) o[mt] = mfma32x32x16(v[mt], hi[h], o[mt]);
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) o[mt] = mfma32x32x16(v[mt], lo[h], o[mt]);
+    }
   };
 
-  load(0);
-  store(0);
+  int mine = share;
   for (int blk = 0; blk < nblocks; ++blk) {
-    if (blk + 1 < nblocks) load(blk + 1);
-    __syncthreads();
-    if (live)
-      for (int pp = share; pp < kWidePairs; pp += shares) pair(blk, pp);
-    if (blk + 1 < nblocks) store(blk + 1);
+    // this block's loads are done: of those behind them kLoads a block may be on their way
+    const int behind = nblocks - 1 - blk;
+    if (behind >= 2)
+      await_loads_before<2 * kLoads>();
+    else if (behind == 1)
+      await_loads_before<kLoads>();
+    else
+      await_loads();
+    __syncthreads();                            // all waves': and the block before is consumed
+    if (blk + kRing - 1 < nblocks) load(blk + kRing - 1);
+    const int pairs = min(kWidePairs, (t1 - t0 - blk * kWideKeys + kPair - 1) / kPair);
+    // the wave's next pair of all, `shares` behind its last one
+    int pp = mine - 2 * blk;
+    if (pp < pairs) read_k(blk, pp);
+    for (; pp < pairs; pp += shares, mine += shares) pair(blk, pp, pp + shares < pairs);
   }
   __syncthreads();
 
   // whole rows through LDS, joining the waves that shared them
-  if (live) {
+  {
     const auto l = __builtin_amdgcn_permlane32_swap(__float_as_uint(l_run), __float_as_uint(l_run),
                                                     false, false);
     if (grp == 0) {
@@ -520,19 +617,23 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
         *reinterpret_cast<f32x4 *>(&lds.o[wave][col][32 * mt + 8 * i + 4 * grp]) =
             f32x4{o[mt][4 * i], o[mt][4 * i + 1], o[mt][4 * i + 2], o[mt][4 * i + 3]};
   }
+  auto first_wave = [&](int p) { return p >= extra ? p - extra : heavy + p; };
   if (__syncthreads_or(odd != 0)) {
     reach_odd<kFp8, kWideThreads>(a, row, bt, g, t0, t1, r0, rows,
-                                  [&](int c) { return &lds.o[c >> 5][c & 31][0]; });
+                                  [&](int c) { return &lds.o[first_wave(c >> 5)][c & 31][0]; });
     __syncthreads();
   }
   for (int idx = tid; idx < rows * (kHeadDim / 4); idx += kWideThreads) {
     const int c = idx / (kHeadDim / 4), d = idx % (kHeadDim / 4) * 4;
+    const bool of_first = c >> 5 >= extra;     // the part's waves
+    const int w0 = first_wave(c >> 5), step = of_first ? few : extra;
+    const int n_waves = of_first ? base : base + 1;
     float M = -INFINITY, lsum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int w = 0; w < shares; ++w) M = fmaxf(M, lds.m[(w << lanes_log) + (c >> 5)][c & 31]);
+    for (int w = 0; w < n_waves; ++w) M = fmaxf(M, lds.m[w0 + w * step][c & 31]);
     const float M_use = M == -INFINITY ? 0.f : M;
-    for (int w = 0; w < shares; ++w) {
-      const int from = (w << lanes_log) + (c >> 5);
+    for (int w = 0; w < n_waves; ++w) {
+      const int from = w0 + w * step;
       const float f = fast_exp2(lds.m[from][c & 31] - M_use);
       acc += f * *reinterpret_cast<const f32x4 *>(&lds.o[from][c & 31][d]);
       lsum += f * lds.l[from][c & 31];
@@ -556,32 +657,56 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
   }
 }
 
-// Joins the splits of one node's heads, a wave a head.
+// Joins the splits of one node and head, a wave each: the weights of up to 64 splits are worked
+// out one a lane, the partial results taken four dims a lane by half a wave a split, four splits
+// of each half in flight. Bound by the partial results' bytes, and for few rows by round trips.
 constexpr int kJoinWaves = 4;
 __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs a) {
-  const int t = blockIdx.x, lane = threadIdx.x & (kWave - 1);
+  const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
+  const int64_t at = (int64_t)blockIdx.x * kJoinWaves + threadIdx.x / kWave;
+  const int t = (int)(at / a.hq);
+  if (t >= a.total_q) return;
   const int b = wave_search(a.B, t, [&](int i) { return a.cu_q[i]; });
   const TreeRow row = tree_row(a, b);
   if (t < row.first || t >= row.first + row.T) return;
   const int n = (row.ctx + row.T + a.split_tokens - 1) / a.split_tokens;
-  for (int h = threadIdx.x / kWave; h < a.hq; h += kJoinWaves) {
-    const size_t head = (size_t)t * a.hq + h, part = head * a.slots;
-    float M = -INFINITY;
-    for (int s = 0; s < n; ++s) M = fmaxf(M, a.ws_m[part + s]);
-    const float M_use = M == -INFINITY ? 0.f : M;
-    float x = 0.f, y = 0.f, lsum = 0.f;
-    for (int s = 0; s < n; ++s) {
-      const float f = fast_exp2(a.ws_m[part + s] - M_use);
-      const float2 v = *reinterpret_cast<const float2 *>(a.ws_o + (part + s) * kHeadDim + 2 * lane);
-      x += f * v.x;
-      y += f * v.y;
-      lsum += f * a.ws_l[part + s];
+  const size_t part = (size_t)at * a.slots;
+  const float *po = a.ws_o + part * kHeadDim + 4 * (lane & 31);
+  float M = -INFINITY;
+  for (int s = lane; s < n; s += kWave) M = fmaxf(M, a.ws_m[part + s]);
+#pragma unroll
+  for (int off = 1; off < kWave; off *= 2) M = fmaxf(M, __shfl_xor(M, off));
+  const float M_use = M == -INFINITY ? 0.f : M;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float lsum = 0.f;
+  for (int s0 = 0; s0 < n; s0 += kWave) {
+    const int m = min(n - s0, kWave);
+    const float f = lane < m ? fast_exp2(a.ws_m[part + s0 + lane] - M_use) : 0.f;
+    if (lane < m) lsum += f * a.ws_l[part + s0 + lane];
+    for (int s = 0; s < m; s += 8) {
+      f32x4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = min(s + 2 * i + half, m - 1);
+        v[i] = *reinterpret_cast<const f32x4 *>(po + (size_t)(s0 + k) * kHeadDim);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int k = s + 2 * i + half;
+        const float fk = __shfl(f, min(k, m - 1));
+        if (k < m) acc += fk * v[i];
+      }
     }
-    const float inv = a.v_scale / lsum;
-    float2 v = {lsum == 0.f ? 0.f : x * inv, lsum == 0.f ? 0.f : y * inv};
-    *reinterpret_cast<float2 *>(a.out + head * kHeadDim + 2 * lane) = v;
-    if (a.lse && lane == 0) a.lse[head] = (M + __log2f(lsum)) * kLn2;
   }
+#pragma unroll
+  for (int off = 1; off < kWave; off *= 2) lsum += __shfl_xor(lsum, off);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    acc[e] += __shfl_xor(acc[e], 32);
+    acc[e] = lsum == 0.f ? 0.f : acc[e] * (a.v_scale / lsum);
+  }
+  if (half == 0) *reinterpret_cast<f32x4 *>(a.out + at * kHeadDim + 4 * lane) = acc;
+  if (a.lse && lane == 0) a.lse[at] = (M + __log2f(lsum)) * kLn2;
 }
 
 }  // namespace
@@ -657,7 +782,8 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
     tree_split_kernel<1, false><<<grid, block, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.slots == 1) return e;
-  tree_join_kernel<<<total_q, kJoinWaves * kWave, 0, stream>>>(a);
+  const int64_t heads = (int64_t)total_q * hq;
+  tree_join_kernel<<<(unsigned)((heads + kJoinWaves - 1) / kJoinWaves), kJoinWaves * kWave, 0, stream>>>(a);
   return hipGetLastError();
 }
 
