@@ -646,7 +646,7 @@ size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hk
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || total_q <= 0 || max_q_len <= 0 ||
       max_q_len > RA_MAX_DRAFT_NODES || max_kv_len <= 0)
     return 0;
-  return ra::tree_workspace_bytes(total_q, Hq, ra::tree_plan(B, Hq, Hkv, max_q_len, max_kv_len));
+  return ra::tree_workspace_bytes(B, ra::tree_plan(B, Hq, Hkv, max_q_len, max_kv_len));
 }
 
 int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *ctx_lens,
@@ -667,7 +667,7 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
     return RA_ERR_UNSUPPORTED;
   const ra::TreePlan plan = ra::tree_plan(B, Hq, kv->num_kv_heads, max_q_len, max_kv_len);
   if (plan.groups > INT32_MAX || (int64_t)total_q * Hq > INT32_MAX) return RA_ERR_UNSUPPORTED;
-  const size_t need = ra::tree_workspace_bytes(total_q, Hq, plan);
+  const size_t need = ra::tree_workspace_bytes(B, plan);
   if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
   if (need > 0 && !aligned16(workspace)) return RA_ERR_UNSUPPORTED;
   return hip_status(ra::launch_tree(static_cast<const uint16_t *>(q), cu_q, ctx_lens, tree_mask,

@@ -137,14 +137,14 @@ hipError_t launch_table_release(const int32_t *lens, const int32_t *keep_lens,
 // ---- trees of drafted tokens ----
 constexpr int32_t kMaxDraftNodes = 1024;       // nodes of a tree
 struct TreePlan {
-  int32_t rows;           // query rows a workgroup takes: 16, 32 or 256
+  int32_t rows;           // query rows of a tile: 16, 32 or 256
+  int32_t piece_rows;     // of them, those that the largest tree has
+  bool direct;            // a workgroup a tile; otherwise equal shares of the work
   int64_t tiles;          // of the query rows of the largest tree, a KV head
-  int32_t split_tokens;   // keys a split
-  int32_t slots;          // splits of the longest row
   int64_t groups;         // workgroups
 };
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len);
-size_t tree_workspace_bytes(int32_t total_q, int32_t hq, const TreePlan &p);
+size_t tree_workspace_bytes(int32_t B, const TreePlan &p);
 hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ctx_lens,
                        const uint64_t *mask, int32_t words, const PagedKV &kv, int32_t B,
                        int32_t hq, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,

@@ -1,13 +1,26 @@
 // Attention of a tree of drafted tokens over the paged cache (rollout_attn_decode_tree).
 //
 // Row b's T nodes lie behind its ctx cached tokens. The query rows of a KV head are its G =
-// Hq / Hkv query heads of all nodes, taken as columns of the matrix products as in decode
-// (ra_decode_split.h), 16 kTiles of them a workgroup: node r / G, head r % G for query row r.
-// All see the context; which of the nodes a node sees is in its bit mask. Keys are cut into
-// splits, whose partial results a second launch joins.
+// Hq / Hkv query heads of all nodes, node r / G and head r % G for query row r, in tiles of 16,
+// 32 or 256 that are columns of the matrix products, so that a key is read once for a tile. All
+// nodes see the context; which of the nodes a node sees is in its bit mask.
+//
+// Softmax is the online form in fp32, base 2. Weights meet the values in two bf16 parts, off by
+// 2^-16 of a weight, as in decode (ra_decode_split.h): one part would be off by 2^-8.
+//
+// The work of a call is a line: its tiles in the order of rows, tiles and KV heads, each as long
+// as its blocks of keys, weighted by what a block costs with the tile's rows. Every workgroup
+// takes an equal share of the line, so that rows of different lengths and trees of different
+// sizes end together, and a tile is cut only where a share ends: a cut tile's pieces go to the
+// workspace and a second launch joins them. (Splits of a fixed length, a workgroup each, left
+// the compute units idle for 13 to 29 % of the time, and wrote 2 to 8 times the partial
+// results.) Calls of rows of up to kDirectKeys keys take a workgroup a tile and one launch.
+#include <type_traits>
+
 #include "ra_device.h"
 #include "ra_internal.h"
 #include "ra_lds.h"
+#include "ra_wave.h"
 
 namespace ra {
 namespace {
@@ -22,10 +35,15 @@ struct TreeArgs {
   const uint64_t *mask;
   const uint16_t *k_pool, *v_pool;
   const int32_t *block_table;
-  float *ws_o, *ws_m, *ws_l;   // [total_q][Hq][slots][128], [total_q][Hq][slots] twice
   float *out, *lse;
+  // workspace: the share's length, where the rows begin on the line, and of each workgroup two
+  // pieces' results: unnormalised O, (maximum, sum)
+  int64_t *share, *start;      // [1], [B]
+  float *ws_o;                 // [2 groups][piece_rows][128]
+  float2 *ws_ml;               // [2 groups][piece_rows]
+  int64_t min_share;
   int32_t B, hq, hkv, group, words, bt_stride, num_pages, total_q, max_q_len, max_kv_len;
-  int32_t split_tokens, slots, tiles;
+  int32_t piece_rows, tiles, direct;
   float scale_log2, v_scale;
 };
 
@@ -45,6 +63,146 @@ __device__ __forceinline__ TreeRow tree_row(const TreeArgs &a, int b) {
 __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) |
          ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
+// What a block of keys costs with a tile's rows, by parts of 32 rows: tiles of up to 128 rows
+// wait for their keys, larger ones for their products.
+template <int kRows>
+__device__ __forceinline__ int block_cost(int rows) {
+  if constexpr (kRows < 256) return 1;
+  const int parts = (rows + 31) / 32;
+  return parts <= 3 ? 8 : parts == 4 ? 9 : parts <= 6 ? 12 : 16;
+}
+template <int kRows>
+__host__ __device__ constexpr int block_keys() { return kRows < 256 ? 128 : 64; }
+
+// A row's tiles on the line: all but the last have kRows query rows.
+template <int kRows>
+struct RowLine {
+  int blocks, tiles, last_cost;
+  __device__ __forceinline__ RowLine(const TreeRow &r, int G) {
+    blocks = r.T > 0 ? (r.ctx + r.T + block_keys<kRows>() - 1) / block_keys<kRows>() : 0;
+    tiles = r.T > 0 ? (r.T * G + kRows - 1) / kRows : 0;
+    last_cost = block_cost<kRows>(r.T * G - (tiles - 1) * kRows);
+  }
+  __device__ __forceinline__ int cost(int tile) const {
+    return tile + 1 < tiles ? block_cost<kRows>(kRows) : last_cost;
+  }
+  __device__ __forceinline__ int64_t before(int tile, int g, int hkv) const {
+    return ((int64_t)tile * hkv * block_cost<kRows>(kRows) + (int64_t)g * cost(tile)) * blocks;
+  }
+  __device__ __forceinline__ int64_t length(int hkv) const {
+    return tiles > 0 ? before(tiles - 1, hkv, hkv) : 0;
+  }
+};
+
+template <int kThreads>
+struct WalkLds {
+  int64_t begin[kThreads + 1];       // of rows on the line
+  int64_t part[kThreads / kWave];
+};
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const u32x2 w = __builtin_bit_cast(u32x2, x);
+  u32x2 r;
+  r[0] = __builtin_amdgcn_readfirstlane(w[0]);
+  r[1] = __builtin_amdgcn_readfirstlane(w[1]);
+  return __builtin_bit_cast(int64_t, r);
+}
+
+__device__ __forceinline__ TreeRow uniform_row(const TreeArgs &a, int b) {
+  TreeRow r = tree_row(a, b);
+  r.first = uniform(r.first);
+  r.T = uniform(r.T);
+  r.ctx = uniform(r.ctx);
+  return r;
+}
+
+// Calls piece(b, row, tile, g, first block, behind the last one, place of the result) for all that
+// is this workgroup's; place -1: a whole tile, whose result is final.
+template <int kRows, int kThreads, typename Piece>
+__device__ __forceinline__ void walk(const TreeArgs &a, WalkLds<kThreads> &lds, Piece piece) {
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int s = blockIdx.x;
+  if (a.direct) {
+    const int g = s % a.hkv, at = s / a.hkv, tile = at % a.tiles, b = at / a.tiles;
+    const TreeRow row = uniform_row(a, b);
+    const RowLine<kRows> line(row, a.group);
+    if (tile < line.tiles) piece(b, row, tile, g, 0, line.blocks, -1);
+    return;
+  }
+  // the rows' places, kThreads rows at a time
+  auto place = [&](int c0) {
+    int64_t mine = 0;
+    if (c0 + tid < a.B) mine = RowLine<kRows>(tree_row(a, c0 + tid), a.group).length(a.hkv);
+    const int64_t sum = wave_sums(mine);
+    __syncthreads();
+    if (lane == kWave - 1) lds.part[wave] = sum;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < kThreads / kWave; ++w) {
+      if (w == wave) before = all;
+      all += lds.part[w];
+    }
+    if (tid == 0) lds.begin[0] = 0;
+    lds.begin[tid + 1] = before + sum;
+    __syncthreads();
+    return uniform(all);
+  };
+  int64_t all = 0;
+  for (int c0 = 0; c0 < a.B; c0 += kThreads) {
+    const int64_t n = place(c0);
+    if (s == 0 && c0 + tid < a.B) a.start[c0 + tid] = all + lds.begin[tid];
+    all += n;
+  }
+  const int64_t even = (all + gridDim.x - 1) / gridDim.x;
+  const int64_t share = even > a.min_share ? even : a.min_share;
+  if (s == 0 && tid == 0) *a.share = share;
+  const int64_t s0 = uniform(s * share), s1 = uniform(min(all, s0 + share));
+  int64_t base = 0;
+  for (int c0 = 0; c0 < a.B && base < s1; c0 += kThreads) {
+    const int rows = min(kThreads, a.B - c0);
+    if (a.B > kThreads) place(c0);
+    const int64_t n = uniform(lds.begin[rows]);
+    if (base + n > s0) {
+      // the last row that begins at or before s0, then those behind it
+      int lo = 0, hi = rows - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) / 2;
+        if (base + uniform(lds.begin[mid]) <= s0) lo = mid; else hi = mid - 1;
+      }
+      for (int i = lo; i < rows; ++i) {
+        const int64_t begin = base + uniform(lds.begin[i]);
+        if (begin >= s1) break;
+        const int b = c0 + i;
+        const TreeRow row = uniform_row(a, b);
+        const RowLine<kRows> line(row, a.group);
+        if (line.tiles == 0) continue;
+        // its first tile and KV head that end behind s0
+        const int64_t off = s0 > begin ? s0 - begin : 0;
+        const int64_t full = line.before(1, 0, a.hkv);       // of a tile that is not the last
+        int tile = uniform(line.tiles > 1 ? (int)min((int64_t)line.tiles - 1, off / full) : 0);
+        int g = uniform((int)((off - line.before(tile, 0, a.hkv)) / ((int64_t)line.cost(tile) * line.blocks)));
+        for (; tile < line.tiles; ++tile, g = 0)
+          for (; g < a.hkv; ++g) {
+            const int64_t at = begin + line.before(tile, g, a.hkv);
+            if (at >= s1) return;
+            const int cost = line.cost(tile);
+            const int b0 = uniform(at >= s0 ? 0 : (int)((s0 - at + cost - 1) / cost));
+            const int b1 = uniform((int)min((int64_t)line.blocks, (s1 - at + cost - 1) / cost));
+            if (b0 >= b1) continue;
+            piece(b, row, tile, g, b0, b1, b0 == 0 && b1 == line.blocks ? -1 : 2 * s + (b0 == 0));
+          }
+      }
+    }
+    base += n;
+  }
+}
+
+// Page ids by the scalar unit: vector loads of them would wait for all that are on their way.
+__device__ __forceinline__ int page_at(const int32_t *bt, int i, int num_pages) {
+  return clamp_page(((const __attribute__((address_space(4))) int32_t *)(uintptr_t)bt)[i], num_pages);
 }
 
 // Which of the 32 keys from position pos on node `mask` sees: those of the context, and the
@@ -85,28 +243,30 @@ __device__ __forceinline__ void reach_odd(const TreeArgs &a, const TreeRow &row,
   }
 }
 
+// ---- narrow tiles ----
+// 16 kTiles query rows by four waves, each of which takes every fourth pair of pages (32 keys)
+// of the piece straight from HBM into its registers:
+//   S^T[key][row] = K[key][:] . Q^T[:][row]       (4 products of 16 x 16 x 32 for 16 keys and rows)
+//   O^T[d][row]  += V^T[d][key] . P^T[key][row]   (8 for 32 keys, twice: the weights' parts)
+// Bound by HBM; the waves are joined through LDS at the end of a piece.
 template <int kTiles>
 struct TreeLds {
+  WalkLds<kSplitWaves * kWave> walk;
   float m[kSplitWaves][16 * kTiles];
   float l[kSplitWaves][16 * kTiles];
   float o[kSplitWaves][16 * kTiles][kOPitch];
 };
 
 template <int kTiles, bool kFp8>
-__global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(TreeArgs a) {
-  __shared__ TreeLds<kTiles> lds;
-  int id = blockIdx.x;
-  const int g = id % a.hkv;
-  id /= a.hkv;
-  const int tile = id % a.tiles;
-  id /= a.tiles;
-  const int split = id % a.slots, b = id / a.slots;
-  const TreeRow row = tree_row(a, b);
+__device__ __forceinline__ void narrow_piece(const TreeArgs &a, TreeLds<kTiles> &lds, int b,
+                                             const TreeRow &row, int tile, int g, int blk0,
+                                             int blk1, int place) {
   const int G = a.group, rows = row.T * G, r0 = tile * 16 * kTiles;
   const int end = row.ctx + row.T;
-  const int t0 = split * a.split_tokens, t1 = min(end, t0 + a.split_tokens);
-  if (r0 >= rows || t0 >= t1) return;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int t0 = blk0 * block_keys<16>(), t1 = min(end, blk1 * block_keys<16>());
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));             // (what follows from it is not kept from piece to piece)
+  const int lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int npairs = (t1 - t0 + kPair - 1) / kPair;
   const int row_pages = (t1 + kPage - 1) / kPage;
@@ -126,6 +286,11 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
       qop[nt][kk] = kFp8 ? load_bf16x8(qrow + 64 * (kk >> 1) + 16 * kgrp + 8 * (kk & 1))
                          : load_bf16x8(qrow + 32 * kk + 8 * kgrp);
   }
+  // arrived before the loop: a wait for them in it would wait for the keys and values as well
+#pragma unroll
+  for (int nt = 0; nt < kTiles; ++nt)
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) asm volatile("" : "+v"(qop[nt][kk]));
   const int ka_sel = col >> 3, ka_slot = 8 * ((col >> 2) & 1) + (col & 3);
   const int sv_sel = lane >> 5, sv_slot = 8 * ((lane >> 4) & 1);
 
@@ -144,9 +309,9 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
   // its own keys.
   size_t kbase = 0, vbase = 0;
   auto pages = [&](int pr) __attribute__((always_inline)) {
-    const int pg = (t0 + pr * kPair) / kPage;
-    const int id0 = clamp_page(bt[pg], a.num_pages);
-    const int id1 = pg + 1 < row_pages ? clamp_page(bt[pg + 1], a.num_pages) : id0;
+    const int pg = t0 / kPage + 2 * pr;
+    const int id0 = page_at(bt, pg, a.num_pages);
+    const int id1 = page_at(bt, min(pg + 1, row_pages - 1), a.num_pages);
     kbase = ((size_t)(ka_sel ? id1 : id0) * a.hkv + g) * head_stride;
     vbase = ((size_t)(sv_sel ? id1 : id0) * a.hkv + g) * head_stride;
   };
@@ -191,9 +356,10 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
     load_k();
     load_v();
   }
-  for (int pr = wave; pr < npairs; pr += kSplitWaves) {
+  // kMore: another pair follows (a load under a condition would make the waits of what is not
+  // under it wait for it too)
+  auto step = [&](int pr, auto kMore) __attribute__((always_inline)) {
     const int tok = t0 + pr * kPair;
-    const bool more = pr + kSplitWaves < npairs;
     bf16x8 ka[2][4], va[8];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -215,10 +381,12 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) st[nt][t] = mfma16x16x32(ka[t][kk], qop[nt][kk], st[nt][t]);
       }
-    if (more) {
+    keep_order();
+    if constexpr (kMore) {
       pages(pr + kSplitWaves);
       load_k();
     }
+    keep_order();
     if constexpr (kFp8) {
       // lanes l and l ^ 16 hold rows 2 j and 2 j + 1 of one page: exchanged, each has the slots
       // that it supplies of both
@@ -289,8 +457,13 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
         o[nt][mt] = mfma16x16x32(va[mt], p_lo, o[nt][mt]);
       }
     }
-    if (more) load_v();
-  }
+    keep_order();
+    if constexpr (kMore) load_v();
+    keep_order();
+  };
+  int pr = wave;
+  for (; pr + kSplitWaves < npairs; pr += kSplitWaves) step(pr, std::true_type{});
+  if (pr < npairs) step(pr, std::false_type{});
 
   // join the waves
 #pragma unroll
@@ -323,20 +496,28 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_split_kernel(Tree
       acc += f * lds.o[w][c][d];
       lsum += f * lds.l[w][c];
     }
-    const int r = r0 + c, node = r / G;
-    const size_t head = (size_t)(row.first + node) * a.hq + (size_t)g * G + (r - node * G);
-    if (a.slots == 1) {
+    if (place < 0) {
+      const int r = r0 + c, node = r / G;
+      const size_t head = (size_t)(row.first + node) * a.hq + (size_t)g * G + (r - node * G);
       a.out[head * kHeadDim + d] = lsum == 0.f ? 0.f : acc / lsum * a.v_scale;
       if (a.lse && d == 0) a.lse[head] = (M + __log2f(lsum)) * kLn2;
     } else {
-      const size_t part = head * a.slots + split;
+      const size_t part = (size_t)place * a.piece_rows + c;
       a.ws_o[part * kHeadDim + d] = acc;
-      if (d == 0) {
-        a.ws_m[part] = M;
-        a.ws_l[part] = lsum;
-      }
+      if (d == 0) a.ws_ml[part] = float2{M, lsum};
     }
   }
+  __syncthreads();                          // the next piece writes there
+}
+
+template <int kTiles, bool kFp8>
+__global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_narrow_kernel(TreeArgs a) {
+  __shared__ TreeLds<kTiles> lds;
+  walk<16 * kTiles>(a, lds.walk,
+                    [&](int b, const TreeRow &row, int tile, int g, int blk0, int blk1, int place)
+                        __attribute__((always_inline)) {
+                          narrow_piece<kTiles, kFp8>(a, lds, b, row, tile, g, blk0, blk1, place);
+                        });
 }
 
 // ---- wide tiles ----
@@ -356,7 +537,6 @@ constexpr int kWideRows = 32 * kWideWaves;
 constexpr int kWideKeys = 64, kWidePages = kWideKeys / kPage, kWidePairs = kWideKeys / kPair;
 constexpr int kRing = 4;
 constexpr int kPageElems = kPage * kHeadDim;
-constexpr int kMaxSplit = 8192;                 // keys of a split
 constexpr float kSlack = 8.f;
 
 struct WideLds {
@@ -365,7 +545,7 @@ struct WideLds {
     __attribute__((aligned(16))) float o[kWideWaves][32][kOPitch];
   };
   float m[kWideWaves][32], l[kWideWaves][32];
-  int32_t page[kMaxSplit / kPage + kWidePages];   // of the split's keys, clamped
+  WalkLds<kWideThreads> walk;
 };
 static_assert(sizeof(WideLds) <= 160 * 1024, "LDS of a compute unit");
 
@@ -387,23 +567,17 @@ __device__ __forceinline__ float pair_max(float x) {
 }
 
 template <bool kFp8>
-__global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
-  __shared__ __attribute__((aligned(1024))) WideLds lds;
-  int id = blockIdx.x;
-  const int g = id % a.hkv;
-  id /= a.hkv;
-  const int tile = id % a.tiles;
-  id /= a.tiles;
-  const int split = id % a.slots, b = id / a.slots;
-  const TreeRow row = tree_row(a, b);
+__device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int b,
+                                           const TreeRow &row, int tile, int g, int blk0, int blk1,
+                                           int place) {
   const int G = a.group, r0 = tile * kWideRows, rows = min(row.T * G - r0, kWideRows);
   const int end = row.ctx + row.T;
-  const int t0 = split * a.split_tokens, t1 = min(end, t0 + a.split_tokens);
-  if (rows <= 0 || t0 >= t1) return;
-  const int tid = threadIdx.x, lane = tid & (kWave - 1);
+  const int t0 = blk0 * kWideKeys, t1 = min(end, blk1 * kWideKeys), nblocks = blk1 - blk0;
+  int tid = threadIdx.x;
+  asm volatile("" : "+v"(tid));                 // (what follows from it is not kept from piece to piece)
+  const int lane = tid & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int col = lane & 31, grp = lane >> 5;
-  const int nblocks = (t1 - t0 + kWideKeys - 1) / kWideKeys;
   const int row_pages = (t1 + kPage - 1) / kPage;
   const int32_t *bt = a.block_table + (size_t)b * a.bt_stride;
 
@@ -439,19 +613,18 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
   const uint16_t *pool = is_v ? a.v_pool : a.k_pool;
   const uint32_t ring = lds_address(lds.in[0][0]);
   constexpr uint32_t kPageBytes = 2 * kPageElems, kBlockBytes = 2 * kWidePages * kPageBytes;
-  // (page ids by way of LDS: a load of them between those to LDS would wait for these)
-  for (int i = tid; i < nblocks * kWidePages; i += kWideThreads)
-    lds.page[i] = clamp_page(bt[min(t0 / kPage + i, row_pages - 1)], a.num_pages);
-  __syncthreads();
-  int next_id = lds.page[my_page];
+  auto page_id = [&](int blk) {
+    return page_at(bt, min(t0 / kPage + blk * kWidePages + my_page, row_pages - 1), a.num_pages);
+  };
+  int next_id = page_id(0);
   auto load = [&](int blk) __attribute__((always_inline)) {
-    const size_t at = ((size_t)__builtin_amdgcn_readfirstlane(next_id) * a.hkv + g) * kPageElems;
+    const size_t at = ((size_t)next_id * a.hkv + g) * kPageElems;
     const uint16_t *base = pool + (kFp8 ? at / 2 : at);
     const uint32_t to = __builtin_amdgcn_readfirstlane(
         ring + blk % kRing * kBlockBytes + (is_v * kWidePages + my_page) * kPageBytes);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) load_to_lds(base, (16 * unit ^ turn * i) + 1024 * i, to + i * 1024);
-    next_id = lds.page[(blk + 1) * kWidePages + my_page];
+    next_id = page_id(blk + 1);
   };
 #pragma unroll
   for (int i = 0; i < kRing - 1; ++i)
@@ -638,42 +811,56 @@ __global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
       acc += f * *reinterpret_cast<const f32x4 *>(&lds.o[from][c & 31][d]);
       lsum += f * lds.l[from][c & 31];
     }
-    const int rr = r0 + c, n = rr / G;
-    const size_t head = (size_t)(row.first + n) * a.hq + (size_t)g * G + (rr - n * G);
-    if (a.slots == 1) {
+    if (place < 0) {
+      const int rr = r0 + c, n = rr / G;
+      const size_t head = (size_t)(row.first + n) * a.hq + (size_t)g * G + (rr - n * G);
       const float inv = a.v_scale / lsum;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = lsum == 0.f ? 0.f : acc[e] * inv;
       *reinterpret_cast<f32x4 *>(a.out + head * kHeadDim + d) = acc;
       if (a.lse && d == 0) a.lse[head] = (M + __log2f(lsum)) * kLn2;
     } else {
-      const size_t at = head * a.slots + split;
+      const size_t at = (size_t)place * a.piece_rows + c;
       *reinterpret_cast<f32x4 *>(a.ws_o + at * kHeadDim + d) = acc;
-      if (d == 0) {
-        a.ws_m[at] = M;
-        a.ws_l[at] = lsum;
-      }
+      if (d == 0) a.ws_ml[at] = float2{M, lsum};
     }
   }
+  __syncthreads();                              // the next piece's loads go there
 }
 
-// Joins the splits of one node and head, a wave each: the weights of up to 64 splits are worked
-// out one a lane, the partial results taken four dims a lane by half a wave a split, four splits
-// of each half in flight. Bound by the partial results' bytes, and for few rows by round trips.
+template <bool kFp8>
+__global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
+  __shared__ __attribute__((aligned(1024))) WideLds lds;
+  walk<kWideRows>(a, lds.walk,
+                  [&](int b, const TreeRow &row, int tile, int g, int blk0, int blk1, int place)
+                      __attribute__((always_inline)) {
+                        wide_piece<kFp8>(a, lds, b, row, tile, g, blk0, blk1, place);
+                      });
+}
+
+// Joins the pieces of one node and head, a wave each: the weights of up to 64 pieces are worked
+// out one a lane, the partial results taken four dims a lane by half a wave a piece, four pieces
+// of each half in flight. Nodes of uncut tiles are final already.
 constexpr int kJoinWaves = 4;
+template <int kRows>
 __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs a) {
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   const int64_t at = (int64_t)blockIdx.x * kJoinWaves + threadIdx.x / kWave;
-  const int t = (int)(at / a.hq);
+  const int t = (int)(at / a.hq), h = (int)(at - (int64_t)t * a.hq);
   if (t >= a.total_q) return;
   const int b = wave_search(a.B, t, [&](int i) { return a.cu_q[i]; });
   const TreeRow row = tree_row(a, b);
   if (t < row.first || t >= row.first + row.T) return;
-  const int n = (row.ctx + row.T + a.split_tokens - 1) / a.split_tokens;
-  const size_t part = (size_t)at * a.slots;
-  const float *po = a.ws_o + part * kHeadDim + 4 * (lane & 31);
+  const RowLine<kRows> line(row, a.group);
+  const int g = h / a.group, r = (t - row.first) * a.group + h - g * a.group, tile = r / kRows;
+  const int64_t share = *a.share, begin = a.start[b] + line.before(tile, g, a.hkv);
+  const int64_t first = begin / share;
+  const int n = (int)((begin + (int64_t)(line.blocks - 1) * line.cost(tile)) / share - first) + 1;
+  if (n == 1) return;
+  // piece i's result, query row r of its tile: the first piece is the last of its share
+  auto piece = [&](int i) { return (size_t)(2 * (first + i) + (i == 0)) * a.piece_rows + (r - tile * kRows); };
   float M = -INFINITY;
-  for (int s = lane; s < n; s += kWave) M = fmaxf(M, a.ws_m[part + s]);
+  for (int s = lane; s < n; s += kWave) M = fmaxf(M, a.ws_ml[piece(s)].x);
 #pragma unroll
   for (int off = 1; off < kWave; off *= 2) M = fmaxf(M, __shfl_xor(M, off));
   const float M_use = M == -INFINITY ? 0.f : M;
@@ -681,14 +868,18 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs 
   float lsum = 0.f;
   for (int s0 = 0; s0 < n; s0 += kWave) {
     const int m = min(n - s0, kWave);
-    const float f = lane < m ? fast_exp2(a.ws_m[part + s0 + lane] - M_use) : 0.f;
-    if (lane < m) lsum += f * a.ws_l[part + s0 + lane];
+    float f = 0.f;
+    if (lane < m) {
+      const float2 ml = a.ws_ml[piece(s0 + lane)];
+      f = fast_exp2(ml.x - M_use);
+      lsum += f * ml.y;
+    }
     for (int s = 0; s < m; s += 8) {
       f32x4 v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int k = min(s + 2 * i + half, m - 1);
-        v[i] = *reinterpret_cast<const f32x4 *>(po + (size_t)(s0 + k) * kHeadDim);
+        v[i] = *reinterpret_cast<const f32x4 *>(a.ws_o + piece(s0 + k) * kHeadDim + 4 * (lane & 31));
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -709,28 +900,46 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs 
   if (a.lse && lane == 0) a.lse[at] = (M + __log2f(lsum)) * kLn2;
 }
 
+template <int kRows>
+void plan_line(TreePlan &p, int64_t units, int32_t max_kv_len, int64_t groups) {
+  constexpr int keys = block_keys<kRows>();
+  const int64_t blocks = units * ((max_kv_len + keys - 1) / keys);
+  p.groups = blocks < groups ? blocks : groups;
+}
+
 }  // namespace
+
+constexpr int kDirectKeys = 512;            // rows of so many keys are not cut
+constexpr int kMinShareKeys = 256;          // of a tile, where there is little work
 
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len) {
   const int64_t rows = (int64_t)max_q_len * (hq / hkv);
   TreePlan p;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kWideRows;
   p.tiles = (rows + p.rows - 1) / p.rows;
+  p.piece_rows = (int32_t)(rows < p.rows ? rows : p.rows);
+  p.direct = max_kv_len <= kDirectKeys;
   const int64_t units = (int64_t)B * hkv * p.tiles;
-  int64_t split = 512;
-  if (p.rows == kWideRows)
-    while (split < 8192 && units * max_kv_len / split > 2048) split *= 2;
+  // as many workgroups as are on the GPU together
+  if (p.direct)
+    p.groups = units;
+  else if (p.rows == 16)
+    plan_line<16>(p, units, max_kv_len, 512);
+  else if (p.rows == 32)
+    plan_line<32>(p, units, max_kv_len, 512);
   else
-    while (split < 4096 && units * max_kv_len / split > 8192) split *= 2;
-  p.split_tokens = (int32_t)split;
-  p.slots = (int32_t)((max_kv_len + split - 1) / split);
-  if (p.slots < 1) p.slots = 1;
-  p.groups = units * p.slots;
+    plan_line<kWideRows>(p, units, max_kv_len, 256);
   return p;
 }
 
-size_t tree_workspace_bytes(int32_t total_q, int32_t hq, const TreePlan &p) {
-  return p.slots == 1 ? 0 : (size_t)total_q * hq * p.slots * (kHeadDim + 2) * sizeof(float);
+namespace {
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+}  // namespace
+
+size_t tree_workspace_bytes(int32_t B, const TreePlan &p) {
+  if (p.direct) return 0;
+  return up256(((size_t)B + 1) * sizeof(int64_t)) +
+         (size_t)2 * p.groups * p.piece_rows * (kHeadDim + 2) * sizeof(float);
 }
 
 hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ctx_lens,
@@ -738,7 +947,6 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
                        int32_t hq, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,
                        float scale, float *out, float *lse, void *workspace, const TreePlan &p,
                        hipStream_t stream) {
-  const size_t parts = (size_t)total_q * hq * p.slots;
   TreeArgs a;
   a.q = q;
   a.cu_q = cu_q;
@@ -747,11 +955,20 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
   a.k_pool = kv.k_pool;
   a.v_pool = kv.v_pool;
   a.block_table = kv.block_table;
-  a.ws_o = static_cast<float *>(workspace);
-  a.ws_m = p.slots == 1 ? nullptr : a.ws_o + parts * kHeadDim;
-  a.ws_l = p.slots == 1 ? nullptr : a.ws_m + parts;
   a.out = out;
   a.lse = lse;
+  a.share = nullptr;
+  a.start = nullptr;
+  a.ws_o = nullptr;
+  a.ws_ml = nullptr;
+  if (!p.direct) {
+    a.share = static_cast<int64_t *>(workspace);
+    a.start = a.share + 1;
+    a.ws_o = reinterpret_cast<float *>(static_cast<char *>(workspace) +
+                                       up256(((size_t)B + 1) * sizeof(int64_t)));
+    a.ws_ml = reinterpret_cast<float2 *>(a.ws_o + (size_t)2 * p.groups * p.piece_rows * kHeadDim);
+  }
+  a.min_share = p.rows == kWideRows ? kMinShareKeys / kWideKeys * 16 : kMinShareKeys / block_keys<16>();
   a.B = B;
   a.hq = hq;
   a.hkv = kv.hkv;
@@ -762,28 +979,34 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
   a.total_q = total_q;
   a.max_q_len = max_q_len;
   a.max_kv_len = max_kv_len;
-  a.split_tokens = p.split_tokens;
-  a.slots = p.slots;
+  a.piece_rows = p.piece_rows;
   a.tiles = (int32_t)p.tiles;
+  a.direct = p.direct;
   a.scale_log2 = scale * kLog2e * kv.k_scale;
   a.v_scale = kv.v_scale;
   const dim3 grid((unsigned)p.groups), block(kSplitWaves * kWave);
+  const int64_t heads = (int64_t)total_q * hq;
+  const dim3 join_grid((unsigned)((heads + kJoinWaves - 1) / kJoinWaves)), join(kJoinWaves * kWave);
   if (p.rows == kWideRows && kv.fp8)
     tree_wide_kernel<true><<<grid, kWideThreads, 0, stream>>>(a);
   else if (p.rows == kWideRows)
     tree_wide_kernel<false><<<grid, kWideThreads, 0, stream>>>(a);
   else if (p.rows == 32 && kv.fp8)
-    tree_split_kernel<2, true><<<grid, block, 0, stream>>>(a);
+    tree_narrow_kernel<2, true><<<grid, block, 0, stream>>>(a);
   else if (p.rows == 32)
-    tree_split_kernel<2, false><<<grid, block, 0, stream>>>(a);
+    tree_narrow_kernel<2, false><<<grid, block, 0, stream>>>(a);
   else if (kv.fp8)
-    tree_split_kernel<1, true><<<grid, block, 0, stream>>>(a);
+    tree_narrow_kernel<1, true><<<grid, block, 0, stream>>>(a);
   else
-    tree_split_kernel<1, false><<<grid, block, 0, stream>>>(a);
+    tree_narrow_kernel<1, false><<<grid, block, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.slots == 1) return e;
-  const int64_t heads = (int64_t)total_q * hq;
-  tree_join_kernel<<<(unsigned)((heads + kJoinWaves - 1) / kJoinWaves), kJoinWaves * kWave, 0, stream>>>(a);
+  if (e != hipSuccess || p.direct) return e;
+  if (p.rows == kWideRows)
+    tree_join_kernel<kWideRows><<<join_grid, join, 0, stream>>>(a);
+  else if (p.rows == 32)
+    tree_join_kernel<32><<<join_grid, join, 0, stream>>>(a);
+  else
+    tree_join_kernel<16><<<join_grid, join, 0, stream>>>(a);
   return hipGetLastError();
 }
 
