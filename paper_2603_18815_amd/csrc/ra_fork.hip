@@ -17,13 +17,16 @@ namespace {
 
 constexpr int kForkThreads = 256;
 constexpr int kMaxRows = 65536;            // rows a block table can have
+constexpr int kSmallForks = 8, kSmallEntries = 4096;   // of calls that one workgroup does
 constexpr int kCode = 1 << 30;             // codes of entries: -(kCode + 1 + place), place < kCode
 
 __device__ __forceinline__ bool page_ok(int id, int num_pages) { return (unsigned)id < (unsigned)num_pages; }
 
-// A workgroup a fork. Every workgroup looks at all forks: whether the call holds decides what
-// each does, and the forks before it say which page is its own. Bound by latency and, for long
-// prompts, by the atomics on the shared pages' counts.
+// A workgroup a fork, or one for all of a small call (kOne), which then sets the list's length
+// itself. Every workgroup looks at all forks: whether the call holds decides what each does, and
+// the forks before it say which page is its own. Bound by latency and, for long prompts, by the
+// atomics on the shared pages' counts.
+template <bool kOne>
 __global__ __launch_bounds__(kForkThreads) void fork_kernel(
     const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens, int32_t n,
     int32_t *block_table, int32_t B, int32_t bt_stride, int32_t *shares, int32_t num_pages,
@@ -32,6 +35,7 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(
   __shared__ uint32_t is_dst[kMaxRows / 32];
   __shared__ int bad, need, before;
   const int tid = threadIdx.x, me = blockIdx.x;
+  const int count = *free_count;
   for (int i = tid; i < (B + 31) / 32; i += kForkThreads) is_dst[i] = 0;
   if (tid == 0) bad = need = before = 0;
   __syncthreads();
@@ -55,27 +59,30 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(
     if (s >= 0 && s < B && (is_dst[s >> 5] >> (s & 31) & 1)) bad = 1;
   }
   __syncthreads();
-  const int count = *free_count;
   const bool ok = !bad && count >= 0 && count <= capacity && need <= count;
-  if (me < n) {
+  int pages = kOne ? 0 : before;                         // taken by the forks before
+  for (int f = kOne ? 0 : me; f < (kOne ? n : min(n, me + 1)); ++f) {
     int from = -1, to = -1;
     if (ok) {
-      const int64_t src = (int64_t)src_rows[me] * bt_stride, dst = (int64_t)dst_rows[me] * bt_stride;
-      const int len = lens[me], full = len / kPage;
+      const int64_t src = (int64_t)src_rows[f] * bt_stride, dst = (int64_t)dst_rows[f] * bt_stride;
+      const int len = lens[f], full = len / kPage;
       for (int j = tid; j < full; j += kForkThreads) {
         const int page = block_table[src + j];
         block_table[dst + j] = page;
         if (page_ok(page, num_pages)) atomicAdd(&shares[page], 1);
       }
-      if (tid == 0 && len % kPage) {
-        from = block_table[src + full];
-        to = free_pages[count - 1 - before];
-        block_table[dst + full] = to;
+      if (len % kPage) {
+        if (tid == 0) {
+          from = block_table[src + full];
+          to = free_pages[count - 1 - pages];
+          block_table[dst + full] = to;
+        }
+        ++pages;
       }
     }
     if (tid == 0) {
-      copy_src[me] = from;
-      copy_dst[me] = to;
+      copy_src[f] = from;
+      copy_dst[f] = to;
     }
   }
   if (me == 0 && tid == 0) {
@@ -120,9 +127,9 @@ __global__ __launch_bounds__(kRowThreads) void shared_sub_kernel(SharedRelease r
   if (b == 0 && tid == 0) {
     r.head[0] = ok;
     r.head[1] = count;
-    if (!ok || r.B == 0) *r.released = ok ? 0 : -1;
+    if (!ok) *r.released = -1;
   }
-  if (!ok || b >= r.B) return;
+  if (!ok) return;
   const int32_t *row = r.block_table + (int64_t)b * r.bt_stride;
   const int end = (int)pages_of(r.lens[b]);
   for (int j = (int)pages_of(r.keep_lens[b]) + tid; j < end; j += kRowThreads) {
@@ -212,6 +219,76 @@ __global__ __launch_bounds__(kRowThreads) void shared_put_kernel(SharedRelease r
   }
 }
 
+// All of it by one workgroup, for tables of up to kSmallEntries entries: the counts change by
+// atomics, so they are read past the first-level cache.
+constexpr int kOneThreads = 1024;
+__global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r) {
+  __shared__ int bad, all, wave_sum[kOneThreads / kWave];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
+  const int count = *r.free_count, entries = r.B * r.bt_stride;
+  if (tid == 0) bad = all = 0;
+  __syncthreads();
+  const int64_t limit = (int64_t)r.bt_stride * kPage;
+  for (int i = tid; i < r.B; i += kOneThreads) {
+    const int64_t len = r.lens[i], keep = r.keep_lens[i];
+    if (keep < 0 || keep > len || len > limit) bad = 1;
+  }
+  __syncthreads();
+  if (bad || count < 0 || count > r.capacity) {
+    if (tid == 0) *r.released = -1;
+    return;
+  }
+  // the entry's page if it is given up, -1 else
+  auto page_of = [&](int x) {
+    if (x >= entries) return -1;
+    const int b = x / r.bt_stride, j = x - b * r.bt_stride;
+    if (j < pages_of(r.keep_lens[b]) || j >= pages_of(r.lens[b])) return -1;
+    const int page = r.block_table[x];
+    return page_ok(page, r.num_pages) ? page : -1;
+  };
+  auto holders = [&](int page) {
+    return __hip_atomic_load(&r.shares[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
+  for (int x = tid; x < entries; x += kOneThreads)
+    if (const int page = page_of(x); page >= 0) atomicSub(&r.shares[page], 1);
+  __threadfence();
+  __syncthreads();
+  for (int x = tid; x < entries; x += kOneThreads)
+    if (const int page = page_of(x); page >= 0 && holders(page) < 0)
+      atomicMin(&r.shares[page], -(kCode + 1) - x);
+  __threadfence();
+  __syncthreads();
+  int mine = 0;
+  for (int x = tid; x < entries; x += kOneThreads)
+    if (const int page = page_of(x); page >= 0) mine += holders(page) == -(kCode + 1) - x;
+  if (mine) atomicAdd(&all, mine);
+  __syncthreads();
+  int rank = 0;
+  for (int x0 = 0; x0 < entries; x0 += kOneThreads) {
+    const int x = x0 + tid, page = page_of(x);
+    const bool free = page >= 0 && holders(page) == -(kCode + 1) - x;
+    const uint64_t votes = __ballot(free);
+    if (lane == 0) wave_sum[wave] = (int)__popcll(votes);
+    __syncthreads();
+    int at = rank + (int)__popcll(votes & ((1ull << lane) - 1)), step = 0;
+    for (int w = 0; w < kOneThreads / kWave; ++w) {
+      if (w < wave) at += wave_sum[w];
+      step += wave_sum[w];
+    }
+    if (free) {
+      const int64_t to = (int64_t)count + all - 1 - at;
+      if (to < r.capacity) r.free_pages[to] = page;
+      __hip_atomic_store(&r.shares[page], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    rank += step;
+    __syncthreads();
+  }
+  if (tid == 0) {
+    *r.released = all;
+    *r.free_count = min(count + all, r.capacity);
+  }
+}
+
 // ---- pages' contents ----
 constexpr int kCopyThreads = 256;
 
@@ -234,56 +311,116 @@ __global__ __launch_bounds__(kCopyThreads) void page_copy_kernel(uint8_t *k_pool
   *reinterpret_cast<u32x4 *>(v_pool + t) = v;
 }
 
-constexpr int kMoveTokens = 32;            // moved together through LDS
+constexpr int kMoveTokens = 32;            // moved together
 constexpr int kMoveThreads = 256;
 
-// The kept tokens of one row and KV head. Indices rise, so a token never moves behind where it
-// was and the tokens of one step lie before the sources of all later ones: a step reads all
-// its tokens into LDS before it writes any.
+// The kept tokens of one row and KV head, up to 32 a step. Indices rise, so a token never moves
+// behind where it was and the tokens of one step lie before the sources of all later ones: a
+// step has all its tokens in registers before it writes any. Keys move 16 bytes a thread; of
+// the values a thread has one dimension of the tokens that go to one half of a page, so that a
+// half whose tokens all move is one store. Bound by round trips: the offsets, the index, the
+// table and the pages, one behind the other.
 template <typename E>
 __global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
     E *k_pool, E *v_pool, const int32_t *block_table, int32_t bt_stride, int32_t num_pages,
     int32_t hkv, const int32_t *start_pos, const int32_t *cu_src, const int32_t *src_index,
     const int32_t *counts, int32_t total, int32_t max_count) {
-  __shared__ E sk[kMoveTokens][kHeadDim], sv[kMoveTokens][kHeadDim];
-  __shared__ int64_t from[kMoveTokens], to[kMoveTokens];   // page * 16 + slot; -1: stays
+  constexpr int kUnit = 16 / sizeof(E), kUnits = kHeadDim / kUnit;      // of a key
+  constexpr int kKeys = kMoveTokens * kUnits / kMoveThreads;            // units a thread
+  constexpr int kHalf = kPage / 2;
+  constexpr int kHalves = kMoveTokens / kHalf + 1;                      // that 32 tokens can lie in
+  constexpr int kValues = (kHalves * kHeadDim + kMoveThreads - 1) / kMoveThreads;
+  constexpr int kWords = kHalf * sizeof(E) / 4;
+  typedef uint32_t Eight __attribute__((ext_vector_type(kWords)));      // a half of a value row
+  struct Move {
+    int from, slot, to, to_slot;           // pages and slots; from -1: stays
+  };
+  __shared__ Move move[kMoveTokens + 2 * kHalf];
   const int b = blockIdx.x / hkv, g = blockIdx.x - b * hkv, tid = threadIdx.x;
   const int first = min(max(cu_src[b], 0), total);
   int n = min(min(max(cu_src[b + 1] - first, 0), total - first), max_count);
   if (counts) n = min(n, max(counts[b], 0));
   const int64_t start = max(start_pos[b], 0), limit = (int64_t)bt_stride * kPage;
   const int32_t *bt = block_table + (int64_t)b * bt_stride;
+  auto block = [&](int page) { return ((size_t)page * hkv + g) * kPage * kHeadDim; };
   for (int i0 = 0; i0 < n; i0 += kMoveTokens) {
     __syncthreads();
     const int m = min(kMoveTokens, n - i0);
-    if (tid < m) {
-      const int i = i0 + tid, j = src_index[first + i];
-      int64_t f = -1, t = -1;
-      if (j > i && start + j < limit) {
-        const int64_t p = start + j, q = start + i;
-        f = (int64_t)clamp_page(bt[p / kPage], num_pages) * kPage + p % kPage;
-        t = (int64_t)clamp_page(bt[q / kPage], num_pages) * kPage + q % kPage;
+    const int lead = (int)((start + i0) % kHalf);          // the first token's place in its half
+    if (tid < kMoveTokens + 2 * kHalf) {                    // entry x: the token of place x - lead
+      const int i = i0 + tid - lead;
+      Move mv = {-1, 0, 0, 0};
+      if (tid >= lead && tid < lead + m) {
+        const int j = src_index[first + i];
+        if (j > i && start + j < limit) {
+          const int64_t p = start + j, q = start + i;
+          mv.from = clamp_page(bt[p / kPage], num_pages);
+          mv.to = clamp_page(bt[q / kPage], num_pages);
+          mv.slot = (int)(p % kPage);
+          mv.to_slot = (int)(q % kPage);
+        }
       }
-      from[tid] = f;
-      to[tid] = t;
+      move[tid] = mv;
     }
     __syncthreads();
-    for (int x = tid; x < m * kHeadDim; x += kMoveThreads) {
-      const int k = x / kHeadDim, d = x % kHeadDim;
-      if (from[k] < 0) continue;
-      const size_t block = ((size_t)(from[k] / kPage) * hkv + g) * kPage * kHeadDim;
-      const int slot = (int)(from[k] % kPage);
-      sk[k][d] = k_pool[block + slot * kHeadDim + d];
-      sv[k][d] = v_pool[block + d * kPage + slot];
+    u32x4 k[kKeys];
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+      const int x = i * kMoveThreads + tid, token = x / kUnits, unit = x % kUnits;
+      const Move mv = move[lead + token];
+      if (token < m && mv.from >= 0)
+        k[i] = *reinterpret_cast<const u32x4 *>(k_pool + block(mv.from) + mv.slot * kHeadDim + unit * kUnit);
     }
+    uint32_t v[kValues][kHalf] = {};
+    uint32_t moved[kValues];                                // bits of the half's slots
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      const int x = i * kMoveThreads + tid, half = x / kHeadDim, d = x % kHeadDim;
+      moved[i] = 0;
+      if (half >= kHalves) continue;
+#pragma unroll
+      for (int s = 0; s < kHalf; ++s) {
+        const Move mv = move[half * kHalf + s];
+        if (mv.from < 0) continue;
+        moved[i] |= 1u << s;
+        v[i][s] = v_pool[block(mv.from) + d * kPage + mv.slot];
+      }
+    }
+    // here before any thread writes
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) asm volatile("" : "+v"(k[i]));
+#pragma unroll
+    for (int i = 0; i < kValues; ++i)
+#pragma unroll
+      for (int s = 0; s < kHalf; ++s) asm volatile("" : "+v"(v[i][s]));
     __syncthreads();
-    for (int x = tid; x < m * kHeadDim; x += kMoveThreads) {
-      const int k = x / kHeadDim, d = x % kHeadDim;
-      if (to[k] < 0) continue;
-      const size_t block = ((size_t)(to[k] / kPage) * hkv + g) * kPage * kHeadDim;
-      const int slot = (int)(to[k] % kPage);
-      k_pool[block + slot * kHeadDim + d] = sk[k][d];
-      v_pool[block + d * kPage + slot] = sv[k][d];
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+      const int x = i * kMoveThreads + tid, token = x / kUnits, unit = x % kUnits;
+      const Move mv = move[lead + token];
+      if (token < m && mv.from >= 0)
+        *reinterpret_cast<u32x4 *>(k_pool + block(mv.to) + mv.to_slot * kHeadDim + unit * kUnit) = k[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kValues; ++i) {
+      const int x = i * kMoveThreads + tid, half = x / kHeadDim, d = x % kHeadDim;
+      if (moved[i] == 0) continue;
+      const Move mv = move[half * kHalf + __ffs(moved[i]) - 1];
+      E *to = v_pool + block(mv.to) + d * kPage + mv.to_slot / kHalf * kHalf;
+      if (moved[i] == (1u << kHalf) - 1) {
+        Eight w;
+#pragma unroll
+        for (int x = 0; x < kWords; ++x) {
+          w[x] = 0;
+#pragma unroll
+          for (int y = 0; y < kHalf / kWords; ++y) w[x] |= v[i][x * kHalf / kWords + y] << (8 * sizeof(E) * y);
+        }
+        *reinterpret_cast<Eight *>(to) = w;
+      } else {
+#pragma unroll
+        for (int s = 0; s < kHalf; ++s)
+          if (moved[i] >> s & 1) to[s] = (E)v[i][s];
+      }
     }
   }
 }
@@ -295,7 +432,13 @@ hipError_t launch_table_fork(const int32_t *src_rows, const int32_t *dst_rows, c
                              int32_t *shares, int32_t num_pages, const int32_t *free_pages,
                              int32_t *free_count, int32_t capacity, int32_t *copy_src,
                              int32_t *copy_dst, int32_t *taken, hipStream_t stream) {
-  fork_kernel<<<n > 0 ? n : 1, kForkThreads, 0, stream>>>(
+  if (n <= kSmallForks && (int64_t)n * bt_stride <= kSmallEntries) {
+    fork_kernel<true><<<1, kForkThreads, 0, stream>>>(
+        src_rows, dst_rows, lens, n, block_table, B, bt_stride, shares, num_pages, free_pages,
+        free_count, capacity, copy_src, copy_dst, taken);
+    return hipGetLastError();
+  }
+  fork_kernel<false><<<n, kForkThreads, 0, stream>>>(
       src_rows, dst_rows, lens, n, block_table, B, bt_stride, shares, num_pages, free_pages,
       free_count, capacity, copy_src, copy_dst, taken);
   if (n > 1) fork_count_kernel<<<1, 1, 0, stream>>>(free_count, taken);
@@ -312,12 +455,14 @@ hipError_t launch_table_release_shared(const int32_t *lens, const int32_t *keep_
   int32_t *head = static_cast<int32_t *>(workspace);
   const SharedRelease r = {lens, keep_lens, block_table, B, bt_stride, num_pages, capacity,
                            shares, free_pages, free_count, released, head, head + 2};
-  shared_sub_kernel<<<B > 0 ? B : 1, kRowThreads, 0, stream>>>(r);
-  if (B > 0) {
-    shared_last_kernel<<<B, kRowThreads, 0, stream>>>(r);
-    shared_count_kernel<<<B, kRowThreads, 0, stream>>>(r);
-    shared_put_kernel<<<B, kRowThreads, 0, stream>>>(r);
+  if ((int64_t)B * bt_stride <= kSmallEntries) {
+    shared_one_kernel<<<1, kOneThreads, 0, stream>>>(r);
+    return hipGetLastError();
   }
+  shared_sub_kernel<<<B, kRowThreads, 0, stream>>>(r);
+  shared_last_kernel<<<B, kRowThreads, 0, stream>>>(r);
+  shared_count_kernel<<<B, kRowThreads, 0, stream>>>(r);
+  shared_put_kernel<<<B, kRowThreads, 0, stream>>>(r);
   return hipGetLastError();
 }
 
