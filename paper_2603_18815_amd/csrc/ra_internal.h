@@ -137,7 +137,7 @@ hipError_t launch_table_release(const int32_t *lens, const int32_t *keep_lens,
 // ---- trees of drafted tokens ----
 constexpr int32_t kMaxDraftNodes = 1024;       // nodes of a tree
 struct TreePlan {
-  int32_t rows;           // query rows of a tile: 16, 32 or 256
+  int32_t rows;           // query rows of a tile: 16, 32, 128 or 256
   int32_t piece_rows;     // of them, those that the largest tree has
   bool direct;            // a workgroup a tile; otherwise equal shares of the work
   int64_t tiles;          // of the query rows of the largest tree, a KV head

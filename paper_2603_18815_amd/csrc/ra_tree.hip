@@ -74,7 +74,7 @@ __device__ __forceinline__ int block_cost(int rows) {
   return parts <= 3 ? 8 : parts == 4 ? 9 : parts <= 6 ? 12 : 16;
 }
 template <int kRows>
-__host__ __device__ constexpr int block_keys() { return kRows < 256 ? 128 : 64; }
+__host__ __device__ constexpr int block_keys() { return kRows <= 32 ? 128 : 64; }
 
 // A row's tiles on the line: all but the last have kRows query rows.
 template <int kRows>
@@ -111,6 +111,11 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
   return __builtin_bit_cast(int64_t, r);
 }
 
+// x / y of numbers that are not negative: by 32 bits where both have no more.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 __device__ __forceinline__ TreeRow uniform_row(const TreeArgs &a, int b) {
   TreeRow r = tree_row(a, b);
   r.first = uniform(r.first);
@@ -132,22 +137,28 @@ __device__ __forceinline__ void walk(const TreeArgs &a, WalkLds<kThreads> &lds, 
     if (tile < line.tiles) piece(b, row, tile, g, 0, line.blocks, -1);
     return;
   }
-  // the rows' places, kThreads rows at a time
+  // the rows' places, kThreads rows at a time; of up to 64 rows every wave works them all out
+  // (and writes the same to LDS), so that none waits for another
+  const bool few = a.B <= kWave;
   auto place = [&](int c0) {
+    const int i = few ? lane : tid;
     int64_t mine = 0;
-    if (c0 + tid < a.B) mine = RowLine<kRows>(tree_row(a, c0 + tid), a.group).length(a.hkv);
+    if (c0 + i < a.B) mine = RowLine<kRows>(tree_row(a, c0 + i), a.group).length(a.hkv);
     const int64_t sum = wave_sums(mine);
-    __syncthreads();
-    if (lane == kWave - 1) lds.part[wave] = sum;
-    __syncthreads();
-    int64_t before = 0, all = 0;
-    for (int w = 0; w < kThreads / kWave; ++w) {
-      if (w == wave) before = all;
-      all += lds.part[w];
+    int64_t before = 0, all = of_lane(sum, kWave - 1);
+    if (!few) {
+      __syncthreads();
+      if (lane == kWave - 1) lds.part[wave] = sum;
+      __syncthreads();
+      all = 0;
+      for (int w = 0; w < kThreads / kWave; ++w) {
+        if (w == wave) before = all;
+        all += lds.part[w];
+      }
     }
-    if (tid == 0) lds.begin[0] = 0;
-    lds.begin[tid + 1] = before + sum;
-    __syncthreads();
+    if (i == 0) lds.begin[0] = 0;
+    lds.begin[i + 1] = before + sum;
+    if (!few) __syncthreads();
     return uniform(all);
   };
   int64_t all = 0;
@@ -156,7 +167,7 @@ __device__ __forceinline__ void walk(const TreeArgs &a, WalkLds<kThreads> &lds, 
     if (s == 0 && c0 + tid < a.B) a.start[c0 + tid] = all + lds.begin[tid];
     all += n;
   }
-  const int64_t even = (all + gridDim.x - 1) / gridDim.x;
+  const int64_t even = quotient(all + gridDim.x - 1, gridDim.x);
   const int64_t share = even > a.min_share ? even : a.min_share;
   if (s == 0 && tid == 0) *a.share = share;
   const int64_t s0 = uniform(s * share), s1 = uniform(min(all, s0 + share));
@@ -182,15 +193,15 @@ __device__ __forceinline__ void walk(const TreeArgs &a, WalkLds<kThreads> &lds, 
         // its first tile and KV head that end behind s0
         const int64_t off = s0 > begin ? s0 - begin : 0;
         const int64_t full = line.before(1, 0, a.hkv);       // of a tile that is not the last
-        int tile = uniform(line.tiles > 1 ? (int)min((int64_t)line.tiles - 1, off / full) : 0);
-        int g = uniform((int)((off - line.before(tile, 0, a.hkv)) / ((int64_t)line.cost(tile) * line.blocks)));
+        int tile = uniform(line.tiles > 1 ? (int)min((int64_t)line.tiles - 1, quotient(off, full)) : 0);
+        int g = uniform((int)quotient(off - line.before(tile, 0, a.hkv), (int64_t)line.cost(tile) * line.blocks));
         for (; tile < line.tiles; ++tile, g = 0)
           for (; g < a.hkv; ++g) {
             const int64_t at = begin + line.before(tile, g, a.hkv);
             if (at >= s1) return;
             const int cost = line.cost(tile);
-            const int b0 = uniform(at >= s0 ? 0 : (int)((s0 - at + cost - 1) / cost));
-            const int b1 = uniform((int)min((int64_t)line.blocks, (s1 - at + cost - 1) / cost));
+            const int b0 = uniform(at >= s0 ? 0 : (int)quotient(s0 - at + cost - 1, cost));
+            const int b1 = uniform((int)min((int64_t)line.blocks, quotient(s1 - at + cost - 1, cost)));
             if (b0 >= b1) continue;
             piece(b, row, tile, g, b0, b1, b0 == 0 && b1 == line.blocks ? -1 : 2 * s + (b0 == 0));
           }
@@ -308,10 +319,13 @@ __device__ __forceinline__ void narrow_piece(const TreeArgs &a, TreeLds<kTiles> 
   // A pair's keys are loaded while the pair before meets its values, its values while it meets
   // its own keys.
   size_t kbase = 0, vbase = 0;
-  auto pages = [&](int pr) __attribute__((always_inline)) {
+  int id0 = 0, id1 = 0;                     // of the pair whose loads come next
+  auto ids = [&](int pr) __attribute__((always_inline)) {
     const int pg = t0 / kPage + 2 * pr;
-    const int id0 = page_at(bt, pg, a.num_pages);
-    const int id1 = page_at(bt, min(pg + 1, row_pages - 1), a.num_pages);
+    id0 = page_at(bt, min(pg, row_pages - 1), a.num_pages);
+    id1 = page_at(bt, min(pg + 1, row_pages - 1), a.num_pages);
+  };
+  auto pages = [&]() __attribute__((always_inline)) {
     kbase = ((size_t)(ka_sel ? id1 : id0) * a.hkv + g) * head_stride;
     vbase = ((size_t)(sv_sel ? id1 : id0) * a.hkv + g) * head_stride;
   };
@@ -352,9 +366,11 @@ __device__ __forceinline__ void narrow_piece(const TreeArgs &a, TreeLds<kTiles> 
     }
   };
   if (wave < npairs) {
-    pages(wave);
+    ids(wave);
+    pages();
     load_k();
     load_v();
+    ids(wave + kSplitWaves);
   }
   // kMore: another pair follows (a load under a condition would make the waits of what is not
   // under it wait for it too)
@@ -383,8 +399,9 @@ __device__ __forceinline__ void narrow_piece(const TreeArgs &a, TreeLds<kTiles> 
       }
     keep_order();
     if constexpr (kMore) {
-      pages(pr + kSplitWaves);
+      pages();
       load_k();
+      ids(pr + 2 * kSplitWaves);
     }
     keep_order();
     if constexpr (kFp8) {
@@ -521,9 +538,9 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_narrow_kernel(Tre
 }
 
 // ---- wide tiles ----
-// 256 query rows of one KV head, by eight waves of 32 rows each: the columns of 32 x 32 matrix
-// tiles, their queries in registers. Blocks of 64 keys are loaded straight into a ring of four
-// LDS buffers, three blocks ahead, one barrier a block:
+// 32 kW query rows of one KV head, by kW waves of 32 rows each: the columns of 32 x 32 matrix
+// tiles, their queries in registers. Blocks of 64 keys are loaded straight into a ring of LDS
+// buffers, one barrier a block:
 //   S^T[key][row] = K[key][:] . Q^T[:][row]       (8 products of 32 x 32 x 16 for 32 keys)
 //   O^T[d][row]  += V^T[d][key] . P^T[key][row]   (8, twice: the weights' two bf16 parts)
 // Keys are ordered inside a pair of pages so that the 16 scores of a lane are the weights it
@@ -531,23 +548,25 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_narrow_kernel(Tre
 // waves that have none of their own, and join them at the end. The running maximum moves
 // only when a score passes it by 8 (in powers of two), so that O is rescaled rarely; weights
 // are at most 2^8 then.
+// kW is 4 for trees of up to 128 query rows, two workgroups a compute unit, each of which works
+// while the other waits, and 8 (a ring of four, three blocks ahead) for larger ones.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-constexpr int kWideWaves = 8, kWideThreads = kWideWaves * kWave;
-constexpr int kWideRows = 32 * kWideWaves;
 constexpr int kWideKeys = 64, kWidePages = kWideKeys / kPage, kWidePairs = kWideKeys / kPair;
-constexpr int kRing = 4;
 constexpr int kPageElems = kPage * kHeadDim;
 constexpr float kSlack = 8.f;
 
+template <int kW>
 struct WideLds {
+  static constexpr int kRing = kW == 8 ? 4 : 2;
   union {
     __attribute__((aligned(16))) uint16_t in[kRing][2 * kWidePages][kPageElems];   // K, then V
-    __attribute__((aligned(16))) float o[kWideWaves][32][kOPitch];
+    __attribute__((aligned(16))) float o[kW][32][kOPitch];
   };
-  float m[kWideWaves][32], l[kWideWaves][32];
-  WalkLds<kWideThreads> walk;
+  float m[kW][32], l[kW][32];
+  WalkLds<kW * kWave> walk;
 };
-static_assert(sizeof(WideLds) <= 160 * 1024, "LDS of a compute unit");
+static_assert(sizeof(WideLds<8>) <= 160 * 1024 && sizeof(WideLds<4>) <= 80 * 1024,
+              "LDS of a compute unit, for one workgroup and for two");
 
 // LDS places. Unit c (16 bytes) of key `slot` of a page is at 16 slot + (c ^ slot), half h of value
 // row d at 2 d + (h ^ bit 3 of d): 16 lanes that read together meet no bank twice. Codes (fp8): 8
@@ -566,10 +585,11 @@ __device__ __forceinline__ float pair_max(float x) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <bool kFp8>
-__device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int b,
+template <int kW, bool kFp8>
+__device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds<kW> &lds, int b,
                                            const TreeRow &row, int tile, int g, int blk0, int blk1,
                                            int place) {
+  constexpr int kWideRows = 32 * kW, kThreads = kW * kWave, kRing = WideLds<kW>::kRing;
   const int G = a.group, r0 = tile * kWideRows, rows = min(row.T * G - r0, kWideRows);
   const int end = row.ctx + row.T;
   const int t0 = blk0 * kWideKeys, t1 = min(end, blk1 * kWideKeys), nblocks = blk1 - blk0;
@@ -581,9 +601,9 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
   const int row_pages = (t1 + kPage - 1) / kPage;
   const int32_t *bt = a.block_table + (size_t)b * a.bt_stride;
 
-  // Which rows and which pairs of a block are this wave's: 8 / parts waves share a part, or one
+  // Which rows and which pairs of a block are this wave's: kW / parts waves share a part, or one
   // more; the parts with fewer have the first waves, which do more and lie on different SIMDs.
-  const int parts = (rows + 31) / 32, base = kWideWaves / parts, extra = kWideWaves % parts;
+  const int parts = (rows + 31) / 32, base = kW / parts, extra = kW % parts;
   const int few = parts - extra, heavy = few * base;
   const bool first_waves = wave < heavy;
   const int part = first_waves ? extra + wave % few : (wave - heavy) % extra;
@@ -603,14 +623,13 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(q[kk]));
   }
-  // ---- loads: a wave the keys or the values of one page of the block, 1 KB an instruction,
-  // each lane the unit that belongs to its place in LDS
-  constexpr int kLoads = kFp8 ? 2 : 4;
-  const int my_page = wave >> 1, is_v = wave & 1;
+  // ---- loads: a wave the keys or the values of one page of the block (of four waves both), 1 KB
+  // an instruction, each lane the unit that belongs to its place in LDS
+  constexpr int kLoads = kFp8 ? 2 : 4;          // of a page's keys or values
+  constexpr int kBoth = kW == 8 ? 1 : 2;
+  const int my_page = kW == 8 ? wave >> 1 : wave, my_kind = kW == 8 ? wave & 1 : 0;
   // the unit in the i-th KB at this lane's place: of values the same in each, of keys xor 4 i
-  const uint32_t unit = is_v ? (kFp8 ? lane : lane ^ (lane >> 4 & 1)) : lane ^ (lane >> 4);
-  const uint32_t turn = is_v ? 0 : 64;
-  const uint16_t *pool = is_v ? a.v_pool : a.k_pool;
+  const uint32_t k_unit = lane ^ (lane >> 4), v_unit = kFp8 ? lane : lane ^ (lane >> 4 & 1);
   const uint32_t ring = lds_address(lds.in[0][0]);
   constexpr uint32_t kPageBytes = 2 * kPageElems, kBlockBytes = 2 * kWidePages * kPageBytes;
   auto page_id = [&](int blk) {
@@ -619,16 +638,24 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
   int next_id = page_id(0);
   auto load = [&](int blk) __attribute__((always_inline)) {
     const size_t at = ((size_t)next_id * a.hkv + g) * kPageElems;
-    const uint16_t *base = pool + (kFp8 ? at / 2 : at);
-    const uint32_t to = __builtin_amdgcn_readfirstlane(
-        ring + blk % kRing * kBlockBytes + (is_v * kWidePages + my_page) * kPageBytes);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) load_to_lds(base, (16 * unit ^ turn * i) + 1024 * i, to + i * 1024);
-    next_id = page_id(blk + 1);
+    for (int j = 0; j < kBoth; ++j) {
+      const int is_v = kBoth == 2 ? j : my_kind;
+      const uint32_t unit = is_v ? v_unit : k_unit, turn = is_v ? 0 : 64;
+      const uint16_t *base = (is_v ? a.v_pool : a.k_pool) + (kFp8 ? at / 2 : at);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(
+          ring + blk % kRing * kBlockBytes + (is_v * kWidePages + my_page) * kPageBytes);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        load_to_lds(base, (16 * unit ^ turn * i) + 1024 * i, to + i * 1024);
+    }
   };
 #pragma unroll
   for (int i = 0; i < kRing - 1; ++i)
-    if (i < nblocks) load(i);
+    if (i < nblocks) {
+      load(i);
+      next_id = page_id(i + 1);
+    }
 
   uint32_t odd = 0;                             // infinite or NaN values of nodes
 
@@ -758,7 +785,7 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
   int mine = share;
   for (int blk = 0; blk < nblocks; ++blk) {
     // this block's loads are done: of those behind them kLoads a block may be on their way
-    const int behind = nblocks - 1 - blk;
+    const int behind = min(kRing - 2, nblocks - 1 - blk);
     if (behind >= 2)
       await_loads_before<2 * kLoads>();
     else if (behind == 1)
@@ -772,6 +799,9 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
     int pp = mine - 2 * blk;
     if (pp < pairs) read_k(blk, pp);
     for (; pp < pairs; pp += shares, mine += shares) pair(blk, pp, pp + shares < pairs);
+    // (the next page's id here, where nothing from LDS is waited for)
+    keep_order();
+    next_id = page_id(blk + kRing);
   }
   __syncthreads();
 
@@ -792,11 +822,11 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
   }
   auto first_wave = [&](int p) { return p >= extra ? p - extra : heavy + p; };
   if (__syncthreads_or(odd != 0)) {
-    reach_odd<kFp8, kWideThreads>(a, row, bt, g, t0, t1, r0, rows,
+    reach_odd<kFp8, kThreads>(a, row, bt, g, t0, t1, r0, rows,
                                   [&](int c) { return &lds.o[first_wave(c >> 5)][c & 31][0]; });
     __syncthreads();
   }
-  for (int idx = tid; idx < rows * (kHeadDim / 4); idx += kWideThreads) {
+  for (int idx = tid; idx < rows * (kHeadDim / 4); idx += kThreads) {
     const int c = idx / (kHeadDim / 4), d = idx % (kHeadDim / 4) * 4;
     const bool of_first = c >> 5 >= extra;     // the part's waves
     const int w0 = first_wave(c >> 5), step = of_first ? few : extra;
@@ -828,14 +858,14 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds &lds, int 
   __syncthreads();                              // the next piece's loads go there
 }
 
-template <bool kFp8>
-__global__ __launch_bounds__(kWideThreads) void tree_wide_kernel(TreeArgs a) {
-  __shared__ __attribute__((aligned(1024))) WideLds lds;
-  walk<kWideRows>(a, lds.walk,
-                  [&](int b, const TreeRow &row, int tile, int g, int blk0, int blk1, int place)
-                      __attribute__((always_inline)) {
-                        wide_piece<kFp8>(a, lds, b, row, tile, g, blk0, blk1, place);
-                      });
+template <int kW, bool kFp8>
+__global__ __launch_bounds__(kW * kWave, 2) void tree_wide_kernel(TreeArgs a) {
+  __shared__ __attribute__((aligned(1024))) WideLds<kW> lds;
+  walk<32 * kW>(a, lds.walk,
+                [&](int b, const TreeRow &row, int tile, int g, int blk0, int blk1, int place)
+                    __attribute__((always_inline)) {
+                      wide_piece<kW, kFp8>(a, lds, b, row, tile, g, blk0, blk1, place);
+                    });
 }
 
 // Joins the pieces of one node and head, a wave each: the weights of up to 64 pieces are worked
@@ -854,8 +884,8 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs 
   const RowLine<kRows> line(row, a.group);
   const int g = h / a.group, r = (t - row.first) * a.group + h - g * a.group, tile = r / kRows;
   const int64_t share = *a.share, begin = a.start[b] + line.before(tile, g, a.hkv);
-  const int64_t first = begin / share;
-  const int n = (int)((begin + (int64_t)(line.blocks - 1) * line.cost(tile)) / share - first) + 1;
+  const int64_t first = quotient(begin, share);
+  const int n = (int)(quotient(begin + (int64_t)(line.blocks - 1) * line.cost(tile), share) - first) + 1;
   if (n == 1) return;
   // piece i's result, query row r of its tile: the first piece is the last of its share
   auto piece = [&](int i) { return (size_t)(2 * (first + i) + (i == 0)) * a.piece_rows + (r - tile * kRows); };
@@ -915,7 +945,7 @@ constexpr int kMinShareKeys = 256;          // of a tile, where there is little 
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len) {
   const int64_t rows = (int64_t)max_q_len * (hq / hkv);
   TreePlan p;
-  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kWideRows;
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
   p.tiles = (rows + p.rows - 1) / p.rows;
   p.piece_rows = (int32_t)(rows < p.rows ? rows : p.rows);
   p.direct = max_kv_len <= kDirectKeys;
@@ -927,8 +957,10 @@ TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_
     plan_line<16>(p, units, max_kv_len, 512);
   else if (p.rows == 32)
     plan_line<32>(p, units, max_kv_len, 512);
+  else if (p.rows == 128)
+    plan_line<128>(p, units, max_kv_len, 512);
   else
-    plan_line<kWideRows>(p, units, max_kv_len, 256);
+    plan_line<256>(p, units, max_kv_len, 256);
   return p;
 }
 
@@ -968,7 +1000,9 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
                                        up256(((size_t)B + 1) * sizeof(int64_t)));
     a.ws_ml = reinterpret_cast<float2 *>(a.ws_o + (size_t)2 * p.groups * p.piece_rows * kHeadDim);
   }
-  a.min_share = p.rows == kWideRows ? kMinShareKeys / kWideKeys * 16 : kMinShareKeys / block_keys<16>();
+  a.min_share = p.rows == 256   ? kMinShareKeys / kWideKeys * 16
+                : p.rows == 128 ? kMinShareKeys / kWideKeys
+                                : kMinShareKeys / block_keys<16>();
   a.B = B;
   a.hq = hq;
   a.hkv = kv.hkv;
@@ -984,30 +1018,34 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
   a.direct = p.direct;
   a.scale_log2 = scale * kLog2e * kv.k_scale;
   a.v_scale = kv.v_scale;
-  const dim3 grid((unsigned)p.groups), block(kSplitWaves * kWave);
+  const dim3 grid((unsigned)p.groups);
   const int64_t heads = (int64_t)total_q * hq;
   const dim3 join_grid((unsigned)((heads + kJoinWaves - 1) / kJoinWaves)), join(kJoinWaves * kWave);
-  if (p.rows == kWideRows && kv.fp8)
-    tree_wide_kernel<true><<<grid, kWideThreads, 0, stream>>>(a);
-  else if (p.rows == kWideRows)
-    tree_wide_kernel<false><<<grid, kWideThreads, 0, stream>>>(a);
-  else if (p.rows == 32 && kv.fp8)
-    tree_narrow_kernel<2, true><<<grid, block, 0, stream>>>(a);
-  else if (p.rows == 32)
-    tree_narrow_kernel<2, false><<<grid, block, 0, stream>>>(a);
-  else if (kv.fp8)
-    tree_narrow_kernel<1, true><<<grid, block, 0, stream>>>(a);
-  else
-    tree_narrow_kernel<1, false><<<grid, block, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.direct) return e;
-  if (p.rows == kWideRows)
-    tree_join_kernel<kWideRows><<<join_grid, join, 0, stream>>>(a);
-  else if (p.rows == 32)
-    tree_join_kernel<32><<<join_grid, join, 0, stream>>>(a);
-  else
-    tree_join_kernel<16><<<join_grid, join, 0, stream>>>(a);
-  return hipGetLastError();
+  auto launch = [&](auto rows) {
+    constexpr int kRows = decltype(rows)::value;
+    if constexpr (kRows > 32) {
+      constexpr int kW = kRows / 32;
+      if (kv.fp8)
+        tree_wide_kernel<kW, true><<<grid, kW * kWave, 0, stream>>>(a);
+      else
+        tree_wide_kernel<kW, false><<<grid, kW * kWave, 0, stream>>>(a);
+    } else {
+      if (kv.fp8)
+        tree_narrow_kernel<kRows / 16, true><<<grid, kSplitWaves * kWave, 0, stream>>>(a);
+      else
+        tree_narrow_kernel<kRows / 16, false><<<grid, kSplitWaves * kWave, 0, stream>>>(a);
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.direct) return e;
+    tree_join_kernel<kRows><<<join_grid, join, 0, stream>>>(a);
+    return hipGetLastError();
+  };
+  switch (p.rows) {
+    case 16: return launch(std::integral_constant<int, 16>{});
+    case 32: return launch(std::integral_constant<int, 32>{});
+    case 128: return launch(std::integral_constant<int, 128>{});
+    default: return launch(std::integral_constant<int, 256>{});
+  }
 }
 
 }  // namespace ra

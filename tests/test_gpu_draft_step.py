@@ -1,0 +1,266 @@
+"""The operators of a speculative step as a rollout uses them: together, captured, on other
+streams.
+
+Rollouts of one prompt: its row's pages are forked, every step checks a drafted tree a row, and
+the tokens it emits must be those of greedy decode one token at a time, with penalties, a bias
+and a grammar mask on the logits.
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_18815_amd as ra
+from tests.draft_util import DEV, Cache, ancestors, cu, i32, pack, random_tree
+
+pytestmark = pytest.mark.gpu
+B, HQ, HKV, V, STRIDE, PROMPT, MOST = 3, 8, 2, 700, 16, 37, 60
+T = [9, 1, 6]                                       # nodes of the rows' trees
+CU = cu(T)
+PARENTS = [[-1, 0, 1, 1, 0, 2, 5, 4, 6], [-1], [-1, 0, 0, 1, 3, 4]]
+CHAINS = [[1, 2, 5, 6, 8], [], [1, 3, 4, 5]]        # the longest way down from the root
+
+
+class Rollouts:
+    def __init__(self, seed, fp8=False):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        rnd = lambda *s: torch.randn(s, generator=g, device=DEV)
+        self.q, self.k, self.v = (rnd(V, h, 128).bfloat16() for h in (HQ, HKV, HKV))
+        self.head = rnd(HQ * 128, V) / math.sqrt(HQ * 128) * 6
+        pages = B * STRIDE
+        self.table = torch.zeros((B, STRIDE), dtype=torch.int32, device=DEV)
+        self.free = torch.randperm(pages, generator=g, device=DEV).to(torch.int32)
+        self.count, self.shares = i32([pages]), torch.zeros(pages, dtype=torch.int32, device=DEV)
+        z = lambda *s: torch.zeros(s, dtype=torch.uint8 if fp8 else torch.bfloat16, device=DEV)
+        self.kv = ra.PagedKV(z(pages, HKV, 16, 128), z(pages, HKV, 128, 16), self.table,
+                             *((0.05, 0.05) if fp8 else ()))
+        rng = np.random.default_rng(seed)
+        prompt = rng.integers(0, V, PROMPT)
+        self.history = torch.zeros((B, MOST + PROMPT + 16), dtype=torch.int32, device=DEV)
+        self.history[:, :PROMPT] = i32(prompt)
+        self.lens, self.prompt_lens = i32([PROMPT] * B), i32([PROMPT] * B)
+        self.root = i32([5, 300, 77])
+        self.f32 = lambda x: torch.tensor(x, dtype=torch.float32, device=DEV)
+        self.rep, self.freq, self.pres = self.f32([1.2, 1.0, 1.5]), self.f32([0.3, 0.5, 0.0]), self.f32([0.0, 0.4, 0.2])
+        self.bias_tokens, self.bias_values, self.cu_bias = i32([4, 9, 4]), self.f32([2.0, -3.0, 1.0]), i32([0, 2, 2, 3])
+        self.allowed = i32(rng.integers(-2**31, 2**31, (1, -(-V // 32))))
+        self.greedy, self.u = self.f32([0.0] * sum(T)), self.f32([0.5] * sum(T))
+        self.parents, self.cu = i32(sum(PARENTS, [])), i32(CU)
+        self.num_new, self.zero = i32(T), i32([0] * B)
+        # the prompt, in row 0, then its pages for the others
+        t = torch.as_tensor(prompt, device=DEV)
+        ra.block_table_extend(self.table[:1], i32([0]), i32([PROMPT]), self.free, self.count,
+                              total_new=PROMPT)
+        self.kv.block_table = self.table
+        ra.kv_page_write(self.k[t], self.v[t], i32([0, PROMPT]), i32([0]), self.kv, PROMPT, PROMPT)
+        src, dst, taken = ra.block_table_fork(self.table, i32([0, 0]), i32([1, 2]),
+                                              i32([PROMPT] * 2), self.shares, self.free, self.count)
+        ra.kv_page_copy(self.kv, src, dst)
+        assert taken.tolist() == [2] and int(self.shares.sum()) == 2 * (PROMPT // 16)
+
+    def adjust(self, logits, **trees):
+        rows = i32([0] * logits.shape[0]) if not trees else trees.pop("rows")
+        return ra.token_logits_adjust(
+            logits, self.history, self.hist_lens, self.prompt_lens, self.rep, self.freq, self.pres,
+            self.bias_tokens, self.bias_values, self.cu_bias, self.allowed, rows, out=logits, **trees)
+
+    def decode(self, steps):
+        """Greedy, one token a step; the tokens that follow the roots, [steps][B]."""
+        lens, root, emitted, gap = self.lens.clone(), self.root.clone(), [], math.inf
+        for _ in range(steps):
+            c, kv_lens, _, taken = ra.block_table_extend(self.table, lens, i32([1] * B), self.free,
+                                                         self.count, total_new=B)
+            assert int(taken) >= 0
+            t = root.long()
+            ra.kv_page_write(self.k[t], self.v[t], c, lens, self.kv, 1, STRIDE * 16)
+            out, _ = ra.decode(self.q[t], self.kv, kv_lens, STRIDE * 16)
+            self.history[torch.arange(B, device=DEV), lens.long()] = root
+            self.hist_lens = kv_lens
+            logits = self.adjust(out.view(B, -1) @ self.head)
+            top = torch.topk(logits, 2, dim=1).values
+            gap = min(gap, float((top[:, 0] - top[:, 1]).min()))
+            root, _ = ra.token_sample(logits, self.u[:B], self.greedy[:B])
+            emitted.append(root.tolist())
+            lens = kv_lens
+        return np.array(emitted), gap
+
+    def step(self, draft):
+        """One step over trees of these drafted tokens (behind the roots'). All on the device."""
+        tokens = draft.clone()
+        tokens[self.cu[:-1].long()] = self.root
+        c, kv_lens, _, self.taken = ra.block_table_extend(self.table, self.lens, self.num_new,
+                                                          self.free, self.count, total_new=sum(T))
+        mask, self.positions = ra.draft_tree_mask(self.parents, c, self.lens, max_q_len=max(T))
+        t = tokens.long()
+        ra.kv_page_write(self.k[t], self.v[t], c, self.lens, self.kv, max(T), STRIDE * 16)
+        out, _ = ra.decode_tree(self.q[t], c, self.lens, mask, self.kv, max_q_len=max(T),
+                                max_kv_len=STRIDE * 16)
+        self.hist_lens = self.lens
+        logits = self.adjust(out.view(sum(T), -1) @ self.head, rows=self.zero[:1].expand(sum(T)).contiguous(),
+                             cu_rows=c, draft_tokens=tokens, tree_mask=mask)
+        chosen, _ = ra.token_sample(logits, self.u, self.greedy)
+        path, emitted, accepted, new_lens, nxt = ra.draft_tree_accept(
+            self.parents, tokens, chosen, c, self.lens, max_q_len=max(T))
+        ra.kv_page_compact(self.kv, self.lens, c, path, accepted, max_count=max(T))
+        released = ra.block_table_release_shared(self.table, kv_lens, new_lens, self.shares,
+                                                 self.free, self.count)
+        # the accepted nodes' tokens into the histories, what is behind them overwritten later
+        row = torch.repeat_interleave(torch.arange(B, device=DEV), self.num_new.long(),
+                                      output_size=sum(T))
+        i = torch.arange(sum(T), device=DEV) - c.long()[row]
+        node = (c.long()[row] + path.long().clamp(min=0))
+        self.history[row, self.lens.long()[row] + i] = tokens[node]
+        self.lens.copy_(new_lens)
+        self.root.copy_(nxt)
+        return path, emitted, accepted, released
+
+    def state(self):
+        return [self.table, self.free, self.count, self.shares, self.kv.k_pool, self.kv.v_pool,
+                self.history, self.lens, self.root]
+
+
+def clear(first, fp8=False):
+    """A seed from `first` on whose greedy choices are all by more than 1e-3 (the logits of the two
+    ways differ by 1e-5), and the tokens chosen."""
+    for seed in range(first, first + 20):
+        truth, gap = Rollouts(seed, fp8).decode(MOST)
+        if gap > 1e-3:
+            return seed, truth
+    raise AssertionError("no clear choices")
+
+
+def drafts(rng, truth, at):
+    """Drafted tokens: on the longest way down the right ones, as far as a random place."""
+    draft, right = rng.integers(0, V, sum(T)), []
+    for b in range(B):
+        n = int(rng.integers(0, len(CHAINS[b]) + 1))
+        for j in range(n):
+            draft[CU[b] + CHAINS[b][j]] = truth[at[b] + j][b]
+        right.append(n)
+    return i32(draft), right
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_trees_emit_the_tokens_of_decode(device, fp8):
+    seed, truth = clear(3, fp8)
+    r, rng, at = Rollouts(seed, fp8), np.random.default_rng(1), [0] * B
+    for _ in range(8):
+        draft, right = drafts(rng, truth, at)
+        path, emitted, accepted, _ = r.step(draft)
+        assert int(r.taken) >= 0
+        for b in range(B):
+            n = int(accepted[b])
+            assert n >= right[b] + 1
+            assert path[CU[b]:CU[b] + n].tolist()[:right[b] + 1] == [0] + CHAINS[b][:right[b]]
+            assert emitted[CU[b]:CU[b] + n].tolist() == truth[at[b]:at[b] + n, b].tolist()
+            at[b] += n
+        assert r.lens.tolist() == [PROMPT + n for n in at]
+    assert max(at) > 16                              # pages were filled behind the shared ones
+    ra.block_table_release_shared(r.table, r.lens, r.zero, r.shares, r.free, r.count)
+    assert int(r.count) == B * STRIDE and not bool(r.shares.any())
+
+
+def test_captured_steps_equal_eager_ones(device):
+    truth, _ = Rollouts(4).decode(MOST)
+    want, got = Rollouts(4), Rollouts(4)
+    rng = np.random.default_rng(2)
+    inputs, at = [], [0] * B
+    for _ in range(6):
+        draft, _ = drafts(rng, truth, at)
+        _, _, accepted, _ = want.step(draft)
+        inputs.append(draft)
+        at = [x + int(n) for x, n in zip(at, accepted)]
+    draft = inputs[0].clone()
+    backup = [t.clone() for t in got.state()]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got.step(draft)                              # warm up, then back to the beginning
+        for t, old in zip(got.state(), backup):
+            t.copy_(old)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        path, emitted, accepted, released = got.step(draft)
+    again, at = Rollouts(4), [0] * B
+    for step in range(6):
+        draft.copy_(inputs[step])
+        graph.replay()
+        p, e, a, rel = again.step(inputs[step])      # eager work between the replays
+        for x, y in ((path, p), (emitted, e), (accepted, a), (released, rel)):
+            assert torch.equal(x, y)
+        for x, y in zip(got.state(), again.state()):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+        torch.cuda.synchronize()
+
+
+def test_graphs_that_share_a_workspace(device):
+    """Two captured calls with one workspace, replayed in turn."""
+    ctx, nodes = [900, 2000, 40], [12, 5, 30]
+    cache = Cache(5, [c + t for c, t in zip(ctx, nodes)], 2)
+    rng = np.random.default_rng(5)
+    mask = torch.as_tensor(pack([ancestors(random_tree(rng, t)) for t in nodes], 1), device=DEV)
+    qs = [torch.randn((47, h, 128), device=DEV).bfloat16() for h in (4, 16)]
+    size = max(ra.decode_tree_workspace_size(3, q.shape[1], 2, 47, 30, 2005) for q in qs)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    kv, c, x = cache.kv(), i32(cu(nodes)), i32(ctx)
+    outs = [torch.empty((47, q.shape[1], 128), device=DEV) for q in qs]
+    call = lambda i, out: ra.decode_tree(qs[i], c, x, mask, kv, 30, 2005, out=out, workspace=ws)
+    want = [call(i, torch.empty_like(outs[i]))[0].clone() for i in range(2)]
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(i, outs[i])
+        graphs.append(g)
+    for _ in range(3):
+        for i in (0, 1, 1, 0):
+            outs[i].fill_(float("nan"))
+            graphs[i].replay()
+            assert torch.equal(outs[i], want[i])
+
+
+def test_other_streams(device):
+    """stream=: outputs of the stream's own memory, ordered behind what is pending on it."""
+    ctx, nodes = [700, 64], [20, 9]
+    cache = Cache(6, [c + t for c, t in zip(ctx, nodes)], 2)
+    rng = np.random.default_rng(6)
+    parents = [random_tree(rng, t) for t in nodes]
+    p, c, x, kv = i32(np.concatenate(parents)), i32(cu(nodes)), i32(ctx), cache.kv()
+    q = torch.randn((29, 8, 128), device=DEV).bfloat16()
+    z = torch.randn((29, 5000), device=DEV)
+    hist, hl, f = i32(rng.integers(0, 5000, (2, 300))), i32([300, 120]), torch.ones(2, device=DEV)
+    tok, chosen = i32(rng.integers(0, 3, 29)), i32(rng.integers(0, 3, 29))
+
+    def run(stream):
+        mask, pos = ra.draft_tree_mask(p, c, x, max_q_len=20, stream=stream)
+        out, lse = ra.decode_tree(q, c, x, mask, kv, 20, 720, want_lse=True, stream=stream)
+        adj = ra.token_logits_adjust(z, hist, hl, frequency=f, cu_rows=c, draft_tokens=tok,
+                                     tree_mask=mask, stream=stream)
+        return [mask, pos, out, lse, adj, *ra.draft_tree_accept(p, tok, chosen, c, x, max_q_len=20,
+                                                                stream=stream)]
+    want = run(None)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        s = torch.cuda.Stream()
+        got = run(s)
+        s.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def test_two_calls_at_once(device):
+    """The same call on two streams, each with its own workspace."""
+    ctx, nodes = [3000] * 4, [8] * 4
+    cache = Cache(7, [3008] * 4, 2)
+    mask = torch.as_tensor(pack([np.tril(np.ones((8, 8), bool))] * 4, 1), device=DEV)
+    kv, c, x = cache.kv(), i32(cu(nodes)), i32(ctx)
+    qs = [torch.randn((32, 8, 128), device=DEV).bfloat16() for _ in range(2)]
+    want = [ra.decode_tree(q, c, x, mask, kv, 8, 3008)[0] for q in qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[ra.decode_tree(q, c, x, mask, kv, 8, 3008, stream=s)[0] for q, s in zip(qs, streams)]
+           for _ in range(10)]
+    torch.cuda.synchronize()
+    for pair in got:
+        assert all(torch.equal(a, b) for a, b in zip(pair, want))

@@ -142,6 +142,19 @@ def test_shorter_bounds_and_unused_rows(device):
     assert torch.equal(a[0], b[0])
 
 
+@pytest.mark.parametrize("Hq,Hkv,most", [(2, 1, 6), (4, 2, 10), (8, 2, 30), (16, 1, 30)])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_many_rows(device, Hq, Hkv, most, fp8):
+    """More rows than a workgroup has threads, empty ones among them, cut at many places."""
+    rng = np.random.default_rng(most)
+    B = 600
+    T = [int(x) if rng.random() < 0.7 else 0 for x in rng.integers(0, most + 1, B)]
+    ctx = [int(x) if rng.random() < 0.8 else 0 for x in rng.integers(0, 600, B)]
+    ctx[7], T[7] = 5000, most
+    cache, q, masks, bits = inputs(16, Hq, Hkv, ctx, T, fp8)
+    check(cache, q, masks, bits, ctx, T)
+
+
 def test_largest_tree(device):
     ctx, T = [77], [1024]
     check(*(lambda c, q, m, b: (c, q, m, b, ctx, T))(*inputs(13, 4, 2, ctx, T)))
