@@ -554,6 +554,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kWideKeys = 64, kWidePages = kWideKeys / kPage, kWidePairs = kWideKeys / kPair;
 constexpr int kPageElems = kPage * kHeadDim;
 constexpr float kSlack = 8.f;
+constexpr int kBeside = 10;                 // vector instructions beside a product
 
 template <int kW>
 struct WideLds {
@@ -622,7 +623,12 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds<kW> &lds, 
     // arrived before the loads to LDS begin: a wait for them later would wait for those too
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(q[kk]));
+    if (a.scale_log2 < 0.f)                     // the scale's sign, so that c below has none
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+        q[kk] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[kk]) ^ 0x80008000u);
   }
+  const float c = fabsf(a.scale_log2);
   // ---- loads: a wave the keys or the values of one page of the block (of four waves both), 1 KB
   // an instruction, each lane the unit that belongs to its place in LDS
   constexpr int kLoads = kFp8 ? 2 : 4;          // of a page's keys or values
@@ -672,15 +678,17 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds<kW> &lds, 
   const int slot = key & 15;
   const uint32_t k_at = (key >> 4) * kPageBytes + 16 * (kFp8 ? slot * 8 + (grp ^ (slot >> 1)) : slot * 16 + (grp ^ slot));
   const uint32_t v_at = kWidePages * kPageBytes + 16 * (kFp8 ? 32 * grp + col : 2 * col + (grp ^ (col >> 3 & 1)));
-  u32x4 kraw[kKReads];
-  auto read_k = [&](int blk, int pp) __attribute__((always_inline)) {
+  struct Keys {
+    u32x4 raw[kKReads];
+  };
+  auto read_k = [&](int blk, int pp, Keys &k) __attribute__((always_inline)) {
     const uint32_t at = ring + blk % kRing * kBlockBytes + 2 * pp * kPageBytes + k_at;
 #pragma unroll
-    for (int i = 0; i < kKReads; ++i) kraw[i] = read_lds(at ^ (32 * i));   // unit 2 i + grp
+    for (int i = 0; i < kKReads; ++i) k.raw[i] = read_lds(at ^ (32 * i));   // unit 2 i + grp
   };
   // Reads are issued a phase ahead: the values before the scores' products, the next pair's keys
   // behind them.
-  auto pair = [&](int blk, int pp, bool more) __attribute__((always_inline)) {
+  auto pair = [&](int blk, int pp, bool more, Keys &keys) __attribute__((always_inline)) {
     const int tok = t0 + blk * kWideKeys + pp * kPair;
     const bool tail = tok + kPair > row.ctx;
     u32x4 vraw[kFp8 ? 4 : 8];
@@ -703,16 +711,16 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds<kW> &lds, 
     for (int kk = 0; kk < 8; ++kk) {
       bf16x8 k;
       if constexpr (kFp8)
-        k = fp8x8_to_bf16x8(u32x2{kraw[kk >> 1][2 * (kk & 1)], kraw[kk >> 1][2 * (kk & 1) + 1]});
+        k = fp8x8_to_bf16x8(u32x2{keys.raw[kk >> 1][2 * (kk & 1)], keys.raw[kk >> 1][2 * (kk & 1) + 1]});
       else
-        k = __builtin_bit_cast(bf16x8, kraw[kk]);
+        k = __builtin_bit_cast(bf16x8, keys.raw[kk]);
       s = mfma32x32x16(k, q[kk], s);
     }
     keep_order();
-    if (more) read_k(blk, pp + 1);             // (shares is 1)
+    if (more) read_k(blk, pp + 1, keys);       // (shares is 1)
     keep_order();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] *= a.scale_log2;
+    for (int i = 0; i < 16; ++i) s[i] *= c;
     if (tail) {
       const uint32_t sees = seen_keys(mask, tok, row.ctx, row.T) >> (8 * grp);
 #pragma unroll
@@ -782,9 +790,111 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds<kW> &lds, 
     }
   };
 
-  int mine = share;
-  for (int blk = 0; blk < nblocks; ++blk) {
-    // this block's loads are done: of those behind them kLoads a block may be on their way
+  // Both pairs of a block of context by one wave: their scores' products side by side, one check of
+  // the maximum, and the second pair's weights worked out while the first pair's meet its values.
+  auto block = [&](int blk) __attribute__((always_inline)) {
+    const uint32_t at = ring + blk % kRing * kBlockBytes;
+    f32x16 s[2];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[0][i] = s[1][i] = 0.f;
+    auto operand = [&](u32x4 w, int kk) __attribute__((always_inline)) {
+      if constexpr (kFp8) return fp8x8_to_bf16x8(u32x2{w[2 * (kk & 1)], w[2 * (kk & 1) + 1]});
+      else return __builtin_bit_cast(bf16x8, w);
+    };
+    constexpr int kStep = kFp8 ? 2 : 4;         // reads of each pair at a time: half of a key
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 k[2][kStep];
+#pragma unroll
+      for (int i = 0; i < kStep; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          k[p][i] = read_lds((at + 2 * p * kPageBytes + k_at) ^ (32 * (h * kStep + i)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+          s[p] = mfma32x32x16(operand(k[p][kFp8 ? i >> 1 : i], i), q[4 * h + i], s[p]);
+    }
+    u32x4 vraw[kFp8 ? 4 : 8];
+    auto read_v = [&](int p) __attribute__((always_inline)) {
+      const uint32_t from = at + 2 * p * kPageBytes + v_at;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < (kFp8 ? 2 : 4); ++i)
+          vraw[(kFp8 ? 2 : 4) * h + i] = read_lds(from + h * kPageBytes + i * 1024);
+    };
+    read_v(0);
+    keep_order();
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[0][i]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[1][i]);
+    mx = pair_max(mx) * c;
+    const bool grows = mx > m_run + kSlack;
+    if (__any(grows)) {
+      const float alpha = grows ? fast_exp2(m_run - mx) : 1.f;
+      m_run = grows ? mx : m_run;
+      l_run *= alpha;
+#pragma unroll
+      for (int mt = 0; mt < 4; ++mt) o[mt] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.f : m_run;
+    bf16x8 hi[2][2], lo[2][2];
+    auto weights = [&](int p) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x8 w;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = fast_exp2(__builtin_fmaf(s[p][8 * h + e], c, -m_use));
+        l_run += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+        hi[p][h] = to_bf16x8(w);
+        lo[p][h] = to_bf16x8(w - to_f32x8(hi[p][h]));
+      }
+    };
+    auto values = [&](int p) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        bf16x8 v[4];
+        if constexpr (kFp8) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const u32x4 w = vraw[2 * h + j];
+            const auto s0 = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+            const auto s1 = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            v[2 * j] = fp8x8_to_bf16x8(u32x2{s0[0], s1[0]});
+            v[2 * j + 1] = fp8x8_to_bf16x8(u32x2{s0[1], s1[1]});
+          }
+        } else {
+#pragma unroll
+          for (int mt = 0; mt < 4; ++mt) v[mt] = __builtin_bit_cast(bf16x8, vraw[4 * h + mt]);
+        }
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) o[mt] = mfma32x32x16(v[mt], hi[p][h], o[mt]);
+#pragma unroll
+        for (int mt = 0; mt < 4; ++mt) o[mt] = mfma32x32x16(v[mt], lo[p][h], o[mt]);
+      }
+    };
+    weights(0);
+    keep_order();
+    values(0);
+    weights(1);
+    // a product, then some of the vector instructions beside it
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x002, kBeside, 0);
+    }
+    keep_order();
+    read_v(1);
+    values(1);
+  };
+
+  // this block's loads are done (of those behind them kLoads a block may be on their way), all
+  // waves', and the block before is consumed
+  auto arrive = [&](int blk) __attribute__((always_inline)) {
     const int behind = min(kRing - 2, nblocks - 1 - blk);
     if (behind >= 2)
       await_loads_before<2 * kLoads>();
@@ -792,16 +902,29 @@ __device__ __forceinline__ void wide_piece(const TreeArgs &a, WideLds<kW> &lds, 
       await_loads_before<kLoads>();
     else
       await_loads();
-    __syncthreads();                            // all waves': and the block before is consumed
+    __syncthreads();
     if (blk + kRing - 1 < nblocks) load(blk + kRing - 1);
+    next_id = page_id(blk + kRing);
+  };
+  int blk = 0;
+  if (shares == 1) {
+    const int full = min(nblocks, max(0, row.ctx - t0) / kWideKeys);
+    for (; blk < full; ++blk) {
+      arrive(blk);
+      block(blk);
+    }
+  }
+  int mine = shares == 1 ? kWidePairs * blk : share;
+  for (; blk < nblocks; ++blk) {
+    arrive(blk);
     const int pairs = min(kWidePairs, (t1 - t0 - blk * kWideKeys + kPair - 1) / kPair);
     // the wave's next pair of all, `shares` behind its last one
-    int pp = mine - 2 * blk;
-    if (pp < pairs) read_k(blk, pp);
-    for (; pp < pairs; pp += shares, mine += shares) pair(blk, pp, pp + shares < pairs);
-    // (the next page's id here, where nothing from LDS is waited for)
-    keep_order();
-    next_id = page_id(blk + kRing);
+    int pp = mine - kWidePairs * blk;
+    if (pp < pairs) {
+      Keys keys;
+      read_k(blk, pp, keys);
+      for (; pp < pairs; pp += shares, mine += shares) pair(blk, pp, pp + shares < pairs, keys);
+    }
   }
   __syncthreads();
 
