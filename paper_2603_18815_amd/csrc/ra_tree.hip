@@ -991,12 +991,12 @@ __global__ __launch_bounds__(kW * kWave, 2) void tree_wide_kernel(TreeArgs a) {
                     });
 }
 
+constexpr int kJoinWaves = 4;
 // Joins the pieces of one node and head, a wave each: the weights of up to 64 pieces are worked
 // out one a lane, the partial results taken four dims a lane by half a wave a piece, four pieces
-// of each half in flight. Nodes of uncut tiles are final already.
-constexpr int kJoinWaves = 4;
+// of each half in flight. For calls of few nodes, whose rows are in many pieces.
 template <int kRows>
-__global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs a) {
+__global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_head_kernel(TreeArgs a) {
   const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
   const int64_t at = (int64_t)blockIdx.x * kJoinWaves + threadIdx.x / kWave;
   const int t = (int)(at / a.hq), h = (int)(at - (int64_t)t * a.hq);
@@ -1053,6 +1053,94 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs 
   if (a.lse && lane == 0) a.lse[at] = (M + __log2f(lsum)) * kLn2;
 }
 
+// Joins the pieces of one node's heads on one KV head, a wave each: four heads at a time and, of
+// each, up to 16 pieces, whose weights are worked out one a lane; the partial results are taken
+// four dims a lane by half a wave a head. Nodes of uncut tiles are final already. Bound by round
+// trips (the node's row, its place on the line, the weights, the results) and by the partial
+// results' bytes.
+constexpr int kJoinHeads = 4, kJoinPieces = 16;
+template <int kRows>
+__global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs a) {
+  const int lane = threadIdx.x & (kWave - 1), half = lane >> 5;
+  const int64_t at = (int64_t)blockIdx.x * kJoinWaves + threadIdx.x / kWave;
+  const int t = (int)(at / a.hkv), g = (int)(at - (int64_t)t * a.hkv);
+  if (t >= a.total_q) return;
+  const int b = uniform(wave_search(a.B, t, [&](int i) { return a.cu_q[i]; }));
+  const TreeRow row = uniform_row(a, b);
+  if (t < row.first || t >= row.first + row.T) return;
+  const RowLine<kRows> line(row, a.group);
+  const int64_t share = uniform(*a.share), start = uniform(a.start[b]);
+  for (int h0 = 0; h0 < a.group; h0 += kJoinHeads) {
+    // the heads' query rows lie in one tile or two
+    const int r = (t - row.first) * a.group + h0 + lane / kJoinPieces;   // this lane's of the weights
+    const int last = min(h0 + kJoinHeads, a.group) - 1 - h0;
+    const int tile0 = ((t - row.first) * a.group + h0) / kRows;
+    const int tile1 = ((t - row.first) * a.group + h0 + last) / kRows;
+    for (int tile = tile0; tile <= tile1; ++tile) {
+      const int64_t begin = start + line.before(tile, g, a.hkv);
+      const int first = (int)quotient(begin, share);
+      const int n =
+          (int)quotient(begin + (int64_t)(line.blocks - 1) * line.cost(tile), share) - first + 1;
+      if (n == 1) continue;
+      // piece i's result of query row r: the first piece is the last of its share
+      auto piece = [&](int i, int r) {
+        return (size_t)(2 * (first + i) + (i == 0)) * a.piece_rows + (r - tile * kRows);
+      };
+      const bool mine = lane / kJoinPieces <= last && r / kRows == tile;
+      float M = -INFINITY;
+      for (int s = lane % kJoinPieces; s < n; s += kJoinPieces)
+        if (mine) M = fmaxf(M, a.ws_ml[piece(s, r)].x);
+#pragma unroll
+      for (int off = 1; off < kJoinPieces; off *= 2) M = fmaxf(M, __shfl_xor(M, off));
+      const float M_use = M == -INFINITY ? 0.f : M;
+      f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};       // heads half, half + 2
+      float lsum = 0.f;
+      for (int s0 = 0; s0 < n; s0 += kJoinPieces) {
+        const int m = min(n - s0, kJoinPieces), s = lane % kJoinPieces;
+        float f = 0.f;
+        if (mine && s < m) {
+          const float2 ml = a.ws_ml[piece(s0 + s, r)];
+          f = fast_exp2(ml.x - M_use);
+          lsum += f * ml.y;
+        }
+        for (int i0 = 0; i0 < m; i0 += 4) {
+          f32x4 v[2][4];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const int h = min(2 * j + half, last), rr = (t - row.first) * a.group + h0 + h;
+            const int safe = min(max(rr, tile * kRows), tile * kRows + kRows - 1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              v[j][i] = *reinterpret_cast<const f32x4 *>(
+                  a.ws_o + piece(s0 + min(i0 + i, m - 1), safe) * kHeadDim + 4 * (lane & 31));
+          }
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float w = __shfl(f, (2 * j + half) * kJoinPieces + min(i0 + i, m - 1));
+              if (i0 + i < m) acc[j] += w * v[j][i];
+            }
+        }
+      }
+#pragma unroll
+      for (int off = 1; off < kJoinPieces; off *= 2) lsum += __shfl_xor(lsum, off);
+      const size_t head = (size_t)t * a.hq + (size_t)g * a.group + h0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int h = 2 * j + half;
+        const float l = __shfl(lsum, h * kJoinPieces);
+        const bool here = h <= last && ((t - row.first) * a.group + h0 + h) / kRows == tile;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][e] = l == 0.f ? 0.f : acc[j][e] * (a.v_scale / l);
+        if (here) *reinterpret_cast<f32x4 *>(a.out + (head + h) * kHeadDim + 4 * (lane & 31)) = acc[j];
+      }
+      if (a.lse && mine && lane % kJoinPieces == 0)
+        a.lse[head + lane / kJoinPieces] = (M + __log2f(lsum)) * kLn2;
+    }
+  }
+}
+
 template <int kRows>
 void plan_line(TreePlan &p, int64_t units, int32_t max_kv_len, int64_t groups) {
   constexpr int keys = block_keys<kRows>();
@@ -1064,6 +1152,11 @@ void plan_line(TreePlan &p, int64_t units, int32_t max_kv_len, int64_t groups) {
 
 constexpr int kDirectKeys = 512;            // rows of so many keys are not cut
 constexpr int kMinShareKeys = 256;          // of a tile, where there is little work
+// (node, head) pairs up to which each has a wave in the join. Call times, a wave a pair and a wave
+// a node and KV head: 4 nodes over 16,000 keys, 32 heads on 8: 25.9 and 35.6 us; 32 nodes 46.4 and
+// 56.3; 64 nodes over 8,000 51.6 and 54.8; 64 rows of 16 nodes (32,768 pairs) 922 and 915; 32 rows
+// of 64 nodes (65,536) 660 and 643.
+constexpr int64_t kFewHeads = 4096;
 
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len) {
   const int64_t rows = (int64_t)max_q_len * (hq / hkv);
@@ -1142,8 +1235,9 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
   a.scale_log2 = scale * kLog2e * kv.k_scale;
   a.v_scale = kv.v_scale;
   const dim3 grid((unsigned)p.groups);
-  const int64_t heads = (int64_t)total_q * hq;
-  const dim3 join_grid((unsigned)((heads + kJoinWaves - 1) / kJoinWaves)), join(kJoinWaves * kWave);
+  const bool by_head = (int64_t)total_q * hq <= kFewHeads;
+  const int64_t joins = (int64_t)total_q * (by_head ? hq : kv.hkv);
+  const dim3 join_grid((unsigned)((joins + kJoinWaves - 1) / kJoinWaves)), join(kJoinWaves * kWave);
   auto launch = [&](auto rows) {
     constexpr int kRows = decltype(rows)::value;
     if constexpr (kRows > 32) {
@@ -1160,7 +1254,10 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.direct) return e;
-    tree_join_kernel<kRows><<<join_grid, join, 0, stream>>>(a);
+    if (by_head)
+      tree_join_head_kernel<kRows><<<join_grid, join, 0, stream>>>(a);
+    else
+      tree_join_kernel<kRows><<<join_grid, join, 0, stream>>>(a);
     return hipGetLastError();
   };
   switch (p.rows) {
