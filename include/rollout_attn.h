@@ -659,11 +659,15 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
  *   workspace   device scratch of at least rollout_attn_decode_tree_workspace_size(B, Hq, Hkv,
  *               total_q, max_q_len, max_kv_len) bytes (contents on entry ignored); NULL where
  *               the size is 0. Calls that share one must not overlap.
- * How keys are split, and with it the order of fp32 sums, depends on B, Hq, Hkv, total_q,
- * max_q_len and max_kv_len alone.
+ * Longer calls (max_kv_len above 512) are cut into equal shares of their work. Where rows are
+ * cut, and with it the order of fp32 sums, depends on the lengths and trees' sizes of all the call's
+ * rows, their order, Hq, Hkv, max_q_len and max_kv_len, and on nothing else: the same call gives
+ * the same bits, while a row's result beside other rows can differ by the order of sums.
+ * Weights meet the values in two bf16 parts, off by 2^-16 of a weight, as in decode (in three, off
+ * by 2^-24, where max_q_len * Hq / Hkv is at most 32 and the pools are bf16).
  * Errors: as rollout_attn_append; RA_ERR_SHAPE also for too few mask_words; RA_ERR_UNSUPPORTED
- *         (Hq / Hkv > 256, B > 65535, max_q_len > RA_MAX_DRAFT_NODES, 2^31 or more workgroups,
- *         q, pools, out or workspace not 16-byte aligned). B == 0, total_q == 0 or max_q_len ==
+ *         (Hq / Hkv > 256, B > 65535, max_q_len > RA_MAX_DRAFT_NODES, max_kv_len > 2^30, total_q *
+ *         Hq >= 2^31, 2^31 or more workgroups, q, pools, out or workspace not 16-byte aligned). B == 0, total_q == 0 or max_q_len ==
  *         0 launch nothing.
  */
 size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
@@ -693,11 +697,13 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
  *                 alignment of an element); out likewise, out_stride apart; out = logits with
  *                 the same stride works in place (and reads and writes only what changes)
  * ra_logits_adjust (all arrays may be NULL where not said otherwise):
- *   history       int32 [B] rows, history_stride apart, of which history_lens[b] (int32 [B],
- *                 needed with history; at most history_stride) are the row's tokens, the first
- *                 prompt_lens[b] (int32 [B]; NULL: 0) of them its prompt
+ *   history       int32 [B] rows of history_width, history_stride apart, of which history_lens[b]
+ *                 (int32 [B], needed with history; more than history_width count as that many)
+ *                 are the row's tokens, the first prompt_lens[b] (int32 [B]; NULL: 0) of them
+ *                 its prompt
  *   repetition, frequency, presence  fp32 [B] (NULL: off)
- *   bias_tokens   int32, bias_values fp32, cu_bias int32 [B+1] (needed with bias_tokens)
+ *   bias_tokens   int32 [num_bias], bias_values fp32 [num_bias], cu_bias int32 [B+1] (needed with
+ *                 bias_tokens)
  *   allowed       uint32 [num_allowed] rows of bits, allowed_stride words apart: bit v % 32 of
  *                 word v / 32; allowed_rows int32 [N]: the row's mask (outside
  *                 [0, num_allowed): none; NULL: mask n)
@@ -708,8 +714,9 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
  *                 n's mask are in its history, behind the prompt
  * What is written must not share memory with another array (but in place as above).
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (N < 0, B < 0, V <= 0, a stride < V with N > 1,
- *         history_stride < 0, allowed_stride < ceil(V / 32), num_allowed < 0, mask_words <= 0
- *         with tree_mask, B != N without cu_rows); RA_ERR_UNSUPPORTED (an unknown
+ *         history_width < 0, history_stride < history_width with B > 1, num_bias < 0,
+ *         allowed_stride < ceil(V / 32), num_allowed < 0, mask_words <= 0 with tree_mask, B != N
+ *         without cu_rows); RA_ERR_UNSUPPORTED (an unknown
  *         logits_dtype, V > 2^24, 2^31 or more workgroups, shared memory); RA_ERR_HIP.
  *         N == 0 or B == 0 launch nothing.
  */
@@ -720,6 +727,7 @@ typedef struct {
   const int32_t *bias_tokens;
   const float *bias_values;
   const int32_t *cu_bias;
+  int32_t history_width, num_bias;
   const uint32_t *allowed;
   const int32_t *allowed_rows;
   int64_t allowed_stride;

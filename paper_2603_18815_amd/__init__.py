@@ -1068,8 +1068,7 @@ def token_logits_adjust(logits: torch.Tensor, history: Optional[torch.Tensor] = 
         if history.dtype != torch.int32:
             raise TypeError(f"history must be torch.int32, got {history.dtype}")
         _shape(history, (B, history.shape[1]), "history")
-        if B <= 1:
-            a.history_stride = history.shape[1]
+        a.history_width = history.shape[1]
         a.history = history.data_ptr()
     give("history_lens", history_lens, torch.int32, (B,))
     give("prompt_lens", prompt_lens, torch.int32, (B,))
@@ -1080,6 +1079,7 @@ def token_logits_adjust(logits: torch.Tensor, history: Optional[torch.Tensor] = 
         if bias_values is None or cu_bias is None:
             raise ValueError("bias_tokens need bias_values and cu_bias")
         give("bias_tokens", bias_tokens, torch.int32, (bias_tokens.numel(),))
+        a.num_bias = bias_tokens.numel()
         give("bias_values", bias_values, torch.float32, (bias_tokens.numel(),))
         give("cu_bias", cu_bias, torch.int32, (B + 1,))
     elif bias_values is not None or cu_bias is not None:

@@ -91,6 +91,8 @@ class RaLogitsAdjust(ctypes.Structure):
         ("bias_tokens", ctypes.c_void_p),
         ("bias_values", ctypes.c_void_p),
         ("cu_bias", ctypes.c_void_p),
+        ("history_width", ctypes.c_int32),
+        ("num_bias", ctypes.c_int32),
         ("allowed", ctypes.c_void_p),
         ("allowed_rows", ctypes.c_void_p),
         ("allowed_stride", ctypes.c_int64),

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kThreads, kMany ? 4 : 8) void adjust_kernel(AdjustA
       __syncthreads();
       if (a.history) {
         const int32_t *h = a.history + (int64_t)r.b * a.history_stride;
-        const int len = (int)min((int64_t)max(a.history_lens[r.b], 0), a.history_stride);
+        const int len = min(max(a.history_lens[r.b], 0), a.history_width);
         const int prompt = min(max(a.prompt_lens ? a.prompt_lens[r.b] : 0, 0), len);
         const uint32_t size = c1 - c0;
         auto one = [&](int t, int v) {
@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kThreads, kMany ? 4 : 8) void adjust_kernel(AdjustA
         }
       }
       if (a.bias_tokens)
-        for (int e = a.cu_bias[r.b] + tid; e < a.cu_bias[r.b + 1]; e += kThreads) {
+        for (int e = max(a.cu_bias[r.b], 0) + tid; e < min(a.cu_bias[r.b + 1], a.num_bias); e += kThreads) {
           const int v = a.bias_tokens[e];
           if (v >= c0 && v < c1) atomicMax(&bias_at[v - e0], e);        // the last one counts
         }

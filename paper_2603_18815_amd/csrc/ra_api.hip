@@ -660,7 +660,7 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
   if ((int64_t)mask_words * 64 < max_q_len) return RA_ERR_SHAPE;
   if ((s = check_kv(kv)) != RA_OK) return s;
   if (Hq % kv->num_kv_heads != 0 || !positions_fit(kv, max_kv_len)) return RA_ERR_SHAPE;
-  if (Hq / kv->num_kv_heads > 256) return RA_ERR_UNSUPPORTED;
+  if (Hq / kv->num_kv_heads > 256 || max_kv_len > (1 << 30)) return RA_ERR_UNSUPPORTED;
   if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
   if (!q || !cu_q || !ctx_lens || !tree_mask || !out) return RA_ERR_NULL;
   if (!aligned16(q) || !aligned16(out) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool))
@@ -685,7 +685,8 @@ int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int
   if (!adjust) return RA_ERR_NULL;
   const ra_logits_adjust &j = *adjust;
   if (!j.cu_rows && B != N) return RA_ERR_SHAPE;
-  if ((j.history && j.history_stride < 0) || (j.tree_mask && j.mask_words <= 0) ||
+  if ((j.history && (j.history_width < 0 || (B > 1 && j.history_stride < j.history_width))) ||
+      (j.bias_tokens && j.num_bias < 0) || (j.tree_mask && j.mask_words <= 0) ||
       (j.allowed && (j.num_allowed < 0 || j.allowed_stride < (V + 31) / 32)))
     return RA_ERR_SHAPE;
   if (N == 0 || B == 0) return RA_OK;
@@ -702,10 +703,12 @@ int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int
   const int64_t written = ((N - 1) * out_stride + V) * size;
   if (overlap({{out, written, true},
                {in_place ? nullptr : logits, ((N - 1) * row_stride + V) * size, false},
-               {j.history, 4 * B * j.history_stride, false}, {j.history_lens, rows, false},
+               {j.history, 4 * ((B - 1) * j.history_stride + j.history_width), false}, {j.history_lens, rows, false},
                {j.prompt_lens, rows, false}, {j.repetition, rows, false},
                {j.frequency, rows, false}, {j.presence, rows, false},
-               {j.cu_bias, rows + 4, false}, {j.allowed, bits, false},
+               {j.bias_tokens, 4 * (int64_t)j.num_bias, false},
+               {j.bias_values, 4 * (int64_t)j.num_bias, false}, {j.cu_bias, rows + 4, false},
+               {j.allowed, bits, false},
                {j.allowed_rows, each, false}, {j.cu_rows, rows + 4, false},
                {j.draft_tokens, each, false}, {j.tree_mask, 2 * each * j.mask_words, false}}))
     return RA_ERR_UNSUPPORTED;
@@ -727,6 +730,8 @@ int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int
   a.bias_tokens = j.bias_tokens;
   a.cu_bias = j.cu_bias;
   a.bias_values = j.bias_values;
+  a.history_width = j.history_width;
+  a.num_bias = j.num_bias;
   a.allowed = j.allowed;
   a.allowed_rows = j.allowed_rows;
   a.allowed_stride = j.allowed_stride;

@@ -171,6 +171,7 @@ struct AdjustArgs {
   const float *repetition, *frequency, *presence;
   const int32_t *bias_tokens, *cu_bias;
   const float *bias_values;
+  int32_t history_width, num_bias;
   const uint32_t *allowed;
   const int32_t *allowed_rows;
   int64_t allowed_stride;

@@ -6,7 +6,8 @@
 // nodes see the context; which of the nodes a node sees is in its bit mask.
 //
 // Softmax is the online form in fp32, base 2. Weights meet the values in two bf16 parts, off by
-// 2^-16 of a weight, as in decode (ra_decode_split.h): one part would be off by 2^-8.
+// 2^-16 of a weight, as in decode (ra_decode_split.h): one part would be off by 2^-8. (Narrow tiles
+// over bf16 pools take a third part, which is free there.)
 //
 // The work of a call is a line: its tiles in the order of rows, tiles and KV heads, each as long
 // as its blocks of keys, weighted by what a block costs with the tile's rows. Every workgroup
@@ -466,12 +467,18 @@ __device__ __forceinline__ void narrow_piece(const TreeArgs &a, TreeLds<kTiles> 
       l_run[nt] = l_run[nt] * alpha + psum;
       m_run[nt] = m_new;
       const bf16x8 p_hi = to_bf16x8(p);
-      const bf16x8 p_lo = to_bf16x8(p - to_f32x8(p_hi));
+      const f32x8 rest = p - to_f32x8(p_hi);
+      const bf16x8 p_lo = to_bf16x8(rest);
+      // a third part of the weights, to fp32, where it is free (64 rows of 8 nodes over 4k to 32k
+      // keys: bf16 pools 807 us with two parts and 808 with three, codes 452 and 487)
+      bf16x8 p_last = {};
+      if constexpr (!kFp8) p_last = to_bf16x8(rest - to_f32x8(p_lo));
 #pragma unroll
       for (int mt = 0; mt < 8; ++mt) {
         o[nt][mt] *= alpha;
         o[nt][mt] = mfma16x16x32(va[mt], p_hi, o[nt][mt]);
         o[nt][mt] = mfma16x16x32(va[mt], p_lo, o[nt][mt]);
+        if constexpr (!kFp8) o[nt][mt] = mfma16x16x32(va[mt], p_last, o[nt][mt]);
       }
     }
     keep_order();

@@ -97,6 +97,8 @@ def test_decode_tree_validation(lib):
                      (dict(dt=1, ks=0.0), SHAPE)):
         bad = pools(**kw)
         assert go(kv=ctypes.byref(bad)) == want
+    far = pools(stride=1 << 27)
+    assert go(kv=ctypes.byref(far), mk=(1 << 30) + 1) == UNSUPPORTED
     long = pools(stride=4096)
     need = lib.rollout_attn_decode_tree_workspace_size(2, 8, 2, 20, 10, 40000)
     assert need > 0
@@ -132,7 +134,9 @@ def test_token_logits_adjust_validation(lib):
     assert go(N=0, B=0, z=None, out=None) == OK
     assert go(dict(cu_rows=at(3)), B=0) == OK
     assert go(dict(history=at(3))) == NULL
-    assert go(dict(history=at(3), history_lens=at(4), history_stride=-1)) == SHAPE
+    assert go(dict(history=at(3), history_lens=at(4), history_width=-1)) == SHAPE
+    assert go(dict(history=at(3), history_lens=at(4), history_width=9, history_stride=8)) == SHAPE
+    assert go(dict(bias_tokens=at(3), bias_values=at(4), cu_bias=at(5), num_bias=-1)) == SHAPE
     assert go(dict(bias_tokens=at(3), bias_values=at(4))) == NULL
     assert go(dict(bias_tokens=at(3), cu_bias=at(4))) == NULL
     assert go(dict(allowed=at(3), allowed_stride=3, num_allowed=4)) == SHAPE
@@ -144,12 +148,12 @@ def test_token_logits_adjust_validation(lib):
     # what is written must not be read elsewhere: in place, or apart
     assert go(out=ctypes.c_void_p(0x1000 + BIG + 4)) == UNSUPPORTED
     assert go(out=at(1), ostride=200) == UNSUPPORTED
-    full = dict(tree, history=at(6), history_lens=at(7), history_stride=9, prompt_lens=at(8),
+    full = dict(tree, history=at(6), history_lens=at(7), history_stride=9, history_width=9, num_bias=5, prompt_lens=at(8),
                 repetition=at(9), frequency=at(10), presence=at(11), bias_tokens=at(12),
                 bias_values=at(13), cu_bias=at(14), allowed=at(15), allowed_stride=4, num_allowed=2,
                 allowed_rows=at(16))
-    for n in set(full) - {"mask_words", "history_stride", "allowed_stride", "num_allowed",
-                          "bias_tokens", "bias_values"}:
+    for n in set(full) - {"mask_words", "history_stride", "history_width", "num_bias",
+                          "allowed_stride", "num_allowed"}:
         assert go(dict(full, **{n: at(2)})) == UNSUPPORTED, n
 
 

@@ -225,3 +225,25 @@ def test_lengths_past_the_history_and_below_zero(device):
     a = ra.token_logits_adjust(z, history_lens=i32([1000, -3]), **kw)
     b = ra.token_logits_adjust(z, history_lens=i32([3, 0]), **kw)
     assert torch.equal(a, b) and torch.equal(a[1], z[1])
+    # of rows cut out of wider ones too
+    wide = i32([[9, 9, 1, 2, 3], [9, 9, 4, 5, 6]])[:, 2:]
+    c = ra.token_logits_adjust(z, history_lens=i32([1000, -3]), history=wide, frequency=kw["frequency"])
+    assert torch.equal(a, c)
+
+
+def test_bias_offsets_past_the_lists(device):
+    z = torch.randn((2, 50), device=DEV)
+    kw = dict(bias_tokens=i32([3, 4, 5]), bias_values=f32([1.0, 2.0, 3.0]))
+    a = ra.token_logits_adjust(z, cu_bias=i32([0, 2, 1 << 30]), **kw)
+    b = ra.token_logits_adjust(z, cu_bias=i32([0, 2, 3]), **kw)
+    assert torch.equal(a, b)
+
+
+def test_masks_of_few_rows_and_ids_outside(device):
+    """Without allowed_rows row n has mask n; rows past the masks have none."""
+    z = torch.randn((3, 40), device=DEV)
+    one = torch.zeros((1, 2), dtype=torch.int32, device=DEV)
+    out = ra.token_logits_adjust(z, allowed=one)
+    assert bool((out[0] == float("-inf")).all()) and torch.equal(out[1:], z[1:])
+    out = ra.token_logits_adjust(z, allowed=one, allowed_rows=i32([-1, 1, 0]))
+    assert torch.equal(out[:2], z[:2]) and bool((out[2] == float("-inf")).all())
