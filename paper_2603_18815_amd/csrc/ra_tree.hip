@@ -2,12 +2,21 @@
 //
 // Row b's T nodes lie behind its ctx cached tokens. The query rows of a KV head are its G =
 // Hq / Hkv query heads of all nodes, node r / G and head r % G for query row r, in tiles of 16,
-// 32 or 256 that are columns of the matrix products, so that a key is read once for a tile. All
-// nodes see the context; which of the nodes a node sees is in its bit mask.
+// 32, 128 or 256 that are columns of the matrix products, so that a key is read once for a tile.
+// All nodes see the context; which of the nodes a node sees is in its bit mask:
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(c q.k_j - max),  j of the keys that the node sees.
 //
 // Softmax is the online form in fp32, base 2. Weights meet the values in two bf16 parts, off by
-// 2^-16 of a weight, as in decode (ra_decode_split.h): one part would be off by 2^-8. (Narrow tiles
-// over bf16 pools take a third part, which is free there.)
+// 2^-16 of a weight: one part would be off by 2^-8. (Narrow tiles over bf16 pools take a third
+// part, which is free there. In wide tiles it costs what the matrix cores do not have: 32 rows
+// of 64 nodes over 2k to 24k keys 666 -> 813 us.)
+//
+// Read: every row's keys and values once a tile, 512 bytes a key and KV head in bf16. Computed:
+// 512 flops a key and query row, 768 with the weights' second part. Bound by HBM up to about 60
+// rows a tile and by the matrix cores, softmax beside them, from about 100. Measured, Hq 32 on 8:
+// 64 rows of 8 nodes over 4k to 32k keys (5.08 GB) 807 us, 6.3 TB/s, as decode of one token
+// (795); of 16 nodes 915-930; 32 rows of 16 to 64 nodes over 2k to 24k 501-535 us (249 GFLOP, 374
+// with the parts: 0.70-0.75 PFLOP/s); 1 row of 4 nodes over 16,000 keys 26 us, of 32 nodes 47.
 //
 // The work of a call is a line: its tiles in the order of rows, tiles and KV heads, each as long
 // as its blocks of keys, weighted by what a block costs with the tile's rows. Every workgroup
@@ -15,7 +24,8 @@
 // sizes end together, and a tile is cut only where a share ends: a cut tile's pieces go to the
 // workspace and a second launch joins them. (Splits of a fixed length, a workgroup each, left
 // the compute units idle for 13 to 29 % of the time, and wrote 2 to 8 times the partial
-// results.) Calls of rows of up to kDirectKeys keys take a workgroup a tile and one launch.
+// results.) Calls of short rows (kDirectKeys) take a workgroup a tile and one launch: there is
+// no join, and no tile begins twice.
 #include <type_traits>
 
 #include "ra_device.h"
@@ -259,8 +269,10 @@ __device__ __forceinline__ void reach_odd(const TreeArgs &a, const TreeRow &row,
 // 16 kTiles query rows by four waves, each of which takes every fourth pair of pages (32 keys)
 // of the piece straight from HBM into its registers:
 //   S^T[key][row] = K[key][:] . Q^T[:][row]       (4 products of 16 x 16 x 32 for 16 keys and rows)
-//   O^T[d][row]  += V^T[d][key] . P^T[key][row]   (8 for 32 keys, twice: the weights' parts)
-// Bound by HBM; the waves are joined through LDS at the end of a piece.
+//   O^T[d][row]  += V^T[d][key] . P^T[key][row]   (8 for 32 keys, once for each of the weights' parts)
+// Bound by HBM: nothing of a key is used by two waves, so LDS would be a detour; the waves are
+// joined through it at the end of a piece. 64 rows of 8 nodes over 4k to 32k keys: 802 us where
+// decode's kernel takes 790, and 9 of the join.
 template <int kTiles>
 struct TreeLds {
   WalkLds<kSplitWaves * kWave> walk;
@@ -556,11 +568,16 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_narrow_kernel(Tre
 // only when a score passes it by 8 (in powers of two), so that O is rescaled rarely; weights
 // are at most 2^8 then.
 // kW is 4 for trees of up to 128 query rows, two workgroups a compute unit, each of which works
-// while the other waits, and 8 (a ring of four, three blocks ahead) for larger ones.
+// while the other waits, and 8 (a ring of four, three blocks ahead) for larger ones. (64 rows
+// of 16 nodes, 64 query rows: 915-930 us, with kW 8 948; over fp8 pools 643-680 and 791.) With
+// few query rows bound by the loads: those of 64 rows of 16 nodes alone take 912 of 956 us
+// (5.6 TB/s); with many by the products and the softmax beside them, which a wave issues in
+// turn: 32 rows of 64 nodes 751 us with a pair of keys a wave at a time, 683 with a block's two
+// pairs by one wave, the second's weights beside the first's products.
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 constexpr int kWideKeys = 64, kWidePages = kWideKeys / kPage, kWidePairs = kWideKeys / kPair;
 constexpr int kPageElems = kPage * kHeadDim;
-constexpr float kSlack = 8.f;
+constexpr float kSlack = 8.f;               // (powers of two that a weight may pass 1 by)
 constexpr int kBeside = 10;                 // vector instructions beside a product
 
 template <int kW>
@@ -1157,8 +1174,18 @@ void plan_line(TreePlan &p, int64_t units, int32_t max_kv_len, int64_t groups) {
 
 }  // namespace
 
-constexpr int kDirectKeys = 512;            // rows of so many keys are not cut
-constexpr int kMinShareKeys = 256;          // of a tile, where there is little work
+// Rows of up to kDirectKeys keys are not cut, nor are those of up to kDirectUnitKeys for each
+// tile and KV head of the call, as far as kDirectMost. Uncut and cut (us, 32 heads on 8, rows
+// from an eighth of the longest on): 1 row of 500, 8 nodes 14.7 and 17.0; 64 rows of up to 400,
+// 8 nodes 24.6 and 48.8, 32 nodes 40 and 83; 8 rows of 900 21.0 and 20.4; 16 rows of up to
+// 1,900 28.4 and 32.7 (32 nodes 55.7 and 53.6); 16 of 3,900 46 and 41 (97 and 70); 64 of
+// 1,900 61 and 95 (102 and 147); 64 of 3,900 122 and 137 (181 and 194); 64 of 8,000 231 and 228
+// (337 and 319); 256 of 3,900 443 and 484 (622 and 683).
+constexpr int kDirectKeys = 512, kDirectUnitKeys = 16, kDirectMost = 4096;
+// The least that a workgroup takes of a tile. Twice as much and half: 4 rows of 1,000 keys, 64
+// nodes 51.5, 40.0 and 40.0 us; 1 of 2,000, 32 nodes 25.2, 23.8 and 25.0; 2 of 2,000, 16 nodes
+// 20.7, 20.9 and 24.3.
+constexpr int kMinShareKeys = 128;
 // (node, head) pairs up to which each has a wave in the join. Call times, a wave a pair and a wave
 // a node and KV head: 4 nodes over 16,000 keys, 32 heads on 8: 25.9 and 35.6 us; 32 nodes 46.4 and
 // 56.3; 64 nodes over 8,000 51.6 and 54.8; 64 rows of 16 nodes (32,768 pairs) 922 and 915; 32 rows
@@ -1171,9 +1198,12 @@ TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
   p.tiles = (rows + p.rows - 1) / p.rows;
   p.piece_rows = (int32_t)(rows < p.rows ? rows : p.rows);
-  p.direct = max_kv_len <= kDirectKeys;
   const int64_t units = (int64_t)B * hkv * p.tiles;
-  // as many workgroups as are on the GPU together
+  p.direct = max_kv_len <= kDirectKeys ||
+             (max_kv_len <= kDirectMost && max_kv_len <= units * kDirectUnitKeys);
+  // As many workgroups as are on the GPU together; half of them: 64 rows of 4k to 32k keys
+  // (4.6 GB), 8 nodes 732 us for 732, fp8 498 for 425, 16 nodes over fp8 713 for 620, but 4 rows
+  // of 8,000 39 for 42; twice as many: 747, 32 rows of 16 to 64 nodes over 2k to 24k 551 for 535.
   if (p.direct)
     p.groups = units;
   else if (p.rows == 16)

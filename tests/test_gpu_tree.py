@@ -155,6 +155,18 @@ def test_many_rows(device, Hq, Hkv, most, fp8):
     check(cache, q, masks, bits, ctx, T)
 
 
+@pytest.mark.parametrize("T", [2, 6, 25, 50])
+def test_rows_of_very_different_lengths_that_are_not_cut(device, T):
+    ctx = [int(x) for x in np.random.default_rng(T).integers(0, 200, 96)]
+    ctx[3], ctx[40], ctx[95] = 3000, 0, 1700
+    trees = [T] * 96
+    trees[10], trees[50] = 0, 1
+    Hq, Hkv = 16, 2
+    assert ra.decode_tree_workspace_size(96, Hq, Hkv, sum(trees), T, max(ctx) + T) == 0
+    cache, q, masks, bits = inputs(17, Hq, Hkv, ctx, trees)
+    check(cache, q, masks, bits, ctx, trees)
+
+
 def test_largest_tree(device):
     ctx, T = [77], [1024]
     check(*(lambda c, q, m, b: (c, q, m, b, ctx, T))(*inputs(13, 4, 2, ctx, T)))
