@@ -17,30 +17,38 @@ namespace {
 
 constexpr int kForkThreads = 256;
 constexpr int kMaxRows = 65536;            // rows a block table can have
-constexpr int kSmallForks = 8, kSmallEntries = 4096;   // of calls that one workgroup does
+// Calls that one workgroup does, up to 8 forks and tables of up to 4,096 entries: a launch is 2-3
+// us of the GPU's time and 4-5 of the host's. A fork of one row, its copy and its release 29 us
+// in place of 39 (in a graph 23 and 21); 7 forks of 7,000 tokens 30 and 43 (24.5 and 25.5); at
+// 8,192 entries the two are even, at 16,384 one workgroup takes 2.5 times as long.
+constexpr int kSmallForks = 8, kSmallThreads = 128, kSmallEntries = 4096;
 constexpr int kCode = 1 << 30;             // codes of entries: -(kCode + 1 + place), place < kCode
 
 __device__ __forceinline__ bool page_ok(int id, int num_pages) { return (unsigned)id < (unsigned)num_pages; }
 
-// A workgroup a fork, or one for all of a small call (kOne), which then sets the list's length
-// itself. Every workgroup looks at all forks: whether the call holds decides what each does, and
-// the forks before it say which page is its own. Bound by latency and, for long prompts, by the
-// atomics on the shared pages' counts.
+// A workgroup a fork, or one for all of a small call (kOne: 128 threads a fork), which then sets
+// the list's length itself. Every workgroup looks at all forks: whether the call holds decides
+// what each does, and the forks before it say which page is its own. Bound by latency and, for
+// long prompts, by the atomics on the shared pages' counts: one fork of 130 tokens 2.6 us, 448 forks of
+// 64 prompts of 2k to 8k tokens (147,000 entries) 11.6 us.
 template <bool kOne>
-__global__ __launch_bounds__(kForkThreads) void fork_kernel(
+__global__ __launch_bounds__(kOne ? kSmallForks * kSmallThreads : kForkThreads) void fork_kernel(
     const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens, int32_t n,
     int32_t *block_table, int32_t B, int32_t bt_stride, int32_t *shares, int32_t num_pages,
     const int32_t *free_pages, int32_t *free_count, int32_t capacity, int32_t *copy_src,
     int32_t *copy_dst, int32_t *taken) {
   __shared__ uint32_t is_dst[kMaxRows / 32];
-  __shared__ int bad, need, before;
-  const int tid = threadIdx.x, me = blockIdx.x;
+  __shared__ int bad, need, before[kOne ? kSmallForks : 1];
+  const int tid = threadIdx.x, threads = blockDim.x;
+  const int f = kOne ? tid / kSmallThreads : blockIdx.x;                // this thread's fork
+  const int t0 = kOne ? tid % kSmallThreads : tid, step = kOne ? kSmallThreads : kForkThreads;
   const int count = *free_count;
-  for (int i = tid; i < (B + 31) / 32; i += kForkThreads) is_dst[i] = 0;
-  if (tid == 0) bad = need = before = 0;
+  for (int i = tid; i < (B + 31) / 32; i += threads) is_dst[i] = 0;
+  if (tid == 0) bad = need = 0;
+  if (t0 == 0) before[kOne ? f : 0] = 0;
   __syncthreads();
   const int64_t limit = (int64_t)bt_stride * kPage;
-  for (int i = tid; i < n; i += kForkThreads) {
+  for (int i = tid; i < n; i += threads) {
     const int s = src_rows[i], d = dst_rows[i], len = lens[i];
     if (s < 0 || s >= B || d < 0 || d >= B || len < 0 || len > limit) {
       bad = 1;
@@ -50,42 +58,42 @@ __global__ __launch_bounds__(kForkThreads) void fork_kernel(
     if (atomicOr(&is_dst[d >> 5], bit) & bit) bad = 1;   // two forks into one row
     if (len % kPage) {
       atomicAdd(&need, 1);
-      if (i < me) atomicAdd(&before, 1);
+      if constexpr (kOne) {
+        for (int j = i + 1; j < n; ++j) atomicAdd(&before[j], 1);
+      } else {
+        if (i < f) atomicAdd(&before[0], 1);
+      }
     }
   }
   __syncthreads();
-  for (int i = tid; i < n; i += kForkThreads) {          // a row forked from is not forked into
+  for (int i = tid; i < n; i += threads) {               // a row forked from is not forked into
     const int s = src_rows[i];
     if (s >= 0 && s < B && (is_dst[s >> 5] >> (s & 31) & 1)) bad = 1;
   }
   __syncthreads();
   const bool ok = !bad && count >= 0 && count <= capacity && need <= count;
-  int pages = kOne ? 0 : before;                         // taken by the forks before
-  for (int f = kOne ? 0 : me; f < (kOne ? n : min(n, me + 1)); ++f) {
+  if (f < n) {
     int from = -1, to = -1;
     if (ok) {
       const int64_t src = (int64_t)src_rows[f] * bt_stride, dst = (int64_t)dst_rows[f] * bt_stride;
       const int len = lens[f], full = len / kPage;
-      for (int j = tid; j < full; j += kForkThreads) {
+      if (t0 == 0 && len % kPage) {
+        from = block_table[src + full];
+        to = free_pages[count - 1 - before[kOne ? f : 0]];
+        block_table[dst + full] = to;
+      }
+      for (int j = t0; j < full; j += step) {
         const int page = block_table[src + j];
         block_table[dst + j] = page;
         if (page_ok(page, num_pages)) atomicAdd(&shares[page], 1);
       }
-      if (len % kPage) {
-        if (tid == 0) {
-          from = block_table[src + full];
-          to = free_pages[count - 1 - pages];
-          block_table[dst + full] = to;
-        }
-        ++pages;
-      }
     }
-    if (tid == 0) {
+    if (t0 == 0) {
       copy_src[f] = from;
       copy_dst[f] = to;
     }
   }
-  if (me == 0 && tid == 0) {
+  if (blockIdx.x == 0 && tid == 0) {
     *taken = ok ? need : -1;
     if (gridDim.x == 1 && ok) *free_count = count - need;
   }
@@ -110,6 +118,10 @@ struct SharedRelease {
 
 __device__ __forceinline__ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 
+// The release of a large table, each step a launch because atomics of all rows have to be there
+// before the next. Of 512 rows and 168,000 entries: 9.7 + 4.2 + 3.4 + 8.5 us, bound by the atomics
+// on shared counts and by round trips.
+//
 // Takes an owner off every entry that is given up.
 __global__ __launch_bounds__(kRowThreads) void shared_sub_kernel(SharedRelease r) {
   __shared__ int bad;
@@ -219,69 +231,77 @@ __global__ __launch_bounds__(kRowThreads) void shared_put_kernel(SharedRelease r
   }
 }
 
-// All of it by one workgroup, for tables of up to kSmallEntries entries: the counts change by
-// atomics, so they are read past the first-level cache.
-constexpr int kOneThreads = 1024;
+// All of it by one workgroup, for tables of up to kSmallEntries entries, which its threads keep:
+// the counts change by atomics, so they are read past the first-level cache. 9.3 us, of round
+// trips: lengths, table, three to the counts, the list.
+constexpr int kOneThreads = 1024, kOneEntries = kSmallEntries / kOneThreads;
 __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r) {
-  __shared__ int bad, all, wave_sum[kOneThreads / kWave];
+  constexpr int kWaves = kOneThreads / kWave;
+  __shared__ int bad, wave_sum[kOneEntries * kWaves];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
   const int count = *r.free_count, entries = r.B * r.bt_stride;
-  if (tid == 0) bad = all = 0;
+  if (tid == 0) bad = 0;
   __syncthreads();
   const int64_t limit = (int64_t)r.bt_stride * kPage;
   for (int i = tid; i < r.B; i += kOneThreads) {
     const int64_t len = r.lens[i], keep = r.keep_lens[i];
     if (keep < 0 || keep > len || len > limit) bad = 1;
   }
+  int page[kOneEntries];                   // of the entries that are given up, -1 else
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u) {
+    const int x = u * kOneThreads + tid;
+    page[u] = -1;
+    if (x >= entries) continue;
+    const int b = x / r.bt_stride, j = x - b * r.bt_stride, id = r.block_table[x];
+    if (j >= pages_of(r.keep_lens[b]) && j < pages_of(r.lens[b]) && page_ok(id, r.num_pages)) page[u] = id;
+  }
   __syncthreads();
   if (bad || count < 0 || count > r.capacity) {
     if (tid == 0) *r.released = -1;
     return;
   }
-  // the entry's page if it is given up, -1 else
-  auto page_of = [&](int x) {
-    if (x >= entries) return -1;
-    const int b = x / r.bt_stride, j = x - b * r.bt_stride;
-    if (j < pages_of(r.keep_lens[b]) || j >= pages_of(r.lens[b])) return -1;
-    const int page = r.block_table[x];
-    return page_ok(page, r.num_pages) ? page : -1;
+  auto holders = [&](int p) {
+    return __hip_atomic_load(&r.shares[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   };
-  auto holders = [&](int page) {
-    return __hip_atomic_load(&r.shares[page], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  };
-  for (int x = tid; x < entries; x += kOneThreads)
-    if (const int page = page_of(x); page >= 0) atomicSub(&r.shares[page], 1);
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u)
+    if (page[u] >= 0) atomicSub(&r.shares[page[u]], 1);
   __threadfence();
   __syncthreads();
-  for (int x = tid; x < entries; x += kOneThreads)
-    if (const int page = page_of(x); page >= 0 && holders(page) < 0)
-      atomicMin(&r.shares[page], -(kCode + 1) - x);
+  int held[kOneEntries];
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u) held[u] = page[u] >= 0 ? holders(page[u]) : 0;
+  // (other entries' codes may be among those read; they too are of pages that nobody holds)
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u)
+    if (held[u] < 0) atomicMin(&r.shares[page[u]], -(kCode + 1) - (u * kOneThreads + tid));
   __threadfence();
   __syncthreads();
-  int mine = 0;
-  for (int x = tid; x < entries; x += kOneThreads)
-    if (const int page = page_of(x); page >= 0) mine += holders(page) == -(kCode + 1) - x;
-  if (mine) atomicAdd(&all, mine);
+  uint64_t votes[kOneEntries];
+  bool free[kOneEntries];
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u)
+    free[u] = held[u] < 0 && holders(page[u]) == -(kCode + 1) - (u * kOneThreads + tid);
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u) {
+    votes[u] = __ballot(free[u]);
+    if (lane == 0) wave_sum[u * kWaves + wave] = (int)__popcll(votes[u]);
+  }
   __syncthreads();
-  int rank = 0;
-  for (int x0 = 0; x0 < entries; x0 += kOneThreads) {
-    const int x = x0 + tid, page = page_of(x);
-    const bool free = page >= 0 && holders(page) == -(kCode + 1) - x;
-    const uint64_t votes = __ballot(free);
-    if (lane == 0) wave_sum[wave] = (int)__popcll(votes);
-    __syncthreads();
-    int at = rank + (int)__popcll(votes & ((1ull << lane) - 1)), step = 0;
-    for (int w = 0; w < kOneThreads / kWave; ++w) {
-      if (w < wave) at += wave_sum[w];
-      step += wave_sum[w];
-    }
-    if (free) {
-      const int64_t to = (int64_t)count + all - 1 - at;
-      if (to < r.capacity) r.free_pages[to] = page;
-      __hip_atomic_store(&r.shares[page], 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    rank += step;
-    __syncthreads();
+  // every wave sums up what lies before each of its places
+  static_assert(kOneEntries * kWaves <= kWave, "a lane a place");
+  const int sum = wave_sums(lane < kOneEntries * kWaves ? wave_sum[lane] : 0);
+  const int all = of_lane(sum, kWave - 1);
+#pragma unroll
+  for (int u = 0; u < kOneEntries; ++u) {
+    const int place = __builtin_amdgcn_readfirstlane(u * kWaves + wave);
+    const int before = place ? of_lane(sum, place - 1) : 0;
+    if (!free[u]) continue;
+    const int at = before + (int)__popcll(votes[u] & ((1ull << lane) - 1));
+    const int64_t to = (int64_t)count + all - 1 - at;
+    if (to < r.capacity) r.free_pages[to] = page[u];
+    r.shares[page[u]] = 0;
   }
   if (tid == 0) {
     *r.released = all;
@@ -292,7 +312,8 @@ __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r
 // ---- pages' contents ----
 constexpr int kCopyThreads = 256;
 
-// One page of one KV head a workgroup, 16 bytes a thread and pool. Bound by HBM.
+// One page of one KV head a workgroup, 16 bytes a thread and pool. Bound by HBM: 434 pages of 8 KV
+// heads in bf16 (57 MB read and written, the sources of eight copies the same) 7.5 us.
 template <bool kFp8>
 __global__ __launch_bounds__(kCopyThreads) void page_copy_kernel(uint8_t *k_pool, uint8_t *v_pool,
                                                                  const int32_t *src,
@@ -318,8 +339,11 @@ constexpr int kMoveThreads = 256;
 // behind where it was and the tokens of one step lie before the sources of all later ones: a
 // step has all its tokens in registers before it writes any. Keys move 16 bytes a thread; of
 // the values a thread has one dimension of the tokens that go to one half of a page, so that a
-// half whose tokens all move is one store. Bound by round trips: the offsets, the index, the
-// table and the pages, one behind the other.
+// half whose tokens all move is one store. Bound by round trips (the offsets, the index, the
+// table and the pages, one behind the other) and, in large calls, by HBM's sectors: of a value
+// row a token has two bytes of a 32-byte sector, so that 58 MB of keys and values are 137 MB
+// in whole sectors. 4 rows of up to 8 tokens 4.1 us; 512 rows, some 16 tokens each, 8 KV heads 32 us
+// (4.3 TB/s of sectors), with single values stored one by one 40.
 template <typename E>
 __global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
     E *k_pool, E *v_pool, const int32_t *block_table, int32_t bt_stride, int32_t num_pages,
@@ -433,7 +457,7 @@ hipError_t launch_table_fork(const int32_t *src_rows, const int32_t *dst_rows, c
                              int32_t *free_count, int32_t capacity, int32_t *copy_src,
                              int32_t *copy_dst, int32_t *taken, hipStream_t stream) {
   if (n <= kSmallForks && (int64_t)n * bt_stride <= kSmallEntries) {
-    fork_kernel<true><<<1, kForkThreads, 0, stream>>>(
+    fork_kernel<true><<<1, kSmallForks * kSmallThreads, 0, stream>>>(
         src_rows, dst_rows, lens, n, block_table, B, bt_stride, shares, num_pages, free_pages,
         free_count, capacity, copy_src, copy_dst, taken);
     return hipGetLastError();
