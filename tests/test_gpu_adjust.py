@@ -174,6 +174,29 @@ def test_many_rows_of_few_trees(device):
     check(ra.token_logits_adjust(z, **kw), z, want, plain)
 
 
+def test_a_large_call_equals_its_trees_one_by_one(device):
+    """Rows enough for the most that a workgroup takes, of trees that begin anywhere in them."""
+    rng = np.random.default_rng(6)
+    V, nodes = 100003, rng.integers(0, 65, 60)
+    B, at = len(nodes), cu(nodes)
+    N = at[-1]
+    z = torch.randn((N, V), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV).bfloat16()
+    history, tokens = i32(rng.integers(0, 3000, (B, 500))), i32(rng.integers(0, 3000, N))
+    mask = torch.as_tensor(pack([ancestors(random_tree(rng, t)) for t in nodes], 1), device=DEV)
+    lens = rng.integers(0, 501, B)
+    par = {k: f32(rng.uniform(0.8, 1.5, B)) for k in PARAMS}
+    out = ra.token_logits_adjust(z, history=history, history_lens=i32(lens), cu_rows=i32(at),
+                                 draft_tokens=tokens, tree_mask=mask, **par)
+    for b in range(B):
+        rows = slice(at[b], at[b + 1])
+        if nodes[b] == 0:
+            continue
+        one = ra.token_logits_adjust(z[rows], history=history[b:b + 1], history_lens=i32(lens[b:b + 1]),
+                                     cu_rows=i32([0, nodes[b]]), draft_tokens=tokens[rows],
+                                     tree_mask=mask[rows], **{k: v[b:b + 1] for k, v in par.items()})
+        assert torch.equal(out[rows], one), b
+
+
 def test_special_values(device):
     inf, nan = float("inf"), float("nan")
     z = f32([[inf, -inf, nan, 0.0, -0.0, 2.0, -2.0, 1e38]] * 4)
