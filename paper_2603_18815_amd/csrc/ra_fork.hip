@@ -19,7 +19,7 @@ constexpr int kForkThreads = 256;
 constexpr int kMaxRows = 65536;            // rows a block table can have
 // Calls that one workgroup does, up to 8 forks and tables of up to 4,096 entries: a launch is 2-3
 // us of the GPU's time and 4-5 of the host's. A fork of one row, its copy and its release 29 us
-// in place of 39 (in a graph 23 and 21); 7 forks of 7,000 tokens 30 and 43 (24.5 and 25.5); at
+// in place of 39 (in a graph 16 and 21); 7 forks of 7,000 tokens 30 and 43 (20 and 25.5); at
 // 8,192 entries the two are even, at 16,384 one workgroup takes 2.5 times as long.
 constexpr int kSmallForks = 8, kSmallThreads = 128, kSmallEntries = 4096;
 constexpr int kCode = 1 << 30;             // codes of entries: -(kCode + 1 + place), place < kCode
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kRowThreads) void shared_put_kernel(SharedRelease r
 }
 
 // All of it by one workgroup, for tables of up to kSmallEntries entries, which its threads keep:
-// the counts change by atomics, so they are read past the first-level cache. 9.3 us, of round
+// the counts change by atomics, so they are read past the first-level cache. 3.0 us, of round
 // trips: lengths, table, three to the counts, the list.
 constexpr int kOneThreads = 1024, kOneEntries = kSmallEntries / kOneThreads;
 __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r) {
@@ -264,10 +264,13 @@ __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r
   auto holders = [&](int p) {
     return __hip_atomic_load(&r.shares[p], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   };
+  // A wave's atomics are in the L2, where all of the workgroup's reads of the counts go: a fence
+  // of the whole GPU would write the L2 back besides, 3 us each time.
+  auto arrived = [] { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
 #pragma unroll
   for (int u = 0; u < kOneEntries; ++u)
     if (page[u] >= 0) atomicSub(&r.shares[page[u]], 1);
-  __threadfence();
+  arrived();
   __syncthreads();
   int held[kOneEntries];
 #pragma unroll
@@ -276,7 +279,7 @@ __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r
 #pragma unroll
   for (int u = 0; u < kOneEntries; ++u)
     if (held[u] < 0) atomicMin(&r.shares[page[u]], -(kCode + 1) - (u * kOneThreads + tid));
-  __threadfence();
+  arrived();
   __syncthreads();
   uint64_t votes[kOneEntries];
   bool free[kOneEntries];
