@@ -17,22 +17,23 @@
 // (the launch and the host); 64 rows of 151,936 fp32 with 4k to 32k tokens each, in place 23 us,
 // out of place 25 (3.1 TB/s), where the counting of the histories, 19 times from the L2, takes
 // most of the time; 256 rows bf16 out of place 58 us; 700 rows in 32 trees, bf16, every
-// adjustment, histories of 2k to 24k, 152 us (441 MB, 2.9 TB/s; a copy of as much would take 90),
-// with histories of 100 to 500 127 us.
+// adjustment, histories of 2k to 24k, 146 us (441 MB, 3.0 TB/s; a copy of as much would take 90),
+// with histories of 100 to 500 123 us.
 #include "ra_device.h"
 #include "ra_internal.h"
 
 namespace ra {
 namespace {
 
-constexpr int kThreads = 512;              // (1,024: no faster)
+constexpr int kThreads = 512;              // (1,024: no faster; 256: 23.5 -> 36 us for the 64 rows)
 constexpr int kMaxRows = 32;               // of a workgroup (16: 2,457 rows of trees 477 us, 32: 463)
 // Words of LDS for a chunk and the 16-byte unit it begins in: four workgroups of them a compute
 // unit. (Twice as many halve how often a history is read, but fewer workgroups are on the
-// unit: 64 rows of 151,936 36 -> 42 us.)
+// unit: 64 rows of 151,936 36 -> 42 us when that was tried. 9,984, the most that leave four:
+// 64 rows in place 23.5 -> 20.8, 256 rows 65 -> 72, 3,278 rows of 32,000 176 -> 190.)
 constexpr int kSlots = 8192;
 constexpr int kChunk = kSlots - 8;         // logits of a chunk
-constexpr int kTogether = 1024;            // workgroups of several rows that are on the GPU together
+constexpr int kTogether = 512;             // workgroups of several rows that are on the GPU together
 constexpr int kBatch = 4;                  // loads of four tokens that a thread has in flight
 constexpr uint32_t kPrompt = 1u << 31;
 
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(kThreads, kMany ? 4 : 8) void adjust_kernel(AdjustA
 // Rows of logits that a workgroup takes: several where the rows of a tree share their history's
 // counts, and as few as let the call end with whole rounds of workgroups, one if it can. bf16 rows
 // of 151,936 in trees, with this rule, one a workgroup, and as many as leave 2,048 workgroups:
-// 138 rows 40, 47 and 47 us; 318 rows 75, 98 and 92; 700 rows 152, 231 and 163.
+// 138 rows 36, 47 and 47 us; 318 rows 73, 98 and 92; 700 rows 146, 231 and 163.
 static int32_t adjust_rows(int32_t N, int32_t chunks, bool trees) {
   if (!trees) return 1;
   for (int64_t round = 1;; ++round) {
