@@ -290,10 +290,10 @@ __global__ __launch_bounds__(kThreads, kMany ? 4 : 8) void adjust_kernel(AdjustA
 // 138 rows 36, 47 and 47 us; 318 rows 73, 98 and 92; 700 rows 146, 231 and 163.
 static int32_t adjust_rows(int32_t N, int32_t chunks, bool trees) {
   if (!trees) return 1;
-  for (int64_t round = 1;; ++round) {
-    const int64_t groups = max((int64_t)1, round * kTogether / chunks);
-    if (const int64_t rows = (N + groups - 1) / groups; rows <= kMaxRows) return (int32_t)max((int64_t)1, rows);
-  }
+  const int64_t least = ((int64_t)N + kMaxRows - 1) / kMaxRows;         // groups of rows
+  const int64_t rounds = (least * chunks + kTogether - 1) / kTogether;
+  const int64_t groups = max((int64_t)1, rounds * kTogether / chunks);
+  return (int32_t)max((int64_t)1, (N + groups - 1) / groups);
 }
 
 static int32_t adjust_chunks(int32_t V) { return (V + kChunk - 1) / kChunk; }
