@@ -627,7 +627,9 @@ int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
  * of its arrays.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (negative sizes, too few mask_words);
  *         RA_ERR_UNSUPPORTED (B > 65535, max_q_len > RA_MAX_DRAFT_NODES, shared memory);
- *         RA_ERR_HIP. B == 0, total_q == 0 or max_q_len == 0 launch nothing.
+ *         RA_ERR_HIP. B == 0 launches nothing, nor does draft_tree_mask with total_q == 0 or
+ *         max_q_len == 0; draft_tree_accept sets the rows' outputs then too (with total_q == 0
+ *         the nodes' arrays may be NULL).
  */
 #define RA_MAX_DRAFT_NODES 1024
 int draft_tree_mask(const int32_t *parents, const int32_t *cu_q, const int32_t *ctx_lens,
@@ -659,16 +661,17 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
  *   workspace   device scratch of at least rollout_attn_decode_tree_workspace_size(B, Hq, Hkv,
  *               total_q, max_q_len, max_kv_len) bytes (contents on entry ignored); NULL where
  *               the size is 0. Calls that share one must not overlap.
- * Longer calls (max_kv_len above 512) are cut into equal shares of their work. Where rows are
- * cut, and with it the order of fp32 sums, depends on the lengths and trees' sizes of all the call's
- * rows, their order, Hq, Hkv, max_q_len and max_kv_len, and on nothing else: the same call gives
+ * Longer calls (max_kv_len above 512, and more where there are many rows and KV heads) are cut
+ * into equal shares of their work. Where rows are cut, and with it the order of fp32 sums, depends on
+ * the lengths and trees' sizes of all the call's rows, their order and number, Hq, Hkv, max_q_len and
+ * max_kv_len, and on nothing else: the same call gives
  * the same bits, while a row's result beside other rows can differ by the order of sums.
  * Weights meet the values in two bf16 parts, off by 2^-16 of a weight, as in decode (in three, off
  * by 2^-24, where max_q_len * Hq / Hkv is at most 32 and the pools are bf16).
  * Errors: as rollout_attn_append; RA_ERR_SHAPE also for too few mask_words; RA_ERR_UNSUPPORTED
  *         (Hq / Hkv > 256, B > 65535, max_q_len > RA_MAX_DRAFT_NODES, max_kv_len > 2^30, total_q *
- *         Hq >= 2^31, 2^31 or more workgroups, q, pools, out or workspace not 16-byte aligned). B == 0, total_q == 0 or max_q_len ==
- *         0 launch nothing.
+ *         Hq >= 2^31, 2^31 or more workgroups, q, pools, out or workspace not 16-byte aligned).
+ *         B == 0, total_q == 0 or max_q_len == 0 launch nothing.
  */
 size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
                                                int32_t total_q, int32_t max_q_len,

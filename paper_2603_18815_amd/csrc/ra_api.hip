@@ -625,9 +625,9 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
                       int32_t *kv_lens, int32_t *next_tokens, hipStream_t stream) {
   const int s = check_draft(B, total_q, max_q_len);
   if (s != RA_OK) return s;
-  if (B == 0 || total_q == 0 || max_q_len == 0) return RA_OK;
-  if (!parents || !draft_tokens || !chosen || !cu_q || !ctx_lens || !path || !tokens ||
-      !accepted || !kv_lens || !next_tokens)
+  if (B == 0) return RA_OK;
+  if (!cu_q || !ctx_lens || !accepted || !kv_lens || !next_tokens ||
+      (total_q > 0 && (!parents || !draft_tokens || !chosen || !path || !tokens)))
     return RA_ERR_NULL;
   const int64_t rows = 4 * (int64_t)B, nodes = 4 * (int64_t)total_q;
   if (overlap({{parents, nodes, false}, {draft_tokens, nodes, false}, {chosen, nodes, false},

@@ -61,9 +61,11 @@ def test_draft_tree_accept_validation(lib):
     go = lambda **kw: call(lib.draft_tree_accept, names, base, **kw)
     for n in arrays:
         assert go(**{n: None}) == NULL
+    for n in ("cu", "ctx", "acc", "lens", "nxt"):      # rows without nodes have results too
+        assert go(total=0, **{n: None}) == NULL and go(mq=0, **{n: None}) == NULL
+    assert go(B=0) == OK
     for n in ("B", "total", "mq"):
         assert go(**{n: -1}) == SHAPE
-        assert go(**{n: 0}) == OK
     assert go(mq=1025) == UNSUPPORTED and go(B=65536) == UNSUPPORTED
     for out in ("path", "tokens", "acc", "lens", "nxt"):
         for other in arrays:

@@ -90,3 +90,10 @@ def test_empty_calls(device):
     assert mask.shape == (0, 1) and pos.shape == (0,)
     got = ra.draft_tree_accept(none, none, none, i32([0]), none)
     assert all(x.numel() == 0 for x in got)
+
+
+def test_rows_without_any_node_have_results(device):
+    none = i32([])
+    path, tokens, acc, lens, nxt = ra.draft_tree_accept(none, none, none, i32([0] * 4), i32([0, 7, 90]))
+    assert path.numel() == 0 and tokens.numel() == 0
+    assert acc.tolist() == [0, 0, 0] and lens.tolist() == [0, 7, 90] and nxt.tolist() == [-1] * 3
