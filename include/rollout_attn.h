@@ -771,8 +771,8 @@ int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int
  *
  * kv_page_copy copies the pages src_pages[i] to dst_pages[i] (int32 [n]) of both pools, all KV
  * heads, bit for bit; pairs with a page outside [0, num_pages) are passed over. No page may be
- * the destination of two pairs, or of one and the source of another. The block table is
- * not used and may be NULL.
+ * the destination of two pairs, or of one and the source of another. The block table and
+ * its bt_stride are not used, whatever they hold.
  *
  * What is written must not share memory with another array. Calls on one free list must not
  * overlap in time.

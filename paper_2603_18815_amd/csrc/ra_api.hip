@@ -799,8 +799,9 @@ int kv_page_copy(const ra_paged_kv *kv, const int32_t *src_pages, const int32_t 
                  int32_t n, hipStream_t stream) {
   if (n < 0) return RA_ERR_SHAPE;
   if (!kv) return RA_ERR_NULL;
-  ra_paged_kv pools = *kv;   // the table is not used
-  if (!pools.block_table) pools.block_table = static_cast<const int32_t *>(pools.k_pool);
+  ra_paged_kv pools = *kv;   // the table is not used, nor checked
+  pools.block_table = static_cast<const int32_t *>(pools.k_pool);
+  pools.bt_stride = 1;
   const int s = check_kv(&pools);
   if (s != RA_OK) return s;
   if (n == 0) return RA_OK;

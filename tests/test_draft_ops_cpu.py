@@ -231,3 +231,14 @@ def test_the_binding_refuses_host_tensors_and_missing_partners():
               lambda: ra.block_table_release_shared(i(2, 4), i(2), i(2), i(9), i(9), i(1))):
         with pytest.raises(ValueError, match="GPU tensor"):
             f()
+
+
+def test_page_copy_takes_pools_without_a_table(lib):
+    """Nothing that describes the block table is looked at."""
+    for kw in (dict(bt=0, stride=0), dict(stride=0), dict(bt=0, stride=-1), dict(bt=0)):
+        bare = pools(**kw)
+        assert lib.kv_page_copy(ctypes.byref(bare), None, None, 0, None) == OK, kw
+        assert lib.kv_page_copy(ctypes.byref(bare), None, at(2), 1, None) == NULL, kw
+    for kw, want in ((dict(k=0), NULL), (dict(v=0), NULL), (dict(num=0), SHAPE), (dict(hkv=0), SHAPE)):
+        bad = pools(bt=0, stride=0, **kw)
+        assert lib.kv_page_copy(ctypes.byref(bad), at(1), at(2), 1, None) == want, kw
