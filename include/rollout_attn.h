@@ -670,7 +670,9 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
  * by 2^-24, where max_q_len * Hq / Hkv is at most 32 and the pools are bf16).
  * Errors: as rollout_attn_append; RA_ERR_SHAPE also for too few mask_words; RA_ERR_UNSUPPORTED
  *         (Hq / Hkv > 256, B > 65535, max_q_len > RA_MAX_DRAFT_NODES, max_kv_len > 2^30, total_q *
- *         Hq >= 2^31, 2^31 or more workgroups, q, pools, out or workspace not 16-byte aligned).
+ *         Hq >= 2^31, a launch of 2^32 threads or more: B * Hkv tiles of up to 128 query rows >= 2^24
+ *         or of 256 >= 2^23 where rows are not cut, total_q * Hkv >= 2^26 where they are; q, pools,
+ *         out or workspace not 16-byte aligned).
  *         B == 0, total_q == 0 or max_q_len == 0 launch nothing.
  */
 size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
@@ -720,7 +722,8 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
  *         history_width < 0, history_stride < history_width with B > 1, num_bias < 0,
  *         allowed_stride < ceil(V / 32), num_allowed < 0, mask_words <= 0 with tree_mask, B != N
  *         without cu_rows); RA_ERR_UNSUPPORTED (an unknown
- *         logits_dtype, V > 2^24, 2^31 or more workgroups, shared memory); RA_ERR_HIP.
+ *         logits_dtype, V > 2^24, a launch of 2^32 threads or more: N * ceil(V / 8184) >= 2^23, with
+ *         cu_rows a 32nd of it, shared memory); RA_ERR_HIP.
  *         N == 0 or B == 0 launch nothing.
  */
 typedef struct {
@@ -778,7 +781,7 @@ int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int
  * overlap in time.
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (negative sizes, bt_stride <= 0, num_pages <= 0,
  *         free_capacity < num_pages for the release); RA_ERR_UNSUPPORTED (B > 65535, n > 65535
- *         for a fork, n * Hkv >= 2^31, B * bt_stride >= 2^30 for the release, bt_stride * 16 >
+ *         for a fork, n * Hkv >= 2^24, B * bt_stride >= 2^30 for the release, bt_stride * 16 >
  *         2^31 - 1, shared memory, pools not 16-byte aligned); RA_ERR_WORKSPACE; RA_ERR_HIP.
  *         n == 0 forks set *taken = 0, B == 0 releases *released = 0; n == 0 copies launch
  *         nothing.
@@ -811,7 +814,7 @@ int kv_page_copy(const ra_paged_kv *kv, const int32_t *src_pages, const int32_t 
  *   counts     int32 [B] or NULL (all of cu_src[b] .. cu_src[b+1]-1)
  *   max_count  host: an upper bound of the tokens of a row
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (negative sizes); RA_ERR_UNSUPPORTED (the page layout,
- *         B > 65535, B * Hkv >= 2^31, pools not 16-byte aligned); RA_ERR_HIP. B == 0, total == 0
+ *         B > 65535, B * Hkv >= 2^24, pools not 16-byte aligned); RA_ERR_HIP. B == 0, total == 0
  *         or max_count == 0 launch nothing.
  */
 int kv_page_compact(const ra_paged_kv *kv, const int32_t *start_pos, const int32_t *cu_src,

@@ -298,10 +298,14 @@ static int32_t adjust_rows(int32_t N, int32_t chunks, bool trees) {
 
 static int32_t adjust_chunks(int32_t V) { return (V + kChunk - 1) / kChunk; }
 
-int64_t adjust_groups(int32_t N, int32_t V, bool trees) {
+static int64_t adjust_groups(int32_t N, int32_t V, bool trees) {
   const int32_t chunks = adjust_chunks(V);
   const int64_t rows = adjust_rows(N, chunks, trees);
   return (N + rows - 1) / rows * chunks;
+}
+
+int64_t adjust_threads(int32_t N, int32_t V, bool trees) {
+  return adjust_groups(N, V, trees) * kThreads;
 }
 
 hipError_t launch_adjust(const AdjustArgs &a, bool bf16, hipStream_t stream) {

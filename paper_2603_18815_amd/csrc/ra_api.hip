@@ -666,7 +666,9 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
   if (!aligned16(q) || !aligned16(out) || !aligned16(kv->k_pool) || !aligned16(kv->v_pool))
     return RA_ERR_UNSUPPORTED;
   const ra::TreePlan plan = ra::tree_plan(B, Hq, kv->num_kv_heads, max_q_len, max_kv_len);
-  if (plan.groups > INT32_MAX || (int64_t)total_q * Hq > INT32_MAX) return RA_ERR_UNSUPPORTED;
+  if ((int64_t)total_q * Hq > INT32_MAX ||
+      ra::tree_threads(plan, total_q, Hq, kv->num_kv_heads) > ra::kMaxThreads)
+    return RA_ERR_UNSUPPORTED;
   const size_t need = ra::tree_workspace_bytes(B, plan);
   if (need > 0 && (!workspace || workspace_bytes < need)) return RA_ERR_WORKSPACE;
   if (need > 0 && !aligned16(workspace)) return RA_ERR_UNSUPPORTED;
@@ -694,7 +696,7 @@ int token_logits_adjust(const void *logits, int32_t logits_dtype, int32_t N, int
       (j.bias_tokens && (!j.bias_values || !j.cu_bias)) || !j.draft_tokens != !j.tree_mask ||
       (j.draft_tokens && !j.cu_rows))
     return RA_ERR_NULL;
-  if (ra::adjust_groups(N, V, j.cu_rows != nullptr) > INT32_MAX) return RA_ERR_UNSUPPORTED;
+  if (ra::adjust_threads(N, V, j.cu_rows != nullptr) > ra::kMaxThreads) return RA_ERR_UNSUPPORTED;
   const bool bf16 = logits_dtype == RA_LOGITS_BF16;
   const int64_t size = bf16 ? 2 : 4, rows = 4 * (int64_t)B, each = 4 * (int64_t)N;
   const bool in_place = out == logits && (N == 1 || out_stride == row_stride);
@@ -806,8 +808,8 @@ int kv_page_copy(const ra_paged_kv *kv, const int32_t *src_pages, const int32_t 
   if (s != RA_OK) return s;
   if (n == 0) return RA_OK;
   if (!src_pages || !dst_pages) return RA_ERR_NULL;
-  if ((int64_t)n * kv->num_kv_heads > INT32_MAX || !aligned16(kv->k_pool) ||
-      !aligned16(kv->v_pool))
+  if ((int64_t)n * kv->num_kv_heads * ra::kPageThreads > ra::kMaxThreads ||
+      !aligned16(kv->k_pool) || !aligned16(kv->v_pool))
     return RA_ERR_UNSUPPORTED;
   return hip_status(ra::launch_page_copy(to_internal(&pools), src_pages, dst_pages, n, stream));
 }
@@ -818,8 +820,8 @@ int kv_page_compact(const ra_paged_kv *kv, const int32_t *start_pos, const int32
   if (B < 0 || total < 0 || max_count < 0) return RA_ERR_SHAPE;
   const int s = check_kv(kv);
   if (s != RA_OK) return s;
-  if (B > kMaxGridYZ || (int64_t)B * kv->num_kv_heads > INT32_MAX || !aligned16(kv->k_pool) ||
-      !aligned16(kv->v_pool))
+  if (B > kMaxGridYZ || (int64_t)B * kv->num_kv_heads * ra::kPageThreads > ra::kMaxThreads ||
+      !aligned16(kv->k_pool) || !aligned16(kv->v_pool))
     return RA_ERR_UNSUPPORTED;
   if (B == 0 || total == 0 || max_count == 0) return RA_OK;
   if (!start_pos || !cu_src || !src_index) return RA_ERR_NULL;

@@ -313,12 +313,10 @@ __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r
 }
 
 // ---- pages' contents ----
-constexpr int kCopyThreads = 256;
-
 // One page of one KV head a workgroup, 16 bytes a thread and pool. Bound by HBM: 434 pages of 8 KV
 // heads in bf16 (57 MB read and written, the sources of eight copies the same) 7.5 us.
 template <bool kFp8>
-__global__ __launch_bounds__(kCopyThreads) void page_copy_kernel(uint8_t *k_pool, uint8_t *v_pool,
+__global__ __launch_bounds__(kPageThreads) void page_copy_kernel(uint8_t *k_pool, uint8_t *v_pool,
                                                                  const int32_t *src,
                                                                  const int32_t *dst, int32_t hkv,
                                                                  int32_t num_pages) {
@@ -336,7 +334,6 @@ __global__ __launch_bounds__(kCopyThreads) void page_copy_kernel(uint8_t *k_pool
 }
 
 constexpr int kMoveTokens = 32;            // moved together
-constexpr int kMoveThreads = 256;
 
 // The kept tokens of one row and KV head, up to 32 a step. Indices rise, so a token never moves
 // behind where it was and the tokens of one step lie before the sources of all later ones: a
@@ -348,15 +345,15 @@ constexpr int kMoveThreads = 256;
 // in whole sectors. 4 rows of up to 8 tokens 4.1 us; 512 rows, some 16 tokens each, 8 KV heads 32 us
 // (4.3 TB/s of sectors), with single values stored one by one 40.
 template <typename E>
-__global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
+__global__ __launch_bounds__(kPageThreads) void page_compact_kernel(
     E *k_pool, E *v_pool, const int32_t *block_table, int32_t bt_stride, int32_t num_pages,
     int32_t hkv, const int32_t *start_pos, const int32_t *cu_src, const int32_t *src_index,
     const int32_t *counts, int32_t total, int32_t max_count) {
   constexpr int kUnit = 16 / sizeof(E), kUnits = kHeadDim / kUnit;      // of a key
-  constexpr int kKeys = kMoveTokens * kUnits / kMoveThreads;            // units a thread
+  constexpr int kKeys = kMoveTokens * kUnits / kPageThreads;            // units a thread
   constexpr int kHalf = kPage / 2;
   constexpr int kHalves = kMoveTokens / kHalf + 1;                      // that 32 tokens can lie in
-  constexpr int kValues = (kHalves * kHeadDim + kMoveThreads - 1) / kMoveThreads;
+  constexpr int kValues = (kHalves * kHeadDim + kPageThreads - 1) / kPageThreads;
   constexpr int kWords = kHalf * sizeof(E) / 4;
   typedef uint32_t Eight __attribute__((ext_vector_type(kWords)));      // a half of a value row
   struct Move {
@@ -393,7 +390,7 @@ __global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
     u32x4 k[kKeys];
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
-      const int x = i * kMoveThreads + tid, token = x / kUnits, unit = x % kUnits;
+      const int x = i * kPageThreads + tid, token = x / kUnits, unit = x % kUnits;
       const Move mv = move[lead + token];
       if (token < m && mv.from >= 0)
         k[i] = *reinterpret_cast<const u32x4 *>(k_pool + block(mv.from) + mv.slot * kHeadDim + unit * kUnit);
@@ -402,7 +399,7 @@ __global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
     uint32_t moved[kValues];                                // bits of the half's slots
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
-      const int x = i * kMoveThreads + tid, half = x / kHeadDim, d = x % kHeadDim;
+      const int x = i * kPageThreads + tid, half = x / kHeadDim, d = x % kHeadDim;
       moved[i] = 0;
       if (half >= kHalves) continue;
 #pragma unroll
@@ -423,14 +420,14 @@ __global__ __launch_bounds__(kMoveThreads) void page_compact_kernel(
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kKeys; ++i) {
-      const int x = i * kMoveThreads + tid, token = x / kUnits, unit = x % kUnits;
+      const int x = i * kPageThreads + tid, token = x / kUnits, unit = x % kUnits;
       const Move mv = move[lead + token];
       if (token < m && mv.from >= 0)
         *reinterpret_cast<u32x4 *>(k_pool + block(mv.to) + mv.to_slot * kHeadDim + unit * kUnit) = k[i];
     }
 #pragma unroll
     for (int i = 0; i < kValues; ++i) {
-      const int x = i * kMoveThreads + tid, half = x / kHeadDim, d = x % kHeadDim;
+      const int x = i * kPageThreads + tid, half = x / kHeadDim, d = x % kHeadDim;
       if (moved[i] == 0) continue;
       const Move mv = move[half * kHalf + __ffs(moved[i]) - 1];
       E *to = v_pool + block(mv.to) + d * kPage + mv.to_slot / kHalf * kHalf;
@@ -498,10 +495,10 @@ hipError_t launch_page_copy(const PagedKV &kv, const int32_t *src_pages, const i
   uint8_t *k = reinterpret_cast<uint8_t *>(kv.k_pool), *v = reinterpret_cast<uint8_t *>(kv.v_pool);
   const unsigned grid = (unsigned)n * (unsigned)kv.hkv;
   if (kv.fp8)
-    page_copy_kernel<true><<<grid, kCopyThreads, 0, stream>>>(k, v, src_pages, dst_pages, kv.hkv,
+    page_copy_kernel<true><<<grid, kPageThreads, 0, stream>>>(k, v, src_pages, dst_pages, kv.hkv,
                                                              kv.num_pages);
   else
-    page_copy_kernel<false><<<grid, kCopyThreads, 0, stream>>>(k, v, src_pages, dst_pages, kv.hkv,
+    page_copy_kernel<false><<<grid, kPageThreads, 0, stream>>>(k, v, src_pages, dst_pages, kv.hkv,
                                                               kv.num_pages);
   return hipGetLastError();
 }
@@ -511,12 +508,12 @@ hipError_t launch_page_compact(const PagedKV &kv, const int32_t *start_pos, cons
                                int32_t total, int32_t max_count, hipStream_t stream) {
   const unsigned grid = (unsigned)B * (unsigned)kv.hkv;
   if (kv.fp8)
-    page_compact_kernel<uint8_t><<<grid, kMoveThreads, 0, stream>>>(
+    page_compact_kernel<uint8_t><<<grid, kPageThreads, 0, stream>>>(
         reinterpret_cast<uint8_t *>(kv.k_pool), reinterpret_cast<uint8_t *>(kv.v_pool),
         kv.block_table, kv.bt_stride, kv.num_pages, kv.hkv, start_pos, cu_src, src_index, counts,
         total, max_count);
   else
-    page_compact_kernel<uint16_t><<<grid, kMoveThreads, 0, stream>>>(
+    page_compact_kernel<uint16_t><<<grid, kPageThreads, 0, stream>>>(
         kv.k_pool, kv.v_pool, kv.block_table, kv.bt_stride, kv.num_pages, kv.hkv, start_pos,
         cu_src, src_index, counts, total, max_count);
   return hipGetLastError();

@@ -134,6 +134,9 @@ hipError_t launch_table_release(const int32_t *lens, const int32_t *keep_lens,
                                 int32_t *free_pages, int32_t *free_count, int32_t capacity,
                                 int32_t max_pages, int32_t *released, hipStream_t stream);
 
+// Threads that a launch can have along its grid.
+constexpr int64_t kMaxThreads = UINT32_MAX;
+
 // ---- trees of drafted tokens ----
 constexpr int32_t kMaxDraftNodes = 1024;       // nodes of a tree
 struct TreePlan {
@@ -143,6 +146,7 @@ struct TreePlan {
   int64_t tiles;          // of the query rows of the largest tree, a KV head
   int64_t groups;         // workgroups
 };
+int64_t tree_threads(const TreePlan &p, int32_t total_q, int32_t hq, int32_t hkv);   // of its largest launch
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len);
 size_t tree_workspace_bytes(int32_t B, const TreePlan &p);
 hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ctx_lens,
@@ -179,10 +183,11 @@ struct AdjustArgs {
   const int32_t *cu_rows, *draft_tokens;
   const uint64_t *tree_mask;
 };
-int64_t adjust_groups(int32_t N, int32_t V, bool trees);   // workgroups
+int64_t adjust_threads(int32_t N, int32_t V, bool trees);
 hipError_t launch_adjust(const AdjustArgs &a, bool bf16, hipStream_t stream);
 
 // ---- rows that share pages ----
+constexpr int32_t kPageThreads = 256;          // of a page or row and KV head, copied or compacted
 hipError_t launch_table_fork(const int32_t *src_rows, const int32_t *dst_rows, const int32_t *lens,
                              int32_t n, int32_t *block_table, int32_t B, int32_t bt_stride,
                              int32_t *shares, int32_t num_pages, const int32_t *free_pages,

@@ -1224,6 +1224,16 @@ TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_
   return p;
 }
 
+static bool join_by_head(int32_t total_q, int32_t hq) { return (int64_t)total_q * hq <= kFewHeads; }
+
+int64_t tree_threads(const TreePlan &p, int32_t total_q, int32_t hq, int32_t hkv) {
+  const int64_t tiles = p.groups * (p.rows == 256 ? 8 : kSplitWaves) * kWave;
+  if (p.direct) return tiles;
+  const int64_t joins = (int64_t)total_q * (join_by_head(total_q, hq) ? hq : hkv);
+  const int64_t join = (joins + kJoinWaves - 1) / kJoinWaves * (kJoinWaves * kWave);
+  return tiles > join ? tiles : join;
+}
+
 namespace {
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
@@ -1279,7 +1289,7 @@ hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ct
   a.scale_log2 = scale * kLog2e * kv.k_scale;
   a.v_scale = kv.v_scale;
   const dim3 grid((unsigned)p.groups);
-  const bool by_head = (int64_t)total_q * hq <= kFewHeads;
+  const bool by_head = join_by_head(total_q, hq);
   const int64_t joins = (int64_t)total_q * (by_head ? hq : kv.hkv);
   const dim3 join_grid((unsigned)((joins + kJoinWaves - 1) / kJoinWaves)), join(kJoinWaves * kWave);
   auto launch = [&](auto rows) {

@@ -242,3 +242,22 @@ def test_page_copy_takes_pools_without_a_table(lib):
     for kw, want in ((dict(k=0), NULL), (dict(v=0), NULL), (dict(num=0), SHAPE), (dict(hkv=0), SHAPE)):
         bad = pools(bt=0, stride=0, **kw)
         assert lib.kv_page_copy(ctypes.byref(bad), at(1), at(2), 1, None) == want, kw
+
+
+def test_launches_of_more_threads_than_a_grid_can_have_are_refused(lib):
+    """A launch has fewer than 2^32 threads: calls just past that, of sizes whose arrays fit the
+    GPU's memory."""
+    z = ctypes.byref(adjust())
+    trees = ctypes.byref(adjust(cu_rows=at(3)))
+    for N, V, a in ((1 << 23, 2, z), (1 << 22, 9000, z), (1 << 28, 2, trees)):
+        for dt in (0, 1):
+            assert lib.token_logits_adjust(at(1), dt, N, V, V, a, N, at(2), V, None) == UNSUPPORTED
+    two, many, wide, cut = pools(), pools(hkv=257), pools(hkv=129, stride=16), pools(hkv=256, stride=512)
+    ref = ctypes.byref
+    assert lib.kv_page_copy(ref(two), at(1), at(2), 1 << 23, None) == UNSUPPORTED
+    assert lib.kv_page_compact(ref(many), at(1), at(2), at(3), None, 65535, 5, 4, None) == UNSUPPORTED
+    for kv, heads, total, nodes, keys in ((many, 257, 65535, 1, 16), (wide, 129, 65535, 129, 200),
+                                          (cut, 256, 1 << 18, 4, 8192)):
+        assert lib.rollout_attn_decode_tree(
+            at(1), at(2), at(3), at(4), 3, ref(kv), 65535, heads, total, nodes, keys, 0.1, at(5), None,
+            at(6), BIG, None) == UNSUPPORTED, heads
