@@ -660,7 +660,11 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
  *               are not touched
  *   workspace   device scratch of at least rollout_attn_decode_tree_workspace_size(B, Hq, Hkv,
  *               total_q, max_q_len, max_kv_len) bytes (contents on entry ignored); NULL where
- *               the size is 0. Calls that share one must not overlap.
+ *               the size is 0. Calls that share one must not overlap. The size can fall, to 0
+ *               too, as B, max_q_len or max_kv_len grows (32 heads on 8, 8 nodes, 4,096 keys: 17 MB
+ *               for 16 rows, none for 64), so that of a loop's largest call need not hold the
+ *               smaller ones: rollout_attn_decode_tree_max_workspace_size is enough for all
+ *               calls of up to that many rows, nodes and keys (at most 68 MB and 8 bytes a row).
  * Longer calls (max_kv_len above 512, and more where there are many rows and KV heads) are cut
  * into equal shares of their work. Where rows are cut, and with it the order of fp32 sums, depends on
  * the lengths and trees' sizes of all the call's rows, their order and number, Hq, Hkv, max_q_len and
@@ -678,6 +682,8 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
 size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
                                                int32_t total_q, int32_t max_q_len,
                                                int32_t max_kv_len);
+size_t rollout_attn_decode_tree_max_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
+                                                   int32_t max_q_len, int32_t max_kv_len);
 int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *ctx_lens,
                              const uint64_t *tree_mask, int32_t mask_words, const ra_paged_kv *kv,
                              int32_t B, int32_t Hq, int32_t total_q, int32_t max_q_len,

@@ -40,6 +40,7 @@ __all__ = ["PagedKV", "decode", "decode_noalloc", "decode_shared_prefix", "appen
            "token_sample", "token_sample_workspace_size", "linear_decode", "linear_append",
            "linear_append_workspace_size", "block_table_extend", "block_table_release",
            "draft_tree_mask", "draft_tree_accept", "decode_tree", "decode_tree_workspace_size",
+           "decode_tree_max_workspace_size",
            "token_logits_adjust", "block_table_fork", "block_table_release_shared",
            "block_table_release_shared_workspace_size", "kv_page_copy", "kv_page_compact",
            "abi_version", "RolloutAttnError"]
@@ -953,6 +954,14 @@ def decode_tree_workspace_size(B: int, Hq: int, Hkv: int, total_q: int, max_q_le
                                max_kv_len: int) -> int:
     return int(_lib.load().rollout_attn_decode_tree_workspace_size(B, Hq, Hkv, total_q, max_q_len,
                                                                    max_kv_len))
+
+
+def decode_tree_max_workspace_size(B: int, Hq: int, Hkv: int, max_q_len: int,
+                                   max_kv_len: int) -> int:
+    """Bytes that are enough for every decode_tree call of up to B rows, max_q_len nodes a row and
+    max_kv_len keys: decode_tree_workspace_size of a call can be less than that of a smaller one."""
+    return int(_lib.load().rollout_attn_decode_tree_max_workspace_size(B, Hq, Hkv, max_q_len,
+                                                                       max_kv_len))
 
 
 def decode_tree(q: torch.Tensor, cu_q: torch.Tensor, ctx_lens: torch.Tensor,

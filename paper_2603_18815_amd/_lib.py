@@ -53,6 +53,7 @@ EXPORTS = (
     "draft_tree_mask",
     "draft_tree_accept",
     "rollout_attn_decode_tree_workspace_size",
+    "rollout_attn_decode_tree_max_workspace_size",
     "rollout_attn_decode_tree",
     "token_logits_adjust",
     "kv_block_table_fork",
@@ -197,6 +198,8 @@ def load() -> ctypes.CDLL:
     lib.draft_tree_accept.restype = ctypes.c_int
     lib.rollout_attn_decode_tree_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32]
     lib.rollout_attn_decode_tree_workspace_size.restype = sz
+    lib.rollout_attn_decode_tree_max_workspace_size.argtypes = [i32, i32, i32, i32, i32]
+    lib.rollout_attn_decode_tree_max_workspace_size.restype = sz
     lib.rollout_attn_decode_tree.argtypes = [vp, vp, vp, vp, i32, kvp, i32, i32, i32, i32, i32, f32,
                                              vp, vp, vp, sz, vp]
     lib.rollout_attn_decode_tree.restype = ctypes.c_int

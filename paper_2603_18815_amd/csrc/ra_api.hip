@@ -649,6 +649,14 @@ size_t rollout_attn_decode_tree_workspace_size(int32_t B, int32_t Hq, int32_t Hk
   return ra::tree_workspace_bytes(B, ra::tree_plan(B, Hq, Hkv, max_q_len, max_kv_len));
 }
 
+size_t rollout_attn_decode_tree_max_workspace_size(int32_t B, int32_t Hq, int32_t Hkv,
+                                                   int32_t max_q_len, int32_t max_kv_len) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_q_len <= 0 ||
+      max_q_len > RA_MAX_DRAFT_NODES || max_kv_len <= 0)
+    return 0;
+  return ra::tree_most_workspace_bytes(B, Hq, Hkv, max_q_len, max_kv_len);
+}
+
 int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *ctx_lens,
                              const uint64_t *tree_mask, int32_t mask_words, const ra_paged_kv *kv,
                              int32_t B, int32_t Hq, int32_t total_q, int32_t max_q_len,

@@ -149,6 +149,9 @@ struct TreePlan {
 int64_t tree_threads(const TreePlan &p, int32_t total_q, int32_t hq, int32_t hkv);   // of its largest launch
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len);
 size_t tree_workspace_bytes(int32_t B, const TreePlan &p);
+// The most that a call of up to so many rows, nodes and keys needs.
+size_t tree_most_workspace_bytes(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len,
+                                 int32_t max_kv_len);
 hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ctx_lens,
                        const uint64_t *mask, int32_t words, const PagedKV &kv, int32_t B,
                        int32_t hq, int32_t total_q, int32_t max_q_len, int32_t max_kv_len,

@@ -26,6 +26,7 @@
 // the compute units idle for 13 to 29 % of the time, and wrote 2 to 8 times the partial
 // results.) Calls of short rows (kDirectKeys) take a workgroup a tile and one launch: there is
 // no join, and no tile begins twice.
+#include <algorithm>
 #include <type_traits>
 
 #include "ra_device.h"
@@ -1172,12 +1173,17 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void tree_join_kernel(TreeArgs 
   }
 }
 
-template <int kRows>
-void plan_line(TreePlan &p, int64_t units, int32_t max_kv_len, int64_t groups) {
-  constexpr int keys = block_keys<kRows>();
-  const int64_t blocks = units * ((max_kv_len + keys - 1) / keys);
-  p.groups = blocks < groups ? blocks : groups;
+// Workgroups of a call that is cut: as many as are on the GPU together, or a block each. Half of
+// them: 64 rows of 4k to 32k keys (4.6 GB), 8 nodes 732 us for 732, fp8 498 for 425, 16 nodes over
+// fp8 713 for 620, but 4 rows of 8,000 39 for 42; twice as many: 747, 32 rows of 16 to 64 nodes over
+// 2k to 24k 551 for 535.
+int64_t line_groups(int32_t tile_rows, int64_t units, int32_t max_kv_len) {
+  const int keys = tile_rows <= 32 ? block_keys<32>() : block_keys<128>();
+  return std::min(units * ((max_kv_len + keys - 1) / keys), (int64_t)(tile_rows == 256 ? 256 : 512));
 }
+
+// The query rows of a call's tiles.
+int32_t tile_rows(int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256; }
 
 }  // namespace
 
@@ -1202,25 +1208,13 @@ constexpr int64_t kFewHeads = 4096;
 TreePlan tree_plan(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len, int32_t max_kv_len) {
   const int64_t rows = (int64_t)max_q_len * (hq / hkv);
   TreePlan p;
-  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 128 ? 128 : 256;
+  p.rows = tile_rows(rows);
   p.tiles = (rows + p.rows - 1) / p.rows;
   p.piece_rows = (int32_t)(rows < p.rows ? rows : p.rows);
   const int64_t units = (int64_t)B * hkv * p.tiles;
   p.direct = max_kv_len <= kDirectKeys ||
              (max_kv_len <= kDirectMost && max_kv_len <= units * kDirectUnitKeys);
-  // As many workgroups as are on the GPU together; half of them: 64 rows of 4k to 32k keys
-  // (4.6 GB), 8 nodes 732 us for 732, fp8 498 for 425, 16 nodes over fp8 713 for 620, but 4 rows
-  // of 8,000 39 for 42; twice as many: 747, 32 rows of 16 to 64 nodes over 2k to 24k 551 for 535.
-  if (p.direct)
-    p.groups = units;
-  else if (p.rows == 16)
-    plan_line<16>(p, units, max_kv_len, 512);
-  else if (p.rows == 32)
-    plan_line<32>(p, units, max_kv_len, 512);
-  else if (p.rows == 128)
-    plan_line<128>(p, units, max_kv_len, 512);
-  else
-    plan_line<256>(p, units, max_kv_len, 256);
+  p.groups = p.direct ? units : line_groups(p.rows, units, max_kv_len);
   return p;
 }
 
@@ -1242,6 +1236,26 @@ size_t tree_workspace_bytes(int32_t B, const TreePlan &p) {
   if (p.direct) return 0;
   return up256(((size_t)B + 1) * sizeof(int64_t)) +
          (size_t)2 * p.groups * p.piece_rows * (kHeadDim + 2) * sizeof(float);
+}
+
+// More keys are cut sooner and into no fewer pieces, so the most keys need most; of each size of
+// tile, the largest tree that has it, and as many tiles and KV heads as are still cut.
+size_t tree_most_workspace_bytes(int32_t B, int32_t hq, int32_t hkv, int32_t max_q_len,
+                                 int32_t max_kv_len) {
+  const int64_t cut = max_kv_len <= kDirectMost ? (max_kv_len - 1) / kDirectUnitKeys : INT64_MAX;
+  if (max_kv_len <= kDirectKeys || cut < hkv) return 0;
+  const int64_t group = hq / hkv;
+  size_t most = 0;
+  for (const int32_t rows : {16, 32, 128, 256}) {
+    const int64_t nodes = rows == 256 ? max_q_len : std::min<int64_t>(max_q_len, rows / group);
+    if (nodes == 0 || tile_rows(nodes * group) != rows) continue;
+    const int64_t tiles = (nodes * group + rows - 1) / rows;
+    const int64_t units = std::min((int64_t)B * hkv * tiles, cut / hkv * hkv);
+    const TreePlan p = {rows, (int32_t)std::min<int64_t>(nodes * group, rows), false, tiles,
+                        line_groups(rows, units, max_kv_len)};
+    most = std::max(most, tree_workspace_bytes(B, p));
+  }
+  return most;
 }
 
 hipError_t launch_tree(const uint16_t *q, const int32_t *cu_q, const int32_t *ctx_lens,

@@ -1,6 +1,8 @@
 """Refusals of the operators on drafted trees, logits and shared pages that need no GPU: through
 the C ABI with addresses that are never dereferenced, and through the binding."""
 import ctypes
+import math
+import random
 
 import pytest
 import torch
@@ -261,3 +263,32 @@ def test_launches_of_more_threads_than_a_grid_can_have_are_refused(lib):
         assert lib.rollout_attn_decode_tree(
             at(1), at(2), at(3), at(4), 3, ref(kv), 65535, heads, total, nodes, keys, 0.1, at(5), None,
             at(6), BIG, None) == UNSUPPORTED, heads
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(32, 8), (8, 1), (12, 4), (5, 5), (200, 1)])
+def test_one_workspace_holds_every_call_of_a_loop(Hq, Hkv):
+    """The size of a call can fall as rows, nodes or keys grow; the largest size is that of the
+    largest call that a loop can make, and not more than a call of it can need."""
+    rng = random.Random(Hq)
+    size, most = ra.decode_tree_workspace_size, ra.decode_tree_max_workspace_size
+    spread = lambda n: min(n, int(2 ** rng.uniform(0, math.log2(n + 1))))
+    falls = False
+    for _ in range(60):
+        B, T, L = spread(300), spread(1024), spread(40000)
+        bound, largest = most(B, Hq, Hkv, T, L), 0
+        # trees just within each size of tile, rows just within and past what is not cut
+        nodes = {t for r in (1, 16, 32, 128, 256, T * Hq) for t in (r * Hkv // Hq,) if 1 <= t <= T} | {1, T}
+        keys = {n for n in (512, 513, 4096, 4097, L, *(spread(L) for _ in range(20))) if n <= L}
+        for b in {1, B, *(spread(B) for _ in range(10))}:
+            for t in nodes | {spread(T) for _ in range(4)}:
+                for n in keys:
+                    need = size(b, Hq, Hkv, b * t, t, n)
+                    assert need <= bound, (B, T, L, b, t, n)
+                    largest = max(largest, need)
+        falls |= size(B, Hq, Hkv, B * T, T, L) < largest
+        if L > 4096:
+            assert bound <= largest + 8 * 300 + 256, (B, T, L, bound, largest)
+    assert falls
+    for zero in ((0, Hq, Hkv, 8, 5000), (4, Hq, Hkv, 0, 5000), (4, Hq, Hkv, 1025, 5000),
+                 (4, Hq, Hkv, 8, 0), (4, Hq, Hkv, 8, 512), (4, Hq + 1, Hkv + 1, 8, 512)):
+        assert most(*zero) == 0, zero

@@ -195,3 +195,23 @@ def test_exact_workspace_and_its_refusal(device):
     with pytest.raises(ra.RolloutAttnError) as e:
         run(cache, q, bits, ctx, T, workspace=ws[:need - 4])
     assert e.value.status == ra._lib.RA_ERR_WORKSPACE
+
+
+def test_one_workspace_for_a_batch_that_shrinks(device):
+    """Rows that end one after another: the calls that are left need more than the first does."""
+    Hq, Hkv, most, keys = 8, 2, 12, 1500
+    B = 60
+    ctx = [int(x) for x in np.random.default_rng(18).integers(0, keys - most, B)]
+    T = [most] * B
+    cache, q, masks, bits = inputs(18, Hq, Hkv, ctx, T, stride=-(-keys // 16))
+    sizes = [ra.decode_tree_workspace_size(b, Hq, Hkv, b * most, most, keys) for b in (60, 3)]
+    size = ra.decode_tree_max_workspace_size(B, Hq, Hkv, most, keys)
+    assert sizes[0] == 0 and 0 < sizes[1] <= size
+    ws = torch.full((size + 16,), 0xff, dtype=torch.uint8, device=DEV)
+    want, want_lse, tol, ltol = tree_reference(q, T, ctx, masks, cache)
+    for b in (60, 47, 46, 20, 3, 1):
+        n = b * most
+        out, lse = run(cache, q[:n], bits[:n], ctx[:b], T[:b], max_q=most, max_kv=keys, workspace=ws[:size])
+        assert bool((ws[size:] == 0xff).all())
+        assert_within(lse, want_lse[:n], ltol[:n], f"lse of {b} rows")
+        assert_within(out, want[:n], tol[:n], f"out of {b} rows")
