@@ -648,8 +648,9 @@ int draft_tree_accept(const int32_t *parents, const int32_t *draft_tokens, const
  *   out[t][h] = softmax_j(scale * <q[t][h], K_j>) . V_j,  lse likewise.
  * One node that sees itself is rollout_attn_decode with kv_lens = ctx_lens + 1; a chain is
  * rollout_attn_append, with decode's precision. A node that sees no key gives out = 0 and lse
- * = -inf. A masked key and value reach no result, infinite or NaN as they may be (a result that an
- * infinite value of a node reaches may hold NaN where the formula has an infinity).
+ * = -inf. A masked key and value reach no result, infinite or NaN as they may be. A result that an
+ * infinite value reaches, of the context or of a node, may hold NaN where the formula has an
+ * infinity: the second part of a weight (below) can be 0 or negative.
  *
  *   q           bf16 [total_q][Hq][128]
  *   cu_q        int32 [B+1];  ctx_lens  int32 [B]

@@ -9,7 +9,8 @@
 // Softmax is the online form in fp32, base 2. Weights meet the values in two bf16 parts, off by
 // 2^-16 of a weight: one part would be off by 2^-8. (Narrow tiles over bf16 pools take a third
 // part, which is free there. In wide tiles it costs what the matrix cores do not have: 32 rows
-// of 64 nodes over 2k to 24k keys 666 -> 813 us.)
+// of 64 nodes over 2k to 24k keys 666 -> 813 us.) The later parts of a weight can be 0 or negative, so
+// that an infinite value of the context gives NaN where the formula has an infinity.
 //
 // Read: every row's keys and values once a tile, 512 bytes a key and KV head in bf16. Computed:
 // 512 flops a key and query row, 768 with the weights' second part. Bound by HBM up to about 60

@@ -215,3 +215,49 @@ def test_one_workspace_for_a_batch_that_shrinks(device):
         assert bool((ws[size:] == 0xff).all())
         assert_within(lse, want_lse[:n], ltol[:n], f"lse of {b} rows")
         assert_within(out, want[:n], tol[:n], f"out of {b} rows")
+
+
+# (Hq, Hkv, nodes of the largest tree) of each size of tile: 16, 32, 128 and 256 query rows
+TILES = {16: (8, 2, 4), 32: (8, 2, 8), 128: (8, 2, 30), 256: (64, 2, 24)}
+
+
+def tiled(rows, cut, seed, fp8=False):
+    """Three rows of such trees; the longest row is cut, or none is."""
+    Hq, Hkv, most = TILES[rows]
+    ctx, T = [70, 5, 1030 if cut else 200], [most, most - 1, most // 2 + 1]
+    n = max(c + t for c, t in zip(ctx, T))
+    assert (ra.decode_tree_workspace_size(3, Hq, Hkv, sum(T), most, n) > 0) == cut
+    return (Hq // Hkv, ctx, T, *inputs(seed, Hq, Hkv, ctx, T, fp8))
+
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("rows", TILES)
+@pytest.mark.parametrize("fp8,bad", [(False, float("nan")), (False, float("inf")),
+                                     (False, float("-inf")), (True, 0x7f)])
+def test_infinite_and_nan_values_of_the_context(device, rows, cut, fp8, bad):
+    """They reach their dimension's result of every node of the row, as an infinity of their sign
+    or NaN, and nothing else; a key that is NaN reaches all that its KV head's queries read."""
+    G, ctx, T, cache, q, masks, bits = tiled(rows, cut, 19, fp8)
+    clean, clean_lse = check(cache, q, masks, bits, ctx, T)
+    first, last = slice(0, T[0]), slice(T[0] + T[1], sum(T))
+    for b, pos, d in ((0, 33, 9), (2, ctx[2] - 1, 77)):
+        page, slot = cache.place(b, pos)
+        cache.v[page, 1, d, slot] = bad
+    out, lse = run(cache, q, bits, ctx, T)
+    assert torch.equal(lse, clean_lse)
+    for nodes, d in ((first, 9), (last, 77)):
+        hit = out[nodes, G:, d]
+        assert not bool(torch.isfinite(hit).any())
+        if not fp8 and bad == bad:
+            assert bool((torch.isnan(hit) | (hit == bad)).all())
+        clean[nodes, G:, d] = hit
+    same = torch.equal(torch.nan_to_num(out, 1e30, 2e30, 3e30), torch.nan_to_num(clean, 1e30, 2e30, 3e30))
+    assert same
+    if fp8 or bad != bad:
+        page, slot = cache.place(1, 3)
+        cache.k[page, 0, slot, 5] = bad
+        second = slice(T[0], T[0] + T[1])
+        out, lse = run(cache, q, bits, ctx, T)
+        assert bool(torch.isnan(out[second, :G]).all()) and bool(torch.isnan(lse[second, :G]).all())
+        clean[second, :G] = float("nan")
+        assert torch.equal(torch.nan_to_num(out, 1e30, 2e30, 3e30), torch.nan_to_num(clean, 1e30, 2e30, 3e30))
