@@ -261,3 +261,43 @@ def test_infinite_and_nan_values_of_the_context(device, rows, cut, fp8, bad):
         assert bool(torch.isnan(out[second, :G]).all()) and bool(torch.isnan(lse[second, :G]).all())
         clean[second, :G] = float("nan")
         assert torch.equal(torch.nan_to_num(out, 1e30, 2e30, 3e30), torch.nan_to_num(clean, 1e30, 2e30, 3e30))
+
+
+@pytest.mark.parametrize("cut", [False, True])
+@pytest.mark.parametrize("rows", TILES)
+@pytest.mark.parametrize("fp8,bad", [(False, float("nan")), (False, float("inf")),
+                                     (False, float("-inf")), (True, 0x7f)])
+def test_infinite_and_nan_nodes_in_every_size_of_tile(device, rows, cut, fp8, bad):
+    G, ctx, T, cache, q, masks, bits = tiled(rows, cut, 20, fp8)
+    clean, clean_lse = check(cache, q, masks, bits, ctx, T)
+    met = []
+    for b, t in enumerate(T):
+        node = t // 2                                     # seen by itself, not by those before it
+        page, slot = cache.place(b, ctx[b] + node)
+        cache.v[page, 1, 9, slot] = bad
+        met.append(masks[b][:, node])
+    met = torch.as_tensor(np.concatenate(met), device=DEV)
+    out, lse = run(cache, q, bits, ctx, T)
+    assert torch.equal(lse, clean_lse)
+    assert torch.equal(out[~met], clean[~met])
+    assert not bool(torch.isfinite(out[met][:, G:, 9]).any())
+    clean[met, G:, 9] = out[met, G:, 9]
+    for x in (out, clean):
+        x[met, G:, 9] = torch.nan_to_num(x[met, G:, 9], 1e30, 2e30, 3e30)
+    assert torch.equal(out, clean)
+    for b, t in enumerate(T):                             # the keys too
+        page, slot = cache.place(b, ctx[b] + t // 2)
+        cache.k[page, 0, slot, 5] = bad
+    out, lse = run(cache, q, bits, ctx, T)
+    assert torch.equal(out[~met], clean[~met]) and torch.equal(lse[~met], clean_lse[~met])
+    if fp8 or bad != bad:
+        assert bool(torch.isnan(out[met][:, :G]).all())
+
+
+@pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
+@pytest.mark.parametrize("rows", TILES)
+@pytest.mark.parametrize("fp8", [False, True])
+def test_scales_in_every_size_of_tile(device, rows, fp8, scale):
+    for cut in (False, True):
+        _, ctx, T, cache, q, masks, bits = tiled(rows, cut, 21, fp8)
+        check(cache, q, masks, bits, ctx, T, scale=scale)
