@@ -707,7 +707,9 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
  *
  *   logits        fp32 or bf16 (logits_dtype) [N] rows of V, row_stride elements apart (any
  *                 alignment of an element); out likewise, out_stride apart; out = logits with
- *                 the same stride works in place (and reads and writes only what changes)
+ *                 the same stride works in place (and reads and writes only what changes).
+ *                 Rows of trees share the counting of their history where rows are a multiple
+ *                 of 16 bytes apart; otherwise each row's is counted by itself (slower)
  * ra_logits_adjust (all arrays may be NULL where not said otherwise):
  *   history       int32 [B] rows of history_width, history_stride apart, of which history_lens[b]
  *                 (int32 [B], needed with history; more than history_width count as that many)

@@ -6,7 +6,9 @@
 // the answer; whole numbers, so the order of the atomics does not matter), and the place of
 // each token's last bias, then passes over the chunk once, 16 bytes a thread and load. The rows
 // of one tree share the history's counts: the tokens of each node's path are added, and taken
-// off with the next node's. All that a row needs is loaded while the row before is worked on.
+// off with the next node's. (Where rows are not a multiple of 16 bytes apart, the logits' places in
+// LDS shift from row to row and the history is counted anew for each.) All that a row needs is
+// loaded while the row before is worked on.
 //
 // Logit z of a token that the history names, n times in the answer: z / rep where z > 0 and
 // z rep elsewhere, then z - n freq - pres if n > 0, then z + bias; -inf where the mask forbids it.

@@ -270,3 +270,55 @@ def test_masks_of_few_rows_and_ids_outside(device):
     assert bool((out[0] == float("-inf")).all()) and torch.equal(out[1:], z[1:])
     out = ra.token_logits_adjust(z, allowed=one, allowed_rows=i32([-1, 1, 0]))
     assert torch.equal(out[:2], z[:2]) and bool((out[2] == float("-inf")).all())
+
+
+# Calls whose workgroups take several rows and count a tree's history once: rows of logits a
+# multiple of 16 bytes apart, and N rows in ceil(V / 8184) chunks over 512 workgroups.
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,pad,nodes,lens", [
+    (16384, 0, [200, 1, 0, 333, 64], [10, 120, 5, 90, 0]),      # 4 rows a workgroup
+    (16384, 16, [7] * 90, list(range(90))),                     # 4, of several trees
+    (12000, 8, [3, 1000, 0, 70], [40, 60, 9, 0]),               # 5; paths through nodes past 512
+    (1200, 0, [1024, 1024], [30, 0]),                           # 4
+])
+def test_rows_that_share_a_history(device, V, pad, nodes, lens, dtype):
+    for use in (ALL, "history frequency"):
+        z, kw, host = case(7, len(nodes), V, lens, use, dtype, nodes=nodes, pad=pad, odd=True)
+        want, plain = reference(z.double().cpu().numpy(), **host)
+        out = ra.token_logits_adjust(z, **kw)
+        check(out, z, want, plain)
+        ra.token_logits_adjust(z, **kw, out=z)
+        assert torch.equal(z.contiguous(), out)
+
+
+def test_rows_that_share_a_history_take_off_each_others_paths(device):
+    """Leaves of one root in falling and rising order of their tokens: a path that stayed would be
+    counted in the rows behind it."""
+    V, T = 8192, 1024
+    N = 2 * T
+    sees = np.eye(T, dtype=bool)
+    sees[:, 0] = True
+    draft = np.concatenate([np.arange(T), np.arange(T)[::-1]]) * 8 % V
+    z = torch.zeros((N, V), device=DEV)
+    out = ra.token_logits_adjust(
+        z, history=i32([[5, 13], [8000, 5]]), history_lens=i32([2, 2]), frequency=f32([1.0, 1.0]),
+        cu_rows=i32([0, T, N]), draft_tokens=i32(draft),
+        tree_mask=torch.as_tensor(pack([sees, sees], T // 64), device=DEV))
+    want = torch.zeros((N, V), device=DEV)
+    for b, seen in enumerate(([5, 13], [8000, 5])):
+        rows = slice(b * T, (b + 1) * T)
+        for v in seen:
+            want[rows, v] -= 1
+        want[rows, int(draft[b * T])] -= 1                # the root
+        at = torch.arange(b * T + 1, (b + 1) * T, device=DEV)
+        want[at, torch.as_tensor(draft[b * T + 1:(b + 1) * T], device=DEV)] -= 1
+    assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("use", USES)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_one_logit_in_place(device, use, dtype):
+    z, kw, _ = case(8, 5, 1, [0, 1, 700, 33, 64], use, dtype, odd=True)
+    out = ra.token_logits_adjust(z, **kw)
+    assert ra.token_logits_adjust(z, **kw, out=z) is z
+    assert torch.equal(z, out)
