@@ -725,7 +725,9 @@ int rollout_attn_decode_tree(const void *q, const int32_t *cu_q, const int32_t *
  *                 logits (rows behind cu_rows[B] are not touched); NULL: B = N, a row each
  *   draft_tokens  int32 [N], tree_mask uint64 [N][mask_words] (both or neither, with cu_rows):
  *                 the rows are nodes of drafted trees; the drafted tokens of the nodes in row
- *                 n's mask are in its history, behind the prompt
+ *                 n's mask are in its history, behind the prompt. The root's is among them, so
+ *                 history ends before the root (history_lens = the step's ctx_lens): a token
+ *                 in both counts twice
  * What is written must not share memory with another array (but in place as above).
  * Errors: RA_ERR_NULL; RA_ERR_SHAPE (N < 0, B < 0, V <= 0, a stride < V with N > 1,
  *         history_width < 0, history_stride < history_width with B > 1, num_bias < 0,

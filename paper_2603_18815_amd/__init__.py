@@ -1053,7 +1053,8 @@ def token_logits_adjust(logits: torch.Tensor, history: Optional[torch.Tensor] = 
     row's mask (outside [0, M): none; None: mask n): tokens whose bit is clear become -inf.
     Row n of the logits has history row n, or with cu_rows int32 [B+1] the b with cu_rows[b] <=
     n < cu_rows[b+1]; draft_tokens int32 [N] and tree_mask int64 [N][words] then add the drafted
-    tokens of the nodes in row n's mask to its history.
+    tokens of the nodes in row n's mask to its history. The root's token is one of them: history
+    ends before it (history_lens = the step's ctx_lens), or it counts twice.
     """
     lib = _lib.load()
     dev = logits.device

@@ -322,3 +322,30 @@ def test_one_logit_in_place(device, use, dtype):
     out = ra.token_logits_adjust(z, **kw)
     assert ra.token_logits_adjust(z, **kw, out=z) is z
     assert torch.equal(z, out)
+
+
+def test_a_nodes_history_is_the_rows_then_its_path_with_the_root(device):
+    """The history ends before the root, whose token is the first of every path: a row of a tree is
+    the row whose history goes on with the path's tokens. A history that holds the root already
+    counts it twice."""
+    V, nodes, lens = 600, [9, 0, 4], [40, 3, 0]
+    z, kw, host = case(9, 3, V, lens, ALL, nodes=nodes)
+    out = ra.token_logits_adjust(z, **kw)
+    longest = max(lens) + max(nodes) + 1
+    for root_twice in (False, True):
+        if root_twice:                                    # as if the root had been appended
+            wide = torch.zeros((3, longest), dtype=torch.int32, device=DEV)
+            wide[:, :kw["history"].shape[1]] = kw["history"]
+            for b, n in enumerate(nodes):
+                if n:
+                    wide[b, lens[b]] = kw["draft_tokens"][cu(nodes)[b]]
+            out = ra.token_logits_adjust(z, **{**kw, "history": wide, "history_lens": i32(np.add(lens, 1))})
+        for n, b in enumerate(host["rows"]):
+            path = host["paths"][n]
+            tokens = [int(t) for t in host["hist"][b][:lens[b]]] + path[:1] * root_twice + path
+            one = dict(history=i32([tokens]), history_lens=i32([len(tokens)]),
+                       prompt_lens=i32([min(int(host["prompt"][b]), lens[b] + root_twice)]),
+                       bias_tokens=kw["bias_tokens"], bias_values=kw["bias_values"],
+                       cu_bias=kw["cu_bias"][b:b + 2].contiguous(), allowed=kw["allowed"],
+                       allowed_rows=kw["allowed_rows"][n:n + 1], **{k: kw[k][b:b + 1] for k in PARAMS})
+            assert torch.equal(ra.token_logits_adjust(z[n:n + 1], **one), out[n:n + 1]), (n, root_twice)
