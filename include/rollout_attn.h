@@ -597,10 +597,13 @@ int kv_block_table_release(const int32_t *lens, const int32_t *keep_lens,
  * its completions one after the other). A row's tree has T nodes, packed at cu_q[b] ..
  * cu_q[b+1]-1; node 0, the root, is the token that is known (the last one drawn), and every
  * other node is a guess that follows its parent, a node before it. A step is
- *   kv_block_table_extend, draft_tree_mask, kv_page_write (node i at position ctx + i, its key
- *   and query rotated at positions[i]), rollout_attn_decode_tree in each layer, the LM head,
+ *   kv_block_table_extend, draft_tree_mask, kv_page_write (node i at position ctx + i),
+ *   rollout_attn_decode_tree in each layer, the LM head,
  *   token_logits_adjust, token_sample (one token a node: chosen), draft_tree_accept,
  *   kv_page_compact in each layer, kv_block_table_release (keep_lens = the new kv_lens).
+ * In a model with rotary embedding a node's key and query are rotated at positions[i], by the
+ * caller and before these calls: kv_page_write_rope and rollout_attn_append_write_rope rotate at
+ * ctx + i, the node's place in the pages, which is not its position where it has siblings.
  * The tokens it emits are those that were drawn, node after node, so their distribution is
  * that of steps of one token whatever the guesses are.
  *

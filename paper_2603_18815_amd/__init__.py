@@ -903,8 +903,9 @@ def draft_tree_mask(parents: torch.Tensor, cu_q: torch.Tensor,
     """Masks and positions of drafted trees (row b's nodes packed at cu_q[b] .. cu_q[b+1]-1):
     parents int32 [total] (a node's parent in its row, before it; -1: none) -> tree_mask int64
     [total][words], bit j of word j / 64 for the node itself and its ancestors, and positions
-    int32 [total], ctx_lens[b] + the node's depth. words: those of the tree_mask given, or as
-    many as max_q_len nodes need."""
+    int32 [total], ctx_lens[b] + the node's depth (where the caller rotates its key and query, in a
+    model that does; kv_page_write's cos_sin= rotates at the place in the pages). words: those of
+    the tree_mask given, or as many as max_q_len nodes need."""
     lib = _lib.load()
     dev, B, total = _draft_inputs(cu_q, ctx_lens, ((parents, "parents"),))
     max_q_len = _nodes(cu_q, max_q_len)

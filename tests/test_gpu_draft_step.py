@@ -264,3 +264,66 @@ def test_two_calls_at_once(device):
     torch.cuda.synchronize()
     for pair in got:
         assert all(torch.equal(a, b) for a, b in zip(pair, want))
+
+
+def rotated(x, table, positions):
+    """Rotary embedding at any positions, in the steps and roundings of the writes that rotate."""
+    x, row = x.float(), table[positions.long()][:, None]
+    a, b, c, s = x[..., :64], x[..., 64:], row[..., :64], row[..., 64:]
+    return torch.cat([a * c - b * s, b * c + a * s], -1).bfloat16()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_trees_of_rotated_queries_and_keys(device, fp8):
+    """Keys and queries rotated at the nodes' positions before the write and the attention: every
+    node is the last token of its path written and rotated one behind the other, and the path
+    that is kept has the same bits in its pages. (The writes that rotate do so at ctx + i, which is
+    a node's place and not its position.)"""
+    parents, ctx, nodes, hq, hkv, stride = PARENTS[0] + PARENTS[2], [21, 40], [9, 6], 8, 2, 8
+    total, at, N = sum(nodes), cu(nodes), sum(nodes)
+    g = torch.Generator(device=DEV).manual_seed(11)
+    rnd = lambda *s: torch.randn(s, generator=g, device=DEV).bfloat16()
+    q, k, v = rnd(total, hq, 128), rnd(total, hkv, 128), rnd(total, hkv, 128)
+    old_k, old_v = rnd(sum(ctx), hkv, 128), rnd(sum(ctx), hkv, 128)
+    angle = torch.arange(128, device=DEV)[:, None] / 1e4 ** (torch.arange(64, device=DEV) / 64)
+    table = torch.cat([torch.cos(angle), torch.sin(angle)], 1).float().contiguous()
+
+    def pools(rows):
+        z = lambda *s: torch.zeros(s, dtype=torch.uint8 if fp8 else torch.bfloat16, device=DEV)
+        return ra.PagedKV(z(rows * stride, hkv, 16, 128), z(rows * stride, hkv, 128, 16),
+                          torch.randperm(rows * stride, generator=g, device=DEV).to(torch.int32).view(rows, stride),
+                          *((0.05, 0.05) if fp8 else ()))
+    kv = pools(2)
+    ra.kv_page_write(old_k, old_v, i32(cu(ctx)), i32([0, 0]), kv, cos_sin=table)
+    mask, pos = ra.draft_tree_mask(i32(parents), i32(at), i32(ctx), max_q_len=9)
+    q = rotated(q, table, pos)
+    ra.kv_page_write(rotated(k, table, pos), v, i32(at), i32(ctx), kv)
+    out, _ = ra.decode_tree(q, i32(at), i32(ctx), mask, kv)
+
+    sees = [ancestors(PARENTS[0]), ancestors(PARENTS[2])]
+    paths = [[int(j) for j in np.flatnonzero(sees[b][i])] for b in range(2) for i in range(nodes[b])]
+    row = [b for b in range(2) for _ in range(nodes[b])]
+    lens = [ctx[row[n]] + len(paths[n]) for n in range(N)]
+    assert pos.tolist() == [n - 1 for n in lens]
+    chain = lambda old, new: torch.cat([torch.cat([old[cu(ctx)[row[n]]:cu(ctx)[row[n] + 1]],
+                                                   new[at[row[n]] + np.array(paths[n])]]) for n in range(N)])
+    each = pools(N)
+    ra.kv_page_write(chain(old_k, k), chain(old_v, v), i32(cu(lens)), i32([0] * N), each, cos_sin=table)
+    want, _ = ra.decode(q, each, i32(lens))
+    # each side: a score off by 132 half steps of at most scale |q| |k|, weights by 2^-16, sums over
+    # fewer than 64 keys by 64 half steps, of values of at most the largest (codes: theirs)
+    norm = lambda x: float(x.double().norm(dim=-1).max()) * (1 + 2.0**-4 * fp8)
+    score = 2.0**-24 * 132 * norm(q) * max(norm(k), norm(old_k)) / math.sqrt(128)
+    most = max(float(v.abs().max()), float(old_v.abs().max())) * (1 + 2.0**-4 * fp8)
+    assert float((out - want).abs().max()) <= 2 * (2.0**-16 + 2 * score + 2.0**-17) * most
+
+    leaf = [6, 5]                                     # the last nodes of two long paths
+    kept = [paths[at[b] + leaf[b]] for b in range(2)]
+    path = i32(sum((p + [-1] * (t - len(p)) for p, t in zip(kept, nodes)), []))
+    ra.kv_page_compact(kv, i32(ctx), i32(at), path, i32([len(p) for p in kept]))
+    got = ra.kv_page_gather(kv, i32([c + len(p) for c, p in zip(ctx, kept)]),
+                            i32(cu([c + len(p) for c, p in zip(ctx, kept)])))
+    all_k, all_v = ra.kv_page_gather(each, i32(lens), i32(cu(lens)))
+    for x, y in zip(got, (all_k, all_v)):
+        y = torch.cat([y[cu(lens)[at[b] + leaf[b]]:cu(lens)[at[b] + leaf[b] + 1]] for b in range(2)])
+        assert torch.equal(x, y)
