@@ -9,8 +9,10 @@
 // one chosen at cur. A wave a row looks at 64 nodes at a time.
 //
 // Bound by latency: some 30 bytes a node, a few dependent steps each. 8 rows of up to 16 nodes:
-// mask 2.8 us, walk 3.4; 512 rows of 48 to 64 nodes: 5.0 and 4.6. A workgroup a row and all of
-// its parents in LDS, so that a step of either walk is an LDS read: nothing is gained by more.
+// mask 2.8 us, walk 3.2; 512 rows of 48 to 64 nodes: 4.9 and 5.2; of chains of 64 that are accepted
+// as a whole 6.4 and 25.7; 8 chains of 1,024: 255 and 361. A workgroup a row and all of its parents in
+// LDS: a step of the walk up is an LDS read, one of the walk down a load of the token chosen there
+// and then LDS reads, 0.35 us.
 #include "ra_device.h"
 #include "ra_internal.h"
 

@@ -119,8 +119,8 @@ struct SharedRelease {
 __device__ __forceinline__ int64_t pages_of(int64_t tokens) { return (tokens + kPage - 1) / kPage; }
 
 // The release of a large table, each step a launch because atomics of all rows have to be there
-// before the next. Of 512 rows and 168,000 entries: 9.7 + 4.2 + 3.4 + 8.5 us, bound by the atomics
-// on shared counts and by round trips.
+// before the next. Of 448 rows' 147,000 entries, in a table of 512: 9.3 + 4.0 + 3.3 + 8.9 us, bound by
+// the atomics on shared counts and by round trips.
 //
 // Takes an owner off every entry that is given up.
 __global__ __launch_bounds__(kRowThreads) void shared_sub_kernel(SharedRelease r) {
@@ -314,7 +314,8 @@ __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r
 
 // ---- pages' contents ----
 // One page of one KV head a workgroup, 16 bytes a thread and pool. Bound by HBM: 434 pages of 8 KV
-// heads in bf16 (57 MB read and written, the sources of eight copies the same) 7.5 us.
+// heads in bf16 (57 MB read and written, the sources of eight copies the same) 7.5 us, in codes, with which half of
+// the threads have nothing to do, 5.4.
 template <bool kFp8>
 __global__ __launch_bounds__(kPageThreads) void page_copy_kernel(uint8_t *k_pool, uint8_t *v_pool,
                                                                  const int32_t *src,
@@ -343,7 +344,7 @@ constexpr int kMoveTokens = 32;            // moved together
 // table and the pages, one behind the other) and, in large calls, by HBM's sectors: of a value
 // row a token has two bytes of a 32-byte sector, so that 58 MB of keys and values are 137 MB
 // in whole sectors. 4 rows of up to 8 tokens 4.1 us; 512 rows, some 16 tokens each, 8 KV heads 32 us
-// (4.3 TB/s of sectors), with single values stored one by one 40.
+// (4.3 TB/s of sectors), with single values stored one by one 40; in codes 18.
 template <typename E>
 __global__ __launch_bounds__(kPageThreads) void page_compact_kernel(
     E *k_pool, E *v_pool, const int32_t *block_table, int32_t bt_stride, int32_t num_pages,

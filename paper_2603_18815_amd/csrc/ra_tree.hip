@@ -578,7 +578,9 @@ __global__ __launch_bounds__(kSplitWaves * kWave, 2) void tree_narrow_kernel(Tre
 // are at most 2^8 then.
 // kW is 4 for trees of up to 128 query rows, two workgroups a compute unit, each of which works
 // while the other waits, and 8 (a ring of four, three blocks ahead) for larger ones. (64 rows
-// of 16 nodes, 64 query rows: 915-930 us, with kW 8 948; over fp8 pools 643-680 and 791.) With
+// of 16 nodes, 64 query rows: 915-930 us, with kW 8 948; over fp8 pools 643-680 and 791. 32 rows of
+// 16 to 64 nodes over 2k to 24k keys in codes 493-512, of 32 nodes 386-397. Codes fill half of a
+// ring's slots, whose size is that of bf16 pages.) With
 // few query rows bound by the loads: those of 64 rows of 16 nodes alone take 912 of 956 us
 // (5.6 TB/s); with many by the products and the softmax beside them, which a wave issues in
 // turn: 32 rows of 64 nodes 751 us with a pair of keys a wave at a time, 683 with a block's two
