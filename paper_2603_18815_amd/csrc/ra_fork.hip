@@ -314,8 +314,8 @@ __global__ __launch_bounds__(kOneThreads) void shared_one_kernel(SharedRelease r
 
 // ---- pages' contents ----
 // One page of one KV head a workgroup, 16 bytes a thread and pool. Bound by HBM: 434 pages of 8 KV
-// heads in bf16 (57 MB read and written, the sources of eight copies the same) 7.5 us, in codes, with which half of
-// the threads have nothing to do, 5.4.
+// heads in bf16 (57 MB read and written, the sources of eight copies the same) 7.5 us; in codes, of
+// which half of the threads have none, 5.4.
 template <bool kFp8>
 __global__ __launch_bounds__(kPageThreads) void page_copy_kernel(uint8_t *k_pool, uint8_t *v_pool,
                                                                  const int32_t *src,
