@@ -349,3 +349,19 @@ def test_a_nodes_history_is_the_rows_then_its_path_with_the_root(device):
                        cu_bias=kw["cu_bias"][b:b + 2].contiguous(), allowed=kw["allowed"],
                        allowed_rows=kw["allowed_rows"][n:n + 1], **{k: kw[k][b:b + 1] for k in PARAMS})
             assert torch.equal(ra.token_logits_adjust(z[n:n + 1], **one), out[n:n + 1]), (n, root_twice)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_one_history_and_trees_without_one(device, dtype):
+    """cu_rows alone: several rows of logits for a history, no path; and paths alone."""
+    V, nodes, lens = 16384, [250, 0, 90, 260], [80, 4, 0, 31]        # 4 rows a workgroup
+    z, kw, host = case(10, 4, V, lens, ALL, dtype, nodes=nodes)
+    rows = {k: v for k, v in kw.items() if k not in ("draft_tokens", "tree_mask")}
+    paths = {k: v for k, v in kw.items() if k not in ("history", "history_lens", "prompt_lens")}
+    for args, view in ((rows, dict(host, paths=[[] for _ in host["paths"]])),
+                       (paths, dict(host, hist=None, prompt=None))):
+        want, plain = reference(z.double().cpu().numpy(), **view)
+        out = ra.token_logits_adjust(z, **args)
+        check(out, z, want, plain)
+        again = z.clone()
+        assert torch.equal(ra.token_logits_adjust(again, **args, out=again), out)
